@@ -220,12 +220,10 @@ def _run_own(state):
             state["outs"] = b.route_outputs(state["logits"], state["k"])
         return b.prsgd_route(state["logits"], state["k"], state["coef"], normalize=state["normalize"], live=state["live"],
                              out=state["outs"], workspace=state["work"])
-    if "work" not in state:
-        state["work"] = b.route_workspace(state["logits"])
+    if "out" not in state:
         state["out"] = torch.empty_like(state["logits"])
     return b.prsgd_route_grad(state["logits"], state["experts"], state["counts"], state["coef"], normalize=state["normalize"],
-                              live=state["live"], dweights=state["dweights"], dloss=state["dloss"], out=state["out"],
-                              workspace=state["work"])
+                              live=state["live"], dweights=state["dweights"], dloss=state["dloss"], out=state["out"])
 
 
 # ---- what a pass cannot do without --------------------------------------------------------------------------
