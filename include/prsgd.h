@@ -472,6 +472,83 @@ int prsgd_average_rows(float* d_P, int64_t N, int64_t m, int64_t row_stride, voi
 int prsgd_mean_rows_noalloc(const float* d_P, int64_t N, int64_t m, int64_t row_stride,
                             float* dst, int dst_on_device, void* cuda_stream);
 
+/* ---- Stand-alone training operators -----------------------------------------------------------------------------
+ * Operators on the caller's own device arrays, like prsgd_average_rows: no context, everything enqueued on cuda_stream
+ * (asynchronous, capturable), nothing allocated.  The device that owns the arrays must be current.  Arguments are
+ * checked on the host before anything is enqueued.  Scratch comes from the caller: d_work of at least the size the
+ * *_workspace_bytes function returns, 256-byte aligned, no particular contents; it holds nothing between calls, so one
+ * workspace serves any number of calls on one stream, and calls that may run at the same time (other streams, two
+ * graphs replayed side by side) need one each.  Array elements are one of the types below; matrices are row-major with
+ * a row stride (elements, >= cols) and a stride between the matrices of a batch.  Inputs may be broadcast over the batch
+ * (batch stride 0); outputs may not overlap.  A batch, side, group or token count of 0 is a call that does nothing
+ * (the router then still writes zero counts and loss). */
+#define PRSGD_TYPE_FP32 0
+#define PRSGD_TYPE_BF16 1
+#define PRSGD_TYPE_FP16 2
+
+/* Newton-Schulz orthogonalisation of each matrix of a batch (the Muon optimiser's use of it):
+ *   X_0 = G / (||G||_F + eps);  steps times:  A = X X^T,  X <- a X + (b A + c A^2) X;  out = scale * X.
+ * With the default coefficients (h_coefs = NULL: 3.4445, -4.7750, 2.0315; HOST array of 3 otherwise, each at most 16 in
+ * magnitude, and such that no singular value grows beyond a few units) five steps bring the singular values of G near
+ * 1 and keep its singular vectors.  Tall matrices are iterated from their short side, the result is the same.
+ * precision: PRSGD_PRECISION_FP32 computes to about fp32 accuracy (products of fp16 pairs, three per product),
+ * PRSGD_PRECISION_BF16 to about 1e-3 of the result's norm (single fp16 operands); both sum in fp32, and the norm in
+ * 64 bits.  A zero matrix gives zeros (eps > 0); one that holds a NaN or an infinity gives NaN and leaves the others
+ * alone.  out may be G itself (same type and strides).  G and out: aligned to their element type; multiples of
+ * 16 bytes in address and strides are fastest. */
+#define PRSGD_ORTHO_MAX_SIDE 65536
+#define PRSGD_ORTHO_MAX_STEPS 16
+int prsgd_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, int32_t precision, size_t* bytes);
+int prsgd_orthogonalize(const void* d_G, int32_t g_type, int64_t g_row_stride, int64_t g_batch_stride,
+                        void* d_out, int32_t out_type, int64_t out_row_stride, int64_t out_batch_stride,
+                        int32_t batch, int32_t rows, int32_t cols, int32_t steps, const float* h_coefs, float scale,
+                        float eps, int32_t precision, void* d_work, size_t work_bytes, void* cuda_stream);
+
+/* Muon step of a batch of weight matrices, in place:
+ *   V <- mu V + G;  U = V, or G + mu V when nesterov is set;
+ *   W <- (1 - lr weight_decay) W - lr scale NS(U),  NS as in prsgd_orthogonalize (same workspace size).
+ * V is fp32; W and G are of any element type.  sqrt(max(1, rows / cols)) and 0.2 sqrt(max(rows, cols)) are the usual
+ * choices of scale. */
+int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_batch_stride,
+                    float* d_V, int64_t v_row_stride, int64_t v_batch_stride,
+                    const void* d_G, int32_t g_type, int64_t g_row_stride, int64_t g_batch_stride,
+                    int32_t batch, int32_t rows, int32_t cols, float lr, float mu, int32_t nesterov, float weight_decay,
+                    int32_t steps, const float* h_coefs, float scale, float eps, int32_t precision,
+                    void* d_work, size_t work_bytes, void* cuda_stream);
+
+/* Device errors of the last call that used this workspace (a bounded wait that expired): PRSGD_OK or
+ * PRSGD_ERR_DEVICE_TIMEOUT, after which that call's outputs are not to be used.  Synchronises the stream. */
+int prsgd_work_status(const void* d_work, void* cuda_stream);
+
+/* Top-k router of an expert layer with its balance loss, per group (worker) g, over the group's live tokens t:
+ *   p_te = softmax_e(logits);  a token's experts: its top_k largest logits, ties to the lowest index, in that order;
+ *   weight = p of the expert, or (normalize) that divided by their sum over the token's experts;
+ *   counts_e = how often e was chosen;  mean_e = (1 / T) sum_t p_te with T = live tokens;
+ *   loss = coef * E * sum_e (counts_e / (top_k T)) mean_e.
+ * logits: [groups][tokens][experts] with row_stride (>= experts) and group_stride, in elements.  d_live: [groups][tokens]
+ * bytes, 0 = padding, or NULL.  Outputs, dense: d_experts, d_weights [groups][tokens][top_k]; d_counts, d_mean
+ * [groups][experts]; d_loss [groups].  A padding token, and one whose every logit is -inf, gets experts -1 and weights
+ * 0 and counts nowhere, whatever its logits hold; a group without live tokens has counts, mean and loss 0.  A NaN in a
+ * live token ranks above every number and makes mean and loss of its group NaN. */
+#define PRSGD_ROUTE_MAX_EXPERTS 1024
+#define PRSGD_ROUTE_MAX_K 32
+int prsgd_route_workspace_bytes(int64_t groups, int64_t tokens, int32_t experts, size_t* bytes);
+int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t group_stride, const uint8_t* d_live,
+                int64_t groups, int64_t tokens, int32_t experts, int32_t top_k, int32_t normalize, float coef,
+                int32_t* d_experts, float* d_weights, int32_t* d_counts, float* d_mean, float* d_loss,
+                void* d_work, size_t work_bytes, void* cuda_stream);
+
+/* Gradient of sum_g dloss_g loss_g + sum dweights * weights with respect to the logits, the choice of experts and the
+ * counts held fixed: with h_te = dloss coef E counts_e / (top_k T) / T + [e chosen by t] d/dp of the weights' part,
+ *   dlogit_te = p_te (h_te - sum_j p_tj h_tj).
+ * d_experts, d_counts: as prsgd_route wrote them (T is taken from the counts).  d_dweights [groups][tokens][top_k] or
+ * NULL, d_dloss [groups] or NULL (zero).  dlogits has the logits' type and may be the logits themselves (same strides);
+ * rows of padding tokens are written as zeros. */
+int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int64_t group_stride, const uint8_t* d_live,
+                     int64_t groups, int64_t tokens, int32_t experts, int32_t top_k, int32_t normalize, float coef,
+                     const int32_t* d_experts, const int32_t* d_counts, const float* d_dweights, const float* d_dloss,
+                     void* d_dlogits, int64_t d_row_stride, int64_t d_group_stride, void* cuda_stream);
+
 /* The minibatch draw zeta_i^t as an integer: the (i+1)-th output of a
  * SplitMix64 stream keyed by the t-th output of the SplitMix64 stream seeded
  * with `seed`, modulo n_blocks.  Pure host function; the device code evaluates

@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -12,7 +14,7 @@ LIB_PATH = os.path.join(HERE, "libprsgd.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-I" + INCLUDE, "-I" + CSRC,
+    "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC,
 ]
 
 
@@ -32,18 +34,28 @@ def is_stale() -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile csrc/prsgd_api.cu (which includes every kernel header) into libprsgd.so."""
+    """Compile every csrc/*.cu (prsgd_api.cu includes the kernel headers of the training step, the others hold the
+    stand-alone operators), one nvcc each side by side, and link them into libprsgd.so."""
     if not force and not is_stale():
         return LIB_PATH
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + [
-        os.path.join(CSRC, "prsgd_api.cu"), "-o", LIB_PATH + ".tmp"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+    units = [f for f in _sources() if f.endswith(".cu")]
+    flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else [])
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, os.path.basename(u) + ".o") for u in units]
+        with ThreadPoolExecutor(len(units)) as pool:
+            runs = list(pool.map(lambda uo: subprocess.run([nvcc] + flags + ["-c", uo[0], "-o", uo[1]], capture_output=True, text=True),
+                                 zip(units, objs)))
+        for res in runs:
+            if res.returncode != 0:
+                raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        link = subprocess.run([nvcc] + NVCC_FLAGS + ["-shared"] + objs + ["-o", LIB_PATH + ".tmp"], capture_output=True, text=True)
+    if link.returncode != 0:
+        raise RuntimeError("linking libprsgd.so failed:\n" + link.stdout + link.stderr)
     os.replace(LIB_PATH + ".tmp", LIB_PATH)
     if verbose:
-        print(res.stderr)
+        for res in runs:
+            print(res.stderr)
     return LIB_PATH
 
 

@@ -55,6 +55,8 @@ EXPORTS = [
     "prsgd_set_worker_offset", "prsgd_partial_sum", "prsgd_assign_rows", "prsgd_stage_data", "prsgd_swap_data",
     "prsgd_alg2_schedule", "prsgd_run_time_varying", "prsgd_run_heterogeneous_epoch",
     "prsgd_set_global_workers", "prsgd_check_finite", "prsgd_local_steps_sum",
+    "prsgd_orthogonalize_workspace_bytes", "prsgd_orthogonalize", "prsgd_muon_step", "prsgd_work_status",
+    "prsgd_route_workspace_bytes", "prsgd_route", "prsgd_route_grad",
 ]
 NOALLOC_MAX_M = 1 << 20
 
@@ -76,6 +78,7 @@ def _load() -> C.CDLL:
             "There is no fallback path.")
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, u64 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64
+    f32, szt = C.c_float, C.c_size_t
     spec_p, szp = C.POINTER(ModelSpec), C.POINTER(C.c_size_t)
     sig = {
         "prsgd_layout": (C.c_int, [spec_p, C.POINTER(Layout)]),
@@ -118,6 +121,14 @@ def _load() -> C.CDLL:
         "prsgd_check_finite": (C.c_int, [vp, C.POINTER(i64), C.POINTER(i32)]),
         "prsgd_partial_sum": (C.c_int, [vp, vp, i64, i64]),
         "prsgd_assign_rows": (C.c_int, [vp, vp, C.c_float, i64, i64]),
+        "prsgd_orthogonalize_workspace_bytes": (C.c_int, [i32, i32, i32, i32, szp]),
+        "prsgd_orthogonalize": (C.c_int, [vp, i32, i64, i64, vp, i32, i64, i64, i32, i32, i32, i32, vp, f32, f32, i32, vp, szt, vp]),
+        "prsgd_muon_step": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, vp, i32, i64, i64, i32, i32, i32, f32, f32, i32, f32,
+                                      i32, vp, f32, f32, i32, vp, szt, vp]),
+        "prsgd_work_status": (C.c_int, [vp, vp]),
+        "prsgd_route_workspace_bytes": (C.c_int, [i64, i64, i32, szp]),
+        "prsgd_route": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, szt, vp]),
+        "prsgd_route_grad": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, i64, i64, vp]),
         "prsgd_last_error": (C.c_char_p, [vp]),
         "prsgd_average_rows": (C.c_int, [vp, i64, i64, i64, vp]),
         "prsgd_draw_block": (u64, [u64, i32, i64, u64]),
@@ -195,6 +206,190 @@ def prsgd_mean_rows_noalloc(P: torch.Tensor, N: int, m: int, row_stride: int, ou
         ptr, on_dev = out.data_ptr(), 1 if out.is_cuda else 0
     with torch.cuda.device(P.device):
         _check(lib.prsgd_mean_rows_noalloc(P.data_ptr(), N, m, row_stride, ptr, on_dev, s.cuda_stream))
+    return out
+
+
+# ---- stand-alone training operators -------------------------------------------------------------------------
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MUON_COEFS = (3.4445, -4.7750, 2.0315)
+
+
+def _run_on(t: torch.Tensor, stream, fn, *args) -> None:
+    """Calls fn(*args, stream) with t's device current, on `stream` or that device's current stream."""
+    d = t.device
+    if d.index == torch.cuda.current_device():
+        _check(fn(*args, (stream or torch.cuda.current_stream(d)).cuda_stream))
+    else:
+        with torch.cuda.device(d):
+            _check(fn(*args, (stream or torch.cuda.current_stream(d)).cuda_stream))
+
+
+def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
+    """A new tensor of the stream the call runs on: its memory is not handed out again before that work is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _matrices(t: torch.Tensor, name: str):
+    """(pointer, type, row stride, batch stride) of a [batch, rows, cols] or [rows, cols] tensor."""
+    if not t.is_cuda or t.dtype not in TYPES:
+        raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor on the GPU")
+    if t.dim() == 3:
+        b, r, c = t.shape
+        sb, sr, sc = t.stride()
+    elif t.dim() == 2:
+        (r, c), (sr, sc), b, sb = t.shape, t.stride(), 1, 0
+    else:
+        raise ValueError(f"{name} must be [batch, rows, cols] or [rows, cols]")
+    if c > 1 and sc != 1:
+        raise ValueError(f"the columns of {name} must be contiguous")
+    if r <= 1 and sr < c:
+        sr = c
+    if b <= 1:
+        sb = 0
+    return t.data_ptr(), TYPES[t.dtype], sr, sb
+
+
+def _size3(t: torch.Tensor):
+    return tuple(t.shape) if t.dim() == 3 else (1, *t.shape)
+
+
+def _precision_for(t: torch.Tensor) -> int:
+    """32-bit results are computed to 32-bit accuracy, 16-bit ones from single 16-bit operands."""
+    return PRECISION_FP32 if t.dtype == torch.float32 else PRECISION_BF16
+
+
+def _same_place(name: str, t: torch.Tensor, ref: torch.Tensor) -> None:
+    if t.device != ref.device:
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {ref.device}")
+
+
+def prsgd_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, precision: int) -> int:
+    n = C.c_size_t()
+    _check(lib.prsgd_orthogonalize_workspace_bytes(batch, rows, cols, precision, C.byref(n)))
+    return n.value
+
+
+def orthogonalize_workspace(G: torch.Tensor, precision: Optional[int] = None, stream=None) -> torch.Tensor:
+    """Workspace of prsgd_orthogonalize for matrices like G (results of G's type unless `precision` says otherwise)."""
+    p = _precision_for(G) if precision is None else precision
+    return _empty(prsgd_orthogonalize_workspace_bytes(*_size3(G), p), torch.uint8, G.device, stream)
+
+
+muon_workspace = orthogonalize_workspace
+
+
+def _coefs(coefs):
+    return None if coefs is None or tuple(coefs) == MUON_COEFS else (C.c_float * 3)(*coefs)
+
+
+def prsgd_orthogonalize(G: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps: int = 5, coefs=None,
+                        scale: float = 1.0, eps: float = 1e-7, precision: Optional[int] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Newton-Schulz orthogonalisation of every matrix of G ([batch, rows, cols] or [rows, cols]); see prsgd.h."""
+    if out is None:
+        out = _empty(G.shape, G.dtype, G.device, stream)
+    elif out.shape != G.shape:
+        raise ValueError("out must have G's shape")
+    p = _precision_for(out) if precision is None else precision
+    if workspace is None:
+        workspace = orthogonalize_workspace(G, p, stream)
+    _same_place("out", out, G)
+    _same_place("workspace", workspace, G)
+    _run_on(G, stream, lib.prsgd_orthogonalize, *_matrices(G, "G"), *_matrices(out, "out"), *_size3(G), steps,
+            _coefs(coefs), scale, eps, p, workspace.data_ptr(), workspace.numel())
+    return out
+
+
+def prsgd_muon_step(W: torch.Tensor, V: torch.Tensor, G: torch.Tensor, lr: float, *, mu: float = 0.95,
+                    nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5, coefs=None, scale: float = 1.0,
+                    eps: float = 1e-7, precision: Optional[int] = None, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    """Muon step of every matrix of W in place, with its fp32 momentum buffers V; see prsgd.h."""
+    if W.shape != V.shape or W.shape != G.shape:
+        raise ValueError("W, V and G must have the same shape")
+    if V.dtype != torch.float32:
+        raise ValueError("V must be float32")
+    p = _precision_for(W) if precision is None else precision
+    if workspace is None:
+        workspace = muon_workspace(W, p, stream)
+    for name, t in (("V", V), ("G", G), ("workspace", workspace)):
+        _same_place(name, t, W)
+    v, _, vr, vb = _matrices(V, "V")
+    _run_on(W, stream, lib.prsgd_muon_step, *_matrices(W, "W"), v, vr, vb, *_matrices(G, "G"), *_size3(W), lr, mu,
+            1 if nesterov else 0, weight_decay, steps, _coefs(coefs), scale, eps, p, workspace.data_ptr(), workspace.numel())
+
+
+def prsgd_work_status(workspace: torch.Tensor, stream=None) -> None:
+    """Raises if a kernel of the last call that used this workspace recorded an error; synchronises the stream."""
+    _run_on(workspace, stream, lib.prsgd_work_status, workspace.data_ptr())
+
+
+def prsgd_route_workspace_bytes(groups: int, tokens: int, experts: int) -> int:
+    n = C.c_size_t()
+    _check(lib.prsgd_route_workspace_bytes(groups, tokens, experts, C.byref(n)))
+    return n.value
+
+
+def route_workspace(logits: torch.Tensor, stream=None) -> torch.Tensor:
+    return _empty(prsgd_route_workspace_bytes(*_size3(logits)), torch.uint8, logits.device, stream)
+
+
+def route_outputs(logits: torch.Tensor, k: int, stream=None):
+    """Tensors for prsgd_route's results: experts, weights [G, T, k], counts, mean [G, E], loss [G]."""
+    (G, T, E), d = _size3(logits), logits.device
+    i, f = torch.int32, torch.float32
+    return tuple(_empty(shape, ty, d, stream) for shape, ty in (((G, T, k), i), ((G, T, k), f), ((G, E), i), ((G, E), f), ((G,), f)))
+
+
+def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, ref: torch.Tensor):
+    """Pointer of a contiguous tensor of `numel` elements next to `ref` (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != ref.device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} elements on {ref.device}")
+    return t.data_ptr()
+
+
+def prsgd_route(logits: torch.Tensor, k: int, coef: float, *, normalize: bool = False, live: Optional[torch.Tensor] = None,
+                out=None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Top-k router with its balance loss over logits [G, T, E] (or [T, E]); returns (experts, weights, counts, mean,
+    loss), see prsgd.h.  `out`: a tuple as route_outputs makes it."""
+    ptr, ty, row, group = _matrices(logits, "logits")
+    G, T, E = _size3(logits)
+    if out is None:
+        out = route_outputs(logits, k, stream)
+    if workspace is None:
+        workspace = route_workspace(logits, stream)
+    _same_place("workspace", workspace, logits)
+    experts, weights, counts, mean, loss = out
+    _run_on(logits, stream, lib.prsgd_route, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, logits),
+            G, T, E, k, 1 if normalize else 0, coef,
+            _dense(experts, "experts", torch.int32, G * T * k, logits), _dense(weights, "weights", torch.float32, G * T * k, logits),
+            _dense(counts, "counts", torch.int32, G * E, logits), _dense(mean, "mean", torch.float32, G * E, logits),
+            _dense(loss, "loss", torch.float32, G, logits), workspace.data_ptr(), workspace.numel())
+    return out
+
+
+def prsgd_route_grad(logits: torch.Tensor, experts: torch.Tensor, counts: torch.Tensor, coef: float, *,
+                     normalize: bool = False, live: Optional[torch.Tensor] = None, dweights: Optional[torch.Tensor] = None,
+                     dloss: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of the router's weights and balance loss with respect to the logits; see prsgd.h."""
+    ptr, ty, row, group = _matrices(logits, "logits")
+    G, T, E = _size3(logits)
+    k = experts.shape[-1]
+    if out is None:
+        out = _empty(logits.shape, logits.dtype, logits.device, stream)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and type")
+    _same_place("out", out, logits)
+    optr, _, orow, ogroup = _matrices(out, "out")
+    _run_on(logits, stream, lib.prsgd_route_grad, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, logits),
+            G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", torch.int32, G * T * k, logits),
+            _dense(counts, "counts", torch.int32, G * E, logits), _dense(dweights, "dweights", torch.float32, G * T * k, logits),
+            _dense(dloss, "dloss", torch.float32, G, logits), optr, orow, ogroup)
     return out
 
 

@@ -1,0 +1,41 @@
+// What the stand-alone training operators share: element types, the device status at the head of a
+// workspace, and the error text of context-free calls.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <algorithm>
+#include <type_traits>
+#include "prsgd_common.cuh"
+
+namespace prsgd {
+
+// Records the text prsgd_last_error(NULL) returns and hands the code back (defined in prsgd_api.cu).
+int op_fail(int code, const std::string& msg);
+
+template <int T> struct ElemOf;
+template <> struct ElemOf<PRSGD_TYPE_FP32> { using type = float; };
+template <> struct ElemOf<PRSGD_TYPE_BF16> { using type = __nv_bfloat16; };
+template <> struct ElemOf<PRSGD_TYPE_FP16> { using type = __half; };
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+inline int type_bytes(int t) { return t == PRSGD_TYPE_FP32 ? 4 : 2; }
+inline bool type_known(int t) { return t == PRSGD_TYPE_FP32 || t == PRSGD_TYPE_BF16 || t == PRSGD_TYPE_FP16; }
+
+// Calls f with std::integral_constant<int, T> for the element type `t` (already known to be one).
+template <typename F> inline auto with_type(int t, F&& f) {
+  if (t == PRSGD_TYPE_FP32) return f(std::integral_constant<int, PRSGD_TYPE_FP32>());
+  if (t == PRSGD_TYPE_BF16) return f(std::integral_constant<int, PRSGD_TYPE_BF16>());
+  return f(std::integral_constant<int, PRSGD_TYPE_FP16>());
+}
+
+__device__ __forceinline__ void op_pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void op_pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+}  // namespace prsgd

@@ -1,0 +1,18 @@
+// Host entries that the context's own local step shares with the stand-alone operators.
+#pragma once
+#include "kernels_ortho.cuh"
+
+namespace prsgd {
+
+struct NsPlan {                    // one orthogonalisation of a batch, arguments already checked
+  NsShape shape;
+  NsSource src; int g_type;
+  NsDest dst;
+  int steps; float a, b, c, eps;
+  int precision;
+};
+size_t ns_workspace_bytes(const NsShape& sh, int precision);
+// Enqueues the whole chain; returns a PRSGD_ code and counts its launches.
+int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches);
+
+}  // namespace prsgd

@@ -1,0 +1,187 @@
+// C entries of the Newton-Schulz orthogonalisation and of the Muon step.  See include/prsgd.h for the contract.
+#include <cmath>
+#include "ops_internal.h"
+
+using namespace prsgd;
+
+namespace prsgd {
+
+static NsBuffers ns_carve(const NsShape& sh, int precision, unsigned char* base, size_t* bytes) {
+  NsBuffers b{};
+  const int64_t s = std::min(sh.rows, sh.cols);
+  const bool split = precision == PRSGD_PRECISION_FP32;
+  b.xp = round_up(sh.cols, 8); b.sp = round_up(s, 8);
+  const int64_t per = (int64_t)sh.rows * sh.cols;
+  b.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kNsChunks, sh.rows), (per + 8191) / 8192));
+  size_t off = 0;
+  auto take = [&](size_t n) { unsigned char* p = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return p; };
+  b.status = reinterpret_cast<DeviceStatus*>(take(sizeof(DeviceStatus)));
+  b.claim = reinterpret_cast<unsigned int*>(take(4));
+  b.done = reinterpret_cast<unsigned int*>(take(4 * (size_t)sh.batch));
+  b.part = reinterpret_cast<double*>(take(8 * (size_t)sh.batch * b.chunks));
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) b.x[i][j] = reinterpret_cast<__half*>(take(2 * (size_t)sh.batch * sh.rows * b.xp));
+  for (int j = 0; j < 2; ++j) {
+    b.A[j] = reinterpret_cast<__half*>(j == 0 || split ? take(2 * (size_t)sh.batch * s * b.sp) : nullptr);
+    b.P[j] = reinterpret_cast<__half*>(j == 0 || split ? take(2 * (size_t)sh.batch * s * b.sp) : nullptr);
+  }
+  *bytes = off;
+  return b;
+}
+
+size_t ns_workspace_bytes(const NsShape& sh, int precision) {
+  size_t n = 0;
+  ns_carve(sh, precision, nullptr, &n);
+  return n;
+}
+
+int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
+  size_t bytes = 0;
+  const NsBuffers buf = ns_carve(p.shape, p.precision, static_cast<unsigned char*>(d_work), &bytes);
+  const int s = std::min(p.shape.rows, p.shape.cols);
+  const bool split = p.precision == PRSGD_PRECISION_FP32;
+  auto fits4 = [](const void* q, int64_t row, int64_t batch, int esz) {
+    return q == nullptr || ((uintptr_t)q % (4 * esz) == 0 && row % 4 == 0 && batch % 4 == 0);
+  };
+  const bool vec = p.shape.cols % 4 == 0 && fits4(p.src.G, p.src.g_row, p.src.g_batch, type_bytes(p.g_type)) &&
+                   fits4(p.src.V, p.src.v_tiled ? 0 : p.src.v_row, p.src.v_batch, 4);
+  const dim3 grid((unsigned)buf.chunks, (unsigned)p.shape.batch);
+  with_type(p.g_type, [&](auto ty) {
+    constexpr int TY = decltype(ty)::value;
+    if (vec) {
+      launch_pdl(ns_norm_kernel<TY, 4>, grid, dim3(256), 0, st, p.shape, p.src, buf);
+      launch_pdl(ns_pack_kernel<TY, 4>, grid, dim3(256), 0, st, p.shape, p.src, buf, p.eps);
+    } else {
+      launch_pdl(ns_norm_kernel<TY, 1>, grid, dim3(256), 0, st, p.shape, p.src, buf);
+      launch_pdl(ns_pack_kernel<TY, 1>, grid, dim3(256), 0, st, p.shape, p.src, buf, p.eps);
+    }
+  });
+  if (launches) *launches += 2;
+  for (int k = 0; k < p.steps; ++k) {
+    for (int kind = 0; kind < 3; ++kind) {
+      NsGemmArgs g{p.shape, buf, p.dst, kind, k & 1, kind == 2 && k + 1 == p.steps, split ? 1 : 0, p.a, p.b, p.c};
+      const int R = kind == 2 ? p.shape.rows : s, C = kind == 2 ? p.shape.cols : s;
+      launch_pdl(ns_gemm_kernel, dim3((C + 63) / 64, (R + 63) / 64, p.shape.batch), dim3(256), 0, st, g);
+      if (launches) *launches += 1;
+    }
+  }
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
+  return PRSGD_OK;
+}
+
+}  // namespace prsgd
+
+namespace {
+
+constexpr float kDefaultCoefs[3] = {3.4445f, -4.7750f, 2.0315f};
+
+// One strided batch of matrices: pointer, alignment, strides.
+int check_matrices(const char* name, const void* p, int type, int64_t row, int64_t batch_stride, int batch, int rows, int cols, bool written) {
+  if (p == nullptr) return op_fail(PRSGD_ERR_ARG, std::string(name) + " is NULL");
+  if (!type_known(type)) return op_fail(PRSGD_ERR_ARG, std::string("unknown element type of ") + name);
+  if (((uintptr_t)p) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, std::string(name) + " is not aligned to its element type");
+  if (row < cols) return op_fail(PRSGD_ERR_ARG, std::string("row stride of ") + name + " is below its columns");
+  if (batch_stride < 0 || (written && batch > 1 && batch_stride < (int64_t)(rows - 1) * row + cols))
+    return op_fail(PRSGD_ERR_ARG, std::string("the matrices of ") + name + " overlap");
+  return PRSGD_OK;
+}
+
+int check_sizes(int batch, int rows, int cols, int precision) {
+  if (batch < 0 || rows < 0 || cols < 0) return op_fail(PRSGD_ERR_ARG, "need batch, rows, cols >= 0");
+  if (batch > 65535 || rows > PRSGD_ORTHO_MAX_SIDE || cols > PRSGD_ORTHO_MAX_SIDE)
+    return op_fail(PRSGD_ERR_SIZE, "more than 65535 matrices or a side above PRSGD_ORTHO_MAX_SIDE");
+  if (precision != PRSGD_PRECISION_FP32 && precision != PRSGD_PRECISION_BF16) return op_fail(PRSGD_ERR_ARG, "unknown precision");
+  return PRSGD_OK;
+}
+
+int check_chain(int steps, const float* coefs, float eps, NsPlan* p) {
+  if (steps < 1 || steps > PRSGD_ORTHO_MAX_STEPS) return op_fail(PRSGD_ERR_ARG, "steps must be in 1..PRSGD_ORTHO_MAX_STEPS");
+  if (!(eps >= 0.f) || std::isinf(eps)) return op_fail(PRSGD_ERR_ARG, "eps must be finite and >= 0");
+  const float* q = coefs ? coefs : kDefaultCoefs;
+  for (int i = 0; i < 3; ++i)
+    if (!(std::fabs(q[i]) <= 16.f)) return op_fail(PRSGD_ERR_ARG, "a coefficient is NaN or beyond 16 in magnitude");
+  p->steps = steps; p->a = q[0]; p->b = q[1]; p->c = q[2]; p->eps = eps;
+  return PRSGD_OK;
+}
+
+int check_work(const NsShape& sh, int precision, const void* work, size_t bytes) {
+  if (work == nullptr || bytes < ns_workspace_bytes(sh, precision))
+    return op_fail(PRSGD_ERR_SIZE, "workspace is NULL or smaller than prsgd_orthogonalize_workspace_bytes");
+  if (((uintptr_t)work) % 256) return op_fail(PRSGD_ERR_ALIGN, "d_work must be 256-byte aligned");
+  return PRSGD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int prsgd_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, int32_t precision, size_t* bytes) {
+  if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
+  int rc = check_sizes(batch, rows, cols, precision);
+  if (rc != PRSGD_OK) return rc;
+  *bytes = ns_workspace_bytes({batch, rows, cols}, precision);
+  return PRSGD_OK;
+}
+
+int prsgd_orthogonalize(const void* d_G, int32_t g_type, int64_t g_row_stride, int64_t g_batch_stride,
+                        void* d_out, int32_t out_type, int64_t out_row_stride, int64_t out_batch_stride,
+                        int32_t batch, int32_t rows, int32_t cols, int32_t steps, const float* h_coefs, float scale,
+                        float eps, int32_t precision, void* d_work, size_t work_bytes, void* cuda_stream) {
+  NsPlan p{};
+  int rc = check_sizes(batch, rows, cols, precision);
+  if (rc == PRSGD_OK) rc = check_chain(steps, h_coefs, eps, &p);
+  if (rc != PRSGD_OK) return rc;
+  if (!std::isfinite(scale)) return op_fail(PRSGD_ERR_ARG, "scale must be finite");
+  if (batch == 0 || rows == 0 || cols == 0) return PRSGD_OK;
+  rc = check_matrices("G", d_G, g_type, g_row_stride, g_batch_stride, batch, rows, cols, false);
+  if (rc == PRSGD_OK) rc = check_matrices("out", d_out, out_type, out_row_stride, out_batch_stride, batch, rows, cols, true);
+  p.shape = {batch, rows, cols}; p.precision = precision; p.g_type = g_type;
+  if (rc == PRSGD_OK) rc = check_work(p.shape, precision, d_work, work_bytes);
+  if (rc != PRSGD_OK) return rc;
+  p.src.G = d_G; p.src.g_row = g_row_stride; p.src.g_batch = g_batch_stride;
+  p.dst.out = d_out; p.dst.type = out_type; p.dst.row = out_row_stride; p.dst.batch = out_batch_stride;
+  p.dst.alpha = scale; p.dst.beta = 0.f;
+  return ns_run(p, d_work, static_cast<cudaStream_t>(cuda_stream), nullptr);
+}
+
+int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_batch_stride,
+                    float* d_V, int64_t v_row_stride, int64_t v_batch_stride,
+                    const void* d_G, int32_t g_type, int64_t g_row_stride, int64_t g_batch_stride,
+                    int32_t batch, int32_t rows, int32_t cols, float lr, float mu, int32_t nesterov, float weight_decay,
+                    int32_t steps, const float* h_coefs, float scale, float eps, int32_t precision,
+                    void* d_work, size_t work_bytes, void* cuda_stream) {
+  NsPlan p{};
+  int rc = check_sizes(batch, rows, cols, precision);
+  if (rc == PRSGD_OK) rc = check_chain(steps, h_coefs, eps, &p);
+  if (rc != PRSGD_OK) return rc;
+  if (!(mu >= 0.f && mu < 1.f)) return op_fail(PRSGD_ERR_ARG, "mu must be in [0, 1)");
+  if (!std::isfinite(lr) || !std::isfinite(scale) || !std::isfinite(weight_decay)) return op_fail(PRSGD_ERR_ARG, "lr, scale and weight_decay must be finite");
+  if (lr * weight_decay == 1.f) return op_fail(PRSGD_ERR_ARG, "lr * weight_decay must not be 1");
+  if (batch == 0 || rows == 0 || cols == 0) return PRSGD_OK;
+  rc = check_matrices("W", d_W, w_type, w_row_stride, w_batch_stride, batch, rows, cols, true);
+  if (rc == PRSGD_OK) rc = check_matrices("V", d_V, PRSGD_TYPE_FP32, v_row_stride, v_batch_stride, batch, rows, cols, true);
+  if (rc == PRSGD_OK) rc = check_matrices("G", d_G, g_type, g_row_stride, g_batch_stride, batch, rows, cols, false);
+  p.shape = {batch, rows, cols}; p.precision = precision; p.g_type = g_type;
+  if (rc == PRSGD_OK) rc = check_work(p.shape, precision, d_work, work_bytes);
+  if (rc != PRSGD_OK) return rc;
+  p.src.G = d_G; p.src.g_row = g_row_stride; p.src.g_batch = g_batch_stride;
+  p.src.V = d_V; p.src.v_row = v_row_stride; p.src.v_batch = v_batch_stride; p.src.mu = mu; p.src.nesterov = nesterov != 0;
+  p.dst.out = d_W; p.dst.type = w_type; p.dst.row = w_row_stride; p.dst.batch = w_batch_stride;
+  p.dst.alpha = -lr * scale; p.dst.beta = 1.f - lr * weight_decay;
+  return ns_run(p, d_work, static_cast<cudaStream_t>(cuda_stream), nullptr);
+}
+
+int prsgd_work_status(const void* d_work, void* cuda_stream) {
+  if (!d_work) return op_fail(PRSGD_ERR_ARG, "d_work is NULL");
+  unsigned int st[2] = {0, 0};
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = cudaMemcpyAsync(st, d_work, sizeof st, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("work_status: ") + cudaGetErrorString(e));
+  if (st[0] != 0u)
+    return op_fail(PRSGD_ERR_DEVICE_TIMEOUT, "a bounded wait expired in an operator's kernel (code " + std::to_string(st[0]) + ", block " + std::to_string(st[1]) + ")");
+  return PRSGD_OK;
+}
+
+}  // extern "C"

@@ -24,6 +24,14 @@ int fail(prsgd_ctx* ctx, int code, const std::string& msg) {
   return code;
 }
 
+}  // namespace
+
+namespace prsgd {
+int op_fail(int code, const std::string& msg) { return fail(nullptr, code, msg); }   // for the stand-alone operators' files
+}  // namespace prsgd
+
+namespace {
+
 #define CUDA_TRY(ctx, expr)                                                                   \
   do {                                                                                        \
     cudaError_t e__ = (expr);                                                                 \

@@ -1,0 +1,111 @@
+// C entries of the top-k router (prsgd_route, prsgd_route_grad).  See include/prsgd.h for the contract.
+#include "kernels_route.cuh"
+
+using namespace prsgd;
+
+namespace {
+
+int route_blocks(int64_t G, int64_t T) {
+  int64_t b = (T + 7) / 8;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kRouteBlocks, (148 * 8 + G - 1) / G));
+  return (int)std::min<int64_t>(b, most);
+}
+
+int check_route(const void* logits, int type, int64_t row_stride, int64_t group_stride, int64_t G, int64_t T, int E, int k) {
+  if (!type_known(type)) return op_fail(PRSGD_ERR_ARG, "unknown element type of the logits");
+  if (G < 0 || T < 0 || E < 1 || k < 1) return op_fail(PRSGD_ERR_ARG, "need groups >= 0, tokens >= 0, experts >= 1, top_k >= 1");
+  if (E > kRouteMaxExperts) return op_fail(PRSGD_ERR_SIZE, "more than PRSGD_ROUTE_MAX_EXPERTS experts");
+  if (k > E || k > kRouteMaxK) return op_fail(PRSGD_ERR_ARG, "top_k exceeds the experts or PRSGD_ROUTE_MAX_K");
+  if (G > 65535) return op_fail(PRSGD_ERR_SIZE, "more than 65535 groups");
+  if (T > (1ll << 31) / k - 1 || T > (1ll << 24)) return op_fail(PRSGD_ERR_SIZE, "more than 2^24 tokens in a group");
+  if (G > 0 && T > 0 && logits == nullptr) return op_fail(PRSGD_ERR_ARG, "logits is NULL");
+  if (row_stride < E || group_stride < 0) return op_fail(PRSGD_ERR_ARG, "need row_stride >= experts, group_stride >= 0");
+  if (((uintptr_t)logits) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, "logits is not aligned to its element type");
+  return PRSGD_OK;
+}
+
+template <typename F> void with_per(int E, F&& f) {
+  if (E <= 32) f(std::integral_constant<int, 1>());
+  else if (E <= 64) f(std::integral_constant<int, 2>());
+  else if (E <= 128) f(std::integral_constant<int, 4>());
+  else if (E <= 256) f(std::integral_constant<int, 8>());
+  else if (E <= 512) f(std::integral_constant<int, 16>());
+  else f(std::integral_constant<int, 32>());
+}
+
+}  // namespace
+
+extern "C" {
+
+int prsgd_route_workspace_bytes(int64_t groups, int64_t tokens, int32_t experts, size_t* bytes) {
+  if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
+  if (groups < 0 || tokens < 0 || experts < 1 || experts > kRouteMaxExperts)
+    return op_fail(PRSGD_ERR_ARG, "need groups >= 0, tokens >= 0, experts in 1..PRSGD_ROUTE_MAX_EXPERTS");
+  const size_t slots = (size_t)groups * (size_t)std::max(1, route_blocks(std::max<int64_t>(groups, 1), tokens));
+  *bytes = 256 + slots * ((size_t)experts * 8 + 4) + 256;
+  return PRSGD_OK;
+}
+
+int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t group_stride, const uint8_t* d_live,
+                int64_t groups, int64_t tokens, int32_t experts, int32_t top_k, int32_t normalize, float coef,
+                int32_t* d_experts, float* d_weights, int32_t* d_counts, float* d_mean, float* d_loss,
+                void* d_work, size_t work_bytes, void* cuda_stream) {
+  int rc = check_route(d_logits, type, row_stride, group_stride, groups, tokens, experts, top_k);
+  if (rc != PRSGD_OK) return rc;
+  if (groups == 0) return PRSGD_OK;
+  if (!d_counts || !d_mean || !d_loss || (tokens > 0 && (!d_experts || !d_weights))) return op_fail(PRSGD_ERR_ARG, "an output is NULL");
+  size_t need = 0;
+  prsgd_route_workspace_bytes(groups, tokens, experts, &need);
+  if (!d_work || work_bytes < need) return op_fail(PRSGD_ERR_SIZE, "workspace is NULL or smaller than prsgd_route_workspace_bytes");
+  if (((uintptr_t)d_work) % 256) return op_fail(PRSGD_ERR_ALIGN, "d_work must be 256-byte aligned");
+  RouteArgs a{};
+  a.logits = d_logits; a.row_stride = row_stride; a.group_stride = group_stride; a.live = d_live;
+  a.G = groups; a.T = tokens; a.E = experts; a.k = top_k; a.normalize = normalize != 0; a.coef = coef;
+  a.experts = d_experts; a.weights = d_weights; a.counts = d_counts; a.mean = d_mean; a.loss = d_loss;
+  a.blocks = route_blocks(groups, tokens);
+  unsigned char* w = static_cast<unsigned char*>(d_work) + 256;
+  a.part_p = reinterpret_cast<float*>(w);
+  a.part_c = reinterpret_cast<int32_t*>(a.part_p + (size_t)groups * a.blocks * experts);
+  a.part_n = a.part_c + (size_t)groups * a.blocks * experts;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (a.blocks > 0)
+    with_type(type, [&](auto ty) {
+      with_per(experts, [&](auto per) {
+        launch_pdl(route_kernel<decltype(ty)::value, decltype(per)::value>, dim3((unsigned)a.blocks, (unsigned)groups), dim3(256), 0, st, a);
+      });
+    });
+  launch_pdl(route_finish_kernel, dim3((unsigned)groups), dim3(256), 0, st, a);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("route: ") + cudaGetErrorString(e));
+  return PRSGD_OK;
+}
+
+int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int64_t group_stride, const uint8_t* d_live,
+                     int64_t groups, int64_t tokens, int32_t experts, int32_t top_k, int32_t normalize, float coef,
+                     const int32_t* d_experts, const int32_t* d_counts, const float* d_dweights, const float* d_dloss,
+                     void* d_dlogits, int64_t d_row_stride, int64_t d_group_stride, void* cuda_stream) {
+  int rc = check_route(d_logits, type, row_stride, group_stride, groups, tokens, experts, top_k);
+  if (rc != PRSGD_OK) return rc;
+  if (groups == 0 || tokens == 0) return PRSGD_OK;
+  if (!d_counts || !d_dlogits || (d_dweights && !d_experts)) return op_fail(PRSGD_ERR_ARG, "counts, dlogits or experts is NULL");
+  if (d_row_stride < experts || (groups > 1 && d_group_stride < (tokens - 1) * d_row_stride + experts))
+    return op_fail(PRSGD_ERR_ARG, "the rows of dlogits overlap");
+  if (((uintptr_t)d_dlogits) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, "dlogits is not aligned to its element type");
+  RouteArgs a{};
+  a.logits = d_logits; a.row_stride = row_stride; a.group_stride = group_stride; a.live = d_live;
+  a.G = groups; a.T = tokens; a.E = experts; a.k = top_k; a.normalize = normalize != 0; a.coef = coef;
+  a.experts = const_cast<int32_t*>(d_experts); a.counts = const_cast<int32_t*>(d_counts);
+  a.dweights = d_dweights; a.dloss = d_dloss; a.dlogits = d_dlogits; a.d_row_stride = d_row_stride; a.d_group_stride = d_group_stride;
+  const int64_t blocks = std::min<int64_t>((tokens + 7) / 8, std::max<int64_t>(1, (148 * 8 + groups - 1) / groups));
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  with_type(type, [&](auto ty) {
+    with_per(experts, [&](auto per) {
+      launch_pdl(route_grad_kernel<decltype(ty)::value, decltype(per)::value>, dim3((unsigned)blocks, (unsigned)groups), dim3(256), 0, st, a);
+    });
+  });
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("route_grad: ") + cudaGetErrorString(e));
+  return PRSGD_OK;
+}
+
+}  // extern "C"
