@@ -37,78 +37,98 @@ struct NsBuffers {
   __half* A[2]; __half* P[2];            // [hi, lo]: [batch][s][sp]
   double* part;                          // [batch][chunks]
   unsigned int* claim;                   // next unclaimed task
-  unsigned int* done;                    // [batch] finished tasks
+  unsigned int* done;                    // [batch][panels] tiles that have been added to a panel
+  int panels;
   DeviceStatus* status;
   int64_t xp, sp;
   int chunks;
 };
 struct NsShape { int batch, rows, cols; };
 
-// Squares of one chunk of rows of a matrix; applies the momentum on the way.  Grid (chunks, batch).
+// VEC neighbouring elements of a row as fp32
 template <int TY, int VEC>
+__device__ __forceinline__ void ns_load(const typename ElemOf<TY>::type* p, float (&u)[VEC]) {
+  using T = typename ElemOf<TY>::type;
+  if constexpr (VEC == 1) {
+    u[0] = to_f32(p[0]);
+  } else if constexpr (TY == PRSGD_TYPE_FP32) {
+#pragma unroll
+    for (int q = 0; q < VEC / 4; ++q) {
+      const float4 x = reinterpret_cast<const float4*>(p)[q];
+      u[4 * q] = x.x; u[4 * q + 1] = x.y; u[4 * q + 2] = x.z; u[4 * q + 3] = x.w;
+    }
+  } else {
+    static_assert(VEC == 4);
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    const T* h = reinterpret_cast<const T*>(&x);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) u[i] = to_f32(h[i]);
+  }
+}
+
+// How a block of 256 threads walks its rows: `tx` threads side by side along a row, 4 rows of a thread at a time so
+// that their loads are in flight together (one at a time both passes waited for latency: 25 + 35 us at 16 x 1024 x 1024).
+constexpr int kNsRows = 4;
+template <int VEC, typename F>
+__device__ __forceinline__ void ns_walk(const NsShape& sh, F&& f) {
+  const int per = (sh.rows + (int)gridDim.x - 1) / (int)gridDim.x;
+  const int r1 = min(sh.rows, ((int)blockIdx.x + 1) * per);
+  int tx = 1;
+  while (tx < 256 && tx * VEC < sh.cols) tx <<= 1;
+  const int cx = (threadIdx.x & (tx - 1)) * VEC, ry = threadIdx.x / tx, dy = 256 / tx;
+  for (int r = (int)blockIdx.x * per + ry; r < r1; r += dy * kNsRows)
+    for (int c = cx; c < sh.cols; c += tx * VEC) f(r, dy, r1, c);
+}
+
+// MODE 0: G alone, 1: V alone, 2: both.  Squares of one chunk of rows of a matrix; applies the momentum on the way.
+// Grid (chunks, batch).
+template <int TY, int VEC, int MODE>
 __global__ void __launch_bounds__(256) ns_norm_kernel(const NsShape sh, const NsSource src, const NsBuffers buf) {
   using T = typename ElemOf<TY>::type;
   op_pdl_wait();
   op_pdl_trigger();
   const int m = blockIdx.y;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    buf.done[m] = 0u;
-    if (m == 0) { *buf.claim = 0u; buf.status->error = 0u; }
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < buf.panels; i += 256) buf.done[(int64_t)m * buf.panels + i] = 0u;
+    if (m == 0 && threadIdx.x == 0) { *buf.claim = 0u; buf.status->error = 0u; }
   }
   __shared__ double s_part[8];
   double sum = 0.0;
   if (src.active == nullptr || src.active[m] != 0) {
-    const int per = (sh.rows + (int)gridDim.x - 1) / (int)gridDim.x;
-    const int r1 = min(sh.rows, ((int)blockIdx.x + 1) * per);
-    int tx = 1;
-    while (tx < 256 && tx * VEC < sh.cols) tx <<= 1;
-    const int cx = (threadIdx.x & (tx - 1)) * VEC, ry = threadIdx.x / tx, dy = 256 / tx;
     const T* g = static_cast<const T*>(src.G) + (int64_t)m * src.g_batch;
     float* v = src.V + (int64_t)m * src.v_batch;
-    for (int r = (int)blockIdx.x * per + ry; r < r1; r += dy) {
-      for (int c = cx; c < sh.cols; c += tx * VEC) {
-        float u[VEC];
-        if (src.G != nullptr) {
-          if constexpr (VEC == 4) {
-            if constexpr (TY == PRSGD_TYPE_FP32) {
-              const float4 q = *reinterpret_cast<const float4*>(g + (int64_t)r * src.g_row + c);
-              u[0] = q.x; u[1] = q.y; u[2] = q.z; u[3] = q.w;
-            } else {
-              const uint2 q = *reinterpret_cast<const uint2*>(g + (int64_t)r * src.g_row + c);
-              const T* h = reinterpret_cast<const T*>(&q);
+    ns_walk<VEC>(sh, [&](int r, int dy, int r1, int c) {
+      float u[kNsRows][VEC], w[kNsRows][VEC];
+      float* at[kNsRows];
 #pragma unroll
-              for (int i = 0; i < VEC; ++i) u[i] = to_f32(h[i]);
-            }
-          } else {
-            u[0] = to_f32(g[(int64_t)r * src.g_row + c]);
-          }
+      for (int k = 0; k < kNsRows; ++k) {
+        const int rr = r + k * dy;
+        const bool on = rr < r1;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) u[k][i] = w[k][i] = 0.f;
+        if (MODE != 1 && on) ns_load<TY, VEC>(g + (int64_t)rr * src.g_row + c, u[k]);
+        if (MODE != 0 && on) {
+          at[k] = v + (src.v_tiled ? wtile_offset(src.v_tile, rr, c) : (int64_t)rr * src.v_row + c);
+          ns_load<PRSGD_TYPE_FP32, VEC>(at[k], w[k]);
         }
-        if (src.V != nullptr) {
-          float* at = v + (src.v_tiled ? wtile_offset(src.v_tile, r, c) : (int64_t)r * src.v_row + c);
-          float w[VEC];
-          if constexpr (VEC == 4) {
-            const float4 q = *reinterpret_cast<const float4*>(at);
-            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-          } else {
-            w[0] = at[0];
-          }
-          if (src.G != nullptr) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              w[i] = fmaf(src.mu, w[i], u[i]);
-              u[i] = src.nesterov ? fmaf(src.mu, w[i], u[i]) : w[i];
-            }
-            if constexpr (VEC == 4) *reinterpret_cast<float4*>(at) = make_float4(w[0], w[1], w[2], w[3]);
-            else at[0] = w[0];
-          } else {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) u[i] = w[i];
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) sum += (double)u[i] * (double)u[i];
       }
-    }
+#pragma unroll
+      for (int k = 0; k < kNsRows; ++k) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          if (MODE == 1) u[k][i] = w[k][i];
+          if (MODE == 2) {
+            w[k][i] = fmaf(src.mu, w[k][i], u[k][i]);
+            u[k][i] = src.nesterov ? fmaf(src.mu, w[k][i], u[k][i]) : w[k][i];
+          }
+          sum += (double)u[k][i] * (double)u[k][i];
+        }
+        if (MODE == 2 && r + k * dy < r1) {
+          if constexpr (VEC == 4) *reinterpret_cast<float4*>(at[k]) = make_float4(w[k][0], w[k][1], w[k][2], w[k][3]);
+          else at[k][0] = w[k][0];
+        }
+      }
+    });
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -127,41 +147,58 @@ __device__ __forceinline__ void ns_split(float x256, __half& hi, __half& lo) {
   lo = __float2half_rn(x256 - __half2float(hi));
 }
 
+// 256 / (||U|| + eps) as two factors that neither overflow nor vanish for any norm fp32 matrices have: a power of two
+// (exact) and the rest (rounded once).  NaN for a norm that is none.
+__device__ __forceinline__ float2 ns_inverse(double norm) {
+  if (!(norm < 1e300)) return make_float2(1.f, __int_as_float(0x7fffffff));
+  const int e = norm > 0.0 ? ilogb(norm) / 2 : 0;
+  const double p = scalbn(1.0, -e);
+  return make_float2((float)p, (float)((double)kNsScale / norm / p));
+}
+
 // X_0 = U / (||U|| + eps).  Grid (chunks, batch).
-template <int TY, int VEC>
+template <int TY, int VEC, int MODE>
 __global__ void __launch_bounds__(256) ns_pack_kernel(const NsShape sh, const NsSource src, const NsBuffers buf, float eps) {
   using T = typename ElemOf<TY>::type;
   op_pdl_wait();
   op_pdl_trigger();
   const int m = blockIdx.y;
   if (src.active != nullptr && src.active[m] == 0) return;
-  double total = 0.0;
-  for (int i = 0; i < buf.chunks; ++i) total += buf.part[(int64_t)m * buf.chunks + i];
-  // (the quotient in 64 bits: a norm beyond fp32's range still divides; 1 / 0 of a zero matrix with eps = 0 gives NaN)
-  const double inv = (double)kNsScale / (sqrt(total) + (double)eps);
-  const int per = (sh.rows + (int)gridDim.x - 1) / (int)gridDim.x;
-  const int r1 = min(sh.rows, ((int)blockIdx.x + 1) * per);
-  int tx = 1;
-  while (tx < 256 && tx * VEC < sh.cols) tx <<= 1;
-  const int cx = (threadIdx.x & (tx - 1)) * VEC, ry = threadIdx.x / tx, dy = 256 / tx;
+  __shared__ float2 s_inv;
+  if (threadIdx.x < 32) {
+    double total = 0.0;
+    for (int i = threadIdx.x; i < buf.chunks; i += 32) total += buf.part[(int64_t)m * buf.chunks + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (threadIdx.x == 0) s_inv = ns_inverse(sqrt(total) + (double)eps);
+  }
+  __syncthreads();
+  const float2 inv = s_inv;
   const T* g = static_cast<const T*>(src.G) + (int64_t)m * src.g_batch;
   const float* v = src.V + (int64_t)m * src.v_batch;
   __half* xh = buf.x[0][0] + (int64_t)m * sh.rows * buf.xp;
   __half* xl = buf.x[0][1] + (int64_t)m * sh.rows * buf.xp;
-  for (int r = (int)blockIdx.x * per + ry; r < r1; r += dy) {
-    for (int c = cx; c < sh.cols; c += tx * VEC) {
-      __half hi[VEC], lo[VEC];
+  ns_walk<VEC>(sh, [&](int r, int dy, int r1, int c) {
+    float u[kNsRows][VEC], w[kNsRows][VEC];
+#pragma unroll
+    for (int k = 0; k < kNsRows; ++k) {
+      const int rr = r + k * dy;
+      const bool on = rr < r1;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) u[k][i] = w[k][i] = 0.f;
+      if (on && (MODE == 0 || (MODE == 2 && src.nesterov))) ns_load<TY, VEC>(g + (int64_t)rr * src.g_row + c, u[k]);
+      if (on && MODE != 0) ns_load<PRSGD_TYPE_FP32, VEC>(v + (src.v_tiled ? wtile_offset(src.v_tile, rr, c) : (int64_t)rr * src.v_row + c), w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kNsRows; ++k) {
+      if (r + k * dy >= r1) break;
+      __align__(8) __half hi[VEC], lo[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        float u = 0.f;
-        if (src.G != nullptr) u = to_f32(g[(int64_t)r * src.g_row + c + i]);
-        if (src.V != nullptr) {
-          const float w = v[src.v_tiled ? wtile_offset(src.v_tile, r, c + i) : (int64_t)r * src.v_row + c + i];
-          u = src.G == nullptr || !src.nesterov ? w : fmaf(src.mu, w, u);
-        }
-        ns_split((float)((double)u * inv), hi[i], lo[i]);
+        const float x = MODE == 0 ? u[k][i] : (MODE == 2 && src.nesterov) ? fmaf(src.mu, w[k][i], u[k][i]) : w[k][i];
+        ns_split(x * inv.x * inv.y, hi[i], lo[i]);
       }
-      const int64_t o = (int64_t)r * buf.xp + c;
+      const int64_t o = (int64_t)(r + k * dy) * buf.xp + c;
       if constexpr (VEC == 4) {
         *reinterpret_cast<uint2*>(xh + o) = *reinterpret_cast<uint2*>(hi);
         *reinterpret_cast<uint2*>(xl + o) = *reinterpret_cast<uint2*>(lo);
@@ -169,7 +206,7 @@ __global__ void __launch_bounds__(256) ns_pack_kernel(const NsShape sh, const Ns
         xh[o] = hi[0]; xl[o] = lo[0];
       }
     }
-  }
+  });
 }
 
 __device__ __forceinline__ void ns_store_final(const NsDest& d, int m, int r, int c, float x) {
@@ -186,72 +223,6 @@ __device__ __forceinline__ void ns_store_final(const NsDest& d, int m, int r, in
     __half* p = static_cast<__half*>(d.out) + o;
     *p = __float2half_rn(d.beta != 0.f ? fmaf(d.alpha, x, d.beta * __half2float(*p)) : d.alpha * x);
   }
-}
-
-// One product of the chain on the CUDA cores, 64 x 64 tiles.  kind 0: A, 1: P, 2: X.
-struct NsGemmArgs {
-  NsShape sh; NsBuffers buf; NsDest dst;
-  int kind, from, last, split;           // from: buffer that holds X
-  float a, b, c;
-};
-
-__global__ void __launch_bounds__(256) ns_gemm_kernel(const NsGemmArgs a) {
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int m = blockIdx.z;
-  if (a.dst.active != nullptr && a.dst.active[m] == 0) return;
-  const bool tall = a.sh.rows > a.sh.cols;
-  const int s = min(a.sh.rows, a.sh.cols), l = max(a.sh.rows, a.sh.cols);
-  const int R = a.kind == 2 ? a.sh.rows : s, C = a.kind == 2 ? a.sh.cols : s, K = a.kind == 0 ? l : s;
-  __shared__ float L[16][65], Rr[16][65];
-  const __half* xh = a.buf.x[a.from][0] + (int64_t)m * a.sh.rows * a.buf.xp;
-  const __half* xl = a.buf.x[a.from][1] + (int64_t)m * a.sh.rows * a.buf.xp;
-  const int64_t so = (int64_t)m * s * a.buf.sp;
-  auto X = [&](int r, int c) { return __half2float(xh[(int64_t)r * a.buf.xp + c]) + (a.split ? __half2float(xl[(int64_t)r * a.buf.xp + c]) : 0.f); };
-  auto S = [&](__half* const* q, int r, int c) {
-    return __half2float(q[0][so + (int64_t)r * a.buf.sp + c]) + (a.split ? __half2float(q[1][so + (int64_t)r * a.buf.sp + c]) : 0.f);
-  };
-  auto left = [&](int i, int k) { return a.kind == 0 ? (tall ? X(k, i) : X(i, k)) : a.kind == 1 ? S(a.buf.A, i, k) : (tall ? X(i, k) : S(a.buf.P, i, k)); };
-  auto right = [&](int k, int j) { return a.kind == 0 ? (tall ? X(k, j) : X(j, k)) : a.kind == 1 ? S(a.buf.A, k, j) : (tall ? S(a.buf.P, k, j) : X(k, j)); };
-  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, ti = threadIdx.x / 16, tj = threadIdx.x % 16;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < K; k0 += 16) {
-    for (int e = threadIdx.x; e < 1024; e += 256) {
-      const int k = e & 15, i = e >> 4;
-      L[k][i] = i0 + i < R && k0 + k < K ? left(i0 + i, k0 + k) : 0.f;
-      Rr[k][i] = j0 + i < C && k0 + k < K ? right(k0 + k, j0 + i) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(L[k][ti * 4 + p], Rr[k][tj * 4 + q], acc[p][q]);
-    __syncthreads();
-  }
-  for (int p = 0; p < 4; ++p)
-    for (int q = 0; q < 4; ++q) {
-      const int i = i0 + ti * 4 + p, j = j0 + tj * 4 + q;
-      if (i >= R || j >= C) continue;
-      float v = acc[p][q] * kNsUnscale;                 // 256 times the product
-      if (a.kind < 2) {
-        if (a.kind == 1) v = a.c * v + a.b * S(a.buf.A, i, j) + (i == j ? a.a * kNsScale : 0.f);
-        __half hi, lo;
-        ns_split(v, hi, lo);
-        __half* const* o = a.kind == 0 ? a.buf.A : a.buf.P;
-        o[0][so + (int64_t)i * a.buf.sp + j] = hi;
-        if (a.split) o[1][so + (int64_t)i * a.buf.sp + j] = lo;
-        continue;
-      }
-      const int64_t xo = (int64_t)m * a.sh.rows * a.buf.xp + (int64_t)i * a.buf.xp + j;
-      if (!a.split && !a.last) v += a.a * __half2float(a.buf.x[a.from][1][xo]);
-      if (a.last) { ns_store_final(a.dst, m, i, j, v * kNsUnscale); continue; }
-      __half hi, lo;
-      ns_split(v, hi, lo);
-      a.buf.x[1 - a.from][0][xo] = hi;
-      a.buf.x[1 - a.from][1][xo] = lo;
-    }
 }
 
 }  // namespace prsgd

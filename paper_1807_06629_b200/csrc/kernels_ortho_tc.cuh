@@ -1,0 +1,623 @@
+// The products of the Newton-Schulz chain on the tensor cores (see kernels_ortho.cuh for the mathematics).
+//
+// One persistent launch runs all 3 * steps products of all matrices.  A pair of CTAs (cta_group::2) forms a 256 x 256
+// tile: each loads half of both operands (128 rows of A, 128 of B, 64 of K per stage) by TMA and keeps 128 rows of
+// the sum in its TMEM, two sums of 256 columns so that the epilogue of one tile runs beside the products of the next.
+// A and P are symmetric: only tiles on and above the diagonal are formed, the epilogue also writes their transpose.
+// Nothing is ever transposed in memory: operands whose contraction runs down the rows are read MN-major.
+//
+// Tiles are claimed in order from a device counter (matrices in groups, within a group product by product), and a
+// tile starts when the panels it reads are counted as done: 256 rows (tall: columns) of X, A or P along the short side,
+// one counter per panel that runs through all products.  A tile of A or P reads panels ti and tj whole and adds to both
+// (its transpose); a tile of X reads one panel of P and adds to one of X.  Reading is always over before the next
+// product writes the same place: a panel of X is done only when all tiles of P that read its panel of A are, and a
+// panel of P needs every panel of A, hence every tile of X before.  A claimed tile waits only for tiles claimed
+// earlier, so the CTAs that run always make progress, whatever share of the grid is resident; and while one matrix's
+// last tiles drain, the pairs that are free work on the next matrix instead of waiting for a grid.
+#pragma once
+#include "kernels_ortho.cuh"
+#include "tc_ptx.cuh"
+
+namespace prsgd {
+
+constexpr int kNsStages = 5, kNsRing = 4, kNsThreads = 384, kNsEpiWarps = 8;
+constexpr uint32_t kNsStageBytes = 32768, kNsWarpBytes = 8192;      // operand stage of a CTA; staging of an epilogue warp
+constexpr size_t kNsSmem = 1024 + (size_t)kNsStages * kNsStageBytes + kNsEpiWarps * kNsWarpBytes;
+constexpr int kNsAhead = 8;            // the next tile is claimed when this many blocks of 64 of the current one are left to load
+constexpr int kNsPromote = 4;          // 32-bit precision: blocks of 64 whose products are summed in TMEM before they join the sum in registers
+enum { NS_ERR_DEP = 0x701, NS_ERR_FULL, NS_ERR_EMPTY, NS_ERR_ACC, NS_ERR_ACC_FREE, NS_ERR_RING, NS_ERR_RING_FREE, NS_ERR_ADD };
+
+struct NsMaps {
+  CUtensorMap x[2][2];                       // operand read MN-major: [buffer][hi, lo], box {64, 64, 1}
+  CUtensorMap xk[2][2], A[2], P[2];          // operands read K-major: box {64, 128, 1}
+  CUtensorMap xs[2][2], As[2], Ps[2];        // what a warp of the epilogue moves: box {32, 32, 1}, 64-byte swizzle
+  CUtensorMap At[2], Pt[2];                  // ... transposed: the same box, not swizzled
+};
+
+struct NsChainArgs {
+  NsShape sh; NsBuffers buf; NsDest dst;
+  int steps, split, tall, s, l;
+  float a, b, c;
+  int ts, tsym, tr, tc;          // tiles along the short side; tiles of A and P on and above the diagonal; tile rows and columns of X
+  int per_step, per_panel;       // tiles of a matrix and step; of them, tiles of one panel
+  int group, total;              // matrices of a group; tiles of the launch
+  int vec_out;                   // result rows can be written 16 bytes at a time
+};
+
+struct NsTask { int m, step, kind, ti, tj; int pi, pj, need; };      // pi, pj: the panels (256 rows or columns along the short side) it takes from and adds to
+
+__device__ __forceinline__ NsTask ns_decode(const NsChainArgs& a, int t) {
+  const int per_group = a.group * a.steps * a.per_step;
+  const int g = t / per_group;
+  int rem = t - g * per_group;
+  const int gs = min(a.group, a.sh.batch - g * a.group);
+  NsTask k;
+  k.step = rem / (gs * a.per_step);
+  rem -= k.step * gs * a.per_step;
+  k.need = k.step * a.per_panel;
+  k.kind = 0;
+  if (rem >= gs * a.tsym) { rem -= gs * a.tsym; k.kind = 1; k.need += a.ts; }
+  if (k.kind == 1 && rem >= gs * a.tsym) { rem -= gs * a.tsym; k.kind = 2; k.need += a.ts; }
+  const int tiles = k.kind == 2 ? a.tr * a.tc : a.tsym;
+  k.m = rem / tiles;
+  const int q = rem - k.m * tiles;
+  k.m += g * a.group;
+  if (k.kind == 2) {                                    // panel by panel
+    if (a.tall) { k.tj = q / a.tr; k.ti = q - k.tj * a.tr; k.pi = k.pj = k.tj; }
+    else        { k.ti = q / a.tc; k.tj = q - k.ti * a.tc; k.pi = k.pj = k.ti; }
+  } else {                                              // q = tj (tj + 1) / 2 + ti, ti <= tj
+    int j = (int)((sqrtf(8.f * (float)q + 1.f) - 1.f) * 0.5f);
+    while (j * (j + 1) / 2 > q) --j;
+    while ((j + 1) * (j + 2) / 2 <= q) ++j;
+    k.tj = k.pj = j; k.ti = k.pi = q - j * (j + 1) / 2;
+  }
+  k.need *= 2 * kNsEpiWarps;                            // every epilogue warp of the pair counts a tile
+  k.pi += k.m * a.ts; k.pj += k.m * a.ts;
+  return k;
+}
+
+namespace ptx {
+// loads into this CTA's shared memory, counted on a barrier that may be the pair's other CTA's
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar_cluster, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"((uint64_t)map), "r"(bar_cluster), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_dst, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish_pair() {
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void mma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// arrives on the barrier at this offset in both CTAs of the pair once the MMAs issued so far have completed
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// mbar_wait for a barrier that the other CTA of the cluster arrives on
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* status, unsigned what) {
+  long long t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
+    if ((it & 63u) == 0u) {
+      if (*abort_flag) return false;
+      const long long now = clock64();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > kWaitLimitCycles) {
+        *abort_flag = 1;
+        if (atomicCAS(&status->error, 0u, what) == 0u) status->where = blockIdx.x;
+        return false;
+      }
+    }
+  }
+}
+// fp16 operands, fp32 sum
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn_major, int b_mn_major) {
+  return (1u << 4) | ((uint32_t)a_mn_major << 15) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+}  // namespace ptx
+
+__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+
+// fp16 pairs of 32 values
+__device__ __forceinline__ void ns_pack(const float (&v)[32], uint32_t (&h)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) h[i] = pack_half2(v[2 * i], v[2 * i + 1]);
+}
+// ... and of what that rounding left
+__device__ __forceinline__ void ns_pack_rest(const float (&v)[32], const uint32_t (&h)[16], uint32_t (&l)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float2 f = unpack_half2(h[i]);
+    l[i] = pack_half2(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+  }
+}
+__device__ __forceinline__ void ns_add(float (&v)[32], const uint32_t (&h)[16], float f) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float2 x = unpack_half2(h[i]);
+    v[2 * i] = fmaf(f, x.x, v[2 * i]);
+    v[2 * i + 1] = fmaf(f, x.y, v[2 * i + 1]);
+  }
+}
+__device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+// A warp's box of 32 rows (a lane each) x 32 halves in shared memory, 64-byte swizzle: chunk c of row r sits at chunk
+// c ^ (r / 2 % 4).
+__device__ __forceinline__ uint32_t ns_chunk(uint32_t box, int lane, int q) {
+  return box + (uint32_t)lane * 64u + (uint32_t)((q ^ ((lane >> 1) & 3)) * 16);
+}
+__device__ __forceinline__ void ns_put(uint32_t box, int lane, const uint32_t (&h)[16]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) st_shared_v4(ns_chunk(box, lane, q), h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+}
+__device__ __forceinline__ void ns_get(uint32_t box, int lane, uint32_t (&h)[16]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint4 u = ld_shared_v4(ns_chunk(box, lane, q));
+    h[4 * q] = u.x; h[4 * q + 1] = u.y; h[4 * q + 2] = u.z; h[4 * q + 3] = u.w;
+  }
+}
+// The same values transposed: 32 rows (the columns) of 32 halves (the lanes), not swizzled.
+__device__ __forceinline__ void ns_put_transposed(uint32_t box, int lane, const uint32_t (&h)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t at = box + (uint32_t)(2 * i) * 64u + (uint32_t)lane * 2u;
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((uint16_t)(h[i] & 0xffffu)) : "memory");
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 64u), "h"((uint16_t)(h[i] >> 16)) : "memory");
+  }
+}
+// acc += f * (32 halves at p, of which n exist); read past L1, which does not see what other SMs wrote meanwhile
+__device__ __forceinline__ void ns_add_row(float (&v)[32], const __half* p, float f, int n) {
+  uint4 u[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) u[q] = q * 8 < n ? __ldcg(reinterpret_cast<const uint4*>(p) + q) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t w[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = unpack_half2(w[i]);
+      v[q * 8 + 2 * i] = fmaf(f, x.x, v[q * 8 + 2 * i]);
+      v[q * 8 + 2 * i + 1] = fmaf(f, x.y, v[q * 8 + 2 * i + 1]);
+    }
+  }
+}
+
+// Columns c .. c + 3 of row r of the result (v: 256 times X); n of them exist.
+__device__ __forceinline__ void ns_finish4(const NsChainArgs& a, int m, int r, int c, float4 v, int n) {
+  const NsDest& d = a.dst;
+  if (!a.vec_out || n < 4) {
+    ns_store_final(d, m, r, c, v.x * kNsUnscale);
+    if (n > 1) ns_store_final(d, m, r, c + 1, v.y * kNsUnscale);
+    if (n > 2) ns_store_final(d, m, r, c + 2, v.z * kNsUnscale);
+    if (n > 3) ns_store_final(d, m, r, c + 3, v.w * kNsUnscale);
+    return;
+  }
+  const int64_t o = (int64_t)m * d.batch + (d.tiled ? wtile_offset(d.tile, r, c) : (int64_t)r * d.row + c);
+  const float al = d.alpha * kNsUnscale;
+  float4 w = make_float4(al * v.x, al * v.y, al * v.z, al * v.w);
+  if (d.type == PRSGD_TYPE_FP32) {
+    float4* p = reinterpret_cast<float4*>(static_cast<float*>(d.out) + o);
+    if (d.beta != 0.f) {
+      const float4 old = *p;
+      w.x = fmaf(d.beta, old.x, w.x); w.y = fmaf(d.beta, old.y, w.y); w.z = fmaf(d.beta, old.z, w.z); w.w = fmaf(d.beta, old.w, w.w);
+    }
+    *p = w;
+    if (d.shadow != nullptr) {
+      const __nv_bfloat162 x = __floats2bfloat162_rn(w.x, w.y), y = __floats2bfloat162_rn(w.z, w.w);
+      *reinterpret_cast<uint2*>(d.shadow + o) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+    }
+    return;
+  }
+  uint2* p = reinterpret_cast<uint2*>(static_cast<uint16_t*>(d.out) + o);
+  const bool bf = d.type == PRSGD_TYPE_BF16;
+  if (d.beta != 0.f) {
+    uint2 u = *p;
+    const float2 x = bf ? __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&u.x)) : unpack_half2(u.x);
+    const float2 y = bf ? __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&u.y)) : unpack_half2(u.y);
+    w.x = fmaf(d.beta, x.x, w.x); w.y = fmaf(d.beta, x.y, w.y); w.z = fmaf(d.beta, y.x, w.z); w.w = fmaf(d.beta, y.y, w.w);
+  }
+  if (bf) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(w.x, w.y), y = __floats2bfloat162_rn(w.z, w.w);
+    *p = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+  } else {
+    *p = make_uint2(pack_half2(w.x, w.y), pack_half2(w.z, w.w));
+  }
+}
+
+// 32 rows x 32 columns of the result, a row per lane, through shared memory so that the lanes of a warp write
+// neighbouring columns (with rows per lane every store touches 32 lines).
+__device__ __forceinline__ void ns_finish(const NsChainArgs& a, int m, int r0, int c0, uint32_t box, int lane, const float (&v)[32]) {
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    st_shared_v4(box + (uint32_t)lane * 128u + (uint32_t)((q ^ (lane & 7)) * 16), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                 __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+  __syncwarp();
+  const int c = c0 + (lane & 7) * 4;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int rr = i * 4 + (lane >> 3);
+    const uint4 u = ld_shared_v4(box + (uint32_t)rr * 128u + (uint32_t)(((lane & 7) ^ (rr & 7)) * 16));
+    if (r0 + rr < a.sh.rows && c < a.sh.cols)
+      ns_finish4(a, m, r0 + rr, c, make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)), min(4, a.sh.cols - c));
+  }
+}
+
+// SPLIT: 32-bit precision, products of fp16 pairs.
+template <bool SPLIT>
+__global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsChainArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * kNsStages + 4 + 2 * kNsRing + kNsEpiWarps + 1];
+  __shared__ __align__(16) uint4 ring[kNsRing];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = blockIdx.x & 1u;                 // clusters of two along x
+  DeviceStatus* status = a.buf.status;
+  auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
+  auto full = [&](int s) { return bar(s); };                              // in the leader (rank 0): its stage has both CTAs' operands
+  auto empty = [&](int s) { return bar(kNsStages + s); };                 // in each: the MMAs that read the stage are done
+  auto tfull = [&](int i) { return bar(2 * kNsStages + i); };             // in each: sum i is complete
+  auto tempty = [&](int i) { return bar(2 * kNsStages + 2 + i); };        // in the leader: all epilogue warps have read sum i
+  auto sfull = [&](int i) { return bar(2 * kNsStages + 4 + i); };         // in each: ring entry i holds a task
+  auto sempty = [&](int i) { return bar(2 * kNsStages + 4 + kNsRing + i); };   // in the leader: everyone has read it
+  auto addend = [&](int w) { return bar(2 * kNsStages + 4 + 2 * kNsRing + w); };      // in each: the epilogue warp's addends have arrived
+  const uint32_t loaded = bar(2 * kNsStages + 4 + 2 * kNsRing + kNsEpiWarps);            // in the leader: all loads of a tile have been issued
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(loaded, 1);
+    for (int w = 0; w < kNsEpiWarps; ++w) ptx::mbar_init(addend(w), 1);
+    for (int s = 0; s < kNsStages; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(tfull(i), 1); ptx::mbar_init(tempty(i), 2 * kNsEpiWarps); }
+    for (int i = 0; i < kNsRing; ++i) { ptx::mbar_init(sfull(i), 1); ptx::mbar_init(sempty(i), 2 * kNsEpiWarps + 5); }
+    abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) ptx::tmem_alloc_pair(ptx::smem_u32(&tmem_slot), 512);
+  __syncthreads();
+  ptx::cluster_arrive_release();
+  ptx::cluster_wait_acquire();
+  ptx::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  if (warp == 1) ptx::tmem_relinquish_pair();
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  volatile int* ab = &abort_flag;
+
+  // the next task from the ring; kind < 0 at the end or when a wait gave up.  Whoever gets it may read what the task
+  // depends on: the scheduler saw it done (acquire) before it handed the task on (release, acquire).
+  auto next_task = [&](int n) -> NsTask {
+    const int r = n % kNsRing;
+    NsTask k;
+    k.kind = -1;
+    if (!ptx::mbar_wait_cluster(sfull(r), (uint32_t)((n / kNsRing) & 1), ab, status, NS_ERR_RING)) return k;
+    const uint4 w = ld_shared_v4(ptx::smem_u32(&ring[r]));
+    k.kind = (int)w.x; k.m = (int)w.y; k.step = (int)w.z; k.ti = (int)(w.w >> 16); k.tj = (int)(w.w & 0xffffu);
+    return k;
+  };
+  auto free_task = [&](int n) { ptx::mbar_arrive_cluster(ptx::cluster_map(sempty(n % kNsRing), 0)); };
+
+  // With 32-bit precision the epilogue's sums take registers from the other warps: 128 * 64 + 256 * 216 of the launch's 384 * 168.
+  if (warp < 4) {
+  if constexpr (SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  if ((warp == 0 || warp == 3) && lane == 0) {           // ---- operand loads: warp 0 A, warp 3 B (one thread's issue rate is not enough)
+    const bool second = warp == 3;
+    uint32_t it = 0;
+    for (int n = 0;; ++n) {
+      const NsTask k = next_task(n);
+      if (k.kind < 0) break;
+      free_task(n);
+      ptx::fence_proxy_async_all();
+      const int from = k.step & 1;
+      const int K = k.kind == 0 ? a.l : a.s;
+      const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
+      const bool mn = (k.kind == 0 && a.tall) || (second && k.kind == 2 && !a.tall);
+      const bool of_x = k.kind == 0 || (k.kind == 2 && second != (a.tall != 0));
+      const int at0 = (second ? k.tj : k.ti) * 256 + (int)rank * 128;
+      const int ask = max(0, blocks - kNsAhead);
+      bool ok = true;
+      for (int p = 0, b = 0; p < (SPLIT ? 3 : 1) && ok; ++p) {
+        const int part = SPLIT && p == (second ? 1 : 0) ? 1 : 0;       // lo hi, hi lo, hi hi: the small ones first
+        const CUtensorMap* map = of_x ? (mn ? &maps.x[from][part] : &maps.xk[from][part]) : k.kind == 1 ? &maps.A[part] : &maps.P[part];
+        for (int q = 0; q < kb; ++q, ++it, ++b) {
+          const int s = (int)(it % kNsStages);
+          if (it >= kNsStages && !ptx::mbar_wait(empty(s), ((it / kNsStages) - 1) & 1, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
+          if (rank == 0 && !second) ptx::mbar_expect_tx(full(s), 2 * kNsStageBytes);
+          const uint32_t fb = ptx::cluster_map(full(s), 0), at = stage0 + (uint32_t)s * kNsStageBytes + (second ? 16384u : 0u);
+          if (mn) {
+            ptx::tma_load_3d_pair(at, map, fb, at0, q * 64, k.m);
+            ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, q * 64, k.m);
+          } else {
+            ptx::tma_load_3d_pair(at, map, fb, q * 64, at0, k.m);
+          }
+          if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
+        }
+      }
+      if (!ok) break;
+    }
+  } else if (warp == 1 && lane == 0 && rank == 0) {      // ---- products (the leader issues for the pair) --------------
+    uint32_t it = 0, sums = 0;
+    for (int n = 0;; ++n) {
+      const NsTask k = next_task(n);
+      if (k.kind < 0) break;
+      free_task(n);
+      const int K = k.kind == 0 ? a.l : a.s;
+      const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
+      const bool a_mn = k.kind == 0 && a.tall, b_mn = (k.kind == 0 && a.tall) || (k.kind == 2 && !a.tall);
+      const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn);
+      bool ok = true;
+      int next = 0;                                      // block that starts a new sum
+      uint32_t acc = 0;
+      for (int q = 0; q < blocks; ++q, ++it) {
+        const bool first = q == next;
+        if (first) {
+          next = !SPLIT ? blocks : q < 2 * kb ? 2 * kb : q + kNsPromote;
+          acc = sums & 1u;
+          if (sums >= 2 && !ptx::mbar_wait_cluster(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
+          ptx::tc_fence_after();
+          ++sums;
+        }
+        const int s = (int)(it % kNsStages);
+        if (!ptx::mbar_wait_cluster(full(s), (it / kNsStages) & 1, ab, status, NS_ERR_FULL)) { ok = false; break; }
+        ptx::tc_fence_after();
+        const uint32_t sa = stage0 + (uint32_t)s * kNsStageBytes, sb = sa + 16384u;
+#pragma unroll
+        for (uint32_t h = 0; h < 4; ++h) {
+          const uint64_t da = a_mn ? ptx::smem_desc_sw128(sa + h * 2048u, 8192u, 1024u) : ptx::smem_desc_sw128(sa + h * 32u, 16u, 1024u);
+          const uint64_t db = b_mn ? ptx::smem_desc_sw128(sb + h * 2048u, 8192u, 1024u) : ptx::smem_desc_sw128(sb + h * 32u, 16u, 1024u);
+          ptx::mma_f16_pair(tmem + acc * 256u, da, db, idesc, !first || h != 0 ? 1u : 0u);
+        }
+        ptx::mma_commit_pair(empty(s));
+        if (q + 1 == blocks || q + 1 == next) ptx::mma_commit_pair(tfull((int)acc));
+      }
+      if (!ok) break;
+    }
+  } else if (warp == 2 && lane == 0 && rank == 0) {      // ---- claims tiles for the pair --------------------------------
+    for (int n = 0;; ++n) {
+      const int r = n % kNsRing;
+      // Not before the last loads of the tile before are being issued: a tile claimed sooner would only keep those that
+      // depend on it waiting.  (Claiming, handing on and the panels' counters take about 2 us.)
+      if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
+      if (n >= kNsRing && !ptx::mbar_wait_cluster(sempty(r), (uint32_t)(((n / kNsRing) - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
+      NsTask k;
+      k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
+      for (;;) {
+        const int t = (int)atomicAdd(a.buf.claim, 1u);
+        if (t >= a.total) break;
+        const NsTask got = ns_decode(a, t);
+        if (a.dst.active != nullptr && a.dst.active[got.m] == 0) continue;
+        k = got;
+        break;
+      }
+      if (k.kind >= 0 && k.need > 0 &&
+          !(ptx::flag_wait(a.buf.done + k.pi, (unsigned)k.need, ab, status, NS_ERR_DEP) &&
+            (k.pj == k.pi || ptx::flag_wait(a.buf.done + k.pj, (unsigned)k.need, ab, status, NS_ERR_DEP))))
+        break;
+#pragma unroll
+      for (uint32_t c = 0; c < 2; ++c) {
+        const uint32_t to = ptx::cluster_map(ptx::smem_u32(&ring[r]), c);
+        ptx::st_cluster_v4(to, make_uint4((uint32_t)k.kind, (uint32_t)k.m, (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
+        ptx::mbar_arrive_cluster(ptx::cluster_map(sfull(r), c));
+      }
+      if (k.kind < 0) break;
+    }
+  }
+  } else {                                               // ---- epilogue ---------------------------------------------
+    if constexpr (SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t boxes = stage0 + kNsStages * kNsStageBytes + (uint32_t)(warp - 4) * kNsWarpBytes;     // four of 2 KB
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+    const uint32_t added = addend(warp - 4);
+    uint32_t sums = 0, adds = 0;
+    for (int n = 0;; ++n) {
+      // lane 0 waits for the warp, so that all lanes leave together when a wait gives up
+      NsTask k;
+      if (lane == 0) k = next_task(n);
+      k.kind = __shfl_sync(0xffffffffu, k.kind, 0);
+      if (k.kind < 0) break;
+      k.m = __shfl_sync(0xffffffffu, k.m, 0); k.step = __shfl_sync(0xffffffffu, k.step, 0);
+      k.ti = __shfl_sync(0xffffffffu, k.ti, 0); k.tj = __shfl_sync(0xffffffffu, k.tj, 0);
+      const int from = k.step & 1;
+      const bool last = k.kind == 2 && k.step + 1 == a.steps, mirror = k.kind < 2 && k.ti != k.tj;
+      const int R = k.kind == 2 ? a.sh.rows : a.s, C = k.kind == 2 ? a.sh.cols : a.s;
+      const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32, c_warp = k.tj * 256 + half * 128;
+      const int units = r0 < R ? min(4, max(0, (C - c_warp + 31) / 32)) : 0;       // of 32 columns
+      // 16-bit precision: b A is added to c A^2, a X_lo to P X_hi; fetched while the product is being formed
+      const bool fetch = !SPLIT && (k.kind == 1 || (k.kind == 2 && !last)) && units > 0;
+      int ok = 1;
+      if (lane == 0) {
+        free_task(n);
+        ptx::tma_wait_group_read0();                     // (what the boxes held has been stored)
+        if (fetch) {
+          ptx::fence_proxy_async_all();
+          const CUtensorMap* map = k.kind == 1 ? &maps.As[0] : &maps.xs[from][1];
+          ptx::mbar_expect_tx(added, 2048u * (uint32_t)units);
+          for (int u = 0; u < units; ++u) ptx::tma_load_3d(boxes + (uint32_t)u * 2048u, map, added, c_warp + u * 32, r0, k.m);
+        }
+        if (!SPLIT) ok = ptx::mbar_wait_cluster(tfull((int)(sums & 1u)), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
+        if (ok && fetch) ok = ptx::mbar_wait(added, adds & 1u, ab, status, NS_ERR_ADD) ? 1 : 0;
+      }
+      if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
+      __syncwarp();
+      adds += fetch ? 1u : 0u;
+      uint32_t extra[SPLIT ? 1 : 4][16];
+      float total[SPLIT ? 128 : 1];
+      uint32_t acc = sums & 1u;
+      if constexpr (SPLIT) {                             // the partial sums of the tile, added in registers: rounded, not cut off
+        const int kb = ((k.kind == 0 ? a.l : a.s) + 63) / 64, parts = 1 + (kb + kNsPromote - 1) / kNsPromote;
+#pragma unroll
+        for (int i = 0; i < 128; ++i) total[i] = 0.f;
+        for (int p = 0; p < parts; ++p, ++sums) {
+          acc = sums & 1u;
+          if (lane == 0) ok = ptx::mbar_wait_cluster(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
+          if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
+          __syncwarp();
+          ptx::tc_fence_after();
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            uint32_t raw[32];
+            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) total[ch * 32 + i] += __uint_as_float(raw[i]);
+          }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
+        }
+        if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
+      } else {
+        ++sums;
+        ptx::tc_fence_after();
+        if (fetch) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) ns_get(boxes + (uint32_t)u * 2048u, lane, extra[u]);
+        }
+        __syncwarp();
+      }
+      const int r = r0 + lane;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float v[32];
+        if constexpr (SPLIT) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = total[u * 32 + i];
+        } else {
+          uint32_t raw[32];
+          ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 32), raw);
+          ptx::tmem_ld_wait();
+          if (u == 3) {                                  // the sum has been read: the next product may overwrite it
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+        }
+        if (u >= units) continue;
+        const int c0 = c_warp + u * 32;
+        const float f = k.kind == 1 ? kNsUnscale * a.c : kNsUnscale;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= f;
+        if (last) {
+          ns_finish(a, k.m, r0, c0, boxes + (uint32_t)(u & 1) * 4096u, lane, v);
+          continue;
+        }
+        if (k.kind == 1) {
+          if constexpr (SPLIT) {
+            if (r < R) {
+              const int64_t o = ((int64_t)k.m * a.s + r) * a.buf.sp + c0;
+              ns_add_row(v, a.buf.A[0] + o, a.b, min(32, C - c0));
+              ns_add_row(v, a.buf.A[1] + o, a.b, min(32, C - c0));
+            }
+          } else {
+            ns_add(v, extra[u], a.b);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c0 + i == r) v[i] += a.a * kNsScale;
+        } else if (k.kind == 2) {
+          if constexpr (!SPLIT) ns_add(v, extra[u], a.a);
+        }
+        // Two boxes a unit, two units in turn: hi and lo, or a symmetric matrix's tile and its transpose.
+        const uint32_t box = boxes + (uint32_t)(u & 1) * 4096u;
+        auto ready = [&]() {                             // the boxes of two units ago have been read
+          if (lane == 0) ptx::tma_wait_group_read1();
+          __syncwarp();
+        };
+        if (u >= 2 || (SPLIT && u > 0)) ready();
+        uint32_t hi[16], lo[16];
+        ns_pack(v, hi);
+        ns_put(box, lane, hi);
+        if (SPLIT || k.kind == 2) {
+          ns_pack_rest(v, hi, lo);
+          ns_put(box + 2048u, lane, lo);
+        } else if (mirror) {
+          ns_put_transposed(box + 2048u, lane, hi);
+        }
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          const CUtensorMap* to = k.kind == 0 ? maps.As : k.kind == 1 ? maps.Ps : maps.xs[1 - from];
+          ptx::tma_store_3d(&to[0], box, c0, r0, k.m);
+          if (SPLIT || k.kind == 2) ptx::tma_store_3d(&to[1], box + 2048u, c0, r0, k.m);
+          else if (mirror) ptx::tma_store_3d(k.kind == 0 ? &maps.At[0] : &maps.Pt[0], box + 2048u, r0, c0, k.m);
+          ptx::tma_commit_group();
+        }
+        if constexpr (SPLIT) {                           // the transposed pair goes through the other two boxes
+          if (mirror) {
+            const uint32_t other = boxes + (uint32_t)((u + 1) & 1) * 4096u;
+            if (u > 0) ready();
+            ns_put_transposed(other, lane, hi);
+            ns_put_transposed(other + 2048u, lane, lo);
+            ptx::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              const CUtensorMap* to = k.kind == 0 ? maps.At : maps.Pt;
+              ptx::tma_store_3d(&to[0], other, r0, c0, k.m);
+              ptx::tma_store_3d(&to[1], other + 2048u, r0, c0, k.m);
+              ptx::tma_commit_group();
+              ptx::tma_wait_group_read0();
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!last && lane == 0) {                          // count the tile once its values have been written
+        ptx::tma_wait_group0();
+        ptx::fence_proxy_async_all();
+        const int pi = k.m * a.ts + (k.kind == 2 && a.tall ? k.tj : k.ti), pj = k.m * a.ts + (k.kind == 2 && !a.tall ? k.ti : k.tj);
+        ptx::red_release_add(a.buf.done + pi, 1u);
+        if (pj != pi) ptx::red_release_add(a.buf.done + pj, 1u);
+      }
+    }
+    if (lane == 0) ptx::tma_wait_group0();               // nothing reads this CTA's shared memory after its exit
+  }
+  __syncwarp();
+  __syncthreads();
+  if (abort_flag) {                                      // copies and products may still be in flight: let them land
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) { }
+  }
+  ptx::tc_fence_before();
+  ptx::cluster_arrive_release();
+  ptx::cluster_wait_acquire();
+  if (warp == 1) ptx::tmem_dealloc_pair(tmem, 512);
+}
+
+}  // namespace prsgd

@@ -1,5 +1,7 @@
 // C entries of the Newton-Schulz orthogonalisation and of the Muon step.  See include/prsgd.h for the contract.
 #include <cmath>
+#include <mutex>
+#include "kernels_ortho_tc.cuh"
 #include "ops_internal.h"
 
 using namespace prsgd;
@@ -12,12 +14,13 @@ static NsBuffers ns_carve(const NsShape& sh, int precision, unsigned char* base,
   const bool split = precision == PRSGD_PRECISION_FP32;
   b.xp = round_up(sh.cols, 8); b.sp = round_up(s, 8);
   const int64_t per = (int64_t)sh.rows * sh.cols;
+  b.panels = (int)((s + 255) / 256);
   b.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kNsChunks, sh.rows), (per + 8191) / 8192));
   size_t off = 0;
   auto take = [&](size_t n) { unsigned char* p = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return p; };
   b.status = reinterpret_cast<DeviceStatus*>(take(sizeof(DeviceStatus)));
   b.claim = reinterpret_cast<unsigned int*>(take(4));
-  b.done = reinterpret_cast<unsigned int*>(take(4 * (size_t)sh.batch));
+  b.done = reinterpret_cast<unsigned int*>(take(4 * (size_t)sh.batch * b.panels));
   b.part = reinterpret_cast<double*>(take(8 * (size_t)sh.batch * b.chunks));
   for (int i = 0; i < 2; ++i)
     for (int j = 0; j < 2; ++j) b.x[i][j] = reinterpret_cast<__half*>(take(2 * (size_t)sh.batch * sh.rows * b.xp));
@@ -27,6 +30,45 @@ static NsBuffers ns_carve(const NsShape& sh, int precision, unsigned char* base,
   }
   *bytes = off;
   return b;
+}
+
+// fp16 [batch][d1][pitch] with d0 elements of a row in use, boxes of b0 x b1, swizzled over `swizzle` bytes; beyond the edges zeros
+static int ns_map(CUtensorMap* m, const void* base, int64_t d0, int64_t d1, int64_t batch, int64_t pitch, int b0, int b1, int swizzle) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode enc = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<Encode>(f) : nullptr;
+  }();
+  if (!enc) return op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const cuuint64_t dims[3] = {(cuuint64_t)d0, (cuuint64_t)d1, (cuuint64_t)batch};
+  const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)pitch * (cuuint64_t)d1 * 2};
+  const cuuint32_t box[3] = {(cuuint32_t)b0, (cuuint32_t)b1, 1}, one[3] = {1, 1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? PRSGD_OK : op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
+}
+
+// The current device: its SM count; its kernels' shared-memory limits are raised on the first call.
+static int ns_device(int* sms) {
+  static std::mutex lock;
+  static int known[64] = {0};
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev < 0 || dev >= 64)) return op_fail(PRSGD_ERR_ARG, "device ordinal out of range");
+  std::lock_guard<std::mutex> hold(lock);
+  if (e == cudaSuccess && known[dev] == 0) {
+    int n = 0;
+    e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_chain_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_chain_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmem);
+    if (e == cudaSuccess) known[dev] = n;
+  }
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
+  *sms = known[dev];
+  return PRSGD_OK;
 }
 
 size_t ns_workspace_bytes(const NsShape& sh, int precision) {
@@ -48,23 +90,61 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   const dim3 grid((unsigned)buf.chunks, (unsigned)p.shape.batch);
   with_type(p.g_type, [&](auto ty) {
     constexpr int TY = decltype(ty)::value;
-    if (vec) {
-      launch_pdl(ns_norm_kernel<TY, 4>, grid, dim3(256), 0, st, p.shape, p.src, buf);
-      launch_pdl(ns_pack_kernel<TY, 4>, grid, dim3(256), 0, st, p.shape, p.src, buf, p.eps);
-    } else {
-      launch_pdl(ns_norm_kernel<TY, 1>, grid, dim3(256), 0, st, p.shape, p.src, buf);
-      launch_pdl(ns_pack_kernel<TY, 1>, grid, dim3(256), 0, st, p.shape, p.src, buf, p.eps);
+    auto passes = [&](auto norm, auto pack) {
+      launch_pdl(norm, grid, dim3(256), 0, st, p.shape, p.src, buf);
+      launch_pdl(pack, grid, dim3(256), 0, st, p.shape, p.src, buf, p.eps);
+    };
+    if (p.src.V == nullptr) {
+      if (vec) passes(ns_norm_kernel<TY, 4, 0>, ns_pack_kernel<TY, 4, 0>);
+      else passes(ns_norm_kernel<TY, 1, 0>, ns_pack_kernel<TY, 1, 0>);
+    } else if (p.src.G != nullptr) {
+      if (vec) passes(ns_norm_kernel<TY, 4, 2>, ns_pack_kernel<TY, 4, 2>);
+      else passes(ns_norm_kernel<TY, 1, 2>, ns_pack_kernel<TY, 1, 2>);
+    } else {                                             // (G's type does not matter)
+      if (vec) passes(ns_norm_kernel<PRSGD_TYPE_FP32, 4, 1>, ns_pack_kernel<PRSGD_TYPE_FP32, 4, 1>);
+      else passes(ns_norm_kernel<PRSGD_TYPE_FP32, 1, 1>, ns_pack_kernel<PRSGD_TYPE_FP32, 1, 1>);
     }
   });
   if (launches) *launches += 2;
-  for (int k = 0; k < p.steps; ++k) {
-    for (int kind = 0; kind < 3; ++kind) {
-      NsGemmArgs g{p.shape, buf, p.dst, kind, k & 1, kind == 2 && k + 1 == p.steps, split ? 1 : 0, p.a, p.b, p.c};
-      const int R = kind == 2 ? p.shape.rows : s, C = kind == 2 ? p.shape.cols : s;
-      launch_pdl(ns_gemm_kernel, dim3((C + 63) / 64, (R + 63) / 64, p.shape.batch), dim3(256), 0, st, g);
-      if (launches) *launches += 1;
+  NsChainArgs a{};
+  a.sh = p.shape; a.buf = buf; a.dst = p.dst; a.steps = p.steps; a.split = split ? 1 : 0;
+  a.tall = p.shape.rows > p.shape.cols; a.s = s; a.l = std::max(p.shape.rows, p.shape.cols);
+  a.a = p.a; a.b = p.b; a.c = p.c;
+  const int ts = (s + 255) / 256;
+  a.tsym = ts * (ts + 1) / 2; a.tr = (p.shape.rows + 255) / 256; a.tc = (p.shape.cols + 255) / 256;
+  a.ts = ts; a.per_step = 2 * a.tsym + a.tr * a.tc; a.per_panel = 2 * ts + (a.tall ? a.tr : a.tc);
+  const int64_t total = (int64_t)p.shape.batch * p.steps * a.per_step;
+  if (total > 0x3fffffffll) return op_fail(PRSGD_ERR_SIZE, "orthogonalize: too many tiles in one call");
+  a.total = (int)total;
+  int sms = 0;
+  int rc = ns_device(&sms);
+  if (rc != PRSGD_OK) return rc;
+  // Groups: while the last tiles of a product of one matrix drain, at least two rounds of tiles of other matrices
+  // are to be claimed before its next product's.
+  a.group = std::min(p.shape.batch, (sms + a.tsym - 1) / a.tsym + 1);
+  const int esz = type_bytes(p.dst.type);
+  a.vec_out = (uintptr_t)p.dst.out % 16 == 0 && (p.dst.tiled || p.dst.row * esz % 16 == 0) && p.dst.batch * esz % 16 == 0;
+  NsMaps maps{};
+  const int64_t rows = p.shape.rows, cols = p.shape.cols, batch = p.shape.batch;
+  auto map_x = [&](CUtensorMap* to, const __half* p, int b0, int b1, int swizzle) { if (rc == PRSGD_OK) rc = ns_map(to, p, cols, rows, batch, buf.xp, b0, b1, swizzle); };
+  auto map_s = [&](CUtensorMap* to, const __half* p, int b0, int b1, int swizzle) { if (rc == PRSGD_OK) rc = ns_map(to, p, s, s, batch, buf.sp, b0, b1, swizzle); };
+  for (int j = 0; j < 2; ++j) {
+    for (int i = 0; i < 2; ++i) {
+      if (j == 0 || split) {                             // lo is an operand with 32-bit precision only
+        map_x(&maps.x[i][j], buf.x[i][j], 64, 64, 128);
+        map_x(&maps.xk[i][j], buf.x[i][j], 64, 128, 128);
+      }
+      map_x(&maps.xs[i][j], buf.x[i][j], 32, 32, 64);
     }
+    if (j == 1 && !split) continue;
+    map_s(&maps.A[j], buf.A[j], 64, 128, 128); map_s(&maps.As[j], buf.A[j], 32, 32, 64); map_s(&maps.At[j], buf.A[j], 32, 32, 0);
+    map_s(&maps.P[j], buf.P[j], 64, 128, 128); map_s(&maps.Ps[j], buf.P[j], 32, 32, 64); map_s(&maps.Pt[j], buf.P[j], 32, 32, 0);
   }
+  if (rc != PRSGD_OK) return rc;
+  const int pairs = (int)std::min<int64_t>(sms / 2, batch * std::max(a.tsym, a.tr * a.tc));
+  if (split) launch_pdl_cluster(ns_chain_kernel<true>, dim3(2 * pairs), dim3(kNsThreads), kNsSmem, st, 2, maps, a);
+  else launch_pdl_cluster(ns_chain_kernel<false>, dim3(2 * pairs), dim3(kNsThreads), kNsSmem, st, 2, maps, a);
+  if (launches) *launches += 1;
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
   return PRSGD_OK;
