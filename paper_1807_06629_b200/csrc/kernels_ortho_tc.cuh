@@ -134,6 +134,31 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
     }
   }
 }
+// mbar_wait by all 32 lanes of a warp, which leave it together.  ACQUIRE_CLUSTER: the barrier also hands on data that the
+// other CTA of the pair wrote.
+template <bool ACQUIRE_CLUSTER>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* status, unsigned what) {
+  long long t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (__all_sync(0xffffffffu, ACQUIRE_CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity))) return true;
+    if ((it & 63u) == 0u) {
+      bool stop = *abort_flag != 0;
+      const long long now = clock64();
+      if (t0 == 0) t0 = now;
+      if (!stop && now - t0 > kWaitLimitCycles) {
+        stop = true;
+        *abort_flag = 1;
+        if (atomicCAS(&status->error, 0u, what) == 0u) status->where = blockIdx.x;
+      }
+      if (__any_sync(0xffffffffu, stop)) return false;
+    }
+  }
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
+  return p != 0;
+}
 // fp16 operands, fp32 sum
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn_major, int b_mn_major) {
   return (1u << 4) | ((uint32_t)a_mn_major << 15) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -319,30 +344,34 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   ptx::pdl_trigger();
   volatile int* ab = &abort_flag;
 
-  // the next task from the ring; kind < 0 at the end or when a wait gave up.  Whoever gets it may read what the task
-  // depends on: the scheduler saw it done (acquire) before it handed the task on (release, acquire).
+  // The next task from the ring, for a whole warp; kind < 0 at the end or when a wait gave up.  Whoever gets it may read
+  // what the task depends on: the scheduler saw it done (acquire) before it handed the task on (release, acquire).
   auto next_task = [&](int n) -> NsTask {
     const int r = n % kNsRing;
     NsTask k;
-    k.kind = -1;
-    if (!ptx::mbar_wait_cluster(sfull(r), (uint32_t)((n / kNsRing) & 1), ab, status, NS_ERR_RING)) return k;
+    k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
+    if (!ptx::warp_wait<true>(sfull(r), (uint32_t)((n / kNsRing) & 1), ab, status, NS_ERR_RING)) return k;
     const uint4 w = ld_shared_v4(ptx::smem_u32(&ring[r]));
-    k.kind = (int)w.x; k.m = (int)w.y; k.step = (int)w.z; k.ti = (int)(w.w >> 16); k.tj = (int)(w.w & 0xffffu);
+    k.kind = __shfl_sync(0xffffffffu, (int)w.x, 0); k.m = __shfl_sync(0xffffffffu, (int)w.y, 0); k.step = __shfl_sync(0xffffffffu, (int)w.z, 0);
+    const uint32_t t = __shfl_sync(0xffffffffu, w.w, 0);
+    k.ti = (int)(t >> 16); k.tj = (int)(t & 0xffffu);
     return k;
   };
   auto free_task = [&](int n) { ptx::mbar_arrive_cluster(ptx::cluster_map(sempty(n % kNsRing), 0)); };
 
+  // The load and product roles are walked by whole warps with one elected lane that issues: in a branch of a single
+  // lane the compiler cannot keep descriptors and addresses in uniform registers, and the instructions between two
+  // MMAs then take longer than an MMA (720 cycles instead of 512 per block of 64 measured).
   // With 32-bit precision the epilogue's sums take registers from the other warps: 128 * 64 + 256 * 216 of the launch's 384 * 168.
   if (warp < 4) {
   if constexpr (SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-  if ((warp == 0 || warp == 3) && lane == 0) {           // ---- operand loads: warp 0 A, warp 3 B (one thread's issue rate is not enough)
-    const bool second = warp == 3;
-    uint32_t it = 0;
+  if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
+    const bool second = warp == 3, issue = ptx::elect_one();
+    uint32_t s = 0, phase = 1;                           // (a fresh barrier passes a wait for the phase before its first)
     for (int n = 0;; ++n) {
       const NsTask k = next_task(n);
       if (k.kind < 0) break;
-      free_task(n);
-      ptx::fence_proxy_async_all();
+      if (issue) { free_task(n); ptx::fence_proxy_async_all(); }
       const int from = k.step & 1;
       const int K = k.kind == 0 ? a.l : a.s;
       const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
@@ -354,56 +383,64 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       for (int p = 0, b = 0; p < (SPLIT ? 3 : 1) && ok; ++p) {
         const int part = SPLIT && p == (second ? 1 : 0) ? 1 : 0;       // lo hi, hi lo, hi hi: the small ones first
         const CUtensorMap* map = of_x ? (mn ? &maps.x[from][part] : &maps.xk[from][part]) : k.kind == 1 ? &maps.A[part] : &maps.P[part];
-        for (int q = 0; q < kb; ++q, ++it, ++b) {
-          const int s = (int)(it % kNsStages);
-          if (it >= kNsStages && !ptx::mbar_wait(empty(s), ((it / kNsStages) - 1) & 1, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
-          if (rank == 0 && !second) ptx::mbar_expect_tx(full(s), 2 * kNsStageBytes);
-          const uint32_t fb = ptx::cluster_map(full(s), 0), at = stage0 + (uint32_t)s * kNsStageBytes + (second ? 16384u : 0u);
-          if (mn) {
-            ptx::tma_load_3d_pair(at, map, fb, at0, q * 64, k.m);
-            ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, q * 64, k.m);
-          } else {
-            ptx::tma_load_3d_pair(at, map, fb, q * 64, at0, k.m);
+        for (int q = 0; q < kb; ++q, ++b) {
+          if (!ptx::warp_wait<false>(empty((int)s), phase, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
+          if (issue) {
+            if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kNsStageBytes);
+            const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kNsStageBytes + (second ? 16384u : 0u);
+            if (mn) {
+              ptx::tma_load_3d_pair(at, map, fb, at0, q * 64, k.m);
+              ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, q * 64, k.m);
+            } else {
+              ptx::tma_load_3d_pair(at, map, fb, q * 64, at0, k.m);
+            }
+            if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
           }
-          if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
+          __syncwarp();
+          if (++s == kNsStages) { s = 0; phase ^= 1u; }
         }
       }
       if (!ok) break;
     }
-  } else if (warp == 1 && lane == 0 && rank == 0) {      // ---- products (the leader issues for the pair) --------------
-    uint32_t it = 0, sums = 0;
+  } else if (warp == 1 && rank == 0) {                   // ---- products (the leader issues for the pair) --------------
+    const bool issue = ptx::elect_one();
+    uint32_t s = 0, phase = 0, sums = 0;
     for (int n = 0;; ++n) {
       const NsTask k = next_task(n);
       if (k.kind < 0) break;
-      free_task(n);
+      if (issue) free_task(n);
       const int K = k.kind == 0 ? a.l : a.s;
       const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
       const bool a_mn = k.kind == 0 && a.tall, b_mn = (k.kind == 0 && a.tall) || (k.kind == 2 && !a.tall);
       const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn);
+      // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
+      const uint64_t da0 = a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u);
+      const uint64_t db0 = b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u);
+      const uint64_t da_k = a_mn ? 128u : 2u, db_k = b_mn ? 128u : 2u;
       bool ok = true;
       int next = 0;                                      // block that starts a new sum
       uint32_t acc = 0;
-      for (int q = 0; q < blocks; ++q, ++it) {
+      for (int q = 0; q < blocks; ++q) {
         const bool first = q == next;
         if (first) {
           next = !SPLIT ? blocks : q < 2 * kb ? 2 * kb : q + kNsPromote;
           acc = sums & 1u;
-          if (sums >= 2 && !ptx::mbar_wait_cluster(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
+          if (sums >= 2 && !ptx::warp_wait<false>(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
           ptx::tc_fence_after();
           ++sums;
         }
-        const int s = (int)(it % kNsStages);
-        if (!ptx::mbar_wait_cluster(full(s), (it / kNsStages) & 1, ab, status, NS_ERR_FULL)) { ok = false; break; }
+        if (!ptx::warp_wait<false>(full((int)s), phase, ab, status, NS_ERR_FULL)) { ok = false; break; }
         ptx::tc_fence_after();
-        const uint32_t sa = stage0 + (uint32_t)s * kNsStageBytes, sb = sa + 16384u;
+        if (issue) {
+          const uint64_t da = da0 + s * (kNsStageBytes >> 4), db = db0 + s * (kNsStageBytes >> 4);
 #pragma unroll
-        for (uint32_t h = 0; h < 4; ++h) {
-          const uint64_t da = a_mn ? ptx::smem_desc_sw128(sa + h * 2048u, 8192u, 1024u) : ptx::smem_desc_sw128(sa + h * 32u, 16u, 1024u);
-          const uint64_t db = b_mn ? ptx::smem_desc_sw128(sb + h * 2048u, 8192u, 1024u) : ptx::smem_desc_sw128(sb + h * 32u, 16u, 1024u);
-          ptx::mma_f16_pair(tmem + acc * 256u, da, db, idesc, !first || h != 0 ? 1u : 0u);
+          for (uint32_t h = 0; h < 4; ++h)
+            ptx::mma_f16_pair(tmem + acc * 256u, da + h * da_k, db + h * db_k, idesc, !first || h != 0 ? 1u : 0u);
+          ptx::mma_commit_pair(empty((int)s));
+          if (q + 1 == blocks || q + 1 == next) ptx::mma_commit_pair(tfull((int)acc));
         }
-        ptx::mma_commit_pair(empty(s));
-        if (q + 1 == blocks || q + 1 == next) ptx::mma_commit_pair(tfull((int)acc));
+        __syncwarp();
+        if (++s == kNsStages) { s = 0; phase ^= 1u; }
       }
       if (!ok) break;
     }
@@ -445,13 +482,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
     const uint32_t added = addend(warp - 4);
     uint32_t sums = 0, adds = 0;
     for (int n = 0;; ++n) {
-      // lane 0 waits for the warp, so that all lanes leave together when a wait gives up
-      NsTask k;
-      if (lane == 0) k = next_task(n);
-      k.kind = __shfl_sync(0xffffffffu, k.kind, 0);
+      const NsTask k = next_task(n);
       if (k.kind < 0) break;
-      k.m = __shfl_sync(0xffffffffu, k.m, 0); k.step = __shfl_sync(0xffffffffu, k.step, 0);
-      k.ti = __shfl_sync(0xffffffffu, k.ti, 0); k.tj = __shfl_sync(0xffffffffu, k.tj, 0);
       const int from = k.step & 1;
       const bool last = k.kind == 2 && k.step + 1 == a.steps, mirror = k.kind < 2 && k.ti != k.tj;
       const int R = k.kind == 2 ? a.sh.rows : a.s, C = k.kind == 2 ? a.sh.cols : a.s;
@@ -459,7 +491,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       const int units = r0 < R ? min(4, max(0, (C - c_warp + 31) / 32)) : 0;       // of 32 columns
       // 16-bit precision: b A is added to c A^2, a X_lo to P X_hi; fetched while the product is being formed
       const bool fetch = !SPLIT && (k.kind == 1 || (k.kind == 2 && !last)) && units > 0;
-      int ok = 1;
+      int ok = 1;                                        // (lane 0 waits from here on, the others at the exchange of what came of it)
       if (lane == 0) {
         free_task(n);
         ptx::tma_wait_group_read0();                     // (what the boxes held has been stored)
@@ -469,7 +501,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
           ptx::mbar_expect_tx(added, 2048u * (uint32_t)units);
           for (int u = 0; u < units; ++u) ptx::tma_load_3d(boxes + (uint32_t)u * 2048u, map, added, c_warp + u * 32, r0, k.m);
         }
-        if (!SPLIT) ok = ptx::mbar_wait_cluster(tfull((int)(sums & 1u)), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
+        if (!SPLIT) ok = ptx::mbar_wait(tfull((int)(sums & 1u)), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
         if (ok && fetch) ok = ptx::mbar_wait(added, adds & 1u, ab, status, NS_ERR_ADD) ? 1 : 0;
       }
       if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
@@ -484,7 +516,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         for (int i = 0; i < 128; ++i) total[i] = 0.f;
         for (int p = 0; p < parts; ++p, ++sums) {
           acc = sums & 1u;
-          if (lane == 0) ok = ptx::mbar_wait_cluster(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
+          if (lane == 0) ok = ptx::mbar_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
           if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
           __syncwarp();
           ptx::tc_fence_after();
