@@ -25,13 +25,11 @@ constexpr uint32_t kNsStageBytes = 32768, kNsWarpBytes = 8192;      // operand s
 constexpr size_t kNsSmem = 1024 + (size_t)kNsStages * kNsStageBytes + kNsEpiWarps * kNsWarpBytes;
 constexpr int kNsAhead = 8;            // the next tile is claimed when this many blocks of 64 of the current one are left to load
 constexpr int kNsPromote = 4;          // 32-bit precision: blocks of 64 whose products are summed in TMEM before they join the sum in registers
-enum { NS_ERR_DEP = 0x701, NS_ERR_FULL, NS_ERR_EMPTY, NS_ERR_ACC, NS_ERR_ACC_FREE, NS_ERR_RING, NS_ERR_RING_FREE, NS_ERR_ADD };
+enum { NS_ERR_DEP = 0x701, NS_ERR_FULL, NS_ERR_EMPTY, NS_ERR_ACC, NS_ERR_ACC_FREE, NS_ERR_RING, NS_ERR_RING_FREE };
 
 struct NsMaps {
   CUtensorMap x[2][2];                       // operand read MN-major: [buffer][hi, lo], box {64, 64, 1}
   CUtensorMap xk[2][2], A[2], P[2];          // operands read K-major: box {64, 128, 1}
-  CUtensorMap xs[2][2], As[2], Ps[2];        // what a warp of the epilogue moves: box {32, 32, 1}, 64-byte swizzle
-  CUtensorMap At[2], Pt[2];                  // ... transposed: the same box, not swizzled
 };
 
 struct NsChainArgs {
@@ -134,6 +132,15 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
     }
   }
 }
+__device__ __forceinline__ void red_add(unsigned int* p, unsigned int v) {       // (relaxed: after a fence)
+  asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+// Hands 16 bytes to a CTA of the cluster and counts them on its barrier (which expects 16 bytes and one arrival).
+__device__ __forceinline__ void send_v4(uint32_t to_cluster, uint32_t bar_cluster, uint4 v) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 16;" ::"r"(bar_cluster) : "memory");
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(to_cluster), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(bar_cluster) : "memory");
+}
 // mbar_wait by all 32 lanes of a warp, which leave it together.  ACQUIRE_CLUSTER: the barrier also hands on data that the
 // other CTA of the pair wrote.
 template <bool ACQUIRE_CLUSTER>
@@ -154,6 +161,19 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     }
   }
 }
+// 32 lanes x 32 consecutive fp32 columns, back into TMEM
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]),
+        "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]),
+        "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]),
+        "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
@@ -176,12 +196,12 @@ __device__ __forceinline__ void ns_pack(const float (&v)[32], uint32_t (&h)[16])
 #pragma unroll
   for (int i = 0; i < 16; ++i) h[i] = pack_half2(v[2 * i], v[2 * i + 1]);
 }
-// ... and of what that rounding left
-__device__ __forceinline__ void ns_pack_rest(const float (&v)[32], const uint32_t (&h)[16], uint32_t (&l)[16]) {
+// ... and, in their place, of what that rounding left
+__device__ __forceinline__ void ns_pack_rest(const float (&v)[32], uint32_t (&h)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float2 f = unpack_half2(h[i]);
-    l[i] = pack_half2(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+    h[i] = pack_half2(v[2 * i] - f.x, v[2 * i + 1] - f.y);
   }
 }
 __device__ __forceinline__ void ns_add(float (&v)[32], const uint32_t (&h)[16], float f) {
@@ -200,10 +220,11 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t at) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-// A warp's box of 32 rows (a lane each) x 32 halves in shared memory, 64-byte swizzle: chunk c of row r sits at chunk
-// c ^ (r / 2 % 4).
-__device__ __forceinline__ uint32_t ns_chunk(uint32_t box, int lane, int q) {
-  return box + (uint32_t)lane * 64u + (uint32_t)((q ^ ((lane >> 1) & 3)) * 16);
+// A warp's box of 32 rows x 32 halves in shared memory, where values change between one row per lane (as they come from
+// TMEM) and one 16-byte chunk per lane, four lanes to a row (as they are best read and written in global memory).
+// Chunk c of row r sits at chunk c ^ (r / 2 % 4): free of bank conflicts both ways.
+__device__ __forceinline__ uint32_t ns_chunk(uint32_t box, int row, int q) {
+  return box + (uint32_t)row * 64u + (uint32_t)((q ^ ((row >> 1) & 3)) * 16);
 }
 __device__ __forceinline__ void ns_put(uint32_t box, int lane, const uint32_t (&h)[16]) {
 #pragma unroll
@@ -216,13 +237,34 @@ __device__ __forceinline__ void ns_get(uint32_t box, int lane, uint32_t (&h)[16]
     h[4 * q] = u.x; h[4 * q + 1] = u.y; h[4 * q + 2] = u.z; h[4 * q + 3] = u.w;
   }
 }
-// The same values transposed: 32 rows (the columns) of 32 halves (the lanes), not swizzled.
+// Starts copying the 32 x 32 block at p (rows `pitch` apart, a multiple of 8), of which `rows` and `cols` exist, into a
+// box (zeros beyond).  cp.async.cg reads past L1, which does not see what other SMs wrote meanwhile.
+__device__ __forceinline__ void ns_fetch(uint32_t box, const __half* p, int64_t pitch, int rows, int cols, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + (lane >> 2), c = (lane & 3) * 8;
+    const bool on = row < rows && c < cols;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ns_chunk(box, row, lane & 3)),
+                 "l"(on ? p + (int64_t)row * pitch + c : p), "r"(on ? 16 : 0) : "memory");
+  }
+}
+__device__ __forceinline__ void ns_store_box(uint32_t box, __half* p, int64_t pitch, int rows, int cols, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + (lane >> 2), c = (lane & 3) * 8;
+    const uint4 u = ld_shared_v4(ns_chunk(box, row, lane & 3));
+    if (row < rows && c < cols) *reinterpret_cast<uint4*>(p + (int64_t)row * pitch + c) = u;
+  }
+}
+// The values of ns_put transposed: value c of lane r becomes element r of row c of the box.
 __device__ __forceinline__ void ns_put_transposed(uint32_t box, int lane, const uint32_t (&h)[16]) {
+  uint32_t at[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) at[x] = box + (uint32_t)((((lane >> 3) ^ x) * 16) + (lane & 7) * 2);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const uint32_t at = box + (uint32_t)(2 * i) * 64u + (uint32_t)lane * 2u;
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((uint16_t)(h[i] & 0xffffu)) : "memory");
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 64u), "h"((uint16_t)(h[i] >> 16)) : "memory");
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at[i & 3] + (uint32_t)(2 * i) * 64u), "h"((uint16_t)(h[i] & 0xffffu)) : "memory");
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at[i & 3] + (uint32_t)(2 * i + 1) * 64u), "h"((uint16_t)(h[i] >> 16)) : "memory");
   }
 }
 // acc += f * (32 halves at p, of which n exist); read past L1, which does not see what other SMs wrote meanwhile
@@ -294,7 +336,7 @@ __device__ __forceinline__ void ns_finish(const NsChainArgs& a, int m, int r0, i
                  __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
   __syncwarp();
   const int c = c0 + (lane & 7) * 4;
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < 8; ++i) {
     const int rr = i * 4 + (lane >> 3);
     const uint4 u = ld_shared_v4(box + (uint32_t)rr * 128u + (uint32_t)(((lane & 7) ^ (rr & 7)) * 16));
@@ -307,7 +349,7 @@ __device__ __forceinline__ void ns_finish(const NsChainArgs& a, int m, int r0, i
 template <bool SPLIT>
 __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsChainArgs a) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * kNsStages + 4 + 2 * kNsRing + kNsEpiWarps + 1];
+  __shared__ __align__(8) uint64_t bars[2 * kNsStages + 4 + 2 * kNsRing + 1];
   __shared__ __align__(16) uint4 ring[kNsRing];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
@@ -322,11 +364,9 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   auto tempty = [&](int i) { return bar(2 * kNsStages + 2 + i); };        // in the leader: all epilogue warps have read sum i
   auto sfull = [&](int i) { return bar(2 * kNsStages + 4 + i); };         // in each: ring entry i holds a task
   auto sempty = [&](int i) { return bar(2 * kNsStages + 4 + kNsRing + i); };   // in the leader: everyone has read it
-  auto addend = [&](int w) { return bar(2 * kNsStages + 4 + 2 * kNsRing + w); };      // in each: the epilogue warp's addends have arrived
-  const uint32_t loaded = bar(2 * kNsStages + 4 + 2 * kNsRing + kNsEpiWarps);            // in the leader: all loads of a tile have been issued
+  const uint32_t loaded = bar(2 * kNsStages + 4 + 2 * kNsRing);            // in the leader: all loads of a tile have been issued
   if (threadIdx.x == 0) {
     ptx::mbar_init(loaded, 1);
-    for (int w = 0; w < kNsEpiWarps; ++w) ptx::mbar_init(addend(w), 1);
     for (int s = 0; s < kNsStages; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(tfull(i), 1); ptx::mbar_init(tempty(i), 2 * kNsEpiWarps); }
     for (int i = 0; i < kNsRing; ++i) { ptx::mbar_init(sfull(i), 1); ptx::mbar_init(sempty(i), 2 * kNsEpiWarps + 5); }
@@ -345,7 +385,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   volatile int* ab = &abort_flag;
 
   // The next task from the ring, for a whole warp; kind < 0 at the end or when a wait gave up.  Whoever gets it may read
-  // what the task depends on: the scheduler saw it done (acquire) before it handed the task on (release, acquire).
+  // what the task depends on: the scheduler saw it done (acquire) before it sent the task, and it is read where it was
+  // made visible, in L2 (TMA behind a proxy fence, cp.async.cg, ld.cg), never through an L1 that could hold older values.
   auto next_task = [&](int n) -> NsTask {
     const int r = n % kNsRing;
     NsTask k;
@@ -467,9 +508,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         break;
 #pragma unroll
       for (uint32_t c = 0; c < 2; ++c) {
-        const uint32_t to = ptx::cluster_map(ptx::smem_u32(&ring[r]), c);
-        ptx::st_cluster_v4(to, make_uint4((uint32_t)k.kind, (uint32_t)k.m, (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
-        ptx::mbar_arrive_cluster(ptx::cluster_map(sfull(r), c));
+        ptx::send_v4(ptx::cluster_map(ptx::smem_u32(&ring[r]), c), ptx::cluster_map(sfull(r), c),
+                     make_uint4((uint32_t)k.kind, (uint32_t)k.m, (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
       }
       if (k.kind < 0) break;
     }
@@ -479,46 +519,39 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
     const int quarter = warp & 3, half = (warp - 4) >> 2;
     const uint32_t boxes = stage0 + kNsStages * kNsStageBytes + (uint32_t)(warp - 4) * kNsWarpBytes;     // four of 2 KB
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
-    const uint32_t added = addend(warp - 4);
-    uint32_t sums = 0, adds = 0;
+    uint32_t sums = 0;
     for (int n = 0;; ++n) {
       const NsTask k = next_task(n);
       if (k.kind < 0) break;
+      if (lane == 0) free_task(n);
       const int from = k.step & 1;
       const bool last = k.kind == 2 && k.step + 1 == a.steps, mirror = k.kind < 2 && k.ti != k.tj;
       const int R = k.kind == 2 ? a.sh.rows : a.s, C = k.kind == 2 ? a.sh.cols : a.s;
-      const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32, c_warp = k.tj * 256 + half * 128;
-      const int units = r0 < R ? min(4, max(0, (C - c_warp + 31) / 32)) : 0;       // of 32 columns
-      // 16-bit precision: b A is added to c A^2, a X_lo to P X_hi; fetched while the product is being formed
-      const bool fetch = !SPLIT && (k.kind == 1 || (k.kind == 2 && !last)) && units > 0;
-      int ok = 1;                                        // (lane 0 waits from here on, the others at the exchange of what came of it)
-      if (lane == 0) {
-        free_task(n);
-        ptx::tma_wait_group_read0();                     // (what the boxes held has been stored)
-        if (fetch) {
-          ptx::fence_proxy_async_all();
-          const CUtensorMap* map = k.kind == 1 ? &maps.As[0] : &maps.xs[from][1];
-          ptx::mbar_expect_tx(added, 2048u * (uint32_t)units);
-          for (int u = 0; u < units; ++u) ptx::tma_load_3d(boxes + (uint32_t)u * 2048u, map, added, c_warp + u * 32, r0, k.m);
-        }
-        if (!SPLIT) ok = ptx::mbar_wait(tfull((int)(sums & 1u)), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
-        if (ok && fetch) ok = ptx::mbar_wait(added, adds & 1u, ab, status, NS_ERR_ADD) ? 1 : 0;
+      const int64_t pitch = k.kind == 2 ? a.buf.xp : a.buf.sp, base = (int64_t)k.m * R * pitch;
+      const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32, c_warp = k.tj * 256 + half * 128, r = r0 + lane;
+      const int rows = min(32, R - r0), units = rows > 0 ? min(4, max(0, (C - c_warp + 31) / 32)) : 0;       // of 32 columns
+      const int64_t at = base + (int64_t)r0 * pitch + c_warp;
+      // 16-bit precision: b A is added to c A^2, a X_lo to P X_hi; copied while the product is being formed
+      const bool fetch = !SPLIT && (k.kind == 1 || (k.kind == 2 && !last));
+      if (fetch) {
+        __syncwarp();                                    // (all lanes are done with the boxes)
+        const __half* p = (k.kind == 1 ? a.buf.A[0] : a.buf.x[from][1]) + at;
+#pragma unroll 1
+        for (int u = 0; u < units; ++u) ns_fetch(boxes + (uint32_t)u * 2048u, p + u * 32, pitch, rows, C - c_warp - u * 32, lane);
       }
-      if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
-      __syncwarp();
-      adds += fetch ? 1u : 0u;
-      uint32_t extra[SPLIT ? 1 : 4][16];
-      float total[SPLIT ? 128 : 1];
       uint32_t acc = sums & 1u;
-      if constexpr (SPLIT) {                             // the partial sums of the tile, added in registers: rounded, not cut off
+      bool ok = true;
+      if constexpr (SPLIT) {
+        // The partial sums of the tile are added in registers, where they are rounded, not cut off; the total goes back
+        // to TMEM, over the last of them, so that what follows is a loop of few instructions.
         const int kb = ((k.kind == 0 ? a.l : a.s) + 63) / 64, parts = 1 + (kb + kNsPromote - 1) / kNsPromote;
+        float total[4][32];
 #pragma unroll
-        for (int i = 0; i < 128; ++i) total[i] = 0.f;
+        for (int i = 0; i < 128; ++i) total[i >> 5][i & 31] = 0.f;
         for (int p = 0; p < parts; ++p, ++sums) {
           acc = sums & 1u;
-          if (lane == 0) ok = ptx::mbar_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC) ? 1 : 0;
-          if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
-          __syncwarp();
+          ok = ptx::warp_wait<false>(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC);
+          if (!ok) break;
           ptx::tc_fence_after();
 #pragma unroll
           for (int ch = 0; ch < 4; ++ch) {
@@ -526,119 +559,92 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
             ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
             ptx::tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) total[ch * 32 + i] += __uint_as_float(raw[i]);
+            for (int i = 0; i < 32; ++i) total[ch][i] += __uint_as_float(raw[i]);
           }
-          ptx::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
-        }
-        if (__shfl_sync(0xffffffffu, ok, 0) == 0) break;
-      } else {
-        ++sums;
-        ptx::tc_fence_after();
-        if (fetch) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) ns_get(boxes + (uint32_t)u * 2048u, lane, extra[u]);
-        }
-        __syncwarp();
-      }
-      const int r = r0 + lane;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float v[32];
-        if constexpr (SPLIT) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = total[u * 32 + i];
-        } else {
-          uint32_t raw[32];
-          ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 32), raw);
-          ptx::tmem_ld_wait();
-          if (u == 3) {                                  // the sum has been read: the next product may overwrite it
+          if (p + 1 < parts) {
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
           }
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
         }
-        if (u >= units) continue;
-        const int c0 = c_warp + u * 32;
-        const float f = k.kind == 1 ? kNsUnscale * a.c : kNsUnscale;
+        if (!ok) break;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= f;
+        for (int ch = 0; ch < 4; ++ch) ptx::tmem_st32(lanes + acc * 256u + (uint32_t)(ch * 32), total[ch]);
+        ptx::tmem_st_wait();
+      } else {
+        ok = ptx::warp_wait<false>(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC);
+        ++sums;
+        if (!ok) break;
+        ptx::tc_fence_after();
+        if (fetch) {
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          __syncwarp();
+        }
+      }
+      // A rolled loop, and short: code that a tile runs through once is fetched anew every time, at about 20 cycles an
+      // instruction (unrolled, this took 8 to 10 thousand cycles a tile, longer than the products of K = 1024).
+#pragma unroll 1
+      for (int u = 0; u < units; ++u) {
+        const int c0 = c_warp + u * 32, cols = C - c0;
+        const int64_t o = at + u * 32;
+        const uint32_t box = boxes + (uint32_t)u * 2048u;
+        float v[32];
+        {
+          uint32_t raw[32];
+          ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 32), raw);
+          ptx::tmem_ld_wait();
+          const float f = k.kind == 1 ? kNsUnscale * a.c : kNsUnscale;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]) * f;
+        }
         if (last) {
-          ns_finish(a, k.m, r0, c0, boxes + (uint32_t)(u & 1) * 4096u, lane, v);
+          ns_finish(a, k.m, r0, c0, boxes, lane, v);
           continue;
         }
-        if (k.kind == 1) {
-          if constexpr (SPLIT) {
-            if (r < R) {
-              const int64_t o = ((int64_t)k.m * a.s + r) * a.buf.sp + c0;
-              ns_add_row(v, a.buf.A[0] + o, a.b, min(32, C - c0));
-              ns_add_row(v, a.buf.A[1] + o, a.b, min(32, C - c0));
-            }
-          } else {
-            ns_add(v, extra[u], a.b);
+        if constexpr (SPLIT) {
+          if (k.kind == 1 && r < R) {
+#pragma unroll 1
+            for (int j = 0; j < 2; ++j) ns_add_row(v, a.buf.A[j] + o + (int64_t)lane * pitch, a.b, min(32, cols));
           }
+        } else if (fetch) {
+          uint32_t w[16];
+          ns_get(box, lane, w);                          // (a lane reads and writes its own row of the box)
+          ns_add(v, w, k.kind == 1 ? a.b : a.a);
+        }
+        if (k.kind == 1 && c0 == r0) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c0 + i == r) v[i] += a.a * kNsScale;
-        } else if (k.kind == 2) {
-          if constexpr (!SPLIT) ns_add(v, extra[u], a.a);
+          for (int i = 0; i < 32; ++i) v[i] += i == lane ? a.a * kNsScale : 0.f;
         }
-        // Two boxes a unit, two units in turn: hi and lo, or a symmetric matrix's tile and its transpose.
-        const uint32_t box = boxes + (uint32_t)(u & 1) * 4096u;
-        auto ready = [&]() {                             // the boxes of two units ago have been read
-          if (lane == 0) ptx::tma_wait_group_read1();
+        __half* to = k.kind == 0 ? a.buf.A[0] : k.kind == 1 ? a.buf.P[0] : a.buf.x[1 - from][0];
+        uint32_t h[16];
+        ns_pack(v, h);
+#pragma unroll 1
+        for (int part = 0;; ++part) {                    // hi, then lo where there is one
+          ns_put(box, lane, h);
           __syncwarp();
-        };
-        if (u >= 2 || (SPLIT && u > 0)) ready();
-        uint32_t hi[16], lo[16];
-        ns_pack(v, hi);
-        ns_put(box, lane, hi);
-        if (SPLIT || k.kind == 2) {
-          ns_pack_rest(v, hi, lo);
-          ns_put(box + 2048u, lane, lo);
-        } else if (mirror) {
-          ns_put_transposed(box + 2048u, lane, hi);
-        }
-        ptx::fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) {
-          const CUtensorMap* to = k.kind == 0 ? maps.As : k.kind == 1 ? maps.Ps : maps.xs[1 - from];
-          ptx::tma_store_3d(&to[0], box, c0, r0, k.m);
-          if (SPLIT || k.kind == 2) ptx::tma_store_3d(&to[1], box + 2048u, c0, r0, k.m);
-          else if (mirror) ptx::tma_store_3d(k.kind == 0 ? &maps.At[0] : &maps.Pt[0], box + 2048u, r0, c0, k.m);
-          ptx::tma_commit_group();
-        }
-        if constexpr (SPLIT) {                           // the transposed pair goes through the other two boxes
+          ns_store_box(box, to + o, pitch, rows, cols, lane);
           if (mirror) {
-            const uint32_t other = boxes + (uint32_t)((u + 1) & 1) * 4096u;
-            if (u > 0) ready();
-            ns_put_transposed(other, lane, hi);
-            ns_put_transposed(other + 2048u, lane, lo);
-            ptx::fence_proxy_async();
             __syncwarp();
-            if (lane == 0) {
-              const CUtensorMap* to = k.kind == 0 ? maps.At : maps.Pt;
-              ptx::tma_store_3d(&to[0], other, r0, c0, k.m);
-              ptx::tma_store_3d(&to[1], other + 2048u, r0, c0, k.m);
-              ptx::tma_commit_group();
-              ptx::tma_wait_group_read0();
-            }
+            ns_put_transposed(box, lane, h);
             __syncwarp();
+            ns_store_box(box, to + base + (int64_t)c0 * pitch + r0, pitch, cols, R - r0, lane);
           }
+          if (part == 1 || !(SPLIT || k.kind == 2)) break;
+          ns_pack_rest(v, h);
+          to = k.kind == 0 ? a.buf.A[1] : k.kind == 1 ? a.buf.P[1] : a.buf.x[1 - from][1];
+          __syncwarp();
         }
       }
-      if (!last && lane == 0) {                          // count the tile once its values have been written
-        ptx::tma_wait_group0();
-        ptx::fence_proxy_async_all();
+      ptx::tc_fence_before();                            // the sum has been read: the next product may overwrite it
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
+      if (!last && lane == 0) {                          // count the tile, everything the warp wrote before it
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
         const int pi = k.m * a.ts + (k.kind == 2 && a.tall ? k.tj : k.ti), pj = k.m * a.ts + (k.kind == 2 && !a.tall ? k.ti : k.tj);
-        ptx::red_release_add(a.buf.done + pi, 1u);
-        if (pj != pi) ptx::red_release_add(a.buf.done + pj, 1u);
+        ptx::red_add(a.buf.done + pi, 1u);
+        if (pj != pi) ptx::red_add(a.buf.done + pj, 1u);
       }
     }
-    if (lane == 0) ptx::tma_wait_group0();               // nothing reads this CTA's shared memory after its exit
   }
   __syncwarp();
   __syncthreads();

@@ -32,8 +32,8 @@ static NsBuffers ns_carve(const NsShape& sh, int precision, unsigned char* base,
   return b;
 }
 
-// fp16 [batch][d1][pitch] with d0 elements of a row in use, boxes of b0 x b1, swizzled over `swizzle` bytes; beyond the edges zeros
-static int ns_map(CUtensorMap* m, const void* base, int64_t d0, int64_t d1, int64_t batch, int64_t pitch, int b0, int b1, int swizzle) {
+// fp16 [batch][d1][pitch] with d0 elements of a row in use, boxes of 64 x box_rows, 128-byte swizzle; beyond the edges zeros
+static int ns_map(CUtensorMap* m, const void* base, int64_t d0, int64_t d1, int64_t batch, int64_t pitch, int box_rows) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static const Encode enc = [] {
@@ -45,9 +45,9 @@ static int ns_map(CUtensorMap* m, const void* base, int64_t d0, int64_t d1, int6
   if (!enc) return op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const cuuint64_t dims[3] = {(cuuint64_t)d0, (cuuint64_t)d1, (cuuint64_t)batch};
   const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)pitch * (cuuint64_t)d1 * 2};
-  const cuuint32_t box[3] = {(cuuint32_t)b0, (cuuint32_t)b1, 1}, one[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
   const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? PRSGD_OK : op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
 }
 
@@ -126,19 +126,14 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   a.vec_out = (uintptr_t)p.dst.out % 16 == 0 && (p.dst.tiled || p.dst.row * esz % 16 == 0) && p.dst.batch * esz % 16 == 0;
   NsMaps maps{};
   const int64_t rows = p.shape.rows, cols = p.shape.cols, batch = p.shape.batch;
-  auto map_x = [&](CUtensorMap* to, const __half* p, int b0, int b1, int swizzle) { if (rc == PRSGD_OK) rc = ns_map(to, p, cols, rows, batch, buf.xp, b0, b1, swizzle); };
-  auto map_s = [&](CUtensorMap* to, const __half* p, int b0, int b1, int swizzle) { if (rc == PRSGD_OK) rc = ns_map(to, p, s, s, batch, buf.sp, b0, b1, swizzle); };
-  for (int j = 0; j < 2; ++j) {
+  auto map_x = [&](CUtensorMap* to, const __half* p, int box) { if (rc == PRSGD_OK) rc = ns_map(to, p, cols, rows, batch, buf.xp, box); };
+  auto map_s = [&](CUtensorMap* to, const __half* p, int box) { if (rc == PRSGD_OK) rc = ns_map(to, p, s, s, batch, buf.sp, box); };
+  for (int j = 0; j < (split ? 2 : 1); ++j) {            // lo is an operand with 32-bit precision only
     for (int i = 0; i < 2; ++i) {
-      if (j == 0 || split) {                             // lo is an operand with 32-bit precision only
-        map_x(&maps.x[i][j], buf.x[i][j], 64, 64, 128);
-        map_x(&maps.xk[i][j], buf.x[i][j], 64, 128, 128);
-      }
-      map_x(&maps.xs[i][j], buf.x[i][j], 32, 32, 64);
+      map_x(&maps.x[i][j], buf.x[i][j], 64);
+      map_x(&maps.xk[i][j], buf.x[i][j], 128);
     }
-    if (j == 1 && !split) continue;
-    map_s(&maps.A[j], buf.A[j], 64, 128, 128); map_s(&maps.As[j], buf.A[j], 32, 32, 64); map_s(&maps.At[j], buf.A[j], 32, 32, 0);
-    map_s(&maps.P[j], buf.P[j], 64, 128, 128); map_s(&maps.Ps[j], buf.P[j], 32, 32, 64); map_s(&maps.Pt[j], buf.P[j], 32, 32, 0);
+    map_s(&maps.A[j], buf.A[j], 128); map_s(&maps.P[j], buf.P[j], 128);
   }
   if (rc != PRSGD_OK) return rc;
   const int pairs = (int)std::min<int64_t>(sms / 2, batch * std::max(a.tsym, a.tr * a.tc));
