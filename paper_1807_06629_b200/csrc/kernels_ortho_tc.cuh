@@ -3,13 +3,13 @@
 // One persistent launch runs all 3 * steps products of all matrices.  A pair of CTAs (cta_group::2) forms a 256 x 256
 // tile: each loads half of both operands (128 rows of A, 128 of B, 64 of K per stage) by TMA and keeps 128 rows of
 // the sum in its TMEM, two sums of 256 columns so that the epilogue of one tile runs beside the products of the next.
-// A and P are symmetric: only tiles on and above the diagonal are formed, the epilogue also writes their transpose.
-// Nothing is ever transposed in memory: operands whose contraction runs down the rows are read MN-major.
+// A and P are symmetric: only tiles on and above the diagonal are formed and stored, and where a product needs one below
+// it reads the stored one MN-major.  Nothing is ever transposed in memory.
 //
 // Tiles are claimed in order from a device counter (matrices in groups, within a group product by product), and a
 // tile starts when the panels it reads are counted as done: 256 rows (tall: columns) of X, A or P along the short side,
-// one counter per panel that runs through all products.  A tile of A or P reads panels ti and tj whole and adds to both
-// (its transpose); a tile of X reads one panel of P and adds to one of X.  Reading is always over before the next
+// one counter per panel that runs through all products.  A tile of A or P reads panels ti and tj whole and belongs to both
+// (as its transpose); a tile of X reads one panel of P and adds to one of X.  Reading is always over before the next
 // product writes the same place: a panel of X is done only when all tiles of P that read its panel of A are, and a
 // panel of P needs every panel of A, hence every tile of X before.  A claimed tile waits only for tiles claimed
 // earlier, so the CTAs that run always make progress, whatever share of the grid is resident; and while one matrix's
@@ -20,7 +20,8 @@
 
 namespace prsgd {
 
-constexpr int kNsStages = 5, kNsRing = 4, kNsThreads = 384, kNsEpiWarps = 8;
+constexpr int kNsStages = 5, kNsRing = 4, kNsEpiWarps = 8, kNsThreads = 32 * (4 + kNsEpiWarps);
+constexpr int kNsWarpCols = 1024 / kNsEpiWarps;       // an epilogue warp takes 32 rows of a CTA's 128 x 256 sums and this many columns
 constexpr uint32_t kNsStageBytes = 32768, kNsWarpBytes = 8192;      // operand stage of a CTA; staging of an epilogue warp
 constexpr size_t kNsSmem = 1024 + (size_t)kNsStages * kNsStageBytes + kNsEpiWarps * kNsWarpBytes;
 constexpr int kNsAhead = 8;            // the next tile is claimed when this many blocks of 64 of the current one are left to load
@@ -28,8 +29,8 @@ constexpr int kNsPromote = 4;          // 32-bit precision: blocks of 64 whose p
 enum { NS_ERR_DEP = 0x701, NS_ERR_FULL, NS_ERR_EMPTY, NS_ERR_ACC, NS_ERR_ACC_FREE, NS_ERR_RING, NS_ERR_RING_FREE };
 
 struct NsMaps {
-  CUtensorMap x[2][2];                       // operand read MN-major: [buffer][hi, lo], box {64, 64, 1}
-  CUtensorMap xk[2][2], A[2], P[2];          // operands read K-major: box {64, 128, 1}
+  CUtensorMap x[2][2], A[2], P[2];           // operands read MN-major: [buffer][hi, lo], box {64, 64, 1}
+  CUtensorMap xk[2][2], Ak[2], Pk[2];        // ... K-major: box {64, 128, 1}
 };
 
 struct NsChainArgs {
@@ -103,34 +104,10 @@ __device__ __forceinline__ void mma_f16_pair(uint32_t d_tmem, uint64_t a_desc, u
 __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
+// Arrives on a barrier of either CTA of the pair.  Relaxed: what is handed on is TMEM (ordered by tcgen05.fence) or a ring
+// entry that has been read; a release would wait for all of the thread's stores, microseconds after an epilogue.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-// mbar_wait for a barrier that the other CTA of the cluster arrives on
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* status, unsigned what) {
-  long long t0 = 0;
-  for (uint32_t it = 1;; ++it) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    if ((it & 63u) == 0u) {
-      if (*abort_flag) return false;
-      const long long now = clock64();
-      if (t0 == 0) t0 = now;
-      if (now - t0 > kWaitLimitCycles) {
-        *abort_flag = 1;
-        if (atomicCAS(&status->error, 0u, what) == 0u) status->where = blockIdx.x;
-        return false;
-      }
-    }
-  }
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
 }
 __device__ __forceinline__ void red_add(unsigned int* p, unsigned int v) {       // (relaxed: after a fence)
   asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
@@ -141,13 +118,11 @@ __device__ __forceinline__ void send_v4(uint32_t to_cluster, uint32_t bar_cluste
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
                ::"r"(to_cluster), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(bar_cluster) : "memory");
 }
-// mbar_wait by all 32 lanes of a warp, which leave it together.  ACQUIRE_CLUSTER: the barrier also hands on data that the
-// other CTA of the pair wrote.
-template <bool ACQUIRE_CLUSTER>
+// mbar_wait by all 32 lanes of a warp, which leave it together
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* status, unsigned what) {
   long long t0 = 0;
   for (uint32_t it = 1;; ++it) {
-    if (__all_sync(0xffffffffu, ACQUIRE_CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     if ((it & 63u) == 0u) {
       bool stop = *abort_flag != 0;
       const long long now = clock64();
@@ -220,67 +195,41 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t at) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-// A warp's box of 32 rows x 32 halves in shared memory, where values change between one row per lane (as they come from
-// TMEM) and one 16-byte chunk per lane, four lanes to a row (as they are best read and written in global memory).
-// Chunk c of row r sits at chunk c ^ (r / 2 % 4): free of bank conflicts both ways.
-__device__ __forceinline__ uint32_t ns_chunk(uint32_t box, int row, int q) {
-  return box + (uint32_t)row * 64u + (uint32_t)((q ^ ((row >> 1) & 3)) * 16);
-}
-__device__ __forceinline__ void ns_put(uint32_t box, int lane, const uint32_t (&h)[16]) {
+// A warp's box of 32 rows x 64 halves in shared memory, where values change between one row per lane (as they come from
+// TMEM, `half` of its columns at a time) and one 16-byte chunk per lane, eight lanes to a row: a store then touches four
+// lines of 128 bytes (with rows of 64 bytes the stores of a tile took twice as long, with a row per lane eight times).
+// Chunk c of row r sits at chunk c ^ (r % 8): free of bank conflicts both ways.
+__device__ __forceinline__ uint32_t ns_chunk(uint32_t box, int row, int q) { return box + (uint32_t)row * 128u + (uint32_t)((q ^ (row & 7)) * 16); }
+__device__ __forceinline__ void ns_put(uint32_t box, int lane, int half, const uint32_t (&h)[16]) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) st_shared_v4(ns_chunk(box, lane, q), h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+  for (int q = 0; q < 4; ++q) st_shared_v4(ns_chunk(box, lane, half * 4 + q), h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
 }
-__device__ __forceinline__ void ns_get(uint32_t box, int lane, uint32_t (&h)[16]) {
+__device__ __forceinline__ void ns_get(uint32_t box, int lane, int half, uint32_t (&h)[16]) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const uint4 u = ld_shared_v4(ns_chunk(box, lane, q));
+    const uint4 u = ld_shared_v4(ns_chunk(box, lane, half * 4 + q));
     h[4 * q] = u.x; h[4 * q + 1] = u.y; h[4 * q + 2] = u.z; h[4 * q + 3] = u.w;
   }
 }
-// Starts copying the 32 x 32 block at p (rows `pitch` apart, a multiple of 8), of which `rows` and `cols` exist, into a
-// box (zeros beyond).  cp.async.cg reads past L1, which does not see what other SMs wrote meanwhile.
-__device__ __forceinline__ void ns_fetch(uint32_t box, const __half* p, int64_t pitch, int rows, int cols, int lane) {
+// The 32 x 64 block at p (rows `pitch` apart, a multiple of 8), of which `rows` and `cols` exist: chunk lane % 8 of row
+// 4 i + lane / 8.  Read past L1, which does not see what other SMs wrote meanwhile.
+__device__ __forceinline__ void ns_fetch(const __half* p, int64_t pitch, int rows, int cols, int lane, uint4 (&u)[8]) {
+  const int row0 = lane >> 3, c = (lane & 7) * 8;
+  const __half* q = p + (int64_t)row0 * pitch + c;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 8 + (lane >> 2), c = (lane & 3) * 8;
-    const bool on = row < rows && c < cols;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ns_chunk(box, row, lane & 3)),
-                 "l"(on ? p + (int64_t)row * pitch + c : p), "r"(on ? 16 : 0) : "memory");
-  }
+  for (int i = 0; i < 8; ++i, q += 4 * pitch) u[i] = row0 + 4 * i < rows && c < cols ? __ldcg(reinterpret_cast<const uint4*>(q)) : make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void ns_put_fetched(uint32_t box, int lane, const uint4 (&u)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) st_shared_v4(ns_chunk(box, 4 * i + (lane >> 3), lane & 7), u[i].x, u[i].y, u[i].z, u[i].w);
 }
 __device__ __forceinline__ void ns_store_box(uint32_t box, __half* p, int64_t pitch, int rows, int cols, int lane) {
+  const int row0 = lane >> 3, c = (lane & 7) * 8;
+  __half* q = p + (int64_t)row0 * pitch + c;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 8 + (lane >> 2), c = (lane & 3) * 8;
-    const uint4 u = ld_shared_v4(ns_chunk(box, row, lane & 3));
-    if (row < rows && c < cols) *reinterpret_cast<uint4*>(p + (int64_t)row * pitch + c) = u;
-  }
-}
-// The values of ns_put transposed: value c of lane r becomes element r of row c of the box.
-__device__ __forceinline__ void ns_put_transposed(uint32_t box, int lane, const uint32_t (&h)[16]) {
-  uint32_t at[4];
-#pragma unroll
-  for (int x = 0; x < 4; ++x) at[x] = box + (uint32_t)((((lane >> 3) ^ x) * 16) + (lane & 7) * 2);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at[i & 3] + (uint32_t)(2 * i) * 64u), "h"((uint16_t)(h[i] & 0xffffu)) : "memory");
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at[i & 3] + (uint32_t)(2 * i + 1) * 64u), "h"((uint16_t)(h[i] >> 16)) : "memory");
-  }
-}
-// acc += f * (32 halves at p, of which n exist); read past L1, which does not see what other SMs wrote meanwhile
-__device__ __forceinline__ void ns_add_row(float (&v)[32], const __half* p, float f, int n) {
-  uint4 u[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) u[q] = q * 8 < n ? __ldcg(reinterpret_cast<const uint4*>(p) + q) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint32_t w[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 x = unpack_half2(w[i]);
-      v[q * 8 + 2 * i] = fmaf(f, x.x, v[q * 8 + 2 * i]);
-      v[q * 8 + 2 * i + 1] = fmaf(f, x.y, v[q * 8 + 2 * i + 1]);
-    }
+  for (int i = 0; i < 8; ++i, q += 4 * pitch) {
+    const uint4 u = ld_shared_v4(ns_chunk(box, row0 + 4 * i, lane & 7));
+    if (row0 + 4 * i < rows && c < cols) *reinterpret_cast<uint4*>(q) = u;
   }
 }
 
@@ -391,7 +340,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
     const int r = n % kNsRing;
     NsTask k;
     k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
-    if (!ptx::warp_wait<true>(sfull(r), (uint32_t)((n / kNsRing) & 1), ab, status, NS_ERR_RING)) return k;
+    if (!ptx::warp_wait(sfull(r), (uint32_t)((n / kNsRing) & 1), ab, status, NS_ERR_RING)) return k;
     const uint4 w = ld_shared_v4(ptx::smem_u32(&ring[r]));
     k.kind = __shfl_sync(0xffffffffu, (int)w.x, 0); k.m = __shfl_sync(0xffffffffu, (int)w.y, 0); k.step = __shfl_sync(0xffffffffu, (int)w.z, 0);
     const uint32_t t = __shfl_sync(0xffffffffu, w.w, 0);
@@ -416,24 +365,26 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       const int from = k.step & 1;
       const int K = k.kind == 0 ? a.l : a.s;
       const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
-      const bool mn = (k.kind == 0 && a.tall) || (second && k.kind == 2 && !a.tall);
       const bool of_x = k.kind == 0 || (k.kind == 2 && second != (a.tall != 0));
-      const int at0 = (second ? k.tj : k.ti) * 256 + (int)rank * 128;
+      const bool x_mn = k.kind == 0 ? a.tall != 0 : second;                      // (of X)
+      const int tile = second ? k.tj : k.ti, at0 = tile * 256 + (int)rank * 128;
       const int ask = max(0, blocks - kNsAhead);
       bool ok = true;
       for (int p = 0, b = 0; p < (SPLIT ? 3 : 1) && ok; ++p) {
         const int part = SPLIT && p == (second ? 1 : 0) ? 1 : 0;       // lo hi, hi lo, hi hi: the small ones first
-        const CUtensorMap* map = of_x ? (mn ? &maps.x[from][part] : &maps.xk[from][part]) : k.kind == 1 ? &maps.A[part] : &maps.P[part];
+        const CUtensorMap* map_mn = of_x ? &maps.x[from][part] : k.kind == 1 ? &maps.A[part] : &maps.P[part];
+        const CUtensorMap* map_k = of_x ? &maps.xk[from][part] : k.kind == 1 ? &maps.Ak[part] : &maps.Pk[part];
         for (int q = 0; q < kb; ++q, ++b) {
-          if (!ptx::warp_wait<false>(empty((int)s), phase, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
+          const bool mn = of_x ? x_mn : (q >> 2) < tile;               // (symmetric: below the diagonal the transpose is stored)
+          if (!ptx::warp_wait(empty((int)s), phase, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
           if (issue) {
             if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kNsStageBytes);
             const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kNsStageBytes + (second ? 16384u : 0u);
             if (mn) {
-              ptx::tma_load_3d_pair(at, map, fb, at0, q * 64, k.m);
-              ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, q * 64, k.m);
+              ptx::tma_load_3d_pair(at, map_mn, fb, at0, q * 64, k.m);
+              ptx::tma_load_3d_pair(at + 8192u, map_mn, fb, at0 + 64, q * 64, k.m);
             } else {
-              ptx::tma_load_3d_pair(at, map, fb, q * 64, at0, k.m);
+              ptx::tma_load_3d_pair(at, map_k, fb, q * 64, at0, k.m);
             }
             if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
           }
@@ -452,28 +403,30 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       if (issue) free_task(n);
       const int K = k.kind == 0 ? a.l : a.s;
       const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
-      const bool a_mn = k.kind == 0 && a.tall, b_mn = (k.kind == 0 && a.tall) || (k.kind == 2 && !a.tall);
-      const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn);
-      // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
-      const uint64_t da0 = a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u);
-      const uint64_t db0 = b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u);
-      const uint64_t da_k = a_mn ? 128u : 2u, db_k = b_mn ? 128u : 2u;
+      // blocks of 64 below which the operands lie MN-major
+      const int a_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && a.tall) ? 0 : 4 * k.ti;
+      const int b_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && !a.tall) ? kb : 4 * k.tj;
       bool ok = true;
       int next = 0;                                      // block that starts a new sum
       uint32_t acc = 0;
-      for (int q = 0; q < blocks; ++q) {
+      for (int q = 0, qk = 0; q < blocks; ++q) {
         const bool first = q == next;
         if (first) {
           next = !SPLIT ? blocks : q < 2 * kb ? 2 * kb : q + kNsPromote;
           acc = sums & 1u;
-          if (sums >= 2 && !ptx::warp_wait<false>(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
+          if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
           ptx::tc_fence_after();
           ++sums;
         }
-        if (!ptx::warp_wait<false>(full((int)s), phase, ab, status, NS_ERR_FULL)) { ok = false; break; }
+        if (!ptx::warp_wait(full((int)s), phase, ab, status, NS_ERR_FULL)) { ok = false; break; }
         ptx::tc_fence_after();
         if (issue) {
-          const uint64_t da = da0 + s * (kNsStageBytes >> 4), db = db0 + s * (kNsStageBytes >> 4);
+          const bool a_mn = qk < a_mn_until, b_mn = qk < b_mn_until;
+          const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn);
+          // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
+          const uint64_t at = s * (kNsStageBytes >> 4), da_k = a_mn ? 128u : 2u, db_k = b_mn ? 128u : 2u;
+          const uint64_t da = at + (a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u));
+          const uint64_t db = at + (b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u));
 #pragma unroll
           for (uint32_t h = 0; h < 4; ++h)
             ptx::mma_f16_pair(tmem + acc * 256u, da + h * da_k, db + h * db_k, idesc, !first || h != 0 ? 1u : 0u);
@@ -482,6 +435,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         }
         __syncwarp();
         if (++s == kNsStages) { s = 0; phase ^= 1u; }
+        if (++qk == kb) qk = 0;
       }
       if (!ok) break;
     }
@@ -491,7 +445,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       // Not before the last loads of the tile before are being issued: a tile claimed sooner would only keep those that
       // depend on it waiting.  (Claiming, handing on and the panels' counters take about 2 us.)
       if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
-      if (n >= kNsRing && !ptx::mbar_wait_cluster(sempty(r), (uint32_t)(((n / kNsRing) - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
+      if (n >= kNsRing && !ptx::mbar_wait(sempty(r), (uint32_t)(((n / kNsRing) - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
       NsTask k;
       k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
       for (;;) {
@@ -516,45 +470,43 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   }
   } else {                                               // ---- epilogue ---------------------------------------------
     if constexpr (SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t boxes = stage0 + kNsStages * kNsStageBytes + (uint32_t)(warp - 4) * kNsWarpBytes;     // four of 2 KB
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+    const int quarter = warp & 3, share = (warp - 4) >> 2;
+    const uint32_t box_hi = stage0 + kNsStages * kNsStageBytes + (uint32_t)(warp - 4) * kNsWarpBytes, box_lo = box_hi + 4096u;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kNsWarpCols);
     uint32_t sums = 0;
     for (int n = 0;; ++n) {
       const NsTask k = next_task(n);
       if (k.kind < 0) break;
       if (lane == 0) free_task(n);
       const int from = k.step & 1;
-      const bool last = k.kind == 2 && k.step + 1 == a.steps, mirror = k.kind < 2 && k.ti != k.tj;
+      const bool last = k.kind == 2 && k.step + 1 == a.steps;
       const int R = k.kind == 2 ? a.sh.rows : a.s, C = k.kind == 2 ? a.sh.cols : a.s;
-      const int64_t pitch = k.kind == 2 ? a.buf.xp : a.buf.sp, base = (int64_t)k.m * R * pitch;
-      const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32, c_warp = k.tj * 256 + half * 128, r = r0 + lane;
-      const int rows = min(32, R - r0), units = rows > 0 ? min(4, max(0, (C - c_warp + 31) / 32)) : 0;       // of 32 columns
-      const int64_t at = base + (int64_t)r0 * pitch + c_warp;
-      // 16-bit precision: b A is added to c A^2, a X_lo to P X_hi; copied while the product is being formed
-      const bool fetch = !SPLIT && (k.kind == 1 || (k.kind == 2 && !last));
-      if (fetch) {
-        __syncwarp();                                    // (all lanes are done with the boxes)
-        const __half* p = (k.kind == 1 ? a.buf.A[0] : a.buf.x[from][1]) + at;
-#pragma unroll 1
-        for (int u = 0; u < units; ++u) ns_fetch(boxes + (uint32_t)u * 2048u, p + u * 32, pitch, rows, C - c_warp - u * 32, lane);
-      }
+      const int64_t pitch = k.kind == 2 ? a.buf.xp : a.buf.sp;
+      const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32, c_warp = k.tj * 256 + share * kNsWarpCols;
+      const int rows = min(32, R - r0), units = rows > 0 ? min(kNsWarpCols / 64, max(0, (C - c_warp + 63) / 64)) : 0;       // of 64 columns
+      const int64_t at = (int64_t)k.m * R * pitch + (int64_t)r0 * pitch + c_warp;
+      // 16-bit precision: b A is added to c A^2, a X_lo to P X_hi; requested a unit ahead.  (32-bit: b A_hi and b A_lo.)
+      const bool fetch = k.kind == 1 || (!SPLIT && k.kind == 2 && !last);
+      const __half* const add_hi = (k.kind == 1 ? a.buf.A[0] : a.buf.x[from][1]) + at;
+      const __half* const add_lo = SPLIT ? a.buf.A[1] + at : nullptr;
+      uint4 ahead[8];
+      if (!SPLIT && fetch) ns_fetch(add_hi, pitch, rows, C - c_warp, lane, ahead);
       uint32_t acc = sums & 1u;
       bool ok = true;
       if constexpr (SPLIT) {
         // The partial sums of the tile are added in registers, where they are rounded, not cut off; the total goes back
         // to TMEM, over the last of them, so that what follows is a loop of few instructions.
         const int kb = ((k.kind == 0 ? a.l : a.s) + 63) / 64, parts = 1 + (kb + kNsPromote - 1) / kNsPromote;
-        float total[4][32];
+        float total[kNsWarpCols / 32][32];
 #pragma unroll
-        for (int i = 0; i < 128; ++i) total[i >> 5][i & 31] = 0.f;
+        for (int i = 0; i < kNsWarpCols; ++i) total[i >> 5][i & 31] = 0.f;
         for (int p = 0; p < parts; ++p, ++sums) {
           acc = sums & 1u;
-          ok = ptx::warp_wait<false>(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC);
+          ok = ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC);
           if (!ok) break;
           ptx::tc_fence_after();
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
+          for (int ch = 0; ch < kNsWarpCols / 32; ++ch) {
             uint32_t raw[32];
             ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
             ptx::tmem_ld_wait();
@@ -569,71 +521,73 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         }
         if (!ok) break;
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) ptx::tmem_st32(lanes + acc * 256u + (uint32_t)(ch * 32), total[ch]);
+        for (int ch = 0; ch < kNsWarpCols / 32; ++ch) ptx::tmem_st32(lanes + acc * 256u + (uint32_t)(ch * 32), total[ch]);
         ptx::tmem_st_wait();
       } else {
-        ok = ptx::warp_wait<false>(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC);
+        ok = ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, NS_ERR_ACC);
         ++sums;
         if (!ok) break;
         ptx::tc_fence_after();
-        if (fetch) {
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          __syncwarp();
-        }
       }
       // A rolled loop, and short: code that a tile runs through once is fetched anew every time, at about 20 cycles an
       // instruction (unrolled, this took 8 to 10 thousand cycles a tile, longer than the products of K = 1024).
 #pragma unroll 1
       for (int u = 0; u < units; ++u) {
-        const int c0 = c_warp + u * 32, cols = C - c0;
-        const int64_t o = at + u * 32;
-        const uint32_t box = boxes + (uint32_t)u * 2048u;
-        float v[32];
-        {
-          uint32_t raw[32];
-          ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 32), raw);
-          ptx::tmem_ld_wait();
-          const float f = k.kind == 1 ? kNsUnscale * a.c : kNsUnscale;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]) * f;
-        }
-        if (last) {
-          ns_finish(a, k.m, r0, c0, boxes, lane, v);
-          continue;
-        }
-        if constexpr (SPLIT) {
-          if (k.kind == 1 && r < R) {
-#pragma unroll 1
-            for (int j = 0; j < 2; ++j) ns_add_row(v, a.buf.A[j] + o + (int64_t)lane * pitch, a.b, min(32, cols));
+        const int cu = c_warp + u * 64;
+        const int64_t o = at + u * 64;
+        __syncwarp();                                    // (all lanes are done with the boxes)
+        if (fetch) {
+          if constexpr (SPLIT) {
+            ns_fetch(add_lo + u * 64, pitch, rows, C - cu, lane, ahead);
+            ns_put_fetched(box_lo, lane, ahead);
+            ns_fetch(add_hi + u * 64, pitch, rows, C - cu, lane, ahead);
+            ns_put_fetched(box_hi, lane, ahead);
+          } else {
+            ns_put_fetched(box_hi, lane, ahead);
+            if (u + 1 < units) ns_fetch(add_hi + (u + 1) * 64, pitch, rows, C - cu - 64, lane, ahead);
           }
-        } else if (fetch) {
-          uint32_t w[16];
-          ns_get(box, lane, w);                          // (a lane reads and writes its own row of the box)
-          ns_add(v, w, k.kind == 1 ? a.b : a.a);
-        }
-        if (k.kind == 1 && c0 == r0) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] += i == lane ? a.a * kNsScale : 0.f;
-        }
-        __half* to = k.kind == 0 ? a.buf.A[0] : k.kind == 1 ? a.buf.P[0] : a.buf.x[1 - from][0];
-        uint32_t h[16];
-        ns_pack(v, h);
-#pragma unroll 1
-        for (int part = 0;; ++part) {                    // hi, then lo where there is one
-          ns_put(box, lane, h);
-          __syncwarp();
-          ns_store_box(box, to + o, pitch, rows, cols, lane);
-          if (mirror) {
-            __syncwarp();
-            ns_put_transposed(box, lane, h);
-            __syncwarp();
-            ns_store_box(box, to + base + (int64_t)c0 * pitch + r0, pitch, cols, R - r0, lane);
-          }
-          if (part == 1 || !(SPLIT || k.kind == 2)) break;
-          ns_pack_rest(v, h);
-          to = k.kind == 0 ? a.buf.A[1] : k.kind == 1 ? a.buf.P[1] : a.buf.x[1 - from][1];
           __syncwarp();
         }
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const int c0 = cu + h * 32;
+          float v[32];
+          {
+            uint32_t raw[32];
+            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 64 + h * 32), raw);
+            ptx::tmem_ld_wait();
+            const float f = k.kind == 1 ? kNsUnscale * a.c : kNsUnscale;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]) * f;
+          }
+          if (last) {
+            ns_finish(a, k.m, r0, c0, h == 0 ? box_hi : box_lo, lane, v);
+            continue;
+          }
+          uint32_t w[16];                                // (a lane reads and writes its own row of the boxes)
+          if (fetch) {
+#pragma unroll 1
+            for (int j = 0; j < (SPLIT ? 2 : 1); ++j) {
+              ns_get(j == 0 ? box_hi : box_lo, lane, h, w);
+              ns_add(v, w, k.kind == 1 ? a.b : a.a);
+            }
+          }
+          if (k.kind == 1 && c0 == r0) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += i == lane ? a.a * kNsScale : 0.f;
+          }
+          ns_pack(v, w);
+          ns_put(box_hi, lane, h, w);
+          if (SPLIT || k.kind == 2) {
+            ns_pack_rest(v, w);
+            ns_put(box_lo, lane, h, w);
+          }
+        }
+        if (last) continue;
+        __syncwarp();
+        ns_store_box(box_hi, (k.kind == 0 ? a.buf.A[0] : k.kind == 1 ? a.buf.P[0] : a.buf.x[1 - from][0]) + o, pitch, rows, C - cu, lane);
+        if (SPLIT || k.kind == 2)
+          ns_store_box(box_lo, (k.kind == 0 ? a.buf.A[1] : k.kind == 1 ? a.buf.P[1] : a.buf.x[1 - from][1]) + o, pitch, rows, C - cu, lane);
       }
       ptx::tc_fence_before();                            // the sum has been read: the next product may overwrite it
       __syncwarp();

@@ -133,7 +133,8 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
       map_x(&maps.x[i][j], buf.x[i][j], 64);
       map_x(&maps.xk[i][j], buf.x[i][j], 128);
     }
-    map_s(&maps.A[j], buf.A[j], 128); map_s(&maps.P[j], buf.P[j], 128);
+    map_s(&maps.A[j], buf.A[j], 64); map_s(&maps.Ak[j], buf.A[j], 128);
+    map_s(&maps.P[j], buf.P[j], 64); map_s(&maps.Pk[j], buf.P[j], 128);
   }
   if (rc != PRSGD_OK) return rc;
   const int pairs = (int)std::min<int64_t>(sms / 2, batch * std::max(a.tsym, a.tr * a.tc));
