@@ -5,11 +5,12 @@ using namespace prsgd;
 
 namespace {
 
-int route_blocks(int64_t G, int64_t T) {
-  int64_t b = (T + 7) / 8;
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kRouteBlocks, (148 * 8 + G - 1) / G));
-  return (int)std::min<int64_t>(b, most);
+// Blocks of a group: its tokens are dealt out in turns of `per_block`, to about as many blocks as the GPU holds at a time.
+int route_blocks(int64_t G, int64_t T, int per_block) {
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kRouteBlocks, (148 * 2 + G - 1) / G));
+  return (int)std::min<int64_t>((T + per_block - 1) / per_block, most);
 }
+int lanes_per_token(int E) { return E <= 8 ? 1 : E <= 16 ? 2 : E <= 128 ? 4 : E <= 256 ? 8 : E <= 512 ? 16 : 32; }
 
 int check_route(const void* logits, int type, int64_t row_stride, int64_t group_stride, int64_t G, int64_t T, int E, int k) {
   if (!type_known(type)) return op_fail(PRSGD_ERR_ARG, "unknown element type of the logits");
@@ -33,6 +34,24 @@ template <typename F> void with_per(int E, F&& f) {
   else f(std::integral_constant<int, 32>());
 }
 
+// f(elements per lane, lanes per token): PER * L >= E
+template <typename F> void with_lanes(int E, F&& f) {
+  using std::integral_constant;
+  if (E <= 8) f(integral_constant<int, 8>(), integral_constant<int, 1>());
+  else if (E <= 16) f(integral_constant<int, 8>(), integral_constant<int, 2>());
+  else if (E <= 32) f(integral_constant<int, 8>(), integral_constant<int, 4>());
+  else if (E <= 64) f(integral_constant<int, 16>(), integral_constant<int, 4>());
+  else if (E <= 128) f(integral_constant<int, 32>(), integral_constant<int, 4>());
+  else if (E <= 256) f(integral_constant<int, 32>(), integral_constant<int, 8>());
+  else if (E <= 512) f(integral_constant<int, 32>(), integral_constant<int, 16>());
+  else f(integral_constant<int, 32>(), integral_constant<int, 32>());
+}
+
+int rows_vectorise(const void* p, int type, int64_t row_stride, int64_t group_stride, int E) {
+  const int v = 16 / type_bytes(type);
+  return (uintptr_t)p % 16 == 0 && row_stride % v == 0 && group_stride % v == 0 && E % v == 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -41,7 +60,7 @@ int prsgd_route_workspace_bytes(int64_t groups, int64_t tokens, int32_t experts,
   if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
   if (groups < 0 || tokens < 0 || experts < 1 || experts > kRouteMaxExperts)
     return op_fail(PRSGD_ERR_ARG, "need groups >= 0, tokens >= 0, experts in 1..PRSGD_ROUTE_MAX_EXPERTS");
-  const size_t slots = (size_t)groups * (size_t)std::max(1, route_blocks(std::max<int64_t>(groups, 1), tokens));
+  const size_t slots = (size_t)groups * (size_t)std::max<int64_t>(1, std::min<int64_t>(kRouteBlocks, (tokens + 7) / 8));
   *bytes = 256 + slots * ((size_t)experts * 8 + 4) + 256;
   return PRSGD_OK;
 }
@@ -62,19 +81,30 @@ int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t 
   a.logits = d_logits; a.row_stride = row_stride; a.group_stride = group_stride; a.live = d_live;
   a.G = groups; a.T = tokens; a.E = experts; a.k = top_k; a.normalize = normalize != 0; a.coef = coef;
   a.experts = d_experts; a.weights = d_weights; a.counts = d_counts; a.mean = d_mean; a.loss = d_loss;
-  a.blocks = route_blocks(groups, tokens);
+  const bool lanes = top_k <= 8;
+  a.blocks = route_blocks(groups, tokens, lanes ? 8 * 32 / lanes_per_token(experts) : 8);
+  a.vec = rows_vectorise(d_logits, type, row_stride, group_stride, experts);
   unsigned char* w = static_cast<unsigned char*>(d_work) + 256;
   a.part_p = reinterpret_cast<float*>(w);
   a.part_c = reinterpret_cast<int32_t*>(a.part_p + (size_t)groups * a.blocks * experts);
   a.part_n = a.part_c + (size_t)groups * a.blocks * experts;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (a.blocks > 0)
+  if (a.blocks > 0) {
+    const dim3 grid((unsigned)a.blocks, (unsigned)groups);
     with_type(type, [&](auto ty) {
-      with_per(experts, [&](auto per) {
-        launch_pdl(route_kernel<decltype(ty)::value, decltype(per)::value>, dim3((unsigned)a.blocks, (unsigned)groups), dim3(256), 0, st, a);
-      });
+      constexpr int TY = decltype(ty)::value;
+      if (!lanes) {
+        with_per(experts, [&](auto per) { launch_pdl(route_kernel<TY, decltype(per)::value>, grid, dim3(256), 0, st, a); });
+      } else {
+        with_lanes(experts, [&](auto per, auto l) {
+          constexpr int PER = decltype(per)::value, L = decltype(l)::value;
+          if (top_k <= 4) launch_pdl(route_lanes_kernel<TY, PER, L, 4>, grid, dim3(256), 0, st, a);
+          else launch_pdl(route_lanes_kernel<TY, PER, L, 8>, grid, dim3(256), 0, st, a);
+        });
+      }
     });
-  launch_pdl(route_finish_kernel, dim3((unsigned)groups), dim3(256), 0, st, a);
+  }
+  if (a.blocks != 1) launch_pdl(route_finish_kernel, dim3((unsigned)groups), dim3(256), 0, st, a);      // (a single block finishes itself)
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("route: ") + cudaGetErrorString(e));
   return PRSGD_OK;
@@ -96,11 +126,14 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
   a.G = groups; a.T = tokens; a.E = experts; a.k = top_k; a.normalize = normalize != 0; a.coef = coef;
   a.experts = const_cast<int32_t*>(d_experts); a.counts = const_cast<int32_t*>(d_counts);
   a.dweights = d_dweights; a.dloss = d_dloss; a.dlogits = d_dlogits; a.d_row_stride = d_row_stride; a.d_group_stride = d_group_stride;
-  const int64_t blocks = std::min<int64_t>((tokens + 7) / 8, std::max<int64_t>(1, (148 * 8 + groups - 1) / groups));
+  a.vec = rows_vectorise(d_logits, type, row_stride, group_stride, experts);
+  a.vec_out = rows_vectorise(d_dlogits, type, d_row_stride, d_group_stride, experts);
+  const int64_t per_block = 8 * 32 / lanes_per_token(experts);
+  const int64_t blocks = std::min<int64_t>((tokens + per_block - 1) / per_block, std::max<int64_t>(1, (148 * 4 + groups - 1) / groups));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   with_type(type, [&](auto ty) {
-    with_per(experts, [&](auto per) {
-      launch_pdl(route_grad_kernel<decltype(ty)::value, decltype(per)::value>, dim3((unsigned)blocks, (unsigned)groups), dim3(256), 0, st, a);
+    with_lanes(experts, [&](auto per, auto l) {
+      launch_pdl(route_grad_kernel<decltype(ty)::value, decltype(per)::value, decltype(l)::value>, dim3((unsigned)blocks, (unsigned)groups), dim3(256), 0, st, a);
     });
   });
   const cudaError_t e = cudaGetLastError();
