@@ -90,7 +90,7 @@ __device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g) {
 
 // For top_k above 8: one warp per token, a lane holds the logits lane, lane + 32, ..., and the largest is taken k times.
 template <int TY, int PER>
-__global__ void __launch_bounds__(256) route_kernel(const RouteArgs a) {
+__global__ void __launch_bounds__(256, 2) route_kernel(const RouteArgs a) {
   using T = typename ElemOf<TY>::type;
   op_pdl_wait();
   op_pdl_trigger();
@@ -197,30 +197,39 @@ __device__ __forceinline__ float route_exp2(float x) {
   return y;
 }
 
-template <int TY> struct RouteKey {                   // bf16, fp16: their 13 lowest bits as fp32 are zero
+template <int TY> struct RouteKey {                   // bf16, fp16: the 16 bits of the logit in order, then the index
   using T = uint32_t;
-  static __device__ __forceinline__ T make(float x, int e) { return (route_order(x) & ~0x1FFFu) | (uint32_t)(1023 - e); }
-  static __device__ __forceinline__ int expert(T k) { return 1023 - (int)(k & 1023u); }
-  static __device__ __forceinline__ float value(T k) { return route_value(k & ~0x1FFFu, 0x1FFFu); }
-  static __device__ __forceinline__ bool none(T k) { return (k | 0x1FFFu) <= 0x007FFFFFu; }       // -inf or no element
-  static __device__ __forceinline__ T other(T k, int o) { return __shfl_xor_sync(0xffffffffu, k, o); }
-  // fp32 bits in order, -0 = +0 and every NaN on top (the addition leaves +0 and the positive NaN)
-  static __device__ __forceinline__ uint32_t route_order(float x) {
-    const uint32_t u = __float_as_uint(x + 0.f);
-    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  using E = typename ElemOf<TY>::type;
+  static constexpr uint32_t kNegInf = TY == PRSGD_TYPE_BF16 ? 0x007Fu : 0x03FFu;      // order of -inf
+  // Keys of the two elements of a word: adding 0 leaves +0 for -0 and the positive NaN for every NaN; then all bits of a
+  // negative number are turned, of a positive one the sign.  Three of these steps run beside the pipe of the sorting.
+  static __device__ __forceinline__ void pair(uint32_t word, int e, T& lo, T& hi) {
+    uint32_t c;
+    if constexpr (TY == PRSGD_TYPE_BF16) asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(c) : "r"(word), "r"(0x3F803F80u), "r"(0u));
+    else asm("add.rn.f16x2 %0, %1, %2;" : "=r"(c) : "r"(word), "r"(0u));
+    const uint32_t order = c ^ ((((c >> 15) & 0x00010001u) * 0x7FFFu) | 0x80008000u);
+    lo = order * 65536u + (uint32_t)(1023 - e);
+    hi = (order & 0xFFFF0000u) | (uint32_t)(1022 - e);
   }
-  static __device__ __forceinline__ float route_value(uint32_t k, uint32_t low) {      // `low`: bits that were dropped
-    return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~(k | low));
+  static __device__ __forceinline__ int expert(T k) { return 1023 - (int)(k & 0xFFFFu); }
+  static __device__ __forceinline__ float value(T k) {
+    const uint16_t o = (uint16_t)(k >> 16), u = (o & 0x8000u) ? o ^ 0x8000u : ~o;
+    return to_f32(*reinterpret_cast<const E*>(&u));
   }
+  static __device__ __forceinline__ bool none(T k) { return (k >> 16) <= kNegInf; }
 };
-template <> struct RouteKey<PRSGD_TYPE_FP32> {
+template <> struct RouteKey<PRSGD_TYPE_FP32> {        // the 32 bits in order, then the index
   using T = unsigned long long;
-  using Word = RouteKey<PRSGD_TYPE_BF16>;
-  static __device__ __forceinline__ T make(float x, int e) { return ((T)Word::route_order(x) << 32) | (uint32_t)(1023 - e); }
+  static __device__ __forceinline__ T make(float x, int e) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return ((T)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (uint32_t)(1023 - e);
+  }
   static __device__ __forceinline__ int expert(T k) { return 1023 - (int)(uint32_t)k; }
-  static __device__ __forceinline__ float value(T k) { return Word::route_value((uint32_t)(k >> 32), 0u); }
+  static __device__ __forceinline__ float value(T k) {
+    const uint32_t o = (uint32_t)(k >> 32);
+    return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o);
+  }
   static __device__ __forceinline__ bool none(T k) { return (uint32_t)(k >> 32) <= 0x007FFFFFu; }
-  static __device__ __forceinline__ T other(T k, int o) { return __shfl_xor_sync(0xffffffffu, k, o); }
 };
 
 template <typename T> __device__ __forceinline__ void route_ce(T& a, T& b) {      // larger first
@@ -255,30 +264,57 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// A lane's PER logits of one row; beyond E, and of a dead token, -inf.
-template <int TY, int PER, int L>
-__device__ __forceinline__ void route_load(const typename ElemOf<TY>::type* p, int E, int sub, bool on, bool vec, float (&x)[PER]) {
+// A lane's PER logits of one row as they are stored, requested one turn ahead of their use.  Beyond E, and of a dead
+// token, they are -inf: there are always top_k real ones, and of equal keys the lower index wins, so none of those
+// beyond E is ever chosen.
+template <int TY, int PER, int L> struct RouteRow {
   using T = typename ElemOf<TY>::type;
-  constexpr int V = 16 / sizeof(T);
+  static constexpr int V = 16 / sizeof(T);
+  static constexpr uint32_t kFill = TY == PRSGD_TYPE_FP32 ? 0xFF800000u : TY == PRSGD_TYPE_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+  uint4 u[PER / V];
+  __device__ __forceinline__ void request(const T* p, int E, int sub, bool on, bool vec) {
 #pragma unroll
-  for (int i = 0; i < PER / V; ++i) {
-    const int e0 = (sub + L * i) * V;
-    if (vec) {
-      uint4 u = make_uint4(0, 0, 0, 0);
-      const bool in = on && e0 < E;                   // (E is a multiple of V here)
-      if (in) u = *reinterpret_cast<const uint4*>(p + e0);
-      const T* h = reinterpret_cast<const T*>(&u);
+    for (int i = 0; i < PER / V; ++i) {
+      const int e0 = (sub + L * i) * V;
+      u[i] = make_uint4(kFill, kFill, kFill, kFill);
+      if (vec) {
+        if (on && e0 < E) u[i] = *reinterpret_cast<const uint4*>(p + e0);      // (E is a multiple of V here)
+      } else {
+        T* h = reinterpret_cast<T*>(&u[i]);
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[i * V + j] = in ? to_f32(h[j]) : -INFINITY;
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) x[i * V + j] = on && e0 + j < E ? to_f32(p[e0 + j]) : -INFINITY;
+        for (int j = 0; j < V; ++j)
+          if (on && e0 + j < E) h[j] = p[e0 + j];
+      }
     }
   }
-}
+  __device__ __forceinline__ void take(float (&x)[PER]) const {
+#pragma unroll
+    for (int i = 0; i < PER / V; ++i) {
+      const T* h = reinterpret_cast<const T*>(&u[i]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[i * V + j] = to_f32(h[j]);
+    }
+  }
+  // element q of the lane is expert (sub + L (q / V)) V + q % V
+  template <int LS> __device__ __forceinline__ void keys(int first, int sub, typename RouteKey<TY>::T (&y)[LS]) const {
+#pragma unroll
+    for (int j = 0; j < LS; j += 2) {
+      const int q = first + j, e = (sub + L * (q / V)) * V + q % V;
+      const uint4& w = u[q / V];
+      if constexpr (TY == PRSGD_TYPE_FP32) {
+        const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+        y[j] = RouteKey<TY>::make(__uint_as_float(r[q % V]), e);
+        y[j + 1] = RouteKey<TY>::make(__uint_as_float(r[q % V + 1]), e + 1);
+      } else {
+        const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+        RouteKey<TY>::pair(r[q % V / 2], e, y[j], y[j + 1]);
+      }
+    }
+  }
+};
 
 template <int TY, int PER, int L, int LS>
-__global__ void __launch_bounds__(256) route_lanes_kernel(const RouteArgs a) {
+__global__ void __launch_bounds__(256, 2) route_lanes_kernel(const RouteArgs a) {
   using T = typename ElemOf<TY>::type;
   using Key = RouteKey<TY>;
   constexpr int V = 16 / sizeof(T), TOK = 32 / L;     // tokens of a warp at a time
@@ -298,20 +334,22 @@ __global__ void __launch_bounds__(256) route_lanes_kernel(const RouteArgs a) {
   int alive = 0;
   const T* logits = static_cast<const T*>(a.logits) + g * a.group_stride;
   const int64_t step = (int64_t)gridDim.x * 8 * TOK;
-  for (int64_t t0 = ((int64_t)blockIdx.x * 8 + warp) * TOK; t0 < a.T; t0 += step) {
+  RouteRow<TY, PER, L> next;
+  auto request = [&](int64_t t) {
+    next.request(logits + t * a.row_stride, a.E, sub, t < a.T && (a.live == nullptr || a.live[g * a.T + t] != 0), a.vec != 0);
+  };
+  const int64_t first = ((int64_t)blockIdx.x * 8 + warp) * TOK;
+  request(first + lane / L);
+  for (int64_t t0 = first; t0 < a.T; t0 += step) {
     const int64_t t = t0 + lane / L, row = g * a.T + t;
-    const bool in = t < a.T, on = in && (a.live == nullptr || a.live[row] != 0);
+    const bool in = t < a.T;
     float x[PER];
-    route_load<TY, PER, L>(logits + t * a.row_stride, a.E, sub, on, a.vec != 0, x);
+    next.take(x);
     typename Key::T l[LS];
 #pragma unroll
     for (int i = 0; i < PER / LS; ++i) {
       typename Key::T y[LS];
-#pragma unroll
-      for (int j = 0; j < LS; ++j) {
-        const int q = i * LS + j, e = (sub + L * (q / V)) * V + q % V;
-        y[j] = e < a.E ? Key::make(x[q], e) : 0;
-      }
+      next.template keys<LS>(i * LS, sub, y);
       route_sort<LS>(y);
       if (i == 0) {
 #pragma unroll
@@ -320,11 +358,12 @@ __global__ void __launch_bounds__(256) route_lanes_kernel(const RouteArgs a) {
         route_merge<LS>(l, y);
       }
     }
+    request(t + step);
 #pragma unroll
     for (int o = 1; o < L; o <<= 1) {
       typename Key::T y[LS];
 #pragma unroll
-      for (int j = 0; j < LS; ++j) y[j] = Key::other(l[j], o);
+      for (int j = 0; j < LS; ++j) y[j] = __shfl_xor_sync(0xffffffffu, l[j], o);
       route_merge<LS>(l, y);
     }
     const bool dead = Key::none(l[0]);                // a dead token, or one whose every logit is -inf
@@ -340,25 +379,32 @@ __global__ void __launch_bounds__(256) route_lanes_kernel(const RouteArgs a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) acc[i] = fmaf(x[i], inv, acc[i]);
     alive += !dead && sub == 0 ? 1 : 0;
-    // the token's entries j, j + L, ... belong to lane j of it
-    float w[(LS + L - 1) / L], chosen = 0.f;
-    int expert[(LS + L - 1) / L];
+    // lane `sub` of a token writes its entries sub * OWN, sub * OWN + 1, ...
+    constexpr int OWN = LS >= L ? LS / L : 1;
+    typename Key::T mine[OWN];
 #pragma unroll
-    for (int j = 0; j < LS; ++j) {
-      if (j % L == sub && j < a.k) {
-        const float y = route_exp2(fmaf(Key::value(l[j]), kLog2E, -top));
-        w[j / L] = y; expert[j / L] = Key::expert(l[j]);
-        chosen += y;
-      }
+    for (int i = 0; i < OWN; ++i) {
+      mine[i] = l[i];
+#pragma unroll
+      for (int q = 1; q < LS / OWN; ++q)
+        if (sub == q) mine[i] = l[q * OWN + i];
+    }
+    float w[OWN], chosen = 0.f;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      w[i] = sub * OWN + i < a.k ? route_exp2(fmaf(Key::value(mine[i]), kLog2E, -top)) : 0.f;
+      chosen += w[i];
     }
     float f = inv;
     if (a.normalize) f = 1.f / lanes_sum<L>(chosen);
 #pragma unroll
-    for (int j = 0; j < LS; ++j) {
-      if (j % L == sub && j < a.k && in) {
-        a.experts[row * a.k + j] = dead ? -1 : expert[j / L];
-        a.weights[row * a.k + j] = dead ? 0.f : w[j / L] * f;
-        if (!dead) atomicAdd(&s_c[expert[j / L]], 1);
+    for (int i = 0; i < OWN; ++i) {
+      const int j = sub * OWN + i;
+      if (j < a.k && in) {
+        const int expert = Key::expert(mine[i]);
+        a.experts[row * a.k + j] = dead ? -1 : expert;
+        a.weights[row * a.k + j] = dead ? 0.f : w[i] * f;
+        if (!dead) atomicAdd(&s_c[expert], 1);
       }
     }
   }
@@ -383,18 +429,18 @@ __global__ void __launch_bounds__(256) route_lanes_kernel(const RouteArgs a) {
   route_leave(a, g);
 }
 
-// Gradient, any top_k.  dlogit_e = p_e (h_e - dot) with h the balance loss's part, the same for all tokens of a group, and
+// Gradient, any top_k (OWN choices of a token to a lane).  dlogit_e = p_e (h_e - dot) with h the balance loss's part, the same for all tokens of a group, and
 // dot = sum_e p_e h_e + sum_j p_j dw_j over the chosen ones, whose own gradient is then p_j (h_j + dw_j - dot): the rows
 // pass through shared memory, where the lanes that own the token's choices put those in.
-template <int TY, int PER, int L>
-__global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a) {
+template <int TY, int PER, int L, int OWN>
+__global__ void __launch_bounds__(256, 2) route_grad_kernel(const RouteArgs a) {
   using T = typename ElemOf<TY>::type;
   constexpr int V = 16 / sizeof(T), TOK = 32 / L;
   op_pdl_wait();
   op_pdl_trigger();
   __shared__ float s_h[PER * L];
   __shared__ int s_w[8];
-  __shared__ __align__(16) T s_row[8][TOK][PER * L];
+  __shared__ __align__(16) T s_row[8][TOK][PER * L + 16 / sizeof(T)];      // (a chunk more: tokens side by side on other banks)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & (L - 1), tok = lane / L;
   const int64_t g = blockIdx.y;
   int total = 0;                                      // sum of the counts = k T
@@ -415,20 +461,42 @@ __global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a) {
   const T* logits = static_cast<const T*>(a.logits) + g * a.group_stride;
   T* out = static_cast<T*>(a.dlogits) + g * a.d_group_stride;
   const int64_t step = (int64_t)gridDim.x * 8 * TOK;
-  for (int64_t t0 = ((int64_t)blockIdx.x * 8 + warp) * TOK; t0 < a.T; t0 += step) {
-    const int64_t t = t0 + tok, row = g * a.T + t;
-    const bool in = t < a.T, on = in && (a.live == nullptr || a.live[row] != 0);
+  RouteRow<TY, PER, L> next;
+  int next_e[OWN];
+  float next_w[OWN];
+  auto request = [&](int64_t t) {
+    const bool on = t < a.T && (a.live == nullptr || a.live[g * a.T + t] != 0);
+    next.request(logits + t * a.row_stride, a.E, sub, on, a.vec != 0);
+#pragma unroll
+    for (int q = 0; q < OWN; ++q) {                   // choice j of the token belongs to lane j % L
+      const int j = q * L + sub;
+      const bool has = on && a.dweights != nullptr && j < a.k;
+      next_e[q] = has ? a.experts[(g * a.T + t) * a.k + j] : -1;
+      next_w[q] = has ? a.dweights[(g * a.T + t) * a.k + j] : 0.f;
+    }
+  };
+  const int64_t first = ((int64_t)blockIdx.x * 8 + warp) * TOK;
+  request(first + tok);
+  for (int64_t t0 = first; t0 < a.T; t0 += step) {
+    const int64_t t = t0 + tok;
+    const bool in = t < a.T;
     const T* p = logits + t * a.row_stride;
     float x[PER], mx = -INFINITY;
-    route_load<TY, PER, L>(p, a.E, sub, on, a.vec != 0, x);
-    bool nan = false;
+    next.take(x);
+    int ej[OWN];
+    float xj[OWN], dw[OWN];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) { mx = fmaxf(mx, x[i]); nan |= x[i] != x[i]; }
-    mx = nan ? INFINITY : mx;                         // (a NaN makes the row's probabilities NaN: inf - inf)
+    for (int q = 0; q < OWN; ++q) {
+      ej[q] = (unsigned)next_e[q] < (unsigned)a.E ? next_e[q] : -1;
+      dw[q] = ej[q] >= 0 ? next_w[q] : 0.f;
+      xj[q] = ej[q] >= 0 ? to_f32(p[ej[q]]) : -INFINITY;
+    }
+    request(t + step);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mx = fmaxf(mx, x[i]);
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const bool dead = mx == -INFINITY;
-    const float top = dead ? 0.f : mx * kLog2E;
+    const float top = mx == -INFINITY ? 0.f : mx * kLog2E;
     float sum = 0.f, dot = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -437,35 +505,26 @@ __global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a) {
       dot = fmaf(x[i], h[i], dot);
     }
     sum = lanes_sum<L>(sum);
-    if (mx == INFINITY) sum = __int_as_float(0x7fffffff);
+    const bool dead = sum == 0.f;                     // (a NaN or +inf among the logits makes the sum NaN, and the row with it)
     const float inv = dead ? 0.f : 1.f / sum;
     dot = lanes_sum<L>(dot) * inv;
-    // choice j of the token belongs to lane j % L
-    constexpr int OWN = kRouteMaxK / L;
-    float pj[OWN], dw[OWN], pick = 0.f, pull = 0.f;
-    int ej[OWN];
+    float pj[OWN];
     if (a.dweights != nullptr) {
+      float pick = 0.f, pull = 0.f;
 #pragma unroll
       for (int q = 0; q < OWN; ++q) {
-        const int j = q * L + sub;
-        ej[q] = -1; pj[q] = dw[q] = 0.f;
-        if (q * L < a.k && j < a.k && !dead) {
-          const int e = a.experts[row * a.k + j];
-          if ((unsigned)e < (unsigned)a.E) {
-            ej[q] = e; dw[q] = a.dweights[row * a.k + j];
-            pj[q] = route_exp2(fmaf(to_f32(p[e]), kLog2E, -top)) * inv;
-            pick += pj[q];
-            pull = fmaf(pj[q], dw[q], pull);
-          }
-        }
+        pj[q] = route_exp2(fmaf(xj[q], kLog2E, -top)) * inv;
+        pick += pj[q];
+        pull = fmaf(pj[q], dw[q], pull);
       }
-      if (a.normalize) {                              // w_j = p_j / S: the weights' gradient through S as well; sum_j p_j dw_j becomes 0
+      if (a.normalize) {                              // w_j = p_j / S: the weights' gradient through S as well
         const float s = lanes_sum<L>(pick), m = lanes_sum<L>(pull);
-#pragma unroll
-        for (int q = 0; q < OWN; ++q) dw[q] = ej[q] >= 0 ? (dw[q] - m / s) / s : 0.f;
         pull = 0.f;
 #pragma unroll
-        for (int q = 0; q < OWN; ++q) pull = fmaf(pj[q], dw[q], pull);
+        for (int q = 0; q < OWN; ++q) {
+          dw[q] = ej[q] >= 0 ? (dw[q] - m / s) / s : 0.f;
+          pull = fmaf(pj[q], dw[q], pull);
+        }
       }
       dot += lanes_sum<L>(pull);
     }
@@ -481,7 +540,7 @@ __global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a) {
     if (a.dweights != nullptr) {
 #pragma unroll
       for (int q = 0; q < OWN; ++q)
-        if (q * L < a.k && ej[q] >= 0) srow[ej[q]] = from_f32<T>(pj[q] * (s_h[ej[q]] + dw[q] - dot));
+        if (ej[q] >= 0) srow[ej[q]] = from_f32<T>(pj[q] * (s_h[ej[q]] + dw[q] - dot));
       __syncwarp();
     }
     if (in) {

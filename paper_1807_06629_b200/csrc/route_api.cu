@@ -5,9 +5,10 @@ using namespace prsgd;
 
 namespace {
 
-// Blocks of a group: its tokens are dealt out in turns of `per_block`, to about as many blocks as the GPU holds at a time.
+// Blocks of a group: its tokens are dealt out in turns of `per_block` to no more blocks than the GPU holds at a time (two
+// an SM by the kernels' launch bounds), so that there is no second, partly filled round of them.
 int route_blocks(int64_t G, int64_t T, int per_block) {
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kRouteBlocks, (148 * 2 + G - 1) / G));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kRouteBlocks, 148 * 2 / G));
   return (int)std::min<int64_t>((T + per_block - 1) / per_block, most);
 }
 int lanes_per_token(int E) { return E <= 8 ? 1 : E <= 16 ? 2 : E <= 128 ? 4 : E <= 256 ? 8 : E <= 512 ? 16 : 32; }
@@ -129,11 +130,14 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
   a.vec = rows_vectorise(d_logits, type, row_stride, group_stride, experts);
   a.vec_out = rows_vectorise(d_dlogits, type, d_row_stride, d_group_stride, experts);
   const int64_t per_block = 8 * 32 / lanes_per_token(experts);
-  const int64_t blocks = std::min<int64_t>((tokens + per_block - 1) / per_block, std::max<int64_t>(1, (148 * 4 + groups - 1) / groups));
+  const int64_t blocks = std::min<int64_t>((tokens + per_block - 1) / per_block, std::max<int64_t>(1, 148 * 2 / groups));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   with_type(type, [&](auto ty) {
     with_lanes(experts, [&](auto per, auto l) {
-      launch_pdl(route_grad_kernel<decltype(ty)::value, decltype(per)::value, decltype(l)::value>, dim3((unsigned)blocks, (unsigned)groups), dim3(256), 0, st, a);
+      constexpr int TY = decltype(ty)::value, PER = decltype(per)::value, L = decltype(l)::value;
+      const dim3 grid((unsigned)blocks, (unsigned)groups);
+      if (top_k <= 8) launch_pdl(route_grad_kernel<TY, PER, L, (8 + L - 1) / L>, grid, dim3(256), 0, st, a);
+      else launch_pdl(route_grad_kernel<TY, PER, L, (kRouteMaxK + L - 1) / L>, grid, dim3(256), 0, st, a);
     });
   });
   const cudaError_t e = cudaGetLastError();
