@@ -214,14 +214,18 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MUON_COEFS = (3.4445, -4.7750, 2.0315)
 
 
-def _run_on(t: torch.Tensor, stream, fn, *args) -> None:
-    """Calls fn(*args, stream) with t's device current, on `stream` or that device's current stream."""
-    d = t.device
-    if d.index == torch.cuda.current_device():
-        _check(fn(*args, (stream or torch.cuda.current_stream(d)).cuda_stream))
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _run_on(index: int, stream, fn, *args) -> None:
+    """Calls fn(*args, stream) with device `index` current, on `stream` or that device's current stream."""
+    if index == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     else:
-        with torch.cuda.device(d):
-            _check(fn(*args, (stream or torch.cuda.current_stream(d)).cuda_stream))
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    if rc != PRSGD_OK:
+        _check(rc)
 
 
 def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
@@ -234,36 +238,37 @@ def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
 
 def _matrices(t: torch.Tensor, name: str):
     """(pointer, type, row stride, batch stride) of a [batch, rows, cols] or [rows, cols] tensor."""
-    if not t.is_cuda or t.dtype not in TYPES:
+    ty = TYPES.get(t.dtype)
+    if ty is None or not t.is_cuda:
         raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor on the GPU")
-    if t.dim() == 3:
-        b, r, c = t.shape
-        sb, sr, sc = t.stride()
-    elif t.dim() == 2:
-        (r, c), (sr, sc), b, sb = t.shape, t.stride(), 1, 0
+    shape, stride = t.shape, t.stride()
+    n = len(shape)
+    if n == 3:
+        b, r, c = shape
+        sb, sr, sc = stride
+    elif n == 2:
+        (r, c), (sr, sc), b, sb = shape, stride, 1, 0
     else:
         raise ValueError(f"{name} must be [batch, rows, cols] or [rows, cols]")
     if c > 1 and sc != 1:
         raise ValueError(f"the columns of {name} must be contiguous")
     if r <= 1 and sr < c:
         sr = c
-    if b <= 1:
-        sb = 0
-    return t.data_ptr(), TYPES[t.dtype], sr, sb
+    return t.data_ptr(), ty, sr, sb if b > 1 else 0
 
 
 def _size3(t: torch.Tensor):
-    return tuple(t.shape) if t.dim() == 3 else (1, *t.shape)
+    return t.shape if t.dim() == 3 else (1, *t.shape)
 
 
 def _precision_for(t: torch.Tensor) -> int:
     """32-bit results are computed to 32-bit accuracy, 16-bit ones from single 16-bit operands."""
-    return PRECISION_FP32 if t.dtype == torch.float32 else PRECISION_BF16
+    return PRECISION_FP32 if t.dtype is torch.float32 else PRECISION_BF16
 
 
-def _same_place(name: str, t: torch.Tensor, ref: torch.Tensor) -> None:
-    if t.device != ref.device:
-        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {ref.device}")
+def _same_place(name: str, t: torch.Tensor, index: int) -> None:
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors on cuda:{index}")
 
 
 def prsgd_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, precision: int) -> int:
@@ -296,9 +301,10 @@ def prsgd_orthogonalize(G: torch.Tensor, out: Optional[torch.Tensor] = None, *, 
     p = _precision_for(out) if precision is None else precision
     if workspace is None:
         workspace = orthogonalize_workspace(G, p, stream)
-    _same_place("out", out, G)
-    _same_place("workspace", workspace, G)
-    _run_on(G, stream, lib.prsgd_orthogonalize, *_matrices(G, "G"), *_matrices(out, "out"), *_size3(G), steps,
+    index = G.get_device()
+    _same_place("out", out, index)
+    _same_place("workspace", workspace, index)
+    _run_on(index, stream, lib.prsgd_orthogonalize, *_matrices(G, "G"), *_matrices(out, "out"), *_size3(G), steps,
             _coefs(coefs), scale, eps, p, workspace.data_ptr(), workspace.numel())
     return out
 
@@ -315,16 +321,18 @@ def prsgd_muon_step(W: torch.Tensor, V: torch.Tensor, G: torch.Tensor, lr: float
     p = _precision_for(W) if precision is None else precision
     if workspace is None:
         workspace = muon_workspace(W, p, stream)
-    for name, t in (("V", V), ("G", G), ("workspace", workspace)):
-        _same_place(name, t, W)
+    index = W.get_device()
+    _same_place("V", V, index)
+    _same_place("G", G, index)
+    _same_place("workspace", workspace, index)
     v, _, vr, vb = _matrices(V, "V")
-    _run_on(W, stream, lib.prsgd_muon_step, *_matrices(W, "W"), v, vr, vb, *_matrices(G, "G"), *_size3(W), lr, mu,
+    _run_on(index, stream, lib.prsgd_muon_step, *_matrices(W, "W"), v, vr, vb, *_matrices(G, "G"), *_size3(W), lr, mu,
             1 if nesterov else 0, weight_decay, steps, _coefs(coefs), scale, eps, p, workspace.data_ptr(), workspace.numel())
 
 
 def prsgd_work_status(workspace: torch.Tensor, stream=None) -> None:
     """Raises if a kernel of the last call that used this workspace recorded an error; synchronises the stream."""
-    _run_on(workspace, stream, lib.prsgd_work_status, workspace.data_ptr())
+    _run_on(workspace.get_device(), stream, lib.prsgd_work_status, workspace.data_ptr())
 
 
 def prsgd_route_workspace_bytes(groups: int, tokens: int, experts: int) -> int:
@@ -344,12 +352,12 @@ def route_outputs(logits: torch.Tensor, k: int, stream=None):
     return tuple(_empty(shape, ty, d, stream) for shape, ty in (((G, T, k), i), ((G, T, k), f), ((G, E), i), ((G, E), f), ((G,), f)))
 
 
-def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, ref: torch.Tensor):
-    """Pointer of a contiguous tensor of `numel` elements next to `ref` (None stays None)."""
+def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, index: int):
+    """Pointer of a contiguous tensor of `numel` elements on device `index` (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != ref.device:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} elements on {ref.device}")
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} elements on cuda:{index}")
     return t.data_ptr()
 
 
@@ -363,13 +371,14 @@ def prsgd_route(logits: torch.Tensor, k: int, coef: float, *, normalize: bool = 
         out = route_outputs(logits, k, stream)
     if workspace is None:
         workspace = route_workspace(logits, stream)
-    _same_place("workspace", workspace, logits)
+    at = logits.get_device()
+    _same_place("workspace", workspace, at)
     experts, weights, counts, mean, loss = out
-    _run_on(logits, stream, lib.prsgd_route, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, logits),
-            G, T, E, k, 1 if normalize else 0, coef,
-            _dense(experts, "experts", torch.int32, G * T * k, logits), _dense(weights, "weights", torch.float32, G * T * k, logits),
-            _dense(counts, "counts", torch.int32, G * E, logits), _dense(mean, "mean", torch.float32, G * E, logits),
-            _dense(loss, "loss", torch.float32, G, logits), workspace.data_ptr(), workspace.numel())
+    i32, f32, n, m = torch.int32, torch.float32, G * T * k, G * E
+    _run_on(at, stream, lib.prsgd_route, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, at),
+            G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", i32, n, at), _dense(weights, "weights", f32, n, at),
+            _dense(counts, "counts", i32, m, at), _dense(mean, "mean", f32, m, at), _dense(loss, "loss", f32, G, at),
+            workspace.data_ptr(), workspace.numel())
     return out
 
 
@@ -384,12 +393,13 @@ def prsgd_route_grad(logits: torch.Tensor, experts: torch.Tensor, counts: torch.
         out = _empty(logits.shape, logits.dtype, logits.device, stream)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
-    _same_place("out", out, logits)
+    at = logits.get_device()
+    _same_place("out", out, at)
     optr, _, orow, ogroup = _matrices(out, "out")
-    _run_on(logits, stream, lib.prsgd_route_grad, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, logits),
-            G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", torch.int32, G * T * k, logits),
-            _dense(counts, "counts", torch.int32, G * E, logits), _dense(dweights, "dweights", torch.float32, G * T * k, logits),
-            _dense(dloss, "dloss", torch.float32, G, logits), optr, orow, ogroup)
+    i32, f32, n = torch.int32, torch.float32, G * T * k
+    _run_on(at, stream, lib.prsgd_route_grad, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, at),
+            G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", i32, n, at), _dense(counts, "counts", i32, G * E, at),
+            _dense(dweights, "dweights", f32, n, at), _dense(dloss, "dloss", f32, G, at), optr, orow, ogroup)
     return out
 
 

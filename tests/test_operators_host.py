@@ -101,7 +101,7 @@ def test_the_binding_checks_tensors(binding):
     with pytest.raises(ValueError):
         binding._matrices(x, "G")                                   # not on the GPU
     with pytest.raises(ValueError):
-        binding._dense(torch.zeros(3), "loss", torch.float32, 2, x)
+        binding._dense(torch.zeros(3), "loss", torch.float32, 2, -1)
 
 
 # ---- the references themselves ---------------------------------------------------------------------------
