@@ -1,0 +1,289 @@
+// Newton-Schulz chain of matrices whose short side is at most 128, in one launch: a cluster of CTAs per matrix holds it in
+// shared memory from its first reading to the result, so that nothing but the matrix itself is read and written.
+//
+// CTA r of the cluster keeps `w` columns (of the long side) of X as fp16 pairs.  Per step it forms its share of
+// A = X X^T on the tensor cores, the shares are summed through distributed shared memory in rank order by every CTA (all
+// get the same bits), each forms P = a I + b A + c A^2 for itself and applies it to its columns.  All products are
+// hi hi + hi lo + lo hi whatever the precision asked for: with so little work the time is that of the waits between
+// the steps, not of the products.  (16 matrices of 10 x 1024: about 150 us as three products a step of the chain's tiles.)
+#pragma once
+#include "kernels_ortho_tc.cuh"
+
+namespace prsgd {
+
+constexpr int kNsSmallThreads = 256, kNsSmallSide = 128, kNsSmallCtas = 8;
+// columns of a CTA that fit beside A and its shares: X 256 bytes a column, A 32 or 64 KB, its shares up to 16 or 64 KB
+__host__ __device__ constexpr int ns_small_cols(int s) { return s <= 64 ? 256 : 192; }
+// The whole of an SM's shared memory, whatever is needed: a second CTA on the SM would wait for the TMEM this one holds,
+// and clusters that wait for one another's TMEM would wait for good.
+constexpr size_t kNsSmallSmem = 225 * 1024;
+enum { NS_ERR_SMALL = 0x711 };
+
+struct NsSmallArgs {
+  NsShape sh; NsSource src; NsDest dst;
+  DeviceStatus* status;
+  int steps, tall, s, l, ctas, w, sp;    // w: columns of a CTA (multiple of 64), sp: short side, multiple of 16
+  float a, b, c, eps;
+  int vec_out;
+};
+
+__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared_b16(uint32_t at, __half h) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__half_as_ushort(h)) : "memory");
+}
+
+// MODE as in ns_norm_kernel.
+template <int TY, int MODE>
+__global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __grid_constant__ NsSmallArgs a) {
+  using T = typename ElemOf<TY>::type;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t bar_mma;
+  __shared__ __align__(8) double s_norm;
+  __shared__ double s_part[8];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int m = (int)blockIdx.x / a.ctas, rank = (int)blockIdx.x % a.ctas;
+  const uint32_t x_hi = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t x_bytes = (uint32_t)(a.w / 64) * 16384u, x_lo = x_hi + x_bytes;
+  const uint32_t s_hi = x_lo + x_bytes, s_bytes = (uint32_t)((a.sp + 63) / 64) * 16384u, s_lo = s_hi + s_bytes;
+  const uint32_t shares = s_lo + s_bytes;               // [sp][sp] fp32: this CTA's share of A
+  const uint32_t bar = ptx::smem_u32(&bar_mma);
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.status->error = 0u;
+  if (a.src.active != nullptr && a.src.active[m] == 0) return;       // (the whole cluster)
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(bar, 1);
+    abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512);
+  for (uint32_t o = threadIdx.x * 16u; o < 2u * (x_bytes + s_bytes); o += kNsSmallThreads * 16u) st_shared_v4(x_hi + o, 0u, 0u, 0u, 0u);
+
+  // element (i, j) of this CTA's X, i along the short side: G[i][j0 + j], or of a tall matrix G[j0 + j][i]
+  const int j0 = rank * a.w, nj = max(0, min(a.w, a.l - j0));
+  const int outer = a.tall ? nj : a.s, inner = a.tall ? a.s : nj;
+  const T* const g = static_cast<const T*>(a.src.G) + (int64_t)m * a.src.g_batch;
+  float* const v = a.src.V + (int64_t)m * a.src.v_batch;
+  // use(i, j, load(row, col)): warps along rows of G, lanes along columns, eight rows of a warp requested together
+  auto each = [&](auto&& load, auto&& use) {
+    constexpr int B = 8, W = kNsSmallThreads / 32;
+    for (int p = warp; p < outer; p += W * B)
+      for (int q = lane; q < inner; q += 32) {
+        float u[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          const int pb = p + W * b;
+          u[b] = pb < outer ? load(a.tall ? j0 + pb : pb, a.tall ? q : j0 + q) : 0.f;
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          const int pb = p + W * b;
+          if (pb < outer) use(a.tall ? q : pb, a.tall ? pb : q, u[b]);
+        }
+      }
+  };
+  auto v_at = [&](int row, int col) { return a.src.v_tiled ? wtile_offset(a.src.v_tile, row, col) : (int64_t)row * a.src.v_row + col; };
+  double sum = 0.0;
+  each([&](int row, int col) -> float {
+    if constexpr (MODE == 0) return to_f32(g[(int64_t)row * a.src.g_row + col]);
+    if constexpr (MODE == 1) return v[v_at(row, col)];
+    const float gr = to_f32(g[(int64_t)row * a.src.g_row + col]);
+    const int64_t o = v_at(row, col);
+    const float w = fmaf(a.src.mu, v[o], gr);
+    v[o] = w;
+    return a.src.nesterov ? fmaf(a.src.mu, w, gr) : w;
+  }, [&](int, int, float u) { sum += (double)u * (double)u; });
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_part[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double t = 0.0;
+    for (int i = 0; i < 8; ++i) t += s_part[i];
+    s_norm = t;
+  }
+  __syncthreads();
+  ptx::cluster_arrive_release();
+  ptx::cluster_wait_acquire();
+  double total = 0.0;
+  for (int r = 0; r < a.ctas; ++r) total += ld_cluster_f64(ptx::cluster_map(ptx::smem_u32(&s_norm), (uint32_t)r));
+  const float2 inv = ns_inverse(sqrt(total) + (double)a.eps);
+  // 16-byte chunks of 8 along a row of 128 bytes, swizzled over 8 rows; 64 columns to a block of 16 KB
+  auto at = [&](int i, int j) { return (uint32_t)(j >> 6) * 16384u + (uint32_t)i * 128u + (uint32_t)((((j & 63) >> 3) ^ (i & 7)) * 16) + (uint32_t)(j & 7) * 2u; };
+  each([&](int row, int col) -> float {
+    if constexpr (MODE == 0) return to_f32(g[(int64_t)row * a.src.g_row + col]);
+    const float w = v[v_at(row, col)];
+    if constexpr (MODE == 1) return w;
+    return a.src.nesterov ? fmaf(a.src.mu, w, to_f32(g[(int64_t)row * a.src.g_row + col])) : w;
+  }, [&](int i, int j, float u) {
+    __half hi, lo;
+    ns_split(u * inv.x * inv.y, hi, lo);
+    st_shared_b16(x_hi + at(i, j), hi);
+    st_shared_b16(x_lo + at(i, j), lo);
+  });
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = tmem_slot, d_s = tmem, d_x = tmem + 256u;      // sums of A and P, of X
+  const int quarter = warp & 3, half = warp >> 2, i = quarter * 32 + lane;
+  const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+  const bool issuer = warp == 0 && ptx::elect_one();
+  uint32_t parity = 0;
+  // products of the pairs (A hi, lo) and (B hi, lo), the small ones first, over k16 steps of 16
+  auto products = [&](uint32_t d, uint32_t n, int k16, uint32_t ah, uint32_t al, uint32_t bh, uint32_t bl, bool b_mn) {
+    ptx::fence_proxy_async();
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (warp == 0) {
+      if (issuer) {
+        const uint32_t idesc = ptx::idesc_f16(128, (int)n, 0, b_mn);
+        for (int p = 0; p < 3; ++p) {
+          const uint32_t sa = p == 0 ? al : ah, sb = p == 1 ? bl : bh;
+#pragma unroll 4
+          for (int k = 0; k < k16; ++k) {
+            const uint32_t in_block = (uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u;
+            const uint64_t da = ptx::smem_desc_sw128(sa + in_block, 16u, 1024u);
+            const uint64_t db = b_mn ? ptx::smem_desc_sw128(sb + (uint32_t)k * 2048u, 16384u, 1024u) : ptx::smem_desc_sw128(sb + in_block, 16u, 1024u);
+            ptx::mma_bf16(d, da, db, idesc, p != 0 || k != 0 ? 1u : 0u);
+          }
+        }
+        ptx::mma_commit(bar);
+      }
+      __syncwarp();
+    }
+    (void)ptx::mbar_wait(bar, parity, &abort_flag, a.status, NS_ERR_SMALL);      // (after an expiry every later wait returns at once)
+    parity ^= 1u;
+    ptx::tc_fence_after();
+  };
+  const int chunks = a.sp / 4;                             // 16-byte chunks of a row of fp32 values of A
+  auto share_at = [&](int row, int q) { return shares + (uint32_t)(row * chunks + (q ^ (row & 3))) * 16u; };
+
+#pragma unroll 1
+  for (int step = 0; step < a.steps; ++step) {
+    const bool last = step + 1 == a.steps;
+    // ---- A = X X^T: this CTA's share, then the sum of all
+    products(d_s, (uint32_t)a.sp, a.w / 16, x_hi, x_lo, x_hi, x_lo, false);
+    if (step > 0) ptx::cluster_wait_acquire();             // everyone has read the last shares
+    if (quarter * 32 < a.sp) {
+#pragma unroll 1
+      for (int c = half * 16; c < a.sp; c += 32) {
+        uint32_t r[16];
+        ptx::tmem_ld16(d_s + lanes + (uint32_t)c, r);
+        ptx::tmem_ld_wait();
+        if (i < a.sp) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) st_shared_v4(share_at(i, c / 4 + q), r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+        }
+      }
+    }
+    ptx::cluster_arrive_release();
+    ptx::cluster_wait_acquire();
+#pragma unroll 1
+    for (int idx = (int)threadIdx.x; idx < a.sp * chunks; idx += kNsSmallThreads) {
+      const int row = idx / chunks, q = idx - row * chunks;
+      const uint32_t from = share_at(row, q);
+      float4 part[kNsSmallCtas], f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int r = 0; r < kNsSmallCtas; ++r)
+        if (r < a.ctas) part[r] = ld_cluster_v4(ptx::cluster_map(from, (uint32_t)r));
+#pragma unroll
+      for (int r = 0; r < kNsSmallCtas; ++r)
+        if (r < a.ctas) { f.x += part[r].x; f.y += part[r].y; f.z += part[r].z; f.w += part[r].w; }
+      f.x *= kNsUnscale; f.y *= kNsUnscale; f.z *= kNsUnscale; f.w *= kNsUnscale;
+      const uint32_t h0 = pack_half2(f.x, f.y), h1 = pack_half2(f.z, f.w);
+      const float2 b0 = unpack_half2(h0), b1 = unpack_half2(h1);
+      const uint32_t o = at(row, q * 4);
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(s_hi + o), "r"(h0), "r"(h1) : "memory");
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(s_lo + o), "r"(pack_half2(f.x - b0.x, f.y - b0.y)), "r"(pack_half2(f.z - b1.x, f.w - b1.y)) : "memory");
+    }
+    ptx::cluster_arrive_release();                         // (waited for before the next shares are written)
+    // ---- P = a I + b A + c A^2, in the place of A
+    products(d_s, (uint32_t)a.sp, a.sp / 16, s_hi, s_lo, s_hi, s_lo, false);
+    if (quarter * 32 < a.sp) {
+#pragma unroll 1
+      for (int c = half * 16; c < a.sp; c += 32) {
+        uint32_t r[16];
+        ptx::tmem_ld16(d_s + lanes + (uint32_t)c, r);
+        ptx::tmem_ld_wait();
+        if (i < a.sp) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {                    // chunks of 8
+            const uint32_t o = at(i, c + 8 * q);
+            const uint4 h = ld_shared_v4(s_hi + o), l = ld_shared_v4(s_lo + o);
+            const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+            uint32_t ho[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 ah = unpack_half2(hw[e]), al = unpack_half2(lw[e]);
+              const int col = c + 8 * q + 2 * e;
+              float y0 = fmaf(kNsUnscale * a.c, __uint_as_float(r[8 * q + 2 * e]), a.b * ah.x) + a.b * al.x;
+              float y1 = fmaf(kNsUnscale * a.c, __uint_as_float(r[8 * q + 2 * e + 1]), a.b * ah.y) + a.b * al.y;
+              if (i < a.s) { y0 += col == i ? a.a * kNsScale : 0.f; y1 += col + 1 == i ? a.a * kNsScale : 0.f; }
+              ho[e] = pack_half2(y0, y1);
+              const float2 b = unpack_half2(ho[e]);
+              lo[e] = pack_half2(y0 - b.x, y1 - b.y);
+            }
+            st_shared_v4(s_hi + o, ho[0], ho[1], ho[2], ho[3]);
+            st_shared_v4(s_lo + o, lo[0], lo[1], lo[2], lo[3]);
+          }
+        }
+      }
+    }
+    // ---- X <- P X, in its place
+    products(d_x, (uint32_t)a.w, a.sp / 16, s_hi, s_lo, x_hi, x_lo, true);
+    if (quarter * 32 < a.s) {
+      const uint32_t box = s_hi + (uint32_t)(warp & 7) * 4096u;          // (P is not needed any more; 32 KB at least)
+#pragma unroll 1
+      for (int c = half * 32; c < a.w; c += 64) {
+        uint32_t raw[32];
+        ptx::tmem_ld32(d_x + lanes + (uint32_t)c, raw);
+        ptx::tmem_ld_wait();
+        float y[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(raw[e]) * kNsUnscale;
+        if (!last) {
+          if (i < a.s) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              uint32_t ho[4], lo[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                ho[e] = pack_half2(y[8 * q + 2 * e], y[8 * q + 2 * e + 1]);
+                const float2 b = unpack_half2(ho[e]);
+                lo[e] = pack_half2(y[8 * q + 2 * e] - b.x, y[8 * q + 2 * e + 1] - b.y);
+              }
+              const uint32_t o = at(i, c + 8 * q);
+              st_shared_v4(x_hi + o, ho[0], ho[1], ho[2], ho[3]);
+              st_shared_v4(x_lo + o, lo[0], lo[1], lo[2], lo[3]);
+            }
+          }
+        } else if (!a.tall) {
+          if (c < nj) ns_finish(a.dst, a.vec_out, m, quarter * 32, j0 + c, a.s, min(a.l, j0 + a.w), box, lane, y);
+        } else if (i < a.s) {                              // (lanes hold neighbouring columns of the result)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c + e < nj) ns_store_final(a.dst, m, j0 + c + e, i, y[e] * kNsUnscale);
+        }
+      }
+    }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_wait_acquire();                             // (no CTA leaves while its memory is read)
+  if (warp == 1) { ptx::tmem_relinquish(); ptx::tmem_dealloc(tmem, 512); }
+}
+
+}  // namespace prsgd

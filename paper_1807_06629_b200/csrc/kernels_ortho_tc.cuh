@@ -234,9 +234,8 @@ __device__ __forceinline__ void ns_store_box(uint32_t box, __half* p, int64_t pi
 }
 
 // Columns c .. c + 3 of row r of the result (v: 256 times X); n of them exist.
-__device__ __forceinline__ void ns_finish4(const NsChainArgs& a, int m, int r, int c, float4 v, int n) {
-  const NsDest& d = a.dst;
-  if (!a.vec_out || n < 4) {
+__device__ __forceinline__ void ns_finish4(const NsDest& d, bool vec, int m, int r, int c, float4 v, int n) {
+  if (!vec || n < 4) {
     ns_store_final(d, m, r, c, v.x * kNsUnscale);
     if (n > 1) ns_store_final(d, m, r, c + 1, v.y * kNsUnscale);
     if (n > 2) ns_store_final(d, m, r, c + 2, v.z * kNsUnscale);
@@ -275,9 +274,10 @@ __device__ __forceinline__ void ns_finish4(const NsChainArgs& a, int m, int r, i
   }
 }
 
-// 32 rows x 32 columns of the result, a row per lane, through shared memory so that the lanes of a warp write
+// 32 rows x 32 columns of the result (of `rows` x `cols`), a row per lane, through shared memory so that the lanes of a warp write
 // neighbouring columns (with rows per lane every store touches 32 lines).
-__device__ __forceinline__ void ns_finish(const NsChainArgs& a, int m, int r0, int c0, uint32_t box, int lane, const float (&v)[32]) {
+__device__ __forceinline__ void ns_finish(const NsDest& d, bool vec, int m, int r0, int c0, int rows, int cols, uint32_t box, int lane,
+                                          const float (&v)[32]) {
   __syncwarp();
 #pragma unroll
   for (int q = 0; q < 8; ++q)
@@ -289,8 +289,8 @@ __device__ __forceinline__ void ns_finish(const NsChainArgs& a, int m, int r0, i
   for (int i = 0; i < 8; ++i) {
     const int rr = i * 4 + (lane >> 3);
     const uint4 u = ld_shared_v4(box + (uint32_t)rr * 128u + (uint32_t)(((lane & 7) ^ (rr & 7)) * 16));
-    if (r0 + rr < a.sh.rows && c < a.sh.cols)
-      ns_finish4(a, m, r0 + rr, c, make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)), min(4, a.sh.cols - c));
+    if (r0 + rr < rows && c < cols)
+      ns_finish4(d, vec, m, r0 + rr, c, make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)), min(4, cols - c));
   }
 }
 
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]) * f;
           }
           if (last) {
-            ns_finish(a, k.m, r0, c0, h == 0 ? box_hi : box_lo, lane, v);
+            ns_finish(a.dst, a.vec_out != 0, k.m, r0, c0, a.sh.rows, a.sh.cols, h == 0 ? box_hi : box_lo, lane, v);
             continue;
           }
           uint32_t w[16];                                // (a lane reads and writes its own row of the boxes)

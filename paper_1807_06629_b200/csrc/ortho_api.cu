@@ -1,7 +1,7 @@
 // C entries of the Newton-Schulz orthogonalisation and of the Muon step.  See include/prsgd.h for the contract.
 #include <cmath>
 #include <mutex>
-#include "kernels_ortho_tc.cuh"
+#include "kernels_ortho_small.cuh"
 #include "ops_internal.h"
 
 using namespace prsgd;
@@ -64,6 +64,10 @@ static int ns_device(int* sms) {
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_chain_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_chain_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmem);
+    auto small = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmallSmem); };
+    small(ns_small_kernel<PRSGD_TYPE_FP32, 0>); small(ns_small_kernel<PRSGD_TYPE_BF16, 0>); small(ns_small_kernel<PRSGD_TYPE_FP16, 0>);
+    small(ns_small_kernel<PRSGD_TYPE_FP32, 2>); small(ns_small_kernel<PRSGD_TYPE_BF16, 2>); small(ns_small_kernel<PRSGD_TYPE_FP16, 2>);
+    small(ns_small_kernel<PRSGD_TYPE_FP32, 1>);
     if (e == cudaSuccess) known[dev] = n;
   }
   if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
@@ -77,6 +81,29 @@ size_t ns_workspace_bytes(const NsShape& sh, int precision) {
   return n;
 }
 
+// Matrices of a short side up to 128 and a long one up to 2048 (short side up to 64) or 1536: a cluster each.
+static int ns_run_small(const NsPlan& p, DeviceStatus* status, int vec_out, int sms, cudaStream_t st, int64_t* launches) {
+  NsSmallArgs a{};
+  a.sh = p.shape; a.src = p.src; a.dst = p.dst; a.status = status;
+  a.steps = p.steps; a.tall = p.shape.rows > p.shape.cols; a.s = std::min(p.shape.rows, p.shape.cols); a.l = std::max(p.shape.rows, p.shape.cols);
+  a.a = p.a; a.b = p.b; a.c = p.c; a.eps = p.eps; a.vec_out = vec_out;
+  a.sp = (a.s + 15) / 16 * 16;
+  // As few CTAs as hold the matrix, or, while all matrices' CTAs have an SM each, more with fewer columns (down to 128).
+  a.ctas = (a.l + ns_small_cols(a.s) - 1) / ns_small_cols(a.s);
+  while (a.ctas < kNsSmallCtas && (a.l + a.ctas - 1) / a.ctas > 128 && (int64_t)p.shape.batch * (a.ctas + 1) <= sms) ++a.ctas;
+  a.w = ((a.l + a.ctas - 1) / a.ctas + 63) / 64 * 64;
+  a.ctas = (a.l + a.w - 1) / a.w;
+  const dim3 grid((unsigned)(p.shape.batch * a.ctas));
+  auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kNsSmallThreads), kNsSmallSmem, st, (unsigned)a.ctas, a); };
+  if (p.src.V == nullptr) with_type(p.g_type, [&](auto ty) { go(ns_small_kernel<decltype(ty)::value, 0>); });
+  else if (p.src.G != nullptr) with_type(p.g_type, [&](auto ty) { go(ns_small_kernel<decltype(ty)::value, 2>); });
+  else go(ns_small_kernel<PRSGD_TYPE_FP32, 1>);
+  if (launches) *launches += 1;
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
+  return PRSGD_OK;
+}
+
 int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   size_t bytes = 0;
   const NsBuffers buf = ns_carve(p.shape, p.precision, static_cast<unsigned char*>(d_work), &bytes);
@@ -88,6 +115,13 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   const bool vec = p.shape.cols % 4 == 0 && fits4(p.src.G, p.src.g_row, p.src.g_batch, type_bytes(p.g_type)) &&
                    fits4(p.src.V, p.src.v_tiled ? 0 : p.src.v_row, p.src.v_batch, 4);
   const dim3 grid((unsigned)buf.chunks, (unsigned)p.shape.batch);
+  int sms = 0;
+  int rc = ns_device(&sms);
+  if (rc != PRSGD_OK) return rc;
+  const int esz = type_bytes(p.dst.type);
+  const int vec_out = (uintptr_t)p.dst.out % 16 == 0 && (p.dst.tiled || p.dst.row * esz % 16 == 0) && p.dst.batch * esz % 16 == 0;
+  const int l = std::max(p.shape.rows, p.shape.cols);
+  if (s <= kNsSmallSide && l <= ns_small_cols(s) * kNsSmallCtas) return ns_run_small(p, buf.status, vec_out, sms, st, launches);
   with_type(p.g_type, [&](auto ty) {
     constexpr int TY = decltype(ty)::value;
     auto passes = [&](auto norm, auto pack) {
@@ -116,14 +150,10 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   const int64_t total = (int64_t)p.shape.batch * p.steps * a.per_step;
   if (total > 0x3fffffffll) return op_fail(PRSGD_ERR_SIZE, "orthogonalize: too many tiles in one call");
   a.total = (int)total;
-  int sms = 0;
-  int rc = ns_device(&sms);
-  if (rc != PRSGD_OK) return rc;
   // Groups: while the last tiles of a product of one matrix drain, at least two rounds of tiles of other matrices
   // are to be claimed before its next product's.
   a.group = std::min(p.shape.batch, (sms + a.tsym - 1) / a.tsym + 1);
-  const int esz = type_bytes(p.dst.type);
-  a.vec_out = (uintptr_t)p.dst.out % 16 == 0 && (p.dst.tiled || p.dst.row * esz % 16 == 0) && p.dst.batch * esz % 16 == 0;
+  a.vec_out = vec_out;
   NsMaps maps{};
   const int64_t rows = p.shape.rows, cols = p.shape.cols, batch = p.shape.batch;
   auto map_x = [&](CUtensorMap* to, const __half* p, int box) { if (rc == PRSGD_OK) rc = ns_map(to, p, cols, rows, batch, buf.xp, box); };
