@@ -2,8 +2,8 @@
 // shared memory from its first reading to the result, so that nothing but the matrix itself is read and written.
 //
 // CTA r of the cluster keeps `w` columns (of the long side) of X as fp16 pairs.  Per step it forms its share of
-// A = X X^T on the tensor cores, the shares are summed through distributed shared memory in rank order by every CTA (all
-// get the same bits), each forms P = a I + b A + c A^2 for itself and applies it to its columns.  All products are
+// A = X X^T on the tensor cores; each CTA sums a part of A over the shares, in rank order, through distributed shared
+// memory and hands it to all; each then forms P = a I + b A + c A^2 for itself and applies it to its columns.  All products are
 // hi hi + hi lo + lo hi whatever the precision asked for: with so little work the time is that of the waits between
 // the steps, not of the products.  (16 matrices of 10 x 1024: about 150 us as three products a step of the chain's tiles.)
 #pragma once
@@ -37,12 +37,12 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void st_shared_b16(uint32_t at, __half h) {
-  asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__half_as_ushort(h)) : "memory");
+__device__ __forceinline__ void st_cluster_v2(uint32_t at, uint32_t x, uint32_t y) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
 }
 
-// MODE as in ns_norm_kernel.
-template <int TY, int MODE>
+// MODE as in ns_norm_kernel; VEC: elements of a row that are read together.
+template <int TY, int MODE, int VEC>
 __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __grid_constant__ NsSmallArgs a) {
   using T = typename ElemOf<TY>::type;
   extern __shared__ unsigned char smem_raw[];
@@ -75,35 +75,66 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   const int outer = a.tall ? nj : a.s, inner = a.tall ? a.s : nj;
   const T* const g = static_cast<const T*>(a.src.G) + (int64_t)m * a.src.g_batch;
   float* const v = a.src.V + (int64_t)m * a.src.v_batch;
-  // use(i, j, load(row, col)): warps along rows of G, lanes along columns, eight rows of a warp requested together
-  auto each = [&](auto&& load, auto&& use) {
-    constexpr int B = 8, W = kNsSmallThreads / 32;
-    for (int p = warp; p < outer; p += W * B)
-      for (int q = lane; q < inner; q += 32) {
-        float u[B];
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-          const int pb = p + W * b;
-          u[b] = pb < outer ? load(a.tall ? j0 + pb : pb, a.tall ? q : j0 + q) : 0.f;
-        }
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-          const int pb = p + W * b;
-          if (pb < outer) use(a.tall ? q : pb, a.tall ? pb : q, u[b]);
-        }
-      }
-  };
+  // 16-byte chunks of 8 along a row of 128 bytes, swizzled over 8 rows; 64 columns to a block of 16 KB
+  auto at = [&](int i, int j) { return (uint32_t)(j >> 6) * 16384u + (uint32_t)i * 128u + (uint32_t)((((j & 63) >> 3) ^ (i & 7)) * 16) + (uint32_t)(j & 7) * 2u; };
+  // U is read once: its squares are summed, and until the norm is known its fp32 bits stay in the two halves of its place
+  // in X.  Warps along rows of G, lanes along columns (VEC of them each), eight rows of a warp requested together.
   auto v_at = [&](int row, int col) { return a.src.v_tiled ? wtile_offset(a.src.v_tile, row, col) : (int64_t)row * a.src.v_row + col; };
   double sum = 0.0;
-  each([&](int row, int col) -> float {
-    if constexpr (MODE == 0) return to_f32(g[(int64_t)row * a.src.g_row + col]);
-    if constexpr (MODE == 1) return v[v_at(row, col)];
-    const float gr = to_f32(g[(int64_t)row * a.src.g_row + col]);
-    const int64_t o = v_at(row, col);
-    const float w = fmaf(a.src.mu, v[o], gr);
-    v[o] = w;
-    return a.src.nesterov ? fmaf(a.src.mu, w, gr) : w;
-  }, [&](int, int, float u) { sum += (double)u * (double)u; });
+  constexpr int B = 8, W = kNsSmallThreads / 32;
+  __syncthreads();                                         // (X has been zeroed)
+#pragma unroll 1
+  for (int p = warp; p < outer; p += W * B)
+#pragma unroll 1
+    for (int q = lane * VEC; q < inner; q += 32 * VEC) {
+      float u[B][VEC];
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        const int pb = p + W * b;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[b][e] = 0.f;
+        if (pb >= outer) continue;
+        const int row = a.tall ? j0 + pb : pb, col = a.tall ? q : j0 + q;
+        if constexpr (MODE != 1) ns_load<TY, VEC>(g + (int64_t)row * a.src.g_row + col, u[b]);
+        if constexpr (MODE != 0) {
+          float* const o = v + v_at(row, col);
+          float w[VEC];
+          ns_load<PRSGD_TYPE_FP32, VEC>(o, w);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            if constexpr (MODE == 1) {
+              u[b][e] = w[e];
+            } else {
+              w[e] = fmaf(a.src.mu, w[e], u[b][e]);
+              u[b][e] = a.src.nesterov ? fmaf(a.src.mu, w[e], u[b][e]) : w[e];
+            }
+          }
+          if constexpr (MODE == 2) {
+            if constexpr (VEC == 4) *reinterpret_cast<float4*>(o) = make_float4(w[0], w[1], w[2], w[3]);
+            else o[0] = w[0];
+          }
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        const int pb = p + W * b;
+        if (pb >= outer) continue;
+        uint32_t top[VEC], low[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          sum += (double)u[b][e] * (double)u[b][e];
+          top[e] = __float_as_uint(u[b][e]) >> 16; low[e] = __float_as_uint(u[b][e]) & 0xffffu;
+        }
+        const uint32_t o = a.tall ? at(q, pb) : at(pb, q);
+        if constexpr (VEC == 4) {
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(x_hi + o), "r"(top[0] | (top[1] << 16)), "r"(top[2] | (top[3] << 16)) : "memory");
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(x_lo + o), "r"(low[0] | (low[1] << 16)), "r"(low[2] | (low[3] << 16)) : "memory");
+        } else {
+          asm volatile("st.shared.b16 [%0], %1;" ::"r"(x_hi + o), "h"((uint16_t)top[0]) : "memory");
+          asm volatile("st.shared.b16 [%0], %1;" ::"r"(x_lo + o), "h"((uint16_t)low[0]) : "memory");
+        }
+      }
+    }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) s_part[warp] = sum;
@@ -119,19 +150,23 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   double total = 0.0;
   for (int r = 0; r < a.ctas; ++r) total += ld_cluster_f64(ptx::cluster_map(ptx::smem_u32(&s_norm), (uint32_t)r));
   const float2 inv = ns_inverse(sqrt(total) + (double)a.eps);
-  // 16-byte chunks of 8 along a row of 128 bytes, swizzled over 8 rows; 64 columns to a block of 16 KB
-  auto at = [&](int i, int j) { return (uint32_t)(j >> 6) * 16384u + (uint32_t)i * 128u + (uint32_t)((((j & 63) >> 3) ^ (i & 7)) * 16) + (uint32_t)(j & 7) * 2u; };
-  each([&](int row, int col) -> float {
-    if constexpr (MODE == 0) return to_f32(g[(int64_t)row * a.src.g_row + col]);
-    const float w = v[v_at(row, col)];
-    if constexpr (MODE == 1) return w;
-    return a.src.nesterov ? fmaf(a.src.mu, w, to_f32(g[(int64_t)row * a.src.g_row + col])) : w;
-  }, [&](int i, int j, float u) {
-    __half hi, lo;
-    ns_split(u * inv.x * inv.y, hi, lo);
-    st_shared_b16(x_hi + at(i, j), hi);
-    st_shared_b16(x_lo + at(i, j), lo);
-  });
+#pragma unroll 1
+  for (int idx = (int)threadIdx.x; idx < a.s * (a.w / 8); idx += kNsSmallThreads) {
+    const int row = idx / (a.w / 8);
+    const uint32_t o = at(row, (idx - row * (a.w / 8)) * 8);
+    const uint4 h = ld_shared_v4(x_hi + o), l = ld_shared_v4(x_lo + o);
+    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+    uint32_t ho[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float y0 = __uint_as_float((hw[e] << 16) | (lw[e] & 0xffffu)) * inv.x * inv.y, y1 = __uint_as_float((hw[e] & 0xffff0000u) | (lw[e] >> 16)) * inv.x * inv.y;
+      ho[e] = pack_half2(y0, y1);
+      const float2 f = unpack_half2(ho[e]);
+      lo[e] = pack_half2(y0 - f.x, y1 - f.y);
+    }
+    st_shared_v4(x_hi + o, ho[0], ho[1], ho[2], ho[3]);
+    st_shared_v4(x_lo + o, lo[0], lo[1], lo[2], lo[3]);
+  }
 
   ptx::tc_fence_before();
   __syncthreads();
@@ -176,7 +211,6 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
     const bool last = step + 1 == a.steps;
     // ---- A = X X^T: this CTA's share, then the sum of all
     products(d_s, (uint32_t)a.sp, a.w / 16, x_hi, x_lo, x_hi, x_lo, false);
-    if (step > 0) ptx::cluster_wait_acquire();             // everyone has read the last shares
     if (quarter * 32 < a.sp) {
 #pragma unroll 1
       for (int c = half * 16; c < a.sp; c += 32) {
@@ -191,8 +225,9 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
     }
     ptx::cluster_arrive_release();
     ptx::cluster_wait_acquire();
+    const int all = a.sp * chunks, mine1 = all * (rank + 1) / a.ctas;
 #pragma unroll 1
-    for (int idx = (int)threadIdx.x; idx < a.sp * chunks; idx += kNsSmallThreads) {
+    for (int idx = all * rank / a.ctas + (int)threadIdx.x; idx < mine1; idx += kNsSmallThreads) {
       const int row = idx / chunks, q = idx - row * chunks;
       const uint32_t from = share_at(row, q);
       float4 part[kNsSmallCtas], f = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -205,11 +240,15 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
       f.x *= kNsUnscale; f.y *= kNsUnscale; f.z *= kNsUnscale; f.w *= kNsUnscale;
       const uint32_t h0 = pack_half2(f.x, f.y), h1 = pack_half2(f.z, f.w);
       const float2 b0 = unpack_half2(h0), b1 = unpack_half2(h1);
-      const uint32_t o = at(row, q * 4);
-      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(s_hi + o), "r"(h0), "r"(h1) : "memory");
-      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(s_lo + o), "r"(pack_half2(f.x - b0.x, f.y - b0.y)), "r"(pack_half2(f.z - b1.x, f.w - b1.y)) : "memory");
+      const uint32_t l0 = pack_half2(f.x - b0.x, f.y - b0.y), l1 = pack_half2(f.z - b1.x, f.w - b1.y), o = at(row, q * 4);
+#pragma unroll 1
+      for (int r = 0; r < a.ctas; ++r) {
+        st_cluster_v2(ptx::cluster_map(s_hi + o, (uint32_t)r), h0, h1);
+        st_cluster_v2(ptx::cluster_map(s_lo + o, (uint32_t)r), l0, l1);
+      }
     }
-    ptx::cluster_arrive_release();                         // (waited for before the next shares are written)
+    ptx::cluster_arrive_release();                         // A is whole, and its shares have been read
+    ptx::cluster_wait_acquire();
     // ---- P = a I + b A + c A^2, in the place of A
     products(d_s, (uint32_t)a.sp, a.sp / 16, s_hi, s_lo, s_hi, s_lo, false);
     if (quarter * 32 < a.sp) {
@@ -281,8 +320,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
     }
   }
   ptx::tc_fence_before();
-  __syncthreads();
-  ptx::cluster_wait_acquire();                             // (no CTA leaves while its memory is read)
+  __syncthreads();                                         // (nobody touches this CTA's memory after the last step's second barrier)
   if (warp == 1) { ptx::tmem_relinquish(); ptx::tmem_dealloc(tmem, 512); }
 }
 

@@ -51,27 +51,43 @@ static int ns_map(CUtensorMap* m, const void* base, int64_t d0, int64_t d1, int6
   return r == CUDA_SUCCESS ? PRSGD_OK : op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
 }
 
-// The current device: its SM count; its kernels' shared-memory limits are raised on the first call.
-static int ns_device(int* sms) {
+// The current device: its SM count, and how many clusters of 1 to 8 CTAs of ns_small_kernel run at a time (a cluster lies
+// within one group of SMs, so that is fewer than the SMs divided by its size).  Found out, and the kernels'
+// shared-memory limits raised, on the first call.
+struct NsDevice { int sms, clusters[kNsSmallCtas + 1]; };
+static int ns_device(NsDevice* out) {
   static std::mutex lock;
-  static int known[64] = {0};
+  static NsDevice known[64];
   int dev = -1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess && (dev < 0 || dev >= 64)) return op_fail(PRSGD_ERR_ARG, "device ordinal out of range");
   std::lock_guard<std::mutex> hold(lock);
-  if (e == cudaSuccess && known[dev] == 0) {
+  if (e == cudaSuccess && known[dev].sms == 0) {
     int n = 0;
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_chain_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_chain_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmem);
-    auto small = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmallSmem); };
-    small(ns_small_kernel<PRSGD_TYPE_FP32, 0>); small(ns_small_kernel<PRSGD_TYPE_BF16, 0>); small(ns_small_kernel<PRSGD_TYPE_FP16, 0>);
-    small(ns_small_kernel<PRSGD_TYPE_FP32, 2>); small(ns_small_kernel<PRSGD_TYPE_BF16, 2>); small(ns_small_kernel<PRSGD_TYPE_FP16, 2>);
-    small(ns_small_kernel<PRSGD_TYPE_FP32, 1>);
-    if (e == cudaSuccess) known[dev] = n;
+    auto small = [&](auto vec) {
+      constexpr int V = decltype(vec)::value;
+      auto raise = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNsSmallSmem); };
+      raise(ns_small_kernel<PRSGD_TYPE_FP32, 0, V>); raise(ns_small_kernel<PRSGD_TYPE_BF16, 0, V>); raise(ns_small_kernel<PRSGD_TYPE_FP16, 0, V>);
+      raise(ns_small_kernel<PRSGD_TYPE_FP32, 2, V>); raise(ns_small_kernel<PRSGD_TYPE_BF16, 2, V>); raise(ns_small_kernel<PRSGD_TYPE_FP16, 2, V>);
+      raise(ns_small_kernel<PRSGD_TYPE_FP32, 1, V>);
+    };
+    small(std::integral_constant<int, 1>()); small(std::integral_constant<int, 4>());
+    for (int c = 1; c <= kNsSmallCtas && e == cudaSuccess; ++c) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)c); cfg.blockDim = dim3(kNsSmallThreads); cfg.dynamicSmemBytes = kNsSmallSmem;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = (unsigned)c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr; cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&known[dev].clusters[c], ns_small_kernel<PRSGD_TYPE_FP32, 0, 4>, &cfg);
+    }
+    if (e == cudaSuccess) known[dev].sms = n;
   }
   if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
-  *sms = known[dev];
+  *out = known[dev];
   return PRSGD_OK;
 }
 
@@ -82,22 +98,28 @@ size_t ns_workspace_bytes(const NsShape& sh, int precision) {
 }
 
 // Matrices of a short side up to 128 and a long one up to 2048 (short side up to 64) or 1536: a cluster each.
-static int ns_run_small(const NsPlan& p, DeviceStatus* status, int vec_out, int sms, cudaStream_t st, int64_t* launches) {
+static int ns_run_small(const NsPlan& p, DeviceStatus* status, bool vec_in, int vec_out, const NsDevice& dev, cudaStream_t st, int64_t* launches) {
   NsSmallArgs a{};
   a.sh = p.shape; a.src = p.src; a.dst = p.dst; a.status = status;
   a.steps = p.steps; a.tall = p.shape.rows > p.shape.cols; a.s = std::min(p.shape.rows, p.shape.cols); a.l = std::max(p.shape.rows, p.shape.cols);
   a.a = p.a; a.b = p.b; a.c = p.c; a.eps = p.eps; a.vec_out = vec_out;
   a.sp = (a.s + 15) / 16 * 16;
-  // As few CTAs as hold the matrix, or, while all matrices' CTAs have an SM each, more with fewer columns (down to 128).
+  // As few CTAs as hold the matrix, or, while all clusters run at a time, more with fewer columns (down to 128).  (16 matrices
+  // of 10 x 1024 in clusters of 8, of which 14 run at a time: 65 us; of 6: 41.)
   a.ctas = (a.l + ns_small_cols(a.s) - 1) / ns_small_cols(a.s);
-  while (a.ctas < kNsSmallCtas && (a.l + a.ctas - 1) / a.ctas > 128 && (int64_t)p.shape.batch * (a.ctas + 1) <= sms) ++a.ctas;
+  while (a.ctas < kNsSmallCtas && (a.l + a.ctas - 1) / a.ctas > 128 && p.shape.batch <= dev.clusters[a.ctas + 1]) ++a.ctas;
   a.w = ((a.l + a.ctas - 1) / a.ctas + 63) / 64 * 64;
   a.ctas = (a.l + a.w - 1) / a.w;
   const dim3 grid((unsigned)(p.shape.batch * a.ctas));
   auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kNsSmallThreads), kNsSmallSmem, st, (unsigned)a.ctas, a); };
-  if (p.src.V == nullptr) with_type(p.g_type, [&](auto ty) { go(ns_small_kernel<decltype(ty)::value, 0>); });
-  else if (p.src.G != nullptr) with_type(p.g_type, [&](auto ty) { go(ns_small_kernel<decltype(ty)::value, 2>); });
-  else go(ns_small_kernel<PRSGD_TYPE_FP32, 1>);
+  auto modes = [&](auto vec) {
+    constexpr int V = decltype(vec)::value;
+    if (p.src.V == nullptr) with_type(p.g_type, [&](auto ty) { go(ns_small_kernel<decltype(ty)::value, 0, V>); });
+    else if (p.src.G != nullptr) with_type(p.g_type, [&](auto ty) { go(ns_small_kernel<decltype(ty)::value, 2, V>); });
+    else go(ns_small_kernel<PRSGD_TYPE_FP32, 1, V>);
+  };
+  if (vec_in && !a.tall) modes(std::integral_constant<int, 4>());
+  else modes(std::integral_constant<int, 1>());
   if (launches) *launches += 1;
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("orthogonalize: ") + cudaGetErrorString(e));
@@ -115,13 +137,14 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   const bool vec = p.shape.cols % 4 == 0 && fits4(p.src.G, p.src.g_row, p.src.g_batch, type_bytes(p.g_type)) &&
                    fits4(p.src.V, p.src.v_tiled ? 0 : p.src.v_row, p.src.v_batch, 4);
   const dim3 grid((unsigned)buf.chunks, (unsigned)p.shape.batch);
-  int sms = 0;
-  int rc = ns_device(&sms);
+  NsDevice dev;
+  int rc = ns_device(&dev);
+  const int sms = dev.sms;
   if (rc != PRSGD_OK) return rc;
   const int esz = type_bytes(p.dst.type);
   const int vec_out = (uintptr_t)p.dst.out % 16 == 0 && (p.dst.tiled || p.dst.row * esz % 16 == 0) && p.dst.batch * esz % 16 == 0;
   const int l = std::max(p.shape.rows, p.shape.cols);
-  if (s <= kNsSmallSide && l <= ns_small_cols(s) * kNsSmallCtas) return ns_run_small(p, buf.status, vec_out, sms, st, launches);
+  if (s <= kNsSmallSide && l <= ns_small_cols(s) * kNsSmallCtas) return ns_run_small(p, buf.status, vec, vec_out, dev, st, launches);
   with_type(p.g_type, [&](auto ty) {
     constexpr int TY = decltype(ty)::value;
     auto passes = [&](auto norm, auto pack) {
