@@ -257,6 +257,27 @@ int prsgd_enable_momentum(prsgd_ctx* ctx, float mu, void* d_velocity, int averag
 /* The momentum buffers, [N][m] in canonical order.  Synchronises the stream. */
 int prsgd_get_velocity_stacked(prsgd_ctx* ctx, float* dst, int dst_on_device);
 
+/* Muon local step: for the layers whose bit l - 1 is set in `layers`, v_l <- mu v_l + G_l as with momentum, then
+ *   W_l <- W_l - gamma * scale_l * NS(v_l),
+ * NS the Newton-Schulz orthogonalisation of prsgd_orthogonalize (its default coefficients, `steps` of them; FP32 or BF16
+ * precision as the context's) and scale_l = sqrt(max(1, d_l / d_{l-1})) (PRSGD_MUON_SCALE_SPECTRAL) or
+ * 0.2 sqrt(max(d_l, d_{l-1})) (PRSGD_MUON_SCALE_RMS).  All biases, and the weights of the other layers (usually the class
+ * layer), take the momentum step.  Needs prsgd_enable_momentum first; the buffers are averaged or not as said there.
+ * Averages run as launches of their own, worker groups as one chain; an inactive worker keeps its point.  d_work: caller-owned,
+ * 256-byte aligned, of at least prsgd_muon_workspace_bytes, kept by reference.  layers = 0 switches back to momentum;
+ * prsgd_enable_momentum(NULL) to plain SGD. */
+#define PRSGD_MUON_SCALE_SPECTRAL 0
+#define PRSGD_MUON_SCALE_RMS      1
+int prsgd_muon_workspace_bytes(prsgd_ctx* ctx, uint32_t layers, size_t* bytes);
+int prsgd_enable_muon(prsgd_ctx* ctx, uint32_t layers, int32_t scale_rule, int32_t steps, void* d_work, size_t work_bytes);
+
+/* Balance loss over the classes, for a model whose outputs are a router's logits: F_i gets
+ *   coef * C * sum_c f_c P_c  added, C = d_L, f_c = share of class c among the top_k largest logits of the minibatch's rows
+ * (ties to the lowest index, held fixed in the gradient), P_c = mean over the rows of the softmax -- prsgd_route's loss with the
+ * worker's minibatch as its tokens.  prsgd_get_losses includes it.  top_k = 0 switches it off; d_L at most
+ * PRSGD_ROUTE_MAX_EXPERTS.  While it is on, the softmax gradient runs as a launch of its own on both paths. */
+int prsgd_set_balance(prsgd_ctx* ctx, float coef, int32_t top_k);
+
 /* Options.  PRSGD_OPT_FUSED_AVERAGE (default 1): on an averaging iteration the
  * update and the average run as one pass over the store instead of an update
  * pass followed by prsgd_average's pass; both produce identical bits. */

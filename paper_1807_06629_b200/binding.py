@@ -40,6 +40,7 @@ OPT_HEAD_FORWARD = 17
 OPT_MERGED_SMALL_AVERAGE = 18
 OPT_TILED_WEIGHTS = 19
 OPT_OVERLAP_UPDATE = 20
+MUON_SCALE_SPECTRAL, MUON_SCALE_RMS = 0, 1
 ERR_DEVICE_TIMEOUT, ERR_NONFINITE = -6, -7
 KERNEL_FAMILIES = ("forward", "softmax", "dx", "update", "update_average", "average", "misc", "head")
 MAX_LAYERS = 16
@@ -57,6 +58,7 @@ EXPORTS = [
     "prsgd_set_global_workers", "prsgd_check_finite", "prsgd_local_steps_sum",
     "prsgd_orthogonalize_workspace_bytes", "prsgd_orthogonalize", "prsgd_muon_step", "prsgd_work_status",
     "prsgd_route_workspace_bytes", "prsgd_route", "prsgd_route_grad",
+    "prsgd_muon_workspace_bytes", "prsgd_enable_muon", "prsgd_set_balance",
 ]
 NOALLOC_MAX_M = 1 << 20
 
@@ -126,6 +128,9 @@ def _load() -> C.CDLL:
         "prsgd_muon_step": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, vp, i32, i64, i64, i32, i32, i32, f32, f32, i32, f32,
                                       i32, vp, f32, f32, i32, vp, szt, vp]),
         "prsgd_work_status": (C.c_int, [vp, vp]),
+        "prsgd_muon_workspace_bytes": (C.c_int, [vp, C.c_uint32, szp]),
+        "prsgd_enable_muon": (C.c_int, [vp, C.c_uint32, i32, i32, vp, szt]),
+        "prsgd_set_balance": (C.c_int, [vp, f32, i32]),
         "prsgd_route_workspace_bytes": (C.c_int, [i64, i64, i32, szp]),
         "prsgd_route": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, szt, vp]),
         "prsgd_route_grad": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, i64, i64, vp]),
@@ -566,6 +571,26 @@ class PRSGD:
             self.velocity = torch.empty(self.N * self.m_pad, dtype=torch.float32, device=self.device)
         self._call(lib.prsgd_enable_momentum, mu, self.velocity.data_ptr(), 1 if average_velocity else 0)
         self.average_velocity = bool(average_velocity)
+
+    def enable_muon(self, layers: Optional[Sequence[int]] = None, scale: int = MUON_SCALE_SPECTRAL, steps: int = 5):
+        """Muon step for the weights of `layers` (1-based; default: all but the class layer; [] switches it off), after
+        enable_momentum; allocates the workspace."""
+        chosen = range(1, len(self.dims) - 1) if layers is None else layers
+        bits = 0
+        for l in chosen:
+            if not 1 <= l < len(self.dims):
+                raise ValueError(f"the model has no layer {l}")
+            bits |= 1 << (l - 1)
+        n = C.c_size_t()
+        self._call(lib.prsgd_muon_workspace_bytes, bits, C.byref(n))
+        with torch.cuda.device(self.device):
+            work = _empty(max(n.value, 1), torch.uint8, self.device, self.stream)
+        self._call(lib.prsgd_enable_muon, bits, scale, steps, work.data_ptr(), n.value)
+        self._muon_work = work
+
+    def set_balance(self, coef: float, top_k: int):
+        """Adds the balance loss over the classes to F_i (top_k = 0: off)."""
+        self._call(lib.prsgd_set_balance, coef, top_k)
 
     def get_velocity_stacked(self) -> np.ndarray:
         out = np.empty((self.N, self.m), dtype=np.float32)

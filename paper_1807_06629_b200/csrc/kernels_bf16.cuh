@@ -2270,7 +2270,7 @@ inline bool tc_forward_early_loads(prsgd_ctx* c) {
   return c->early_loads != 0 && quiet;
 }
 
-inline bool tc_epilogues_fused(const prsgd_ctx* c) { return c->fused_epilogues != 0 && c->dims[c->L] <= 128; }
+inline bool tc_epilogues_fused(const prsgd_ctx* c) { return c->fused_epilogues != 0 && c->dims[c->L] <= 128 && c->balance_k == 0; }
 
 // Right after a node average every worker's row holds the same bits (Algorithm 1: all workers restart from y),
 // so the launches of the iteration that follows may read worker 0's weights for every worker.  Safe for

@@ -42,6 +42,7 @@ struct GemmF32Args {
   int64_t params_worker_stride;
   const float* mask_src; // DX: a_{l-1} of the same shape as out (ReLU mask: a > 0)
   float gamma;
+  int keep_weights;      // DW: only the momentum buffers of W_l take the gradient (its step is made elsewhere)
   const uint8_t* active; // per-worker flag or nullptr
   float* vel;            // DW: momentum buffers laid out like the store, or nullptr
   float mu;
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(256) gemm_f32_kernel(const GemmF32Args g) {
             step = fmaf(g.mu, *vp, step);
             *vp = step;
           }
-          float xi = is_active ? fmaf(-g.gamma, step, w) : w;
+          float xi = is_active && !g.keep_weights ? fmaf(-g.gamma, step, w) : w;
           if (FUSE) sum[r][c] += xi;
           else W[(int64_t)i * g.Nn + j] = xi;
         }
@@ -297,6 +298,71 @@ __global__ void __launch_bounds__(256) softmax_ce_kernel(const SoftmaxArgs a) {
     if (a.delta_bk) a.delta_bk[((int64_t)n * a.B + b) * a.ld_bf + c] = f32_to_bf16_rn(d);
   }
   if (lane == 0) a.row_losses[(int64_t)n * a.B + b] = lse - z[label];
+}
+
+// The same with a balance loss added to F_i (prsgd_set_balance): with p_bc the softmax, c_c the number of rows that have
+// class c among their k largest logits (ties: lowest index) and f_c = c_c / (k B),
+//   loss_b += coef C dot_b,  dot_b = sum_c f_c p_bc;   delta_bc += coef C / B p_bc (f_c - dot_b).
+// One block of 256 threads per worker: the counts need all rows before any gradient.
+constexpr int kBalanceMaxClasses = 1024;
+__global__ void __launch_bounds__(256) softmax_ce_balance_kernel(const SoftmaxArgs a, float coef, int k) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __shared__ int s_count[kBalanceMaxClasses];
+  const int n = blockIdx.x;
+  if (a.active != nullptr && a.active[n] == 0) return;
+  if (a.status != nullptr && a.status->error != 0u) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t blk = draw_block(a.draw.seed, a.draw.worker0 + n, draw_t(a.draw), a.draw.n_blocks);
+  if (threadIdx.x == 0) a.draws[n] = (int32_t)blk;
+  for (int c = threadIdx.x; c < a.C; c += 256) s_count[c] = 0;
+  __syncthreads();
+  for (int b = warp; b < a.B; b += 8) {
+    const float* z = a.logits + ((int64_t)n * a.B + b) * a.ldz;
+    unsigned long long above = ~0ull;                    // (order of the logit, 2^32 - 1 - index) of the choice before
+    for (int j = 0; j < k; ++j) {
+      unsigned long long best = 0ull;
+      for (int c = lane; c < a.C; c += 32) {
+        const uint32_t u = __float_as_uint(z[c] + 0.f);
+        const unsigned long long key = ((unsigned long long)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (0xFFFFFFFFu - (uint32_t)c);
+        if (key < above && key > best) best = key;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
+        best = other > best ? other : best;
+      }
+      above = best;
+      if (lane == 0) atomicAdd(&s_count[0xFFFFFFFFu - (uint32_t)best], 1);
+    }
+  }
+  __syncthreads();
+  const float invB = 1.f / (float)a.B, per = 1.f / ((float)k * (float)a.B), pull = coef * (float)a.C;
+  for (int b = warp; b < a.B; b += 8) {
+    const float* z = a.logits + ((int64_t)n * a.B + b) * a.ldz;
+    float mx = -INFINITY;
+    for (int c = lane; c < a.C; c += 32) mx = fmaxf(mx, z[c]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    float s = 0.f, dot = 0.f;
+    for (int c = lane; c < a.C; c += 32) {
+      const float e = expf(z[c] - mx);
+      s += e;
+      dot = fmaf(e, (float)s_count[c] * per, dot);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) { s += __shfl_xor_sync(0xffffffffu, s, o); dot += __shfl_xor_sync(0xffffffffu, dot, o); }
+    dot /= s;
+    const float lse = mx + logf(s);
+    const int label = a.Y[(int64_t)n * a.P + (int64_t)blk * a.B + b];
+    for (int c = lane; c < a.C; c += 32) {
+      const float p = expf(z[c] - lse);
+      const float d = (p - (c == label ? 1.f : 0.f) + pull * p * ((float)s_count[c] * per - dot)) * invB;
+      if (a.delta) a.delta[((int64_t)n * a.B + b) * a.ldz + c] = d;
+      if (a.delta_bk) a.delta_bk[((int64_t)n * a.B + b) * a.ld_bf + c] = f32_to_bf16_rn(d);
+    }
+    if (lane == 0) a.row_losses[(int64_t)n * a.B + b] = lse - z[label] + pull * dot;
+  }
 }
 
 }  // namespace prsgd

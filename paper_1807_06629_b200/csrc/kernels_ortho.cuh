@@ -40,6 +40,7 @@ struct NsBuffers {
   unsigned int* done;                    // [batch][panels] tiles that have been added to a panel
   int panels;
   DeviceStatus* status;
+  int own_status;                        // the workspace's own: cleared by the call.  0: a context's, an error in it turns the call into a no-op
   int64_t xp, sp;
   int chunks;
 };
@@ -90,8 +91,12 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const NsShape sh, const Ns
   const int m = blockIdx.y;
   if (blockIdx.x == 0) {
     for (int i = threadIdx.x; i < buf.panels; i += 256) buf.done[(int64_t)m * buf.panels + i] = 0u;
-    if (m == 0 && threadIdx.x == 0) { *buf.claim = 0u; buf.status->error = 0u; }
+    if (m == 0 && threadIdx.x == 0) {
+      *buf.claim = 0u;
+      if (buf.own_status) buf.status->error = 0u;
+    }
   }
+  if (!buf.own_status && buf.status->error != 0u) return;
   __shared__ double s_part[8];
   double sum = 0.0;
   if (src.active == nullptr || src.active[m] != 0) {

@@ -22,6 +22,7 @@ enum { NS_ERR_SMALL = 0x711 };
 struct NsSmallArgs {
   NsShape sh; NsSource src; NsDest dst;
   DeviceStatus* status;
+  int own_status;
   int steps, tall, s, l, ctas, w, sp;    // w: columns of a CTA (multiple of 64), sp: short side, multiple of 16
   float a, b, c, eps;
   int vec_out;
@@ -60,7 +61,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   const uint32_t bar = ptx::smem_u32(&bar_mma);
   ptx::pdl_wait();
   ptx::pdl_trigger();
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.status->error = 0u;
+  if (a.own_status && blockIdx.x == 0 && threadIdx.x == 0) a.status->error = 0u;
   if (a.src.active != nullptr && a.src.active[m] == 0) return;       // (the whole cluster)
   if (threadIdx.x == 0) {
     ptx::mbar_init(bar, 1);
@@ -309,6 +310,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
               st_shared_v4(x_lo + o, lo[0], lo[1], lo[2], lo[3]);
             }
           }
+        } else if (!a.own_status && a.status->error != 0u) {      // (a context whose device error stands keeps its parameters)
         } else if (!a.tall) {
           if (c < nj) ns_finish(a.dst, a.vec_out, m, quarter * 32, j0 + c, a.s, min(a.l, j0 + a.w), box, lane, y);
         } else if (i < a.s) {                              // (lanes hold neighbouring columns of the result)

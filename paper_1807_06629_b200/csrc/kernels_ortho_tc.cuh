@@ -25,7 +25,7 @@ constexpr int kNsWarpCols = 1024 / kNsEpiWarps;       // an epilogue warp takes 
 constexpr uint32_t kNsStageBytes = 32768, kNsWarpBytes = 8192;      // operand stage of a CTA; staging of an epilogue warp
 constexpr size_t kNsSmem = 1024 + (size_t)kNsStages * kNsStageBytes + kNsEpiWarps * kNsWarpBytes;
 constexpr int kNsAhead = 8;            // the next tile is claimed when this many blocks of 64 of the current one are left to load
-constexpr int kNsPromote = 4;          // 32-bit precision: blocks of 64 whose products are summed in TMEM before they join the sum in registers
+constexpr int kNsPromote = 2;          // 32-bit precision: blocks of 64 whose products are summed in TMEM before they join the sum in registers
 enum { NS_ERR_DEP = 0x701, NS_ERR_FULL, NS_ERR_EMPTY, NS_ERR_ACC, NS_ERR_ACC_FREE, NS_ERR_RING, NS_ERR_RING_FREE };
 
 struct NsMaps {
@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
       for (;;) {
         const int t = (int)atomicAdd(a.buf.claim, 1u);
-        if (t >= a.total) break;
+        if (t >= a.total || (n == 0 && !a.buf.own_status && status->error != 0u)) break;
         const NsTask got = ns_decode(a, t);
         if (a.dst.active != nullptr && a.dst.active[got.m] == 0) continue;
         k = got;

@@ -91,6 +91,8 @@ static int ns_device(NsDevice* out) {
   return PRSGD_OK;
 }
 
+int ns_prepare() { NsDevice d; return ns_device(&d); }
+
 size_t ns_workspace_bytes(const NsShape& sh, int precision) {
   size_t n = 0;
   ns_carve(sh, precision, nullptr, &n);
@@ -98,9 +100,9 @@ size_t ns_workspace_bytes(const NsShape& sh, int precision) {
 }
 
 // Matrices of a short side up to 128 and a long one up to 2048 (short side up to 64) or 1536: a cluster each.
-static int ns_run_small(const NsPlan& p, DeviceStatus* status, bool vec_in, int vec_out, const NsDevice& dev, cudaStream_t st, int64_t* launches) {
+static int ns_run_small(const NsPlan& p, const NsBuffers& buf, bool vec_in, int vec_out, const NsDevice& dev, cudaStream_t st, int64_t* launches) {
   NsSmallArgs a{};
-  a.sh = p.shape; a.src = p.src; a.dst = p.dst; a.status = status;
+  a.sh = p.shape; a.src = p.src; a.dst = p.dst; a.status = buf.status; a.own_status = buf.own_status;
   a.steps = p.steps; a.tall = p.shape.rows > p.shape.cols; a.s = std::min(p.shape.rows, p.shape.cols); a.l = std::max(p.shape.rows, p.shape.cols);
   a.a = p.a; a.b = p.b; a.c = p.c; a.eps = p.eps; a.vec_out = vec_out;
   a.sp = (a.s + 15) / 16 * 16;
@@ -128,7 +130,9 @@ static int ns_run_small(const NsPlan& p, DeviceStatus* status, bool vec_in, int 
 
 int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   size_t bytes = 0;
-  const NsBuffers buf = ns_carve(p.shape, p.precision, static_cast<unsigned char*>(d_work), &bytes);
+  NsBuffers buf = ns_carve(p.shape, p.precision, static_cast<unsigned char*>(d_work), &bytes);
+  buf.own_status = p.status == nullptr ? 1 : 0;
+  if (p.status != nullptr) buf.status = p.status;
   const int s = std::min(p.shape.rows, p.shape.cols);
   const bool split = p.precision == PRSGD_PRECISION_FP32;
   auto fits4 = [](const void* q, int64_t row, int64_t batch, int esz) {
@@ -144,7 +148,7 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   const int esz = type_bytes(p.dst.type);
   const int vec_out = (uintptr_t)p.dst.out % 16 == 0 && (p.dst.tiled || p.dst.row * esz % 16 == 0) && p.dst.batch * esz % 16 == 0;
   const int l = std::max(p.shape.rows, p.shape.cols);
-  if (s <= kNsSmallSide && l <= ns_small_cols(s) * kNsSmallCtas) return ns_run_small(p, buf.status, vec, vec_out, dev, st, launches);
+  if (s <= kNsSmallSide && l <= ns_small_cols(s) * kNsSmallCtas) return ns_run_small(p, buf, vec, vec_out, dev, st, launches);
   with_type(p.g_type, [&](auto ty) {
     constexpr int TY = decltype(ty)::value;
     auto passes = [&](auto norm, auto pack) {

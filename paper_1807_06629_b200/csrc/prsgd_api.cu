@@ -11,6 +11,7 @@
 #include "kernels_f32.cuh"
 #include "kernels_avg.cuh"
 #include "kernels_bf16.cuh"
+#include "ops_internal.h"
 
 using namespace prsgd;
 
@@ -287,6 +288,46 @@ void launch_gemm_f32(prsgd_ctx* c, const GemmF32Args& g) {
   launch_pdl(gemm_f32_kernel<TM, A_PC, B_PC, EPI, FUSE>, grid, dim3(256), 0, c->stream, g);
 }
 
+bool muon_layer(const prsgd_ctx* c, int l) { return (c->muon_layers >> (l - 1)) & 1u; }
+
+// W_l <- W_l - gamma scale_l NS(v_l) for the layers that take the Muon step: at the end of an iteration, when every launch
+// that reads their weights or writes their momentum buffers has been enqueued.
+int muon_steps(prsgd_ctx* c) {
+  for (int l = 1; l <= c->L; ++l) {
+    if (!muon_layer(c, l)) continue;
+    const Layer& ly = c->layer[l - 1];
+    NsPlan p{};
+    p.shape = {c->N, ly.d_out, ly.d_in};
+    p.steps = c->muon_steps; p.a = 3.4445f; p.b = -4.7750f; p.c = 2.0315f; p.eps = 1e-7f;
+    p.precision = c->precision; p.status = c->status;
+    const uint8_t* active = c->has_mask ? c->active : nullptr;
+    p.src.V = c->velocity + ly.w_off; p.src.v_row = ly.d_in; p.src.v_batch = c->m_pad; p.src.active = active;
+    p.dst.out = c->params + ly.w_off; p.dst.type = PRSGD_TYPE_FP32; p.dst.row = ly.d_in; p.dst.batch = c->m_pad; p.dst.active = active;
+    if (c->precision == PRSGD_PRECISION_BF16) {
+      p.src.v_tile = p.dst.tile = tc_wtile(c, l);
+      p.src.v_tiled = p.dst.tiled = p.src.v_tile.tiled;
+      p.dst.shadow = c->shadow + ly.w_off;
+    }
+    const float scale = c->muon_scale == PRSGD_MUON_SCALE_RMS ? 0.2f * std::sqrt((float)std::max(ly.d_out, ly.d_in))
+                                                               : std::sqrt(std::max(1.f, (float)ly.d_out / (float)ly.d_in));
+    p.dst.alpha = -c->gamma * scale; p.dst.beta = 1.f;
+    prof_begin(c, PRSGD_KERNEL_UPDATE);
+    int64_t n = 0;
+    const int rc = ns_run(p, c->muon_work, c->stream, &n);
+    if (rc != PRSGD_OK) return fail(c, rc, g_last_error);
+    c->launches += n;
+    c->open_launches += (int)n - 1;
+    c->upper_weights_quiet = false;
+    prof_end(c);
+  }
+  return PRSGD_OK;
+}
+
+void launch_softmax(prsgd_ctx* c, const SoftmaxArgs& a) {
+  if (c->balance_k > 0) launch_pdl(softmax_ce_balance_kernel, dim3(c->N), dim3(256), 0, c->stream, a, c->balance_coef, c->balance_k);
+  else launch_pdl(softmax_ce_kernel, dim3(c->N, (c->B + 7) / 8), dim3(256), 0, c->stream, a);
+}
+
 // One iteration of Algorithm 1 on the fp32-operand path.
 int step_f32(prsgd_ctx* c, int64_t t, bool averaging) {
   const int L = c->L, B = c->B, N = c->N;
@@ -321,7 +362,7 @@ int step_f32(prsgd_ctx* c, int64_t t, bool averaging) {
     a.Y = c->Y; a.P = c->P; a.B = B; a.C = c->dims[L]; a.draw = dr;
     a.row_losses = c->losses; a.draws = c->draws; a.active = act_mask; a.status = c->status;
     prof_begin(c, PRSGD_KERNEL_SOFTMAX);
-    launch_pdl(softmax_ce_kernel, dim3(N, (B + 7) / 8), dim3(256), 0, c->stream, a);
+    launch_softmax(c, a);
     LAUNCH_CHECK(c);
   }
   for (int l = L; l >= 1; --l) {          // backward, layer by layer: dX_l reads W_l before it is updated
@@ -345,13 +386,13 @@ int step_f32(prsgd_ctx* c, int64_t t, bool averaging) {
     else        g.Bo = {c->buf.act_f32[l - 1], (int64_t)B * ly.d_in, ly.d_in, 1, 0};
     g.M = ly.d_out; g.Nn = ly.d_in; g.K = B; g.N = N; g.draw = dr;
     g.out = c->params; g.out_worker_stride = c->m_pad; g.w_off = ly.w_off; g.b_off = ly.b_off;
-    g.gamma = c->gamma; g.active = act_mask; g.vel = c->velocity; g.mu = c->mu; g.status = c->status;
+    g.gamma = c->gamma; g.keep_weights = muon_layer(c, l) ? 1 : 0; g.active = act_mask; g.vel = c->velocity; g.mu = c->mu; g.status = c->status;
     prof_begin(c, fuse ? PRSGD_KERNEL_UPDATE_AVERAGE : PRSGD_KERNEL_UPDATE);
     if (fuse) launch_gemm_f32<64, false, false, EPI_DW, true>(c, g);
     else      launch_gemm_f32<64, false, false, EPI_DW, false>(c, g);
     LAUNCH_CHECK(c);
   }
-  return PRSGD_OK;
+  return c->muon_layers != 0 ? muon_steps(c) : PRSGD_OK;
 }
 
 // One iteration of Algorithm 1 on the bf16-operand tensor-core path.
@@ -359,13 +400,14 @@ int step_f32(prsgd_ctx* c, int64_t t, bool averaging) {
 int step_bf16(prsgd_ctx* c, int64_t t, bool averaging, bool more_follow) {
   const int L = c->L, N = c->N;
   const uint8_t* act_mask = worker_mask(c);
-  const bool fuse = averaging && c->fused_average;
+  const bool muon = c->muon_layers != 0;               // its layers' steps follow the backward pass, as launches of their own
+  const bool fuse = averaging && c->fused_average && !muon;
   const bool avg_vel = c->velocity != nullptr && c->average_velocity;
   const DrawArgs dr = draw_args(c, t);
   // Layer 1's update can form a_1 of iteration t + 1 as well (its input is the data pool), which saves that
   // iteration's first forward launch and the write of W_1's shadow: only on a plain SGD iteration that is
   // not an averaging one and is followed by another one of the same call.
-  const bool next_fwd = c->next_forward && more_follow && !averaging && L > 1 && tc_epilogues_fused(c);
+  const bool next_fwd = c->next_forward && more_follow && !averaging && L > 1 && tc_epilogues_fused(c) && !muon;
   const bool skip_f1 = c->a1_ready;
   c->a1_ready = false;
   if (!skip_f1) c->a1_sel = 0;          // this iteration's first forward launch writes a_1: into the first buffer
@@ -397,12 +439,12 @@ int step_bf16(prsgd_ctx* c, int64_t t, bool averaging, bool more_follow) {
     a.Y = c->Y; a.P = c->P; a.B = c->B; a.C = c->dims[L]; a.draw = dr;
     a.row_losses = c->losses; a.draws = c->draws; a.active = act_mask; a.status = c->status;
     prof_begin(c, PRSGD_KERNEL_SOFTMAX);
-    launch_pdl(softmax_ce_kernel, dim3(N, (c->B + 7) / 8), dim3(256), 0, c->stream, a);
+    launch_softmax(c, a);
     LAUNCH_CHECK(c);
   }
   // Layers >= 2 whose update is the plain SGD step: one launch forms dZ_{l-1} and applies the step of W_l (the
   // fused update + average of an averaging iteration owns a tile across workers instead and keeps dX separate).
-  const bool dx_in_upd = c->dx_in_update && tc_epilogues_fused(c);
+  const bool dx_in_upd = c->dx_in_update && tc_epilogues_fused(c) && !muon;
   if (head) {
     prof_begin(c, PRSGD_KERNEL_HEAD);
     tc_launch_head(c, dr, act_mask, head_fwd);
@@ -473,7 +515,11 @@ int step_bf16(prsgd_ctx* c, int64_t t, bool averaging, bool more_follow) {
             c->no_early_once = true;
           }
         } else {
+          // (Muon: this launch leaves the weights where they are, at rate 0, and updates the momentum buffers)
+          const float gamma = c->gamma;
+          if (muon_layer(c, l)) c->gamma = 0.f;
           tc_launch_update(c, l, dr, act_mask, fuse_l, false, late);
+          c->gamma = gamma;
         }
         LAUNCH_CHECK(c);
       }
@@ -514,7 +560,7 @@ int step_bf16(prsgd_ctx* c, int64_t t, bool averaging, bool more_follow) {
   // a plain iteration ends with layer 1's update: nothing in flight writes W_2..W_L, unless layer 2's update was
   // enqueued last; a fused averaging iteration ends with launches that write them
   c->upper_weights_quiet = !deferred && !fuse;
-  return PRSGD_OK;
+  return muon ? muon_steps(c) : PRSGD_OK;
 }
 
 int launch_average(prsgd_ctx* c) {
@@ -765,7 +811,7 @@ int run_iterations_on_stream(prsgd_ctx* c, int64_t t_first, int64_t count, int64
     const bool more_follow = t + 1 < t_call_end;
     int rc = c->precision == PRSGD_PRECISION_BF16 ? step_bf16(c, t, averaging, more_follow) : step_f32(c, t, averaging);
     // (the fp32 path has no fused form for the momentum step)
-    const bool separate_average = !c->fused_average || (c->velocity != nullptr && c->precision == PRSGD_PRECISION_FP32);
+    const bool separate_average = !c->fused_average || c->muon_layers != 0 || (c->velocity != nullptr && c->precision == PRSGD_PRECISION_FP32);
     if (rc == PRSGD_OK && averaging && separate_average) rc = launch_average(c);
     if (rc != PRSGD_OK) {
       c->a1_ready = false;      // a launch failed: the next iteration must not count on an a_1 formed ahead
@@ -800,7 +846,7 @@ int run_iterations(prsgd_ctx* c, int64_t t_first, int64_t count) {
     // the run of plain iterations that starts here
     int64_t plain = 0;
     while (t + plain < t_end && !(c->I > 0 && ((t + plain) % c->I) == 0)) ++plain;
-    const bool grouped = c->worker_groups > 1 && c->precision == PRSGD_PRECISION_BF16 && !c->has_mask && !c->profile &&
+    const bool grouped = c->worker_groups > 1 && c->precision == PRSGD_PRECISION_BF16 && !c->has_mask && !c->profile && c->muon_layers == 0 &&
                          plain >= 2 && c->N >= 2 * c->worker_groups;
     if (!grouped) {
       const int64_t n = plain > 0 ? plain : 1;           // the plain run, or the averaging iteration it ends at
@@ -837,7 +883,7 @@ int run_iterations(prsgd_ctx* c, int64_t t_first, int64_t count) {
   return PRSGD_OK;
 }
 
-void period_key(const prsgd_ctx* c, uint64_t (&key)[13]) {
+void period_key(const prsgd_ctx* c, uint64_t (&key)[16]) {
   uint32_t gbits, mbits;
   std::memcpy(&gbits, &c->gamma, 4);
   std::memcpy(&mbits, &c->mu, 4);
@@ -849,13 +895,18 @@ void period_key(const prsgd_ctx* c, uint64_t (&key)[13]) {
             ((uint64_t)c->worker_groups << 3) | ((uint64_t)c->dx_shared_pair << 6) | ((uint64_t)c->head_kernel << 7) |
             ((uint64_t)c->common_point << 9) | ((uint64_t)c->split_blocks << 11) | ((uint64_t)c->head_forward << 13) |
             ((uint64_t)c->merged_small_average << 14) | ((uint64_t)c->tiled_weights << 15) | ((uint64_t)c->overlap_update << 16);      // (rows_identical: the period's first iteration may share reads)
+  uint32_t cbits;
+  std::memcpy(&cbits, &c->balance_coef, 4);
+  key[13] = (uint64_t)c->muon_layers | ((uint64_t)c->muon_scale << 16) | ((uint64_t)c->muon_steps << 17);
+  key[14] = reinterpret_cast<uint64_t>(c->muon_work);
+  key[15] = (uint64_t)cbits | ((uint64_t)c->balance_k << 32);
 }
 
 // One whole averaging period (I iterations starting right after an average) as a CUDA graph: the
 // kernels take the iteration number as device counter + offset, so one capture serves every period.
 // Returns nullptr when capture is not possible (the caller then launches directly).
 prsgd_ctx::PeriodGraph* get_period_graph(prsgd_ctx* c) {
-  uint64_t key[13];
+  uint64_t key[16];
   period_key(c, key);
   for (auto& g : c->graphs)
     if (std::memcmp(g.key, key, sizeof key) == 0) return &g;
@@ -956,7 +1007,15 @@ int prsgd_local_steps_sum(prsgd_ctx* c, int64_t k) {
   // iteration t + k: the local step in its fused form, with the summed rows divided by 1 instead of N
   c->avg_divisor = 1.f;
   const int fused_keep = c->fused_average;
-  if (c->precision == PRSGD_PRECISION_BF16) {
+  if (c->precision == PRSGD_PRECISION_BF16 && c->muon_layers != 0) {      // (no fused form)
+    rc = step_bf16(c, c->t + k, /*averaging=*/false, /*more_follow=*/false);
+    if (rc == PRSGD_OK) {
+      prof_begin(c, PRSGD_KERNEL_AVERAGE);
+      average_rows_kernel<0, true><<<grid1d(c->m_pad / 4, 256), 256, 0, c->stream>>>(c->params, c->N, c->m_pad, c->m_pad, nullptr,
+                                                                                   c->shadow, c->status, 1.f);
+      LAUNCH_CHECK(c);
+    }
+  } else if (c->precision == PRSGD_PRECISION_BF16) {
     c->fused_average = 1;
     rc = step_bf16(c, c->t + k, /*averaging=*/true, /*more_follow=*/false);
   } else {
@@ -1034,7 +1093,7 @@ int prsgd_get_average(prsgd_ctx* c, float* dst, int dst_on_device) {
 int prsgd_enable_momentum(prsgd_ctx* c, float mu, void* d_velocity, int average_velocity) {
   if (!c) return fail(nullptr, PRSGD_ERR_ARG, "ctx is NULL");
   if (d_velocity == nullptr) {                 // back to plain SGD
-    c->velocity = nullptr; c->mu = 0.f; c->average_velocity = 0;
+    c->velocity = nullptr; c->mu = 0.f; c->average_velocity = 0; c->muon_layers = 0;
     return PRSGD_OK;
   }
   if (!(mu >= 0.f && mu < 1.f)) return fail(c, PRSGD_ERR_ARG, "mu must be in [0, 1)");
@@ -1046,6 +1105,52 @@ int prsgd_enable_momentum(prsgd_ctx* c, float mu, void* d_velocity, int average_
     int trc = tc_bind_velocity(c, &terr);
     if (trc != PRSGD_OK) { c->velocity = nullptr; c->mu = 0.f; return fail(c, trc, terr); }
   }
+  return PRSGD_OK;
+}
+
+static int muon_sizes(prsgd_ctx* c, uint32_t layers, size_t* bytes) {
+  if (!c) return fail(nullptr, PRSGD_ERR_ARG, "ctx is NULL");
+  if (layers >> c->L) return fail(c, PRSGD_ERR_ARG, "a bit of layers names no layer of the model");
+  size_t most = 0;
+  for (int l = 1; l <= c->L; ++l) {
+    if (!((layers >> (l - 1)) & 1u)) continue;
+    if (c->dims[l] > PRSGD_ORTHO_MAX_SIDE || c->dims[l - 1] > PRSGD_ORTHO_MAX_SIDE) return fail(c, PRSGD_ERR_SIZE, "a layer's side is above PRSGD_ORTHO_MAX_SIDE");
+    most = std::max(most, ns_workspace_bytes({c->N, c->dims[l], c->dims[l - 1]}, c->precision));
+  }
+  *bytes = most;
+  return PRSGD_OK;
+}
+
+int prsgd_muon_workspace_bytes(prsgd_ctx* c, uint32_t layers, size_t* bytes) {
+  if (!bytes) return fail(c, PRSGD_ERR_ARG, "bytes is NULL");
+  return muon_sizes(c, layers, bytes);
+}
+
+int prsgd_enable_muon(prsgd_ctx* c, uint32_t layers, int32_t scale_rule, int32_t steps, void* d_work, size_t work_bytes) {
+  size_t need = 0;
+  int rc = muon_sizes(c, layers, &need);
+  if (rc != PRSGD_OK) return rc;
+  if (layers == 0) { c->muon_layers = 0; return PRSGD_OK; }
+  if (!c->velocity) return fail(c, PRSGD_ERR_STATE, "prsgd_enable_momentum must come before prsgd_enable_muon");
+  if (scale_rule != PRSGD_MUON_SCALE_SPECTRAL && scale_rule != PRSGD_MUON_SCALE_RMS) return fail(c, PRSGD_ERR_ARG, "unknown scale rule");
+  if (steps < 1 || steps > PRSGD_ORTHO_MAX_STEPS) return fail(c, PRSGD_ERR_ARG, "steps must be in 1..PRSGD_ORTHO_MAX_STEPS");
+  if (!d_work || work_bytes < need) return fail(c, PRSGD_ERR_SIZE, "workspace is NULL or smaller than prsgd_muon_workspace_bytes");
+  if (!aligned(d_work, 256)) return fail(c, PRSGD_ERR_ALIGN, "d_work must be 256-byte aligned");
+  rc = ns_prepare();
+  if (rc != PRSGD_OK) return fail(c, rc, g_last_error);
+  c->muon_layers = layers; c->muon_scale = scale_rule; c->muon_steps = steps; c->muon_work = d_work;
+  c->a1_ready = false;
+  return PRSGD_OK;
+}
+
+int prsgd_set_balance(prsgd_ctx* c, float coef, int32_t top_k) {
+  if (!c) return fail(nullptr, PRSGD_ERR_ARG, "ctx is NULL");
+  if (top_k == 0) { c->balance_k = 0; c->balance_coef = 0.f; c->a1_ready = false; return PRSGD_OK; }
+  if (!std::isfinite(coef)) return fail(c, PRSGD_ERR_ARG, "coef must be finite");
+  if (top_k < 0 || top_k > c->dims[c->L] || top_k > PRSGD_ROUTE_MAX_K) return fail(c, PRSGD_ERR_ARG, "top_k must be in 0..min(d_L, PRSGD_ROUTE_MAX_K)");
+  if (c->dims[c->L] > kBalanceMaxClasses) return fail(c, PRSGD_ERR_SIZE, "more classes than PRSGD_ROUTE_MAX_EXPERTS");
+  c->balance_coef = coef; c->balance_k = top_k;
+  c->a1_ready = false;
   return PRSGD_OK;
 }
 

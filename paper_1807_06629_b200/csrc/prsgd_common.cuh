@@ -128,6 +128,12 @@ struct prsgd_ctx {
   float mu = 0.f;                // momentum of the local step (0 = plain SGD)
   float* velocity = nullptr;     // [N][m_pad] fp32 momentum buffers, caller-owned
   int average_velocity = 0;      // average the buffers together with the models
+  // Muon step of the weights of some layers (prsgd_enable_muon), with the momentum buffers above
+  uint32_t muon_layers = 0;      // bit l - 1: layer l (0 = off)
+  int muon_scale = 0, muon_steps = 0;
+  void* muon_work = nullptr;     // caller-owned
+  float balance_coef = 0.f;      // balance loss over the classes (prsgd_set_balance); top_k 0 = off
+  int balance_k = 0;
   int upd_tile = 0;              // column width of the update kernel's tile: 0 = chosen per launch, 64 or 128
   int dx_shared_pair = 1;        // 64-wide update + dX: one pair of bf16 tiles behind the stages (more stages) instead of one per stage
   int split_blocks = 0;          // layer 1's update + next forward: row blocks cut at run boundaries so that every CTA streams the same number of tiles
@@ -206,7 +212,7 @@ struct prsgd_ctx {
 
   // whole averaging periods captured as CUDA graphs (PRSGD_OPT_GRAPH)
   struct PeriodGraph {
-    uint64_t key[13];
+    uint64_t key[16];
     cudaGraphExec_t exec;
     int64_t launches;            // kernel launches one replay stands for
   };
