@@ -528,7 +528,7 @@ int prsgd_orthogonalize(const void* d_G, int32_t g_type, int64_t g_row_stride, i
 /* Muon step of a batch of weight matrices, in place:
  *   V <- mu V + G;  U = V, or G + mu V when nesterov is set;
  *   W <- (1 - lr weight_decay) W - lr scale NS(U),  NS as in prsgd_orthogonalize (same workspace size).
- * V is fp32; W and G are of any element type.  sqrt(max(1, rows / cols)) and 0.2 sqrt(max(rows, cols)) are the usual
+ * V is fp32; W and G are of any element type.  mu in [0, 1); lr * weight_decay must not be 1.  sqrt(max(1, rows / cols)) and 0.2 sqrt(max(rows, cols)) are the usual
  * choices of scale. */
 int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_batch_stride,
                     float* d_V, int64_t v_row_stride, int64_t v_batch_stride,
@@ -562,7 +562,7 @@ int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t 
 /* Gradient of sum_g dloss_g loss_g + sum dweights * weights with respect to the logits, the choice of experts and the
  * counts held fixed: with h_te = dloss coef E counts_e / (top_k T) / T + [e chosen by t] d/dp of the weights' part,
  *   dlogit_te = p_te (h_te - sum_j p_tj h_tj).
- * d_experts, d_counts: as prsgd_route wrote them (T is taken from the counts).  d_dweights [groups][tokens][top_k] or
+ * d_experts, d_counts: as prsgd_route wrote them, a token's experts distinct (T is taken from the counts).  d_dweights [groups][tokens][top_k] or
  * NULL, d_dloss [groups] or NULL (zero).  dlogits has the logits' type and may be the logits themselves (same strides);
  * rows of padding tokens are written as zeros. */
 int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int64_t group_stride, const uint8_t* d_live,

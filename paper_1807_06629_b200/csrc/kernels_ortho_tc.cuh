@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
 
   // The next task from the ring, for a whole warp; kind < 0 at the end or when a wait gave up.  Whoever gets it may read
   // what the task depends on: the scheduler saw it done (acquire) before it sent the task, and it is read where it was
-  // made visible, in L2 (TMA behind a proxy fence, cp.async.cg, ld.cg), never through an L1 that could hold older values.
+  // made visible, in L2 (TMA behind a proxy fence, ld.cg), never through an L1 that could hold older values.
   auto next_task = [&](int n) -> NsTask {
     const int r = n % kNsRing;
     NsTask k;
@@ -354,120 +354,120 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   // MMAs then take longer than an MMA (720 cycles instead of 512 per block of 64 measured).
   // With 32-bit precision the epilogue's sums take registers from the other warps: 128 * 64 + 256 * 216 of the launch's 384 * 168.
   if (warp < 4) {
-  if constexpr (SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-  if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
-    const bool second = warp == 3, issue = ptx::elect_one();
-    uint32_t s = 0, phase = 1;                           // (a fresh barrier passes a wait for the phase before its first)
-    for (int n = 0;; ++n) {
-      const NsTask k = next_task(n);
-      if (k.kind < 0) break;
-      if (issue) { free_task(n); ptx::fence_proxy_async_all(); }
-      const int from = k.step & 1;
-      const int K = k.kind == 0 ? a.l : a.s;
-      const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
-      const bool of_x = k.kind == 0 || (k.kind == 2 && second != (a.tall != 0));
-      const bool x_mn = k.kind == 0 ? a.tall != 0 : second;                      // (of X)
-      const int tile = second ? k.tj : k.ti, at0 = tile * 256 + (int)rank * 128;
-      const int ask = max(0, blocks - kNsAhead);
-      bool ok = true;
-      for (int p = 0, b = 0; p < (SPLIT ? 3 : 1) && ok; ++p) {
-        const int part = SPLIT && p == (second ? 1 : 0) ? 1 : 0;       // lo hi, hi lo, hi hi: the small ones first
-        const CUtensorMap* map_mn = of_x ? &maps.x[from][part] : k.kind == 1 ? &maps.A[part] : &maps.P[part];
-        const CUtensorMap* map_k = of_x ? &maps.xk[from][part] : k.kind == 1 ? &maps.Ak[part] : &maps.Pk[part];
-        for (int q = 0; q < kb; ++q, ++b) {
-          const bool mn = of_x ? x_mn : (q >> 2) < tile;               // (symmetric: below the diagonal the transpose is stored)
-          if (!ptx::warp_wait(empty((int)s), phase, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
-          if (issue) {
-            if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kNsStageBytes);
-            const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kNsStageBytes + (second ? 16384u : 0u);
-            if (mn) {
-              ptx::tma_load_3d_pair(at, map_mn, fb, at0, q * 64, k.m);
-              ptx::tma_load_3d_pair(at + 8192u, map_mn, fb, at0 + 64, q * 64, k.m);
-            } else {
-              ptx::tma_load_3d_pair(at, map_k, fb, q * 64, at0, k.m);
+    if constexpr (SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
+      const bool second = warp == 3, issue = ptx::elect_one();
+      uint32_t s = 0, phase = 1;                           // (a fresh barrier passes a wait for the phase before its first)
+      for (int n = 0;; ++n) {
+        const NsTask k = next_task(n);
+        if (k.kind < 0) break;
+        if (issue) { free_task(n); ptx::fence_proxy_async_all(); }
+        const int from = k.step & 1;
+        const int K = k.kind == 0 ? a.l : a.s;
+        const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
+        const bool of_x = k.kind == 0 || (k.kind == 2 && second != (a.tall != 0));
+        const bool x_mn = k.kind == 0 ? a.tall != 0 : second;                      // (of X)
+        const int tile = second ? k.tj : k.ti, at0 = tile * 256 + (int)rank * 128;
+        const int ask = max(0, blocks - kNsAhead);
+        bool ok = true;
+        for (int p = 0, b = 0; p < (SPLIT ? 3 : 1) && ok; ++p) {
+          const int part = SPLIT && p == (second ? 1 : 0) ? 1 : 0;       // lo hi, hi lo, hi hi: the small ones first
+          const CUtensorMap* map_mn = of_x ? &maps.x[from][part] : k.kind == 1 ? &maps.A[part] : &maps.P[part];
+          const CUtensorMap* map_k = of_x ? &maps.xk[from][part] : k.kind == 1 ? &maps.Ak[part] : &maps.Pk[part];
+          for (int q = 0; q < kb; ++q, ++b) {
+            const bool mn = of_x ? x_mn : (q >> 2) < tile;               // (symmetric: below the diagonal the transpose is stored)
+            if (!ptx::warp_wait(empty((int)s), phase, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
+            if (issue) {
+              if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kNsStageBytes);
+              const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kNsStageBytes + (second ? 16384u : 0u);
+              if (mn) {
+                ptx::tma_load_3d_pair(at, map_mn, fb, at0, q * 64, k.m);
+                ptx::tma_load_3d_pair(at + 8192u, map_mn, fb, at0 + 64, q * 64, k.m);
+              } else {
+                ptx::tma_load_3d_pair(at, map_k, fb, q * 64, at0, k.m);
+              }
+              if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
             }
-            if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
+            __syncwarp();
+            if (++s == kNsStages) { s = 0; phase ^= 1u; }
+          }
+        }
+        if (!ok) break;
+      }
+    } else if (warp == 1 && rank == 0) {                   // ---- products (the leader issues for the pair) --------------
+      const bool issue = ptx::elect_one();
+      uint32_t s = 0, phase = 0, sums = 0;
+      for (int n = 0;; ++n) {
+        const NsTask k = next_task(n);
+        if (k.kind < 0) break;
+        if (issue) free_task(n);
+        const int K = k.kind == 0 ? a.l : a.s;
+        const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
+        // blocks of 64 below which the operands lie MN-major
+        const int a_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && a.tall) ? 0 : 4 * k.ti;
+        const int b_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && !a.tall) ? kb : 4 * k.tj;
+        bool ok = true;
+        int next = 0;                                      // block that starts a new sum
+        uint32_t acc = 0;
+        for (int q = 0, qk = 0; q < blocks; ++q) {
+          const bool first = q == next;
+          if (first) {
+            next = !SPLIT ? blocks : q < 2 * kb ? 2 * kb : q + kNsPromote;
+            acc = sums & 1u;
+            if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
+            ptx::tc_fence_after();
+            ++sums;
+          }
+          if (!ptx::warp_wait(full((int)s), phase, ab, status, NS_ERR_FULL)) { ok = false; break; }
+          ptx::tc_fence_after();
+          if (issue) {
+            const bool a_mn = qk < a_mn_until, b_mn = qk < b_mn_until;
+            const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn);
+            // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
+            const uint64_t at = s * (kNsStageBytes >> 4), da_k = a_mn ? 128u : 2u, db_k = b_mn ? 128u : 2u;
+            const uint64_t da = at + (a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u));
+            const uint64_t db = at + (b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u));
+  #pragma unroll
+            for (uint32_t h = 0; h < 4; ++h)
+              ptx::mma_f16_pair(tmem + acc * 256u, da + h * da_k, db + h * db_k, idesc, !first || h != 0 ? 1u : 0u);
+            ptx::mma_commit_pair(empty((int)s));
+            if (q + 1 == blocks || q + 1 == next) ptx::mma_commit_pair(tfull((int)acc));
           }
           __syncwarp();
           if (++s == kNsStages) { s = 0; phase ^= 1u; }
+          if (++qk == kb) qk = 0;
         }
+        if (!ok) break;
       }
-      if (!ok) break;
-    }
-  } else if (warp == 1 && rank == 0) {                   // ---- products (the leader issues for the pair) --------------
-    const bool issue = ptx::elect_one();
-    uint32_t s = 0, phase = 0, sums = 0;
-    for (int n = 0;; ++n) {
-      const NsTask k = next_task(n);
-      if (k.kind < 0) break;
-      if (issue) free_task(n);
-      const int K = k.kind == 0 ? a.l : a.s;
-      const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
-      // blocks of 64 below which the operands lie MN-major
-      const int a_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && a.tall) ? 0 : 4 * k.ti;
-      const int b_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && !a.tall) ? kb : 4 * k.tj;
-      bool ok = true;
-      int next = 0;                                      // block that starts a new sum
-      uint32_t acc = 0;
-      for (int q = 0, qk = 0; q < blocks; ++q) {
-        const bool first = q == next;
-        if (first) {
-          next = !SPLIT ? blocks : q < 2 * kb ? 2 * kb : q + kNsPromote;
-          acc = sums & 1u;
-          if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, NS_ERR_ACC_FREE)) { ok = false; break; }
-          ptx::tc_fence_after();
-          ++sums;
+    } else if (warp == 2 && lane == 0 && rank == 0) {      // ---- claims tiles for the pair --------------------------------
+      for (int n = 0;; ++n) {
+        const int r = n % kNsRing;
+        // Not before the last loads of the tile before are being issued: a tile claimed sooner would only keep those that
+        // depend on it waiting.  (Claiming, handing on and the panels' counters take about 2 us.)
+        if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
+        if (n >= kNsRing && !ptx::mbar_wait(sempty(r), (uint32_t)(((n / kNsRing) - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
+        NsTask k;
+        k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
+        for (;;) {
+          const int t = (int)atomicAdd(a.buf.claim, 1u);
+          if (t >= a.total || (n == 0 && !a.buf.own_status && status->error != 0u)) break;
+          const NsTask got = ns_decode(a, t);
+          if (a.dst.active != nullptr && a.dst.active[got.m] == 0) continue;
+          k = got;
+          break;
         }
-        if (!ptx::warp_wait(full((int)s), phase, ab, status, NS_ERR_FULL)) { ok = false; break; }
-        ptx::tc_fence_after();
-        if (issue) {
-          const bool a_mn = qk < a_mn_until, b_mn = qk < b_mn_until;
-          const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn);
-          // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
-          const uint64_t at = s * (kNsStageBytes >> 4), da_k = a_mn ? 128u : 2u, db_k = b_mn ? 128u : 2u;
-          const uint64_t da = at + (a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u));
-          const uint64_t db = at + (b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u));
-#pragma unroll
-          for (uint32_t h = 0; h < 4; ++h)
-            ptx::mma_f16_pair(tmem + acc * 256u, da + h * da_k, db + h * db_k, idesc, !first || h != 0 ? 1u : 0u);
-          ptx::mma_commit_pair(empty((int)s));
-          if (q + 1 == blocks || q + 1 == next) ptx::mma_commit_pair(tfull((int)acc));
+        if (k.kind >= 0 && k.need > 0 &&
+            !(ptx::flag_wait(a.buf.done + k.pi, (unsigned)k.need, ab, status, NS_ERR_DEP) &&
+              (k.pj == k.pi || ptx::flag_wait(a.buf.done + k.pj, (unsigned)k.need, ab, status, NS_ERR_DEP))))
+          break;
+  #pragma unroll
+        for (uint32_t c = 0; c < 2; ++c) {
+          ptx::send_v4(ptx::cluster_map(ptx::smem_u32(&ring[r]), c), ptx::cluster_map(sfull(r), c),
+                       make_uint4((uint32_t)k.kind, (uint32_t)k.m, (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
         }
-        __syncwarp();
-        if (++s == kNsStages) { s = 0; phase ^= 1u; }
-        if (++qk == kb) qk = 0;
+        if (k.kind < 0) break;
       }
-      if (!ok) break;
     }
-  } else if (warp == 2 && lane == 0 && rank == 0) {      // ---- claims tiles for the pair --------------------------------
-    for (int n = 0;; ++n) {
-      const int r = n % kNsRing;
-      // Not before the last loads of the tile before are being issued: a tile claimed sooner would only keep those that
-      // depend on it waiting.  (Claiming, handing on and the panels' counters take about 2 us.)
-      if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
-      if (n >= kNsRing && !ptx::mbar_wait(sempty(r), (uint32_t)(((n / kNsRing) - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
-      NsTask k;
-      k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
-      for (;;) {
-        const int t = (int)atomicAdd(a.buf.claim, 1u);
-        if (t >= a.total || (n == 0 && !a.buf.own_status && status->error != 0u)) break;
-        const NsTask got = ns_decode(a, t);
-        if (a.dst.active != nullptr && a.dst.active[got.m] == 0) continue;
-        k = got;
-        break;
-      }
-      if (k.kind >= 0 && k.need > 0 &&
-          !(ptx::flag_wait(a.buf.done + k.pi, (unsigned)k.need, ab, status, NS_ERR_DEP) &&
-            (k.pj == k.pi || ptx::flag_wait(a.buf.done + k.pj, (unsigned)k.need, ab, status, NS_ERR_DEP))))
-        break;
-#pragma unroll
-      for (uint32_t c = 0; c < 2; ++c) {
-        ptx::send_v4(ptx::cluster_map(ptx::smem_u32(&ring[r]), c), ptx::cluster_map(sfull(r), c),
-                     make_uint4((uint32_t)k.kind, (uint32_t)k.m, (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
-      }
-      if (k.kind < 0) break;
-    }
-  }
   } else {                                               // ---- epilogue ---------------------------------------------
     if constexpr (SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int quarter = warp & 3, share = (warp - 4) >> 2;

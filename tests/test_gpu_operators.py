@@ -411,6 +411,54 @@ def test_route_grad_against_differences_of_the_kernel_itself(b):
             assert abs((f[0] - f[1]) / 2e-2 - grad[0, t, e].item()) <= 5e-5
 
 
+# ---- beyond 32 bits, and a first call inside a capture ---------------------------------------------------------
+def test_offsets_beyond_32_bits(b):
+    """Groups and matrices more than 2^31 elements apart."""
+    far = (1 << 31) + 4096
+    buf = torch.zeros(far + 20000, dtype=BF16, device="cuda:0")
+    x = buf.as_strided((2, 50, 64), (far, 64, 1))
+    x.copy_(logits_of(90, 2, 50, 64, BF16))
+    check_route(b, x, 4)
+    chosen, _, counts, _, _ = ref.route(x, 4, 0.05)
+    dl = torch.ones(2, device="cuda:0") * 50
+    want = b.prsgd_route_grad(x.contiguous(), chosen.int(), counts.int(), 0.05, dloss=dl)
+    assert torch.equal(b.prsgd_route_grad(x, chosen.int(), counts.int(), 0.05, dloss=dl, out=x), want) and torch.equal(x, want)
+    for shape in ((2, 60, 80), (2, 140, 130)):         # both forms of the chain
+        G = buf.as_strided(shape, (far, shape[2], 1))
+        G.copy_(matrices(91, *shape, dtype=BF16))
+        want = b.prsgd_orthogonalize(G.contiguous())
+        assert torch.equal(b.prsgd_orthogonalize(G), want)
+        assert torch.equal(b.prsgd_orthogonalize(G, out=G), want) and torch.equal(G, want)
+
+
+def test_a_process_whose_first_call_is_captured(b):
+    """The library finds out what it needs of the device on the first call, which may be inside a capture."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_1807_06629_b200 import binding as b
+G = [torch.randn(2, 40, 90, device="cuda:0"), torch.randn(2, 200, 300, device="cuda:0")]
+x = torch.randn(2, 30, 16, device="cuda:0")
+work = [b.orthogonalize_workspace(g) for g in G]
+out, outs, w = [torch.empty_like(g) for g in G], b.route_outputs(x, 2), b.route_workspace(x)
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    for g, o, k in zip(G, out, work):
+        b.prsgd_orthogonalize(g, out=o, workspace=k)
+    b.prsgd_route(x, 2, 0.1, out=outs, workspace=w)
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(b.prsgd_orthogonalize(g), o) for g, o in zip(G, out))
+assert all(torch.equal(p, q) for p, q in zip(b.prsgd_route(x, 2, 0.1), outs))
+print("same")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "same" in run.stdout, run.stderr[-2000:]
+
+
 # ---- together ------------------------------------------------------------------------------------------------
 def test_a_period_of_router_training(b):
     """What the operators are for: N workers train a router's weights by local Muon steps on the balance loss and the
