@@ -40,35 +40,56 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sums a group's partial results in block order and forms its loss; all 256 threads of a block.
+// Sums a group's partial results in a fixed order and forms its loss; all 256 threads of a block.  Each warp takes every
+// eighth block's sums, lanes along the experts, so that their loads are in flight together (a thread per expert that
+// walked all blocks took 16 us for 18 blocks of 100 experts).
 __device__ __forceinline__ void route_finish(const RouteArgs& a, int64_t g) {
+  __shared__ float s_p[8][256];
+  __shared__ int s_c[8][256];
   __shared__ float s_w[8];
   __shared__ int s_alive;
-  if (threadIdx.x < 32) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (warp == 0) {
     int n = 0;
-    for (int b = threadIdx.x; b < a.blocks; b += 32) n += a.part_n[g * a.blocks + b];
+    for (int b = lane; b < a.blocks; b += 32) n += a.part_n[g * a.blocks + b];
     n = __reduce_add_sync(0xffffffffu, n);
-    if (threadIdx.x == 0) s_alive = n;
+    if (lane == 0) s_alive = n;
   }
-  __syncthreads();
-  const float live = s_alive > 0 ? (float)s_alive : 1.f;
   float mine = 0.f;
-  for (int e = threadIdx.x; e < a.E; e += 256) {
-    float p = 0.f; int c = 0;
-    const float* pp = a.part_p + g * a.blocks * a.E + e;
-    const int32_t* pc = a.part_c + g * a.blocks * a.E + e;
-#pragma unroll 8
-    for (int b = 0; b < a.blocks; ++b) { p += pp[(int64_t)b * a.E]; c += pc[(int64_t)b * a.E]; }
-    p /= live;
-    a.mean[g * a.E + e] = p;
-    a.counts[g * a.E + e] = c;
-    mine += ((float)c / ((float)a.k * live)) * p;
+  for (int e0 = 0; e0 < a.E; e0 += 256) {
+    for (int e = e0 + lane; e < min(a.E, e0 + 256); e += 32) {
+      float p = 0.f;
+      int c = 0;
+#pragma unroll 4
+      for (int b = warp; b < a.blocks; b += 8) {
+        const int64_t at = (g * a.blocks + b) * a.E + e;
+        p += a.part_p[at];
+        c += a.part_c[at];
+      }
+      s_p[warp][e - e0] = p;
+      s_c[warp][e - e0] = c;
+    }
+    __syncthreads();
+    const float live = s_alive > 0 ? (float)s_alive : 1.f;
+    const int e = e0 + (int)threadIdx.x;
+    if (e < a.E) {
+      float p = 0.f;
+      int c = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) { p += s_p[w][threadIdx.x]; c += s_c[w][threadIdx.x]; }
+      p /= live;
+      a.mean[g * a.E + e] = p;
+      a.counts[g * a.E + e] = c;
+      mine += ((float)c / ((float)a.k * live)) * p;
+    }
+    __syncthreads();
   }
   mine = warp_sum(mine);
-  if ((threadIdx.x & 31) == 0) s_w[threadIdx.x >> 5] = mine;
+  if (lane == 0) s_w[warp] = mine;
   __syncthreads();
   if (threadIdx.x == 0) {
     float s = 0.f;
+#pragma unroll
     for (int w = 0; w < 8; ++w) s += s_w[w];
     a.loss[g] = a.coef * (float)a.E * s;
   }
@@ -80,11 +101,40 @@ __global__ void __launch_bounds__(256) route_finish_kernel(const RouteArgs a) {
   route_finish(a, blockIdx.x);
 }
 
-// What a block adds to its group: slot b of the group's partial sums, or, of a group of one block, the group's results.
-__device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g) {
-  if (a.blocks == 1) {
-    __syncthreads();                                  // (the block's own global writes, visible to its threads)
-    route_finish(a, g);
+// What a block adds to its group (p: its 8 warps' sums over tokens, n tokens): a row of the group's partial sums, or, of a
+// group of one block, the group's results.
+template <int W>
+__device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g, const float (&p)[8][W], const int* c, int n) {
+  __shared__ float s_loss[8];
+  const int64_t slot = g * a.blocks + blockIdx.x;
+  const float live = n > 0 ? (float)n : 1.f;
+  float mine = 0.f;
+  for (int e = threadIdx.x; e < a.E; e += 256) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += p[w][e];
+    if (a.blocks > 1) {
+      a.part_p[slot * a.E + e] = s;
+      a.part_c[slot * a.E + e] = c[e];
+    } else {
+      s /= live;
+      a.mean[g * a.E + e] = s;
+      a.counts[g * a.E + e] = c[e];
+      mine += ((float)c[e] / ((float)a.k * live)) * s;
+    }
+  }
+  if (a.blocks > 1) {
+    if (threadIdx.x == 0) a.part_n[slot] = n;
+    return;
+  }
+  mine = warp_sum(mine);
+  if ((threadIdx.x & 31) == 0) s_loss[threadIdx.x >> 5] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += s_loss[w];
+    a.loss[g] = a.coef * (float)a.E * s;
   }
 }
 
@@ -171,16 +221,7 @@ __global__ void __launch_bounds__(256, 2) route_kernel(const RouteArgs a) {
   for (int i = 0; i < PER; ++i) s_p[warp][lane + 32 * i] = acc[i];
   if (lane == 0 && alive) atomicAdd(&s_n, alive);
   __syncthreads();
-  const int64_t slot = g * a.blocks + blockIdx.x;
-  for (int e = threadIdx.x; e < a.E; e += 256) {
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) s += s_p[w][e];
-    a.part_p[slot * a.E + e] = s;
-    a.part_c[slot * a.E + e] = s_c[e];
-  }
-  if (threadIdx.x == 0) a.part_n[slot] = s_n;
-  route_leave(a, g);
+  route_leave(a, g, s_p, s_c, s_n);
 }
 
 // ---- top_k <= 8: a few lanes per token ------------------------------------------------------------------------
@@ -417,23 +458,15 @@ __global__ void __launch_bounds__(256, 2) route_lanes_kernel(const RouteArgs a) 
   alive = __reduce_add_sync(0xffffffffu, alive);
   if (lane == 0 && alive) atomicAdd(&s_n, alive);
   __syncthreads();
-  const int64_t slot = g * a.blocks + blockIdx.x;
-  for (int e = threadIdx.x; e < a.E; e += 256) {
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) s += s_p[w][e];
-    a.part_p[slot * a.E + e] = s;
-    a.part_c[slot * a.E + e] = s_c[e];
-  }
-  if (threadIdx.x == 0) a.part_n[slot] = s_n;
-  route_leave(a, g);
+  route_leave(a, g, s_p, s_c, s_n);
 }
 
 // Gradient, any top_k (OWN choices of a token to a lane).  dlogit_e = p_e (h_e - dot) with h the balance loss's part, the same for all tokens of a group, and
 // dot = sum_e p_e h_e + sum_j p_j dw_j over the chosen ones, whose own gradient is then p_j (h_j + dw_j - dot): the rows
 // pass through shared memory, where the lanes that own the token's choices put those in.
+__host__ __device__ constexpr int route_grad_blocks(int per) { return per <= 16 ? 3 : 2; }      // blocks an SM
 template <int TY, int PER, int L, int OWN>
-__global__ void __launch_bounds__(256, 2) route_grad_kernel(const RouteArgs a) {
+__global__ void __launch_bounds__(256, route_grad_blocks(PER)) route_grad_kernel(const RouteArgs a) {
   using T = typename ElemOf<TY>::type;
   constexpr int V = 16 / sizeof(T), TOK = 32 / L;
   op_pdl_wait();

@@ -48,6 +48,17 @@ template <typename F> void with_lanes(int E, F&& f) {
   else f(integral_constant<int, 32>(), integral_constant<int, 32>());
 }
 
+// The gradient keeps half as many elements a lane where a row is long: it needs registers for more than the row.
+template <typename F> void with_grad_lanes(int E, F&& f) {
+  using std::integral_constant;
+  if (E <= 64) with_lanes(E, f);
+  else if (E <= 128) f(integral_constant<int, 16>(), integral_constant<int, 8>());
+  else if (E <= 256) f(integral_constant<int, 16>(), integral_constant<int, 16>());
+  else if (E <= 512) f(integral_constant<int, 16>(), integral_constant<int, 32>());
+  else f(integral_constant<int, 32>(), integral_constant<int, 32>());
+}
+int grad_lanes_per_token(int E) { return E <= 64 ? lanes_per_token(E) : E <= 128 ? 8 : E <= 256 ? 16 : 32; }
+
 int rows_vectorise(const void* p, int type, int64_t row_stride, int64_t group_stride, int E) {
   const int v = 16 / type_bytes(type);
   return (uintptr_t)p % 16 == 0 && row_stride % v == 0 && group_stride % v == 0 && E % v == 0;
@@ -129,11 +140,12 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
   a.dweights = d_dweights; a.dloss = d_dloss; a.dlogits = d_dlogits; a.d_row_stride = d_row_stride; a.d_group_stride = d_group_stride;
   a.vec = rows_vectorise(d_logits, type, row_stride, group_stride, experts);
   a.vec_out = rows_vectorise(d_dlogits, type, d_row_stride, d_group_stride, experts);
-  const int64_t per_block = 8 * 32 / lanes_per_token(experts);
-  const int64_t blocks = std::min<int64_t>((tokens + per_block - 1) / per_block, std::max<int64_t>(1, 148 * 2 / groups));
+  const int64_t per_block = 8 * 32 / grad_lanes_per_token(experts);
+  const int64_t resident = 148 * (experts <= 512 ? route_grad_blocks(16) : route_grad_blocks(32));
+  const int64_t blocks = std::min<int64_t>((tokens + per_block - 1) / per_block, std::max<int64_t>(1, resident / groups));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   with_type(type, [&](auto ty) {
-    with_lanes(experts, [&](auto per, auto l) {
+    with_grad_lanes(experts, [&](auto per, auto l) {
       constexpr int TY = decltype(ty)::value, PER = decltype(per)::value, L = decltype(l)::value;
       const dim3 grid((unsigned)blocks, (unsigned)groups);
       if (top_k <= 8) launch_pdl(route_grad_kernel<TY, PER, L, (8 + L - 1) / L>, grid, dim3(256), 0, st, a);
