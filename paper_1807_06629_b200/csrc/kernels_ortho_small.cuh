@@ -148,8 +148,10 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   __syncthreads();
   ptx::cluster_arrive_release();
   ptx::cluster_wait_acquire();
-  double total = 0.0;
-  for (int r = 0; r < a.ctas; ++r) total += ld_cluster_f64(ptx::cluster_map(ptx::smem_u32(&s_norm), (uint32_t)r));
+  double total = lane < a.ctas ? ld_cluster_f64(ptx::cluster_map(ptx::smem_u32(&s_norm), (uint32_t)lane)) : 0.0;
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);      // (lanes 0 to 7 hold the parts)
+  total = __shfl_sync(0xffffffffu, total, 0);
   const float2 inv = ns_inverse(sqrt(total) + (double)a.eps);
 #pragma unroll 1
   for (int idx = (int)threadIdx.x; idx < a.s * (a.w / 8); idx += kNsSmallThreads) {
@@ -177,27 +179,41 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const bool issuer = warp == 0 && ptx::elect_one();
   uint32_t parity = 0;
-  // products of the pairs (A hi, lo) and (B hi, lo), the small ones first, over k16 steps of 16
-  auto products = [&](uint32_t d, uint32_t n, int k16, uint32_t ah, uint32_t al, uint32_t bh, uint32_t bl, bool b_mn) {
+  // Products of the pairs (A hi, lo) and (B hi, lo) over k16 steps of 16, the small ones first.  (Four steps to a turn, at
+  // fixed distances: computing descriptors between the MMAs took longer than the MMAs.)
+  auto products = [&](auto b_is_mn, uint32_t d, uint32_t n, int k16, uint32_t ah, uint32_t al, uint32_t bh, uint32_t bl) {
+    constexpr bool b_mn = decltype(b_is_mn)::value;
     ptx::fence_proxy_async();
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
     if (warp == 0) {
-      if (issuer) {
-        const uint32_t idesc = ptx::idesc_f16(128, (int)n, 0, b_mn);
-        for (int p = 0; p < 3; ++p) {
-          const uint32_t sa = p == 0 ? al : ah, sb = p == 1 ? bl : bh;
-#pragma unroll 4
-          for (int k = 0; k < k16; ++k) {
-            const uint32_t in_block = (uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u;
-            const uint64_t da = ptx::smem_desc_sw128(sa + in_block, 16u, 1024u);
-            const uint64_t db = b_mn ? ptx::smem_desc_sw128(sb + (uint32_t)k * 2048u, 16384u, 1024u) : ptx::smem_desc_sw128(sb + in_block, 16u, 1024u);
-            ptx::mma_bf16(d, da, db, idesc, p != 0 || k != 0 ? 1u : 0u);
+      const uint32_t idesc = ptx::idesc_f16(128, (int)n, 0, b_mn);
+      const uint64_t a_of = ptx::smem_desc_sw128(0u, 16u, 1024u), b_of = b_mn ? ptx::smem_desc_sw128(0u, 16384u, 1024u) : a_of;
+      constexpr uint64_t b_k = b_mn ? 128u : 2u, b_block = b_mn ? 512u : 1024u;
+#pragma unroll 1
+      for (int p = 0; p < 3; ++p) {
+        // (a shared address carries the CTA's rank above its 18 bits)
+        uint64_t da = a_of + (((p == 0 ? al : ah) & 0x3FFFFu) >> 4), db = b_of + (((p == 1 ? bl : bh) & 0x3FFFFu) >> 4);
+        uint32_t more = p != 0 ? 1u : 0u;
+        int k = k16;
+#pragma unroll 1
+        for (; k >= 4; k -= 4, da += 1024u, db += b_block) {
+          if (issuer) {
+            ptx::mma_bf16(d, da, db, idesc, more);
+            ptx::mma_bf16(d, da + 2u, db + b_k, idesc, 1u);
+            ptx::mma_bf16(d, da + 4u, db + 2u * b_k, idesc, 1u);
+            ptx::mma_bf16(d, da + 6u, db + 3u * b_k, idesc, 1u);
           }
+          more = 1u;
         }
-        ptx::mma_commit(bar);
+#pragma unroll 1
+        for (; k > 0; --k, da += 2u, db += b_k) {
+          if (issuer) ptx::mma_bf16(d, da, db, idesc, more);
+          more = 1u;
+        }
       }
+      if (issuer) ptx::mma_commit(bar);
       __syncwarp();
     }
     (void)ptx::mbar_wait(bar, parity, &abort_flag, a.status, NS_ERR_SMALL);      // (after an expiry every later wait returns at once)
@@ -211,7 +227,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   for (int step = 0; step < a.steps; ++step) {
     const bool last = step + 1 == a.steps;
     // ---- A = X X^T: this CTA's share, then the sum of all
-    products(d_s, (uint32_t)a.sp, a.w / 16, x_hi, x_lo, x_hi, x_lo, false);
+    products(std::false_type(), d_s, (uint32_t)a.sp, a.w / 16, x_hi, x_lo, x_hi, x_lo);
     if (quarter * 32 < a.sp) {
 #pragma unroll 1
       for (int c = half * 16; c < a.sp; c += 32) {
@@ -227,7 +243,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
     ptx::cluster_arrive_release();
     ptx::cluster_wait_acquire();
     const int all = a.sp * chunks, mine1 = all * (rank + 1) / a.ctas;
-#pragma unroll 1
+#pragma unroll 2
     for (int idx = all * rank / a.ctas + (int)threadIdx.x; idx < mine1; idx += kNsSmallThreads) {
       const int row = idx / chunks, q = idx - row * chunks;
       const uint32_t from = share_at(row, q);
@@ -251,7 +267,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
     ptx::cluster_arrive_release();                         // A is whole, and its shares have been read
     ptx::cluster_wait_acquire();
     // ---- P = a I + b A + c A^2, in the place of A
-    products(d_s, (uint32_t)a.sp, a.sp / 16, s_hi, s_lo, s_hi, s_lo, false);
+    products(std::false_type(), d_s, (uint32_t)a.sp, a.sp / 16, s_hi, s_lo, s_hi, s_lo);
     if (quarter * 32 < a.sp) {
 #pragma unroll 1
       for (int c = half * 16; c < a.sp; c += 32) {
@@ -283,7 +299,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
       }
     }
     // ---- X <- P X, in its place
-    products(d_x, (uint32_t)a.w, a.sp / 16, s_hi, s_lo, x_hi, x_lo, true);
+    products(std::true_type(), d_x, (uint32_t)a.w, a.sp / 16, s_hi, s_lo, x_hi, x_lo);
     if (quarter * 32 < a.s) {
       const uint32_t box = s_hi + (uint32_t)(warp & 7) * 4096u;          // (P is not needed any more; 32 KB at least)
 #pragma unroll 1

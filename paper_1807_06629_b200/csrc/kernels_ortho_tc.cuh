@@ -233,45 +233,28 @@ __device__ __forceinline__ void ns_store_box(uint32_t box, __half* p, int64_t pi
   }
 }
 
-// Columns c .. c + 3 of row r of the result (v: 256 times X); n of them exist.
-__device__ __forceinline__ void ns_finish4(const NsDest& d, bool vec, int m, int r, int c, float4 v, int n) {
-  if (!vec || n < 4) {
-    ns_store_final(d, m, r, c, v.x * kNsUnscale);
-    if (n > 1) ns_store_final(d, m, r, c + 1, v.y * kNsUnscale);
-    if (n > 2) ns_store_final(d, m, r, c + 2, v.z * kNsUnscale);
-    if (n > 3) ns_store_final(d, m, r, c + 3, v.w * kNsUnscale);
-    return;
-  }
-  const int64_t o = (int64_t)m * d.batch + (d.tiled ? wtile_offset(d.tile, r, c) : (int64_t)r * d.row + c);
-  const float al = d.alpha * kNsUnscale;
-  float4 w = make_float4(al * v.x, al * v.y, al * v.z, al * v.w);
-  if (d.type == PRSGD_TYPE_FP32) {
-    float4* p = reinterpret_cast<float4*>(static_cast<float*>(d.out) + o);
-    if (d.beta != 0.f) {
-      const float4 old = *p;
-      w.x = fmaf(d.beta, old.x, w.x); w.y = fmaf(d.beta, old.y, w.y); w.z = fmaf(d.beta, old.z, w.z); w.w = fmaf(d.beta, old.w, w.w);
-    }
-    *p = w;
-    if (d.shadow != nullptr) {
-      const __nv_bfloat162 x = __floats2bfloat162_rn(w.x, w.y), y = __floats2bfloat162_rn(w.z, w.w);
-      *reinterpret_cast<uint2*>(d.shadow + o) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-    }
-    return;
-  }
-  uint2* p = reinterpret_cast<uint2*>(static_cast<uint16_t*>(d.out) + o);
+// Columns c .. c + 3 of row r of what is there, where the result is added to it and the whole four can be read together.
+__device__ __forceinline__ float4 ns_old4(const NsDest& d, int64_t o) {
+  if (d.type == PRSGD_TYPE_FP32) return *reinterpret_cast<const float4*>(static_cast<const float*>(d.out) + o);
+  uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(d.out) + o);
   const bool bf = d.type == PRSGD_TYPE_BF16;
-  if (d.beta != 0.f) {
-    uint2 u = *p;
-    const float2 x = bf ? __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&u.x)) : unpack_half2(u.x);
-    const float2 y = bf ? __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&u.y)) : unpack_half2(u.y);
-    w.x = fmaf(d.beta, x.x, w.x); w.y = fmaf(d.beta, x.y, w.y); w.z = fmaf(d.beta, y.x, w.z); w.w = fmaf(d.beta, y.y, w.w);
+  const float2 x = bf ? __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&u.x)) : unpack_half2(u.x);
+  const float2 y = bf ? __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&u.y)) : unpack_half2(u.y);
+  return make_float4(x.x, x.y, y.x, y.y);
+}
+__device__ __forceinline__ void ns_write4(const NsDest& d, int64_t o, float4 w) {
+  if (d.type == PRSGD_TYPE_FP32) {
+    *reinterpret_cast<float4*>(static_cast<float*>(d.out) + o) = w;
+    if (d.shadow == nullptr) return;
   }
-  if (bf) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(w.x, w.y), y = __floats2bfloat162_rn(w.z, w.w);
-    *p = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+  uint2 u;
+  if (d.type == PRSGD_TYPE_FP16) {
+    u = make_uint2(pack_half2(w.x, w.y), pack_half2(w.z, w.w));
   } else {
-    *p = make_uint2(pack_half2(w.x, w.y), pack_half2(w.z, w.w));
+    const __nv_bfloat162 x = __floats2bfloat162_rn(w.x, w.y), y = __floats2bfloat162_rn(w.z, w.w);
+    u = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
   }
+  *reinterpret_cast<uint2*>((d.type == PRSGD_TYPE_FP32 ? d.shadow : static_cast<uint16_t*>(d.out)) + o) = u;
 }
 
 // 32 rows x 32 columns of the result (of `rows` x `cols`), a row per lane, through shared memory so that the lanes of a warp write
@@ -284,13 +267,44 @@ __device__ __forceinline__ void ns_finish(const NsDest& d, bool vec, int m, int 
     st_shared_v4(box + (uint32_t)lane * 128u + (uint32_t)((q ^ (lane & 7)) * 16), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
                  __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
   __syncwarp();
-  const int c = c0 + (lane & 7) * 4;
+  const int c = c0 + (lane & 7) * 4, row0 = r0 + (lane >> 3);
+  if (vec && c + 4 <= cols) {                              // four rows together, so that what is added to is requested together
+    const float al = d.alpha * kNsUnscale;
+#pragma unroll 1
+    for (int i = 0; i < 8; i += 4) {
+      float4 w[4], old[4];
+      int64_t o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int rr = row0 + 4 * (i + j);
+        o[j] = (int64_t)m * d.batch + (d.tiled ? wtile_offset(d.tile, rr, c) : (int64_t)rr * d.row + c);
+        old[j] = d.beta != 0.f && rr < rows ? ns_old4(d, o[j]) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const int br = 4 * (i + j) + (lane >> 3);
+        const uint4 u = ld_shared_v4(box + (uint32_t)br * 128u + (uint32_t)(((lane & 7) ^ (br & 7)) * 16));
+        w[j] = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (row0 + 4 * (i + j) >= rows) continue;
+        if (d.beta != 0.f) {
+          w[j] = make_float4(fmaf(d.beta, old[j].x, al * w[j].x), fmaf(d.beta, old[j].y, al * w[j].y), fmaf(d.beta, old[j].z, al * w[j].z), fmaf(d.beta, old[j].w, al * w[j].w));
+        } else {
+          w[j] = make_float4(al * w[j].x, al * w[j].y, al * w[j].z, al * w[j].w);
+        }
+        ns_write4(d, o[j], w[j]);
+      }
+    }
+    return;
+  }
 #pragma unroll 1
   for (int i = 0; i < 8; ++i) {
-    const int rr = i * 4 + (lane >> 3);
-    const uint4 u = ld_shared_v4(box + (uint32_t)rr * 128u + (uint32_t)(((lane & 7) ^ (rr & 7)) * 16));
-    if (r0 + rr < rows && c < cols)
-      ns_finish4(d, vec, m, r0 + rr, c, make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)), min(4, cols - c));
+    const int br = i * 4 + (lane >> 3);
+    const uint4 u = ld_shared_v4(box + (uint32_t)br * 128u + (uint32_t)(((lane & 7) ^ (br & 7)) * 16));
+    if (r0 + br >= rows) continue;
+    const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < cols) ns_store_final(d, m, r0 + br, c + e, w[e] * kNsUnscale);
   }
 }
 
