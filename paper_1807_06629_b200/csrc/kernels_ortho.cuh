@@ -39,6 +39,11 @@ struct NsBuffers {
   unsigned int* claim;                   // next unclaimed task
   unsigned int* done;                    // [batch][panels] tiles that have been added to a panel
   int panels;
+  // A's tiles formed in `parts` parts of the contraction (few tiles of long ones): the parts' sums and, per warp of a tile's
+  // epilogue, how many have been left
+  int parts, gram_tiles;                 // (gram_tiles: of a matrix)
+  float* part_sums;                      // [batch][tiles][parts][16][4096]
+  unsigned int* part_count;              // [batch][tiles][16]
   DeviceStatus* status;
   int own_status;                        // the workspace's own: cleared by the call.  0: a context's, an error in it turns the call into a no-op
   int64_t xp, sp;
@@ -91,6 +96,8 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const NsShape sh, const Ns
   const int m = blockIdx.y;
   if (blockIdx.x == 0) {
     for (int i = threadIdx.x; i < buf.panels; i += 256) buf.done[(int64_t)m * buf.panels + i] = 0u;
+    if (buf.parts > 1)
+      for (int i = threadIdx.x; i < buf.gram_tiles * 16; i += 256) buf.part_count[(int64_t)m * buf.gram_tiles * 16 + i] = 0u;
     if (m == 0 && threadIdx.x == 0) {
       *buf.claim = 0u;
       if (buf.own_status) buf.status->error = 0u;

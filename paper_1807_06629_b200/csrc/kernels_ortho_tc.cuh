@@ -38,12 +38,13 @@ struct NsChainArgs {
   int steps, split, tall, s, l;
   float a, b, c;
   int ts, tsym, tr, tc;          // tiles along the short side; tiles of A and P on and above the diagonal; tile rows and columns of X
-  int per_step, per_panel;       // tiles of a matrix and step; of them, tiles of one panel
-  int group, total;              // matrices of a group; tiles of the launch
+  int parts;                     // parts of the contraction of A's tiles, a task each
+  int per_step, per_panel;       // tasks of a matrix and step; tiles of one panel
+  int group, total;              // matrices of a group; tasks of the launch
   int vec_out;                   // result rows can be written 16 bytes at a time
 };
 
-struct NsTask { int m, step, kind, ti, tj; int pi, pj, need; };      // pi, pj: the panels (256 rows or columns along the short side) it takes from and adds to
+struct NsTask { int m, step, kind, part, ti, tj; int pi, pj, need; };      // pi, pj: the panels (256 rows or columns along the short side) it takes from and adds to
 
 __device__ __forceinline__ NsTask ns_decode(const NsChainArgs& a, int t) {
   const int per_group = a.group * a.steps * a.per_step;
@@ -55,12 +56,14 @@ __device__ __forceinline__ NsTask ns_decode(const NsChainArgs& a, int t) {
   rem -= k.step * gs * a.per_step;
   k.need = k.step * a.per_panel;
   k.kind = 0;
-  if (rem >= gs * a.tsym) { rem -= gs * a.tsym; k.kind = 1; k.need += a.ts; }
+  if (rem >= gs * a.tsym * a.parts) { rem -= gs * a.tsym * a.parts; k.kind = 1; k.need += a.ts; }
   if (k.kind == 1 && rem >= gs * a.tsym) { rem -= gs * a.tsym; k.kind = 2; k.need += a.ts; }
-  const int tiles = k.kind == 2 ? a.tr * a.tc : a.tsym;
+  const int tiles = k.kind == 2 ? a.tr * a.tc : k.kind == 1 ? a.tsym : a.tsym * a.parts;
   k.m = rem / tiles;
-  const int q = rem - k.m * tiles;
+  int q = rem - k.m * tiles;
   k.m += g * a.group;
+  k.part = 0;
+  if (k.kind == 0) { k.part = q % a.parts; q /= a.parts; }
   if (k.kind == 2) {                                    // panel by panel
     if (a.tall) { k.tj = q / a.tr; k.ti = q - k.tj * a.tr; k.pi = k.pj = k.tj; }
     else        { k.ti = q / a.tc; k.tj = q - k.ti * a.tc; k.pi = k.pj = k.ti; }
@@ -73,6 +76,15 @@ __device__ __forceinline__ NsTask ns_decode(const NsChainArgs& a, int t) {
   k.need *= 2 * kNsEpiWarps;                            // every epilogue warp of the pair counts a tile
   k.pi += k.m * a.ts; k.pj += k.m * a.ts;
   return k;
+}
+
+// The blocks of 64 of a task's contraction: first and number.
+__device__ __forceinline__ int ns_blocks(const NsChainArgs& a, const NsTask& k, int& n) {
+  const int kb = ((k.kind == 0 ? a.l : a.s) + 63) / 64;
+  if (k.kind != 0 || a.parts == 1) { n = kb; return 0; }
+  const int first = kb * k.part / a.parts;
+  n = kb * (k.part + 1) / a.parts - first;
+  return first;
 }
 
 namespace ptx {
@@ -353,10 +365,12 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   auto next_task = [&](int n) -> NsTask {
     const int r = n % kNsRing;
     NsTask k;
-    k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
+    k.kind = -1; k.m = k.step = k.part = k.ti = k.tj = 0;
     if (!ptx::warp_wait(sfull(r), (uint32_t)((n / kNsRing) & 1), ab, status, NS_ERR_RING)) return k;
     const uint4 w = ld_shared_v4(ptx::smem_u32(&ring[r]));
-    k.kind = __shfl_sync(0xffffffffu, (int)w.x, 0); k.m = __shfl_sync(0xffffffffu, (int)w.y, 0); k.step = __shfl_sync(0xffffffffu, (int)w.z, 0);
+    k.kind = __shfl_sync(0xffffffffu, (int)w.x, 0); k.m = __shfl_sync(0xffffffffu, (int)w.y, 0); 
+    const uint32_t sp = __shfl_sync(0xffffffffu, w.z, 0);
+    k.step = (int)(sp & 0xffffu); k.part = (int)(sp >> 16);
     const uint32_t t = __shfl_sync(0xffffffffu, w.w, 0);
     k.ti = (int)(t >> 16); k.tj = (int)(t & 0xffffu);
     return k;
@@ -377,8 +391,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         if (k.kind < 0) break;
         if (issue) { free_task(n); ptx::fence_proxy_async_all(); }
         const int from = k.step & 1;
-        const int K = k.kind == 0 ? a.l : a.s;
-        const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
+        int kb;
+        const int k0 = ns_blocks(a, k, kb), blocks = kb * (SPLIT ? 3 : 1);
         const bool of_x = k.kind == 0 || (k.kind == 2 && second != (a.tall != 0));
         const bool x_mn = k.kind == 0 ? a.tall != 0 : second;                      // (of X)
         const int tile = second ? k.tj : k.ti, at0 = tile * 256 + (int)rank * 128;
@@ -388,7 +402,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
           const int part = SPLIT && p == (second ? 1 : 0) ? 1 : 0;       // lo hi, hi lo, hi hi: the small ones first
           const CUtensorMap* map_mn = of_x ? &maps.x[from][part] : k.kind == 1 ? &maps.A[part] : &maps.P[part];
           const CUtensorMap* map_k = of_x ? &maps.xk[from][part] : k.kind == 1 ? &maps.Ak[part] : &maps.Pk[part];
-          for (int q = 0; q < kb; ++q, ++b) {
+          for (int q = k0; q < k0 + kb; ++q, ++b) {
             const bool mn = of_x ? x_mn : (q >> 2) < tile;               // (symmetric: below the diagonal the transpose is stored)
             if (!ptx::warp_wait(empty((int)s), phase, ab, status, NS_ERR_EMPTY)) { ok = false; break; }
             if (issue) {
@@ -415,8 +429,9 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         const NsTask k = next_task(n);
         if (k.kind < 0) break;
         if (issue) free_task(n);
-        const int K = k.kind == 0 ? a.l : a.s;
-        const int kb = (K + 63) / 64, blocks = kb * (SPLIT ? 3 : 1);
+        int kb;
+        (void)ns_blocks(a, k, kb);
+        const int blocks = kb * (SPLIT ? 3 : 1);
         // blocks of 64 below which the operands lie MN-major
         const int a_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && a.tall) ? 0 : 4 * k.ti;
         const int b_mn_until = k.kind == 0 ? (a.tall ? kb : 0) : (k.kind == 2 && !a.tall) ? kb : 4 * k.tj;
@@ -461,7 +476,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
         if (n >= kNsRing && !ptx::mbar_wait(sempty(r), (uint32_t)(((n / kNsRing) - 1) & 1), ab, status, NS_ERR_RING_FREE)) break;
         NsTask k;
-        k.kind = -1; k.m = k.step = k.ti = k.tj = 0;
+        k.kind = -1; k.m = k.step = k.part = k.ti = k.tj = 0;
         for (;;) {
           const int t = (int)atomicAdd(a.buf.claim, 1u);
           if (t >= a.total || (n == 0 && !a.buf.own_status && status->error != 0u)) break;
@@ -477,7 +492,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
   #pragma unroll
         for (uint32_t c = 0; c < 2; ++c) {
           ptx::send_v4(ptx::cluster_map(ptx::smem_u32(&ring[r]), c), ptx::cluster_map(sfull(r), c),
-                       make_uint4((uint32_t)k.kind, (uint32_t)k.m, (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
+                       make_uint4((uint32_t)k.kind, (uint32_t)k.m, ((uint32_t)k.part << 16) | (uint32_t)k.step, ((uint32_t)k.ti << 16) | (uint32_t)k.tj));
         }
         if (k.kind < 0) break;
       }
@@ -510,7 +525,9 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
       if constexpr (SPLIT) {
         // The partial sums of the tile are added in registers, where they are rounded, not cut off; the total goes back
         // to TMEM, over the last of them, so that what follows is a loop of few instructions.
-        const int kb = ((k.kind == 0 ? a.l : a.s) + 63) / 64, parts = 1 + (kb + kNsPromote - 1) / kNsPromote;
+        int kb;
+        (void)ns_blocks(a, k, kb);
+        const int parts = 1 + (kb + kNsPromote - 1) / kNsPromote;
         float total[kNsWarpCols / 32][32];
 #pragma unroll
         for (int i = 0; i < kNsWarpCols; ++i) total[i >> 5][i & 31] = 0.f;
@@ -542,6 +559,59 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_co
         ++sums;
         if (!ok) break;
         ptx::tc_fence_after();
+      }
+      // A tile of A in parts: leave this part's sum; whichever warp leaves the last one of its 32 x 128 values adds them up, in
+      // the parts' order, and goes on with the total in TMEM.  Nobody waits.
+      if (k.kind == 0 && a.parts > 1) {
+        const int64_t tile = (int64_t)k.m * a.tsym + k.tj * (k.tj + 1) / 2 + k.ti;
+        const int slot = (int)rank * kNsEpiWarps + warp - 4;
+        float4* const sums_of = reinterpret_cast<float4*>(a.buf.part_sums) + (tile * a.parts * 16 + slot) * 1024 + lane;
+        if (units > 0) {
+#pragma unroll 1
+          for (int ch = 0; ch < 4; ++ch) {
+            uint32_t raw[32];
+            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
+            ptx::tmem_ld_wait();
+            float4* const to = sums_of + (int64_t)k.part * 16384 + ch * 256;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              __stcg(to + q * 32, make_float4(__uint_as_float(raw[4 * q]), __uint_as_float(raw[4 * q + 1]), __uint_as_float(raw[4 * q + 2]), __uint_as_float(raw[4 * q + 3])));
+          }
+        }
+        __syncwarp();
+        unsigned int left = 0;
+        if (lane == 0) {
+          asm volatile("fence.acq_rel.gpu;" ::: "memory");
+          left = atomicAdd(a.buf.part_count + tile * 16 + slot, 1u);
+          asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        }
+        left = __shfl_sync(0xffffffffu, left, 0);
+        if (left + 1u != (unsigned)a.parts) {
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
+          continue;
+        }
+        if (lane == 0) a.buf.part_count[tile * 16 + slot] = 0u;      // (for the next step, whose tiles wait for this one)
+        if (units > 0) {
+#pragma unroll 1
+          for (int ch = 0; ch < 4; ++ch) {
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 1
+            for (int p = 0; p < a.parts; ++p) {
+              const float4* const from_part = sums_of + (int64_t)p * 16384 + ch * 256;
+#pragma unroll
+              for (int q = 0; q < 8; ++q) {
+                const float4 x = __ldcg(from_part + q * 32);
+                v[4 * q] += x.x; v[4 * q + 1] += x.y; v[4 * q + 2] += x.z; v[4 * q + 3] += x.w;
+              }
+            }
+            ptx::tmem_st32(lanes + acc * 256u + (uint32_t)(ch * 32), v);
+          }
+          ptx::tmem_st_wait();
+        }
       }
       // A rolled loop, and short: code that a tile runs through once is fetched anew every time, at about 20 cycles an
       // instruction (unrolled, this took 8 to 10 thousand cycles a tile, longer than the products of K = 1024).

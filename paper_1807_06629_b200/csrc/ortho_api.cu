@@ -8,6 +8,15 @@ using namespace prsgd;
 
 namespace prsgd {
 
+// Into how many parts the contraction of A = X X^T is cut: while A has fewer tiles than there are pairs of CTAs (74), as
+// many as there are pairs for, but no part below 12 blocks of 64 products (6 us of products against about 4 for leaving a
+// part's sum and adding it up).  4 x 500 x 1900, fp32: 12 tiles in 6 parts.
+static int ns_parts(const NsShape& sh, int precision) {
+  const int64_t s = std::min(sh.rows, sh.cols), l = std::max(sh.rows, sh.cols), ts = (s + 255) / 256, kb = (l + 63) / 64;
+  const int64_t tiles = (int64_t)sh.batch * ts * (ts + 1) / 2, blocks = kb * (precision == PRSGD_PRECISION_FP32 ? 3 : 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(74 / std::max<int64_t>(tiles, 1), blocks / 12), std::min<int64_t>(kb, 16)));
+}
+
 static NsBuffers ns_carve(const NsShape& sh, int precision, unsigned char* base, size_t* bytes) {
   NsBuffers b{};
   const int64_t s = std::min(sh.rows, sh.cols);
@@ -22,6 +31,10 @@ static NsBuffers ns_carve(const NsShape& sh, int precision, unsigned char* base,
   b.claim = reinterpret_cast<unsigned int*>(take(4));
   b.done = reinterpret_cast<unsigned int*>(take(4 * (size_t)sh.batch * b.panels));
   b.part = reinterpret_cast<double*>(take(8 * (size_t)sh.batch * b.chunks));
+  b.parts = ns_parts(sh, precision); b.gram_tiles = b.panels * (b.panels + 1) / 2;
+  const size_t sums = b.parts > 1 ? (size_t)sh.batch * b.gram_tiles : 0;
+  b.part_count = reinterpret_cast<unsigned int*>(take(sums * 16 * 4));
+  b.part_sums = reinterpret_cast<float*>(take(sums * b.parts * 16 * 4096 * 4));
   for (int i = 0; i < 2; ++i)
     for (int j = 0; j < 2; ++j) b.x[i][j] = reinterpret_cast<__half*>(take(2 * (size_t)sh.batch * sh.rows * b.xp));
   for (int j = 0; j < 2; ++j) {
@@ -173,7 +186,7 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
   a.a = p.a; a.b = p.b; a.c = p.c;
   const int ts = (s + 255) / 256;
   a.tsym = ts * (ts + 1) / 2; a.tr = (p.shape.rows + 255) / 256; a.tc = (p.shape.cols + 255) / 256;
-  a.ts = ts; a.per_step = 2 * a.tsym + a.tr * a.tc; a.per_panel = 2 * ts + (a.tall ? a.tr : a.tc);
+  a.ts = ts; a.parts = buf.parts; a.per_step = a.tsym * (a.parts + 1) + a.tr * a.tc; a.per_panel = 2 * ts + (a.tall ? a.tr : a.tc);
   const int64_t total = (int64_t)p.shape.batch * p.steps * a.per_step;
   if (total > 0x3fffffffll) return op_fail(PRSGD_ERR_SIZE, "orthogonalize: too many tiles in one call");
   a.total = (int)total;
@@ -194,7 +207,7 @@ int ns_run(const NsPlan& p, void* d_work, cudaStream_t st, int64_t* launches) {
     map_s(&maps.P[j], buf.P[j], 64); map_s(&maps.Pk[j], buf.P[j], 128);
   }
   if (rc != PRSGD_OK) return rc;
-  const int pairs = (int)std::min<int64_t>(sms / 2, batch * std::max(a.tsym, a.tr * a.tc));
+  const int pairs = (int)std::min<int64_t>(sms / 2, batch * std::max(a.tsym * a.parts, a.tr * a.tc));
   if (split) launch_pdl_cluster(ns_chain_kernel<true>, dim3(2 * pairs), dim3(kNsThreads), kNsSmem, st, 2, maps, a);
   else launch_pdl_cluster(ns_chain_kernel<false>, dim3(2 * pairs), dim3(kNsThreads), kNsSmem, st, 2, maps, a);
   if (launches) *launches += 1;
