@@ -1,22 +1,32 @@
 // Newton-Schulz chain of matrices whose short side is at most 128, in one launch: a cluster of CTAs per matrix holds it in
 // shared memory from its first reading to the result, so that nothing but the matrix itself is read and written.
 //
-// CTA r of the cluster keeps `w` columns (of the long side) of X as fp16 pairs.  Per step it forms its share of
-// A = X X^T on the tensor cores; each CTA sums a part of A over the shares, in rank order, through distributed shared
-// memory and hands it to all; each then forms P = a I + b A + c A^2 for itself and applies it to its columns.  All products are
-// hi hi + hi lo + lo hi whatever the precision asked for: with so little work the time is that of the waits between
-// the steps, not of the products.  (16 matrices of 10 x 1024: about 150 us as three products a step of the chain's tiles.)
+// CTA r of the cluster keeps `w` columns (of the long side) of X as fp16 pairs.  Per step it forms its share of A = X X^T on
+// the tensor cores.  Up to a short side of 32 it sends its share to all (st.async, counted on the receiver's barrier), and every
+// CTA sums all of A, in rank order, and forms P = a I + b A + c A^2 in fp32 for itself (16 matrices of 10 x 1024: 37 -> 24 us,
+// against the form for longer sides); above, each CTA fetches and sums a part of A and hands it to all, and P is formed on the
+// tensor cores.  (Shares sent to the CTAs that sum them, a lane to a row: 8 x 64 x 1024 43 -> 55 us; what crosses between CTAs has to
+// go from neighbouring lanes to neighbouring places.)  All products but that of P in fp32 are hi hi + hi lo + lo hi whatever
+// the precision asked for: with so little work the time is that of the waits between the steps, not of the products.
+// (16 matrices of 10 x 1024: about 150 us as three products a step of the chain's tiles.)
 #pragma once
 #include "kernels_ortho_tc.cuh"
 
 namespace prsgd {
 
 constexpr int kNsSmallThreads = 256, kNsSmallSide = 128, kNsSmallCtas = 8;
-// columns of a CTA that fit beside A and its shares: X 256 bytes a column, A 32 or 64 KB, its shares up to 16 or 64 KB
+// columns of a CTA that fit beside A and its shares: X 256 bytes a column (512 above a short side of 64), A 32 or 64 KB,
+// its shares up to 128 KB (short side up to 32), 16 KB (up to 64) or 64 KB
 __host__ __device__ constexpr int ns_small_cols(int s) { return s <= 64 ? 256 : 192; }
 // The whole of an SM's shared memory, whatever is needed: a second CTA on the SM would wait for the TMEM this one holds,
 // and clusters that wait for one another's TMEM would wait for good.
 constexpr size_t kNsSmallSmem = 225 * 1024;
+__host__ __device__ constexpr int ns_small_share_bytes(int sp, int ctas) { return sp * sp * 4 * (sp <= 32 ? 4 * ctas : 1); }
+__host__ __device__ constexpr int ns_small_bytes(int sp, int ctas, int w) {
+  return w / 64 * 16384 * (sp <= 64 ? 1 : 2) + 2 * ((sp + 63) / 64) * 16384 + ns_small_share_bytes(sp, ctas) + 1024;
+}
+static_assert(ns_small_bytes(32, kNsSmallCtas, 256) <= (int)kNsSmallSmem && ns_small_bytes(64, kNsSmallCtas, 256) <= (int)kNsSmallSmem &&
+              ns_small_bytes(128, kNsSmallCtas, 192) <= (int)kNsSmallSmem, "shared memory of the small form");
 enum { NS_ERR_SMALL = 0x711 };
 
 struct NsSmallArgs {
@@ -28,10 +38,15 @@ struct NsSmallArgs {
   int vec_out;
 };
 
-__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
-  double v;
-  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
-  return v;
+namespace ptx {
+// stores into a CTA's shared memory that count their bytes on a barrier there
+__device__ __forceinline__ void send_f64(uint32_t to_cluster, uint32_t bar_cluster, double v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];"
+               ::"r"(to_cluster), "l"(__double_as_longlong(v)), "r"(bar_cluster) : "memory");
+}
+__device__ __forceinline__ void send_data_v4(uint32_t to_cluster, uint32_t bar_cluster, float x, float y, float z, float w) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(to_cluster), "f"(x), "f"(y), "f"(z), "f"(w), "r"(bar_cluster) : "memory");
 }
 __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
   float4 v;
@@ -41,35 +56,68 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
 __device__ __forceinline__ void st_cluster_v2(uint32_t at, uint32_t x, uint32_t y) {
   asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
 }
+// A bounded wait for what other CTAs of the cluster have sent.
+__device__ __forceinline__ bool mbar_wait_sent(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* status, unsigned what) {
+  long long t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+    if ((it & 63u) == 0u) {
+      if (*abort_flag) return false;
+      const long long now = clock64();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > kWaitLimitCycles) {
+        *abort_flag = 1;
+        if (atomicCAS(&status->error, 0u, what) == 0u) status->where = blockIdx.x;
+        return false;
+      }
+    }
+  }
+}
+}  // namespace ptx
+
+__device__ __forceinline__ float ld_shared_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
 
 // MODE as in ns_norm_kernel; VEC: elements of a row that are read together.
 template <int TY, int MODE, int VEC>
 __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __grid_constant__ NsSmallArgs a) {
   using T = typename ElemOf<TY>::type;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t bar_mma;
-  __shared__ __align__(8) double s_norm;
+  __shared__ __align__(8) uint64_t bars[4];                // products; norms; shares of even and of odd steps
+  __shared__ __align__(8) double s_norms[kNsSmallCtas];
   __shared__ double s_part[8];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int m = (int)blockIdx.x / a.ctas, rank = (int)blockIdx.x % a.ctas;
   const uint32_t x_hi = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t x_bytes = (uint32_t)(a.w / 64) * 16384u, x_lo = x_hi + x_bytes;
-  const uint32_t s_hi = x_lo + x_bytes, s_bytes = (uint32_t)((a.sp + 63) / 64) * 16384u, s_lo = s_hi + s_bytes;
-  const uint32_t shares = s_lo + s_bytes;               // [sp][sp] fp32: this CTA's share of A
-  const uint32_t bar = ptx::smem_u32(&bar_mma);
+  // Up to a short side of 64 the 128 rows of an operand block hold X_hi and, from row sp on, X_lo: a product with both has
+  // all parts.
+  const bool stacked = a.sp <= 64, everyone = a.sp <= 32;
+  const uint32_t x_bytes = (uint32_t)(a.w / 64) * 16384u, x_lo = x_hi + (stacked ? (uint32_t)a.sp * 128u : x_bytes);
+  const uint32_t s_hi = x_hi + (stacked ? 1u : 2u) * x_bytes, s_bytes = (uint32_t)((a.sp + 63) / 64) * 16384u, s_lo = s_hi + s_bytes;
+  // Shares of A, 16-byte chunks: [step & 1][sender][hi or lo rows][all], or this CTA's own: [all]
+  const uint32_t shares = s_lo + s_bytes;
+  const uint32_t bar = ptx::smem_u32(&bars[0]), bar_norm = bar + 8u, bar_share = bar + 16u;
   ptx::pdl_wait();
   ptx::pdl_trigger();
   if (a.own_status && blockIdx.x == 0 && threadIdx.x == 0) a.status->error = 0u;
   if (a.src.active != nullptr && a.src.active[m] == 0) return;       // (the whole cluster)
   if (threadIdx.x == 0) {
-    ptx::mbar_init(bar, 1);
+#pragma unroll 1
+    for (uint32_t b = 0; b < 4; ++b) ptx::mbar_init(bar + b * 8u, 1);
     abort_flag = 0;
     ptx::fence_mbar_init();
   }
+  ptx::cluster_arrive_release();                           // (the barriers are there: waited for before the first is sent to)
   if (warp == 1) ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512);
-  for (uint32_t o = threadIdx.x * 16u; o < 2u * (x_bytes + s_bytes); o += kNsSmallThreads * 16u) st_shared_v4(x_hi + o, 0u, 0u, 0u, 0u);
+  for (uint32_t o = threadIdx.x * 16u; o < s_hi - x_hi + 2u * s_bytes; o += kNsSmallThreads * 16u) st_shared_v4(x_hi + o, 0u, 0u, 0u, 0u);
 
   // element (i, j) of this CTA's X, i along the short side: G[i][j0 + j], or of a tall matrix G[j0 + j][i]
   const int j0 = rank * a.w, nj = max(0, min(a.w, a.l - j0));
@@ -140,15 +188,15 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) s_part[warp] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) {
+  ptx::cluster_wait_acquire();
+  if ((int)threadIdx.x < a.ctas) {
     double t = 0.0;
     for (int i = 0; i < 8; ++i) t += s_part[i];
-    s_norm = t;
+    if (threadIdx.x == 0) ptx::mbar_expect_tx(bar_norm, (uint32_t)a.ctas * 8u);
+    ptx::send_f64(ptx::cluster_map(ptx::smem_u32(&s_norms[rank]), threadIdx.x), ptx::cluster_map(bar_norm, threadIdx.x), t);
   }
-  __syncthreads();
-  ptx::cluster_arrive_release();
-  ptx::cluster_wait_acquire();
-  double total = lane < a.ctas ? ld_cluster_f64(ptx::cluster_map(ptx::smem_u32(&s_norm), (uint32_t)lane)) : 0.0;
+  (void)ptx::mbar_wait_sent(bar_norm, 0u, &abort_flag, a.status, NS_ERR_SMALL);      // (after an expiry every later wait returns at once)
+  double total = lane < a.ctas ? s_norms[lane] : 0.0;
 #pragma unroll
   for (int o = 4; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);      // (lanes 0 to 7 hold the parts)
   total = __shfl_sync(0xffffffffu, total, 0);
@@ -179,78 +227,200 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const bool issuer = warp == 0 && ptx::elect_one();
   uint32_t parity = 0;
-  // Products of the pairs (A hi, lo) and (B hi, lo) over k16 steps of 16, the small ones first.  (Four steps to a turn, at
-  // fixed distances: computing descriptors between the MMAs took longer than the MMAs.)
-  auto products = [&](auto b_is_mn, uint32_t d, uint32_t n, int k16, uint32_t ah, uint32_t al, uint32_t bh, uint32_t bl) {
-    constexpr bool b_mn = decltype(b_is_mn)::value;
+  // One product over k16 steps of 16.  (Four steps to a turn, at fixed distances: computing descriptors between the MMAs took
+  // longer than the MMAs.)
+  const uint64_t k_of = ptx::smem_desc_sw128(0u, 16u, 1024u), mn_of = ptx::smem_desc_sw128(0u, 16384u, 1024u);
+  auto product = [&](auto a_is_mn, auto b_is_mn, uint32_t d, uint32_t n, int k16, uint32_t x, uint32_t y, uint32_t more) {
+    constexpr bool a_mn = decltype(a_is_mn)::value, b_mn = decltype(b_is_mn)::value;
+    constexpr uint64_t a_k = a_mn ? 128u : 2u, b_k = b_mn ? 128u : 2u, a_block = a_mn ? 512u : 1024u, b_block = b_mn ? 512u : 1024u;
+    const uint32_t idesc = ptx::idesc_f16(128, (int)n, a_mn, b_mn);
+    // (a shared address carries the CTA's rank above its 18 bits)
+    uint64_t da = (a_mn ? mn_of : k_of) + ((x & 0x3FFFFu) >> 4), db = (b_mn ? mn_of : k_of) + ((y & 0x3FFFFu) >> 4);
+    int k = k16;
+#pragma unroll 1
+    for (; k >= 4; k -= 4, da += a_block, db += b_block) {
+      if (issuer) {
+        ptx::mma_bf16(d, da, db, idesc, more);
+        ptx::mma_bf16(d, da + a_k, db + b_k, idesc, 1u);
+        ptx::mma_bf16(d, da + 2u * a_k, db + 2u * b_k, idesc, 1u);
+        ptx::mma_bf16(d, da + 3u * a_k, db + 3u * b_k, idesc, 1u);
+      }
+      more = 1u;
+    }
+#pragma unroll 1
+    for (; k > 0; --k, da += a_k, db += b_k) {
+      if (issuer) ptx::mma_bf16(d, da, db, idesc, more);
+      more = 1u;
+    }
+  };
+  // Those that `issue` makes, of what has been written to shared memory before.
+  auto products = [&](auto issue) {
     ptx::fence_proxy_async();
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
     if (warp == 0) {
-      const uint32_t idesc = ptx::idesc_f16(128, (int)n, 0, b_mn);
-      const uint64_t a_of = ptx::smem_desc_sw128(0u, 16u, 1024u), b_of = b_mn ? ptx::smem_desc_sw128(0u, 16384u, 1024u) : a_of;
-      constexpr uint64_t b_k = b_mn ? 128u : 2u, b_block = b_mn ? 512u : 1024u;
-#pragma unroll 1
-      for (int p = 0; p < 3; ++p) {
-        // (a shared address carries the CTA's rank above its 18 bits)
-        uint64_t da = a_of + (((p == 0 ? al : ah) & 0x3FFFFu) >> 4), db = b_of + (((p == 1 ? bl : bh) & 0x3FFFFu) >> 4);
-        uint32_t more = p != 0 ? 1u : 0u;
-        int k = k16;
-#pragma unroll 1
-        for (; k >= 4; k -= 4, da += 1024u, db += b_block) {
-          if (issuer) {
-            ptx::mma_bf16(d, da, db, idesc, more);
-            ptx::mma_bf16(d, da + 2u, db + b_k, idesc, 1u);
-            ptx::mma_bf16(d, da + 4u, db + 2u * b_k, idesc, 1u);
-            ptx::mma_bf16(d, da + 6u, db + 3u * b_k, idesc, 1u);
-          }
-          more = 1u;
-        }
-#pragma unroll 1
-        for (; k > 0; --k, da += 2u, db += b_k) {
-          if (issuer) ptx::mma_bf16(d, da, db, idesc, more);
-          more = 1u;
-        }
-      }
+      issue();
       if (issuer) ptx::mma_commit(bar);
       __syncwarp();
     }
-    (void)ptx::mbar_wait(bar, parity, &abort_flag, a.status, NS_ERR_SMALL);      // (after an expiry every later wait returns at once)
+    (void)ptx::mbar_wait(bar, parity, &abort_flag, a.status, NS_ERR_SMALL);
     parity ^= 1u;
     ptx::tc_fence_after();
   };
-  const int chunks = a.sp / 4;                             // 16-byte chunks of a row of fp32 values of A
-  auto share_at = [&](int row, int q) { return shares + (uint32_t)(row * chunks + (q ^ (row & 3))) * 16u; };
+  const std::false_type along_k;
+  const std::true_type along_mn;
+  const int chunks = a.sp / 4, all = a.sp * chunks;        // 16-byte chunks of fp32 values of a row of A, of A
+  const int senders = a.ctas * (a.sp == 16 ? 1 : 2);       // (a short side up to 16: hi and lo rows are added in the warp that has both)
+  auto sent_at = [&](int buf, int from, int idx) { return (uint32_t)((buf * senders + from) * all + (idx ^ ((idx >> 3) & 7))) * 16u; };
+  auto own_at = [&](int row, int q) { return shares + (uint32_t)(row * chunks + (q ^ (row & 3))) * 16u; };
+  const int mine0 = all * rank / a.ctas, mine1 = all * (rank + 1) / a.ctas;            // the part of A that this CTA sums
+  const uint32_t gram = s_hi + 8192u;                      // if everyone sums: A in fp32, [sp][sp], below the rows of P
 
 #pragma unroll 1
   for (int step = 0; step < a.steps; ++step) {
     const bool last = step + 1 == a.steps;
     // ---- A = X X^T: this CTA's share, then the sum of all
-    products(std::false_type(), d_s, (uint32_t)a.sp, a.w / 16, x_hi, x_lo, x_hi, x_lo);
-    if (quarter * 32 < a.sp) {
+    products([&] {
+      if (everyone) {
+        product(along_k, along_k, d_s, 2u * a.sp, a.w / 16, x_hi, x_hi, 0u);           // [hi; lo] [hi; lo]^T
+      } else if (stacked) {
+        product(along_k, along_k, d_s, 2u * a.sp, a.w / 16, x_hi, x_hi, 0u);           // hi [hi; lo]^T, and lo hi^T added to the right half
+        product(along_k, along_k, d_s + a.sp, a.sp, a.w / 16, x_lo, x_hi, 1u);
+      } else {
+        product(along_k, along_k, d_s, a.sp, a.w / 16, x_lo, x_hi, 0u);
+        product(along_k, along_k, d_s, a.sp, a.w / 16, x_hi, x_lo, 1u);
+        product(along_k, along_k, d_s, a.sp, a.w / 16, x_hi, x_hi, 1u);
+      }
+    });
+    // (what is sent alternates between two places: a sender may be a step ahead of a receiver)
+    const uint32_t got = bar_share + (uint32_t)(step & 1) * 8u;
+    if (everyone && threadIdx.x == 0) ptx::mbar_expect_tx(got, (uint32_t)(senders * all) * 16u);
+    const int rows = everyone ? 2 * a.sp : a.sp;
+    if (quarter * 32 < rows) {
+      const int lo = i >= a.sp ? 1 : 0, row = i - lo * a.sp;
 #pragma unroll 1
-      for (int c = half * 16; c < a.sp; c += 32) {
+      for (int c = everyone ? 0 : half * 16; c < a.sp; c += everyone ? 16 : 32) {
         uint32_t r[16];
+        float y[16];
         ptx::tmem_ld16(d_s + lanes + (uint32_t)c, r);
         ptx::tmem_ld_wait();
-        if (i < a.sp) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) st_shared_v4(share_at(i, c / 4 + q), r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+        for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(r[e]);
+        if (stacked) {                                     // the small products (lo rows of [hi; lo]: lo hi only)
+          ptx::tmem_ld16(d_s + lanes + (uint32_t)(a.sp + c), r);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] += lo ? 0.f : __uint_as_float(r[e]);
+        }
+        if (everyone) {                                    // (the two warps of a quarter send to half of the CTAs each)
+          if (a.sp == 16) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] += __shfl_down_sync(0xffffffffu, y[e], 16);
+          }
+          if (i < (a.sp == 16 ? 16 : rows)) {
+            const int from = a.sp == 16 ? rank : 2 * rank + lo, idx = row * chunks + c / 4;
+#pragma unroll 1
+            for (int r2 = half; r2 < a.ctas; r2 += 2) {
+              const uint32_t there = ptx::cluster_map(got, (uint32_t)r2), to = ptx::cluster_map(shares, (uint32_t)r2);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) ptx::send_data_v4(to + sent_at(step & 1, from, idx + q), there, y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+            }
+          }
+        } else if (i < rows) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            st_shared_v4(own_at(row, c / 4 + q), __float_as_uint(y[4 * q]), __float_as_uint(y[4 * q + 1]), __float_as_uint(y[4 * q + 2]), __float_as_uint(y[4 * q + 3]));
         }
       }
     }
+    if (everyone) {
+      (void)ptx::mbar_wait_sent(got, (uint32_t)(step >> 1) & 1u, &abort_flag, a.status, NS_ERR_SMALL);
+      if ((int)threadIdx.x < all) {
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int r = 0; r < senders; ++r) {
+          const uint4 u = ld_shared_v4(shares + sent_at(step & 1, r, (int)threadIdx.x));
+          f.x += __uint_as_float(u.x); f.y += __uint_as_float(u.y); f.z += __uint_as_float(u.z); f.w += __uint_as_float(u.w);
+        }
+        st_shared_v4(gram + threadIdx.x * 16u, __float_as_uint(f.x * kNsUnscale), __float_as_uint(f.y * kNsUnscale), __float_as_uint(f.z * kNsUnscale),
+                     __float_as_uint(f.w * kNsUnscale));
+      }
+      __syncthreads();
+      // ---- P = a I + b A + c A^2 in fp32: a lane to a column (or two warp halves to 16 of them), four rows a warp at most
+      const int col = a.sp == 16 ? lane & 15 : lane, row0 = a.sp == 16 ? warp * 2 + (lane >> 4) : warp;
+      const uint32_t pitch = (uint32_t)a.sp * 4u;
+      float sq[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int k = 0; k < a.sp; k += 4) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = ld_shared_f32(gram + (uint32_t)(k + e) * pitch + (uint32_t)col * 4u);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          if (n > 0 && a.sp == 16) break;
+          const uint4 u = ld_shared_v4(gram + (uint32_t)(row0 + 8 * n) * pitch + (uint32_t)k * 4u);
+          sq[n] = fmaf(__uint_as_float(u.x), x[0], sq[n]); sq[n] = fmaf(__uint_as_float(u.y), x[1], sq[n]);
+          sq[n] = fmaf(__uint_as_float(u.z), x[2], sq[n]); sq[n] = fmaf(__uint_as_float(u.w), x[3], sq[n]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        if (n > 0 && a.sp == 16) break;
+        const int row = row0 + 8 * n;
+        float y = fmaf(kNsUnscale * a.c, sq[n], a.b * ld_shared_f32(gram + (uint32_t)row * pitch + (uint32_t)col * 4u));
+        if (row == col && row < a.s) y += a.a * kNsScale;
+        const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(s_hi + at(row, col)), "h"(__half_as_ushort(h)) : "memory");
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(s_lo + at(row, col)), "h"(__half_as_ushort(l)) : "memory");
+      }
+      // ---- X <- P X as X^T P, whose rows, columns of X, keep all warps busy
+      products([&] {
+#pragma unroll 1
+        for (int g = 0; g < (a.w + 127) / 128; ++g) {
+          const uint32_t d = d_x + (uint32_t)(g * a.sp), further = (uint32_t)g * 32768u;
+          product(along_mn, along_k, d, a.sp, a.sp / 16, x_lo + further, s_hi, 0u);
+          product(along_mn, along_k, d, a.sp, a.sp / 16, x_hi + further, s_lo, 1u);
+          product(along_mn, along_k, d, a.sp, a.sp / 16, x_hi + further, s_hi, 1u);
+        }
+      });
+      const bool keep = last && !a.own_status && a.status->error != 0u;    // (a context whose device error stands keeps its parameters)
+      const int j = warp * 32 + lane;
+      if (warp * 32 < a.w) {
+#pragma unroll 1
+        for (int c = 0; c < a.sp; c += 16) {
+          uint32_t r[16];
+          ptx::tmem_ld16(d_x + lanes + (uint32_t)(half * a.sp + c), r);
+          ptx::tmem_ld_wait();
+          if (!last) {
+            const uint32_t o = (uint32_t)(j >> 6) * 16384u + (uint32_t)c * 128u + (uint32_t)(j & 7) * 2u, chunk = (uint32_t)(j & 63) >> 3;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float y = __uint_as_float(r[e]) * kNsUnscale;
+              const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
+              const uint32_t to = x_hi + o + (uint32_t)e * 128u + ((chunk ^ (uint32_t)(e & 7)) * 16u);
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(__half_as_ushort(h)) : "memory");
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + (x_lo - x_hi)), "h"(__half_as_ushort(l)) : "memory");
+            }
+          } else if (j < nj && !keep) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (c + e < a.s) ns_store_final(a.dst, m, a.tall ? j0 + j : c + e, a.tall ? c + e : j0 + j, __uint_as_float(r[e]) * (kNsUnscale * kNsUnscale));
+          }
+        }
+      }
+      continue;
+    }
     ptx::cluster_arrive_release();
     ptx::cluster_wait_acquire();
-    const int all = a.sp * chunks, mine1 = all * (rank + 1) / a.ctas;
 #pragma unroll 2
-    for (int idx = all * rank / a.ctas + (int)threadIdx.x; idx < mine1; idx += kNsSmallThreads) {
+    for (int idx = mine0 + (int)threadIdx.x; idx < mine1; idx += kNsSmallThreads) {
       const int row = idx / chunks, q = idx - row * chunks;
-      const uint32_t from = share_at(row, q);
+      const uint32_t from = own_at(row, q);
       float4 part[kNsSmallCtas], f = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int r = 0; r < kNsSmallCtas; ++r)
-        if (r < a.ctas) part[r] = ld_cluster_v4(ptx::cluster_map(from, (uint32_t)r));
+        if (r < a.ctas) part[r] = ptx::ld_cluster_v4(ptx::cluster_map(from, (uint32_t)r));
 #pragma unroll
       for (int r = 0; r < kNsSmallCtas; ++r)
         if (r < a.ctas) { f.x += part[r].x; f.y += part[r].y; f.z += part[r].z; f.w += part[r].w; }
@@ -260,14 +430,18 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
       const uint32_t l0 = pack_half2(f.x - b0.x, f.y - b0.y), l1 = pack_half2(f.z - b1.x, f.w - b1.y), o = at(row, q * 4);
 #pragma unroll 1
       for (int r = 0; r < a.ctas; ++r) {
-        st_cluster_v2(ptx::cluster_map(s_hi + o, (uint32_t)r), h0, h1);
-        st_cluster_v2(ptx::cluster_map(s_lo + o, (uint32_t)r), l0, l1);
+        ptx::st_cluster_v2(ptx::cluster_map(s_hi + o, (uint32_t)r), h0, h1);
+        ptx::st_cluster_v2(ptx::cluster_map(s_lo + o, (uint32_t)r), l0, l1);
       }
     }
     ptx::cluster_arrive_release();                         // A is whole, and its shares have been read
     ptx::cluster_wait_acquire();
     // ---- P = a I + b A + c A^2, in the place of A
-    products(std::false_type(), d_s, (uint32_t)a.sp, a.sp / 16, s_hi, s_lo, s_hi, s_lo);
+    products([&] {
+      product(along_k, along_k, d_s, a.sp, a.sp / 16, s_lo, s_hi, 0u);
+      product(along_k, along_k, d_s, a.sp, a.sp / 16, s_hi, s_lo, 1u);
+      product(along_k, along_k, d_s, a.sp, a.sp / 16, s_hi, s_hi, 1u);
+    });
     if (quarter * 32 < a.sp) {
 #pragma unroll 1
       for (int c = half * 16; c < a.sp; c += 32) {
@@ -299,7 +473,12 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
       }
     }
     // ---- X <- P X, in its place
-    products(std::true_type(), d_x, (uint32_t)a.w, a.sp / 16, s_hi, s_lo, x_hi, x_lo);
+    products([&] {
+      product(along_k, along_mn, d_x, a.w, a.sp / 16, s_lo, x_hi, 0u);
+      product(along_k, along_mn, d_x, a.w, a.sp / 16, s_hi, x_lo, 1u);
+      product(along_k, along_mn, d_x, a.w, a.sp / 16, s_hi, x_hi, 1u);
+    });
+    const bool keep = last && !a.own_status && a.status->error != 0u;      // (a context whose device error stands keeps its parameters)
     if (quarter * 32 < a.s) {
       const uint32_t box = s_hi + (uint32_t)(warp & 7) * 4096u;          // (P is not needed any more; 32 KB at least)
 #pragma unroll 1
@@ -326,7 +505,7 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
               st_shared_v4(x_lo + o, lo[0], lo[1], lo[2], lo[3]);
             }
           }
-        } else if (!a.own_status && a.status->error != 0u) {      // (a context whose device error stands keeps its parameters)
+        } else if (keep) {
         } else if (!a.tall) {
           if (c < nj) ns_finish(a.dst, a.vec_out, m, quarter * 32, j0 + c, a.s, min(a.l, j0 + a.w), box, lane, y);
         } else if (i < a.s) {                              // (lanes hold neighbouring columns of the result)
@@ -337,8 +516,14 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
       }
     }
   }
+  if (abort_flag) {                                        // what others have sent may still be in flight: let it land
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) { }
+  }
   ptx::tc_fence_before();
-  __syncthreads();                                         // (nobody touches this CTA's memory after the last step's second barrier)
+  __syncthreads();
+  ptx::cluster_arrive_release();                           // (nobody ends while something may be sent to it)
+  ptx::cluster_wait_acquire();
   if (warp == 1) { ptx::tmem_relinquish(); ptx::tmem_dealloc(tmem, 512); }
 }
 
