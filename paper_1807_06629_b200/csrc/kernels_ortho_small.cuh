@@ -56,6 +56,11 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
 __device__ __forceinline__ void st_cluster_v2(uint32_t at, uint32_t x, uint32_t y) {
   asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
 }
+__device__ __forceinline__ uint32_t tmem_ld1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
+  return r;
+}
 // A bounded wait for what other CTAs of the cluster have sent.
 __device__ __forceinline__ bool mbar_wait_sent(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* status, unsigned what) {
   long long t0 = 0;
@@ -117,7 +122,12 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
   }
   ptx::cluster_arrive_release();                           // (the barriers are there: waited for before the first is sent to)
   if (warp == 1) ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512);
-  for (uint32_t o = threadIdx.x * 16u; o < s_hi - x_hi + 2u * s_bytes; o += kNsSmallThreads * 16u) st_shared_v4(x_hi + o, 0u, 0u, 0u, 0u);
+  // X is zeroed: its rows that a product's result depends on (rows of an operand block beyond them reach only rows of the
+  // result that nobody reads, and all of A and P is written)
+  const uint32_t rows_bytes = (uint32_t)(stacked ? 2 * a.sp : a.sp) * 128u;
+#pragma unroll 1
+  for (uint32_t block = x_hi; block < s_hi; block += 16384u)
+    for (uint32_t o = threadIdx.x * 16u; o < rows_bytes; o += kNsSmallThreads * 16u) st_shared_v4(block + o, 0u, 0u, 0u, 0u);
 
   // element (i, j) of this CTA's X, i along the short side: G[i][j0 + j], or of a tall matrix G[j0 + j][i]
   const int j0 = rank * a.w, nj = max(0, min(a.w, a.l - j0));
@@ -320,8 +330,9 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
           }
           if (i < (a.sp == 16 ? 16 : rows)) {
             const int from = a.sp == 16 ? rank : 2 * rank + lo, idx = row * chunks + c / 4;
-#pragma unroll 1
-            for (int r2 = half; r2 < a.ctas; r2 += 2) {
+#pragma unroll
+            for (int r2 = half; r2 < kNsSmallCtas; r2 += 2) {
+              if (r2 >= a.ctas) break;
               const uint32_t there = ptx::cluster_map(got, (uint32_t)r2), to = ptx::cluster_map(shares, (uint32_t)r2);
 #pragma unroll
               for (int q = 0; q < 4; ++q) ptx::send_data_v4(to + sent_at(step & 1, from, idx + q), there, y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
@@ -376,23 +387,31 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
       }
       // ---- X <- P X as X^T P, whose rows, columns of X, keep all warps busy
       products([&] {
+        const uint32_t idesc = ptx::idesc_f16(128, a.sp, 1, 0);
+        const uint64_t xh = mn_of + ((x_hi & 0x3FFFFu) >> 4), xl = mn_of + ((x_lo & 0x3FFFFu) >> 4), ph = k_of + ((s_hi & 0x3FFFFu) >> 4), pl = k_of + ((s_lo & 0x3FFFFu) >> 4);
 #pragma unroll 1
-        for (int g = 0; g < (a.w + 127) / 128; ++g) {
-          const uint32_t d = d_x + (uint32_t)(g * a.sp), further = (uint32_t)g * 32768u;
-          product(along_mn, along_k, d, a.sp, a.sp / 16, x_lo + further, s_hi, 0u);
-          product(along_mn, along_k, d, a.sp, a.sp / 16, x_hi + further, s_lo, 1u);
-          product(along_mn, along_k, d, a.sp, a.sp / 16, x_hi + further, s_hi, 1u);
+        for (uint32_t k = 0; k < (uint32_t)a.sp / 16u; ++k) {
+          if (issuer) {
+#pragma unroll
+            for (uint32_t g = 0; g < 2; ++g) {             // 128 columns of X each (of the second, whatever lies behind w <= 128: not read)
+              const uint64_t x_at = g * 2048u + k * 128u;
+              ptx::mma_bf16(d_x + g * a.sp, xl + x_at, ph + 2u * k, idesc, k != 0u ? 1u : 0u);
+              ptx::mma_bf16(d_x + g * a.sp, xh + x_at, pl + 2u * k, idesc, 1u);
+              ptx::mma_bf16(d_x + g * a.sp, xh + x_at, ph + 2u * k, idesc, 1u);
+            }
+          }
         }
       });
       const bool keep = last && !a.own_status && a.status->error != 0u;    // (a context whose device error stands keeps its parameters)
       const int j = warp * 32 + lane;
       if (warp * 32 < a.w) {
+        const uint32_t from = d_x + lanes + (uint32_t)(half * a.sp);
+        if (!last) {
 #pragma unroll 1
-        for (int c = 0; c < a.sp; c += 16) {
-          uint32_t r[16];
-          ptx::tmem_ld16(d_x + lanes + (uint32_t)(half * a.sp + c), r);
-          ptx::tmem_ld_wait();
-          if (!last) {
+          for (int c = 0; c < a.sp; c += 16) {
+            uint32_t r[16];
+            ptx::tmem_ld16(from + (uint32_t)c, r);
+            ptx::tmem_ld_wait();
             const uint32_t o = (uint32_t)(j >> 6) * 16384u + (uint32_t)c * 128u + (uint32_t)(j & 7) * 2u, chunk = (uint32_t)(j & 63) >> 3;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -402,10 +421,12 @@ __global__ void __launch_bounds__(kNsSmallThreads, 1) ns_small_kernel(const __gr
               asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(__half_as_ushort(h)) : "memory");
               asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + (x_lo - x_hi)), "h"(__half_as_ushort(l)) : "memory");
             }
-          } else if (j < nj && !keep) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (c + e < a.s) ns_store_final(a.dst, m, a.tall ? j0 + j : c + e, a.tall ? c + e : j0 + j, __uint_as_float(r[e]) * (kNsUnscale * kNsUnscale));
+          }
+        } else if (!keep) {                                // (rolled: what runs once is fetched anew, at about 20 cycles an instruction)
+#pragma unroll 1
+          for (int c = 0; c < a.s; ++c) {
+            const float y = __uint_as_float(ptx::tmem_ld1(from + (uint32_t)c)) * (kNsUnscale * kNsUnscale);
+            if (j < nj) ns_store_final(a.dst, m, a.tall ? j0 + j : c, a.tall ? c : j0 + j, y);
           }
         }
       }

@@ -86,6 +86,20 @@ def test_orthogonalize_matches_the_formula(b, shape, precision):
         assert rel(got[i], want[i]) <= TOL[precision] * 2
 
 
+@pytest.mark.parametrize("steps", [1, 2, 5])
+@pytest.mark.parametrize("shape", [(3, 15, 900), (9, 16, 129), (2, 17, 2048), (2, 32, 2048), (2, 2047, 31), (40, 32, 64), (1, 33, 1500), (2, 700, 48), (3, 64, 2048),
+                                   (3, 65, 1536), (2, 112, 1300), (4, 1000, 10), (2, 300, 2500), (1, 2700, 520)])
+def test_orthogonalize_forms_by_short_side_and_number_of_parts(b, shape, steps):
+    """Short sides around 16, 32, 64 and 128 in clusters of 1 to 8, and chains whose X X^T is formed in parts; twice, the same bits."""
+    G = matrices(23, *shape)
+    for precision in (0, 1):
+        got = b.prsgd_orthogonalize(G, steps=steps, precision=precision, workspace=(w := workspace(b, G, precision)))
+        again = b.prsgd_orthogonalize(G, steps=steps, precision=precision, workspace=w)
+        b.prsgd_work_status(w)
+        assert torch.equal(got, again)
+        assert rel(got, ref.orthogonalize(G, steps=steps)) <= TOL[precision]
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("out_dtype", [F32, BF16, F16])
 def test_orthogonalize_types(b, dtype, out_dtype):
