@@ -5,11 +5,13 @@
 //   dlogit_te = p_te (h_te - sum_j p_tj h_tj),  h_te = dloss coef E c_e / (k T) / T + [e chosen] dweight
 #pragma once
 #include "ops_common.cuh"
+#include "tc_ptx.cuh"
 
 namespace prsgd {
 
 constexpr int kRouteMaxExperts = 1024;
 constexpr int kRouteMaxK = 32;
+constexpr int kRouteCluster = 8;        // most blocks of a group that make a cluster
 constexpr int kRouteBlocks = 64;        // most blocks of a group: rows of its partial sums in the workspace
 
 struct RouteArgs {
@@ -22,6 +24,7 @@ struct RouteArgs {
   int32_t* counts; float* mean; float* loss;   // [G][E], [G][E], [G]
   float* part_p; int32_t* part_c; int32_t* part_n;   // [G][blocks][E] twice, [G][blocks]
   int blocks;
+  int clustered;                // the blocks of a group are a cluster, whose first finishes the group
   int vec, vec_out;             // rows can be read / written 16 bytes at a time
   // gradient
   const float* dweights; const float* dloss; void* dlogits; int64_t d_row_stride, d_group_stride;
@@ -40,49 +43,53 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sums a group's partial results in a fixed order and forms its loss; all 256 threads of a block.  Each warp takes every
-// eighth block's sums, lanes along the experts, so that their loads are in flight together (a thread per expert that
-// walked all blocks took 16 us for 18 blocks of 100 experts).
-__device__ __forceinline__ void route_finish(const RouteArgs& a, int64_t g) {
-  __shared__ float s_p[8][256];
-  __shared__ int s_c[8][256];
-  __shared__ float s_w[8];
+// Sums a group's partial results in a fixed order and forms its loss: a cluster, of which each block takes a multiple of 32
+// experts.  Each warp takes every eighth row of sums, lanes along the experts, so that their loads are in flight together (a
+// thread per expert that walked all rows took 16 us for 18 rows of 100 experts; with one block for all experts of a group the
+// whole call took 79 us at 4 x 4096 x 1024, now 40, and 52.6 us at 16 x 16384 x 128, now 50.4).
+constexpr int kRouteFinish = 8, kRouteFinishExperts = kRouteMaxExperts / kRouteFinish;
+__host__ __device__ constexpr int route_finish_blocks(int E) { return E >= 32 * kRouteFinish ? kRouteFinish : (E + 31) / 32; }
+__global__ void __launch_bounds__(256) route_finish_kernel(const RouteArgs a) {
+  op_pdl_wait();
+  op_pdl_trigger();
+  __shared__ float s_p[8][kRouteFinishExperts];
+  __shared__ int s_c[8][kRouteFinishExperts];
+  __shared__ float s_w[8], s_loss;
   __shared__ int s_alive;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, parts = (int)gridDim.x;
+  const int64_t g = blockIdx.y;
+  const int width = ((a.E + parts - 1) / parts + 31) / 32 * 32, e0 = (int)blockIdx.x * width;
   if (warp == 0) {
     int n = 0;
     for (int b = lane; b < a.blocks; b += 32) n += a.part_n[g * a.blocks + b];
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) s_alive = n;
   }
-  float mine = 0.f;
-  for (int e0 = 0; e0 < a.E; e0 += 256) {
-    for (int e = e0 + lane; e < min(a.E, e0 + 256); e += 32) {
-      float p = 0.f;
-      int c = 0;
+  for (int q = lane; q < width && e0 + q < a.E; q += 32) {
+    float p = 0.f;
+    int c = 0;
 #pragma unroll 4
-      for (int b = warp; b < a.blocks; b += 8) {
-        const int64_t at = (g * a.blocks + b) * a.E + e;
-        p += a.part_p[at];
-        c += a.part_c[at];
-      }
-      s_p[warp][e - e0] = p;
-      s_c[warp][e - e0] = c;
+    for (int b = warp; b < a.blocks; b += 8) {
+      const int64_t at = (g * a.blocks + b) * a.E + e0 + q;
+      p += a.part_p[at];
+      c += a.part_c[at];
     }
-    __syncthreads();
-    const float live = s_alive > 0 ? (float)s_alive : 1.f;
-    const int e = e0 + (int)threadIdx.x;
-    if (e < a.E) {
-      float p = 0.f;
-      int c = 0;
+    s_p[warp][q] = p;
+    s_c[warp][q] = c;
+  }
+  __syncthreads();
+  const float live = s_alive > 0 ? (float)s_alive : 1.f;
+  const int q = (int)threadIdx.x, e = e0 + q;
+  float mine = 0.f;
+  if (q < width && e < a.E) {
+    float p = 0.f;
+    int c = 0;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) { p += s_p[w][threadIdx.x]; c += s_c[w][threadIdx.x]; }
-      p /= live;
-      a.mean[g * a.E + e] = p;
-      a.counts[g * a.E + e] = c;
-      mine += ((float)c / ((float)a.k * live)) * p;
-    }
-    __syncthreads();
+    for (int w = 0; w < 8; ++w) { p += s_p[w][q]; c += s_c[w][q]; }
+    p /= live;
+    a.mean[g * a.E + e] = p;
+    a.counts[g * a.E + e] = c;
+    mine = ((float)c / ((float)a.k * live)) * p;
   }
   mine = warp_sum(mine);
   if (lane == 0) s_w[warp] = mine;
@@ -91,29 +98,72 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, int64_t g) {
     float s = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) s += s_w[w];
+    s_loss = s;
+  }
+  ptx::cluster_arrive_release();
+  ptx::cluster_wait_acquire();
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    float s = s_loss;
+    for (int r = 1; r < parts; ++r) s += ptx::ld_cluster_f32(ptx::cluster_map(ptx::smem_u32(&s_loss), (uint32_t)r));
     a.loss[g] = a.coef * (float)a.E * s;
   }
-}
-
-__global__ void __launch_bounds__(256) route_finish_kernel(const RouteArgs a) {
-  op_pdl_wait();
-  op_pdl_trigger();
-  route_finish(a, blockIdx.x);
+  ptx::cluster_arrive_release();                         // (nobody ends while its sum may be read)
+  ptx::cluster_wait_acquire();
 }
 
 // What a block adds to its group (p: its 8 warps' sums over tokens, n tokens): a row of the group's partial sums, or, of a
-// group of one block, the group's results.
+// group of one block or one cluster, the group's results.
 template <int W>
-__device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g, const float (&p)[8][W], const int* c, int n) {
+__device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g, float (&p)[8][W], int* c, int* p_n) {
   __shared__ float s_loss[8];
   const int64_t slot = g * a.blocks + blockIdx.x;
+  int n = *p_n;
+  if (a.clustered) {                                     // the first block adds the others' sums, in their order, to its own
+    for (int e = threadIdx.x; e < a.E; e += 256) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) s += p[w][e];
+      p[0][e] = s;
+    }
+    ptx::cluster_arrive_release();
+    ptx::cluster_wait_acquire();
+    if (blockIdx.x == 0) {
+      const uint32_t at_p = ptx::smem_u32(&p[0][0]), at_c = ptx::smem_u32(c), at_n = ptx::smem_u32(p_n);
+      for (int r = 1; r < a.blocks; ++r) n += (int)ptx::ld_cluster_u32(ptx::cluster_map(at_n, (uint32_t)r));
+      for (int e = threadIdx.x; e < a.E; e += 256) {
+        float s[kRouteCluster];
+        int k[kRouteCluster];
+#pragma unroll
+        for (int r = 1; r < kRouteCluster; ++r)
+          if (r < a.blocks) {
+            s[r] = ptx::ld_cluster_f32(ptx::cluster_map(at_p, (uint32_t)r) + 4u * (uint32_t)e);
+            k[r] = (int)ptx::ld_cluster_u32(ptx::cluster_map(at_c, (uint32_t)r) + 4u * (uint32_t)e);
+          }
+        float sum = p[0][e];
+        int count = c[e];
+#pragma unroll
+        for (int r = 1; r < kRouteCluster; ++r)
+          if (r < a.blocks) { sum += s[r]; count += k[r]; }
+        p[0][e] = sum;
+        c[e] = count;
+      }
+    }
+    ptx::cluster_arrive_release();                       // (nobody ends while its sums may be read)
+    ptx::cluster_wait_acquire();
+    if (blockIdx.x != 0) return;
+  }
+  const bool whole = a.blocks == 1 || a.clustered;
   const float live = n > 0 ? (float)n : 1.f;
   float mine = 0.f;
   for (int e = threadIdx.x; e < a.E; e += 256) {
     float s = 0.f;
+    if (a.clustered) {
+      s = p[0][e];
+    } else {
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += p[w][e];
-    if (a.blocks > 1) {
+      for (int w = 0; w < 8; ++w) s += p[w][e];
+    }
+    if (!whole) {
       a.part_p[slot * a.E + e] = s;
       a.part_c[slot * a.E + e] = c[e];
     } else {
@@ -123,7 +173,7 @@ __device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g, const
       mine += ((float)c[e] / ((float)a.k * live)) * s;
     }
   }
-  if (a.blocks > 1) {
+  if (!whole) {
     if (threadIdx.x == 0) a.part_n[slot] = n;
     return;
   }
@@ -221,7 +271,7 @@ __global__ void __launch_bounds__(256, 2) route_kernel(const RouteArgs a) {
   for (int i = 0; i < PER; ++i) s_p[warp][lane + 32 * i] = acc[i];
   if (lane == 0 && alive) atomicAdd(&s_n, alive);
   __syncthreads();
-  route_leave(a, g, s_p, s_c, s_n);
+  route_leave(a, g, s_p, s_c, &s_n);
 }
 
 // ---- top_k <= 8: a few lanes per token ------------------------------------------------------------------------
@@ -458,7 +508,7 @@ __global__ void __launch_bounds__(256, 2) route_lanes_kernel(const RouteArgs a) 
   alive = __reduce_add_sync(0xffffffffu, alive);
   if (lane == 0 && alive) atomicAdd(&s_n, alive);
   __syncthreads();
-  route_leave(a, g, s_p, s_c, s_n);
+  route_leave(a, g, s_p, s_c, &s_n);
 }
 
 // Gradient, any top_k (OWN choices of a token to a lane).  dlogit_e = p_e (h_e - dot) with h the balance loss's part, the same for all tokens of a group, and

@@ -297,6 +297,20 @@ def test_route_masks(b, E, k):
     check_route(b, x, k, live=live, normalize=True)
 
 
+@pytest.mark.parametrize("E,k,G,T", [(64, 8, 5, 65), (64, 8, 36, 512), (64, 8, 37, 513), (64, 4, 3, 1024), (64, 4, 3, 1025), (1000, 2, 2, 128), (1000, 8, 2, 129), (128, 8, 140, 128),
+                                     (7, 2, 2, 4096), (129, 3, 1, 513), (1024, 3, 2, 3000)])
+def test_route_groups_of_one_cluster_and_of_many_blocks(b, E, k, G, T):
+    """Both sides of where a group's blocks are a cluster; twice, the same bits; every third token off, one group all off."""
+    x = logits_of(48, G, T, E)
+    live = torch.ones(G, T, dtype=torch.uint8, device="cuda:0")
+    live[:, ::3] = 0
+    live[G - 1] = 0
+    got = check_route(b, x, k, live=live, normalize=True)
+    again = b.prsgd_route(x, k, 0.1, normalize=True, live=live)
+    for p, q in zip(got[:4], again[:4]):
+        assert torch.equal(p, q)
+
+
 def test_route_with_nan_in_a_live_token(b):
     x = logits_of(44, 3, 40, 16)
     x[1, 5, 3] = float("nan")
