@@ -513,8 +513,8 @@ int prsgd_mean_rows_noalloc(const float* d_P, int64_t N, int64_t m, int64_t row_
  * magnitude, and such that no singular value grows beyond a few units) five steps bring the singular values of G near
  * 1 and keep its singular vectors.  Tall matrices are iterated from their short side, the result is the same.
  * precision: PRSGD_PRECISION_FP32 computes to about fp32 accuracy (products of fp16 pairs, three per product),
- * PRSGD_PRECISION_BF16 to about 1e-3 of the result's norm (single fp16 operands); both sum in fp32, and the norm in
- * 64 bits.  A zero matrix gives zeros (eps > 0); one that holds a NaN or an infinity gives NaN and leaves the others
+ * PRSGD_PRECISION_BF16 to about 2e-3 of the result's norm (single fp16 operands: half a rounding of bfloat16, but five of
+ * float16); both sum in fp32, and the norm in 64 bits.  A zero matrix gives zeros (eps > 0); one that holds a NaN or an infinity gives NaN and leaves the others
  * alone.  out may be G itself (same type and strides).  G and out: aligned to their element type; multiples of
  * 16 bytes in address and strides are fastest. */
 #define PRSGD_ORTHO_MAX_SIDE 65536

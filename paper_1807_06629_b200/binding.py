@@ -267,8 +267,13 @@ def _size3(t: torch.Tensor):
 
 
 def _precision_for(t: torch.Tensor) -> int:
-    """32-bit results are computed to 32-bit accuracy, 16-bit ones from single 16-bit operands."""
+    """Of a step on weights of t's type: 16-bit ones are rounded by more than single 16-bit operands cost the step."""
     return PRECISION_FP32 if t.dtype is torch.float32 else PRECISION_BF16
+
+
+def _precision_for_result(t: torch.Tensor) -> int:
+    """Of a result of t's type: single 16-bit operands cost about 2e-3, half a rounding of bfloat16, but five of float16."""
+    return PRECISION_BF16 if t.dtype is torch.bfloat16 else PRECISION_FP32
 
 
 def _same_place(name: str, t: torch.Tensor, index: int) -> None:
@@ -284,11 +289,13 @@ def prsgd_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, precis
 
 def orthogonalize_workspace(G: torch.Tensor, precision: Optional[int] = None, stream=None) -> torch.Tensor:
     """Workspace of prsgd_orthogonalize for matrices like G (results of G's type unless `precision` says otherwise)."""
-    p = _precision_for(G) if precision is None else precision
+    p = _precision_for_result(G) if precision is None else precision
     return _empty(prsgd_orthogonalize_workspace_bytes(*_size3(G), p), torch.uint8, G.device, stream)
 
 
-muon_workspace = orthogonalize_workspace
+def muon_workspace(W: torch.Tensor, precision: Optional[int] = None, stream=None) -> torch.Tensor:
+    """Workspace of prsgd_muon_step for weights like W."""
+    return orthogonalize_workspace(W, _precision_for(W) if precision is None else precision, stream)
 
 
 def _coefs(coefs):
@@ -303,7 +310,7 @@ def prsgd_orthogonalize(G: torch.Tensor, out: Optional[torch.Tensor] = None, *, 
         out = _empty(G.shape, G.dtype, G.device, stream)
     elif out.shape != G.shape:
         raise ValueError("out must have G's shape")
-    p = _precision_for(out) if precision is None else precision
+    p = _precision_for_result(out) if precision is None else precision
     if workspace is None:
         workspace = orthogonalize_workspace(G, p, stream)
     index = G.get_device()

@@ -86,6 +86,18 @@ def test_orthogonalize_matches_the_formula(b, shape, precision):
         assert rel(got[i], want[i]) <= TOL[precision] * 2
 
 
+@pytest.mark.parametrize("shape", [(2, 300, 515), (1, 700, 260), (2, 60, 90)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_orthogonalize_of_a_type_is_as_exact_as_the_type(b, dtype, shape):
+    """Without a precision asked for: a half-step of the result's type beside what the chain allows, single operands for
+    bfloat16, pairs for float16 and float32."""
+    G = matrices(29, *shape, dtype=dtype)
+    got = b.prsgd_orthogonalize(G)
+    assert got.dtype == dtype
+    assert rel(got, ref.orthogonalize(G)) <= half_step(dtype) + (TOL[1] if dtype == BF16 else TOL[0])
+    assert torch.equal(got, b.prsgd_orthogonalize(G, workspace=b.orthogonalize_workspace(G)))
+
+
 @pytest.mark.parametrize("steps", [1, 2, 5])
 @pytest.mark.parametrize("shape", [(3, 15, 900), (9, 16, 129), (2, 17, 2048), (2, 32, 2048), (2, 2047, 31), (40, 32, 64), (1, 33, 1500), (2, 700, 48), (3, 64, 2048),
                                    (3, 65, 1536), (2, 112, 1300), (4, 1000, 10), (2, 300, 2500), (1, 2700, 520)])
