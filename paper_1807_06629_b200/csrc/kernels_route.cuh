@@ -592,16 +592,18 @@ __global__ void __launch_bounds__(256, route_grad_blocks(PER)) route_grad_kernel
     for (int i = 0; i < PER; ++i) mx = fmaxf(mx, x[i]);
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const float top = mx == -INFINITY ? 0.f : mx * kLog2E;
+    const float top = mx == -INFINITY ? 0.f : mx;
     float sum = 0.f, dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      x[i] = route_exp2(fmaf(x[i], kLog2E, -top));
+    for (int i = 0; i < PER; i += 2) {
+      route_exp_below(x[i], x[i + 1], top);
       sum += x[i];
+      sum += x[i + 1];
       dot = fmaf(x[i], h[i], dot);
+      dot = fmaf(x[i + 1], h[i + 1], dot);
     }
     sum = lanes_sum<L>(sum);
-    const bool dead = sum == 0.f;                     // (a NaN or +inf among the logits makes the sum NaN, and the row with it)
+    const bool dead = sum == 0.f;                     // only of a row of -inf: else the largest adds 1 (a NaN or +inf makes the sum NaN, and the row with it)
     const float inv = dead ? 0.f : 1.f / sum;
     dot = lanes_sum<L>(dot) * inv;
     float pj[OWN];
@@ -609,7 +611,7 @@ __global__ void __launch_bounds__(256, route_grad_blocks(PER)) route_grad_kernel
       float pick = 0.f, pull = 0.f;
 #pragma unroll
       for (int q = 0; q < OWN; ++q) {
-        pj[q] = route_exp2(fmaf(xj[q], kLog2E, -top)) * inv;
+        pj[q] = route_exp_below(xj[q], top) * inv;
         pick += pj[q];
         pull = fmaf(pj[q], dw[q], pull);
       }

@@ -74,3 +74,33 @@ def test_a_group_with_a_row_of_the_lowest_value_keeps_its_loss(b):
         want = ref.route(x, 8, 0.01)
         assert torch.equal(experts.long(), want[0]) and (weights[1, 300].double() - 1 / 64).abs().max() <= 5e-6 / 64
         assert ((loss.double() - want[4]).abs() <= 1e-5 * want[4].abs()).all() and mean.isfinite().all()
+
+
+@pytest.mark.parametrize("use", [("dw",), ("dl",), ("dw", "dl")], ids="+".join)
+@pytest.mark.parametrize("normalize", [False, True])
+@pytest.mark.parametrize("E,k", [(6, 2), (8, 8), (64, 8), (64, 9), (130, 4), (300, 1), (1000, 8), (40, 20)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_route_grad_of_very_large_logits(b, dtype, E, k, normalize, use):
+    """Rows are live, whatever finite numbers they hold: no NaN, and no zeros for them."""
+    x = extremes(dtype, E)
+    G, T = x.shape[:2]
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(9)
+    chosen, _, counts, _, _ = ref.route(x, k, 0.05, normalize)
+    dw = torch.randn(G, T, k, generator=g, device="cuda:0") if "dw" in use else None
+    dl = (torch.rand(G, generator=g, device="cuda:0") + 0.5) * T * T if "dl" in use else None
+    got = b.prsgd_route_grad(x, chosen.int(), counts.int(), 0.05, normalize=normalize, dweights=dw, dloss=dl)
+    want = ref.route_grad(x, chosen, counts, 0.05, normalize, None, dw, dl)
+    p = torch.softmax(x.double(), -1)
+    # |h| of a token: the balance part's largest, and of the weights' part dw, over the sum of the chosen p where that is divided out
+    up = torch.zeros(G, T, 1, dtype=torch.float64, device="cuda:0")
+    if dl is not None:
+        up += (dl.double() * 0.05 * E / T * counts.amax(1) / (k * T))[:, None, None]
+    if dw is not None:
+        scale = p.gather(-1, chosen).sum(-1, keepdim=True) if normalize else 1.0
+        up += 2 * dw.abs().amax(-1, keepdim=True) / scale
+    half = 0.0 if dtype == F32 else torch.finfo(dtype).eps / 2
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    assert ((got.double() - want).abs() <= 2e-5 * p.amax(-1, keepdim=True) * up + half * want.abs() * 1.01 + tiny).all()
+    if "dl" in use and k < E:
+        assert (got[0, ::3] != 0).any(-1).all()        # (rows of one value: each has a part of the balance loss's gradient)
