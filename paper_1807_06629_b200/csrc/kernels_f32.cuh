@@ -2,6 +2,7 @@
 // with the forward, backward and SGD-update epilogues fused in, and the
 // softmax cross-entropy gradient.  All sums run in a fixed order.
 #pragma once
+#include "choice_key.h"
 #include "prsgd_common.cuh"
 
 namespace prsgd {
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(256) softmax_ce_kernel(const SoftmaxArgs a) {
 }
 
 // The same with a balance loss added to F_i (prsgd_set_balance): with p_bc the softmax, c_c the number of rows that have
-// class c among their k largest logits (ties: lowest index) and f_c = c_c / (k B),
+// class c among their k largest logits (ties: lowest index; a NaN ranks first) and f_c = c_c / (k B),
 //   loss_b += coef C dot_b,  dot_b = sum_c f_c p_bc;   delta_bc += coef C / B p_bc (f_c - dot_b).
 // One block of 256 threads per worker: the counts need all rows before any gradient.
 constexpr int kBalanceMaxClasses = 1024;
@@ -319,12 +320,11 @@ __global__ void __launch_bounds__(256) softmax_ce_balance_kernel(const SoftmaxAr
   __syncthreads();
   for (int b = warp; b < a.B; b += 8) {
     const float* z = a.logits + ((int64_t)n * a.B + b) * a.ldz;
-    unsigned long long above = ~0ull;                    // (order of the logit, 2^32 - 1 - index) of the choice before
+    unsigned long long above = kChoiceAll;               // the choice before
     for (int j = 0; j < k; ++j) {
       unsigned long long best = 0ull;
       for (int c = lane; c < a.C; c += 32) {
-        const uint32_t u = __float_as_uint(z[c] + 0.f);
-        const unsigned long long key = ((unsigned long long)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (0xFFFFFFFFu - (uint32_t)c);
+        const unsigned long long key = choice_key(__float_as_uint(z[c]), (uint32_t)c);
         if (key < above && key > best) best = key;
       }
 #pragma unroll
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(256) softmax_ce_balance_kernel(const SoftmaxAr
         best = other > best ? other : best;
       }
       above = best;
-      if (lane == 0) atomicAdd(&s_count[0xFFFFFFFFu - (uint32_t)best], 1);
+      if (lane == 0) atomicAdd(&s_count[choice_index(best)], 1);
     }
   }
   __syncthreads();
