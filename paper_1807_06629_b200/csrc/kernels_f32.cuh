@@ -2,6 +2,7 @@
 // with the forward, backward and SGD-update epilogues fused in, and the
 // softmax cross-entropy gradient.  All sums run in a fixed order.
 #pragma once
+#include <cuda_bf16.h>
 #include "choice_key.h"
 #include "prsgd_common.cuh"
 
@@ -264,11 +265,8 @@ struct SoftmaxArgs {
   const DeviceStatus* status;   // tensor-core path: a recorded expired wait turns the launch into a no-op
 };
 
-__device__ __forceinline__ uint16_t f32_to_bf16_rn(float f) {
-  uint32_t u = __float_as_uint(f);
-  u += 0x7FFFu + ((u >> 16) & 1u);
-  return (uint16_t)(u >> 16);
-}
+// (a NaN stays one: adding the rounding to its bits would make a zero of it, and hide a worker that has diverged)
+__device__ __forceinline__ uint16_t f32_to_bf16_rn(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
 
 __global__ void __launch_bounds__(256) softmax_ce_kernel(const SoftmaxArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");   // no-op unless launched as a programmatic dependent

@@ -59,3 +59,24 @@ def test_every_class_chosen_is_an_even_share(w):
     step = np.linalg.norm(out[0][0] - x0)
     # deltas differ by C 2^-23 coef / B of at most 1 / B: relative to their norm far below 1e-4; on the bf16 path one in a few may round the other way
     assert np.linalg.norm(out[1][0] - out[0][0]) <= (1e-4 if w.precision == 0 else 2.0 ** -8) * step
+
+
+@pytest.mark.parametrize("balance", [False, True])
+@pytest.mark.parametrize("w", [F32, BF16, BF16.with_(dims=(128, 192, 200)), BF16.with_(dims=(64, 10))], ids=["f32", "bf16", "200-classes", "one-layer"])
+def test_a_nan_in_the_outputs_reaches_the_weights(w, balance):
+    """A diverged worker is seen in its parameters: NaN deltas do not become zeros when they are rounded to bf16, and the step of every
+    class's weights and bias is NaN."""
+    C = w.dims[-1]
+    X, Y, x0 = make_inputs(w)
+    x = np.tile(x0, (w.N, 1)).astype(np.float32)
+    x[1, x.shape[1] - C] = np.nan
+    p = make_ctx(w, X, Y, x0, I=0)
+    p.set_params_stacked(x)
+    if balance:
+        p.set_balance(0.5, 2)
+    else:
+        p.set_option(5, 0)                             # PRSGD_OPT_FUSED_EPILOGUES
+    p.local_steps(1)
+    after = p.get_params_stacked()
+    p.close()
+    assert np.isnan(after[1, -C * (w.dims[-2] + 1):]).all() and np.isfinite(after[[0, 2]]).all()
