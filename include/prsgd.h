@@ -502,7 +502,7 @@ int prsgd_mean_rows_noalloc(const float* d_P, int64_t N, int64_t m, int64_t row_
  * graphs replayed side by side) need one each.  Array elements are one of the types below; matrices are row-major with
  * a row stride (elements, >= cols) and a stride between the matrices of a batch.  Inputs may be broadcast over the batch
  * (batch stride 0); outputs may not overlap.  A batch, side, group or token count of 0 is a call that does nothing
- * (the router then still writes zero counts and loss). */
+ * (the router then still writes zero counts and loss, and any call clears the status of the workspace it is given). */
 #define PRSGD_TYPE_FP32 0
 #define PRSGD_TYPE_BF16 1
 #define PRSGD_TYPE_FP16 2
@@ -537,7 +537,7 @@ int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_b
                     int32_t steps, const float* h_coefs, float scale, float eps, int32_t precision,
                     void* d_work, size_t work_bytes, void* cuda_stream);
 
-/* Device errors of the last call that used this workspace (a bounded wait that expired): PRSGD_OK or
+/* Device errors of the last call that was given this workspace, the router included (a bounded wait that expired): PRSGD_OK or
  * PRSGD_ERR_DEVICE_TIMEOUT, after which that call's outputs are not to be used.  Synchronises the stream. */
 int prsgd_work_status(const void* d_work, void* cuda_stream);
 

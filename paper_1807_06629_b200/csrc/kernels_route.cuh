@@ -23,6 +23,7 @@ struct RouteArgs {
   int32_t* experts; float* weights;       // [G][T][k]
   int32_t* counts; float* mean; float* loss;   // [G][E], [G][E], [G]
   float* part_p; int32_t* part_c; int32_t* part_n;   // [G][blocks][E] twice, [G][blocks]
+  DeviceStatus* status;         // of the workspace: cleared by the call (the router waits for nothing that could expire)
   int blocks;
   int clustered;                // the blocks of a group are a cluster, whose first finishes the group
   int vec, vec_out;             // rows can be read / written 16 bytes at a time
@@ -43,6 +44,10 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+__device__ __forceinline__ void route_clear_status(const RouteArgs& a) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.status->error = 0u;
+}
+
 // Sums a group's partial results in a fixed order and forms its loss: a cluster, of which each block takes a multiple of 32
 // experts.  Each warp takes every eighth row of sums, lanes along the experts, so that their loads are in flight together (a
 // thread per expert that walked all rows took 16 us for 18 rows of 100 experts; with one block for all experts of a group the
@@ -52,6 +57,7 @@ __host__ __device__ constexpr int route_finish_blocks(int E) { return E >= 32 * 
 __global__ void __launch_bounds__(256) route_finish_kernel(const RouteArgs a) {
   op_pdl_wait();
   op_pdl_trigger();
+  if (a.blocks == 0) route_clear_status(a);              // (no tokens: the only launch)
   __shared__ float s_p[8][kRouteFinishExperts];
   __shared__ int s_c[8][kRouteFinishExperts];
   __shared__ float s_w[8], s_loss;
@@ -194,6 +200,7 @@ __global__ void __launch_bounds__(256, 2) route_kernel(const RouteArgs a) {
   using T = typename ElemOf<TY>::type;
   op_pdl_wait();
   op_pdl_trigger();
+  route_clear_status(a);
   __shared__ float s_p[8][PER * 32];
   __shared__ int s_c[PER * 32];
   __shared__ int s_n;
@@ -423,6 +430,7 @@ __global__ void __launch_bounds__(256, 2) route_lanes_kernel(const RouteArgs a) 
   constexpr int V = 16 / sizeof(T), TOK = 32 / L;     // tokens of a warp at a time
   op_pdl_wait();
   op_pdl_trigger();
+  route_clear_status(a);
   __shared__ float s_p[8][PER * L];
   __shared__ int s_c[PER * L];
   __shared__ int s_n;

@@ -12,6 +12,13 @@ namespace prsgd {
 // Records the text prsgd_last_error(NULL) returns and hands the code back (defined in prsgd_api.cu).
 int op_fail(int code, const std::string& msg);
 
+// The status words at the head of the workspace of a call that has nothing to compute (a call without a workspace has none).
+inline int op_clear_status(void* d_work, size_t bytes, void* stream) {
+  if (d_work == nullptr || bytes < sizeof(DeviceStatus)) return PRSGD_OK;
+  const cudaError_t e = cudaMemsetAsync(d_work, 0, sizeof(DeviceStatus), static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PRSGD_OK : op_fail(PRSGD_ERR_CUDA, std::string("clearing a workspace's status: ") + cudaGetErrorString(e));
+}
+
 template <int T> struct ElemOf;
 template <> struct ElemOf<PRSGD_TYPE_FP32> { using type = float; };
 template <> struct ElemOf<PRSGD_TYPE_BF16> { using type = __nv_bfloat16; };

@@ -280,7 +280,7 @@ int prsgd_orthogonalize(const void* d_G, int32_t g_type, int64_t g_row_stride, i
   if (rc == PRSGD_OK) rc = check_chain(steps, h_coefs, eps, &p);
   if (rc != PRSGD_OK) return rc;
   if (!std::isfinite(scale)) return op_fail(PRSGD_ERR_ARG, "scale must be finite");
-  if (batch == 0 || rows == 0 || cols == 0) return PRSGD_OK;
+  if (batch == 0 || rows == 0 || cols == 0) return op_clear_status(d_work, work_bytes, cuda_stream);
   rc = check_matrices("G", d_G, g_type, g_row_stride, g_batch_stride, batch, rows, cols, false);
   if (rc == PRSGD_OK) rc = check_matrices("out", d_out, out_type, out_row_stride, out_batch_stride, batch, rows, cols, true);
   p.shape = {batch, rows, cols}; p.precision = precision; p.g_type = g_type;
@@ -305,7 +305,7 @@ int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_b
   if (!(mu >= 0.f && mu < 1.f)) return op_fail(PRSGD_ERR_ARG, "mu must be in [0, 1)");
   if (!std::isfinite(lr) || !std::isfinite(scale) || !std::isfinite(weight_decay)) return op_fail(PRSGD_ERR_ARG, "lr, scale and weight_decay must be finite");
   if (lr * weight_decay == 1.f) return op_fail(PRSGD_ERR_ARG, "lr * weight_decay must not be 1");
-  if (batch == 0 || rows == 0 || cols == 0) return PRSGD_OK;
+  if (batch == 0 || rows == 0 || cols == 0) return op_clear_status(d_work, work_bytes, cuda_stream);
   rc = check_matrices("W", d_W, w_type, w_row_stride, w_batch_stride, batch, rows, cols, true);
   if (rc == PRSGD_OK) rc = check_matrices("V", d_V, PRSGD_TYPE_FP32, v_row_stride, v_batch_stride, batch, rows, cols, true);
   if (rc == PRSGD_OK) rc = check_matrices("G", d_G, g_type, g_row_stride, g_batch_stride, batch, rows, cols, false);

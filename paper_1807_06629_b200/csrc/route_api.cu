@@ -83,7 +83,7 @@ int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t 
                 void* d_work, size_t work_bytes, void* cuda_stream) {
   int rc = check_route(d_logits, type, row_stride, group_stride, groups, tokens, experts, top_k);
   if (rc != PRSGD_OK) return rc;
-  if (groups == 0) return PRSGD_OK;
+  if (groups == 0) return op_clear_status(d_work, work_bytes, cuda_stream);
   if (!d_counts || !d_mean || !d_loss || (tokens > 0 && (!d_experts || !d_weights))) return op_fail(PRSGD_ERR_ARG, "an output is NULL");
   size_t need = 0;
   prsgd_route_workspace_bytes(groups, tokens, experts, &need);
@@ -105,6 +105,7 @@ int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t 
     a.clustered = 1;
     a.blocks = (int)cluster;
   }
+  a.status = static_cast<DeviceStatus*>(d_work);
   unsigned char* w = static_cast<unsigned char*>(d_work) + 256;
   a.part_p = reinterpret_cast<float*>(w);
   a.part_c = reinterpret_cast<int32_t*>(a.part_p + (size_t)groups * a.blocks * experts);
