@@ -288,8 +288,9 @@ def prsgd_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, precis
 
 
 def orthogonalize_workspace(G: torch.Tensor, precision: Optional[int] = None, stream=None) -> torch.Tensor:
-    """Workspace of prsgd_orthogonalize for matrices like G (results of G's type unless `precision` says otherwise)."""
-    p = _precision_for_result(G) if precision is None else precision
+    """Workspace of prsgd_orthogonalize for matrices like G: for results of any type (the larger one, of 32-bit precision), or for
+    calls of that `precision` alone."""
+    p = PRECISION_FP32 if precision is None else precision
     return _empty(prsgd_orthogonalize_workspace_bytes(*_size3(G), p), torch.uint8, G.device, stream)
 
 

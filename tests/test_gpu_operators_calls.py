@@ -1,0 +1,35 @@
+"""Calls of the operators that their documentation allows: workspaces, types and layouts of outputs, masks."""
+import pytest
+import torch
+
+import operator_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_1807_06629_b200 import _build
+    _build.build_library()
+    from paper_1807_06629_b200 import binding
+    assert torch.cuda.is_available()
+    return binding
+
+
+def randn(seed, *shape, dtype=F32):
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda:0").to(dtype)
+
+
+@pytest.mark.parametrize("out_dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("shape", [(2, 40, 90), (2, 200, 2500), (1, 300, 270)])
+def test_orthogonalize_workspace_for_any_type_of_result(b, shape, dtype, out_dtype):
+    G = randn(1, *shape, dtype=dtype)
+    work = b.orthogonalize_workspace(G).fill_(0xFF)
+    got = b.prsgd_orthogonalize(G, out=torch.empty(shape, dtype=out_dtype, device="cuda:0"), workspace=work)
+    b.prsgd_work_status(work)
+    assert torch.equal(got, b.prsgd_orthogonalize(G, out=torch.empty(shape, dtype=out_dtype, device="cuda:0")))
