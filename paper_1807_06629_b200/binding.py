@@ -281,6 +281,13 @@ def _same_place(name: str, t: torch.Tensor, index: int) -> None:
         raise ValueError(f"{name} is on {t.device}, the call's other tensors on cuda:{index}")
 
 
+def _scratch(t: torch.Tensor, index: int):
+    """(pointer, bytes) of a workspace on device `index`: one piece of memory, whatever its element type."""
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def prsgd_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, precision: int) -> int:
     n = C.c_size_t()
     _check(lib.prsgd_orthogonalize_workspace_bytes(batch, rows, cols, precision, C.byref(n)))
@@ -316,9 +323,9 @@ def prsgd_orthogonalize(G: torch.Tensor, out: Optional[torch.Tensor] = None, *, 
         workspace = orthogonalize_workspace(G, p, stream)
     index = G.get_device()
     _same_place("out", out, index)
-    _same_place("workspace", workspace, index)
+    work, size = _scratch(workspace, index)
     _run_on(index, stream, lib.prsgd_orthogonalize, *_matrices(G, "G"), *_matrices(out, "out"), *_size3(G), steps,
-            _coefs(coefs), scale, eps, p, workspace.data_ptr(), workspace.numel())
+            _coefs(coefs), scale, eps, p, work, size)
     return out
 
 
@@ -337,10 +344,10 @@ def prsgd_muon_step(W: torch.Tensor, V: torch.Tensor, G: torch.Tensor, lr: float
     index = W.get_device()
     _same_place("V", V, index)
     _same_place("G", G, index)
-    _same_place("workspace", workspace, index)
+    work, size = _scratch(workspace, index)
     v, _, vr, vb = _matrices(V, "V")
     _run_on(index, stream, lib.prsgd_muon_step, *_matrices(W, "W"), v, vr, vb, *_matrices(G, "G"), *_size3(W), lr, mu,
-            1 if nesterov else 0, weight_decay, steps, _coefs(coefs), scale, eps, p, workspace.data_ptr(), workspace.numel())
+            1 if nesterov else 0, weight_decay, steps, _coefs(coefs), scale, eps, p, work, size)
 
 
 def prsgd_work_status(workspace: torch.Tensor, stream=None) -> None:
@@ -385,13 +392,13 @@ def prsgd_route(logits: torch.Tensor, k: int, coef: float, *, normalize: bool = 
     if workspace is None:
         workspace = route_workspace(logits, stream)
     at = logits.get_device()
-    _same_place("workspace", workspace, at)
+    work, size = _scratch(workspace, at)
     experts, weights, counts, mean, loss = out
     i32, f32, n, m = torch.int32, torch.float32, G * T * k, G * E
     _run_on(at, stream, lib.prsgd_route, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, at),
             G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", i32, n, at), _dense(weights, "weights", f32, n, at),
             _dense(counts, "counts", i32, m, at), _dense(mean, "mean", f32, m, at), _dense(loss, "loss", f32, G, at),
-            workspace.data_ptr(), workspace.numel())
+            work, size)
     return out
 
 

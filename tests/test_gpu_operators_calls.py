@@ -33,3 +33,13 @@ def test_orthogonalize_workspace_for_any_type_of_result(b, shape, dtype, out_dty
     got = b.prsgd_orthogonalize(G, out=torch.empty(shape, dtype=out_dtype, device="cuda:0"), workspace=work)
     b.prsgd_work_status(work)
     assert torch.equal(got, b.prsgd_orthogonalize(G, out=torch.empty(shape, dtype=out_dtype, device="cuda:0")))
+
+
+def test_a_workspace_is_one_piece_of_memory(b):
+    x = randn(2, 2, 40, 16)
+    n = b.prsgd_route_workspace_bytes(*x.shape)
+    for work in (torch.zeros(1, dtype=torch.uint8, device="cuda:0").expand(n), torch.zeros(2 * n, dtype=torch.uint8, device="cuda:0")[::2], torch.zeros(n, dtype=torch.uint8)):
+        with pytest.raises(ValueError, match="workspace must be"):
+            b.prsgd_route(x, 2, 0.1, workspace=work)
+    words = torch.zeros((n + 3) // 4, dtype=F32, device="cuda:0")       # of any type
+    assert all(torch.equal(p, q) for p, q in zip(b.prsgd_route(x, 2, 0.1, workspace=words), b.prsgd_route(x, 2, 0.1)))

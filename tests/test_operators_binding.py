@@ -21,3 +21,21 @@ def test_a_workspace_serves_results_of_any_type(b, shape, dtype):
         assert work.numel() >= b.prsgd_orthogonalize_workspace_bytes(*b._size3(G), b._precision_for_result(torch.empty(1, dtype=out)))
     for p in (b.PRECISION_FP32, b.PRECISION_BF16):
         assert b.orthogonalize_workspace(G, p).numel() == b.prsgd_orthogonalize_workspace_bytes(*b._size3(G), p)
+
+
+def not_one_piece():
+    return [torch.zeros(1, dtype=torch.uint8).expand(1 << 24), torch.zeros(1 << 12, 1 << 12, dtype=torch.uint8).t()[::2]]
+
+
+def test_a_workspace_is_one_piece_of_memory(b):
+    """A view whose elements share memory, or lie apart, is larger by its count than what it may be written through."""
+    G = torch.zeros(2, 10, 100)
+    for work in not_one_piece():
+        with pytest.raises(ValueError, match="workspace must be"):
+            b.prsgd_orthogonalize(G, out=G, workspace=work)
+        with pytest.raises(ValueError, match="workspace must be"):
+            b.prsgd_muon_step(G, G.clone(), G.clone(), 0.1, workspace=work)
+        with pytest.raises(ValueError, match="workspace must be"):
+            b._scratch(work, -1)
+    words = torch.zeros(100, dtype=torch.float32)
+    assert b._scratch(words, -1) == (words.data_ptr(), 400)
