@@ -381,10 +381,15 @@ def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, index: int):
     return t.data_ptr()
 
 
+def _mask(live: Optional[torch.Tensor], numel: int, index: int):
+    """Pointer of the live tokens' mask: bytes or truth values, 0 = padding."""
+    return _dense(live, "live", torch.bool if live is not None and live.dtype is torch.bool else torch.uint8, numel, index)
+
+
 def prsgd_route(logits: torch.Tensor, k: int, coef: float, *, normalize: bool = False, live: Optional[torch.Tensor] = None,
                 out=None, workspace: Optional[torch.Tensor] = None, stream=None):
     """Top-k router with its balance loss over logits [G, T, E] (or [T, E]); returns (experts, weights, counts, mean,
-    loss), see prsgd.h.  `out`: a tuple as route_outputs makes it."""
+    loss), see prsgd.h.  `live`: uint8 or bool [G, T], 0 = padding; `out`: a tuple as route_outputs makes it."""
     ptr, ty, row, group = _matrices(logits, "logits")
     G, T, E = _size3(logits)
     if out is None:
@@ -395,7 +400,7 @@ def prsgd_route(logits: torch.Tensor, k: int, coef: float, *, normalize: bool = 
     work, size = _scratch(workspace, at)
     experts, weights, counts, mean, loss = out
     i32, f32, n, m = torch.int32, torch.float32, G * T * k, G * E
-    _run_on(at, stream, lib.prsgd_route, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, at),
+    _run_on(at, stream, lib.prsgd_route, ptr, ty, row, group, _mask(live, G * T, at),
             G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", i32, n, at), _dense(weights, "weights", f32, n, at),
             _dense(counts, "counts", i32, m, at), _dense(mean, "mean", f32, m, at), _dense(loss, "loss", f32, G, at),
             work, size)
@@ -417,7 +422,7 @@ def prsgd_route_grad(logits: torch.Tensor, experts: torch.Tensor, counts: torch.
     _same_place("out", out, at)
     optr, _, orow, ogroup = _matrices(out, "out")
     i32, f32, n = torch.int32, torch.float32, G * T * k
-    _run_on(at, stream, lib.prsgd_route_grad, ptr, ty, row, group, _dense(live, "live", torch.uint8, G * T, at),
+    _run_on(at, stream, lib.prsgd_route_grad, ptr, ty, row, group, _mask(live, G * T, at),
             G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", i32, n, at), _dense(counts, "counts", i32, G * E, at),
             _dense(dweights, "dweights", f32, n, at), _dense(dloss, "dloss", f32, G, at), optr, orow, ogroup)
     return out

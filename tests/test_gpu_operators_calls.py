@@ -43,3 +43,11 @@ def test_a_workspace_is_one_piece_of_memory(b):
             b.prsgd_route(x, 2, 0.1, workspace=work)
     words = torch.zeros((n + 3) // 4, dtype=F32, device="cuda:0")       # of any type
     assert all(torch.equal(p, q) for p, q in zip(b.prsgd_route(x, 2, 0.1, workspace=words), b.prsgd_route(x, 2, 0.1)))
+
+
+def test_a_mask_of_truth_values_is_one_of_bytes(b):
+    x, live = randn(3, 3, 50, 24), randn(4, 3, 50) > 0
+    got, want = b.prsgd_route(x, 3, 0.1, live=live), b.prsgd_route(x, 3, 0.1, live=live.to(torch.uint8))
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and (got[0][~live] == -1).all()
+    kw = dict(dweights=randn(5, 3, 50, 3), dloss=randn(6, 3))
+    assert torch.equal(b.prsgd_route_grad(x, got[0], got[2], 0.1, live=live, **kw), b.prsgd_route_grad(x, got[0], got[2], 0.1, live=live.to(torch.uint8), **kw))

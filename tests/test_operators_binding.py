@@ -39,3 +39,13 @@ def test_a_workspace_is_one_piece_of_memory(b):
             b._scratch(work, -1)
     words = torch.zeros(100, dtype=torch.float32)
     assert b._scratch(words, -1) == (words.data_ptr(), 400)
+
+
+def test_a_mask_is_bytes_or_truth_values(b):
+    for dtype in (torch.uint8, torch.bool):
+        live = torch.zeros(3, 4, dtype=dtype)
+        assert b._mask(live, 12, -1) == live.data_ptr()
+    assert b._mask(None, 12, -1) is None
+    for bad in (torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, 5, dtype=torch.bool), torch.zeros(4, 3, dtype=torch.bool).t()):
+        with pytest.raises(ValueError, match="live"):
+            b._mask(bad, 12, -1)
