@@ -1,4 +1,5 @@
 // C entries of the top-k router (prsgd_route, prsgd_route_grad).  See include/prsgd.h for the contract.
+#include <initializer_list>
 #include "kernels_route.cuh"
 
 using namespace prsgd;
@@ -23,6 +24,13 @@ int check_route(const void* logits, int type, int64_t row_stride, int64_t group_
   if (G > 0 && T > 0 && logits == nullptr) return op_fail(PRSGD_ERR_ARG, "logits is NULL");
   if (row_stride < E || group_stride < 0) return op_fail(PRSGD_ERR_ARG, "need row_stride >= experts, group_stride >= 0");
   if (((uintptr_t)logits) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, "logits is not aligned to its element type");
+  return PRSGD_OK;
+}
+
+// The arrays of 32-bit words are read and written as such.
+int check_words(std::initializer_list<const void*> arrays) {
+  for (const void* p : arrays)
+    if (((uintptr_t)p) % 4) return op_fail(PRSGD_ERR_ALIGN, "experts, weights, counts, mean and loss, and the gradients of weights and loss, must be 4-byte aligned");
   return PRSGD_OK;
 }
 
@@ -85,6 +93,8 @@ int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t 
   if (rc != PRSGD_OK) return rc;
   if (groups == 0) return op_clear_status(d_work, work_bytes, cuda_stream);
   if (!d_counts || !d_mean || !d_loss || (tokens > 0 && (!d_experts || !d_weights))) return op_fail(PRSGD_ERR_ARG, "an output is NULL");
+  rc = check_words({d_experts, d_weights, d_counts, d_mean, d_loss});
+  if (rc != PRSGD_OK) return rc;
   size_t need = 0;
   prsgd_route_workspace_bytes(groups, tokens, experts, &need);
   if (!d_work || work_bytes < need) return op_fail(PRSGD_ERR_SIZE, "workspace is NULL or smaller than prsgd_route_workspace_bytes");
@@ -147,6 +157,8 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
   if (rc != PRSGD_OK) return rc;
   if (groups == 0 || tokens == 0) return PRSGD_OK;
   if (!d_counts || !d_dlogits || (d_dweights && !d_experts)) return op_fail(PRSGD_ERR_ARG, "counts, dlogits or experts is NULL");
+  rc = check_words({d_experts, d_counts, d_dweights, d_dloss});
+  if (rc != PRSGD_OK) return rc;
   if (d_row_stride < experts || (groups > 1 && d_group_stride < (tokens - 1) * d_row_stride + experts))
     return op_fail(PRSGD_ERR_ARG, "the rows of dlogits overlap");
   if (((uintptr_t)d_dlogits) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, "dlogits is not aligned to its element type");
