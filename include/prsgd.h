@@ -501,7 +501,7 @@ int prsgd_mean_rows_noalloc(const float* d_P, int64_t N, int64_t m, int64_t row_
  * workspace serves any number of calls on one stream, and calls that may run at the same time (other streams, two
  * graphs replayed side by side) need one each.  Array elements are one of the types below; matrices are row-major with
  * a row stride (elements, >= cols) and a stride between the matrices of a batch.  Inputs may be broadcast over the batch
- * (batch stride 0); outputs may not overlap.  A batch, side, group or token count of 0 is a call that does nothing
+ * (batch stride 0); the rows of an output may not overlap, but those of its matrices may lie in turn ([rows][batch][cols]).  A batch, side, group or token count of 0 is a call that does nothing
  * (the router then still writes zero counts and loss, and any call clears the status of the workspace it is given). */
 #define PRSGD_TYPE_FP32 0
 #define PRSGD_TYPE_BF16 1

@@ -12,6 +12,13 @@ namespace prsgd {
 // Records the text prsgd_last_error(NULL) returns and hands the code back (defined in prsgd_api.cu).
 int op_fail(int code, const std::string& msg);
 
+// Whether the rows (`width` elements, `row` >= width apart) of `batch` matrices `stride` apart are all different memory: matrix behind
+// matrix, or a row of each in turn ([rows][batch][width] seen as [batch][rows][width]).
+inline bool rows_apart(int64_t batch, int64_t stride, int64_t rows, int64_t row, int64_t width) {
+  if (batch <= 1 || rows < 1 || width < 1) return true;
+  return (__int128)stride >= (__int128)(rows - 1) * row + width || (stride >= width && (rows <= 1 || (__int128)row >= (__int128)(batch - 1) * stride + width));
+}
+
 // The status words at the head of the workspace of a call that has nothing to compute (a call without a workspace has none).
 inline int op_clear_status(void* d_work, size_t bytes, void* stream) {
   if (d_work == nullptr || bytes < sizeof(DeviceStatus)) return PRSGD_OK;

@@ -229,7 +229,7 @@ int check_matrices(const char* name, const void* p, int type, int64_t row, int64
   if (!type_known(type)) return op_fail(PRSGD_ERR_ARG, std::string("unknown element type of ") + name);
   if (((uintptr_t)p) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, std::string(name) + " is not aligned to its element type");
   if (row < cols) return op_fail(PRSGD_ERR_ARG, std::string("row stride of ") + name + " is below its columns");
-  if (batch_stride < 0 || (written && batch > 1 && batch_stride < (int64_t)(rows - 1) * row + cols))
+  if (batch_stride < 0 || (written && !rows_apart(batch, batch_stride, rows, row, cols)))
     return op_fail(PRSGD_ERR_ARG, std::string("the matrices of ") + name + " overlap");
   return PRSGD_OK;
 }

@@ -159,7 +159,7 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
   if (!d_counts || !d_dlogits || (d_dweights && !d_experts)) return op_fail(PRSGD_ERR_ARG, "counts, dlogits or experts is NULL");
   rc = check_words({d_experts, d_counts, d_dweights, d_dloss});
   if (rc != PRSGD_OK) return rc;
-  if (d_row_stride < experts || (groups > 1 && d_group_stride < (tokens - 1) * d_row_stride + experts))
+  if (d_row_stride < experts || d_group_stride < 0 || !rows_apart(groups, d_group_stride, tokens, d_row_stride, experts))
     return op_fail(PRSGD_ERR_ARG, "the rows of dlogits overlap");
   if (((uintptr_t)d_dlogits) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, "dlogits is not aligned to its element type");
   RouteArgs a{};

@@ -33,3 +33,19 @@ def test_arrays_of_words_are_aligned_to_them(lib, off):
     for name in ("e", "c", "dw", "dl"):
         assert grad(lib, **{name: 256 + off}) == ALIGN, name
     assert lib.prsgd_last_error(None)
+
+
+def orthogonalize(lib, **kw):
+    a = dict(G=4096, gt=0, gr=64, gb=4096, out=8192, ot=0, orow=64, ob=4096, batch=3, rows=64, cols=64, steps=5, coefs=None,
+             scale=1.0, eps=1e-7, precision=1, work=65536, bytes=1 << 30)
+    a.update(kw)
+    return lib.prsgd_orthogonalize(*a.values(), None)
+
+
+def test_rows_of_an_output_that_overlap(lib):
+    for kw in (dict(ob=0), dict(ob=63), dict(ob=64), dict(ob=64, orow=191), dict(ob=4095, orow=64), dict(ob=63, orow=4096), dict(ob=100, orow=263)):
+        assert orthogonalize(lib, **kw) == ARG, kw
+    for kw in (dict(dgs=64), dict(dgs=64, drs=127), dict(dgs=63, drs=6400), dict(dgs=6399), dict(dgs=0), dict(G=3, dgs=100, drs=263)):
+        assert grad(lib, **kw) == ARG, kw
+    big = (1 << 62) + (1 << 61)                        # (a row stride whose product with the rows passes 64 bits)
+    assert orthogonalize(lib, ob=63, orow=big) == ARG
