@@ -515,7 +515,7 @@ int prsgd_mean_rows_noalloc(const float* d_P, int64_t N, int64_t m, int64_t row_
  * precision: PRSGD_PRECISION_FP32 computes to about fp32 accuracy (products of fp16 pairs, three per product),
  * PRSGD_PRECISION_BF16 to about 2e-3 of the result's norm (single fp16 operands: half a rounding of bfloat16, but five of
  * float16); both sum in fp32, and the norm in 64 bits.  A zero matrix gives zeros (eps > 0); one that holds a NaN or an infinity gives NaN and leaves the others
- * alone.  out may be G itself (same type and strides).  G and out: aligned to their element type; multiples of
+ * alone.  out may be G itself (same type and strides, else the call is refused); it may share no memory with G in another way.  G and out: aligned to their element type; multiples of
  * 16 bytes in address and strides are fastest. */
 #define PRSGD_ORTHO_MAX_SIDE 65536
 #define PRSGD_ORTHO_MAX_STEPS 16
@@ -528,7 +528,7 @@ int prsgd_orthogonalize(const void* d_G, int32_t g_type, int64_t g_row_stride, i
 /* Muon step of a batch of weight matrices, in place:
  *   V <- mu V + G;  U = V, or G + mu V when nesterov is set;
  *   W <- (1 - lr weight_decay) W - lr scale NS(U),  NS as in prsgd_orthogonalize (same workspace size).
- * V is fp32; W and G are of any element type.  mu in [0, 1); lr * weight_decay must not be 1.  sqrt(max(1, rows / cols)) and 0.2 sqrt(max(rows, cols)) are the usual
+ * V is fp32; W and G are of any element type; no two of them may share memory.  mu in [0, 1); lr * weight_decay must not be 1.  sqrt(max(1, rows / cols)) and 0.2 sqrt(max(rows, cols)) are the usual
  * choices of scale. */
 int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_batch_stride,
                     float* d_V, int64_t v_row_stride, int64_t v_batch_stride,
@@ -563,7 +563,7 @@ int prsgd_route(const void* d_logits, int32_t type, int64_t row_stride, int64_t 
  * counts held fixed: with h_te = dloss coef E counts_e / (top_k T) / T + [e chosen by t] d/dp of the weights' part,
  *   dlogit_te = p_te (h_te - sum_j p_tj h_tj).
  * d_experts, d_counts: as prsgd_route wrote them, a token's experts distinct (T is taken from the counts).  d_dweights [groups][tokens][top_k] or
- * NULL, d_dloss [groups] or NULL (zero).  dlogits has the logits' type and may be the logits themselves (same strides);
+ * NULL, d_dloss [groups] or NULL (zero).  dlogits has the logits' type and may be the logits themselves (same strides, else the call is refused);
  * rows of padding tokens are written as zeros. */
 int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int64_t group_stride, const uint8_t* d_live,
                      int64_t groups, int64_t tokens, int32_t experts, int32_t top_k, int32_t normalize, float coef,

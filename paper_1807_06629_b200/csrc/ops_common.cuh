@@ -19,6 +19,11 @@ inline bool rows_apart(int64_t batch, int64_t stride, int64_t rows, int64_t row,
   return (__int128)stride >= (__int128)(rows - 1) * row + width || (stride >= width && (rows <= 1 || (__int128)row >= (__int128)(batch - 1) * stride + width));
 }
 
+// An output that starts where an input does: only as the same array, element for element.
+inline bool same_layout(int64_t batch, int64_t stride_a, int64_t stride_b, int64_t rows, int64_t row_a, int64_t row_b) {
+  return (batch <= 1 || stride_a == stride_b) && (rows <= 1 || row_a == row_b);
+}
+
 // The status words at the head of the workspace of a call that has nothing to compute (a call without a workspace has none).
 inline int op_clear_status(void* d_work, size_t bytes, void* stream) {
   if (d_work == nullptr || bytes < sizeof(DeviceStatus)) return PRSGD_OK;

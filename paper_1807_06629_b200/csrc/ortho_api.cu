@@ -283,6 +283,8 @@ int prsgd_orthogonalize(const void* d_G, int32_t g_type, int64_t g_row_stride, i
   if (batch == 0 || rows == 0 || cols == 0) return op_clear_status(d_work, work_bytes, cuda_stream);
   rc = check_matrices("G", d_G, g_type, g_row_stride, g_batch_stride, batch, rows, cols, false);
   if (rc == PRSGD_OK) rc = check_matrices("out", d_out, out_type, out_row_stride, out_batch_stride, batch, rows, cols, true);
+  if (rc == PRSGD_OK && d_out == d_G && (g_type != out_type || !same_layout(batch, g_batch_stride, out_batch_stride, rows, g_row_stride, out_row_stride)))
+    return op_fail(PRSGD_ERR_ARG, "out is G's memory with another type or other strides");
   p.shape = {batch, rows, cols}; p.precision = precision; p.g_type = g_type;
   if (rc == PRSGD_OK) rc = check_work(p.shape, precision, d_work, work_bytes);
   if (rc != PRSGD_OK) return rc;
@@ -309,6 +311,7 @@ int prsgd_muon_step(void* d_W, int32_t w_type, int64_t w_row_stride, int64_t w_b
   rc = check_matrices("W", d_W, w_type, w_row_stride, w_batch_stride, batch, rows, cols, true);
   if (rc == PRSGD_OK) rc = check_matrices("V", d_V, PRSGD_TYPE_FP32, v_row_stride, v_batch_stride, batch, rows, cols, true);
   if (rc == PRSGD_OK) rc = check_matrices("G", d_G, g_type, g_row_stride, g_batch_stride, batch, rows, cols, false);
+  if (rc == PRSGD_OK && (d_W == static_cast<void*>(d_V) || d_W == d_G || d_V == d_G)) return op_fail(PRSGD_ERR_ARG, "two of W, V and G are the same memory");
   p.shape = {batch, rows, cols}; p.precision = precision; p.g_type = g_type;
   if (rc == PRSGD_OK) rc = check_work(p.shape, precision, d_work, work_bytes);
   if (rc != PRSGD_OK) return rc;

@@ -161,6 +161,8 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
   if (rc != PRSGD_OK) return rc;
   if (d_row_stride < experts || d_group_stride < 0 || !rows_apart(groups, d_group_stride, tokens, d_row_stride, experts))
     return op_fail(PRSGD_ERR_ARG, "the rows of dlogits overlap");
+  if (d_dlogits == d_logits && !same_layout(groups, group_stride, d_group_stride, tokens, row_stride, d_row_stride))
+    return op_fail(PRSGD_ERR_ARG, "dlogits are the logits' memory with other strides");
   if (((uintptr_t)d_dlogits) % type_bytes(type)) return op_fail(PRSGD_ERR_ALIGN, "dlogits is not aligned to its element type");
   RouteArgs a{};
   a.logits = d_logits; a.row_stride = row_stride; a.group_stride = group_stride; a.live = d_live;

@@ -49,3 +49,21 @@ def test_rows_of_an_output_that_overlap(lib):
         assert grad(lib, **kw) == ARG, kw
     big = (1 << 62) + (1 << 61)                        # (a row stride whose product with the rows passes 64 bits)
     assert orthogonalize(lib, ob=63, orow=big) == ARG
+
+
+def test_in_place_calls_keep_type_and_strides(lib):
+    """Written while rows that lie elsewhere are still to be read, the result would depend on the order of the blocks."""
+    for kw in (dict(ot=1, gt=2), dict(orow=65, ob=65 * 64), dict(ob=4097), dict(gb=0), dict(gr=65)):
+        assert orthogonalize(lib, **{**dict(G=8192, out=8192), **kw}) == ARG, kw
+    for kw in (dict(drs=65, dgs=6500), dict(dgs=6401), dict(gs=0), dict(rs=65)):
+        assert grad(lib, **{**dict(x=8192, d=8192), **kw}) == ARG, kw
+
+
+def test_muon_arrays_are_three(lib):
+    def call(**kw):
+        a = dict(W=4096, wt=0, wr=64, wb=4096, V=8192, vr=64, vb=4096, G=12288, gt=0, gr=64, gb=4096, batch=2, rows=64, cols=64,
+                 lr=0.1, mu=0.9, nesterov=1, wd=0.0, steps=5, coefs=None, scale=1.0, eps=1e-7, precision=0, work=65536, bytes=1 << 30)
+        a.update(kw)
+        return lib.prsgd_muon_step(*a.values(), None)
+    for kw in (dict(V=4096), dict(G=4096), dict(G=8192)):
+        assert call(**kw) == ARG, kw
