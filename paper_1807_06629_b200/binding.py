@@ -307,7 +307,12 @@ def muon_workspace(W: torch.Tensor, precision: Optional[int] = None, stream=None
 
 
 def _coefs(coefs):
-    return None if coefs is None or tuple(coefs) == MUON_COEFS else (C.c_float * 3)(*coefs)
+    """The three coefficients as the C entry takes them (None: the default ones)."""
+    if coefs is None or tuple(coefs) == MUON_COEFS:
+        return None
+    if len(coefs) != 3:
+        raise ValueError("coefs must be the three of a X + (b A + c A^2) X")
+    return (C.c_float * 3)(*coefs)
 
 
 def prsgd_orthogonalize(G: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps: int = 5, coefs=None,

@@ -49,3 +49,10 @@ def test_a_mask_is_bytes_or_truth_values(b):
     for bad in (torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, 5, dtype=torch.bool), torch.zeros(4, 3, dtype=torch.bool).t()):
         with pytest.raises(ValueError, match="live"):
             b._mask(bad, 12, -1)
+
+
+def test_coefficients_are_three(b):
+    assert b._coefs(None) is None and b._coefs(list(b.MUON_COEFS)) is None and list(b._coefs((1.5, -0.5, 0.0))) == [1.5, -0.5, 0.0]
+    for bad in ((), (1.5,), (1.5, -0.5), (1.5, -0.5, 0.0, 0.0)):
+        with pytest.raises(ValueError, match="coefs"):
+            b._coefs(bad)
