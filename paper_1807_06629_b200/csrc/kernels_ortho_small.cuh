@@ -3,7 +3,7 @@
 //
 // CTA r of the cluster keeps `w` columns (of the long side) of X as fp16 pairs.  Per step it forms its share of A = X X^T on
 // the tensor cores.  Up to a short side of 32 it sends its share to all (st.async, counted on the receiver's barrier), and every
-// CTA sums all of A, in rank order, and forms P = a I + b A + c A^2 in fp32 for itself (16 matrices of 10 x 1024: 37 -> 21.6 us,
+// CTA sums all of A, in rank order, and forms P = a I + b A + c A^2 in fp32 for itself (16 matrices of 10 x 1024: 37 -> 19.6 us,
 // against the form for longer sides); above, each CTA fetches and sums a part of A and hands it to all, and P is formed on the
 // tensor cores.  (Shares sent to the CTAs that sum them, a lane to a row: 8 x 64 x 1024 43 -> 55 us; what crosses between CTAs has to
 // go from neighbouring lanes to neighbouring places.)  All products but that of P in fp32 are hi hi + hi lo + lo hi whatever

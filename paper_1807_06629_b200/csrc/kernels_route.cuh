@@ -194,7 +194,8 @@ __device__ __forceinline__ void route_leave(const RouteArgs& a, int64_t g, float
   }
 }
 
-// For top_k above 8: one warp per token, a lane holds the logits lane, lane + 32, ..., and the largest is taken k times.
+// For top_k above 8: one warp per token, a lane holds the logits lane, lane + 32, ..., and the largest is taken k times
+// (16 x 16384 x 128 bf16: top 9 373 us, top 16 556, top 32 958; the kernels below: top 4 41, top 8 50).
 template <int TY, int PER>
 __global__ void __launch_bounds__(256, 2) route_kernel(const RouteArgs a) {
   using T = typename ElemOf<TY>::type;
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(256, 2) route_kernel(const RouteArgs a) {
 // experts for every token, so the sums over tokens stay in registers.  A lane's LS largest come from sorting networks:
 // batches of LS elements sorted and merged into a sorted list (70 min / max steps per 8 elements), then the lists of
 // the L lanes merged across lanes; taking the maximum k times over a warp, as above, took 380 instructions a token,
-// this 95.  Elements are ordered by (key, lowest index): of 16-bit logits one 32-bit word (16 to 19 bits of key, 10 of
+// this 95.  Elements are ordered by (key, lowest index): of 16-bit logits one 32-bit word (16 bits of order, 16 of
 // index), so that a step is one min and one max; of fp32 logits 64 bits.
 constexpr float kLog2E = 1.4426950408889634f;
 __device__ __forceinline__ float route_exp2(float x) {

@@ -121,7 +121,7 @@ static int ns_run_small(const NsPlan& p, const NsBuffers& buf, bool vec_in, int 
   a.sp = (a.s + 15) / 16 * 16;
   // As few CTAs as hold the matrix, or, while all clusters run at a time, more with fewer columns (down to 128).  (16 matrices
   // of 10 x 1024 in clusters of 8, of which 14 run at a time, took 1.6 times as long as in clusters of 6; 8 of 64 x 1024 with 128
-  // columns a CTA 41 us, with 192 46, with 256 49.)
+  // columns a CTA 40 us, with 192 46, with 256 49.)
   a.ctas = (a.l + ns_small_cols(a.s) - 1) / ns_small_cols(a.s);
   while (a.ctas < kNsSmallCtas && (a.l + a.ctas - 1) / a.ctas > 128 && p.shape.batch <= dev.clusters[a.ctas + 1]) ++a.ctas;
   a.w = ((a.l + a.ctas - 1) / a.ctas + 63) / 64 * 64;
