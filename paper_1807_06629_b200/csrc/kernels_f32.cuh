@@ -351,15 +351,15 @@ __global__ void __launch_bounds__(256) softmax_ce_balance_kernel(const SoftmaxAr
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) { s += __shfl_xor_sync(0xffffffffu, s, o); dot += __shfl_xor_sync(0xffffffffu, dot, o); }
     dot /= s;
-    const float lse = mx + logf(s);
+    const float inv = 1.f / s;                           // (not e^(z - mx - log s): beside a large mx the rounding of mx + log s is left in p)
     const int label = a.Y[(int64_t)n * a.P + (int64_t)blk * a.B + b];
     for (int c = lane; c < a.C; c += 32) {
-      const float p = expf(z[c] - lse);
+      const float p = expf(z[c] - mx) * inv;
       const float d = (p - (c == label ? 1.f : 0.f) + pull * p * ((float)s_count[c] * per - dot)) * invB;
       if (a.delta) a.delta[((int64_t)n * a.B + b) * a.ldz + c] = d;
       if (a.delta_bk) a.delta_bk[((int64_t)n * a.B + b) * a.ld_bf + c] = f32_to_bf16_rn(d);
     }
-    if (lane == 0) a.row_losses[(int64_t)n * a.B + b] = lse - z[label] + pull * dot;
+    if (lane == 0) a.row_losses[(int64_t)n * a.B + b] = (mx - z[label]) + logf(s) + pull * dot;
   }
 }
 

@@ -80,3 +80,29 @@ def test_a_nan_in_the_outputs_reaches_the_weights(w, balance):
     after = p.get_params_stacked()
     p.close()
     assert np.isnan(after[1, -C * (w.dims[-2] + 1):]).all() and np.isfinite(after[[0, 2]]).all()
+
+
+@pytest.mark.parametrize("k", [1, 3])
+@pytest.mark.parametrize("size", [1e3, 1e6, 1e10, -1e30])
+@pytest.mark.parametrize("w", [F32.with_(dims=(40, 10)), BF16.with_(dims=(64, 10))], ids=["f32", "bf16"])
+def test_large_logits_keep_their_softmax(w, size, k):
+    """Equal logits of any size: p = 1 / C, the first k classes are chosen (f = 1 / k), and with weights of 0 the step of W is
+    -gamma delta^T X.  p is off by the sum and the division (10 2^-24), delta by as much of (1 + coef C): below 1e-5 of its norm,
+    sums over B rows included; deltas are rounded to bf16 on that path (2^-8)."""
+    X, Y, x0 = make_inputs(w)
+    C, D, coef = w.dims[-1], w.dims[0], 0.5
+    x = np.zeros_like(x0)
+    x[-C:] = size
+    p = make_ctx(w, X, Y, x, I=0)
+    p.set_balance(coef, k)
+    p.local_steps(1)
+    after, losses, draws = p.get_params_stacked().astype(np.float64), p.get_losses(), p.get_draws()
+    p.close()
+    f = np.where(np.arange(C) < k, 1.0 / k, 0.0)
+    for i in range(w.N):
+        rows = slice(draws[i] * w.B, (draws[i] + 1) * w.B)
+        delta = (1 / C - np.eye(C)[Y[i, rows]] + coef * (f - 1 / C)) / w.B
+        want = -w.gamma * delta.T @ X[i, rows].astype(np.float64)
+        got = after[i, :C * D].reshape(C, D)
+        assert abs(losses[i] - (np.log(C) + coef)) <= 1e-5 * (np.log(C) + coef)
+        assert np.linalg.norm(got - want) <= (1e-5 if w.precision == 0 else 2.0 ** -8 + 1e-5) * np.linalg.norm(want)
