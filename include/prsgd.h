@@ -570,6 +570,75 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
                      const int32_t* d_experts, const int32_t* d_counts, const float* d_dweights, const float* d_dloss,
                      void* d_dlogits, int64_t d_row_stride, int64_t d_group_stride, void* cuda_stream);
 
+/* ---- The two ends of stacked workers' language models ----------------------------------------------------------------
+ * One table and one batch of tokens per group (worker).  Tokens are int32 [groups][tokens], dense; one outside [0, vocab) is
+ * padding.  Arrays of rows are [groups][rows][columns] with a row stride (elements, >= columns) and a group stride; an input that
+ * all groups share has group stride 0. */
+#define PRSGD_VOCAB_MAX (1 << 24)
+
+/* Lookup of token embeddings: out_t = scale * table[id_t], zeros for padding, rounded once to out's type. */
+int prsgd_embed(const void* d_table, int32_t type, int64_t row_stride, int64_t group_stride, const int32_t* d_ids,
+                int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, float scale,
+                void* d_out, int32_t out_type, int64_t out_row_stride, int64_t out_group_stride, void* cuda_stream);
+
+/* Its gradient with respect to the table: dtable_v = scale * sum of dout_t over the tokens with id_t = v, or (accumulate) that added
+ * to what dtable holds.  Tokens are sorted by id, sums are fp32 in an order that depends on the ids alone: the same call gives
+ * the same bits.  Without accumulate rows of ids that do not occur are written as zeros; with it they are neither read nor
+ * written.  The rows of dtable may not overlap (a table that all groups share has one gradient: call with groups = 1 and the
+ * groups' tokens behind one another), and dtable may share no memory with dout. */
+int prsgd_embed_grad_workspace_bytes(int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, size_t* bytes);
+int prsgd_embed_grad(const void* d_dout, int32_t type, int64_t row_stride, int64_t group_stride, const int32_t* d_ids,
+                     int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, float scale,
+                     void* d_dtable, int32_t dtable_type, int64_t dtable_row_stride, int64_t dtable_group_stride, int32_t accumulate,
+                     void* d_work, size_t work_bytes, void* cuda_stream);
+
+/* Dropout: out = keep * x / (1 - q) (+ residual), computed in fp32 and rounded once; keep is drawn with probability 1 - q,
+ * q = round(65536 p) / 65536, and never stored: prsgd_dropout_keep evaluates it for one element.  Column c of row r of group g takes the
+ * (c % 8)th 16 bits (lower half of a word first) of Philox4x32-10 (Salmon et al., 2011) with key = seed and counter
+ * (c / 8, r, first_group + g, step + *d_step), each modulo 2^32, and is kept when they are >= 65536 q.  So the draw depends on neither
+ * type, strides nor the number of groups of a call, and a group of a sharded job draws as it would in the whole one.  d_step:
+ * DEVICE pointer to a counter (a captured graph draws anew at each replay when the caller advances it), or NULL for 0.
+ * The gradient with respect to x is the same call with the gradient in x's place and no residual; that of the residual
+ * is the gradient itself.  A dropped element is 0 (+ residual) whatever x holds.  x, residual (or NULL) and out have one type;
+ * out may be x or the residual themselves (same strides, else the call is refused).  p in [0, 1 - 2^-17]. */
+int prsgd_dropout(const void* d_x, int32_t type, int64_t row_stride, int64_t group_stride,
+                  const void* d_residual, int64_t residual_row_stride, int64_t residual_group_stride,
+                  void* d_out, int64_t out_row_stride, int64_t out_group_stride,
+                  int64_t groups, int64_t rows, int64_t cols, double p, uint64_t seed, int64_t step, const int64_t* d_step,
+                  int64_t first_group, void* cuda_stream);
+/* 1 when that element is kept, 0 when it is dropped.  Pure host function; the device code evaluates the same function. */
+int prsgd_dropout_keep(uint64_t seed, int64_t group, int64_t row, int64_t col, int64_t step, double p);
+
+/* Softmax cross entropy of a class layer over a vocabulary, whose logits z_tv = H_t . W_v are formed in pieces and never kept:
+ *   loss_t = log sum_v e^z_tv - z_ty,  y the token's label;  stats_t = (max_v z_tv, log sum_v e^(z_tv - max)), whose sum is the
+ * logarithm of the softmax's denominator.  H: [groups][tokens][dim]; W: [groups][vocab][dim], row-major like the class layer's
+ * weights; both of one type.  A token whose label is padding has loss 0 and stats 0 whatever its row of H holds.  loss: [groups][tokens],
+ * stats: [groups][tokens][2], fp32, dense.  Products of 16-bit types are summed in fp32; fp32 operands are taken as pairs of
+ * fp16 values (22 bits, scaled by powers of two per group), three products each.
+ * The workspace depends on whether W's rows begin on 16-byte boundaries (address and both strides multiples of 16 bytes: w_aligned
+ * 1; else, or for fp32, it holds a copy of W). */
+int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes);
+int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stride,
+                     const void* d_W, int64_t w_row_stride, int64_t w_group_stride, int32_t type, const int32_t* d_labels,
+                     int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, float* d_loss, float* d_stats,
+                     void* d_work, size_t work_bytes, void* cuda_stream);
+
+/* Gradient of sum dloss_t loss_t + sum dlse_t lse_t (lse the sum of the stats) with respect to H and W:
+ *   G_tv = (dloss_t + dlse_t) e^(z_tv - lse_t) - dloss_t [v = y_t],   dH = G W,   dW = G^T H (or, accumulate, added to what dW holds).
+ * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is held in the type of the operands (fp32:
+ * as pairs), a piece of the vocabulary at a time.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
+ * whose label is padding take no part: their rows of dH are zeros, whatever their H, stats, dloss and dlse hold.  The rows of dH and of dW may
+ * not overlap (W shared by all groups has one gradient: call with groups = 1 and the groups' tokens behind one another);
+ * neither may share memory with another array of the call. */
+int prsgd_vocab_loss_grad_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes);
+int prsgd_vocab_loss_grad(const void* d_H, int64_t h_row_stride, int64_t h_group_stride,
+                          const void* d_W, int64_t w_row_stride, int64_t w_group_stride, int32_t type, const int32_t* d_labels,
+                          int64_t groups, int64_t tokens, int64_t vocab, int32_t dim,
+                          const float* d_stats, const float* d_dloss, const float* d_dlse,
+                          void* d_dH, int64_t dh_row_stride, int64_t dh_group_stride,
+                          void* d_dW, int32_t dw_type, int64_t dw_row_stride, int64_t dw_group_stride, int32_t accumulate,
+                          void* d_work, size_t work_bytes, void* cuda_stream);
+
 /* The minibatch draw zeta_i^t as an integer: the (i+1)-th output of a
  * SplitMix64 stream keyed by the t-th output of the SplitMix64 stream seeded
  * with `seed`, modulo n_blocks.  Pure host function; the device code evaluates

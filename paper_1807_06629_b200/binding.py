@@ -59,6 +59,8 @@ EXPORTS = [
     "prsgd_orthogonalize_workspace_bytes", "prsgd_orthogonalize", "prsgd_muon_step", "prsgd_work_status",
     "prsgd_route_workspace_bytes", "prsgd_route", "prsgd_route_grad",
     "prsgd_muon_workspace_bytes", "prsgd_enable_muon", "prsgd_set_balance",
+    "prsgd_embed", "prsgd_embed_grad_workspace_bytes", "prsgd_embed_grad", "prsgd_dropout", "prsgd_dropout_keep",
+    "prsgd_vocab_loss_workspace_bytes", "prsgd_vocab_loss", "prsgd_vocab_loss_grad_workspace_bytes", "prsgd_vocab_loss_grad",
 ]
 NOALLOC_MAX_M = 1 << 20
 
@@ -134,6 +136,16 @@ def _load() -> C.CDLL:
         "prsgd_route_workspace_bytes": (C.c_int, [i64, i64, i32, szp]),
         "prsgd_route": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, szt, vp]),
         "prsgd_route_grad": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, i64, i64, vp]),
+        "prsgd_embed": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i64, i32, f32, vp, i32, i64, i64, vp]),
+        "prsgd_embed_grad_workspace_bytes": (C.c_int, [i64, i64, i64, i32, szp]),
+        "prsgd_embed_grad": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, i64, i32, f32, vp, i32, i64, i64, i32, vp, szt, vp]),
+        "prsgd_dropout": (C.c_int, [vp, i32, i64, i64, vp, i64, i64, vp, i64, i64, i64, i64, i64, C.c_double, u64, i64, vp, i64, vp]),
+        "prsgd_dropout_keep": (C.c_int, [u64, i64, i64, i64, i64, C.c_double]),
+        "prsgd_vocab_loss_workspace_bytes": (C.c_int, [i32, i64, i64, i64, i32, i32, szp]),
+        "prsgd_vocab_loss": (C.c_int, [vp, i64, i64, vp, i64, i64, i32, vp, i64, i64, i64, i32, vp, vp, vp, szt, vp]),
+        "prsgd_vocab_loss_grad_workspace_bytes": (C.c_int, [i32, i64, i64, i64, i32, i32, szp]),
+        "prsgd_vocab_loss_grad": (C.c_int, [vp, i64, i64, vp, i64, i64, i32, vp, i64, i64, i64, i32, vp, vp, vp, vp, i64, i64,
+                                            vp, i32, i64, i64, i32, vp, szt, vp]),
         "prsgd_last_error": (C.c_char_p, [vp]),
         "prsgd_average_rows": (C.c_int, [vp, i64, i64, i64, vp]),
         "prsgd_draw_block": (u64, [u64, i32, i64, u64]),
@@ -431,6 +443,186 @@ def prsgd_route_grad(logits: torch.Tensor, experts: torch.Tensor, counts: torch.
             G, T, E, k, 1 if normalize else 0, coef, _dense(experts, "experts", i32, n, at), _dense(counts, "counts", i32, G * E, at),
             _dense(dweights, "dweights", f32, n, at), _dense(dloss, "dloss", f32, G, at), optr, orow, ogroup)
     return out
+
+
+# ---- the two ends of stacked workers' language models -------------------------------------------------------
+def prsgd_embed(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                stream=None) -> torch.Tensor:
+    """Rows of table ([G, V, D], or [V, D] with ids [T]) for int32 ids [G, T], times scale; zeros where an id is outside [0, V).  A
+    table that all groups share: table.expand(G, V, D).  See prsgd.h."""
+    ptr, ty, row, group = _matrices(table, "table")
+    (G, V, D), at = _size3(table), table.get_device()
+    if ids.dim() != table.dim() - 1 or (ids.dim() == 2 and ids.shape[0] != G):
+        raise ValueError("ids must be [groups, tokens] beside a table [groups, vocab, dim], or [tokens] beside [vocab, dim]")
+    T = ids.shape[-1]
+    shape = (*ids.shape, D)
+    if out is None:
+        out = _empty(shape, table.dtype, table.device, stream)
+    elif tuple(out.shape) != shape:
+        raise ValueError("out must be [groups, tokens, dim]")
+    _same_place("out", out, at)
+    _run_on(at, stream, lib.prsgd_embed, ptr, ty, row, group, _dense(ids, "ids", torch.int32, G * T, at), G, T, V, D, scale, *_matrices(out, "out"))
+    return out
+
+
+def prsgd_embed_grad_workspace_bytes(groups: int, tokens: int, vocab: int, dim: int) -> int:
+    n = C.c_size_t()
+    _check(lib.prsgd_embed_grad_workspace_bytes(groups, tokens, vocab, dim, C.byref(n)))
+    return n.value
+
+
+def embed_grad_workspace(dout: torch.Tensor, dtable: torch.Tensor, stream=None) -> torch.Tensor:
+    (G, T, D), V = _size3(dout), _size3(dtable)[1]
+    return _empty(prsgd_embed_grad_workspace_bytes(G, T, V, D), torch.uint8, dout.device, stream)
+
+
+def prsgd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, *, scale: float = 1.0, accumulate: bool = False,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of prsgd_embed with respect to its table, written into (accumulate: added to) dtable [G, V, D]; see prsgd.h."""
+    ptr, ty, row, group = _matrices(dout, "dout")
+    (G, T, D), at = _size3(dout), dout.get_device()
+    if dtable.dim() != dout.dim() or _size3(dtable)[0] != G or dtable.shape[-1] != D:
+        raise ValueError("dtable must be [groups, vocab, dim] with dout's groups and dim")
+    _same_place("dtable", dtable, at)
+    if workspace is None:
+        workspace = embed_grad_workspace(dout, dtable, stream)
+    work, size = _scratch(workspace, at)
+    _run_on(at, stream, lib.prsgd_embed_grad, ptr, ty, row, group, _dense(ids, "ids", torch.int32, G * T, at), G, T, dtable.shape[-2], D,
+            scale, *_matrices(dtable, "dtable"), 1 if accumulate else 0, work, size)
+    return dtable
+
+
+def prsgd_dropout_keep(seed: int, group: int, row: int, col: int, step: int, p: float) -> bool:
+    """Whether prsgd_dropout keeps that element."""
+    rc = lib.prsgd_dropout_keep(seed, group, row, col, step, p)
+    if rc < 0:
+        _check(rc)
+    return rc == 1
+
+
+def prsgd_dropout(x: torch.Tensor, p: float, seed: int, *, step: int = 0, step_counter: Optional[torch.Tensor] = None,
+                  residual: Optional[torch.Tensor] = None, first_group: int = 0, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """keep * x / (1 - p) (+ residual) for x [G, rows, cols] or [rows, cols]; the gradient with respect to x is the same call on the
+    gradient.  `step_counter`: an int64 tensor of one element on the GPU that is added to step.  See prsgd.h."""
+    ptr, ty, row, group = _matrices(x, "x")
+    at = x.get_device()
+    if out is None:
+        out = _empty(x.shape, x.dtype, x.device, stream)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have x's shape and type")
+    _same_place("out", out, at)
+    optr, _, orow, ogroup = _matrices(out, "out")
+    res = (None, 0, 0)
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype != x.dtype:
+            raise ValueError("residual must have x's shape and type")
+        _same_place("residual", residual, at)
+        rptr, _, rrow, rgroup = _matrices(residual, "residual")
+        res = (rptr, rrow, rgroup)
+    _run_on(at, stream, lib.prsgd_dropout, ptr, ty, row, group, *res, optr, orow, ogroup, *_size3(x), p, seed, step,
+            _dense(step_counter, "step_counter", torch.int64, 1, at), first_group)
+    return out
+
+
+def _rows_aligned(t: torch.Tensor) -> int:
+    """Whether every row of t begins on a 16-byte boundary."""
+    ptr, _, row, group = _matrices(t, "W")
+    v = 16 // t.element_size()
+    return 1 if ptr % 16 == 0 and row % v == 0 and group % v == 0 else 0
+
+
+def _vocab_bytes(fn, type_: int, groups: int, tokens: int, vocab: int, dim: int, w_aligned: int) -> int:
+    n = C.c_size_t()
+    _check(fn(type_, groups, tokens, vocab, dim, w_aligned, C.byref(n)))
+    return n.value
+
+
+def prsgd_vocab_loss_workspace_bytes(type_: int, groups: int, tokens: int, vocab: int, dim: int, w_aligned: int) -> int:
+    return _vocab_bytes(lib.prsgd_vocab_loss_workspace_bytes, type_, groups, tokens, vocab, dim, w_aligned)
+
+
+def prsgd_vocab_loss_grad_workspace_bytes(type_: int, groups: int, tokens: int, vocab: int, dim: int, w_aligned: int) -> int:
+    return _vocab_bytes(lib.prsgd_vocab_loss_grad_workspace_bytes, type_, groups, tokens, vocab, dim, w_aligned)
+
+
+def vocab_loss_workspace(H: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
+    (G, T, D), V = _size3(H), _size3(W)[1]
+    return _empty(prsgd_vocab_loss_workspace_bytes(TYPES[H.dtype], G, T, V, D, _rows_aligned(W)), torch.uint8, H.device, stream)
+
+
+def vocab_loss_grad_workspace(H: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
+    (G, T, D), V = _size3(H), _size3(W)[1]
+    return _empty(prsgd_vocab_loss_grad_workspace_bytes(TYPES[H.dtype], G, T, V, D, _rows_aligned(W)), torch.uint8, H.device, stream)
+
+
+def vocab_loss_outputs(H: torch.Tensor, stream=None):
+    """Tensors for prsgd_vocab_loss's results: loss [G, T], stats [G, T, 2]."""
+    G, T, _ = _size3(H)
+    return _empty((G, T), torch.float32, H.device, stream), _empty((G, T, 2), torch.float32, H.device, stream)
+
+
+def _vocab_inputs(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor):
+    """What both entries begin with, and (G, T, V, D, device)."""
+    h, ty, hr, hg = _matrices(H, "H")
+    w, wty, wr, wg = _matrices(W, "W")
+    (G, T, D), (wG, V, wD), at = _size3(H), _size3(W), H.get_device()
+    if wty != ty or wG != G or wD != D or H.dim() != W.dim():
+        raise ValueError("W must be [groups, vocab, dim] with H's groups, dim and type")
+    _same_place("W", W, at)
+    return (h, hr, hg, w, wr, wg, ty, _dense(labels, "labels", torch.int32, G * T, at), G, T, V, D), (G, T, V, D, at)
+
+
+def prsgd_vocab_loss(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, *, out=None, workspace: Optional[torch.Tensor] = None,
+                     stream=None):
+    """Softmax cross entropy of the class layer W [G, V, D] over H [G, T, D] (or [V, D], [T, D]) with int32 labels [G, T]; returns (loss,
+    stats), see prsgd.h.  `out`: a tuple as vocab_loss_outputs makes it."""
+    args, (G, T, V, D, at) = _vocab_inputs(H, W, labels)
+    if out is None:
+        out = vocab_loss_outputs(H, stream)
+    if workspace is None:
+        workspace = vocab_loss_workspace(H, W, stream)
+    work, size = _scratch(workspace, at)
+    loss, stats = out
+    _run_on(at, stream, lib.prsgd_vocab_loss, *args, _dense(loss, "loss", torch.float32, G * T, at),
+            _dense(stats, "stats", torch.float32, 2 * G * T, at), work, size)
+    return out
+
+
+def prsgd_vocab_loss_grad(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, stats: torch.Tensor, *,
+                          dloss: Optional[torch.Tensor] = None, dlse: Optional[torch.Tensor] = None, dH: Optional[torch.Tensor] = None,
+                          dW: Optional[torch.Tensor] = None, accumulate: bool = False, want_dH: bool = True, want_dW: bool = True,
+                          workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients (dH, dW) of the loss (dloss [G, T]) and of the logarithm of the softmax's denominator (dlse [G, T]); accumulate: added to what
+    dW, of W's type or float32, holds.  One that is not wanted stays None.  See prsgd.h."""
+    args, (G, T, V, D, at) = _vocab_inputs(H, W, labels)
+    if (dH is not None and not want_dH) or (dW is not None and not want_dW):
+        raise ValueError("a gradient is given that is not wanted")
+    if accumulate and want_dW and dW is None:
+        raise ValueError("accumulate needs the dW that is added to")
+    if want_dH and dH is None:
+        dH = _empty(H.shape, H.dtype, H.device, stream)
+    if want_dW and dW is None:
+        dW = _empty(W.shape, W.dtype, W.device, stream)
+    h, w = (None, 0, 0), (None, 0, 0, 0)
+    if dH is not None:
+        if dH.shape != H.shape or dH.dtype != H.dtype:
+            raise ValueError("dH must have H's shape and type")
+        _same_place("dH", dH, at)
+        ptr, _, row, group = _matrices(dH, "dH")
+        h = (ptr, row, group)
+    if dW is not None:
+        if dW.shape != W.shape or dW.dtype not in (W.dtype, torch.float32):
+            raise ValueError("dW must have W's shape and its type or float32")
+        _same_place("dW", dW, at)
+        w = _matrices(dW, "dW")
+    if workspace is None:
+        workspace = vocab_loss_grad_workspace(H, W, stream)
+    work, size = _scratch(workspace, at)
+    f32, n = torch.float32, G * T
+    _run_on(at, stream, lib.prsgd_vocab_loss_grad, *args, _dense(stats, "stats", f32, 2 * n, at), _dense(dloss, "dloss", f32, n, at),
+            _dense(dlse, "dlse", f32, n, at), *h, *w, 1 if accumulate else 0, work, size)
+    return dH, dW
 
 
 def _host_ptr(a: np.ndarray) -> int:
