@@ -1,201 +1,324 @@
-// Softmax cross entropy over a vocabulary and its gradient, logits formed in pieces: z = H W^T, G = (dloss + dlse) softmax(z) -
-// dloss onehot, dH = G W, dW = G^T H.  Products of 64 x 64 tiles on the CUDA cores.
+// Softmax cross entropy over a vocabulary and its gradient: the passes before and behind the products (kernels_vocab_tc.cuh).
+//
+// The tokens that have a label are moved together: row c of the operand H' of a group is its c-th live token (index[c] in the
+// call's order).  Padding then costs nothing in the products, whatever its rows hold reaches nothing, and the copy (4 D
+// bytes a token beside 2 V D operations) brings any stride, alignment and type to one form: rows of 16-bit values on 16-byte
+// boundaries.  fp32 operands become pairs of fp16 values (hi, and lo = what hi rounded off) of x 2^e, e per group such that the
+// largest finite magnitude lies in [2^14, 2^15): 22 bits, nothing below 2^-39 of that largest.  W is read where it lies unless
+// it is fp32 or its rows do not begin on 16-byte boundaries; then it is copied the same way.
 #pragma once
 #include "rows_io.cuh"
 
 namespace prsgd {
 
-constexpr int kVocabTile = 64, kVocabK = 16, kVocabRun = 8;    // tiles of a block's run along the vocabulary
+constexpr int kVocabAmaxBlocks = 64;           // partial maxima per group and operand
 
-struct VocabArgs {
-  const void* H; int64_t h_row, h_group;
-  const void* W; int64_t w_row, w_group;
-  const int32_t* labels;
-  int64_t T, V;
-  int D;
-  int runs;
-  float2* part;              // [groups][T][runs] (max, sum of e^(z - max))
-  float* zy;                 // [groups][T]
-  float* loss; float* stats;
-  const float* in_stats; const float* dloss; const float* dlse;
-  float* G;                  // [groups][T][piece]
-  float* acc;                // [groups][T][D]
-  int64_t piece, v0, pv;     // columns of a piece; first of this one, how many
-  void* dH; int64_t dh_row, dh_group;
-  void* dW; int64_t dw_row, dw_group;
-  int accumulate;
-  DeviceStatus* status;
+// Factors of a group, two for each power of two that may lie outside a float's range.
+struct VocabScale {
+  float z1, z2;              // logit = sum * z1 * z2
+  float g;                   // G is held times g
+  float dh1, dh2;            // dH = sum * dh1 * dh2
+  float dw1, dw2;
+  float h, w;                // operands are held times these
+  float pad[7];
 };
 
-// 64 x 64 sums of a(row, k) b(col, k) over k, 4 x 4 a thread of 16 x 16: element (4 ty + i, 4 tx + j)
-template <typename FA, typename FB>
-__device__ __forceinline__ void vocab_tile(int64_t K, FA&& fa, FB&& fb, float (&acc)[4][4], float (&sa)[kVocabK][kVocabTile + 4], float (&sb)[kVocabK][kVocabTile + 4]) {
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-  for (int64_t k0 = 0; k0 < K; k0 += kVocabK) {
-    for (int e = threadIdx.x; e < kVocabK * kVocabTile; e += 256) {
-      const int k = e & 15, r = e >> 4;
-      sa[k][r] = k0 + k < K ? fa(r, k0 + k) : 0.f;
-      sb[k][r] = k0 + k < K ? fb(r, k0 + k) : 0.f;
+struct VocabPrep {
+  const void* H; int64_t h_row, h_group;
+  const void* W; int64_t w_row, w_group;
+  int h_type;                // element type of the call
+  const int32_t* labels;
+  const float* stats; const float* dloss; const float* dlse;
+  int64_t groups, T, V;
+  int D, grad, vec_h, vec_w;
+  int64_t Tp;                // rows of H' (T rounded up to 64)
+  int pitch;                 // elements of an operand row (D rounded up to 8)
+  int w_groups;              // groups of W (1: shared)
+  uint16_t* Hc[2]; uint16_t* Wc[2];            // [groups][Tp][pitch], [w_groups][V][pitch] or nullptr
+  float4* rowp;              // [groups][Tp]: (max, log sum, dloss + dlse, dloss)
+  int* rowy; int* index;     // [groups][Tp]: label; token
+  int* live;                 // [groups]
+  VocabScale* scale;         // [groups]
+  float* amax;               // [groups][2][kVocabAmaxBlocks]
+  float* loss; float* out_stats;
+  void* dH; int64_t dh_row, dh_group; int vec_dh;
+  unsigned int* counters; int n_counters;
+  DeviceStatus* status;
+  int h_blocks, w_blocks;    // blocks of a group
+};
+
+__device__ __forceinline__ float vocab_block_max(float v, float* sm) {
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = sm[threadIdx.x & 7];
+  for (int o = 4; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ int vocab_block_sum(int v, int* sm) {
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = sm[threadIdx.x & 7];
+  for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float finite_abs(float x) { return fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.f; }
+// e with x 2^e in [2^top, 2^(top + 1)), 0 for x = 0; within a normal float's exponents
+__device__ __forceinline__ int vocab_exponent(float x, int top) { return x > 0.f ? max(-126, min(126, top - ilogbf(x))) : 0; }
+__device__ __forceinline__ void vocab_halves(int n, float& a, float& b) { a = exp2f((float)(n / 2)); b = exp2f((float)(n - n / 2)); }
+
+// Largest finite magnitudes of the live rows of H and of W (fp32 operands only).
+__global__ void __launch_bounds__(256) vocab_amax_kernel(const VocabPrep a) {
+  __shared__ float sm[8];
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.y;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool of_w = blockIdx.x >= kVocabAmaxBlocks;
+  const int blk = blockIdx.x % kVocabAmaxBlocks;
+  const float* x = of_w ? static_cast<const float*>(a.W) + (a.w_groups > 1 ? g : 0) * a.w_group : static_cast<const float*>(a.H) + g * a.h_group;
+  const int64_t rows = of_w ? a.V : a.T, pitch = of_w ? a.w_row : a.h_row;
+  float most = 0.f;
+  for (int64_t r = blk * 8 + warp; r < rows; r += kVocabAmaxBlocks * 8) {
+    if (!of_w) {
+      const int y = a.labels[g * a.T + r];
+      if (y < 0 || y >= a.V) continue;
     }
-    __syncthreads();
+    const float* row = x + r * pitch;
+    for (int c = lane; c < a.D; c += 32) most = fmaxf(most, finite_abs(row[c]));
+  }
+  most = vocab_block_max(most, sm);
+  if (threadIdx.x == 0) a.amax[(g * 2 + of_w) * kVocabAmaxBlocks + blk] = most;
+}
+
+// A row of D elements into operand rows (of one plane or two), a warp's lanes eight elements each.
+template <int TY, bool VEC>
+__device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* from, uint16_t* hi, uint16_t* lo, int D, float scale, int lane) {
+  for (int c = lane * 8; c < D; c += 256) {
+    const int n = min(8, D - c);
+    uint4 u, w = make_uint4(0, 0, 0, 0);
+    if constexpr (TY == PRSGD_TYPE_FP32) {
+      float v[8];
+      load8<TY, VEC>(from + c, n, v);
+      __half* p = reinterpret_cast<__half*>(&u);
+      __half* q = reinterpret_cast<__half*>(&w);
 #pragma unroll
-    for (int k = 0; k < kVocabK; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty * 4 + i], sb[k][tx * 4 + j], acc[i][j]);
+      for (int i = 0; i < 8; ++i) {
+        const float x = v[i] * scale;
+        p[i] = __float2half_rn(x);
+        q[i] = __float2half_rn(x - __half2float(p[i]));
+      }
+      *reinterpret_cast<uint4*>(lo + c) = w;
+    } else if (VEC && n == 8) {
+      u = *reinterpret_cast<const uint4*>(from + c);
+    } else {
+      u = make_uint4(0, 0, 0, 0);
+      typename ElemOf<TY>::type* p = reinterpret_cast<typename ElemOf<TY>::type*>(&u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = from[c + i];
+    }
+    *reinterpret_cast<uint4*>(hi + c) = u;
+  }
+}
+
+// Blocks x < h_blocks of a group move its live rows together, the others copy W.  A block counts the live tokens before its own; the
+// group's first block counts all, finds the scales, and zeroes the rows behind the last live one that a product may read.
+template <int TY>
+__global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
+  using T = typename ElemOf<TY>::type;
+  __shared__ float smf[8];
+  __shared__ int smi[8];
+  __shared__ int place[256];
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.y;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int eh = 0, ew = 0;
+  if constexpr (TY == PRSGD_TYPE_FP32) {
+    const float* m = a.amax + g * 2 * kVocabAmaxBlocks;
+    eh = vocab_exponent(vocab_block_max(threadIdx.x < kVocabAmaxBlocks ? m[threadIdx.x] : 0.f, smf), 14);
+    ew = vocab_exponent(vocab_block_max(threadIdx.x < kVocabAmaxBlocks ? m[kVocabAmaxBlocks + threadIdx.x] : 0.f, smf), 14);
+  }
+  if ((int)blockIdx.x >= a.h_blocks) {                     // ---- W
+    if (g >= a.w_groups) return;
+    const float scale = exp2f((float)ew);
+    const T* W = static_cast<const T*>(a.W) + g * a.w_group;
+    for (int64_t v = (int64_t)(blockIdx.x - a.h_blocks) * 8 + warp; v < a.V; v += (int64_t)a.w_blocks * 8) {
+      const int64_t o = (g * a.V + v) * a.pitch;
+      uint16_t* lo = TY == PRSGD_TYPE_FP32 ? a.Wc[1] + o : nullptr;
+      if (a.vec_w) vocab_copy_row<TY, true>(W + v * a.w_row, a.Wc[0] + o, lo, a.D, scale, lane);
+      else vocab_copy_row<TY, false>(W + v * a.w_row, a.Wc[0] + o, lo, a.D, scale, lane);
+    }
+    return;
+  }
+  const int32_t* labels = a.labels + g * a.T;
+  const int64_t per = (a.T + a.h_blocks - 1) / a.h_blocks, begin = blockIdx.x * per, end = min(a.T, begin + per);
+  auto is_live = [&](int y) { return y >= 0 && y < a.V; };
+  int before = 0;
+  for (int64_t t = threadIdx.x; t < begin; t += 256) before += is_live(labels[t]) ? 1 : 0;
+  before = vocab_block_sum(before, smi);
+  const float hs = exp2f((float)eh);
+  if (blockIdx.x == 0) {
+    if (g == 0) {
+      if (threadIdx.x < sizeof(DeviceStatus) / 4) reinterpret_cast<unsigned int*>(a.status)[threadIdx.x] = 0u;
+      for (int i = threadIdx.x; i < a.n_counters; i += 256) a.counters[i] = 0u;
+    }
+    int all = 0;
+    float most = 0.f;
+    for (int64_t t = threadIdx.x; t < a.T; t += 256) {
+      if (!is_live(labels[t])) continue;
+      ++all;
+      if (a.grad) most = fmaxf(most, finite_abs((a.dloss ? fabsf(a.dloss[g * a.T + t]) : 0.f) + (a.dlse ? fabsf(a.dlse[g * a.T + t]) : 0.f)));
+    }
+    all = vocab_block_sum(all, smi);
+    most = vocab_block_max(most, smf);
+    if (threadIdx.x == 0) {
+      a.live[g] = all;
+      const int e = vocab_exponent(most, 13);
+      VocabScale s{};
+      vocab_halves(-(eh + ew), s.z1, s.z2);
+      s.g = exp2f((float)e);
+      vocab_halves(-(e + ew), s.dh1, s.dh2);
+      vocab_halves(-(e + eh), s.dw1, s.dw2);
+      s.h = hs; s.w = exp2f((float)ew);
+      a.scale[g] = s;
+    }
+    if (a.grad) {
+      const int64_t last = min((int64_t)(all + 63) / 64 * 64, a.Tp);
+      for (int64_t r = all + warp; r < last; r += 8)
+        for (int c = lane * 8; c < a.pitch; c += 256) {
+          const int64_t o = (g * a.Tp + r) * a.pitch + c;
+          *reinterpret_cast<uint4*>(a.Hc[0] + o) = make_uint4(0, 0, 0, 0);
+          if (TY == PRSGD_TYPE_FP32) *reinterpret_cast<uint4*>(a.Hc[1] + o) = make_uint4(0, 0, 0, 0);
+        }
+    }
+  }
+  const T* H = static_cast<const T*>(a.H) + g * a.h_group;
+  for (int64_t t0 = begin; t0 < end; t0 += 256) {
+    const int64_t t = t0 + threadIdx.x;
+    const int y = t < end ? labels[t] : -1;
+    const bool on = is_live(y);
+    const unsigned int mask = __ballot_sync(0xffffffffu, on);
     __syncthreads();
+    if (lane == 0) smi[warp] = __popc(mask);
+    __syncthreads();
+    int at = before + __popc(mask & ((1u << lane) - 1u));
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) at += smi[w];
+      before += smi[w];
+    }
+    place[threadIdx.x] = on ? at : -1;
+    if (t < end) {
+      const int64_t c = g * a.Tp + at, o = g * a.T + t;
+      if (on) {
+        a.rowy[c] = y;
+        a.index[c] = (int)t;
+        if (a.grad) {
+          const float dl = a.dloss ? a.dloss[o] : 0.f, both = dl + (a.dlse ? a.dlse[o] : 0.f);
+          a.rowp[c] = make_float4(a.stats[2 * o], a.stats[2 * o + 1], both, dl);
+        }
+      } else if (!a.grad) {
+        a.loss[o] = 0.f;
+        a.out_stats[2 * o] = 0.f;
+        a.out_stats[2 * o + 1] = 0.f;
+      }
+    }
+    __syncthreads();
+    const int here = (int)min((int64_t)256, end - t0);
+    for (int i = warp; i < here; i += 8) {
+      const int c = place[i];
+      if (c >= 0) {
+        const int64_t o = (g * a.Tp + c) * a.pitch;
+        uint16_t* lo = TY == PRSGD_TYPE_FP32 ? a.Hc[1] + o : nullptr;
+        if (a.vec_h) vocab_copy_row<TY, true>(H + (t0 + i) * a.h_row, a.Hc[0] + o, lo, a.D, hs, lane);
+        else vocab_copy_row<TY, false>(H + (t0 + i) * a.h_row, a.Hc[0] + o, lo, a.D, hs, lane);
+      } else if (a.dH != nullptr) {
+        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        T* to = static_cast<T*>(a.dH) + g * a.dh_group + (t0 + i) * a.dh_row;
+        for (int q = lane * 8; q < a.D; q += 256) {
+          if (a.vec_dh) store8<TY, true>(to + q, min(8, a.D - q), zero);
+          else store8<TY, false>(to + q, min(8, a.D - q), zero);
+        }
+      }
+    }
   }
 }
 
-template <int TY>
-__global__ void __launch_bounds__(256) vocab_stats_kernel(const VocabArgs a) {
+// Largest logit and sum of every live token from those of its runs of the vocabulary: a block takes 32 tokens, eight lanes each.
+struct VocabJoin {
+  const float2* part;        // [groups][runs][Tp]
+  const float* zy; const int* index; const int* live;
+  int64_t Tp, T;
+  int runs;
+  float* loss; float* stats;
+};
+__global__ void __launch_bounds__(256) vocab_join_kernel(const VocabJoin a) {
+  __shared__ float2 got[8][32];
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.y;
+  const int live = a.live[g], row = blockIdx.x * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
+  if ((int)blockIdx.x * 32 >= live) return;
+  constexpr float kLog2e = 1.4426950408889634f;
+  float m = -INFINITY, s = 0.f;
+  if (row < live) {
+    const float2* part = a.part + g * a.runs * a.Tp + row;
+#pragma unroll 4
+    for (int r = share; r < a.runs; r += 8) {
+      const float2 p = part[(int64_t)r * a.Tp];
+      const float most = fmaxf(m, p.x);
+      if (most == -INFINITY && p.y == 0.f) continue;       // (a run without columns)
+      s = s * exp2f((m - most) * kLog2e) + p.y * exp2f((p.x - most) * kLog2e);
+      m = most;
+    }
+  }
+  got[share][threadIdx.x & 31] = make_float2(m, s);
+  __syncthreads();
+  if (share != 0 || row >= live) return;
+  for (int k = 1; k < 8; ++k) m = fmaxf(m, got[k][row & 31].x);
+  s = 0.f;
+  for (int k = 0; k < 8; ++k) {
+    const float2 p = got[k][row & 31];
+    if (p.x == -INFINITY && p.y == 0.f) continue;
+    s += p.y * exp2f((p.x - m) * kLog2e);
+  }
+  const float log_sum = logf(s);
+  const int64_t o = g * a.T + a.index[g * a.Tp + row];
+  a.loss[o] = log_sum + (m - a.zy[g * a.Tp + row]);
+  a.stats[2 * o] = m;
+  a.stats[2 * o + 1] = log_sum;
+}
+
+// dH of the live tokens from its parts along the vocabulary, in order.
+struct VocabSum {
+  const float* acc;          // [groups][parts][Tp][acc_pitch]
+  const int* index; const int* live;
+  int64_t Tp, groups;
+  int parts, acc_pitch, D;
+  void* dH; int64_t dh_row, dh_group;
+};
+template <int TY, bool VEC>
+__global__ void __launch_bounds__(256) vocab_sum_kernel(const VocabSum a) {
   using T = typename ElemOf<TY>::type;
-  __shared__ float sa[kVocabK][kVocabTile + 4], sb[kVocabK][kVocabTile + 4];
   op_pdl_wait();
   op_pdl_trigger();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < sizeof(DeviceStatus) / 4) reinterpret_cast<unsigned int*>(a.status)[threadIdx.x] = 0u;
-  const int64_t g = blockIdx.z, t0 = (int64_t)blockIdx.x * kVocabTile;
-  const T* H = static_cast<const T*>(a.H) + g * a.h_group;
-  const T* W = static_cast<const T*>(a.W) + g * a.w_group;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float m[4], s[4];
-  int y[4];
-  for (int i = 0; i < 4; ++i) {
-    m[i] = -INFINITY; s[i] = 0.f;
-    y[i] = t0 + ty * 4 + i < a.T ? a.labels[g * a.T + t0 + ty * 4 + i] : -1;
-  }
-  for (int64_t v0 = (int64_t)blockIdx.y * kVocabRun * kVocabTile, n = 0; n < kVocabRun && v0 < a.V; ++n, v0 += kVocabTile) {
-    float z[4][4];
-    vocab_tile(a.D, [&](int r, int64_t k) { return t0 + r < a.T ? to_f32(H[(t0 + r) * a.h_row + k]) : 0.f; },
-               [&](int r, int64_t k) { return v0 + r < a.V ? to_f32(W[(v0 + r) * a.w_row + k]) : 0.f; }, z, sa, sb);
-    for (int i = 0; i < 4; ++i) {
-      float most = -INFINITY;
-      for (int j = 0; j < 4; ++j)
-        if (v0 + tx * 4 + j < a.V) most = z[i][j] != z[i][j] ? z[i][j] : fmaxf(most, z[i][j]);
-      for (int o = 1; o < 16; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      most = fmaxf(most, m[i]);
-      float sum = 0.f;
-      for (int j = 0; j < 4; ++j)
-        if (v0 + tx * 4 + j < a.V) sum += expf(z[i][j] - most);
-      for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      s[i] = s[i] * expf(m[i] - most) + sum;
-      if (m[i] == -INFINITY) s[i] = sum;
-      m[i] = most;
-      for (int j = 0; j < 4; ++j)
-        if (y[i] >= 0 && v0 + tx * 4 + j == y[i] && y[i] < a.V) a.zy[g * a.T + t0 + ty * 4 + i] = z[i][j];
+  const int64_t g = blockIdx.z;
+  const int c = ((int)blockIdx.y * 32 + (threadIdx.x & 31)) * 8, live = a.live[g];
+  if (c >= a.D) return;
+  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < live; r += (int64_t)gridDim.x * 8) {
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v[8];
+    const float* from = a.acc + (g * a.parts * a.Tp + r) * a.acc_pitch + c;
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+      load8<PRSGD_TYPE_FP32, true>(from + (int64_t)p * a.Tp * a.acc_pitch, 8, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += v[i];
     }
-  }
-  if (tx == 0)
-    for (int i = 0; i < 4; ++i)
-      if (t0 + ty * 4 + i < a.T) a.part[(g * a.T + t0 + ty * 4 + i) * a.runs + blockIdx.y] = make_float2(m[i], s[i]);
-}
-
-__global__ void __launch_bounds__(256) vocab_join_kernel(const VocabArgs a) {
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, at = blockIdx.y * a.T + t;
-  if (t >= a.T) return;
-  const int y = a.labels[at];
-  float loss = 0.f, m = 0.f, log_sum = 0.f;
-  if (y >= 0 && y < a.V) {
-    m = -INFINITY;
-    for (int r = 0; r < a.runs; ++r) m = fmaxf(m, a.part[at * a.runs + r].x);
-    float s = 0.f;
-    for (int r = 0; r < a.runs; ++r) {
-      const float2 p = a.part[at * a.runs + r];
-      s += p.y * expf(p.x - m);
-    }
-    log_sum = logf(s);
-    loss = log_sum + (m - a.zy[at]);
-  }
-  a.loss[at] = loss;
-  a.stats[2 * at] = m;
-  a.stats[2 * at + 1] = log_sum;
-}
-
-template <int TY>
-__global__ void __launch_bounds__(256) vocab_g_kernel(const VocabArgs a) {
-  using T = typename ElemOf<TY>::type;
-  __shared__ float sa[kVocabK][kVocabTile + 4], sb[kVocabK][kVocabTile + 4];
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int64_t g = blockIdx.z, t0 = (int64_t)blockIdx.x * kVocabTile, v0 = a.v0 + (int64_t)blockIdx.y * kVocabTile, vend = a.v0 + a.pv;
-  const T* H = static_cast<const T*>(a.H) + g * a.h_group;
-  const T* W = static_cast<const T*>(a.W) + g * a.w_group;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float z[4][4];
-  vocab_tile(a.D, [&](int r, int64_t k) { return t0 + r < a.T ? to_f32(H[(t0 + r) * a.h_row + k]) : 0.f; },
-             [&](int r, int64_t k) { return v0 + r < vend ? to_f32(W[(v0 + r) * a.w_row + k]) : 0.f; }, z, sa, sb);
-  for (int i = 0; i < 4; ++i) {
-    const int64_t t = t0 + ty * 4 + i, at = g * a.T + t;
-    if (t >= a.T) break;
-    const int y = a.labels[at];
-    const bool live = y >= 0 && y < a.V;
-    const float dl = live && a.dloss ? a.dloss[at] : 0.f, both = dl + (live && a.dlse ? a.dlse[at] : 0.f);
-    for (int j = 0; j < 4; ++j) {
-      const int64_t v = v0 + tx * 4 + j;
-      if (v >= vend) break;
-      const float p = live ? expf((z[i][j] - a.in_stats[2 * at]) - a.in_stats[2 * at + 1]) : 0.f;
-      a.G[at * a.piece + v - a.v0] = live ? both * p - (v == y ? dl : 0.f) : 0.f;
-    }
-  }
-}
-
-template <int TY>
-__global__ void __launch_bounds__(256) vocab_dh_kernel(const VocabArgs a) {
-  using T = typename ElemOf<TY>::type;
-  __shared__ float sa[kVocabK][kVocabTile + 4], sb[kVocabK][kVocabTile + 4];
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int64_t g = blockIdx.z, t0 = (int64_t)blockIdx.x * kVocabTile;
-  const int d0 = blockIdx.y * kVocabTile;
-  const T* W = static_cast<const T*>(a.W) + g * a.w_group;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float z[4][4];
-  vocab_tile(a.pv, [&](int r, int64_t k) { return t0 + r < a.T ? a.G[(g * a.T + t0 + r) * a.piece + k] : 0.f; },
-             [&](int r, int64_t k) { return d0 + r < a.D ? to_f32(W[(a.v0 + k) * a.w_row + d0 + r]) : 0.f; }, z, sa, sb);
-  for (int i = 0; i < 4; ++i) {
-    const int64_t t = t0 + ty * 4 + i;
-    if (t >= a.T) break;
-    const int y = a.labels[g * a.T + t];
-    for (int j = 0; j < 4; ++j) {
-      const int d = d0 + tx * 4 + j;
-      if (d >= a.D) break;
-      float* to = a.acc + (g * a.T + t) * a.D + d;
-      const float v = y >= 0 && y < a.V ? (a.v0 > 0 ? *to : 0.f) + z[i][j] : 0.f;
-      *to = v;
-      if (a.v0 + a.pv == a.V) static_cast<T*>(a.dH)[g * a.dh_group + t * a.dh_row + d] = from_f32<T>(v);
-    }
-  }
-}
-
-template <int TY, int OTY>
-__global__ void __launch_bounds__(256) vocab_dw_kernel(const VocabArgs a) {
-  using T = typename ElemOf<TY>::type;
-  using O = typename ElemOf<OTY>::type;
-  __shared__ float sa[kVocabK][kVocabTile + 4], sb[kVocabK][kVocabTile + 4];
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int64_t g = blockIdx.z, v0 = (int64_t)blockIdx.x * kVocabTile;
-  const int d0 = blockIdx.y * kVocabTile;
-  const T* H = static_cast<const T*>(a.H) + g * a.h_group;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float z[4][4];
-  vocab_tile(a.T, [&](int r, int64_t k) { return v0 + r < a.pv ? a.G[(g * a.T + k) * a.piece + v0 + r] : 0.f; },
-             [&](int r, int64_t k) {
-               const int y = a.labels[g * a.T + k];
-               return d0 + r < a.D && y >= 0 && y < a.V ? to_f32(H[k * a.h_row + d0 + r]) : 0.f;
-             }, z, sa, sb);
-  for (int i = 0; i < 4; ++i) {
-    const int64_t v = v0 + ty * 4 + i;
-    if (v >= a.pv) break;
-    for (int j = 0; j < 4; ++j) {
-      const int d = d0 + tx * 4 + j;
-      if (d >= a.D) break;
-      O* to = static_cast<O*>(a.dW) + g * a.dw_group + (a.v0 + v) * a.dw_row + d;
-      *to = from_f32<O>((a.accumulate ? to_f32(*to) : 0.f) + z[i][j]);
-    }
+    store8<TY, VEC>(static_cast<T*>(a.dH) + g * a.dh_group + a.index[g * a.Tp + r] * a.dh_row + c, min(8, a.D - c), sum);
   }
 }
 

@@ -1,0 +1,679 @@
+// The products of the vocabulary loss and of its gradient on the tensor cores, one persistent launch each.
+//
+// A pair of CTAs (cta_group::2) forms a 256 x 256 tile: each loads half of both operands (128 rows of A, 128 of B, 64 of the
+// contraction per stage) by TMA and keeps 128 rows of the sum in its TMEM, two sums of 256 columns so that the epilogue of one
+// tile runs beside the products of the next.  Tokens are the rows of a tile of logits, so a thread of the epilogue owns a
+// token: maxima and sums of exponentials need no exchange between threads.
+//  * Loss: a task is a run of tiles along the vocabulary for one block of 256 tokens; its epilogue keeps each token's running (max, sum of
+//    e^(z - max)) in registers and leaves them once per run.  Runs are ordered so that the pairs which work at a time share them: W comes
+//    from HBM once, H' stays in L2.
+//  * Gradient: the vocabulary is taken in pieces.  Tiles of G of a piece (logits again, then the softmax's gradient in the epilogue, held in
+//    16 bits) and tiles of dW = G^T H' and dH += G W that use it are tasks of one list: G of piece k, then the uses of piece k - lag, so
+//    that what a task waits for was claimed a phase earlier.  Pieces are sized so that a few of them stay in L2 (126 MB).  G^T, W^T and H'^T are read
+//    MN-major: nothing is transposed in memory.  dH of several pieces adds up in fp32 in the workspace, each tile in the order of
+//    the pieces; a long contraction is cut into parts with sums of their own, added up by a last launch.
+// Tasks are claimed in order from a device counter, and a claimed task waits only for tasks claimed earlier, so the CTAs that run
+// always make progress, whatever share of the grid is resident.
+#pragma once
+#include "kernels_vocab.cuh"
+#include "tc_pair.cuh"
+
+namespace prsgd {
+
+constexpr int kVtEpiWarps = 8, kVtThreads = 32 * (4 + kVtEpiWarps), kVtRing = 4;
+constexpr int kVtWarpCols = 128;               // an epilogue warp takes 32 rows of a CTA's 128 x 256 sums and this many columns
+constexpr uint32_t kVtStageBytes = 32768, kVtWarpBytes = 8192;
+__host__ __device__ constexpr int vt_stages(bool grad) { return grad ? 5 : 6; }            // (the gradient's epilogue needs shared memory too)
+constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kVtStageBytes + (grad ? kVtEpiWarps * kVtWarpBytes : 0); }
+constexpr int kVtAhead = 8;                    // the next task is claimed when this many blocks of 64 of the current one are left to load
+enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE };
+enum { VT_STATS = 0, VT_G, VT_DH, VT_DW };
+
+struct VocabMaps {
+  CUtensorMap hk[2], wk[2];                    // [hi, lo] H', W read K-major: box {64, 128}
+  CUtensorMap hm[2], wm[2], gk[2], gm[2];      // MN-major (box {64, 64}); G both ways
+};
+
+struct VocabChain {
+  int groups, D;
+  int64_t T, V, Tp;
+  int w_shared, w_swap;                        // W of all groups is one; W's groups lie row by row in turn: map dimensions (D, groups, V)
+  int bf16;                                    // operands are bf16 (else fp16)
+  const int* live; const float4* rowp; const int* rowy; const int* index; const VocabScale* scale;
+  // loss
+  int runs, run;                               // runs of the vocabulary, tiles of one
+  float2* part; float* zy;
+  // gradient
+  int pieces, piece, gp;                       // pieces of a group, columns of one (a multiple of 256), columns of a row of G (a multiple of 64)
+  int slots, lag, parts;
+  uint16_t* G[2];                              // [slots][Tp][gp]
+  float* acc; int acc_pitch;                   // [groups][parts][Tp][acc_pitch] or nullptr: one piece, one part
+  void* dH; int64_t dh_row, dh_group; int dh_type, vec_dh;
+  void* dW; int64_t dw_row, dw_group; int dw_type, vec_dw, accumulate;
+  unsigned int* claim; unsigned int* done_g; unsigned int* done_u;     // [groups * pieces] epilogue warps done with tiles of G, with uses of them
+  DeviceStatus* status;
+};
+
+struct VTask { int kind, g, ti, tj, n, p, seq, live; };
+
+// Tasks of the pieces, numbered through all groups (seq = g * pieces + p).
+struct VPiece { int tm, nv, td, pv; };
+__device__ __forceinline__ VPiece vt_piece(const VocabChain& a, int seq, int live) {
+  VPiece k;
+  k.tm = (live + 255) / 256;
+  k.pv = (int)min((int64_t)a.piece, a.V - (int64_t)(seq % a.pieces) * a.piece);
+  k.nv = (k.pv + 255) / 256;
+  k.td = (a.D + 255) / 256;
+  return k;
+}
+__device__ __forceinline__ int vt_uses_h(const VocabChain& a, const VPiece& k) { return a.dH != nullptr ? k.tm * k.td * a.parts : 0; }
+__device__ __forceinline__ int vt_uses_w(const VocabChain& a, const VPiece& k) { return a.dW != nullptr ? k.nv * k.td : 0; }
+__device__ __forceinline__ unsigned int vt_need_g(const VPiece& k) { return (unsigned)(k.tm * k.nv) * 2u * kVtEpiWarps; }
+__device__ __forceinline__ unsigned int vt_need_u(const VocabChain& a, const VPiece& k) { return (unsigned)(vt_uses_h(a, k) + vt_uses_w(a, k)) * 2u * kVtEpiWarps; }
+
+// The blocks of 64 of a task's contraction: first and number.
+__device__ __forceinline__ int vt_blocks(const VocabChain& a, const VTask& k, int& n) {
+  if (k.kind <= VT_G) { n = (a.D + 63) / 64; return 0; }
+  if (k.kind == VT_DW) { n = (k.live + 63) / 64; return 0; }
+  const int nb = ((int)min((int64_t)a.piece, a.V - (int64_t)k.p * a.piece) + 63) / 64;
+  const int first = (int)((int64_t)nb * k.n / a.parts);
+  n = (int)((int64_t)nb * (k.n + 1) / a.parts) - first;
+  return first;
+}
+
+// The list of tasks, walked in order by the thread that claims them.
+struct VWalk {
+  int phase, phases;
+  long long base, count;       // tasks before this phase, in it
+  int live_g, live_u;          // live tokens of the group whose G, whose uses are in it
+};
+template <bool GRAD>
+__device__ __forceinline__ void vt_enter(const VocabChain& a, VWalk& w) {
+  const int last = GRAD ? a.groups * a.pieces : a.groups;
+  w.count = 0;
+  if constexpr (!GRAD) {
+    w.live_g = a.live[w.phase];
+    w.count = (long long)((w.live_g + 255) / 256) * a.runs;
+  } else {
+    if (w.phase < last) {
+      w.live_g = a.live[w.phase / a.pieces];
+      const VPiece k = vt_piece(a, w.phase, w.live_g);
+      w.count += (long long)k.tm * k.nv;
+    }
+    if (w.phase >= a.lag) {
+      w.live_u = a.live[(w.phase - a.lag) / a.pieces];
+      const VPiece k = vt_piece(a, w.phase - a.lag, w.live_u);
+      w.count += vt_uses_h(a, k) + vt_uses_w(a, k);
+    }
+  }
+}
+template <bool GRAD>
+__device__ __forceinline__ bool vt_decode(const VocabChain& a, VWalk& w, long long t, VTask& k) {
+  while (t >= w.base + w.count) {
+    w.base += w.count;
+    if (++w.phase >= w.phases) return false;
+    vt_enter<GRAD>(a, w);
+  }
+  int q = (int)(t - w.base);
+  k.p = k.seq = k.n = 0;
+  if constexpr (!GRAD) {
+    const int tm = (w.live_g + 255) / 256, tiles = (int)((a.V + 255) / 256);
+    k.kind = VT_STATS; k.g = w.phase; k.live = w.live_g;
+    k.tj = q / tm;
+    k.ti = q - k.tj * tm;
+    k.p = k.tj;                                  // (the run)
+    k.tj *= a.run;
+    k.n = min(a.run, tiles - k.tj);
+    return true;
+  }
+  if (w.phase < a.groups * a.pieces) {
+    const VPiece c = vt_piece(a, w.phase, w.live_g);
+    if (q < c.tm * c.nv) {
+      k.kind = VT_G; k.seq = w.phase; k.g = w.phase / a.pieces; k.p = w.phase % a.pieces; k.live = w.live_g;
+      k.tj = q / c.tm;
+      k.ti = q - k.tj * c.tm;
+      return true;
+    }
+    q -= c.tm * c.nv;
+  }
+  const int seq = w.phase - a.lag;
+  const VPiece c = vt_piece(a, seq, w.live_u);
+  k.seq = seq; k.g = seq / a.pieces; k.p = seq % a.pieces; k.live = w.live_u;
+  const int uw = vt_uses_w(a, c);
+  if (q < uw) {
+    k.kind = VT_DW;
+    k.ti = q / c.td;
+    k.tj = q - k.ti * c.td;
+    return true;
+  }
+  q -= uw;
+  k.kind = VT_DH;
+  k.n = q / (c.tm * c.td);
+  q -= k.n * (c.tm * c.td);
+  k.ti = q / c.td;
+  k.tj = q - k.ti * c.td;
+  return true;
+}
+
+namespace ptx {
+// Hands 32 bytes to a CTA of the cluster and counts them on its barrier (which expects them and one arrival).
+__device__ __forceinline__ void send_2v4(uint32_t to_cluster, uint32_t bar_cluster, uint4 v, uint4 w) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 32;" ::"r"(bar_cluster) : "memory");
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(to_cluster), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(bar_cluster) : "memory");
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(to_cluster + 16u), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w), "r"(bar_cluster) : "memory");
+}
+}  // namespace ptx
+
+// A warp's box of 32 rows x 128 bytes, where values change between one row per lane (as they come from TMEM) and 16 bytes per
+// lane, eight lanes to a row.  Chunk c of row r sits at chunk c ^ (r % 8): free of bank conflicts both ways.
+__device__ __forceinline__ uint32_t vt_chunk(uint32_t box, int row, int q) { return box + (uint32_t)row * 128u + (uint32_t)((q ^ (row & 7)) * 16); }
+
+__device__ __forceinline__ float vt_exp2(float x) {        // (to 2 ulp; results below 2^-126 are 0)
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two values as 16-bit ones.
+__device__ __forceinline__ uint32_t vt_pack(int bf16, float x, float y) {
+  if (bf16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return pack_half2(x, y);
+}
+__device__ __forceinline__ void vt_write1(void* out, int type, int64_t o, float v) {
+  if (type == PRSGD_TYPE_FP32) static_cast<float*>(out)[o] = v;
+  else if (type == PRSGD_TYPE_BF16) static_cast<__nv_bfloat16*>(out)[o] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(out)[o] = __float2half_rn(v);
+}
+__device__ __forceinline__ float vt_read1(const void* out, int type, int64_t o) {
+  if (type == PRSGD_TYPE_FP32) return static_cast<const float*>(out)[o];
+  if (type == PRSGD_TYPE_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(out)[o]);
+  return __half2float(static_cast<const __half*>(out)[o]);
+}
+
+// Where a tile of dH or dW goes.
+struct VOut {
+  void* out; int type; int64_t row;            // first row's place is out + at(0)
+  const int* index;                            // rows through index, or one after another
+  int rows, cols;                              // rows of this warp's 32 that exist; columns of the array
+  int add, vec;                                // added to what is there; rows begin on 16-byte boundaries
+  __device__ __forceinline__ int64_t at(int r) const { return (index ? (int64_t)index[r] : (int64_t)r) * row; }
+};
+
+// 32 rows x 32 columns (from column c0) of fp32 values, a row per lane, to where they go, through `box`: a lane writes four columns.
+__device__ __forceinline__ void vt_out32(const VOut& d, uint32_t box, int lane, int c0, const float (&v)[32]) {
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    st_shared_v4(vt_chunk(box, lane, q), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+  __syncwarp();
+  const int c = c0 + (lane & 7) * 4;
+  const bool whole = d.vec && c + 4 <= d.cols;
+#pragma unroll 1
+  for (int i = 0; i < 8; i += 4) {
+    float4 w[4], old[4];
+    int64_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 4 * (i + j) + (lane >> 3);
+      o[j] = r < d.rows ? d.at(r) + c : -1;
+      old[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (d.add && o[j] >= 0) {                            // (past L1, which does not see what other SMs wrote meanwhile)
+        if (whole && d.type == PRSGD_TYPE_FP32) {
+          old[j] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(d.out) + o[j]));
+        } else {
+          float* e = reinterpret_cast<float*>(&old[j]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c + k < d.cols) e[k] = vt_read1(d.out, d.type, o[j] + k);
+        }
+      }
+      const uint4 u = ld_shared_v4(vt_chunk(box, r, lane & 7));
+      w[j] = make_float4(__uint_as_float(u.x) + old[j].x, __uint_as_float(u.y) + old[j].y, __uint_as_float(u.z) + old[j].z, __uint_as_float(u.w) + old[j].w);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (o[j] < 0) continue;
+      if (whole && d.type == PRSGD_TYPE_FP32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(d.out) + o[j]) = w[j];
+      } else {
+        const float* e = reinterpret_cast<const float*>(&w[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k < d.cols) vt_write1(d.out, d.type, o[j] + k, e[k]);
+      }
+    }
+  }
+}
+// 32 rows x 64 columns of 16-bit values already in the box.
+__device__ __forceinline__ void vt_out64(const VOut& d, uint32_t box, int lane, int c0) {
+  const int c = c0 + (lane & 7) * 8;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = 4 * i + (lane >> 3);
+    const uint4 u = ld_shared_v4(vt_chunk(box, r, lane & 7));
+    if (r >= d.rows) continue;
+    uint16_t* to = static_cast<uint16_t*>(d.out) + d.at(r) + c;
+    if (c + 8 <= d.cols) {
+      *reinterpret_cast<uint4*>(to) = u;
+    } else {
+      const uint16_t* e = reinterpret_cast<const uint16_t*>(&u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < d.cols) to[k] = e[k];
+    }
+  }
+}
+
+// SPLIT: fp32 operands, products of fp16 pairs.
+template <bool GRAD, bool SPLIT>
+__global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
+  constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1;
+  constexpr float kLog2e = 1.4426950408889634f;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kVtRing + 1];
+  __shared__ __align__(16) uint4 ring[2 * kVtRing];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = blockIdx.x & 1u;                 // clusters of two along x
+  DeviceStatus* status = a.status;
+  auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
+  auto full = [&](int s) { return bar(s); };                              // in the leader (rank 0): its stage has both CTAs' operands
+  auto empty = [&](int s) { return bar(kStages + s); };                   // in each: the MMAs that read the stage are done
+  auto tfull = [&](int i) { return bar(2 * kStages + i); };               // in each: sum i is complete
+  auto tempty = [&](int i) { return bar(2 * kStages + 2 + i); };          // in the leader: all epilogue warps have read sum i
+  auto sfull = [&](int i) { return bar(2 * kStages + 4 + i); };           // in each: ring entry i holds a task
+  auto sempty = [&](int i) { return bar(2 * kStages + 4 + kVtRing + i); };     // in the leader: everyone has read it
+  const uint32_t loaded = bar(2 * kStages + 4 + 2 * kVtRing);             // in the leader: all loads of a task have been issued
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(loaded, 1);
+    for (int s = 0; s < kStages; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(tfull(i), 1); ptx::mbar_init(tempty(i), 2 * kVtEpiWarps); }
+    for (int i = 0; i < kVtRing; ++i) { ptx::mbar_init(sfull(i), 1); ptx::mbar_init(sempty(i), 2 * kVtEpiWarps + 5); }
+    abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) ptx::tmem_alloc_pair(ptx::smem_u32(&tmem_slot), 512);
+  __syncthreads();
+  ptx::cluster_arrive_release();
+  ptx::cluster_wait_acquire();
+  ptx::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  if (warp == 1) ptx::tmem_relinquish_pair();
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  volatile int* ab = &abort_flag;
+
+  // The next task from the ring, for a whole warp; kind < 0 at the end or when a wait gave up.  Whoever gets it may read
+  // what the task depends on: the scheduler saw it done (acquire) before it sent the task, and it is read where it was
+  // made visible, in L2 (TMA behind a proxy fence, ld.cg).
+  auto next_task = [&](int n) -> VTask {
+    const int r = n % kVtRing;
+    VTask k;
+    k.kind = -1; k.g = k.ti = k.tj = k.n = k.p = k.seq = k.live = 0;
+    if (!ptx::warp_wait(sfull(r), (uint32_t)((n / kVtRing) & 1), ab, status, VT_ERR_RING)) return k;
+    const uint4 w = ld_shared_v4(ptx::smem_u32(&ring[2 * r])), x = ld_shared_v4(ptx::smem_u32(&ring[2 * r + 1]));
+    auto all = [&](uint32_t v) { return (int)__shfl_sync(0xffffffffu, v, 0); };
+    k.kind = all(w.x); k.g = all(w.y); k.ti = all(w.z); k.tj = all(w.w);
+    k.n = all(x.x); k.p = all(x.y); k.seq = all(x.z); k.live = all(x.w);
+    return k;
+  };
+  auto free_task = [&](int n) { ptx::mbar_arrive_cluster(ptx::cluster_map(sempty(n % kVtRing), 0)); };
+
+  // The load and product roles are walked by whole warps with one elected lane that issues, so that descriptors and addresses stay
+  // in uniform registers.
+  if (warp < 4) {
+    if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
+      const bool second = warp == 3, issue = ptx::elect_one();
+      uint32_t s = 0, phase = 1;                           // (a fresh barrier passes a wait for the phase before its first)
+      for (int n = 0;; ++n) {
+        const VTask k = next_task(n);
+        if (k.kind < 0) break;
+        if (issue) { free_task(n); ptx::fence_proxy_async_all(); }
+        int kb;
+        const int k0 = vt_blocks(a, k, kb), tiles = k.kind == VT_STATS ? k.n : 1, blocks = tiles * kb * kPasses, ask = max(0, blocks - kVtAhead);
+        const int wg = a.w_shared ? 0 : k.g, slot = GRAD ? k.seq % a.slots : 0;
+        const bool of_w = second ? k.kind != VT_DW : false, of_g = !second && k.kind >= VT_DH;
+        const bool mn = GRAD && (k.kind == VT_DW || (second && k.kind == VT_DH));
+        const int z = of_w ? wg : of_g ? slot : k.g;
+        const bool swap = of_w && a.w_swap;
+        if (issue && blocks == 0 && rank == 0 && !second) ptx::mbar_arrive(loaded);
+        bool ok = true;
+        for (int j = 0, b = 0; j < tiles && ok; ++j) {
+          // first row (column) of this CTA's half of the operand, first of the contraction
+          int at0 = (second ? k.tj + j : k.ti) * 256 + (int)rank * 128, q0 = 0;
+          if (GRAD && of_w) {
+            if (k.kind == VT_G) at0 += k.p * a.piece;
+            else q0 = k.p * a.piece;
+          }
+          for (int p = 0; p < kPasses && ok; ++p) {
+            const int plane = SPLIT && p == (second ? 1 : 0) ? 1 : 0;      // lo hi, hi lo, hi hi: the small ones first
+            const CUtensorMap* map = of_w ? (mn ? &maps.wm[plane] : &maps.wk[plane]) : of_g ? (mn ? &maps.gm[plane] : &maps.gk[plane])
+                                          : (mn ? &maps.hm[plane] : &maps.hk[plane]);
+            for (int q = k0; q < k0 + kb; ++q, ++b) {
+              if (!ptx::warp_wait(empty((int)s), phase, ab, status, VT_ERR_EMPTY)) { ok = false; break; }
+              if (issue) {
+                if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kVtStageBytes);
+                const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kVtStageBytes + (second ? 16384u : 0u);
+                if (mn) {
+                  const int y = q0 + q * 64;
+                  ptx::tma_load_3d_pair(at, map, fb, at0, swap ? z : y, swap ? y : z);
+                  ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, swap ? z : y, swap ? y : z);
+                } else {
+                  ptx::tma_load_3d_pair(at, map, fb, q * 64, swap ? z : at0, swap ? at0 : z);
+                }
+                if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
+              }
+              __syncwarp();
+              if (++s == kStages) { s = 0; phase ^= 1u; }
+            }
+          }
+        }
+        if (!ok) break;
+      }
+    } else if (warp == 1 && rank == 0) {                   // ---- products (the leader issues for the pair) --------------
+      const bool issue = ptx::elect_one();
+      const uint32_t format = a.bf16 ? (1u << 7) | (1u << 10) : 0u;
+      uint32_t s = 0, phase = 0, sums = 0;
+      for (int n = 0;; ++n) {
+        const VTask k = next_task(n);
+        if (k.kind < 0) break;
+        if (issue) free_task(n);
+        int kb;
+        (void)vt_blocks(a, k, kb);
+        const int blocks = kb * kPasses, tiles = blocks > 0 ? (k.kind == VT_STATS ? k.n : 1) : 0;
+        const bool a_mn = GRAD && k.kind == VT_DW, b_mn = GRAD && k.kind >= VT_DH;
+        const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn) | format;
+        // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
+        const uint64_t da_k = a_mn ? 128u : 2u, db_k = b_mn ? 128u : 2u;
+        const uint64_t da0 = a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u);
+        const uint64_t db0 = b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u);
+        bool ok = true;
+        for (int j = 0; j < tiles && ok; ++j, ++sums) {
+          const uint32_t acc = sums & 1u;
+          if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, VT_ERR_ACC_FREE)) { ok = false; break; }
+          ptx::tc_fence_after();
+          for (int q = 0; q < blocks; ++q) {
+            if (!ptx::warp_wait(full((int)s), phase, ab, status, VT_ERR_FULL)) { ok = false; break; }
+            ptx::tc_fence_after();
+            if (issue) {
+              const uint64_t at = s * (kVtStageBytes >> 4);
+#pragma unroll
+              for (uint32_t h = 0; h < 4; ++h)
+                ptx::mma_f16_pair(tmem + acc * 256u, da0 + at + h * da_k, db0 + at + h * db_k, idesc, q != 0 || h != 0 ? 1u : 0u);
+              ptx::mma_commit_pair(empty((int)s));
+              if (q + 1 == blocks) ptx::mma_commit_pair(tfull((int)acc));
+            }
+            __syncwarp();
+            if (++s == kStages) { s = 0; phase ^= 1u; }
+          }
+        }
+        if (!ok) break;
+      }
+    } else if (warp == 2 && lane == 0 && rank == 0) {      // ---- claims tasks for the pair --------------------------------
+      VWalk w;
+      w.phase = 0; w.phases = GRAD ? a.groups * a.pieces + a.lag : a.groups;
+      w.base = 0; w.live_g = w.live_u = 0;
+      vt_enter<GRAD>(a, w);
+      int ready_g = -1, ready_u = -1;                      // pieces seen to be done
+      for (int n = 0;; ++n) {
+        const int r = n % kVtRing;
+        // Not before the last loads of the task before are being issued: a task claimed sooner would only keep those that
+        // depend on it waiting.
+        if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, VT_ERR_RING_FREE)) break;
+        if (n >= kVtRing && !ptx::mbar_wait(sempty(r), (uint32_t)(((n / kVtRing) - 1) & 1), ab, status, VT_ERR_RING_FREE)) break;
+        VTask k;
+        k.kind = -1; k.g = k.ti = k.tj = k.n = k.p = k.seq = k.live = 0;
+        const long long t = (long long)atomicAdd(a.claim, 1u);
+        VTask got;
+        if (vt_decode<GRAD>(a, w, t, got)) k = got;
+        if (GRAD && k.kind >= 0) {
+          // what it waits for: tiles of G; the uses of the piece whose place it takes; for dH, the piece before of the same group
+          int wait_g = -1, wait_u = -1;
+          if (k.kind == VT_G) wait_u = k.seq - a.slots;
+          else wait_g = k.seq;
+          if (k.kind == VT_DH && k.p > 0) wait_u = k.seq - 1;
+          if (wait_g > ready_g) {
+            const unsigned int need = vt_need_g(vt_piece(a, wait_g, k.live));
+            if (need > 0 && !ptx::flag_wait(a.done_g + wait_g, need, ab, status, VT_ERR_DEP)) break;
+            ready_g = wait_g;
+          }
+          if (wait_u >= 0 && wait_u != ready_u) {
+            const unsigned int need = vt_need_u(a, vt_piece(a, wait_u, a.live[wait_u / a.pieces]));
+            if (need > 0 && !ptx::flag_wait(a.done_u + wait_u, need, ab, status, VT_ERR_DEP)) break;
+            ready_u = wait_u;
+          }
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < 2; ++c)
+          ptx::send_2v4(ptx::cluster_map(ptx::smem_u32(&ring[2 * r]), c), ptx::cluster_map(sfull(r), c),
+                        make_uint4((uint32_t)k.kind, (uint32_t)k.g, (uint32_t)k.ti, (uint32_t)k.tj),
+                        make_uint4((uint32_t)k.n, (uint32_t)k.p, (uint32_t)k.seq, (uint32_t)k.live));
+        if (k.kind < 0) break;
+      }
+    }
+  } else {                                               // ---- epilogue ---------------------------------------------
+    const int quarter = warp & 3, share = (warp - 4) >> 2;
+    const uint32_t box_hi = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes, box_lo = box_hi + 4096u;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kVtWarpCols);
+    uint32_t sums = 0;
+    for (int n = 0;; ++n) {
+      const VTask k = next_task(n);
+      if (k.kind < 0) break;
+      if (lane == 0) free_task(n);
+      const VocabScale* sc = a.scale + k.g;
+      const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32;
+      bool ok = true;
+      auto release = [&](uint32_t acc) {                 // the sum has been read: the next product may overwrite it
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
+      };
+      if constexpr (!GRAD) {
+        const int row = r0 + lane;
+        const int y = row < k.live ? a.rowy[(int64_t)k.g * a.Tp + row] : -1;
+        float m = -INFINITY, sum = 0.f, zs1 = 1.f, zs2 = 1.f;
+        if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
+        for (int j = 0; j < k.n; ++j, ++sums) {
+          const uint32_t acc = sums & 1u;
+          ok = ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const int64_t c_warp = (int64_t)(k.tj + j) * 256 + share * kVtWarpCols;
+#pragma unroll 1
+          for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
+            const int64_t c0 = c_warp + ch * 32;
+            if (c0 >= a.V) break;
+            uint32_t raw[32];
+            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
+            ptx::tmem_ld_wait();
+            float z[32];
+            const int cols = (int)min((int64_t)32, a.V - c0);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) z[i] = SPLIT ? __uint_as_float(raw[i]) * zs1 * zs2 : __uint_as_float(raw[i]);
+            if (cols < 32) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) z[i] = i < cols ? z[i] : -INFINITY;
+            }
+            const int64_t mine = y - c0;
+            if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
+              float at = 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) at = mine == i ? z[i] : at;
+              if (y >= 0 && mine >= 0 && mine < 32) a.zy[(int64_t)k.g * a.Tp + row] = at;
+            }
+            float most[4] = {m, z[1], z[2], z[3]};
+            most[0] = fmaxf(m, z[0]);
+#pragma unroll
+            for (int i = 4; i < 32; ++i) most[i & 3] = fmaxf(most[i & 3], z[i]);
+            const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            float part[4] = {sum * vt_exp2((m - top) * kLog2e), 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 32; ++i) part[i & 3] += vt_exp2((z[i] - top) * kLog2e);
+            sum = (part[0] + part[1]) + (part[2] + part[3]);
+            m = top;
+          }
+          release(acc);
+        }
+        if (!ok) break;
+        if (row < k.live) a.part[((int64_t)k.g * a.runs * 2 + k.p * 2 + share) * a.Tp + row] = make_float2(m, sum);
+      } else {
+        int kb;
+        (void)vt_blocks(a, k, kb);
+        const uint32_t acc = sums & 1u;
+        if (kb > 0) {
+          ok = ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC);
+          ++sums;
+          if (!ok) break;
+          ptx::tc_fence_after();
+        }
+        if (k.kind == VT_G) {
+          const int row = r0 + lane;
+          const bool on = row < k.live;
+          const int64_t at = (int64_t)k.g * a.Tp + row;
+          const float4 rp = on ? a.rowp[at] : make_float4(0.f, 0.f, 0.f, 0.f);
+          const int y = on ? a.rowy[at] : -1;
+          float zs1 = 1.f, zs2 = 1.f;
+          if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
+          const float both = rp.z * sc->g, hot = rp.w * sc->g;
+          const int64_t v0 = (int64_t)k.p * a.piece;
+          const int c_warp = k.tj * 256 + share * kVtWarpCols, slot = k.seq % a.slots;
+          // the rows a product reads: up to the next multiple of 64, zeros behind the last live one
+          VOut d;
+          d.type = PRSGD_TYPE_FP16; d.row = a.gp; d.index = nullptr; d.add = 0; d.vec = 1; d.cols = a.gp;
+          d.rows = min(32, (k.live + 63) / 64 * 64 - r0);
+#pragma unroll 1
+          for (int u = 0; u < kVtWarpCols / 64; ++u) {
+            const int cu = c_warp + u * 64;
+            if (cu >= a.gp || d.rows <= 0) break;
+            __syncwarp();
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              const int64_t c0 = v0 + cu + h * 32;
+              uint32_t raw[32];
+              ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 64 + h * 32), raw);
+              ptx::tmem_ld_wait();
+              float v[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float z = SPLIT ? __uint_as_float(raw[i]) * zs1 * zs2 : __uint_as_float(raw[i]);
+                v[i] = both * vt_exp2(((z - rp.x) - rp.y) * kLog2e);
+              }
+              const int64_t mine = y - c0;
+              if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] -= y >= 0 && mine == i ? hot : 0.f;
+              }
+              const int cols = on ? (int)min((int64_t)32, a.V - c0) : 0;
+              if (cols < 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : 0.f;
+              }
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = vt_pack(SPLIT ? 0 : a.bf16, v[8 * q + 2 * i], v[8 * q + 2 * i + 1]);
+                st_shared_v4(vt_chunk(box_hi, lane, h * 4 + q), w[0], w[1], w[2], w[3]);
+                if constexpr (SPLIT) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const float2 f = unpack_half2(w[i]);
+                    w[i] = pack_half2(v[8 * q + 2 * i] - f.x, v[8 * q + 2 * i + 1] - f.y);
+                  }
+                  st_shared_v4(vt_chunk(box_lo, lane, h * 4 + q), w[0], w[1], w[2], w[3]);
+                }
+              }
+            }
+            __syncwarp();
+            const int64_t o = ((int64_t)slot * a.Tp + r0) * a.gp;
+            d.out = a.G[0] + o;
+            vt_out64(d, box_hi, lane, cu);
+            if constexpr (SPLIT) {
+              d.out = a.G[1] + o;
+              vt_out64(d, box_lo, lane, cu);
+            }
+          }
+        } else {
+          const bool of_w = k.kind == VT_DW;
+          const float s1 = of_w ? sc->dw1 : sc->dh1, s2 = of_w ? sc->dw2 : sc->dh2;
+          VOut d;
+          d.cols = a.D; d.index = nullptr;
+          if (of_w) {
+            const int64_t v0 = (int64_t)k.p * a.piece;
+            d.rows = (int)max((int64_t)-1, min((int64_t)32, min((int64_t)a.piece, a.V - v0) - r0));
+            d.type = a.dw_type; d.row = a.dw_row; d.add = a.accumulate; d.vec = a.vec_dw;
+            const int64_t o = (int64_t)k.g * a.dw_group + (v0 + r0) * a.dw_row;
+            d.out = static_cast<char*>(a.dW) + o * (a.dw_type == PRSGD_TYPE_FP32 ? 4 : 2);
+          } else {
+            d.rows = min(32, k.live - r0);
+            if (a.acc == nullptr) {
+              d.type = a.dh_type; d.row = a.dh_row; d.add = 0; d.vec = a.vec_dh;
+              d.index = a.index + (int64_t)k.g * a.Tp + r0;
+              d.out = static_cast<char*>(a.dH) + (int64_t)k.g * a.dh_group * (a.dh_type == PRSGD_TYPE_FP32 ? 4 : 2);
+            } else {
+              d.type = PRSGD_TYPE_FP32; d.row = a.acc_pitch; d.add = k.p > 0; d.vec = 1;
+              d.out = a.acc + (((int64_t)k.g * a.parts + k.n) * a.Tp + r0) * a.acc_pitch;
+            }
+          }
+          const bool narrow = d.type != PRSGD_TYPE_FP32 && !d.add && d.vec;
+          const int c_warp = k.tj * 256 + share * kVtWarpCols;
+          const bool skip = d.rows <= 0 || (kb == 0 && d.add);
+#pragma unroll 1
+          for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
+            const int c0 = c_warp + ch * 32;
+            if (c0 >= a.D || skip) break;
+            float v[32];
+            if (kb > 0) {
+              uint32_t raw[32];
+              ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]) * s1 * s2;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            }
+            if (!narrow) {
+              vt_out32(d, box_hi, lane, c0, v);
+              continue;
+            }
+            if ((ch & 1) == 0) __syncwarp();
+            const int bf = d.type == PRSGD_TYPE_BF16;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              st_shared_v4(vt_chunk(box_hi, lane, (ch & 1) * 4 + q), vt_pack(bf, v[8 * q], v[8 * q + 1]), vt_pack(bf, v[8 * q + 2], v[8 * q + 3]),
+                           vt_pack(bf, v[8 * q + 4], v[8 * q + 5]), vt_pack(bf, v[8 * q + 6], v[8 * q + 7]));
+            if ((ch & 1) == 1 || c0 + 32 >= a.D) {
+              __syncwarp();
+              vt_out64(d, box_hi, lane, c0 - (ch & 1) * 32);
+            }
+          }
+        }
+        if (kb > 0) release(acc);
+        __syncwarp();
+        if (lane == 0) {                                 // count the task, everything the warp wrote before it
+          asm volatile("fence.acq_rel.gpu;" ::: "memory");
+          ptx::red_add((k.kind == VT_G ? a.done_g : a.done_u) + k.seq, 1u);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (abort_flag) {                                      // copies and products may still be in flight: let them land
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) { }
+  }
+  ptx::tc_fence_before();
+  ptx::cluster_arrive_release();
+  ptx::cluster_wait_acquire();
+  if (warp == 1) ptx::tmem_dealloc_pair(tmem, 512);
+}
+
+}  // namespace prsgd

@@ -1,5 +1,6 @@
 // C entries of the cross entropy over a vocabulary.  See include/prsgd.h for the contract.
-#include "kernels_vocab.cuh"
+#include <mutex>
+#include "kernels_vocab_tc.cuh"
 
 using namespace prsgd;
 
@@ -13,23 +14,161 @@ int check_vocab(int type, int64_t groups, int64_t tokens, int64_t vocab, int dim
   return PRSGD_OK;
 }
 
-VocabArgs vocab_carve(int64_t groups, int64_t tokens, int64_t vocab, int dim, bool grad, unsigned char* base, size_t* bytes) {
-  VocabArgs a{};
-  a.T = tokens; a.V = vocab; a.D = dim;
-  a.runs = (int)((vocab + kVocabRun * kVocabTile - 1) / (kVocabRun * kVocabTile));
-  a.piece = std::min<int64_t>(vocab, 8192);
+constexpr int kPairs = 74;                     // CTA pairs of the GPU (148 SMs)
+
+// How a call is cut up and what its workspace holds.
+struct VocabPlan {
+  VocabPrep prep{};
+  VocabChain chain{};
+  bool grad = false, split = false, copy_w = false;
+  size_t bytes = 0;
+};
+
+int64_t up(int64_t x, int64_t by) { return (x + by - 1) / by; }
+
+VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool w_aligned, bool grad, unsigned char* base) {
+  VocabPlan p;
+  p.grad = grad; p.split = type == PRSGD_TYPE_FP32; p.copy_w = p.split || !w_aligned;
+  const int planes = p.split ? 2 : 1;
+  VocabPrep& a = p.prep;
+  VocabChain& c = p.chain;
+  a.groups = groups; a.T = T; a.V = V; a.D = D; a.grad = grad; a.h_type = type;
+  a.Tp = round_up(std::max<int64_t>(T, 1), 64); a.pitch = (int)round_up(D, 8);
+  a.w_groups = (int)groups;
+  const int64_t tm = up(a.Tp, 256), nv = up(V, 256), td = up(D, 256);
+  c.groups = (int)groups; c.D = D; c.T = T; c.V = V; c.Tp = a.Tp; c.bf16 = type == PRSGD_TYPE_BF16;
   size_t off = 0;
-  auto take = [&](size_t n) { unsigned char* p = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return p; };
-  a.status = reinterpret_cast<DeviceStatus*>(take(sizeof(DeviceStatus)));
-  if (grad) {
-    a.G = reinterpret_cast<float*>(take(4 * (size_t)groups * tokens * a.piece));
-    a.acc = reinterpret_cast<float*>(take(4 * (size_t)groups * tokens * dim));
-  } else {
-    a.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * tokens * a.runs));
-    a.zy = reinterpret_cast<float*>(take(4 * (size_t)groups * tokens));
+  auto take = [&](size_t n) { unsigned char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
+  a.status = c.status = reinterpret_cast<DeviceStatus*>(take(sizeof(DeviceStatus)));
+  c.live = a.live = reinterpret_cast<int*>(take(4 * (size_t)groups));
+  c.scale = a.scale = reinterpret_cast<VocabScale*>(take(sizeof(VocabScale) * (size_t)groups));
+  a.amax = reinterpret_cast<float*>(take(p.split ? (size_t)groups * 2 * kVocabAmaxBlocks * 4 : 0));
+  c.rowy = a.rowy = reinterpret_cast<int*>(take(4 * (size_t)groups * a.Tp));
+  c.index = a.index = reinterpret_cast<int*>(take(4 * (size_t)groups * a.Tp));
+  for (int i = 0; i < planes; ++i) {
+    a.Hc[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
+    a.Wc[i] = reinterpret_cast<uint16_t*>(take(p.copy_w ? 2 * (size_t)groups * V * a.pitch : 0));
   }
-  *bytes = off;
-  return a;
+  if (!grad) {
+    // A run: tiles along the vocabulary whose maxima and sums one task keeps in registers; longer ones leave fewer parts behind, as long
+    // as every pair gets eight.
+    c.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * tm * nv / (8 * kPairs)));
+    c.runs = (int)up(nv, c.run);
+    c.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * 2 * c.runs * a.Tp));
+    c.zy = reinterpret_cast<float*>(take(4 * (size_t)groups * a.Tp));
+    a.n_counters = 1;
+    a.counters = c.claim = reinterpret_cast<unsigned int*>(take(4));
+    p.bytes = off;
+    return p;
+  }
+  c.rowp = a.rowp = reinterpret_cast<float4*>(take(16 * (size_t)groups * a.Tp));
+  // A piece of G takes about 32 MB, so that the one that is written and the one that is read stay in L2 beside the operands.
+  const int64_t fit = (32ll << 20) / (a.Tp * 2 * planes) / 256 * 256;
+  c.piece = (int)std::min<int64_t>(nv * 256, std::max<int64_t>(512, fit));
+  c.pieces = (int)up(V, c.piece);
+  c.piece = (int)(up(nv, c.pieces) * 256);     // (equal ones)
+  c.pieces = (int)up(V, c.piece);
+  c.gp = (int)round_up(std::min<int64_t>(c.piece, V), 64);
+  const int64_t npv = c.piece / 256, seqs = groups * c.pieces;
+  // Parts of dH's contraction: of 4096 columns or fewer, and more while there are not two tiles a pair, but of 1024 or more.
+  const int64_t few = up(2 * kPairs, tm * td);
+  c.parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(c.piece / 4096, std::min<int64_t>(few, c.piece / 1024)), 32));
+  // Uses of a piece follow its tiles of G by as many pieces as hold two tasks a pair; a piece's place is taken again as many later.
+  const int64_t tasks = tm * npv + npv * td + tm * td * c.parts;
+  c.lag = (int)std::max<int64_t>(1, std::min<int64_t>(seqs, up(2 * kPairs, tasks)));
+  c.slots = (int)std::min<int64_t>(seqs, 2 * c.lag + 1);
+  for (int i = 0; i < planes; ++i) c.G[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)c.slots * a.Tp * c.gp));
+  c.acc_pitch = (int)round_up(D, 8);
+  c.acc = reinterpret_cast<float*>(take(c.pieces * c.parts > 1 ? 4 * (size_t)groups * c.parts * a.Tp * c.acc_pitch : 0));
+  if (c.pieces * c.parts == 1) c.acc = nullptr;
+  a.n_counters = (int)(1 + 2 * seqs);
+  a.counters = c.claim = reinterpret_cast<unsigned int*>(take(4 * (size_t)a.n_counters));
+  c.done_g = c.claim + 1; c.done_u = c.done_g + seqs;
+  p.bytes = off;
+  return p;
+}
+
+// 16-bit values, box {64, box_y, box_z}, 128-byte swizzle; zeros beyond the edges
+int vt_map(CUtensorMap* m, const void* base, int64_t dx, int64_t dy, int64_t dz, int64_t sy, int64_t sz, int box_y, int box_z) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode enc = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<Encode>(f) : nullptr;
+  }();
+  if (!enc) return op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const cuuint64_t dims[3] = {(cuuint64_t)dx, (cuuint64_t)dy, (cuuint64_t)dz}, strides[2] = {(cuuint64_t)sy * 2, (cuuint64_t)sz * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_y, (cuuint32_t)box_z}, one[3] = {1, 1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? PRSGD_OK : op_fail(PRSGD_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
+}
+
+// SMs of the current device; the kernels' shared memory is raised on the first call on it.
+int vocab_device(int* sms) {
+  static std::mutex lock;
+  static int known[64];
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev < 0 || dev >= 64)) return op_fail(PRSGD_ERR_ARG, "device ordinal out of range");
+  std::lock_guard<std::mutex> hold(lock);
+  if (e == cudaSuccess && known[dev] == 0) {
+    int n = 0;
+    e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    auto raise = [&](auto kernel, bool grad) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)vt_smem(grad)); };
+    raise(vocab_chain_kernel<false, false>, false); raise(vocab_chain_kernel<false, true>, false);
+    raise(vocab_chain_kernel<true, false>, true); raise(vocab_chain_kernel<true, true>, true);
+    if (e == cudaSuccess) known[dev] = n;
+  }
+  if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("vocab_loss: ") + cudaGetErrorString(e));
+  *sms = known[dev];
+  return PRSGD_OK;
+}
+
+// The passes before the products, and the products.
+int vocab_run(VocabPlan& p, cudaStream_t st) {
+  int sms = 0;
+  int rc = vocab_device(&sms);
+  if (rc != PRSGD_OK) return rc;
+  VocabPrep& a = p.prep;
+  VocabChain& c = p.chain;
+  const int planes = p.split ? 2 : 1, D = a.D;
+  const int64_t G = a.groups;
+  c.w_shared = a.w_groups == 1;
+  VocabMaps maps{};
+  for (int i = 0; i < planes && rc == PRSGD_OK; ++i) {
+    rc = vt_map(&maps.hk[i], a.Hc[i], D, a.Tp, G, a.pitch, a.Tp * a.pitch, 128, 1);
+    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], a.Hc[i], D, a.Tp, G, a.pitch, a.Tp * a.pitch, 64, 1);
+    const void* w = p.copy_w ? a.Wc[i] : a.W;
+    const int64_t row = p.copy_w ? a.pitch : a.w_row, group = a.w_groups == 1 ? row : p.copy_w ? a.V * a.pitch : a.w_group;
+    c.w_swap = a.w_groups > 1 && group < row;
+    for (int mn = 0; mn < (p.grad ? 2 : 1) && rc == PRSGD_OK; ++mn) {
+      CUtensorMap* to = mn ? &maps.wm[i] : &maps.wk[i];
+      const int box = mn ? 64 : 128;
+      rc = c.w_swap ? vt_map(to, w, D, a.w_groups, a.V, group, row, 1, box) : vt_map(to, w, D, a.V, a.w_groups, row, group, box, 1);
+    }
+    if (!p.grad) continue;
+    if (rc == PRSGD_OK) rc = vt_map(&maps.gk[i], c.G[i], c.gp, a.Tp, c.slots, c.gp, a.Tp * c.gp, 128, 1);
+    if (rc == PRSGD_OK) rc = vt_map(&maps.gm[i], c.G[i], c.gp, a.Tp, c.slots, c.gp, a.Tp * c.gp, 64, 1);
+  }
+  if (rc != PRSGD_OK) return rc;
+  // eight rows a block and turn, two rounds of blocks over all groups
+  const int64_t most = std::max<int64_t>(1, 148 * 8 / G);
+  a.h_blocks = (int)std::min<int64_t>(up(a.T, 8), most);
+  a.w_blocks = p.copy_w ? (int)std::min<int64_t>(up(a.V, 8), most) : 0;
+  if (p.split) launch_pdl(vocab_amax_kernel, dim3(2 * kVocabAmaxBlocks, (unsigned)G), dim3(256), 0, st, a);
+  with_type(a.h_type, [&](auto ty) { launch_pdl(vocab_prep_kernel<decltype(ty)::value>, dim3((unsigned)(a.h_blocks + a.w_blocks), (unsigned)G), dim3(256), 0, st, a); });
+  const int64_t tm = up(a.T, 256), td = up(D, 256);
+  const int64_t tasks = p.grad ? G * c.pieces * (tm * (c.piece / 256) + (c.piece / 256) * td + tm * td * c.parts) : G * tm * c.runs;
+  const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, tasks));
+  auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kVtThreads), vt_smem(p.grad), st, 2, maps, c); };
+  if (p.grad && p.split) go(vocab_chain_kernel<true, true>);
+  else if (p.grad) go(vocab_chain_kernel<true, false>);
+  else if (p.split) go(vocab_chain_kernel<false, true>);
+  else go(vocab_chain_kernel<false, false>);
+  return PRSGD_OK;
 }
 
 int check_inputs(const void* H, int64_t hr, int64_t hg, const void* W, int64_t wr, int64_t wg, int type, const int32_t* labels, int64_t G, int64_t T, int64_t V, int D) {
@@ -38,6 +177,19 @@ int check_inputs(const void* H, int64_t hr, int64_t hg, const void* W, int64_t w
   if (rc != PRSGD_OK) return rc;
   if (labels == nullptr) return op_fail(PRSGD_ERR_ARG, "labels is NULL");
   return PRSGD_OK;
+}
+
+int check_work(const void* work, size_t bytes, size_t need) {
+  if (!work || bytes < need) return op_fail(PRSGD_ERR_SIZE, "workspace is NULL or smaller than its *_workspace_bytes function says");
+  if (((uintptr_t)work) % 256) return op_fail(PRSGD_ERR_ALIGN, "d_work must be 256-byte aligned");
+  return PRSGD_OK;
+}
+
+void set_inputs(VocabPrep& a, const void* H, int64_t hr, int64_t hg, const void* W, int64_t wr, int64_t wg, int type, const int32_t* labels) {
+  a.H = H; a.h_row = hr; a.h_group = hg; a.vec_h = rows_16(H, type, hr, hg);
+  a.W = W; a.w_row = wr; a.w_group = wg; a.vec_w = rows_16(W, type, wr, wg);
+  if (wg == 0) a.w_groups = 1;
+  a.labels = labels;
 }
 
 int check_floats(const void* a, const void* b, const void* c, const void* d) {
@@ -53,14 +205,14 @@ extern "C" {
 int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes) {
   if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
   const int rc = check_vocab(type, groups, tokens, vocab, dim);
-  if (rc == PRSGD_OK) vocab_carve(groups, tokens, vocab, dim, false, nullptr, bytes);
+  if (rc == PRSGD_OK) *bytes = vocab_plan(type, groups, tokens, vocab, dim, w_aligned != 0, false, nullptr).bytes;
   return rc;
 }
 
 int prsgd_vocab_loss_grad_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes) {
   if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
   const int rc = check_vocab(type, groups, tokens, vocab, dim);
-  if (rc == PRSGD_OK) vocab_carve(groups, tokens, vocab, dim, true, nullptr, bytes);
+  if (rc == PRSGD_OK) *bytes = vocab_plan(type, groups, tokens, vocab, dim, w_aligned != 0, true, nullptr).bytes;
   return rc;
 }
 
@@ -75,16 +227,19 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
   if (rc == PRSGD_OK) rc = check_floats(d_labels, d_loss, d_stats, nullptr);
   if (rc != PRSGD_OK) return rc;
   if (!d_loss || !d_stats) return op_fail(PRSGD_ERR_ARG, "an output is NULL");
-  size_t need = 0;
-  VocabArgs a = vocab_carve(groups, tokens, vocab, dim, false, static_cast<unsigned char*>(d_work), &need);
-  if (!d_work || work_bytes < need) return op_fail(PRSGD_ERR_SIZE, "workspace is NULL or smaller than prsgd_vocab_loss_workspace_bytes");
-  if (((uintptr_t)d_work) % 256) return op_fail(PRSGD_ERR_ALIGN, "d_work must be 256-byte aligned");
-  a.H = d_H; a.h_row = h_row_stride; a.h_group = h_group_stride; a.W = d_W; a.w_row = w_row_stride; a.w_group = w_group_stride;
-  a.labels = d_labels; a.loss = d_loss; a.stats = d_stats;
+  VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), false, static_cast<unsigned char*>(d_work));
+  rc = check_work(d_work, work_bytes, p.bytes);
+  if (rc != PRSGD_OK) return rc;
+  VocabPrep& a = p.prep;
+  set_inputs(a, d_H, h_row_stride, h_group_stride, d_W, w_row_stride, w_group_stride, type, d_labels);
+  a.loss = d_loss; a.out_stats = d_stats;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const dim3 grid((unsigned)((tokens + kVocabTile - 1) / kVocabTile), (unsigned)a.runs, (unsigned)groups);
-  with_type(type, [&](auto ty) { launch_pdl(vocab_stats_kernel<decltype(ty)::value>, grid, dim3(256), 0, st, a); });
-  launch_pdl(vocab_join_kernel, dim3((unsigned)((tokens + 255) / 256), (unsigned)groups), dim3(256), 0, st, a);
+  rc = vocab_run(p, st);
+  if (rc != PRSGD_OK) return rc;
+  VocabJoin j{};
+  j.part = p.chain.part; j.zy = p.chain.zy; j.index = a.index; j.live = a.live; j.Tp = a.Tp; j.T = tokens; j.runs = 2 * p.chain.runs;
+  j.loss = d_loss; j.stats = d_stats;
+  launch_pdl(vocab_join_kernel, dim3((unsigned)up(tokens, 32), (unsigned)groups), dim3(256), 0, st, j);
   return op_launched("vocab_loss");
 }
 
@@ -109,30 +264,39 @@ int prsgd_vocab_loss_grad(const void* d_H, int64_t h_row_stride, int64_t h_group
       rc = op_fail(PRSGD_ERR_ARG, "dH or dW is another array's memory");
   }
   if (rc != PRSGD_OK) return rc;
-  size_t need = 0;
-  VocabArgs a = vocab_carve(groups, tokens, vocab, dim, true, static_cast<unsigned char*>(d_work), &need);
-  if (!d_work || work_bytes < need) return op_fail(PRSGD_ERR_SIZE, "workspace is NULL or smaller than prsgd_vocab_loss_grad_workspace_bytes");
-  if (((uintptr_t)d_work) % 256) return op_fail(PRSGD_ERR_ALIGN, "d_work must be 256-byte aligned");
-  a.H = d_H; a.h_row = h_row_stride; a.h_group = h_group_stride; a.W = d_W; a.w_row = w_row_stride; a.w_group = w_group_stride;
-  a.labels = d_labels; a.in_stats = d_stats; a.dloss = d_dloss; a.dlse = d_dlse;
-  a.dH = d_dH; a.dh_row = dh_row_stride; a.dh_group = dh_group_stride;
-  a.dW = d_dW; a.dw_row = dw_row_stride; a.dw_group = dw_group_stride; a.accumulate = accumulate != 0;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  rc = op_clear_status(d_work, work_bytes, cuda_stream);
+  if (tokens == 0) {                                     // no term in any sum
+    const size_t size = (size_t)type_bytes(dw_type);
+    cudaError_t e = cudaSuccess;
+    for (int64_t g = 0; g < groups && e == cudaSuccess; ++g)
+      e = cudaMemset2DAsync(static_cast<char*>(d_dW) + g * dw_group_stride * size, dw_row_stride * size, 0, dim * size, vocab, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("vocab_loss_grad: ") + cudaGetErrorString(e));
+    return op_clear_status(d_work, work_bytes, cuda_stream);
+  }
+  if (!d_dH && !d_dW) return op_clear_status(d_work, work_bytes, cuda_stream);
+  VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), true, static_cast<unsigned char*>(d_work));
+  rc = check_work(d_work, work_bytes, p.bytes);
   if (rc != PRSGD_OK) return rc;
-  const unsigned tt = (unsigned)((tokens + kVocabTile - 1) / kVocabTile), dt = (unsigned)((dim + kVocabTile - 1) / kVocabTile), G = (unsigned)groups;
-  with_type(type, [&](auto ty) {
-    constexpr int TY = decltype(ty)::value;
-    for (a.v0 = 0; a.v0 < vocab; a.v0 += a.piece) {
-      a.pv = std::min(a.piece, vocab - a.v0);
-      const unsigned vt = (unsigned)((a.pv + kVocabTile - 1) / kVocabTile);
-      if (tt > 0) launch_pdl(vocab_g_kernel<TY>, dim3(tt, vt, G), dim3(256), 0, st, a);
-      if (d_dH && tt > 0) launch_pdl(vocab_dh_kernel<TY>, dim3(tt, dt, G), dim3(256), 0, st, a);
-      if (!d_dW) continue;
-      if (dw_type == TY) launch_pdl(vocab_dw_kernel<TY, TY>, dim3(vt, dt, G), dim3(256), 0, st, a);
-      else launch_pdl(vocab_dw_kernel<TY, PRSGD_TYPE_FP32>, dim3(vt, dt, G), dim3(256), 0, st, a);
-    }
-  });
+  VocabPrep& a = p.prep;
+  VocabChain& c = p.chain;
+  set_inputs(a, d_H, h_row_stride, h_group_stride, d_W, w_row_stride, w_group_stride, type, d_labels);
+  a.stats = d_stats; a.dloss = d_dloss; a.dlse = d_dlse;
+  a.dH = d_dH; a.dh_row = dh_row_stride; a.dh_group = dh_group_stride; a.vec_dh = d_dH && rows_16(d_dH, type, dh_row_stride, dh_group_stride);
+  c.dH = d_dH; c.dh_row = dh_row_stride; c.dh_group = dh_group_stride; c.dh_type = type; c.vec_dh = a.vec_dh;
+  c.dW = d_dW; c.dw_row = dw_row_stride; c.dw_group = dw_group_stride; c.dw_type = dw_type; c.accumulate = accumulate != 0;
+  c.vec_dw = d_dW && rows_16(d_dW, dw_type, dw_row_stride, dw_group_stride);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  rc = vocab_run(p, st);
+  if (rc != PRSGD_OK) return rc;
+  if (d_dH && c.acc) {
+    VocabSum s{};
+    s.acc = c.acc; s.index = a.index; s.live = a.live; s.Tp = a.Tp; s.groups = groups; s.parts = c.parts; s.acc_pitch = c.acc_pitch; s.D = dim;
+    s.dH = d_dH; s.dh_row = dh_row_stride; s.dh_group = dh_group_stride;
+    const dim3 grid((unsigned)std::min<int64_t>(up(tokens, 8), 65536), (unsigned)up(dim, 256), (unsigned)groups);
+    with_type(type, [&](auto ty) {
+      if (a.vec_dh) launch_pdl(vocab_sum_kernel<decltype(ty)::value, true>, grid, dim3(256), 0, st, s);
+      else launch_pdl(vocab_sum_kernel<decltype(ty)::value, false>, grid, dim3(256), 0, st, s);
+    });
+  }
   return op_launched("vocab_loss_grad");
 }
 
