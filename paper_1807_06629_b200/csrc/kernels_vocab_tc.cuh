@@ -25,6 +25,10 @@ constexpr int kVtWarpCols = 128;               // an epilogue warp takes 32 rows
 constexpr uint32_t kVtStageBytes = 32768, kVtWarpBytes = 8192;
 __host__ __device__ constexpr int vt_stages(bool grad) { return grad ? 5 : 6; }            // (the gradient's epilogue needs shared memory too)
 constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kVtStageBytes + (grad ? kVtEpiWarps * kVtWarpBytes : 0); }
+// A tensor core cuts off what the running sum does not hold, 2^-24 of it a step of 16 on average and always towards zero: what has to be
+// exact to fp32 is summed in TMEM over this many blocks of 64 only, and those sums are added in registers, where they are rounded (stats at
+// 16384 x 131072 x 2048: off by 1.9e-6 with one sum, by 4.3e-7 with sums of 512 products, for 2 to 5 % of the time).
+__host__ __device__ constexpr int vt_promote(bool split) { return split ? 4 : 8; }
 constexpr int kVtAhead = 8;                    // the next task is claimed when this many blocks of 64 of the current one are left to load
 enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE };
 enum { VT_STATS = 0, VT_G, VT_DH, VT_DW };
@@ -79,6 +83,13 @@ __device__ __forceinline__ int vt_blocks(const VocabChain& a, const VTask& k, in
   const int first = (int)((int64_t)nb * k.n / a.parts);
   n = (int)((int64_t)nb * (k.n + 1) / a.parts) - first;
   return first;
+}
+
+// Sums of a tile: one, or (PROMOTE) one of the small products of pairs and one per vt_promote blocks.
+template <bool SPLIT, bool PROMOTE>
+__device__ __forceinline__ int vt_sums(int kb) {
+  if (!PROMOTE) return 1;
+  return (SPLIT ? 1 : 0) + (kb + vt_promote(SPLIT) - 1) / vt_promote(SPLIT);
 }
 
 // The list of tasks, walked in order by the thread that claims them.
@@ -200,8 +211,16 @@ struct VOut {
   const int* index;                            // rows through index, or one after another
   int rows, cols;                              // rows of this warp's 32 that exist; columns of the array
   int add, vec;                                // added to what is there; rows begin on 16-byte boundaries
+  int reduce;                                  // the adding is left to L2 (fp32 rows on 16-byte boundaries whose pitch is a multiple of 4)
   __device__ __forceinline__ int64_t at(int r) const { return (index ? (int64_t)index[r] : (int64_t)r) * row; }
 };
+
+// Adds four floats to memory in L2.  (A sum read, added to and written back by the SM waits for its old values: about 1 us four times
+// a tile, as long as the products of a tile of dH.)
+__device__ __forceinline__ void vt_red4(float* p, uint4 v) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+               ::"l"(p), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
+}
 
 // 32 rows x 32 columns (from column c0) of fp32 values, a row per lane, to where they go, through `box`: a lane writes four columns.
 __device__ __forceinline__ void vt_out32(const VOut& d, uint32_t box, int lane, int c0, const float (&v)[32]) {
@@ -211,6 +230,16 @@ __device__ __forceinline__ void vt_out32(const VOut& d, uint32_t box, int lane, 
     st_shared_v4(vt_chunk(box, lane, q), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
   __syncwarp();
   const int c = c0 + (lane & 7) * 4;
+  if (d.reduce) {
+    if (c >= d.cols) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + (lane >> 3);
+      const uint4 u = ld_shared_v4(vt_chunk(box, r, lane & 7));
+      if (r < d.rows) vt_red4(static_cast<float*>(d.out) + (int64_t)r * d.row + c, u);
+    }
+    return;
+  }
   const bool whole = d.vec && c + 4 <= d.cols;
 #pragma unroll 1
   for (int i = 0; i < 8; i += 4) {
@@ -271,7 +300,8 @@ __device__ __forceinline__ void vt_out64(const VOut& d, uint32_t box, int lane, 
 // SPLIT: fp32 operands, products of fp16 pairs.
 template <bool GRAD, bool SPLIT>
 __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
-  constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1;
+  constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1, kPromote = vt_promote(SPLIT);
+  constexpr bool PROMOTE = SPLIT || !GRAD;               // (gradients of 16-bit types are rounded by far more)
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kVtRing + 1];
@@ -326,8 +356,9 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
   auto free_task = [&](int n) { ptx::mbar_arrive_cluster(ptx::cluster_map(sempty(n % kVtRing), 0)); };
 
   // The load and product roles are walked by whole warps with one elected lane that issues, so that descriptors and addresses stay
-  // in uniform registers.
+  // in uniform registers.  Sums in registers take them from the other warps: 128 * 64 + 256 * 216 of the launch's 384 * 168.
   if (warp < 4) {
+    if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
       const bool second = warp == 3, issue = ptx::elect_one();
       uint32_t s = 0, phase = 1;                           // (a fresh barrier passes a wait for the phase before its first)
@@ -394,20 +425,27 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         const uint64_t da0 = a_mn ? ptx::smem_desc_sw128(stage0, 8192u, 1024u) : ptx::smem_desc_sw128(stage0, 16u, 1024u);
         const uint64_t db0 = b_mn ? ptx::smem_desc_sw128(stage0 + 16384u, 8192u, 1024u) : ptx::smem_desc_sw128(stage0 + 16384u, 16u, 1024u);
         bool ok = true;
-        for (int j = 0; j < tiles && ok; ++j, ++sums) {
-          const uint32_t acc = sums & 1u;
-          if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, VT_ERR_ACC_FREE)) { ok = false; break; }
-          ptx::tc_fence_after();
+        for (int j = 0; j < tiles && ok; ++j) {
+          int next = 0;                                    // block that starts a new sum
+          uint32_t acc = 0;
           for (int q = 0; q < blocks; ++q) {
+            const bool first = q == next;
+            if (first) {
+              next = !PROMOTE ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + kPromote);
+              acc = sums & 1u;
+              if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, VT_ERR_ACC_FREE)) { ok = false; break; }
+              ptx::tc_fence_after();
+              ++sums;
+            }
             if (!ptx::warp_wait(full((int)s), phase, ab, status, VT_ERR_FULL)) { ok = false; break; }
             ptx::tc_fence_after();
             if (issue) {
               const uint64_t at = s * (kVtStageBytes >> 4);
 #pragma unroll
               for (uint32_t h = 0; h < 4; ++h)
-                ptx::mma_f16_pair(tmem + acc * 256u, da0 + at + h * da_k, db0 + at + h * db_k, idesc, q != 0 || h != 0 ? 1u : 0u);
+                ptx::mma_f16_pair(tmem + acc * 256u, da0 + at + h * da_k, db0 + at + h * db_k, idesc, !first || h != 0 ? 1u : 0u);
               ptx::mma_commit_pair(empty((int)s));
-              if (q + 1 == blocks) ptx::mma_commit_pair(tfull((int)acc));
+              if (q + 1 == next) ptx::mma_commit_pair(tfull((int)acc));
             }
             __syncwarp();
             if (++s == kStages) { s = 0; phase ^= 1u; }
@@ -458,6 +496,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
       }
     }
   } else {                                               // ---- epilogue ---------------------------------------------
+    if constexpr (PROMOTE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int quarter = warp & 3, share = (warp - 4) >> 2;
     const uint32_t box_hi = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes, box_lo = box_hi + 4096u;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kVtWarpCols);
@@ -474,16 +513,50 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
       };
+      int kb;
+      (void)vt_blocks(a, k, kb);
+      const int parts = vt_sums<SPLIT, PROMOTE>(kb);
+      // Waits for a tile's sum; several are added in registers and the total goes back to TMEM, over the last of them, so that what
+      // follows is a loop of few instructions.
+      auto gather = [&](uint32_t& acc) -> bool {
+        if (!PROMOTE || parts == 1) {
+          acc = sums & 1u;
+          if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
+          ++sums;
+          ptx::tc_fence_after();
+          return true;
+        }
+        float total[kVtWarpCols / 32][32];
+#pragma unroll
+        for (int i = 0; i < kVtWarpCols; ++i) total[i >> 5][i & 31] = 0.f;
+        for (int p = 0; p < parts; ++p, ++sums) {
+          acc = sums & 1u;
+          if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
+          ptx::tc_fence_after();
+#pragma unroll
+          for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
+            uint32_t raw[32];
+            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) total[ch][i] += __uint_as_float(raw[i]);
+          }
+          if (p + 1 < parts) release(acc);
+        }
+#pragma unroll
+        for (int ch = 0; ch < kVtWarpCols / 32; ++ch) ptx::tmem_st32(lanes + acc * 256u + (uint32_t)(ch * 32), total[ch]);
+        ptx::tmem_st_wait();
+        return true;
+      };
       if constexpr (!GRAD) {
         const int row = r0 + lane;
         const int y = row < k.live ? a.rowy[(int64_t)k.g * a.Tp + row] : -1;
         float m = -INFINITY, sum = 0.f, zs1 = 1.f, zs2 = 1.f;
         if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
-        for (int j = 0; j < k.n; ++j, ++sums) {
-          const uint32_t acc = sums & 1u;
-          ok = ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC);
+        for (int j = 0; j < k.n; ++j) {
+          uint32_t acc;
+          ok = gather(acc);
           if (!ok) break;
-          ptx::tc_fence_after();
           const int64_t c_warp = (int64_t)(k.tj + j) * 256 + share * kVtWarpCols;
 #pragma unroll 1
           for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
@@ -523,15 +596,9 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         if (!ok) break;
         if (row < k.live) a.part[((int64_t)k.g * a.runs * 2 + k.p * 2 + share) * a.Tp + row] = make_float2(m, sum);
       } else {
-        int kb;
-        (void)vt_blocks(a, k, kb);
-        const uint32_t acc = sums & 1u;
-        if (kb > 0) {
-          ok = ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC);
-          ++sums;
-          if (!ok) break;
-          ptx::tc_fence_after();
-        }
+        uint32_t acc = 0;
+        if (kb > 0) ok = gather(acc);
+        if (!ok) break;
         if (k.kind == VT_G) {
           const int row = r0 + lane;
           const bool on = row < k.live;
@@ -603,7 +670,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           const bool of_w = k.kind == VT_DW;
           const float s1 = of_w ? sc->dw1 : sc->dh1, s2 = of_w ? sc->dw2 : sc->dh2;
           VOut d;
-          d.cols = a.D; d.index = nullptr;
+          d.cols = a.D; d.index = nullptr; d.reduce = 0;
           if (of_w) {
             const int64_t v0 = (int64_t)k.p * a.piece;
             d.rows = (int)max((int64_t)-1, min((int64_t)32, min((int64_t)a.piece, a.V - v0) - r0));
@@ -617,7 +684,8 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
               d.index = a.index + (int64_t)k.g * a.Tp + r0;
               d.out = static_cast<char*>(a.dH) + (int64_t)k.g * a.dh_group * (a.dh_type == PRSGD_TYPE_FP32 ? 4 : 2);
             } else {
-              d.type = PRSGD_TYPE_FP32; d.row = a.acc_pitch; d.add = k.p > 0; d.vec = 1;
+              d.type = PRSGD_TYPE_FP32; d.row = a.acc_pitch; d.add = d.reduce = k.p > 0; d.vec = 1;
+              d.cols = a.acc_pitch;
               d.out = a.acc + (((int64_t)k.g * a.parts + k.n) * a.Tp + r0) * a.acc_pitch;
             }
           }

@@ -62,8 +62,8 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
     return p;
   }
   c.rowp = a.rowp = reinterpret_cast<float4*>(take(16 * (size_t)groups * a.Tp));
-  // A piece of G takes about 32 MB, so that the one that is written and the one that is read stay in L2 beside the operands.
-  const int64_t fit = (32ll << 20) / (a.Tp * 2 * planes) / 256 * 256;
+  // A piece of G takes about 64 MB (8192 x 65536 x 2048: 16 MB 5.85 ms, 32 5.34, 64 5.04, 128 and 256 5.05: dH is added to once a piece).
+  const int64_t fit = (64ll << 20) / (a.Tp * 2 * planes) / 256 * 256;
   c.piece = (int)std::min<int64_t>(nv * 256, std::max<int64_t>(512, fit));
   c.pieces = (int)up(V, c.piece);
   c.piece = (int)(up(nv, c.pieces) * 256);     // (equal ones)
