@@ -24,7 +24,12 @@ struct DropoutArgs {
   const int64_t* d_step;
 };
 
-template <int TY, bool VEC, bool RES>
+__device__ __forceinline__ Words4 dropout_words(const DropoutArgs& a, const RowPiece& at, uint32_t step) {
+  return philox4x32_10({at.chunk, (uint32_t)at.row, a.group0 + blockIdx.y, step}, a.seed);
+}
+
+// Rows that begin on 16-byte boundaries and end on multiples of eight columns.
+template <int TY, bool RES>
 __global__ void __launch_bounds__(kRowThreads) dropout_kernel(const DropoutArgs a) {
   using T = typename ElemOf<TY>::type;
   op_pdl_wait();
@@ -34,34 +39,74 @@ __global__ void __launch_bounds__(kRowThreads) dropout_kernel(const DropoutArgs 
   const T* res = RES ? static_cast<const T*>(a.res) + g * a.res_group : nullptr;
   T* out = static_cast<T*>(a.out) + g * a.out_group;
   const uint32_t step = a.step + (a.d_step ? (uint32_t)*a.d_step : 0u);
-  const int64_t first = (int64_t)blockIdx.x * kRowItems;
-  const RowStart s = row_start(a.walk, first);
-  int64_t row[kRowUnroll];
-  uint32_t chunk[kRowUnroll];
-  float v[kRowUnroll][8], r[kRowUnroll][8];
+  const RowStart s = row_start(a.walk, (int64_t)blockIdx.x * kRowItems);
+  RowPiece at[kRowUnroll];
+  Raw8<TY> v[kRowUnroll], r[kRowUnroll];
 #pragma unroll
   for (int u = 0; u < kRowUnroll; ++u) {
-    const uint32_t i = s.chunk + u * kRowThreads + threadIdx.x, over = a.walk.by_chunks.div(i);
-    row[u] = s.row + over;
-    chunk[u] = i - over * a.walk.chunks;
-    if (row[u] >= a.walk.rows) continue;
-    const int n = (int)min((int64_t)8, a.walk.cols - (int64_t)chunk[u] * 8);
-    load8<TY, VEC>(x + row[u] * a.x_row + (int64_t)chunk[u] * 8, n, v[u]);
-    if (RES) load8<TY, VEC>(res + row[u] * a.res_row + (int64_t)chunk[u] * 8, n, r[u]);
+    at[u] = row_piece(a.walk, s, u * kRowThreads + threadIdx.x);
+    if (at[u].row >= a.walk.rows) continue;
+    v[u] = load_raw<TY>(x + at[u].row * a.x_row + (int64_t)at[u].chunk * 8);
+    if (RES) r[u] = load_raw<TY>(res + at[u].row * a.res_row + (int64_t)at[u].chunk * 8);
   }
 #pragma unroll
   for (int u = 0; u < kRowUnroll; ++u) {
-    if (row[u] >= a.walk.rows) break;
-    const int n = (int)min((int64_t)8, a.walk.cols - (int64_t)chunk[u] * 8);
-    const Words4 w = philox4x32_10({chunk[u], (uint32_t)row[u], a.group0 + (uint32_t)g, step}, a.seed);
+    if (at[u].row >= a.walk.rows) break;
+    const Words4 w = dropout_words(a, at[u], step);
     const uint32_t bits[4] = {w.x, w.y, w.z, w.w};
+    float y[8], more[8];
+    unpack8<TY>(v[u], y);
+    if (RES) unpack8<TY>(r[u], more);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t b = i & 1 ? bits[i >> 1] >> 16 : bits[i >> 1] & 0xFFFFu;
-      const float kept = b >= a.threshold ? v[u][i] * a.scale : 0.f;
-      v[u][i] = RES ? kept + r[u][i] : kept;
+      const float kept = b >= a.threshold ? y[i] * a.scale : 0.f;
+      y[i] = RES ? kept + more[i] : kept;
     }
-    store8<TY, VEC>(out + row[u] * a.out_row + (int64_t)chunk[u] * 8, n, v[u]);
+    store_raw<TY>(out + at[u].row * a.out_row + (int64_t)at[u].chunk * 8, y);
+  }
+}
+
+// Any rows: the lanes of a warp draw for 32 pieces, then take neighbouring columns, whose bits they find in shared memory.
+template <int TY, bool RES>
+__global__ void __launch_bounds__(kRowThreads) dropout_any_kernel(const DropoutArgs a) {
+  using T = typename ElemOf<TY>::type;
+  __shared__ uint4 drawn[kRowThreads];
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.y;
+  const T* x = static_cast<const T*>(a.x) + g * a.x_group;
+  const T* res = RES ? static_cast<const T*>(a.res) + g * a.res_group : nullptr;
+  T* out = static_cast<T*>(a.out) + g * a.out_group;
+  const uint32_t step = a.step + (a.d_step ? (uint32_t)*a.d_step : 0u);
+  const RowStart s = row_start(a.walk, (int64_t)blockIdx.x * kRowItems);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint16_t* bits = reinterpret_cast<const uint16_t*>(drawn + warp * 32);
+#pragma unroll 1
+  for (int u = 0; u < kRowUnroll; ++u) {
+    const uint32_t first = u * kRowThreads + warp * 32;
+    T v[8], r[8];
+    int64_t row[8];
+    uint32_t col[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const RowPiece p = row_piece(a.walk, s, first + j * 4 + (lane >> 3));
+      row[j] = p.row;
+      col[j] = p.chunk * 8 + (lane & 7);
+      if (p.row >= a.walk.rows || col[j] >= a.walk.cols) { row[j] = -1; continue; }
+      v[j] = x[p.row * a.x_row + col[j]];
+      if (RES) r[j] = res[p.row * a.res_row + col[j]];
+    }
+    const Words4 w = dropout_words(a, row_piece(a.walk, s, first + lane), step);
+    __syncwarp();
+    drawn[threadIdx.x] = make_uint4(w.x, w.y, w.z, w.w);
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (row[j] < 0) continue;
+      const float kept = bits[j * 32 + lane] >= a.threshold ? to_f32(v[j]) * a.scale : 0.f;
+      out[row[j] * a.out_row + col[j]] = from_f32<T>(RES ? kept + to_f32(r[j]) : kept);
+    }
   }
 }
 
@@ -105,16 +150,16 @@ int prsgd_dropout(const void* d_x, int32_t type, int64_t row_stride, int64_t gro
   a.seed = seed; a.step = (uint32_t)step; a.group0 = (uint32_t)first_group; a.d_step = d_step;
   const int64_t blocks = (a.walk.items + kRowItems - 1) / kRowItems;
   if (blocks > 0x7fffffffll) return op_fail(PRSGD_ERR_SIZE, "more than 2^44 elements in a group");
-  const bool vec = rows_16(d_x, type, row_stride, group_stride) && rows_16(d_out, type, out_row_stride, out_group_stride) &&
-                   (!d_residual || rows_16(d_residual, type, residual_row_stride, residual_group_stride));
+  const bool whole = cols % 8 == 0 && rows_16(d_x, type, row_stride, group_stride) && rows_16(d_out, type, out_row_stride, out_group_stride) &&
+                     (!d_residual || rows_16(d_residual, type, residual_row_stride, residual_group_stride));
   const dim3 grid((unsigned)blocks, (unsigned)groups);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   with_type(type, [&](auto ty) {
     constexpr int TY = decltype(ty)::value;
-    if (vec && d_residual) launch_pdl(dropout_kernel<TY, true, true>, grid, dim3(kRowThreads), 0, st, a);
-    else if (vec) launch_pdl(dropout_kernel<TY, true, false>, grid, dim3(kRowThreads), 0, st, a);
-    else if (d_residual) launch_pdl(dropout_kernel<TY, false, true>, grid, dim3(kRowThreads), 0, st, a);
-    else launch_pdl(dropout_kernel<TY, false, false>, grid, dim3(kRowThreads), 0, st, a);
+    if (whole && d_residual) launch_pdl(dropout_kernel<TY, true>, grid, dim3(kRowThreads), 0, st, a);
+    else if (whole) launch_pdl(dropout_kernel<TY, false>, grid, dim3(kRowThreads), 0, st, a);
+    else if (d_residual) launch_pdl(dropout_any_kernel<TY, true>, grid, dim3(kRowThreads), 0, st, a);
+    else launch_pdl(dropout_any_kernel<TY, false>, grid, dim3(kRowThreads), 0, st, a);
   });
   return op_launched("dropout");
 }

@@ -18,9 +18,11 @@ int check_tokens(const int32_t* ids, int64_t groups, int64_t tokens, int64_t voc
   return PRSGD_OK;
 }
 
-// Sorted tokens of a unit: enough units to fill the GPU several times over, but of 32 tokens or more, so that the parts left
-// for the last launch stay a small share of what is read.
-int embed_unit(int64_t tokens) { return (int)std::max<int64_t>(32, std::min<int64_t>(256, tokens / 4096)); }
+// Sorted tokens of a unit: such that two threads' worth of units and columns falls on each place of the GPU, 8 at least, 256 at most.
+int embed_unit(int64_t groups, int64_t tokens, int chunks) {
+  const int64_t fit = groups * tokens * chunks / (148 * 2048);
+  return (int)std::max<int64_t>(8, std::min<int64_t>(256, fit / 8 * 8));
+}
 
 EmbedGradArgs embed_grad_carve(int64_t groups, int64_t tokens, int64_t vocab, int dim, unsigned char* base, size_t* bytes) {
   EmbedGradArgs a{};
@@ -30,7 +32,7 @@ EmbedGradArgs embed_grad_carve(int64_t groups, int64_t tokens, int64_t vocab, in
   int bits = 1;
   while ((1ll << bits) < vocab) ++bits;
   a.passes = (bits + kSortBits - 1) / kSortBits;
-  a.unit = embed_unit(tokens);
+  a.unit = embed_unit(groups, tokens, a.chunks);
   a.units = (int)((tokens + a.unit - 1) / a.unit);
   size_t off = 0;
   auto take = [&](size_t n) { unsigned char* p = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return p; };
@@ -51,7 +53,7 @@ int embed_prepare() {
   if (e == cudaSuccess && (dev < 0 || dev >= 64)) return op_fail(PRSGD_ERR_ARG, "device ordinal out of range");
   std::lock_guard<std::mutex> hold(lock);
   if (e == cudaSuccess && !known[dev]) {
-    auto raise = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSortSmem); };
+    auto raise = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(kSortShared)); };
     raise(embed_sort_kernel<PRSGD_TYPE_FP32, true>); raise(embed_sort_kernel<PRSGD_TYPE_BF16, true>); raise(embed_sort_kernel<PRSGD_TYPE_FP16, true>);
     raise(embed_sort_kernel<PRSGD_TYPE_FP32, false>); raise(embed_sort_kernel<PRSGD_TYPE_BF16, false>); raise(embed_sort_kernel<PRSGD_TYPE_FP16, false>);
     known[dev] = e == cudaSuccess;
@@ -82,11 +84,11 @@ int prsgd_embed(const void* d_table, int32_t type, int64_t row_stride, int64_t g
   a.tokens = tokens; a.vocab = vocab; a.scale = scale;
   const dim3 grid((unsigned)((a.walk.items + kRowItems - 1) / kRowItems), (unsigned)groups);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool vec = rows_16(d_table, type, row_stride, group_stride) && rows_16(d_out, out_type, out_row_stride, out_group_stride);
+  const bool whole = dim % 8 == 0 && rows_16(d_table, type, row_stride, group_stride) && rows_16(d_out, out_type, out_row_stride, out_group_stride);
   with_type(type, [&](auto ty) {
     with_type(out_type, [&](auto oty) {
-      if (vec) launch_pdl(embed_kernel<decltype(ty)::value, decltype(oty)::value, true>, grid, dim3(kRowThreads), 0, st, a);
-      else launch_pdl(embed_kernel<decltype(ty)::value, decltype(oty)::value, false>, grid, dim3(kRowThreads), 0, st, a);
+      if (whole) launch_pdl(embed_kernel<decltype(ty)::value, decltype(oty)::value>, grid, dim3(kRowThreads), 0, st, a);
+      else launch_pdl(embed_any_kernel<decltype(ty)::value, decltype(oty)::value>, grid, dim3(kRowThreads), 0, st, a);
     });
   });
   return op_launched("embed");
@@ -131,15 +133,18 @@ int prsgd_embed_grad(const void* d_dout, int32_t type, int64_t row_stride, int64
     constexpr int OTY = decltype(oty)::value;
     auto both = [&](auto ov) {
       constexpr bool OV = decltype(ov)::value;
-      launch_pdl(embed_sort_kernel<OTY, OV>, dim3((unsigned)(groups + zeros)), dim3(1024), kSortSmem, st, a);
+      launch_pdl(embed_sort_kernel<OTY, OV>, dim3((unsigned)(groups + zeros)), dim3(1024), sort_smem(tokens), st, a);
       if (tokens == 0) return;
-      const int per = kRowThreads / a.lanes;
+      // threads of a block: whole rows of lanes, fewer of them while that gives the GPU more blocks
+      int threads = kRowThreads;
+      while (threads > 64 && threads / 2 >= a.lanes && groups * a.units * a.lanes / threads < 148 * 4) threads /= 2;
+      const int per = threads / a.lanes;
       const dim3 grid((unsigned)((a.units + per - 1) / per), (unsigned)((a.chunks + a.lanes - 1) / a.lanes), (unsigned)groups);
       with_type(type, [&](auto ty) {
-        if (vec) launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, true, OV>, grid, dim3(kRowThreads), 0, st, a);
-        else launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, false, OV>, grid, dim3(kRowThreads), 0, st, a);
+        if (vec) launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, true, OV>, grid, dim3(threads), 0, st, a);
+        else launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, false, OV>, grid, dim3(threads), 0, st, a);
       });
-      if (a.units > 1) launch_pdl(embed_join_kernel<OTY, OV>, grid, dim3(kRowThreads), 0, st, a);
+      if (a.units > 1) launch_pdl(embed_join_kernel<OTY, OV>, grid, dim3(threads), 0, st, a);
     };
     if (ovec) both(std::integral_constant<bool, true>());
     else both(std::integral_constant<bool, false>());

@@ -19,7 +19,8 @@ struct EmbedArgs {
   float scale;
 };
 
-template <int TY, int OTY, bool VEC>
+// Rows that begin on 16-byte boundaries and end on multiples of eight columns.
+template <int TY, int OTY>
 __global__ void __launch_bounds__(kRowThreads) embed_kernel(const EmbedArgs a) {
   using T = typename ElemOf<TY>::type;
   using O = typename ElemOf<OTY>::type;
@@ -30,36 +31,67 @@ __global__ void __launch_bounds__(kRowThreads) embed_kernel(const EmbedArgs a) {
   O* out = static_cast<O*>(a.out) + g * a.out_group;
   const int32_t* ids = a.ids + g * a.tokens;
   const RowStart s = row_start(a.walk, (int64_t)blockIdx.x * kRowItems);
-  int64_t row[kRowUnroll];
-  uint32_t chunk[kRowUnroll];
+  RowPiece at[kRowUnroll];
   int id[kRowUnroll];
-  float v[kRowUnroll][8];
+  Raw8<TY> v[kRowUnroll];
 #pragma unroll
   for (int u = 0; u < kRowUnroll; ++u) {
-    const uint32_t i = s.chunk + u * kRowThreads + threadIdx.x, over = a.walk.by_chunks.div(i);
-    row[u] = s.row + over;
-    chunk[u] = i - over * a.walk.chunks;
-    id[u] = row[u] < a.walk.rows ? ids[row[u]] : -1;
+    at[u] = row_piece(a.walk, s, u * kRowThreads + threadIdx.x);
+    id[u] = at[u].row < a.walk.rows ? ids[at[u].row] : -1;
   }
 #pragma unroll
+  for (int u = 0; u < kRowUnroll; ++u)
+    v[u] = id[u] >= 0 && id[u] < a.vocab ? load_raw<TY>(table + id[u] * a.row + (int64_t)at[u].chunk * 8) : zero_raw<TY>();
+#pragma unroll
   for (int u = 0; u < kRowUnroll; ++u) {
-    const int n = (int)min((int64_t)8, a.walk.cols - (int64_t)chunk[u] * 8);
-    const bool some = id[u] >= 0 && id[u] < a.vocab;
-    load8<TY, VEC>(table + (some ? id[u] : 0) * a.row + (int64_t)chunk[u] * 8, some ? n : 0, v[u]);
+    if (at[u].row >= a.walk.rows) break;
+    float y[8];
+    unpack8<TY>(v[u], y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] *= a.scale;
+    store_raw<OTY>(out + at[u].row * a.out_row + (int64_t)at[u].chunk * 8, y);
   }
-#pragma unroll
+}
+
+// Any rows: the lanes of a warp take neighbouring columns of its 32 pieces.
+template <int TY, int OTY>
+__global__ void __launch_bounds__(kRowThreads) embed_any_kernel(const EmbedArgs a) {
+  using T = typename ElemOf<TY>::type;
+  using O = typename ElemOf<OTY>::type;
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.y;
+  const T* table = static_cast<const T*>(a.table) + g * a.group;
+  O* out = static_cast<O*>(a.out) + g * a.out_group;
+  const int32_t* ids = a.ids + g * a.tokens;
+  const RowStart s = row_start(a.walk, (int64_t)blockIdx.x * kRowItems);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
   for (int u = 0; u < kRowUnroll; ++u) {
-    if (row[u] >= a.walk.rows) break;
-    const int n = (int)min((int64_t)8, a.walk.cols - (int64_t)chunk[u] * 8);
+    int64_t row[8];
+    uint32_t col[8];
+    int id[8];
+    T v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[u][i] *= a.scale;
-    store8<OTY, VEC>(out + row[u] * a.out_row + (int64_t)chunk[u] * 8, n, v[u]);
+    for (int j = 0; j < 8; ++j) {
+      const RowPiece p = row_piece(a.walk, s, u * kRowThreads + warp * 32 + j * 4 + (lane >> 3));
+      col[j] = p.chunk * 8 + (lane & 7);
+      row[j] = p.row < a.walk.rows && col[j] < a.walk.cols ? p.row : -1;
+      id[j] = row[j] >= 0 ? ids[row[j]] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = id[j] >= 0 && id[j] < a.vocab ? table[id[j] * a.row + col[j]] : from_f32<T>(0.f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (row[j] >= 0) out[row[j] * a.out_row + col[j]] = from_f32<O>(to_f32(v[j]) * a.scale);
   }
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------
-constexpr int kSortBits = 9, kSortDigits = 1 << kSortBits, kSortWarps = 32, kSortPitch = kSortDigits + 1;
-constexpr size_t kSortSmem = (size_t)kSortWarps * kSortPitch * 4;
+constexpr int kSortBits = 9, kSortDigits = 1 << kSortBits, kSortWarps = 32, kSortPitch = kSortDigits + 1, kSortBatch = 8;
+constexpr int kSortShared = kSortWarps * 32 * kSortBatch;            // tokens that are sorted in shared memory
+constexpr size_t kSortCounts = ((size_t)kSortWarps * kSortPitch * 4 + 15) / 16 * 16;
+inline size_t sort_smem(int64_t tokens) { return kSortCounts + (tokens <= kSortShared ? 8 * (size_t)tokens : 0); }
 
 struct EmbedGradArgs {
   const void* dout; int64_t row, group;
@@ -79,30 +111,42 @@ struct EmbedGradArgs {
 };
 
 // Tokens of a group by id.  A warp takes an equal share of them, counts its digits, and places them behind those of smaller
-// digits and of earlier warps; within a warp's 32 the order is the lanes'.
+// digits and of earlier warps; within a warp's 32 the order is the lanes'.  Up to kSortShared tokens a thread keeps its own eight in
+// registers and they change places in shared memory (8192 tokens, two digits: 24 us when every step of 32 was read from memory twice a digit).
 __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) {
   __shared__ uint32_t sums[kSortWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int32_t* ids = a.ids + g * a.tokens;
   uint32_t* mine = counts + warp * kSortPitch;
-  int64_t n = a.tokens;
+  uint2* shared = reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(counts) + kSortCounts);
+  const bool in_shared = a.tokens <= kSortShared;
+  int n = (int)a.tokens;
   for (int p = 0; p < a.passes; ++p) {
-    const uint2* from = a.keys[p & 1] + g * a.tokens;
-    uint2* to = a.keys[(p + 1) & 1] + g * a.tokens;
-    const int64_t share = ((n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32, begin = warp * share, end = min(n, begin + share);
-    auto get = [&](int64_t i) -> uint2 {         // (digit out of range: none)
-      if (i >= end) return make_uint2(0xFFFFFFFFu, 0u);
-      if (p == 0) {
-        const int id = ids[i];
-        return id >= 0 && id < a.vocab ? make_uint2((uint32_t)id, (uint32_t)i) : make_uint2(0xFFFFFFFFu, 0u);
+    const bool last = p + 1 == a.passes;
+    const uint2* from = in_shared ? shared : a.keys[p & 1] + g * a.tokens;
+    uint2* to = in_shared && !last ? shared : a.keys[(p + 1) & 1] + g * a.tokens;
+    const int share = ((n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32, begin = min(n, warp * share), end = min(n, begin + share);
+    uint2 key[kSortBatch];                       // (id, token), or (-1, ) for none
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j) {
+        const int i = i0 + j * 32 + lane;
+        if (p == 0) {
+          const int id = i < end ? ids[i] : -1;
+          key[j] = id >= 0 && id < a.vocab ? make_uint2((uint32_t)id, (uint32_t)i) : make_uint2(0xFFFFFFFFu, 0u);
+        } else {
+          key[j] = i < end ? from[i] : make_uint2(0xFFFFFFFFu, 0u);
+        }
       }
-      return from[i];
     };
+    auto digit = [&](uint2 k) { return (k.x >> (p * kSortBits)) & (kSortDigits - 1); };
     for (int d = lane; d < kSortDigits; d += 32) mine[d] = 0;
     __syncwarp();
-    for (int64_t i = begin + lane; i - lane < end; i += 32) {
-      const uint2 k = get(i);
-      if (k.x != 0xFFFFFFFFu) atomicAdd(mine + ((k.x >> (p * kSortBits)) & (kSortDigits - 1)), 1u);
+    for (int i = begin; i < end; i += 32 * kSortBatch) {
+      load(i);
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j)
+        if (key[j].x != 0xFFFFFFFFu) atomicAdd(mine + digit(key[j]), 1u);
     }
     __syncthreads();
     // exclusive sums, digit by digit and within one warp by warp: a thread takes half the warps of a digit
@@ -127,7 +171,7 @@ __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) 
       }
       __syncthreads();
       run += (warp > 0 ? sums[warp - 1] : 0u) - total;
-      n = sums[kSortWarps - 1];
+      n = (int)sums[kSortWarps - 1];
       for (int w = 0; w < kSortWarps / 2; ++w) {
         uint32_t* c = counts + (w0 + w) * kSortPitch + d;
         const uint32_t here = *c;
@@ -136,21 +180,24 @@ __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) 
       }
     }
     __syncthreads();
-    for (int64_t i = begin + lane; i - lane < end; i += 32) {
-      const uint2 k = get(i);
-      const bool some = k.x != 0xFFFFFFFFu;
-      const uint32_t digit = some ? (k.x >> (p * kSortBits)) & (kSortDigits - 1) : kSortDigits;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit);
-      uint32_t at = 0;
-      if (some) at = mine[digit] + __popc(same & ((1u << lane) - 1u));
-      __syncwarp();
-      if (some && (same >> lane) == 1u) mine[digit] = at + 1u;      // (the last of its digit)
-      __syncwarp();
-      if (some) to[at] = k;
+    for (int i = begin; i < end; i += 32 * kSortBatch) {
+      if (!in_shared) load(i);                   // (else they are in registers still)
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j) {
+        const bool some = key[j].x != 0xFFFFFFFFu;
+        const uint32_t d = some ? digit(key[j]) : kSortDigits;
+        const uint32_t same = __match_any_sync(0xffffffffu, d);
+        uint32_t at = 0;
+        if (some) at = mine[d] + __popc(same & ((1u << lane) - 1u));
+        __syncwarp();
+        if (some && (same >> lane) == 1u) mine[d] = at + 1u;        // (the last of its digit)
+        __syncwarp();
+        if (some) to[at] = key[j];
+      }
     }
     __syncthreads();
   }
-  if (threadIdx.x == 0) a.live[g] = (int)n;
+  if (threadIdx.x == 0) a.live[g] = n;
 }
 
 // The first `groups` blocks sort; the others write zeros meanwhile, rows whose ids occur included (their sums follow).
@@ -176,14 +223,13 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const EmbedGradArgs a)
   }
 }
 
+// Rows of a run's sum, eight columns a thread (`n` of which exist; VEC: all, on a 16-byte boundary).
 template <int OTY, bool VEC>
-__device__ __forceinline__ void embed_write(const EmbedGradArgs& a, int64_t g, int64_t id, int c, const float (&sum)[8]) {
-  using O = typename ElemOf<OTY>::type;
-  O* to = static_cast<O*>(a.dtable) + g * a.t_group + id * a.t_row + c * 8;
-  const int n = min(8, a.dim - c * 8);
+__device__ __forceinline__ void embed_write(const EmbedGradArgs& a, typename ElemOf<OTY>::type* to, int n, const Raw8<OTY>& old, const float (&sum)[8]) {
   float v[8];
   if (a.accumulate) {
-    load8<OTY, VEC>(to, n, v);
+    if (VEC) unpack8<OTY>(old, v);
+    else load8<OTY, false>(to, n, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = fmaf(a.scale, sum[i], v[i]);
   } else {
@@ -193,77 +239,110 @@ __device__ __forceinline__ void embed_write(const EmbedGradArgs& a, int64_t g, i
   store8<OTY, VEC>(to, n, v);
 }
 
+// One unit's sums for one thread's columns.  Rows of dout, and what the sums are added to, are requested several tokens ahead.
 template <int TY, int OTY, bool VEC, bool OVEC>
-__global__ void __launch_bounds__(kRowThreads) embed_sum_kernel(const EmbedGradArgs a) {
+__device__ __forceinline__ void embed_unit_sum(const EmbedGradArgs& a, int64_t g, int u, int c, int n, int live, int begin, int end) {
   using T = typename ElemOf<TY>::type;
-  constexpr int kAhead = 8;
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int64_t g = blockIdx.z;
-  const int per = kRowThreads / a.lanes, sub = threadIdx.x / a.lanes;
-  const int u = blockIdx.x * per + sub, c = blockIdx.y * a.lanes + threadIdx.x - sub * a.lanes;
-  if (sub >= per || u >= a.units || c >= a.chunks) return;
-  const int live = a.live[g], begin = u * a.unit, end = min(live, begin + a.unit);
-  if (begin >= end) return;
+  using O = typename ElemOf<OTY>::type;
+  constexpr int kAhead = VEC ? 4 : 2;
   const uint2* keys = a.keys[a.passes & 1] + g * a.tokens;
   const T* dout = static_cast<const T*>(a.dout) + g * a.group + c * 8;
+  O* table = static_cast<O*>(a.dtable) + g * a.t_group + c * 8;
   float* parts = a.parts + ((g * a.units + u) * 2) * (int64_t)a.chunks * 8 + c * 8;
-  const int n = min(8, a.dim - c * 8);
   bool inner = begin == 0 || keys[begin - 1].x != keys[begin].x;        // the current run began in this unit
-  const bool goes_on = end < live && keys[end].x == keys[end - 1].x;    // the last run does not end in it
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  uint32_t id = keys[begin].x;
   for (int i = begin; i < end; i += kAhead) {
-    uint2 k[kAhead];
-    float v[kAhead][8];
+    uint2 k[kAhead + 1];
+    Raw8<TY> v[kAhead];
+    Raw8<OTY> old[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) k[j] = i + j < end ? keys[i + j] : make_uint2(0u, 0u);
+    for (int j = 0; j <= kAhead; ++j) k[j] = i + j < live ? keys[i + j] : make_uint2(0xFFFFFFFFu, 0u);
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) load8<TY, VEC>(dout + (int64_t)k[j].y * a.row, i + j < end ? n : 0, v[j]);
+    for (int j = 0; j < kAhead; ++j) {
+      if (VEC) v[j] = i + j < end ? load_raw<TY>(dout + (int64_t)k[j].y * a.row) : zero_raw<TY>();
+      if (OVEC && a.accumulate && i + j < end && k[j].x != k[j + 1].x) old[j] = load_raw<OTY>(table + k[j].x * a.t_row);
+    }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (i + j >= end) break;
-      if (k[j].x != id) {
-        if (inner) embed_write<OTY, OVEC>(a, g, id, c, sum);
-        else store8<PRSGD_TYPE_FP32, true>(parts, 8, sum);
-        inner = true;
-        id = k[j].x;
+      float x[8];
+      if (VEC) unpack8<TY>(v[j], x);
+      else load8<TY, false>(dout + (int64_t)k[j].y * a.row, n, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-      }
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+      if (k[j].x == k[j + 1].x) continue;                // the run goes on
+      if (inner) embed_write<OTY, OVEC>(a, table + k[j].x * a.t_row, n, old[j], sum);
+      else store_raw<PRSGD_TYPE_FP32>(parts, sum);
+      inner = true;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[j][e];
+      for (int e = 0; e < 8; ++e) sum[e] = 0.f;
     }
   }
-  if (inner && !goes_on) embed_write<OTY, OVEC>(a, g, id, c, sum);
-  else store8<PRSGD_TYPE_FP32, true>(inner ? parts + (int64_t)a.chunks * 8 : parts, 8, sum);
+  // a run that the next unit goes on with
+  if (end < live && keys[end - 1].x == keys[end].x) store_raw<PRSGD_TYPE_FP32>(inner ? parts + (int64_t)a.chunks * 8 : parts, sum);
+}
+
+template <int TY, int OTY, bool VEC, bool OVEC>
+__global__ void __launch_bounds__(kRowThreads) embed_sum_kernel(const EmbedGradArgs a) {
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.z;
+  const int per = blockDim.x / a.lanes, sub = threadIdx.x / a.lanes;
+  const int u = blockIdx.x * per + sub, c = blockIdx.y * a.lanes + threadIdx.x - sub * a.lanes;
+  if (sub >= per || u >= a.units || c >= a.chunks) return;
+  const int live = a.live[g], begin = u * a.unit, end = min(live, begin + a.unit), n = min(8, a.dim - c * 8);
+  if (begin >= end) return;
+  if (n == 8) embed_unit_sum<TY, OTY, VEC, OVEC>(a, g, u, c, n, live, begin, end);
+  else embed_unit_sum<TY, OTY, false, false>(a, g, u, c, n, live, begin, end);
 }
 
 // The runs that cross borders: the unit in which a run begins adds the parts behind it, in order.
 template <int OTY, bool OVEC>
 __global__ void __launch_bounds__(kRowThreads) embed_join_kernel(const EmbedGradArgs a) {
+  using O = typename ElemOf<OTY>::type;
+  constexpr int kAhead = 8;
   op_pdl_wait();
   op_pdl_trigger();
   const int64_t g = blockIdx.z;
-  const int per = kRowThreads / a.lanes, sub = threadIdx.x / a.lanes;
+  const int per = blockDim.x / a.lanes, sub = threadIdx.x / a.lanes;
   const int u = blockIdx.x * per + sub, c = blockIdx.y * a.lanes + threadIdx.x - sub * a.lanes;
   if (sub >= per || u >= a.units || c >= a.chunks) return;
   const int live = a.live[g], begin = u * a.unit, end = min(live, begin + a.unit);
   if (begin >= end || end >= live) return;
   const uint2* keys = a.keys[a.passes & 1] + g * a.tokens;
-  const uint32_t id = keys[end - 1].x;
-  if (keys[end].x != id) return;                                        // ends here
-  if (begin > 0 && keys[begin].x == id && keys[begin - 1].x == id) return;      // began earlier
+  const uint32_t id = keys[end - 1].x, next = keys[end].x, first = keys[begin].x, before = begin > 0 ? keys[begin - 1].x : 0xFFFFFFFFu;
+  if (next != id || (first == id && before == id)) return;              // ends here, or began earlier
   const int64_t pitch = (int64_t)a.chunks * 8;
-  const float* part = a.parts + ((g * a.units + u) * 2 + 1) * pitch + c * 8;
-  float sum[8], more[8];
-  load8<PRSGD_TYPE_FP32, true>(part, 8, sum);
-  for (int w = u + 1; (int64_t)w * a.unit < live && keys[(int64_t)w * a.unit].x == id; ++w) {
-    load8<PRSGD_TYPE_FP32, true>(a.parts + (g * a.units + w) * 2 * pitch + c * 8, 8, more);
+  const float* parts = a.parts + g * a.units * 2 * pitch + c * 8;
+  float sum[8];
+  unpack8<PRSGD_TYPE_FP32>(load_raw<PRSGD_TYPE_FP32>(parts + ((int64_t)u * 2 + 1) * pitch), sum);
+  const int n = min(8, a.dim - c * 8);
+  O* to = static_cast<O*>(a.dtable) + g * a.t_group + id * a.t_row + c * 8;
+  Raw8<OTY> old = zero_raw<OTY>();
+  if (OVEC && n == 8 && a.accumulate) old = load_raw<OTY>(to);
+  for (int w = u + 1; (int64_t)w * a.unit < live; w += kAhead) {
+    bool in[kAhead];
+    Raw8<PRSGD_TYPE_FP32> more[kAhead];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += more[e];
+    for (int j = 0; j < kAhead; ++j) {
+      const int64_t at = (int64_t)(w + j) * a.unit;
+      in[j] = at < live && keys[at].x == id;
+    }
+    if (!in[0]) break;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (in[j]) more[j] = load_raw<PRSGD_TYPE_FP32>(parts + (int64_t)(w + j) * 2 * pitch);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (!in[j]) break;
+      float x[8];
+      unpack8<PRSGD_TYPE_FP32>(more[j], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
   }
-  embed_write<OTY, OVEC>(a, g, id, c, sum);
+  if (OVEC && n == 8) embed_write<OTY, true>(a, to, n, old, sum);
+  else embed_write<OTY, false>(a, to, n, old, sum);
 }
 
 }  // namespace prsgd

@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
   }
 }
 
-// Largest logit and sum of every live token from those of its runs of the vocabulary: a block takes 32 tokens, eight lanes each.
+// Largest logit and sum of every live token from those of its runs of the vocabulary: a block takes ROWS tokens, 256 / ROWS threads each.
 struct VocabJoin {
   const float2* part;        // [groups][runs][Tp]
   const float* zy; const int* index; const int* live;
@@ -256,40 +256,44 @@ struct VocabJoin {
   int runs;
   float* loss; float* stats;
 };
+__device__ __forceinline__ float2 vocab_merge(float2 p, float2 q) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  const float m = fmaxf(p.x, q.x);
+  if (m == -INFINITY && p.y == 0.f && q.y == 0.f) return make_float2(m, 0.f);      // (runs without columns)
+  return make_float2(m, p.y * exp2f((p.x - m) * kLog2e) + q.y * exp2f((q.x - m) * kLog2e));
+}
+template <int ROWS>
 __global__ void __launch_bounds__(256) vocab_join_kernel(const VocabJoin a) {
-  __shared__ float2 got[8][32];
+  constexpr int LANES = 256 / ROWS, kAhead = 8;
+  __shared__ float2 got[LANES][ROWS];
   op_pdl_wait();
   op_pdl_trigger();
   const int64_t g = blockIdx.y;
-  const int live = a.live[g], row = blockIdx.x * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
-  if ((int)blockIdx.x * 32 >= live) return;
-  constexpr float kLog2e = 1.4426950408889634f;
-  float m = -INFINITY, s = 0.f;
+  const int live = a.live[g], r = threadIdx.x % ROWS, row = blockIdx.x * ROWS + r, share = threadIdx.x / ROWS;
+  if ((int)blockIdx.x * ROWS >= live) return;
+  float2 sum = make_float2(-INFINITY, 0.f);
   if (row < live) {
     const float2* part = a.part + g * a.runs * a.Tp + row;
-#pragma unroll 4
-    for (int r = share; r < a.runs; r += 8) {
-      const float2 p = part[(int64_t)r * a.Tp];
-      const float most = fmaxf(m, p.x);
-      if (most == -INFINITY && p.y == 0.f) continue;       // (a run without columns)
-      s = s * exp2f((m - most) * kLog2e) + p.y * exp2f((p.x - most) * kLog2e);
-      m = most;
+    for (int k = share; k < a.runs; k += LANES * kAhead) {
+      float2 p[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) p[j] = k + j * LANES < a.runs ? part[(int64_t)(k + j * LANES) * a.Tp] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) sum = vocab_merge(sum, p[j]);
     }
   }
-  got[share][threadIdx.x & 31] = make_float2(m, s);
+  got[share][r] = sum;
   __syncthreads();
-  if (share != 0 || row >= live) return;
-  for (int k = 1; k < 8; ++k) m = fmaxf(m, got[k][row & 31].x);
-  s = 0.f;
-  for (int k = 0; k < 8; ++k) {
-    const float2 p = got[k][row & 31];
-    if (p.x == -INFINITY && p.y == 0.f) continue;
-    s += p.y * exp2f((p.x - m) * kLog2e);
+  for (int n = LANES / 2; n > 0; n >>= 1) {
+    if (share < n) got[share][r] = vocab_merge(got[share][r], got[share + n][r]);
+    __syncthreads();
   }
-  const float log_sum = logf(s);
+  if (share != 0 || row >= live) return;
+  sum = got[0][r];
+  const float log_sum = logf(sum.y);
   const int64_t o = g * a.T + a.index[g * a.Tp + row];
-  a.loss[o] = log_sum + (m - a.zy[g * a.Tp + row]);
-  a.stats[2 * o] = m;
+  a.loss[o] = log_sum + (sum.x - a.zy[g * a.Tp + row]);
+  a.stats[2 * o] = sum.x;
   a.stats[2 * o + 1] = log_sum;
 }
 

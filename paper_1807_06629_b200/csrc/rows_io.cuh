@@ -44,6 +44,11 @@ inline RowWalk row_walk(int64_t rows, int64_t cols) {
 }
 // Row and first column of item `i` of the block that begins with item `first`.
 struct RowStart { int64_t row; uint32_t chunk; };
+struct RowPiece { int64_t row; uint32_t chunk; };
+__device__ __forceinline__ RowPiece row_piece(const RowWalk& w, const RowStart& s, uint32_t i) {
+  const uint32_t k = s.chunk + i, over = w.by_chunks.div(k);
+  return {s.row + over, k - over * w.chunks};
+}
 __device__ __forceinline__ RowStart row_start(const RowWalk& w, int64_t first) {
   RowStart s;
   if (first >> 32) {
@@ -62,20 +67,44 @@ inline bool rows_16(const void* p, int type, int64_t row_stride, int64_t group_s
   return (uintptr_t)p % 16 == 0 && row_stride % v == 0 && group_stride % v == 0;
 }
 
-// Eight neighbouring elements as fp32, `n` of which exist; VEC: p lies on a 16-byte boundary.
+// Eight neighbouring elements as they lie in memory, on a 16-byte boundary: loaded apart from their conversion, so that the loads of several
+// pieces are in flight together.
+template <int TY> struct Raw8 { uint4 q[TY == PRSGD_TYPE_FP32 ? 2 : 1]; };
+template <int TY>
+__device__ __forceinline__ Raw8<TY> load_raw(const typename ElemOf<TY>::type* p) {
+  Raw8<TY> r;
+  r.q[0] = reinterpret_cast<const uint4*>(p)[0];
+  if constexpr (TY == PRSGD_TYPE_FP32) r.q[1] = reinterpret_cast<const uint4*>(p)[1];
+  return r;
+}
+template <int TY>
+__device__ __forceinline__ Raw8<TY> zero_raw() {
+  Raw8<TY> r;
+  r.q[0] = make_uint4(0, 0, 0, 0);
+  if constexpr (TY == PRSGD_TYPE_FP32) r.q[1] = make_uint4(0, 0, 0, 0);
+  return r;
+}
+template <int TY>
+__device__ __forceinline__ void unpack8(const Raw8<TY>& r, float (&v)[8]) {
+  const typename ElemOf<TY>::type* h = reinterpret_cast<const typename ElemOf<TY>::type*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = to_f32(h[i]);
+}
+template <int TY>
+__device__ __forceinline__ void store_raw(typename ElemOf<TY>::type* p, const float (&v)[8]) {
+  using T = typename ElemOf<TY>::type;
+  Raw8<TY> r;
+  T* h = reinterpret_cast<T*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h[i] = from_f32<T>(v[i]);
+  reinterpret_cast<uint4*>(p)[0] = r.q[0];
+  if constexpr (TY == PRSGD_TYPE_FP32) reinterpret_cast<uint4*>(p)[1] = r.q[1];
+}
+// The same with `n` of the eight there, of which the others are not touched; VEC: p lies on a 16-byte boundary.
 template <int TY, bool VEC>
 __device__ __forceinline__ void load8(const typename ElemOf<TY>::type* p, int n, float (&v)[8]) {
-  using T = typename ElemOf<TY>::type;
   if (VEC && n >= 8) {
-    if constexpr (TY == PRSGD_TYPE_FP32) {
-      const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      const uint4 u = *reinterpret_cast<const uint4*>(p);
-      const T* h = reinterpret_cast<const T*>(&u);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = to_f32(h[i]);
-    }
+    unpack8<TY>(load_raw<TY>(p), v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
@@ -83,22 +112,12 @@ __device__ __forceinline__ void load8(const typename ElemOf<TY>::type* p, int n,
 }
 template <int TY, bool VEC>
 __device__ __forceinline__ void store8(typename ElemOf<TY>::type* p, int n, const float (&v)[8]) {
-  using T = typename ElemOf<TY>::type;
   if (VEC && n >= 8) {
-    if constexpr (TY == PRSGD_TYPE_FP32) {
-      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      uint4 u;
-      T* h = reinterpret_cast<T*>(&u);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = from_f32<T>(v[i]);
-      *reinterpret_cast<uint4*>(p) = u;
-    }
+    store_raw<TY>(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = from_f32<T>(v[i]);
+      if (i < n) p[i] = from_f32<typename ElemOf<TY>::type>(v[i]);
   }
 }
 

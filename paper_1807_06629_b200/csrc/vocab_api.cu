@@ -239,7 +239,8 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
   VocabJoin j{};
   j.part = p.chain.part; j.zy = p.chain.zy; j.index = a.index; j.live = a.live; j.Tp = a.Tp; j.T = tokens; j.runs = 2 * p.chain.runs;
   j.loss = d_loss; j.stats = d_stats;
-  launch_pdl(vocab_join_kernel, dim3((unsigned)up(tokens, 32), (unsigned)groups), dim3(256), 0, st, j);
+  if (tokens <= 8) launch_pdl(vocab_join_kernel<1>, dim3((unsigned)tokens, (unsigned)groups), dim3(256), 0, st, j);
+  else launch_pdl(vocab_join_kernel<32>, dim3((unsigned)up(tokens, 32), (unsigned)groups), dim3(256), 0, st, j);
   return op_launched("vocab_loss");
 }
 
