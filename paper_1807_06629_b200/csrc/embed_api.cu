@@ -32,6 +32,7 @@ EmbedGradArgs embed_grad_carve(int64_t groups, int64_t tokens, int64_t vocab, in
   int bits = 1;
   while ((1ll << bits) < vocab) ++bits;
   a.passes = (bits + kSortBits - 1) / kSortBits;
+  a.bits = (bits + a.passes - 1) / a.passes;
   a.unit = embed_unit(groups, tokens, a.chunks);
   a.units = (int)((tokens + a.unit - 1) / a.unit);
   size_t off = 0;

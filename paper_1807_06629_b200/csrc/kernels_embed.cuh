@@ -88,10 +88,10 @@ __global__ void __launch_bounds__(kRowThreads) embed_any_kernel(const EmbedArgs 
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------
-constexpr int kSortBits = 9, kSortDigits = 1 << kSortBits, kSortWarps = 32, kSortPitch = kSortDigits + 1, kSortBatch = 8;
-constexpr int kSortShared = kSortWarps * 32 * kSortBatch;            // tokens that are sorted in shared memory
+constexpr int kSortBits = 9, kSortWarps = 32, kSortPitch = (1 << kSortBits) + 1;
+constexpr int kSortShared = 8192;                // tokens that are sorted in shared memory
 constexpr size_t kSortCounts = ((size_t)kSortWarps * kSortPitch * 4 + 15) / 16 * 16;
-inline size_t sort_smem(int64_t tokens) { return kSortCounts + (tokens <= kSortShared ? 8 * (size_t)tokens : 0); }
+inline size_t sort_smem(int64_t tokens) { return kSortCounts + (tokens <= kSortShared ? 16 * (size_t)tokens : 0); }
 
 struct EmbedGradArgs {
   const void* dout; int64_t row, group;
@@ -101,7 +101,7 @@ struct EmbedGradArgs {
   int dim, chunks;
   float scale;
   int accumulate;
-  int passes;                                    // digits of an id
+  int passes, bits;                              // digits of an id; bits of a digit
   int unit, units;                               // sorted tokens of a unit; units of a group
   int lanes;                                     // threads side by side along a row; kRowThreads / lanes units share a block
   uint2* keys[2];                                // [groups][tokens] (id, token), sorted ones in keys[passes & 1]
@@ -111,8 +111,9 @@ struct EmbedGradArgs {
 };
 
 // Tokens of a group by id.  A warp takes an equal share of them, counts its digits, and places them behind those of smaller
-// digits and of earlier warps; within a warp's 32 the order is the lanes'.  Up to kSortShared tokens a thread keeps its own eight in
-// registers and they change places in shared memory (8192 tokens, two digits: 24 us when every step of 32 was read from memory twice a digit).
+// digits and of earlier warps; within a warp's 32 the order is the lanes'.  Counted without atomics: the many equal digits of
+// frequent ids took turns.  Up to kSortShared tokens change places in shared memory.  Its loops are rolled: code that is run through once is
+// fetched anew at every launch, at about 20 cycles an instruction.
 __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) {
   __shared__ uint32_t sums[kSortWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -120,41 +121,67 @@ __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) 
   uint32_t* mine = counts + warp * kSortPitch;
   uint2* shared = reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(counts) + kSortCounts);
   const bool in_shared = a.tokens <= kSortShared;
+  const int digits = 1 << a.bits;
+  const int turns = ((int)a.tokens + kSortWarps * 32 - 1) / (kSortWarps * 32);     // (the same for all warps and digits, and seen to be)
   int n = (int)a.tokens;
-  for (int p = 0; p < a.passes; ++p) {
-    const bool last = p + 1 == a.passes;
-    const uint2* from = in_shared ? shared : a.keys[p & 1] + g * a.tokens;
-    uint2* to = in_shared && !last ? shared : a.keys[(p + 1) & 1] + g * a.tokens;
-    const int share = ((n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32, begin = min(n, warp * share), end = min(n, begin + share);
-    uint2 key[kSortBatch];                       // (id, token), or (-1, ) for none
-    auto load = [&](int i0) {
+  {                                              // (id, token), or (-1, ) for none
+    uint2* to = in_shared ? shared : a.keys[0] + g * a.tokens;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 8192) {
+      int id[8];
 #pragma unroll
-      for (int j = 0; j < kSortBatch; ++j) {
-        const int i = i0 + j * 32 + lane;
-        if (p == 0) {
-          const int id = i < end ? ids[i] : -1;
-          key[j] = id >= 0 && id < a.vocab ? make_uint2((uint32_t)id, (uint32_t)i) : make_uint2(0xFFFFFFFFu, 0u);
-        } else {
-          key[j] = i < end ? from[i] : make_uint2(0xFFFFFFFFu, 0u);
-        }
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + j * 1024 + (int)threadIdx.x;
+        id[j] = i < n ? ids[i] : -1;
       }
-    };
-    auto digit = [&](uint2 k) { return (k.x >> (p * kSortBits)) & (kSortDigits - 1); };
-    for (int d = lane; d < kSortDigits; d += 32) mine[d] = 0;
-    __syncwarp();
-    for (int i = begin; i < end; i += 32 * kSortBatch) {
-      load(i);
 #pragma unroll
-      for (int j = 0; j < kSortBatch; ++j)
-        if (key[j].x != 0xFFFFFFFFu) atomicAdd(mine + digit(key[j]), 1u);
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + j * 1024 + (int)threadIdx.x;
+        if (i < n) to[i] = make_uint2(id[j] >= 0 && id[j] < a.vocab ? (uint32_t)id[j] : 0xFFFFFFFFu, (uint32_t)i);
+      }
+    }
+  }
+  for (int p = 0; p < a.passes; ++p) {
+    uint2* from = in_shared ? shared + (p & 1) * a.tokens : a.keys[p & 1] + g * a.tokens;
+    uint2* to = in_shared && p + 1 < a.passes ? shared + ((p + 1) & 1) * a.tokens : a.keys[(p + 1) & 1] + g * a.tokens;
+    const int begin = min(n, warp * turns * 32), end = min(n, begin + turns * 32);
+    auto digit = [&](uint2 k) { return (k.x >> (p * a.bits)) & (uint32_t)(digits - 1); };
+    for (int d = lane; d < digits; d += 32) mine[d] = 0;
+    __syncthreads();
+    auto place = [&](uint2 k) -> uint32_t {
+      const bool some = k.x != 0xFFFFFFFFu;
+      const uint32_t d = digit(k);
+      uint32_t same = __ballot_sync(0xffffffffu, some), at = 0;     // lanes of this digit, bit by bit
+#pragma unroll
+      for (int b = 0; b < kSortBits; ++b) {
+        if (b >= a.bits) break;
+        const uint32_t bit = (d >> b) & 1u, with = __ballot_sync(0xffffffffu, bit != 0u);
+        same &= with ^ (bit - 1u);
+      }
+      if (some) at = mine[d] + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (some && (same >> lane) == 1u) mine[d] = at + 1u;          // (the last of its digit)
+      __syncwarp();
+      return at;
+    };
+#pragma unroll 1
+    for (int turn = 0; turn < turns; ++turn) {
+      const int i = begin + turn * 32 + lane;
+      const uint2 k = i < end ? from[i] : make_uint2(0xFFFFFFFFu, 0u);
+      const uint32_t at = place(k);
+      if (in_shared && i < end) from[i].y = (k.y & 0xFFFFu) | at << 16;    // (below 8192 tokens, 256 of them a warp's)
     }
     __syncthreads();
     // exclusive sums, digit by digit and within one warp by warp: a thread takes half the warps of a digit
     {
       const int d = threadIdx.x >> 1, w0 = (threadIdx.x & 1) * (kSortWarps / 2);
       uint32_t total = 0;
-      for (int w = 0; w < kSortWarps / 2; ++w) total += counts[(w0 + w) * kSortPitch + d];
+      if (d < digits) {
+#pragma unroll 4
+        for (int w = 0; w < kSortWarps / 2; ++w) total += counts[(w0 + w) * kSortPitch + d];
+      }
       uint32_t run = total;
+#pragma unroll 1
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t up = __shfl_up_sync(0xffffffffu, run, o);
         if (lane >= o) run += up;
@@ -163,6 +190,7 @@ __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) 
       __syncthreads();
       if (warp == 0) {
         uint32_t s = sums[lane];
+#pragma unroll 1
         for (int o = 1; o < 32; o <<= 1) {
           const uint32_t up = __shfl_up_sync(0xffffffffu, s, o);
           if (lane >= o) s += up;
@@ -172,27 +200,26 @@ __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) 
       __syncthreads();
       run += (warp > 0 ? sums[warp - 1] : 0u) - total;
       n = (int)sums[kSortWarps - 1];
-      for (int w = 0; w < kSortWarps / 2; ++w) {
-        uint32_t* c = counts + (w0 + w) * kSortPitch + d;
-        const uint32_t here = *c;
-        *c = run;
-        run += here;
+      if (d < digits) {
+#pragma unroll 4
+        for (int w = 0; w < kSortWarps / 2; ++w) {
+          uint32_t* c = counts + (w0 + w) * kSortPitch + d;
+          const uint32_t here = *c;
+          *c = run;
+          run += here;
+        }
       }
     }
     __syncthreads();
-    for (int i = begin; i < end; i += 32 * kSortBatch) {
-      if (!in_shared) load(i);                   // (else they are in registers still)
-#pragma unroll
-      for (int j = 0; j < kSortBatch; ++j) {
-        const bool some = key[j].x != 0xFFFFFFFFu;
-        const uint32_t d = some ? digit(key[j]) : kSortDigits;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
-        uint32_t at = 0;
-        if (some) at = mine[d] + __popc(same & ((1u << lane) - 1u));
-        __syncwarp();
-        if (some && (same >> lane) == 1u) mine[d] = at + 1u;        // (the last of its digit)
-        __syncwarp();
-        if (some) to[at] = key[j];
+#pragma unroll 1
+    for (int turn = 0; turn < turns; ++turn) {
+      const int i = begin + turn * 32 + lane;
+      const uint2 k = i < end ? from[i] : make_uint2(0xFFFFFFFFu, 0u);
+      if (in_shared) {
+        if (k.x != 0xFFFFFFFFu) to[mine[digit(k)] + (k.y >> 16)] = make_uint2(k.x, k.y & 0xFFFFu);
+      } else {
+        const uint32_t at = place(k);
+        if (k.x != 0xFFFFFFFFu) to[at] = k;
       }
     }
     __syncthreads();
@@ -324,14 +351,13 @@ __global__ void __launch_bounds__(kRowThreads) embed_join_kernel(const EmbedGrad
     bool in[kAhead];
     Raw8<PRSGD_TYPE_FP32> more[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
+    for (int j = 0; j < kAhead; ++j) {                   // (parts are requested before it is known whether they are this run's)
       const int64_t at = (int64_t)(w + j) * a.unit;
-      in[j] = at < live && keys[at].x == id;
+      in[j] = at < live;
+      if (in[j]) more[j] = load_raw<PRSGD_TYPE_FP32>(parts + (int64_t)(w + j) * 2 * pitch);
+      if (in[j]) in[j] = keys[at].x == id;
     }
     if (!in[0]) break;
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (in[j]) more[j] = load_raw<PRSGD_TYPE_FP32>(parts + (int64_t)(w + j) * 2 * pitch);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (!in[j]) break;
