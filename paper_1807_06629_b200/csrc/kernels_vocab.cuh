@@ -256,11 +256,16 @@ struct VocabJoin {
   int runs;
   float* loss; float* stats;
 };
+__device__ __forceinline__ float vt_exp2(float x) {        // (to 2 ulp; results below 2^-126 are 0)
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float2 vocab_merge(float2 p, float2 q) {
   constexpr float kLog2e = 1.4426950408889634f;
   const float m = fmaxf(p.x, q.x);
   if (m == -INFINITY && p.y == 0.f && q.y == 0.f) return make_float2(m, 0.f);      // (runs without columns)
-  return make_float2(m, p.y * exp2f((p.x - m) * kLog2e) + q.y * exp2f((q.x - m) * kLog2e));
+  return make_float2(m, p.y * vt_exp2((p.x - m) * kLog2e) + q.y * vt_exp2((q.x - m) * kLog2e));
 }
 template <int ROWS>
 __global__ void __launch_bounds__(256) vocab_join_kernel(const VocabJoin a) {

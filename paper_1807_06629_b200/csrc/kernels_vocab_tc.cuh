@@ -20,9 +20,9 @@
 
 namespace prsgd {
 
-constexpr int kVtEpiWarps = 8, kVtThreads = 32 * (4 + kVtEpiWarps), kVtRing = 4;
-constexpr int kVtWarpCols = 128;               // an epilogue warp takes 32 rows of a CTA's 128 x 256 sums and this many columns
-constexpr uint32_t kVtStageBytes = 32768, kVtWarpBytes = 8192;
+constexpr int kVtEpiWarps = 16, kVtThreads = 32 * (4 + kVtEpiWarps), kVtRing = 4;
+constexpr int kVtShares = kVtEpiWarps / 4;     // an epilogue warp takes 32 rows of a CTA's 128 x 256 sums and 64 columns
+constexpr uint32_t kVtStageBytes = 32768, kVtWarpBytes = 4096;
 __host__ __device__ constexpr int vt_stages(bool grad) { return grad ? 5 : 6; }            // (the gradient's epilogue needs shared memory too)
 constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kVtStageBytes + (grad ? kVtEpiWarps * kVtWarpBytes : 0); }
 // A tensor core cuts off what the running sum does not hold, 2^-24 of it a step of 16 on average and always towards zero: what has to be
@@ -49,7 +49,10 @@ struct VocabChain {
   float2* part; float* zy;
   // gradient
   int pieces, piece, gp;                       // pieces of a group, columns of one (a multiple of 256), columns of a row of G (a multiple of 64)
-  int slots, lag, parts;
+  int slots, lag, parts, run_w;                // ...; parts of dH's contraction; tiles of dW along the vocabulary of one task
+  int tiles, td, kd, kpart, last_tiles, last_blocks;   // tiles along the vocabulary, along D; blocks of 64 of D, of a part; tiles, blocks of a group's last piece
+  int h_first;                                 // dH before dW among the uses of a piece
+  FastDiv by_td, by_run_w;
   uint16_t* G[2];                              // [slots][Tp][gp]
   float* acc; int acc_pitch;                   // [groups][parts][Tp][acc_pitch] or nullptr: one piece, one part
   void* dH; int64_t dh_row, dh_group; int dh_type, vec_dh;
@@ -58,32 +61,9 @@ struct VocabChain {
   DeviceStatus* status;
 };
 
-struct VTask { int kind, g, ti, tj, n, p, seq, live; };
-
-// Tasks of the pieces, numbered through all groups (seq = g * pieces + p).
-struct VPiece { int tm, nv, td, pv; };
-__device__ __forceinline__ VPiece vt_piece(const VocabChain& a, int seq, int live) {
-  VPiece k;
-  k.tm = (live + 255) / 256;
-  k.pv = (int)min((int64_t)a.piece, a.V - (int64_t)(seq % a.pieces) * a.piece);
-  k.nv = (k.pv + 255) / 256;
-  k.td = (a.D + 255) / 256;
-  return k;
-}
-__device__ __forceinline__ int vt_uses_h(const VocabChain& a, const VPiece& k) { return a.dH != nullptr ? k.tm * k.td * a.parts : 0; }
-__device__ __forceinline__ int vt_uses_w(const VocabChain& a, const VPiece& k) { return a.dW != nullptr ? k.nv * k.td : 0; }
-__device__ __forceinline__ unsigned int vt_need_g(const VPiece& k) { return (unsigned)(k.tm * k.nv) * 2u * kVtEpiWarps; }
-__device__ __forceinline__ unsigned int vt_need_u(const VocabChain& a, const VPiece& k) { return (unsigned)(vt_uses_h(a, k) + vt_uses_w(a, k)) * 2u * kVtEpiWarps; }
-
-// The blocks of 64 of a task's contraction: first and number.
-__device__ __forceinline__ int vt_blocks(const VocabChain& a, const VTask& k, int& n) {
-  if (k.kind <= VT_G) { n = (a.D + 63) / 64; return 0; }
-  if (k.kind == VT_DW) { n = (k.live + 63) / 64; return 0; }
-  const int nb = ((int)min((int64_t)a.piece, a.V - (int64_t)k.p * a.piece) + 63) / 64;
-  const int first = (int)((int64_t)nb * k.n / a.parts);
-  n = (int)((int64_t)nb * (k.n + 1) / a.parts) - first;
-  return first;
-}
+// A task as its pair's warps get it: tile (ti, tj) of group g, of piece p of the vocabulary; n tiles or part n; k0, kb: blocks of 64 of its
+// contraction; seq = g * pieces + p and the place of that piece's G; live tokens of the group.
+struct VTask { int kind, g, ti, tj, n, p, seq, slot, live, k0, kb, pad; };
 
 // Sums of a tile: one, or (PROMOTE) one of the small products of pairs and one per vt_promote blocks.
 template <bool SPLIT, bool PROMOTE>
@@ -92,88 +72,107 @@ __device__ __forceinline__ int vt_sums(int kb) {
   return (SPLIT ? 1 : 0) + (kb + vt_promote(SPLIT) - 1) / vt_promote(SPLIT);
 }
 
-// The list of tasks, walked in order by the thread that claims them.
+__device__ __forceinline__ int vt_tiles(int n) { return (n + 255) >> 8; }
+__device__ __forceinline__ int vt_piece_tiles(const VocabChain& a, int p) { return p + 1 == a.pieces ? a.last_tiles : a.piece >> 8; }
+__device__ __forceinline__ int vt_uses_h(const VocabChain& a, int tm) { return a.dH != nullptr ? tm * a.td * a.parts : 0; }
+__device__ __forceinline__ int vt_uses_w(const VocabChain& a, int nv) { return a.dW != nullptr ? (int)a.by_run_w.div((uint32_t)(nv + a.run_w - 1)) * a.td : 0; }
+
+// The list of tasks, walked in order by the thread that claims them, without a division on the way (one thread's divisions were most
+// of the 3 to 5 us that a claim took): a phase holds the tiles of G of one piece and the uses of the one `lag` before.
 struct VWalk {
   int phase, phases;
-  long long base, count;       // tasks before this phase, in it
-  int live_g, live_u;          // live tokens of the group whose G, whose uses are in it
+  unsigned int base, count;    // tasks before this phase, in it
+  int g, p, slot, live;        // piece whose G is in it (loss: its group)
+  int gu, pu, slot_u, live_u;  // piece whose uses are
+  int n_g, n_w, n_h;           // tiles of G, tasks of dW and of dH
 };
 template <bool GRAD>
-__device__ __forceinline__ void vt_enter(const VocabChain& a, VWalk& w) {
-  const int last = GRAD ? a.groups * a.pieces : a.groups;
-  w.count = 0;
+__device__ __forceinline__ void vt_fill(const VocabChain& a, VWalk& w) {
   if constexpr (!GRAD) {
-    w.live_g = a.live[w.phase];
-    w.count = (long long)((w.live_g + 255) / 256) * a.runs;
+    w.count = (unsigned)(vt_tiles(w.live) * a.runs);
   } else {
-    if (w.phase < last) {
-      w.live_g = a.live[w.phase / a.pieces];
-      const VPiece k = vt_piece(a, w.phase, w.live_g);
-      w.count += (long long)k.tm * k.nv;
-    }
-    if (w.phase >= a.lag) {
-      w.live_u = a.live[(w.phase - a.lag) / a.pieces];
-      const VPiece k = vt_piece(a, w.phase - a.lag, w.live_u);
-      w.count += vt_uses_h(a, k) + vt_uses_w(a, k);
-    }
+    w.n_g = w.g < a.groups ? vt_tiles(w.live) * vt_piece_tiles(a, w.p) : 0;
+    w.n_w = w.gu >= 0 ? vt_uses_w(a, vt_piece_tiles(a, w.pu)) : 0;
+    w.n_h = w.gu >= 0 ? vt_uses_h(a, vt_tiles(w.live_u)) : 0;
+    w.count = (unsigned)(w.n_g + w.n_w + w.n_h);
   }
 }
 template <bool GRAD>
-__device__ __forceinline__ bool vt_decode(const VocabChain& a, VWalk& w, long long t, VTask& k) {
-  while (t >= w.base + w.count) {
+__device__ __forceinline__ void vt_first(const VocabChain& a, VWalk& w) {
+  w.phase = 0; w.phases = GRAD ? a.groups * a.pieces + a.lag : a.groups;
+  w.base = 0; w.g = w.p = w.slot = 0; w.live = a.live[0];
+  w.gu = -1; w.pu = w.slot_u = w.live_u = 0; w.n_g = w.n_w = w.n_h = 0;
+  vt_fill<GRAD>(a, w);
+}
+template <bool GRAD>
+__device__ __forceinline__ bool vt_decode(const VocabChain& a, VWalk& w, unsigned int t, VTask& k) {
+  while (t - w.base >= w.count) {
     w.base += w.count;
     if (++w.phase >= w.phases) return false;
-    vt_enter<GRAD>(a, w);
-  }
-  int q = (int)(t - w.base);
-  k.p = k.seq = k.n = 0;
-  if constexpr (!GRAD) {
-    const int tm = (w.live_g + 255) / 256, tiles = (int)((a.V + 255) / 256);
-    k.kind = VT_STATS; k.g = w.phase; k.live = w.live_g;
-    k.tj = q / tm;
-    k.ti = q - k.tj * tm;
-    k.p = k.tj;                                  // (the run)
-    k.tj *= a.run;
-    k.n = min(a.run, tiles - k.tj);
-    return true;
-  }
-  if (w.phase < a.groups * a.pieces) {
-    const VPiece c = vt_piece(a, w.phase, w.live_g);
-    if (q < c.tm * c.nv) {
-      k.kind = VT_G; k.seq = w.phase; k.g = w.phase / a.pieces; k.p = w.phase % a.pieces; k.live = w.live_g;
-      k.tj = q / c.tm;
-      k.ti = q - k.tj * c.tm;
-      return true;
+    if (!GRAD || ++w.p == a.pieces) {
+      w.p = 0;
+      if (++w.g < a.groups) w.live = a.live[w.g];
     }
-    q -= c.tm * c.nv;
+    if (GRAD) {
+      if (++w.slot == a.slots) w.slot = 0;
+      if (w.phase == a.lag) {
+        w.gu = 0; w.live_u = a.live[0];
+      } else if (w.phase > a.lag) {
+        if (++w.slot_u == a.slots) w.slot_u = 0;
+        if (++w.pu == a.pieces) { w.pu = 0; w.live_u = a.live[++w.gu]; }
+      }
+    }
+    vt_fill<GRAD>(a, w);
   }
-  const int seq = w.phase - a.lag;
-  const VPiece c = vt_piece(a, seq, w.live_u);
-  k.seq = seq; k.g = seq / a.pieces; k.p = seq % a.pieces; k.live = w.live_u;
-  const int uw = vt_uses_w(a, c);
-  if (q < uw) {
-    k.kind = VT_DW;
-    k.ti = q / c.td;
-    k.tj = q - k.ti * c.td;
+  unsigned int q = t - w.base;
+  k.n = k.k0 = 0;
+  k.kb = a.kd;
+  if (!GRAD || q < (unsigned)w.n_g) {
+    const unsigned int tm = (unsigned)vt_tiles(w.live);
+    k.kind = GRAD ? VT_G : VT_STATS;
+    k.g = w.g; k.p = w.p; k.seq = w.phase; k.slot = w.slot; k.live = w.live;
+    k.tj = (int)(q / tm);
+    k.ti = (int)(q - (unsigned)k.tj * tm);
+    if (!GRAD) {
+      k.p = k.tj;                                // (the run)
+      k.tj *= a.run;
+      k.n = min(a.run, a.tiles - k.tj);
+    }
     return true;
   }
-  q -= uw;
+  q -= (unsigned)w.n_g;
+  k.g = w.gu; k.p = w.pu; k.seq = w.phase - a.lag; k.slot = w.slot_u; k.live = w.live_u;
+  const bool of_h = a.h_first ? q < (unsigned)w.n_h : q >= (unsigned)w.n_w;
+  if (!of_h) {
+    if (a.h_first) q -= (unsigned)w.n_h;
+    k.kind = VT_DW;
+    k.ti = (int)a.by_td.div(q);
+    k.tj = (int)q - k.ti * a.td;
+    k.ti *= a.run_w;
+    k.n = min(a.run_w, vt_piece_tiles(a, w.pu) - k.ti);
+    k.kb = (w.live_u + 63) >> 6;
+    return true;
+  }
+  if (!a.h_first) q -= (unsigned)w.n_w;
   k.kind = VT_DH;
-  k.n = q / (c.tm * c.td);
-  q -= k.n * (c.tm * c.td);
-  k.ti = q / c.td;
-  k.tj = q - k.ti * c.td;
+  const unsigned int tiles = (unsigned)(vt_tiles(w.live_u) * a.td);
+  k.n = a.parts > 1 ? (int)(q / tiles) : 0;
+  q -= (unsigned)k.n * tiles;
+  k.ti = (int)a.by_td.div(q);
+  k.tj = (int)q - k.ti * a.td;
+  k.k0 = k.n * a.kpart;
+  k.kb = max(0, min(a.kpart, (w.pu + 1 == a.pieces ? a.last_blocks : a.piece >> 6) - k.k0));
   return true;
 }
 
 namespace ptx {
-// Hands 32 bytes to a CTA of the cluster and counts them on its barrier (which expects them and one arrival).
-__device__ __forceinline__ void send_2v4(uint32_t to_cluster, uint32_t bar_cluster, uint4 v, uint4 w) {
-  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 32;" ::"r"(bar_cluster) : "memory");
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
-               ::"r"(to_cluster), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(bar_cluster) : "memory");
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
-               ::"r"(to_cluster + 16u), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w), "r"(bar_cluster) : "memory");
+// Hands 48 bytes to a CTA of the cluster and counts them on its barrier (which expects them and one arrival).
+__device__ __forceinline__ void send_48(uint32_t to_cluster, uint32_t bar_cluster, const uint4 (&v)[3]) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 48;" ::"r"(bar_cluster) : "memory");
+#pragma unroll
+  for (uint32_t i = 0; i < 3; ++i)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(to_cluster + 16u * i), "r"(v[i].x), "r"(v[i].y), "r"(v[i].z), "r"(v[i].w), "r"(bar_cluster) : "memory");
 }
 }  // namespace ptx
 
@@ -181,11 +180,6 @@ __device__ __forceinline__ void send_2v4(uint32_t to_cluster, uint32_t bar_clust
 // lane, eight lanes to a row.  Chunk c of row r sits at chunk c ^ (r % 8): free of bank conflicts both ways.
 __device__ __forceinline__ uint32_t vt_chunk(uint32_t box, int row, int q) { return box + (uint32_t)row * 128u + (uint32_t)((q ^ (row & 7)) * 16); }
 
-__device__ __forceinline__ float vt_exp2(float x) {        // (to 2 ulp; results below 2^-126 are 0)
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // Two values as 16-bit ones.
 __device__ __forceinline__ uint32_t vt_pack(int bf16, float x, float y) {
   if (bf16) {
@@ -205,15 +199,22 @@ __device__ __forceinline__ float vt_read1(const void* out, int type, int64_t o) 
   return __half2float(static_cast<const __half*>(out)[o]);
 }
 
-// Where a tile of dH or dW goes.
+// Where 32 rows of a tile go.
 struct VOut {
-  void* out; int type; int64_t row;            // first row's place is out + at(0)
+  void* out; int type; int64_t row;            // first row's place; elements between rows
   const int* index;                            // rows through index, or one after another
-  int rows, cols;                              // rows of this warp's 32 that exist; columns of the array
+  int rows, cols;                              // rows of the 32 that exist; columns of the array
   int add, vec;                                // added to what is there; rows begin on 16-byte boundaries
   int reduce;                                  // the adding is left to L2 (fp32 rows on 16-byte boundaries whose pitch is a multiple of 4)
-  __device__ __forceinline__ int64_t at(int r) const { return (index ? (int64_t)index[r] : (int64_t)r) * row; }
 };
+// Element offsets of rows lane / 8 + 4 i, i = 0..7 (-1: not there).
+__device__ __forceinline__ void vt_rows(const VOut& d, int lane, int64_t (&o)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = 4 * i + (lane >> 3);
+    o[i] = r < d.rows ? (d.index ? (int64_t)d.index[r] : (int64_t)r) * d.row : -1;
+  }
+}
 
 // Adds four floats to memory in L2.  (A sum read, added to and written back by the SM waits for its old values: about 1 us four times
 // a tile, as long as the products of a tile of dH.)
@@ -230,62 +231,69 @@ __device__ __forceinline__ void vt_out32(const VOut& d, uint32_t box, int lane, 
     st_shared_v4(vt_chunk(box, lane, q), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
   __syncwarp();
   const int c = c0 + (lane & 7) * 4;
+  if (c >= d.cols) return;
+  int64_t o[8];
+  vt_rows(d, lane, o);
   if (d.reduce) {
-    if (c >= d.cols) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int r = 4 * i + (lane >> 3);
-      const uint4 u = ld_shared_v4(vt_chunk(box, r, lane & 7));
-      if (r < d.rows) vt_red4(static_cast<float*>(d.out) + (int64_t)r * d.row + c, u);
+      const uint4 u = ld_shared_v4(vt_chunk(box, 4 * i + (lane >> 3), lane & 7));
+      if (o[i] >= 0) vt_red4(static_cast<float*>(d.out) + o[i] + c, u);
     }
     return;
   }
-  const bool whole = d.vec && c + 4 <= d.cols;
-#pragma unroll 1
+  const bool whole = d.vec && c + 4 <= d.cols && d.type == PRSGD_TYPE_FP32;
+#pragma unroll
   for (int i = 0; i < 8; i += 4) {
-    float4 w[4], old[4];
-    int64_t o[4];
+    float4 old[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = 4 * (i + j) + (lane >> 3);
-      o[j] = r < d.rows ? d.at(r) + c : -1;
       old[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (d.add && o[j] >= 0) {                            // (past L1, which does not see what other SMs wrote meanwhile)
-        if (whole && d.type == PRSGD_TYPE_FP32) {
-          old[j] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(d.out) + o[j]));
-        } else {
-          float* e = reinterpret_cast<float*>(&old[j]);
+      if (!d.add || o[i + j] < 0) continue;
+      if (whole) {
+        old[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(d.out) + o[i + j] + c);
+      } else {
+        float* e = reinterpret_cast<float*>(&old[j]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (c + k < d.cols) e[k] = vt_read1(d.out, d.type, o[j] + k);
-        }
+        for (int k = 0; k < 4; ++k)
+          if (c + k < d.cols) e[k] = vt_read1(d.out, d.type, o[i + j] + c + k);
       }
-      const uint4 u = ld_shared_v4(vt_chunk(box, r, lane & 7));
-      w[j] = make_float4(__uint_as_float(u.x) + old[j].x, __uint_as_float(u.y) + old[j].y, __uint_as_float(u.z) + old[j].z, __uint_as_float(u.w) + old[j].w);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (o[j] < 0) continue;
-      if (whole && d.type == PRSGD_TYPE_FP32) {
-        *reinterpret_cast<float4*>(static_cast<float*>(d.out) + o[j]) = w[j];
+      const uint4 u = ld_shared_v4(vt_chunk(box, 4 * (i + j) + (lane >> 3), lane & 7));
+      if (o[i + j] < 0) continue;
+      const float4 w = make_float4(__uint_as_float(u.x) + old[j].x, __uint_as_float(u.y) + old[j].y, __uint_as_float(u.z) + old[j].z, __uint_as_float(u.w) + old[j].w);
+      if (whole) {
+        *reinterpret_cast<float4*>(static_cast<float*>(d.out) + o[i + j] + c) = w;
       } else {
-        const float* e = reinterpret_cast<const float*>(&w[j]);
+        const float* e = reinterpret_cast<const float*>(&w);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (c + k < d.cols) vt_write1(d.out, d.type, o[j] + k, e[k]);
+          if (c + k < d.cols) vt_write1(d.out, d.type, o[i + j] + c + k, e[k]);
       }
     }
   }
 }
-// 32 rows x 64 columns of 16-bit values already in the box.
+// 32 rows x 64 columns of 16-bit values, a row per lane, through `box`: 32 columns (half h) into it, and from there eight columns a lane.
+__device__ __forceinline__ void vt_put32(int bf16, uint32_t box, int lane, int h, const float (&v)[32]) {
+  if (h == 0) __syncwarp();
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    st_shared_v4(vt_chunk(box, lane, h * 4 + q), vt_pack(bf16, v[8 * q], v[8 * q + 1]), vt_pack(bf16, v[8 * q + 2], v[8 * q + 3]),
+                 vt_pack(bf16, v[8 * q + 4], v[8 * q + 5]), vt_pack(bf16, v[8 * q + 6], v[8 * q + 7]));
+}
 __device__ __forceinline__ void vt_out64(const VOut& d, uint32_t box, int lane, int c0) {
+  __syncwarp();
   const int c = c0 + (lane & 7) * 8;
+  if (c >= d.cols) return;
+  int64_t o[8];
+  vt_rows(d, lane, o);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int r = 4 * i + (lane >> 3);
-    const uint4 u = ld_shared_v4(vt_chunk(box, r, lane & 7));
-    if (r >= d.rows) continue;
-    uint16_t* to = static_cast<uint16_t*>(d.out) + d.at(r) + c;
+    const uint4 u = ld_shared_v4(vt_chunk(box, 4 * i + (lane >> 3), lane & 7));
+    if (o[i] < 0) continue;
+    uint16_t* to = static_cast<uint16_t*>(d.out) + o[i] + c;
     if (c + 8 <= d.cols) {
       *reinterpret_cast<uint4*>(to) = u;
     } else {
@@ -305,9 +313,10 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kVtRing + 1];
-  __shared__ __align__(16) uint4 ring[2 * kVtRing];
+  __shared__ __align__(16) uint4 ring[3 * kVtRing];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
+  __shared__ float2 shares[GRAD ? 1 : 2][GRAD ? 1 : 128][kVtShares];
   const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = blockIdx.x & 1u;                 // clusters of two along x
@@ -345,20 +354,22 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
   auto next_task = [&](int n) -> VTask {
     const int r = n % kVtRing;
     VTask k;
-    k.kind = -1; k.g = k.ti = k.tj = k.n = k.p = k.seq = k.live = 0;
+    k.kind = -1;
     if (!ptx::warp_wait(sfull(r), (uint32_t)((n / kVtRing) & 1), ab, status, VT_ERR_RING)) return k;
-    const uint4 w = ld_shared_v4(ptx::smem_u32(&ring[2 * r])), x = ld_shared_v4(ptx::smem_u32(&ring[2 * r + 1]));
+    const uint32_t at = ptx::smem_u32(&ring[3 * r]);
+    const uint4 w = ld_shared_v4(at), x = ld_shared_v4(at + 16u), y = ld_shared_v4(at + 32u);
     auto all = [&](uint32_t v) { return (int)__shfl_sync(0xffffffffu, v, 0); };
     k.kind = all(w.x); k.g = all(w.y); k.ti = all(w.z); k.tj = all(w.w);
-    k.n = all(x.x); k.p = all(x.y); k.seq = all(x.z); k.live = all(x.w);
+    k.n = all(x.x); k.p = all(x.y); k.seq = all(x.z); k.slot = all(x.w);
+    k.live = all(y.x); k.k0 = all(y.y); k.kb = all(y.z);
     return k;
   };
   auto free_task = [&](int n) { ptx::mbar_arrive_cluster(ptx::cluster_map(sempty(n % kVtRing), 0)); };
 
   // The load and product roles are walked by whole warps with one elected lane that issues, so that descriptors and addresses stay
-  // in uniform registers.  Sums in registers take them from the other warps: 128 * 64 + 256 * 216 of the launch's 384 * 168.
+  // in uniform registers.  The epilogue's sums take registers from them: 128 * 64 + 512 * 104 of the launch's 640 * 96.
   if (warp < 4) {
-    if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
       const bool second = warp == 3, issue = ptx::elect_one();
       uint32_t s = 0, phase = 1;                           // (a fresh barrier passes a wait for the phase before its first)
@@ -366,18 +377,17 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         const VTask k = next_task(n);
         if (k.kind < 0) break;
         if (issue) { free_task(n); ptx::fence_proxy_async_all(); }
-        int kb;
-        const int k0 = vt_blocks(a, k, kb), tiles = k.kind == VT_STATS ? k.n : 1, blocks = tiles * kb * kPasses, ask = max(0, blocks - kVtAhead);
-        const int wg = a.w_shared ? 0 : k.g, slot = GRAD ? k.seq % a.slots : 0;
+        const int k0 = k.k0, kb = k.kb, tiles = k.kind == VT_STATS || k.kind == VT_DW ? k.n : 1, blocks = tiles * kb * kPasses, ask = max(0, blocks - kVtAhead);
+        const int wg = a.w_shared ? 0 : k.g;
         const bool of_w = second ? k.kind != VT_DW : false, of_g = !second && k.kind >= VT_DH;
         const bool mn = GRAD && (k.kind == VT_DW || (second && k.kind == VT_DH));
-        const int z = of_w ? wg : of_g ? slot : k.g;
+        const int z = of_w ? wg : of_g ? k.slot : k.g;
         const bool swap = of_w && a.w_swap;
         if (issue && blocks == 0 && rank == 0 && !second) ptx::mbar_arrive(loaded);
         bool ok = true;
         for (int j = 0, b = 0; j < tiles && ok; ++j) {
           // first row (column) of this CTA's half of the operand, first of the contraction
-          int at0 = (second ? k.tj + j : k.ti) * 256 + (int)rank * 128, q0 = 0;
+          int at0 = (second ? k.tj + (k.kind == VT_STATS ? j : 0) : k.ti + (k.kind == VT_DW ? j : 0)) * 256 + (int)rank * 128, q0 = 0;
           if (GRAD && of_w) {
             if (k.kind == VT_G) at0 += k.p * a.piece;
             else q0 = k.p * a.piece;
@@ -415,9 +425,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         const VTask k = next_task(n);
         if (k.kind < 0) break;
         if (issue) free_task(n);
-        int kb;
-        (void)vt_blocks(a, k, kb);
-        const int blocks = kb * kPasses, tiles = blocks > 0 ? (k.kind == VT_STATS ? k.n : 1) : 0;
+        const int kb = k.kb, blocks = kb * kPasses, tiles = blocks > 0 ? (k.kind == VT_STATS || k.kind == VT_DW ? k.n : 1) : 0;
         const bool a_mn = GRAD && k.kind == VT_DW, b_mn = GRAD && k.kind >= VT_DH;
         const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn) | format;
         // a step of 16 along the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major block
@@ -455,9 +463,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
       }
     } else if (warp == 2 && lane == 0 && rank == 0) {      // ---- claims tasks for the pair --------------------------------
       VWalk w;
-      w.phase = 0; w.phases = GRAD ? a.groups * a.pieces + a.lag : a.groups;
-      w.base = 0; w.live_g = w.live_u = 0;
-      vt_enter<GRAD>(a, w);
+      vt_first<GRAD>(a, w);
       int ready_g = -1, ready_u = -1;                      // pieces seen to be done
       for (int n = 0;; ++n) {
         const int r = n % kVtRing;
@@ -466,10 +472,11 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         if (n > 0 && !ptx::mbar_wait(loaded, (uint32_t)((n - 1) & 1), ab, status, VT_ERR_RING_FREE)) break;
         if (n >= kVtRing && !ptx::mbar_wait(sempty(r), (uint32_t)(((n / kVtRing) - 1) & 1), ab, status, VT_ERR_RING_FREE)) break;
         VTask k;
-        k.kind = -1; k.g = k.ti = k.tj = k.n = k.p = k.seq = k.live = 0;
-        const long long t = (long long)atomicAdd(a.claim, 1u);
-        VTask got;
-        if (vt_decode<GRAD>(a, w, t, got)) k = got;
+        const unsigned int t = atomicAdd(a.claim, 1u);
+        if (!vt_decode<GRAD>(a, w, t, k)) {
+          k.kind = -1;
+          k.g = k.ti = k.tj = k.n = k.p = k.seq = k.slot = k.live = k.k0 = k.kb = 0;
+        }
         if (GRAD && k.kind >= 0) {
           // what it waits for: tiles of G; the uses of the piece whose place it takes; for dH, the piece before of the same group
           int wait_g = -1, wait_u = -1;
@@ -477,29 +484,30 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           else wait_g = k.seq;
           if (k.kind == VT_DH && k.p > 0) wait_u = k.seq - 1;
           if (wait_g > ready_g) {
-            const unsigned int need = vt_need_g(vt_piece(a, wait_g, k.live));
+            const unsigned int need = (unsigned)(vt_tiles(k.live) * vt_piece_tiles(a, k.p)) * 2u * kVtEpiWarps;
             if (need > 0 && !ptx::flag_wait(a.done_g + wait_g, need, ab, status, VT_ERR_DEP)) break;
             ready_g = wait_g;
           }
           if (wait_u >= 0 && wait_u != ready_u) {
-            const unsigned int need = vt_need_u(a, vt_piece(a, wait_u, a.live[wait_u / a.pieces]));
+            const int g = wait_u / a.pieces, p = wait_u - g * a.pieces;
+            const unsigned int need = (unsigned)(vt_uses_h(a, vt_tiles(a.live[g])) + vt_uses_w(a, vt_piece_tiles(a, p))) * 2u * kVtEpiWarps;
             if (need > 0 && !ptx::flag_wait(a.done_u + wait_u, need, ab, status, VT_ERR_DEP)) break;
             ready_u = wait_u;
           }
         }
+        const uint4 words[3] = {make_uint4((uint32_t)k.kind, (uint32_t)k.g, (uint32_t)k.ti, (uint32_t)k.tj),
+                                make_uint4((uint32_t)k.n, (uint32_t)k.p, (uint32_t)k.seq, (uint32_t)k.slot),
+                                make_uint4((uint32_t)k.live, (uint32_t)k.k0, (uint32_t)k.kb, 0u)};
 #pragma unroll
-        for (uint32_t c = 0; c < 2; ++c)
-          ptx::send_2v4(ptx::cluster_map(ptx::smem_u32(&ring[2 * r]), c), ptx::cluster_map(sfull(r), c),
-                        make_uint4((uint32_t)k.kind, (uint32_t)k.g, (uint32_t)k.ti, (uint32_t)k.tj),
-                        make_uint4((uint32_t)k.n, (uint32_t)k.p, (uint32_t)k.seq, (uint32_t)k.live));
+        for (uint32_t c = 0; c < 2; ++c) ptx::send_48(ptx::cluster_map(ptx::smem_u32(&ring[3 * r]), c), ptx::cluster_map(sfull(r), c), words);
         if (k.kind < 0) break;
       }
     }
   } else {                                               // ---- epilogue ---------------------------------------------
-    if constexpr (PROMOTE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     const int quarter = warp & 3, share = (warp - 4) >> 2;
-    const uint32_t box_hi = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes, box_lo = box_hi + 4096u;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kVtWarpCols);
+    const uint32_t box = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * 64);
     uint32_t sums = 0;
     for (int n = 0;; ++n) {
       const VTask k = next_task(n);
@@ -507,18 +515,16 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
       if (lane == 0) free_task(n);
       const VocabScale* sc = a.scale + k.g;
       const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32;
-      bool ok = true;
-      auto release = [&](uint32_t acc) {                 // the sum has been read: the next product may overwrite it
+      const int kb = k.kb, parts = vt_sums<SPLIT, PROMOTE>(kb);
+      // Waits for the warp's 64 columns of a tile's sum; several sums (PROMOTE) are added in registers and the total goes back to TMEM, over
+      // the last of them, so that what follows needs registers for 32 columns only.
+      uint32_t acc = 0;
+      auto release = [&]() {                             // the sum has been read: the next products may overwrite it
         ptx::tc_fence_before();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
       };
-      int kb;
-      (void)vt_blocks(a, k, kb);
-      const int parts = vt_sums<SPLIT, PROMOTE>(kb);
-      // Waits for a tile's sum; several are added in registers and the total goes back to TMEM, over the last of them, so that what
-      // follows is a loop of few instructions.
-      auto gather = [&](uint32_t& acc) -> bool {
+      auto gather = [&]() -> bool {
         if (!PROMOTE || parts == 1) {
           acc = sums & 1u;
           if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
@@ -526,207 +532,193 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           ptx::tc_fence_after();
           return true;
         }
-        float total[kVtWarpCols / 32][32];
+        float total[2][32];
 #pragma unroll
-        for (int i = 0; i < kVtWarpCols; ++i) total[i >> 5][i & 31] = 0.f;
+        for (int i = 0; i < 64; ++i) total[i >> 5][i & 31] = 0.f;
+#pragma unroll 1
         for (int p = 0; p < parts; ++p, ++sums) {
           acc = sums & 1u;
           if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
           ptx::tc_fence_after();
 #pragma unroll
-          for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
-            uint32_t raw[32];
-            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
+          for (int q = 0; q < 4; ++q) {
+            uint32_t raw[16];
+            ptx::tmem_ld16(lanes + acc * 256u + (uint32_t)(q * 16), raw);
             ptx::tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) total[ch][i] += __uint_as_float(raw[i]);
+            for (int i = 0; i < 16; ++i) total[q >> 1][(q & 1) * 16 + i] += __uint_as_float(raw[i]);
           }
-          if (p + 1 < parts) release(acc);
+          if (p + 1 < parts) release();
         }
-#pragma unroll
-        for (int ch = 0; ch < kVtWarpCols / 32; ++ch) ptx::tmem_st32(lanes + acc * 256u + (uint32_t)(ch * 32), total[ch]);
+        ptx::tmem_st32(lanes + acc * 256u, total[0]);
+        ptx::tmem_st32(lanes + acc * 256u + 32u, total[1]);
         ptx::tmem_st_wait();
         return true;
       };
+      auto half = [&](int h, float (&v)[32]) {
+        ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(h * 32), *reinterpret_cast<uint32_t(*)[32]>(v));
+        ptx::tmem_ld_wait();
+      };
+      bool ok = true;
       if constexpr (!GRAD) {
         const int row = r0 + lane;
         const int y = row < k.live ? a.rowy[(int64_t)k.g * a.Tp + row] : -1;
         float m = -INFINITY, sum = 0.f, zs1 = 1.f, zs2 = 1.f;
         if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
-        for (int j = 0; j < k.n; ++j) {
-          uint32_t acc;
-          ok = gather(acc);
-          if (!ok) break;
-          const int64_t c_warp = (int64_t)(k.tj + j) * 256 + share * kVtWarpCols;
 #pragma unroll 1
-          for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
-            const int64_t c0 = c_warp + ch * 32;
-            if (c0 >= a.V) break;
-            uint32_t raw[32];
-            ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
-            ptx::tmem_ld_wait();
-            float z[32];
-            const int cols = (int)min((int64_t)32, a.V - c0);
+        for (int j = 0; j < k.n; ++j) {
+          ok = gather();
+          if (!ok) break;
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            const int64_t c0 = (int64_t)(k.tj + j) * 256 + share * 64 + h * 32;
+            const int cols = (int)min((int64_t)32, a.V - c0), mine = (int)(y - c0);
+            if (cols <= 0) break;
+            float v[32];
+            half(h, v);
+            if (SPLIT) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) z[i] = SPLIT ? __uint_as_float(raw[i]) * zs1 * zs2 : __uint_as_float(raw[i]);
+              for (int i = 0; i < 32; ++i) v[i] = v[i] * zs1 * zs2;
+            }
             if (cols < 32) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) z[i] = i < cols ? z[i] : -INFINITY;
+              for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : -INFINITY;
             }
-            const int64_t mine = y - c0;
             if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
               float at = 0.f;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) at = mine == i ? z[i] : at;
+              for (int i = 0; i < 32; ++i) at = mine == i ? v[i] : at;
               if (y >= 0 && mine >= 0 && mine < 32) a.zy[(int64_t)k.g * a.Tp + row] = at;
             }
-            float most[4] = {m, z[1], z[2], z[3]};
-            most[0] = fmaxf(m, z[0]);
+            float most[4] = {m, v[1], v[2], v[3]};
+            most[0] = fmaxf(m, v[0]);
 #pragma unroll
-            for (int i = 4; i < 32; ++i) most[i & 3] = fmaxf(most[i & 3], z[i]);
+            for (int i = 4; i < 32; ++i) most[i & 3] = fmaxf(most[i & 3], v[i]);
             const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
             float part[4] = {sum * vt_exp2((m - top) * kLog2e), 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) part[i & 3] += vt_exp2((z[i] - top) * kLog2e);
+            for (int i = 0; i < 32; ++i) part[i & 3] += vt_exp2((v[i] - top) * kLog2e);
             sum = (part[0] + part[1]) + (part[2] + part[3]);
             m = top;
           }
-          release(acc);
+          release();
         }
         if (!ok) break;
-        if (row < k.live) a.part[((int64_t)k.g * a.runs * 2 + k.p * 2 + share) * a.Tp + row] = make_float2(m, sum);
+        // The four warps that share the rows put theirs together: one pair of numbers a token and run.  (Places of alternate runs: a
+        // warp two runs on has passed a barrier that the reader of this one reached behind its reading.)
+        float2* const at = shares[n & 1][quarter * 32 + lane];
+        at[share] = make_float2(m, sum);
+        ptx::named_bar_sync(1 + quarter, 32 * kVtShares);
+        if (share == 0 && row < k.live) {
+          const float2 all = vocab_merge(vocab_merge(at[0], at[1]), vocab_merge(at[2], at[3]));
+          a.part[((int64_t)k.g * a.runs + k.p) * a.Tp + row] = all;
+        }
       } else {
-        uint32_t acc = 0;
-        if (kb > 0) ok = gather(acc);
-        if (!ok) break;
         if (k.kind == VT_G) {
-          const int row = r0 + lane;
+          const int row = r0 + lane, cu = k.tj * 256 + share * 64;
           const bool on = row < k.live;
-          const int64_t at = (int64_t)k.g * a.Tp + row;
+          const int64_t at = (int64_t)k.g * a.Tp + row, v0 = (int64_t)k.p * a.piece + cu;
           const float4 rp = on ? a.rowp[at] : make_float4(0.f, 0.f, 0.f, 0.f);
           const int y = on ? a.rowy[at] : -1;
           float zs1 = 1.f, zs2 = 1.f;
           if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
           const float both = rp.z * sc->g, hot = rp.w * sc->g;
-          const int64_t v0 = (int64_t)k.p * a.piece;
-          const int c_warp = k.tj * 256 + share * kVtWarpCols, slot = k.seq % a.slots;
           // the rows a product reads: up to the next multiple of 64, zeros behind the last live one
           VOut d;
-          d.type = PRSGD_TYPE_FP16; d.row = a.gp; d.index = nullptr; d.add = 0; d.vec = 1; d.cols = a.gp;
+          d.type = PRSGD_TYPE_FP16; d.row = a.gp; d.index = nullptr; d.add = 0; d.vec = 1; d.cols = a.gp; d.reduce = 0;
           d.rows = min(32, (k.live + 63) / 64 * 64 - r0);
+          const int64_t o = ((int64_t)k.slot * a.Tp + r0) * a.gp;
+          const bool some = d.rows > 0 && cu < a.gp;
+          ok = gather();
+          if (!ok) break;
+          // (pairs: what the first rounding left goes through the box in a second round)
 #pragma unroll 1
-          for (int u = 0; u < kVtWarpCols / 64; ++u) {
-            const int cu = c_warp + u * 64;
-            if (cu >= a.gp || d.rows <= 0) break;
-            __syncwarp();
+          for (int plane = 0; plane < (SPLIT ? 2 : 1); ++plane) {
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
-              const int64_t c0 = v0 + cu + h * 32;
-              uint32_t raw[32];
-              ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(u * 64 + h * 32), raw);
-              ptx::tmem_ld_wait();
+              const int64_t c0 = v0 + h * 32;
+              const int mine = (int)(y - c0), cols = on ? (int)max((int64_t)0, min((int64_t)32, a.V - c0)) : 0;
               float v[32];
+              half(h, v);
+              if (h == 1 && plane == (SPLIT ? 1 : 0)) release();
+              if (!some) continue;
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
-                const float z = SPLIT ? __uint_as_float(raw[i]) * zs1 * zs2 : __uint_as_float(raw[i]);
+                const float z = SPLIT ? v[i] * zs1 * zs2 : v[i];
                 v[i] = both * vt_exp2(((z - rp.x) - rp.y) * kLog2e);
               }
-              const int64_t mine = y - c0;
               if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] -= y >= 0 && mine == i ? hot : 0.f;
               }
-              const int cols = on ? (int)min((int64_t)32, a.V - c0) : 0;
               if (cols < 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : 0.f;
               }
+              if (SPLIT && plane == 1) {
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = vt_pack(SPLIT ? 0 : a.bf16, v[8 * q + 2 * i], v[8 * q + 2 * i + 1]);
-                st_shared_v4(vt_chunk(box_hi, lane, h * 4 + q), w[0], w[1], w[2], w[3]);
-                if constexpr (SPLIT) {
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    const float2 f = unpack_half2(w[i]);
-                    w[i] = pack_half2(v[8 * q + 2 * i] - f.x, v[8 * q + 2 * i + 1] - f.y);
-                  }
-                  st_shared_v4(vt_chunk(box_lo, lane, h * 4 + q), w[0], w[1], w[2], w[3]);
+                for (int i = 0; i < 32; i += 2) {
+                  const float2 f = unpack_half2(pack_half2(v[i], v[i + 1]));
+                  v[i] -= f.x; v[i + 1] -= f.y;
                 }
               }
+              vt_put32(SPLIT ? 0 : a.bf16, box, lane, h, v);
             }
-            __syncwarp();
-            const int64_t o = ((int64_t)slot * a.Tp + r0) * a.gp;
-            d.out = a.G[0] + o;
-            vt_out64(d, box_hi, lane, cu);
-            if constexpr (SPLIT) {
-              d.out = a.G[1] + o;
-              vt_out64(d, box_lo, lane, cu);
-            }
+            d.out = a.G[plane] + o;
+            if (some) vt_out64(d, box, lane, cu);
           }
         } else {
           const bool of_w = k.kind == VT_DW;
-          const float s1 = of_w ? sc->dw1 : sc->dh1, s2 = of_w ? sc->dw2 : sc->dh2;
+          const float s1 = of_w ? sc->dw1 : sc->dh1, s2 = of_w ? sc->dw2 : sc->dh2, s12 = s1 * s2;
+          const int cu = k.tj * 256 + share * 64;
           VOut d;
           d.cols = a.D; d.index = nullptr; d.reduce = 0;
-          if (of_w) {
-            const int64_t v0 = (int64_t)k.p * a.piece;
-            d.rows = (int)max((int64_t)-1, min((int64_t)32, min((int64_t)a.piece, a.V - v0) - r0));
-            d.type = a.dw_type; d.row = a.dw_row; d.add = a.accumulate; d.vec = a.vec_dw;
-            const int64_t o = (int64_t)k.g * a.dw_group + (v0 + r0) * a.dw_row;
-            d.out = static_cast<char*>(a.dW) + o * (a.dw_type == PRSGD_TYPE_FP32 ? 4 : 2);
-          } else {
-            d.rows = min(32, k.live - r0);
-            if (a.acc == nullptr) {
-              d.type = a.dh_type; d.row = a.dh_row; d.add = 0; d.vec = a.vec_dh;
-              d.index = a.index + (int64_t)k.g * a.Tp + r0;
-              d.out = static_cast<char*>(a.dH) + (int64_t)k.g * a.dh_group * (a.dh_type == PRSGD_TYPE_FP32 ? 4 : 2);
-            } else {
-              d.type = PRSGD_TYPE_FP32; d.row = a.acc_pitch; d.add = d.reduce = k.p > 0; d.vec = 1;
-              d.cols = a.acc_pitch;
-              d.out = a.acc + (((int64_t)k.g * a.parts + k.n) * a.Tp + r0) * a.acc_pitch;
-            }
-          }
-          const bool narrow = d.type != PRSGD_TYPE_FP32 && !d.add && d.vec;
-          const int c_warp = k.tj * 256 + share * kVtWarpCols;
-          const bool skip = d.rows <= 0 || (kb == 0 && d.add);
 #pragma unroll 1
-          for (int ch = 0; ch < kVtWarpCols / 32; ++ch) {
-            const int c0 = c_warp + ch * 32;
-            if (c0 >= a.D || skip) break;
-            float v[32];
-            if (kb > 0) {
-              uint32_t raw[32];
-              ptx::tmem_ld32(lanes + acc * 256u + (uint32_t)(ch * 32), raw);
-              ptx::tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]) * s1 * s2;
+          for (int j = 0; j < (of_w ? k.n : 1); ++j) {
+            if (of_w) {
+              const int rj = r0 + j * 256;               // first row of this warp's part of the tile
+              const int64_t v0 = (int64_t)k.p * a.piece + rj, o = (int64_t)k.g * a.dw_group + v0 * a.dw_row;
+              d.rows = (int)max((int64_t)-1, min((int64_t)min(32, a.piece - rj), a.V - v0));
+              d.type = a.dw_type; d.row = a.dw_row; d.add = a.accumulate; d.vec = a.vec_dw;
+              d.out = static_cast<char*>(a.dW) + o * (a.dw_type == PRSGD_TYPE_FP32 ? 4 : 2);
             } else {
+              d.rows = min(32, k.live - r0);
+              if (a.acc == nullptr) {
+                d.type = a.dh_type; d.row = a.dh_row; d.add = 0; d.vec = a.vec_dh;
+                d.index = a.index + (int64_t)k.g * a.Tp + r0;
+                d.out = static_cast<char*>(a.dH) + (int64_t)k.g * a.dh_group * (a.dh_type == PRSGD_TYPE_FP32 ? 4 : 2);
+              } else {
+                d.type = PRSGD_TYPE_FP32; d.row = a.acc_pitch; d.add = d.reduce = k.p > 0; d.vec = 1;
+                d.cols = a.acc_pitch;
+                d.out = a.acc + (((int64_t)k.g * a.parts + k.n) * a.Tp + r0) * a.acc_pitch;
+              }
+            }
+            if (kb > 0) ok = gather();
+            if (!ok) break;
+            const bool narrow = d.type != PRSGD_TYPE_FP32 && !d.add && d.vec, some = cu < a.D && d.rows > 0 && !(kb == 0 && d.add);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              float v[32];
+              if (kb > 0) {
+                half(h, v);
+                if (h == 1) release();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = 0.f;
-            }
-            if (!narrow) {
-              vt_out32(d, box_hi, lane, c0, v);
-              continue;
-            }
-            if ((ch & 1) == 0) __syncwarp();
-            const int bf = d.type == PRSGD_TYPE_BF16;
+                for (int i = 0; i < 32; ++i) v[i] = SPLIT ? v[i] * s1 * s2 : v[i] * s12;
+              } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              st_shared_v4(vt_chunk(box_hi, lane, (ch & 1) * 4 + q), vt_pack(bf, v[8 * q], v[8 * q + 1]), vt_pack(bf, v[8 * q + 2], v[8 * q + 3]),
-                           vt_pack(bf, v[8 * q + 4], v[8 * q + 5]), vt_pack(bf, v[8 * q + 6], v[8 * q + 7]));
-            if ((ch & 1) == 1 || c0 + 32 >= a.D) {
-              __syncwarp();
-              vt_out64(d, box_hi, lane, c0 - (ch & 1) * 32);
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+              }
+              if (!some) continue;
+              if (narrow) vt_put32(d.type == PRSGD_TYPE_BF16, box, lane, h, v);
+              else vt_out32(d, box, lane, cu + h * 32, v);
             }
+            if (narrow && some) vt_out64(d, box, lane, cu);
           }
+          if (!ok) break;
         }
-        if (kb > 0) release(acc);
         __syncwarp();
-        if (lane == 0) {                                 // count the task, everything the warp wrote before it
-          asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        if (lane == 0) {                                 // count the task, what others read of it before it
+          if (k.kind == VT_G || (k.kind == VT_DH && a.pieces > 1)) asm volatile("fence.acq_rel.gpu;" ::: "memory");
           ptx::red_add((k.kind == VT_G ? a.done_g : a.done_u) + k.seq, 1u);
         }
       }

@@ -49,12 +49,13 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
     a.Hc[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
     a.Wc[i] = reinterpret_cast<uint16_t*>(take(p.copy_w ? 2 * (size_t)groups * V * a.pitch : 0));
   }
+  c.tiles = (int)nv; c.td = (int)td; c.kd = (int)up(D, 64); c.by_td = FastDiv((uint32_t)td);
   if (!grad) {
     // A run: tiles along the vocabulary whose maxima and sums one task keeps in registers; longer ones leave fewer parts behind, as long
     // as every pair gets eight.
     c.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * tm * nv / (8 * kPairs)));
     c.runs = (int)up(nv, c.run);
-    c.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * 2 * c.runs * a.Tp));
+    c.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * c.runs * a.Tp));
     c.zy = reinterpret_cast<float*>(take(4 * (size_t)groups * a.Tp));
     a.n_counters = 1;
     a.counters = c.claim = reinterpret_cast<unsigned int*>(take(4));
@@ -73,9 +74,16 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
   // Parts of dH's contraction: of 4096 columns or fewer, and more while there are not two tiles a pair, but of 1024 or more.
   const int64_t few = up(2 * kPairs, tm * td);
   c.parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(c.piece / 4096, std::min<int64_t>(few, c.piece / 1024)), 32));
-  // Uses of a piece follow its tiles of G by as many pieces as hold two tasks a pair; a piece's place is taken again as many later.
-  const int64_t tasks = tm * npv + npv * td + tm * td * c.parts;
-  c.lag = (int)std::max<int64_t>(1, std::min<int64_t>(seqs, up(2 * kPairs, tasks)));
+  // Tiles of dW along the vocabulary that are one task: claiming takes about 2 us, as long as the products of 8 blocks of 64 tokens.
+  c.run_w = (int)std::max<int64_t>(1, std::min<int64_t>(8 * 64 / std::min<int64_t>(a.Tp, 512), groups * c.pieces * npv * td / (4 * kPairs)));
+  c.kpart = (int)up(up(std::min<int64_t>(c.piece, V), 64), c.parts);
+  c.h_first = c.kpart > a.Tp / 64 * c.run_w;   // the longer uses of a piece first
+  c.by_run_w = FastDiv((uint32_t)c.run_w);
+  c.last_tiles = (int)(nv - (c.pieces - 1) * npv);
+  c.last_blocks = (int)up(V - (int64_t)(c.pieces - 1) * c.piece, 64);
+  // Uses of a piece follow its tiles of G by as many pieces as hold two tiles a pair (16 groups of 64 tokens and 1000 classes: all G first); a
+  // piece's place is taken again as many later.
+  c.lag = (int)std::max<int64_t>(1, std::min<int64_t>(seqs, up(2 * kPairs, tm * npv)));
   c.slots = (int)std::min<int64_t>(seqs, 2 * c.lag + 1);
   for (int i = 0; i < planes; ++i) c.G[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)c.slots * a.Tp * c.gp));
   c.acc_pitch = (int)round_up(D, 8);
@@ -237,9 +245,10 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
   rc = vocab_run(p, st);
   if (rc != PRSGD_OK) return rc;
   VocabJoin j{};
-  j.part = p.chain.part; j.zy = p.chain.zy; j.index = a.index; j.live = a.live; j.Tp = a.Tp; j.T = tokens; j.runs = 2 * p.chain.runs;
+  j.part = p.chain.part; j.zy = p.chain.zy; j.index = a.index; j.live = a.live; j.Tp = a.Tp; j.T = tokens; j.runs = p.chain.runs;
   j.loss = d_loss; j.stats = d_stats;
   if (tokens <= 8) launch_pdl(vocab_join_kernel<1>, dim3((unsigned)tokens, (unsigned)groups), dim3(256), 0, st, j);
+  else if (groups * tokens <= 16384) launch_pdl(vocab_join_kernel<8>, dim3((unsigned)up(tokens, 8), (unsigned)groups), dim3(256), 0, st, j);
   else launch_pdl(vocab_join_kernel<32>, dim3((unsigned)up(tokens, 32), (unsigned)groups), dim3(256), 0, st, j);
   return op_launched("vocab_loss");
 }
