@@ -70,7 +70,7 @@ __device__ __forceinline__ float finite_abs(float x) { return fabsf(x) <= 3.4028
 __device__ __forceinline__ int vocab_exponent(float x, int top) { return x > 0.f ? max(-126, min(126, top - ilogbf(x))) : 0; }
 __device__ __forceinline__ void vocab_halves(int n, float& a, float& b) { a = exp2f((float)(n / 2)); b = exp2f((float)(n - n / 2)); }
 
-// Largest finite magnitudes of the live rows of H and of W (fp32 operands only).
+// Largest finite magnitudes of the live rows of H and of W (fp32 operands only), a warp a row and four requests of a lane at a time.
 __global__ void __launch_bounds__(256) vocab_amax_kernel(const VocabPrep a) {
   __shared__ float sm[8];
   op_pdl_wait();
@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(256) vocab_amax_kernel(const VocabPrep a) {
   const int blk = blockIdx.x % kVocabAmaxBlocks;
   const float* x = of_w ? static_cast<const float*>(a.W) + (a.w_groups > 1 ? g : 0) * a.w_group : static_cast<const float*>(a.H) + g * a.h_group;
   const int64_t rows = of_w ? a.V : a.T, pitch = of_w ? a.w_row : a.h_row;
+  const bool vec = (of_w ? a.vec_w : a.vec_h) != 0;
   float most = 0.f;
   for (int64_t r = blk * 8 + warp; r < rows; r += kVocabAmaxBlocks * 8) {
     if (!of_w) {
@@ -88,40 +89,69 @@ __global__ void __launch_bounds__(256) vocab_amax_kernel(const VocabPrep a) {
       if (y < 0 || y >= a.V) continue;
     }
     const float* row = x + r * pitch;
-    for (int c = lane; c < a.D; c += 32) most = fmaxf(most, finite_abs(row[c]));
+    const int wide = vec ? a.D & ~3 : 0;
+    for (int c0 = 0; c0 < wide; c0 += 512) {
+      float4 f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = c0 + (j * 32 + lane) * 4;
+        f[j] = c < wide ? *reinterpret_cast<const float4*>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = fmaxf(fmaxf(fmaxf(most, finite_abs(f[j].x)), fmaxf(finite_abs(f[j].y), finite_abs(f[j].z))), finite_abs(f[j].w));
+    }
+    for (int c0 = wide; c0 < a.D; c0 += 128) {
+      float f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = c0 + j * 32 + lane < a.D ? row[c0 + j * 32 + lane] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = fmaxf(most, finite_abs(f[j]));
+    }
   }
   most = vocab_block_max(most, sm);
   if (threadIdx.x == 0) a.amax[(g * 2 + of_w) * kVocabAmaxBlocks + blk] = most;
 }
 
-// A row of D elements into operand rows (of one plane or two), a warp's lanes eight elements each.
+// A row of D elements into operand rows (of one plane or two), a warp's lanes eight elements each, several pieces in flight.
 template <int TY, bool VEC>
 __device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* from, uint16_t* hi, uint16_t* lo, int D, float scale, int lane) {
-  for (int c = lane * 8; c < D; c += 256) {
-    const int n = min(8, D - c);
-    uint4 u, w = make_uint4(0, 0, 0, 0);
-    if constexpr (TY == PRSGD_TYPE_FP32) {
-      float v[8];
-      load8<TY, VEC>(from + c, n, v);
-      __half* p = reinterpret_cast<__half*>(&u);
-      __half* q = reinterpret_cast<__half*>(&w);
+  using T = typename ElemOf<TY>::type;
+  constexpr int kAhead = TY == PRSGD_TYPE_FP32 ? 2 : 4;
+  for (int c0 = lane * 8; c0 < D; c0 += 256 * kAhead) {
+    Raw8<TY> r[kAhead];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = v[i] * scale;
-        p[i] = __float2half_rn(x);
-        q[i] = __float2half_rn(x - __half2float(p[i]));
+    for (int j = 0; j < kAhead; ++j) {
+      const int c = c0 + j * 256;
+      if (VEC && c + 8 <= D) {
+        r[j] = load_raw<TY>(from + c);
+      } else {
+        T* e = reinterpret_cast<T*>(&r[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = c + i < D ? from[c + i] : from_f32<T>(0.f);
       }
-      *reinterpret_cast<uint4*>(lo + c) = w;
-    } else if (VEC && n == 8) {
-      u = *reinterpret_cast<const uint4*>(from + c);
-    } else {
-      u = make_uint4(0, 0, 0, 0);
-      typename ElemOf<TY>::type* p = reinterpret_cast<typename ElemOf<TY>::type*>(&u);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = from[c + i];
     }
-    *reinterpret_cast<uint4*>(hi + c) = u;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int c = c0 + j * 256;
+      if (c >= D) break;
+      if constexpr (TY == PRSGD_TYPE_FP32) {
+        float v[8];
+        unpack8<TY>(r[j], v);
+        uint4 u, w;
+        __half* p = reinterpret_cast<__half*>(&u);
+        __half* q = reinterpret_cast<__half*>(&w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = v[i] * scale;
+          p[i] = __float2half_rn(x);
+          q[i] = __float2half_rn(x - __half2float(p[i]));
+        }
+        *reinterpret_cast<uint4*>(hi + c) = u;
+        *reinterpret_cast<uint4*>(lo + c) = w;
+      } else {
+        *reinterpret_cast<uint4*>(hi + c) = r[j].q[0];
+      }
+    }
   }
 }
 
@@ -138,10 +168,16 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
   const int64_t g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int eh = 0, ew = 0;
-  if constexpr (TY == PRSGD_TYPE_FP32) {
+  if constexpr (TY == PRSGD_TYPE_FP32) {                   // (every warp by itself)
     const float* m = a.amax + g * 2 * kVocabAmaxBlocks;
-    eh = vocab_exponent(vocab_block_max(threadIdx.x < kVocabAmaxBlocks ? m[threadIdx.x] : 0.f, smf), 14);
-    ew = vocab_exponent(vocab_block_max(threadIdx.x < kVocabAmaxBlocks ? m[kVocabAmaxBlocks + threadIdx.x] : 0.f, smf), 14);
+    float h = fmaxf(m[lane], m[lane + 32]), w = fmaxf(m[lane + 64], m[lane + 96]);
+    static_assert(kVocabAmaxBlocks == 64);
+    for (int o = 16; o > 0; o >>= 1) {
+      h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, o));
+      w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, o));
+    }
+    eh = vocab_exponent(h, 14);
+    ew = vocab_exponent(w, 14);
   }
   if ((int)blockIdx.x >= a.h_blocks) {                     // ---- W
     if (g >= a.w_groups) return;
@@ -188,7 +224,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
       a.scale[g] = s;
     }
     if (a.grad) {
-      const int64_t last = min((int64_t)(all + 63) / 64 * 64, a.Tp);
+      const int64_t last = min((int64_t)(all + 63) / 64 * 64, a.T);      // (behind T the tensor maps read zeros)
       for (int64_t r = all + warp; r < last; r += 8)
         for (int c = lane * 8; c < a.pitch; c += 256) {
           const int64_t o = (g * a.Tp + r) * a.pitch + c;
@@ -310,24 +346,40 @@ struct VocabSum {
   int parts, acc_pitch, D;
   void* dH; int64_t dh_row, dh_group;
 };
-template <int TY, bool VEC>
+// SHARED: the warps of a block take every eighth part of one row, else a row each.
+template <int TY, bool VEC, bool SHARED>
 __global__ void __launch_bounds__(256) vocab_sum_kernel(const VocabSum a) {
   using T = typename ElemOf<TY>::type;
+  __shared__ float sums[SHARED ? 8 : 1][SHARED ? 256 : 1];
   op_pdl_wait();
   op_pdl_trigger();
   const int64_t g = blockIdx.z;
-  const int c = ((int)blockIdx.y * 32 + (threadIdx.x & 31)) * 8, live = a.live[g];
-  if (c >= a.D) return;
-  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < live; r += (int64_t)gridDim.x * 8) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = ((int)blockIdx.y * 32 + lane) * 8, live = a.live[g];
+  const int64_t step = a.Tp * a.acc_pitch;
+  for (int64_t r = SHARED ? blockIdx.x : (int64_t)blockIdx.x * 8 + warp; r < live; r += (int64_t)gridDim.x * (SHARED ? 1 : 8)) {
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v[8];
     const float* from = a.acc + (g * a.parts * a.Tp + r) * a.acc_pitch + c;
+    if (c < a.D) {
 #pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-      load8<PRSGD_TYPE_FP32, true>(from + (int64_t)p * a.Tp * a.acc_pitch, 8, v);
+      for (int p = SHARED ? warp : 0; p < a.parts; p += SHARED ? 8 : 1) {
+        unpack8<PRSGD_TYPE_FP32>(load_raw<PRSGD_TYPE_FP32>(from + p * step), v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+      }
     }
-    store8<TY, VEC>(static_cast<T*>(a.dH) + g * a.dh_group + a.index[g * a.Tp + r] * a.dh_row + c, min(8, a.D - c), sum);
+    if constexpr (SHARED) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sums[warp][i * 32 + lane] = sum[i];
+      __syncthreads();
+      if (warp == 0) {
+        for (int w = 1; w < 8; ++w)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[i] += sums[w][i * 32 + lane];
+      }
+      __syncthreads();
+      if (warp != 0) continue;
+    }
+    if (c < a.D) store8<TY, VEC>(static_cast<T*>(a.dH) + g * a.dh_group + a.index[g * a.Tp + r] * a.dh_row + c, min(8, a.D - c), sum);
   }
 }
 

@@ -28,7 +28,7 @@ constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kV
 // A tensor core cuts off what the running sum does not hold, 2^-24 of it a step of 16 on average and always towards zero: what has to be
 // exact to fp32 is summed in TMEM over this many blocks of 64 only, and those sums are added in registers, where they are rounded (stats at
 // 16384 x 131072 x 2048: off by 1.9e-6 with one sum, by 4.3e-7 with sums of 512 products, for 2 to 5 % of the time).
-__host__ __device__ constexpr int vt_promote(bool split) { return split ? 4 : 8; }
+constexpr int kVtPromote = 8;
 constexpr int kVtAhead = 8;                    // the next task is claimed when this many blocks of 64 of the current one are left to load
 enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE };
 enum { VT_STATS = 0, VT_G, VT_DH, VT_DW };
@@ -65,11 +65,11 @@ struct VocabChain {
 // contraction; seq = g * pieces + p and the place of that piece's G; live tokens of the group.
 struct VTask { int kind, g, ti, tj, n, p, seq, slot, live, k0, kb, pad; };
 
-// Sums of a tile: one, or (PROMOTE) one of the small products of pairs and one per vt_promote blocks.
+// Sums of a tile: one, or (PROMOTE) one of the small products of pairs and one per kVtPromote blocks.
 template <bool SPLIT, bool PROMOTE>
 __device__ __forceinline__ int vt_sums(int kb) {
   if (!PROMOTE) return 1;
-  return (SPLIT ? 1 : 0) + (kb + vt_promote(SPLIT) - 1) / vt_promote(SPLIT);
+  return (SPLIT ? 1 : 0) + (kb + kVtPromote - 1) / kVtPromote;
 }
 
 __device__ __forceinline__ int vt_tiles(int n) { return (n + 255) >> 8; }
@@ -308,7 +308,7 @@ __device__ __forceinline__ void vt_out64(const VOut& d, uint32_t box, int lane, 
 // SPLIT: fp32 operands, products of fp16 pairs.
 template <bool GRAD, bool SPLIT>
 __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
-  constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1, kPromote = vt_promote(SPLIT);
+  constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1;
   constexpr bool PROMOTE = SPLIT || !GRAD;               // (gradients of 16-bit types are rounded by far more)
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ unsigned char smem_raw[];
@@ -383,6 +383,9 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         const bool mn = GRAD && (k.kind == VT_DW || (second && k.kind == VT_DH));
         const int z = of_w ? wg : of_g ? k.slot : k.g;
         const bool swap = of_w && a.w_swap;
+        // tokens are the rows of A (but in dW): the half of a tile that has none is not loaded, what its sums hold goes nowhere
+        const bool half = k.kind != VT_DW && k.ti * 256 + 128 >= k.live, idle = half && rank == 1 && !second;
+        const uint32_t expect = 2 * kVtStageBytes - (half ? 16384u : 0u);
         if (issue && blocks == 0 && rank == 0 && !second) ptx::mbar_arrive(loaded);
         bool ok = true;
         for (int j = 0, b = 0; j < tiles && ok; ++j) {
@@ -399,13 +402,13 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
             for (int q = k0; q < k0 + kb; ++q, ++b) {
               if (!ptx::warp_wait(empty((int)s), phase, ab, status, VT_ERR_EMPTY)) { ok = false; break; }
               if (issue) {
-                if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kVtStageBytes);
+                if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), expect);
                 const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kVtStageBytes + (second ? 16384u : 0u);
                 if (mn) {
                   const int y = q0 + q * 64;
                   ptx::tma_load_3d_pair(at, map, fb, at0, swap ? z : y, swap ? y : z);
                   ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, swap ? z : y, swap ? y : z);
-                } else {
+                } else if (!idle) {
                   ptx::tma_load_3d_pair(at, map, fb, q * 64, swap ? z : at0, swap ? at0 : z);
                 }
                 if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           for (int q = 0; q < blocks; ++q) {
             const bool first = q == next;
             if (first) {
-              next = !PROMOTE ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + kPromote);
+              next = !PROMOTE ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + kVtPromote);
               acc = sums & 1u;
               if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, VT_ERR_ACC_FREE)) { ok = false; break; }
               ptx::tc_fence_after();
@@ -623,10 +626,11 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           float zs1 = 1.f, zs2 = 1.f;
           if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
           const float both = rp.z * sc->g, hot = rp.w * sc->g;
-          // the rows a product reads: up to the next multiple of 64, zeros behind the last live one
+          // the rows a product reads: up to the next multiple of 64 (behind the call's last token zeros are read in any case), zeros
+          // behind the last live one
           VOut d;
           d.type = PRSGD_TYPE_FP16; d.row = a.gp; d.index = nullptr; d.add = 0; d.vec = 1; d.cols = a.gp; d.reduce = 0;
-          d.rows = min(32, (k.live + 63) / 64 * 64 - r0);
+          d.rows = (int)min((int64_t)32, min(a.T, (int64_t)((k.live + 63) & ~63)) - r0);
           const int64_t o = ((int64_t)k.slot * a.Tp + r0) * a.gp;
           const bool some = d.rows > 0 && cu < a.gp;
           ok = gather();

@@ -148,7 +148,7 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   VocabMaps maps{};
   for (int i = 0; i < planes && rc == PRSGD_OK; ++i) {
     rc = vt_map(&maps.hk[i], a.Hc[i], D, a.Tp, G, a.pitch, a.Tp * a.pitch, 128, 1);
-    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], a.Hc[i], D, a.Tp, G, a.pitch, a.Tp * a.pitch, 64, 1);
+    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], a.Hc[i], D, a.T, G, a.pitch, a.Tp * a.pitch, 64, 1);
     const void* w = p.copy_w ? a.Wc[i] : a.W;
     const int64_t row = p.copy_w ? a.pitch : a.w_row, group = a.w_groups == 1 ? row : p.copy_w ? a.V * a.pitch : a.w_group;
     c.w_swap = a.w_groups > 1 && group < row;
@@ -159,7 +159,7 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
     }
     if (!p.grad) continue;
     if (rc == PRSGD_OK) rc = vt_map(&maps.gk[i], c.G[i], c.gp, a.Tp, c.slots, c.gp, a.Tp * c.gp, 128, 1);
-    if (rc == PRSGD_OK) rc = vt_map(&maps.gm[i], c.G[i], c.gp, a.Tp, c.slots, c.gp, a.Tp * c.gp, 64, 1);
+    if (rc == PRSGD_OK) rc = vt_map(&maps.gm[i], c.G[i], c.gp, a.T, c.slots, c.gp, a.Tp * c.gp, 64, 1);
   }
   if (rc != PRSGD_OK) return rc;
   // eight rows a block and turn, two rounds of blocks over all groups
@@ -301,10 +301,15 @@ int prsgd_vocab_loss_grad(const void* d_H, int64_t h_row_stride, int64_t h_group
     VocabSum s{};
     s.acc = c.acc; s.index = a.index; s.live = a.live; s.Tp = a.Tp; s.groups = groups; s.parts = c.parts; s.acc_pitch = c.acc_pitch; s.D = dim;
     s.dH = d_dH; s.dh_row = dh_row_stride; s.dh_group = dh_group_stride;
-    const dim3 grid((unsigned)std::min<int64_t>(up(tokens, 8), 65536), (unsigned)up(dim, 256), (unsigned)groups);
+    // eight rows a block, or, where they are few and their parts many, one whose parts the warps share
+    const bool shared = c.parts >= 8 && groups * tokens <= 1024;
+    const dim3 grid((unsigned)std::min<int64_t>(shared ? tokens : up(tokens, 8), 65536), (unsigned)up(dim, 256), (unsigned)groups);
     with_type(type, [&](auto ty) {
-      if (a.vec_dh) launch_pdl(vocab_sum_kernel<decltype(ty)::value, true>, grid, dim3(256), 0, st, s);
-      else launch_pdl(vocab_sum_kernel<decltype(ty)::value, false>, grid, dim3(256), 0, st, s);
+      constexpr int TY = decltype(ty)::value;
+      auto go = [&](auto kernel) { launch_pdl(kernel, grid, dim3(256), 0, st, s); };
+      if (shared) { if (a.vec_dh) go(vocab_sum_kernel<TY, true, true>); else go(vocab_sum_kernel<TY, false, true>); }
+      else if (a.vec_dh) go(vocab_sum_kernel<TY, true, false>);
+      else go(vocab_sum_kernel<TY, false, false>);
     });
   }
   return op_launched("vocab_loss_grad");
