@@ -21,7 +21,10 @@
 namespace prsgd {
 
 constexpr int kVtEpiWarps = 16, kVtThreads = 32 * (4 + kVtEpiWarps), kVtRing = 4;
-constexpr int kVtShares = kVtEpiWarps / 4;     // an epilogue warp takes 32 rows of a CTA's 128 x 256 sums and 64 columns
+// Epilogue warps take 32 rows of a CTA's 128 x 256 sums each.  Where sums are added in registers all sixteen share a tile, 64 columns each; else
+// eight take the tiles of one TMEM sum and eight those of the other, 128 columns each, so that one tile's stores run beside the next one's
+// exponentials (gradient, 256 x 256 tiles of G with D = 1024: 10.9 thousand cycles a tile, products 8.2).
+constexpr int kVtShares = kVtEpiWarps / 4;
 constexpr uint32_t kVtStageBytes = 32768, kVtWarpBytes = 4096;
 __host__ __device__ constexpr int vt_stages(bool grad) { return grad ? 5 : 6; }            // (the gradient's epilogue needs shared memory too)
 constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kVtStageBytes + (grad ? kVtEpiWarps * kVtWarpBytes : 0); }
@@ -232,46 +235,37 @@ __device__ __forceinline__ void vt_out32(const VOut& d, uint32_t box, int lane, 
   __syncwarp();
   const int c = c0 + (lane & 7) * 4;
   if (c >= d.cols) return;
-  int64_t o[8];
-  vt_rows(d, lane, o);
-  if (d.reduce) {
+  if (d.vec && c + 4 <= d.cols && d.type == PRSGD_TYPE_FP32) {
+    float* const out = static_cast<float*>(d.out) + c;
+    int64_t o[8];
+    vt_rows(d, lane, o);
+    if (d.reduce) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint4 u = ld_shared_v4(vt_chunk(box, 4 * i + (lane >> 3), lane & 7));
+        if (o[i] >= 0) vt_red4(out + o[i], u);
+      }
+      return;
+    }
+    float4 old[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) old[i] = d.add && o[i] >= 0 ? *reinterpret_cast<const float4*>(out + o[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint4 u = ld_shared_v4(vt_chunk(box, 4 * i + (lane >> 3), lane & 7));
-      if (o[i] >= 0) vt_red4(static_cast<float*>(d.out) + o[i] + c, u);
+      if (o[i] >= 0)
+        *reinterpret_cast<float4*>(out + o[i]) = make_float4(__uint_as_float(u.x) + old[i].x, __uint_as_float(u.y) + old[i].y, __uint_as_float(u.z) + old[i].z, __uint_as_float(u.w) + old[i].w);
     }
     return;
   }
-  const bool whole = d.vec && c + 4 <= d.cols && d.type == PRSGD_TYPE_FP32;
-#pragma unroll
-  for (int i = 0; i < 8; i += 4) {
-    float4 old[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      old[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (!d.add || o[i + j] < 0) continue;
-      if (whole) {
-        old[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(d.out) + o[i + j] + c);
-      } else {
-        float* e = reinterpret_cast<float*>(&old[j]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (c + k < d.cols) e[k] = vt_read1(d.out, d.type, o[i + j] + c + k);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint4 u = ld_shared_v4(vt_chunk(box, 4 * (i + j) + (lane >> 3), lane & 7));
-      if (o[i + j] < 0) continue;
-      const float4 w = make_float4(__uint_as_float(u.x) + old[j].x, __uint_as_float(u.y) + old[j].y, __uint_as_float(u.z) + old[j].z, __uint_as_float(u.w) + old[j].w);
-      if (whole) {
-        *reinterpret_cast<float4*>(static_cast<float*>(d.out) + o[i + j] + c) = w;
-      } else {
-        const float* e = reinterpret_cast<const float*>(&w);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (c + k < d.cols) vt_write1(d.out, d.type, o[i + j] + c + k, e[k]);
-      }
+#pragma unroll 1
+  for (int r = lane >> 3; r < d.rows; r += 4) {            // (in few instructions: code is fetched where others' is in use)
+    const int64_t o = (d.index ? (int64_t)d.index[r] : (int64_t)r) * d.row + c;
+#pragma unroll 1
+    for (int k = 0; k < 4 && c + k < d.cols; ++k) {
+      float w;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w) : "r"(vt_chunk(box, r, lane & 7) + 4u * (uint32_t)k) : "memory");
+      vt_write1(d.out, d.type, o + k, d.add ? w + vt_read1(d.out, d.type, o + k) : w);
     }
   }
 }
@@ -310,6 +304,7 @@ template <bool GRAD, bool SPLIT>
 __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
   constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1;
   constexpr bool PROMOTE = SPLIT || !GRAD;               // (gradients of 16-bit types are rounded by far more)
+  constexpr int kGroups = PROMOTE ? 1 : 2, kWarpCols = PROMOTE ? 64 : 128;
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kVtRing + 1];
@@ -332,7 +327,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
   if (threadIdx.x == 0) {
     ptx::mbar_init(loaded, 1);
     for (int s = 0; s < kStages; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(tfull(i), 1); ptx::mbar_init(tempty(i), 2 * kVtEpiWarps); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(tfull(i), 1); ptx::mbar_init(tempty(i), 2 * kVtEpiWarps / kGroups); }
     for (int i = 0; i < kVtRing; ++i) { ptx::mbar_init(sfull(i), 1); ptx::mbar_init(sempty(i), 2 * kVtEpiWarps + 5); }
     abort_flag = 0;
     ptx::fence_mbar_init();
@@ -368,6 +363,8 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
 
   // The load and product roles are walked by whole warps with one elected lane that issues, so that descriptors and addresses stay
   // in uniform registers.  The epilogue's sums take registers from them: 128 * 64 + 512 * 104 of the launch's 640 * 96.
+  // Every load warp of the pair has a part in every stage, rows without tokens included: one that only waited for stages to be free
+  // could fall two rounds behind, and would take the barrier's phase for another.
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 || warp == 3) {                          // ---- operand loads: warp 0 A, warp 3 B --------------------------
@@ -383,9 +380,6 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         const bool mn = GRAD && (k.kind == VT_DW || (second && k.kind == VT_DH));
         const int z = of_w ? wg : of_g ? k.slot : k.g;
         const bool swap = of_w && a.w_swap;
-        // tokens are the rows of A (but in dW): the half of a tile that has none is not loaded, what its sums hold goes nowhere
-        const bool half = k.kind != VT_DW && k.ti * 256 + 128 >= k.live, idle = half && rank == 1 && !second;
-        const uint32_t expect = 2 * kVtStageBytes - (half ? 16384u : 0u);
         if (issue && blocks == 0 && rank == 0 && !second) ptx::mbar_arrive(loaded);
         bool ok = true;
         for (int j = 0, b = 0; j < tiles && ok; ++j) {
@@ -402,13 +396,13 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
             for (int q = k0; q < k0 + kb; ++q, ++b) {
               if (!ptx::warp_wait(empty((int)s), phase, ab, status, VT_ERR_EMPTY)) { ok = false; break; }
               if (issue) {
-                if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), expect);
+                if (rank == 0 && !second) ptx::mbar_expect_tx(full((int)s), 2 * kVtStageBytes);
                 const uint32_t fb = ptx::cluster_map(full((int)s), 0), at = stage0 + s * kVtStageBytes + (second ? 16384u : 0u);
                 if (mn) {
                   const int y = q0 + q * 64;
                   ptx::tma_load_3d_pair(at, map, fb, at0, swap ? z : y, swap ? y : z);
                   ptx::tma_load_3d_pair(at + 8192u, map, fb, at0 + 64, swap ? z : y, swap ? y : z);
-                } else if (!idle) {
+                } else {
                   ptx::tma_load_3d_pair(at, map, fb, q * 64, swap ? z : at0, swap ? at0 : z);
                 }
                 if (b == ask && rank == 0 && !second) ptx::mbar_arrive(loaded);
@@ -508,9 +502,9 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
     }
   } else {                                               // ---- epilogue ---------------------------------------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    const int quarter = warp & 3, share = (warp - 4) >> 2;
+    const int quarter = warp & 3, group = PROMOTE ? 0 : (warp - 4) >> 3, share = ((warp - 4) >> 2) & (kVtShares / kGroups - 1);
     const uint32_t box = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * 64);
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kWarpCols);
     uint32_t sums = 0;
     for (int n = 0;; ++n) {
       const VTask k = next_task(n);
@@ -529,7 +523,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
       };
       auto gather = [&]() -> bool {
         if (!PROMOTE || parts == 1) {
-          acc = sums & 1u;
+          acc = sums & 1u;                               // (one group: the sum is its own)
           if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
           ++sums;
           ptx::tc_fence_after();
@@ -556,6 +550,11 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         ptx::tmem_st32(lanes + acc * 256u, total[0]);
         ptx::tmem_st32(lanes + acc * 256u + 32u, total[1]);
         ptx::tmem_st_wait();
+        return true;
+      };
+      auto others = [&]() -> bool {                      // a tile of the other group
+        if (kGroups == 1 || (sums & 1u) == (uint32_t)group) return false;
+        ++sums;
         return true;
       };
       auto half = [&](int h, float (&v)[32]) {
@@ -618,67 +617,71 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         }
       } else {
         if (k.kind == VT_G) {
-          const int row = r0 + lane, cu = k.tj * 256 + share * 64;
-          const bool on = row < k.live;
-          const int64_t at = (int64_t)k.g * a.Tp + row, v0 = (int64_t)k.p * a.piece + cu;
-          const float4 rp = on ? a.rowp[at] : make_float4(0.f, 0.f, 0.f, 0.f);
-          const int y = on ? a.rowy[at] : -1;
-          float zs1 = 1.f, zs2 = 1.f;
-          if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
-          const float both = rp.z * sc->g, hot = rp.w * sc->g;
-          // the rows a product reads: up to the next multiple of 64 (behind the call's last token zeros are read in any case), zeros
-          // behind the last live one
-          VOut d;
-          d.type = PRSGD_TYPE_FP16; d.row = a.gp; d.index = nullptr; d.add = 0; d.vec = 1; d.cols = a.gp; d.reduce = 0;
-          d.rows = (int)min((int64_t)32, min(a.T, (int64_t)((k.live + 63) & ~63)) - r0);
-          const int64_t o = ((int64_t)k.slot * a.Tp + r0) * a.gp;
-          const bool some = d.rows > 0 && cu < a.gp;
-          ok = gather();
-          if (!ok) break;
-          // (pairs: what the first rounding left goes through the box in a second round)
+          if (!others()) {
+            const int row = r0 + lane;
+            const bool on = row < k.live;
+            const int64_t at = (int64_t)k.g * a.Tp + row, piece0 = (int64_t)k.p * a.piece;
+            const float4 rp = on ? a.rowp[at] : make_float4(0.f, 0.f, 0.f, 0.f);
+            const int64_t y = on ? a.rowy[at] - piece0 : -1;       // its label's column of the piece
+            float zs1 = 1.f, zs2 = 1.f;
+            if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
+            const float both = rp.z * sc->g, hot = rp.w * sc->g;
+            // the rows a product reads: up to the next multiple of 64 (behind the call's last token zeros are read in any case), zeros
+            // behind the last live one
+            VOut d;
+            d.type = PRSGD_TYPE_FP16; d.row = a.gp; d.index = nullptr; d.add = 0; d.vec = 1; d.cols = a.gp; d.reduce = 0;
+            d.rows = (int)min((int64_t)32, min(a.T, (int64_t)((k.live + 63) & ~63)) - r0);
+            const int64_t o = ((int64_t)k.slot * a.Tp + r0) * a.gp, width = a.V - piece0;
+            ok = gather();
+            if (!ok) break;
+            // 64 columns through the box at a time (pairs: what the first rounding left goes in a second round)
+            constexpr int kRounds = SPLIT ? 2 : kWarpCols / 64;
 #pragma unroll 1
-          for (int plane = 0; plane < (SPLIT ? 2 : 1); ++plane) {
+            for (int round = 0; round < kRounds; ++round) {
+              const int unit = SPLIT ? 0 : round, cu = k.tj * 256 + share * kWarpCols + unit * 64;
+              const bool some = d.rows > 0 && cu < a.gp;
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-              const int64_t c0 = v0 + h * 32;
-              const int mine = (int)(y - c0), cols = on ? (int)max((int64_t)0, min((int64_t)32, a.V - c0)) : 0;
-              float v[32];
-              half(h, v);
-              if (h == 1 && plane == (SPLIT ? 1 : 0)) release();
-              if (!some) continue;
+              for (int h = 0; h < 2; ++h) {
+                const int c0 = cu + h * 32, cols = on ? (int)max((int64_t)0, min((int64_t)32, width - c0)) : 0;
+                const int64_t mine = y - c0;
+                float v[32];
+                half(unit * 2 + h, v);
+                if (h == 1 && round == kRounds - 1) release();
+                if (!some) continue;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float z = SPLIT ? v[i] * zs1 * zs2 : v[i];
-                v[i] = both * vt_exp2(((z - rp.x) - rp.y) * kLog2e);
-              }
-              if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] -= y >= 0 && mine == i ? hot : 0.f;
-              }
-              if (cols < 32) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : 0.f;
-              }
-              if (SPLIT && plane == 1) {
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                  const float2 f = unpack_half2(pack_half2(v[i], v[i + 1]));
-                  v[i] -= f.x; v[i + 1] -= f.y;
+                for (int i = 0; i < 32; ++i) {
+                  const float z = SPLIT ? v[i] * zs1 * zs2 : v[i];
+                  v[i] = both * vt_exp2(((z - rp.x) - rp.y) * kLog2e);
                 }
+                if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) v[i] -= y >= 0 && mine == i ? hot : 0.f;
+                }
+                if (cols < 32) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : 0.f;
+                }
+                if (SPLIT && round == 1) {
+#pragma unroll
+                  for (int i = 0; i < 32; i += 2) {
+                    const float2 f = unpack_half2(pack_half2(v[i], v[i + 1]));
+                    v[i] -= f.x; v[i + 1] -= f.y;
+                  }
+                }
+                vt_put32(SPLIT ? 0 : a.bf16, box, lane, h, v);
               }
-              vt_put32(SPLIT ? 0 : a.bf16, box, lane, h, v);
+              d.out = a.G[SPLIT ? round : 0] + o;
+              if (some) vt_out64(d, box, lane, cu);
             }
-            d.out = a.G[plane] + o;
-            if (some) vt_out64(d, box, lane, cu);
           }
         } else {
           const bool of_w = k.kind == VT_DW;
           const float s1 = of_w ? sc->dw1 : sc->dh1, s2 = of_w ? sc->dw2 : sc->dh2, s12 = s1 * s2;
-          const int cu = k.tj * 256 + share * 64;
           VOut d;
           d.cols = a.D; d.index = nullptr; d.reduce = 0;
 #pragma unroll 1
           for (int j = 0; j < (of_w ? k.n : 1); ++j) {
+            if (kb > 0 ? others() : kGroups == 2 && (j & 1) != group) continue;
             if (of_w) {
               const int rj = r0 + j * 256;               // first row of this warp's part of the tile
               const int64_t v0 = (int64_t)k.p * a.piece + rj, o = (int64_t)k.g * a.dw_group + v0 * a.dw_row;
@@ -699,24 +702,29 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
             }
             if (kb > 0) ok = gather();
             if (!ok) break;
-            const bool narrow = d.type != PRSGD_TYPE_FP32 && !d.add && d.vec, some = cu < a.D && d.rows > 0 && !(kb == 0 && d.add);
+            const bool narrow = d.type != PRSGD_TYPE_FP32 && !d.add && d.vec;
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-              float v[32];
-              if (kb > 0) {
-                half(h, v);
-                if (h == 1) release();
+            for (int unit = 0; unit < kWarpCols / 64; ++unit) {
+              const int cu = k.tj * 256 + share * kWarpCols + unit * 64;
+              const bool some = cu < a.D && d.rows > 0 && !(kb == 0 && d.add);
+#pragma unroll 1
+              for (int h = 0; h < 2; ++h) {
+                float v[32];
+                if (kb > 0) {
+                  half(unit * 2 + h, v);
+                  if (h == 1 && unit == kWarpCols / 64 - 1) release();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = SPLIT ? v[i] * s1 * s2 : v[i] * s12;
-              } else {
+                  for (int i = 0; i < 32; ++i) v[i] = SPLIT ? v[i] * s1 * s2 : v[i] * s12;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                  for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                }
+                if (!some) continue;
+                if (narrow) vt_put32(d.type == PRSGD_TYPE_BF16, box, lane, h, v);
+                else vt_out32(d, box, lane, cu + h * 32, v);
               }
-              if (!some) continue;
-              if (narrow) vt_put32(d.type == PRSGD_TYPE_BF16, box, lane, h, v);
-              else vt_out32(d, box, lane, cu + h * 32, v);
+              if (narrow && some) vt_out64(d, box, lane, cu);
             }
-            if (narrow && some) vt_out64(d, box, lane, cu);
           }
           if (!ok) break;
         }

@@ -324,6 +324,28 @@ def test_vocab_loss_grad(b, G, T, V, D, dtype, kind):
     assert untouched(dH, aH) and untouched(dW, aW)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("G,T,V,D", [(3, 2100, 17000, 40), (2, 9000, 9000, 72), (5, 300, 20000, 24), (40, 64, 1000, 128)])
+def test_vocab_loss_pieces(b, G, T, V, D, dtype):
+    """Several pieces of the vocabulary and groups whose G takes turns in its places; forty calls, each checked for an expired wait and for
+    the same bits."""
+    H, W, y = case(35, G, T, V, D, dtype)
+    y[0, : T // 2] = -1
+    got = b.prsgd_vocab_loss(H, W, y)
+    check_loss(got, H, W, y)
+    stats, dloss = exact_stats(H, W, y), randn(38, G, T)
+    work = b.vocab_loss_grad_workspace(H, W)
+    first = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, workspace=work)
+    for g in range(G):
+        one = slice(g, g + 1)
+        check_grad((first[0][one], first[1][one]), H[one], W[one], y[one], dloss[one], None)
+    dH, dW = torch.empty_like(H), torch.empty_like(W)
+    for n in range(40):
+        b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dH=dH, dW=dW, workspace=work)
+        b.prsgd_work_status(work)
+        assert torch.equal(dH, first[0]) and torch.equal(dW, first[1]), n
+
+
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("G,T,V,D", [(2, 130, 700, 500), (1, 20, 9000, 64)])
