@@ -33,7 +33,7 @@ constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kV
 // 16384 x 131072 x 2048: off by 1.9e-6 with one sum, by 4.3e-7 with sums of 512 products, for 2 to 5 % of the time).
 constexpr int kVtPromote = 8;
 constexpr int kVtAhead = 8;                    // the next task is claimed when this many blocks of 64 of the current one are left to load
-enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE };
+enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE, VT_ERR_MEET };
 enum { VT_STATS = 0, VT_G, VT_DH, VT_DW };
 
 struct VocabMaps {
@@ -311,7 +311,8 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
   __shared__ __align__(16) uint4 ring[3 * kVtRing];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
-  __shared__ float2 shares[GRAD ? 1 : 2][GRAD ? 1 : 128][kVtShares];
+  __shared__ float2 shares[GRAD ? 1 : 4][GRAD ? 1 : 128][kVtShares];
+  __shared__ __align__(8) uint64_t meet[4][4];
   const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = blockIdx.x & 1u;                 // clusters of two along x
@@ -329,6 +330,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
     for (int s = 0; s < kStages; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(tfull(i), 1); ptx::mbar_init(tempty(i), 2 * kVtEpiWarps / kGroups); }
     for (int i = 0; i < kVtRing; ++i) { ptx::mbar_init(sfull(i), 1); ptx::mbar_init(sempty(i), 2 * kVtEpiWarps + 5); }
+    for (int i = 0; i < 16; ++i) ptx::mbar_init(ptx::smem_u32(&meet[i >> 2][i & 3]), kVtShares - 1);
     abort_flag = 0;
     ptx::fence_mbar_init();
   }
@@ -606,14 +608,21 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           release();
         }
         if (!ok) break;
-        // The four warps that share the rows put theirs together: one pair of numbers a token and run.  (Places of alternate runs: a
-        // warp two runs on has passed a barrier that the reader of this one reached behind its reading.)
-        float2* const at = shares[n & 1][quarter * 32 + lane];
+        // The four warps that share the rows put theirs together: one pair of numbers a token and run.  Three leave theirs, the first waits
+        // for them (bounded).  A warp is at most two runs ahead of the first one, which has to release a run's sums before the products of the run
+        // after next are formed, so four places do.
+        float2* const at = shares[n & 3][quarter * 32 + lane];
         at[share] = make_float2(m, sum);
-        ptx::named_bar_sync(1 + quarter, 32 * kVtShares);
-        if (share == 0 && row < k.live) {
-          const float2 all = vocab_merge(vocab_merge(at[0], at[1]), vocab_merge(at[2], at[3]));
-          a.part[((int64_t)k.g * a.runs + k.p) * a.Tp + row] = all;
+        __syncwarp();
+        const uint32_t met = ptx::smem_u32(&meet[n & 3][quarter]);
+        if (share != 0) {
+          if (lane == 0) ptx::mbar_arrive(met);
+        } else {
+          if (!ptx::warp_wait(met, (uint32_t)((n >> 2) & 1), ab, status, VT_ERR_MEET)) break;
+          if (row < k.live) {
+            const float2 all = vocab_merge(vocab_merge(at[0], at[1]), vocab_merge(at[2], at[3]));
+            a.part[((int64_t)k.g * a.runs + k.p) * a.Tp + row] = all;
+          }
         }
       } else {
         if (k.kind == VT_G) {
