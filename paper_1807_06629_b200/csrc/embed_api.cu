@@ -33,6 +33,10 @@ EmbedGradArgs embed_grad_carve(int64_t groups, int64_t tokens, int64_t vocab, in
   while ((1ll << bits) < vocab) ++bits;
   a.passes = (bits + kSortBits - 1) / kSortBits;
   a.bits = (bits + a.passes - 1) / a.passes;
+  // as many blocks as have a turn each, so that up to 8192 tokens take one
+  a.ctas = 1;
+  while (a.ctas < kSortCtas && a.ctas * kSortTurn < tokens) a.ctas *= 2;
+  a.turns = (int)std::max<int64_t>(1, (tokens + a.ctas * kSortTurn - 1) / (a.ctas * kSortTurn));
   a.unit = embed_unit(groups, tokens, a.chunks);
   a.units = (int)((tokens + a.unit - 1) / a.unit);
   size_t off = 0;
@@ -54,7 +58,7 @@ int embed_prepare() {
   if (e == cudaSuccess && (dev < 0 || dev >= 64)) return op_fail(PRSGD_ERR_ARG, "device ordinal out of range");
   std::lock_guard<std::mutex> hold(lock);
   if (e == cudaSuccess && !known[dev]) {
-    auto raise = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(kSortShared)); };
+    auto raise = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSortSmem); };
     raise(embed_sort_kernel<PRSGD_TYPE_FP32, true>); raise(embed_sort_kernel<PRSGD_TYPE_BF16, true>); raise(embed_sort_kernel<PRSGD_TYPE_FP16, true>);
     raise(embed_sort_kernel<PRSGD_TYPE_FP32, false>); raise(embed_sort_kernel<PRSGD_TYPE_BF16, false>); raise(embed_sort_kernel<PRSGD_TYPE_FP16, false>);
     known[dev] = e == cudaSuccess;
@@ -134,18 +138,19 @@ int prsgd_embed_grad(const void* d_dout, int32_t type, int64_t row_stride, int64
     constexpr int OTY = decltype(oty)::value;
     auto both = [&](auto ov) {
       constexpr bool OV = decltype(ov)::value;
-      launch_pdl(embed_sort_kernel<OTY, OV>, dim3((unsigned)(groups + zeros)), dim3(1024), sort_smem(tokens), st, a);
+      const unsigned grid = (unsigned)((groups * a.ctas + zeros + a.ctas - 1) / a.ctas * a.ctas);
+      launch_pdl_cluster(embed_sort_kernel<OTY, OV>, dim3(grid), dim3(1024), kSortSmem, st, (unsigned)a.ctas, a);
       if (tokens == 0) return;
       // threads of a block: whole rows of lanes, fewer of them while that gives the GPU more blocks
       int threads = kRowThreads;
       while (threads > 64 && threads / 2 >= a.lanes && groups * a.units * a.lanes / threads < 148 * 4) threads /= 2;
       const int per = threads / a.lanes;
-      const dim3 grid((unsigned)((a.units + per - 1) / per), (unsigned)((a.chunks + a.lanes - 1) / a.lanes), (unsigned)groups);
+      const dim3 sum_grid((unsigned)((a.units + per - 1) / per), (unsigned)((a.chunks + a.lanes - 1) / a.lanes), (unsigned)groups);
       with_type(type, [&](auto ty) {
-        if (vec) launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, true, OV>, grid, dim3(threads), 0, st, a);
-        else launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, false, OV>, grid, dim3(threads), 0, st, a);
+        if (vec) launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, true, OV>, sum_grid, dim3(threads), 0, st, a);
+        else launch_pdl(embed_sum_kernel<decltype(ty)::value, OTY, false, OV>, sum_grid, dim3(threads), 0, st, a);
       });
-      if (a.units > 1) launch_pdl(embed_join_kernel<OTY, OV>, grid, dim3(threads), 0, st, a);
+      if (a.units > 1) launch_pdl(embed_join_kernel<OTY, OV>, sum_grid, dim3(threads), 0, st, a);
     };
     if (ovec) both(std::integral_constant<bool, true>());
     else both(std::integral_constant<bool, false>());

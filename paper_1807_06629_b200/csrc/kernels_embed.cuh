@@ -7,6 +7,7 @@
 // finished there, one that crosses a border leaves its parts in the workspace for a last launch that adds them in order.
 #pragma once
 #include "rows_io.cuh"
+#include "tc_ptx.cuh"
 
 namespace prsgd {
 
@@ -89,9 +90,9 @@ __global__ void __launch_bounds__(kRowThreads) embed_any_kernel(const EmbedArgs 
 
 // ---- gradient -------------------------------------------------------------------------------------------------
 constexpr int kSortBits = 9, kSortWarps = 32, kSortPitch = (1 << kSortBits) + 1;
-constexpr int kSortShared = 8192;                // tokens that are sorted in shared memory
+constexpr int kSortCtas = 8, kSortTurn = 32 * kSortWarps;            // most blocks that share a group's tokens; tokens of a block's turn
 constexpr size_t kSortCounts = ((size_t)kSortWarps * kSortPitch * 4 + 15) / 16 * 16;
-inline size_t sort_smem(int64_t tokens) { return kSortCounts + (tokens <= kSortShared ? 16 * (size_t)tokens : 0); }
+constexpr size_t kSortSmem = kSortCounts + (4 << kSortBits);
 
 struct EmbedGradArgs {
   const void* dout; int64_t row, group;
@@ -102,6 +103,7 @@ struct EmbedGradArgs {
   float scale;
   int accumulate;
   int passes, bits;                              // digits of an id; bits of a digit
+  int ctas, turns;                               // blocks (a cluster) that sort a group; 1024 tokens each they take at a time
   int unit, units;                               // sorted tokens of a unit; units of a group
   int lanes;                                     // threads side by side along a row; kRowThreads / lanes units share a block
   uint2* keys[2];                                // [groups][tokens] (id, token), sorted ones in keys[passes & 1]
@@ -110,42 +112,29 @@ struct EmbedGradArgs {
   DeviceStatus* status;
 };
 
-// Tokens of a group by id.  A warp takes an equal share of them, counts its digits, and places them behind those of smaller
-// digits and of earlier warps; within a warp's 32 the order is the lanes'.  Counted without atomics: the many equal digits of
-// frequent ids took turns.  Up to kSortShared tokens change places in shared memory.  Its loops are rolled: code that is run through once is
-// fetched anew at every launch, at about 20 cycles an instruction.
-__device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) {
+// Tokens of a group by id, by a cluster of blocks.  A warp takes an equal share of them, counts its digits, and places them behind those of smaller
+// digits, of earlier blocks and of earlier warps; within a warp's 32 the order is the lanes'.  Counted without atomics: the many
+// equal digits of frequent ids took turns.  Loops are rolled: code that is run through once is fetched anew at every launch, at about 20
+// cycles an instruction.  (8192 tokens, two digits: a block alone 18 us, of which 11 thousand cycles a digit went into the ballots of eight turns.)
+__device__ void embed_sort(const EmbedGradArgs& a, int64_t g, int cta, uint32_t* counts) {
   __shared__ uint32_t sums[kSortWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, digits = 1 << a.bits, turns = a.turns;
   const int32_t* ids = a.ids + g * a.tokens;
   uint32_t* mine = counts + warp * kSortPitch;
-  uint2* shared = reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(counts) + kSortCounts);
-  const bool in_shared = a.tokens <= kSortShared;
-  const int digits = 1 << a.bits;
-  const int turns = ((int)a.tokens + kSortWarps * 32 - 1) / (kSortWarps * 32);     // (the same for all warps and digits, and seen to be)
+  uint32_t* totals = reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(counts) + kSortCounts);    // of this block, read by the others
   int n = (int)a.tokens;
-  {                                              // (id, token), or (-1, ) for none
-    uint2* to = in_shared ? shared : a.keys[0] + g * a.tokens;
-#pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += 8192) {
-      int id[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = i0 + j * 1024 + (int)threadIdx.x;
-        id[j] = i < n ? ids[i] : -1;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = i0 + j * 1024 + (int)threadIdx.x;
-        if (i < n) to[i] = make_uint2(id[j] >= 0 && id[j] < a.vocab ? (uint32_t)id[j] : 0xFFFFFFFFu, (uint32_t)i);
-      }
-    }
-  }
   for (int p = 0; p < a.passes; ++p) {
-    uint2* from = in_shared ? shared + (p & 1) * a.tokens : a.keys[p & 1] + g * a.tokens;
-    uint2* to = in_shared && p + 1 < a.passes ? shared + ((p + 1) & 1) * a.tokens : a.keys[(p + 1) & 1] + g * a.tokens;
-    const int begin = min(n, warp * turns * 32), end = min(n, begin + turns * 32);
+    const uint2* from = a.keys[p & 1] + g * a.tokens;
+    uint2* to = a.keys[(p + 1) & 1] + g * a.tokens;
+    const int begin = min(n, (cta * kSortWarps + warp) * turns * 32), end = min(n, begin + turns * 32);
     auto digit = [&](uint2 k) { return (k.x >> (p * a.bits)) & (uint32_t)(digits - 1); };
+    auto get = [&](int turn) -> uint2 {          // (id, token), or (-1, ) for none
+      const int i = begin + turn * 32 + lane;
+      if (i >= end) return make_uint2(0xFFFFFFFFu, 0u);
+      if (p > 0) return __ldcg(from + i);        // (written by other blocks meanwhile)
+      const int id = ids[i];
+      return make_uint2(id >= 0 && id < a.vocab ? (uint32_t)id : 0xFFFFFFFFu, (uint32_t)i);
+    };
     for (int d = lane; d < digits; d += 32) mine[d] = 0;
     __syncthreads();
     auto place = [&](uint2 k) -> uint32_t {
@@ -164,86 +153,108 @@ __device__ void embed_sort(const EmbedGradArgs& a, int64_t g, uint32_t* counts) 
       __syncwarp();
       return at;
     };
+    uint2 key = make_uint2(0xFFFFFFFFu, 0u);     // of a single turn: kept, with its number among the warp's of its digit
+    uint32_t within = 0;
 #pragma unroll 1
     for (int turn = 0; turn < turns; ++turn) {
-      const int i = begin + turn * 32 + lane;
-      const uint2 k = i < end ? from[i] : make_uint2(0xFFFFFFFFu, 0u);
-      const uint32_t at = place(k);
-      if (in_shared && i < end) from[i].y = (k.y & 0xFFFFu) | at << 16;    // (below 8192 tokens, 256 of them a warp's)
+      key = get(turn);
+      within = place(key);
     }
     __syncthreads();
-    // exclusive sums, digit by digit and within one warp by warp: a thread takes half the warps of a digit
-    {
-      const int d = threadIdx.x >> 1, w0 = (threadIdx.x & 1) * (kSortWarps / 2);
-      uint32_t total = 0;
-      if (d < digits) {
+    // exclusive sums, digit by digit, within one block by block and warp by warp: a thread takes half the warps of a digit
+    const int d = threadIdx.x >> 1, w0 = (threadIdx.x & 1) * (kSortWarps / 2);
+    uint32_t part = 0, first_half = 0, before = 0, total = 0;
+    if (d < digits) {
 #pragma unroll 4
-        for (int w = 0; w < kSortWarps / 2; ++w) total += counts[(w0 + w) * kSortPitch + d];
+      for (int w = 0; w < kSortWarps / 2; ++w) part += counts[(w0 + w) * kSortPitch + d];
+    }
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, part, 1);
+    if (threadIdx.x & 1) first_half = other;
+    if (d < digits && (threadIdx.x & 1) == 0) totals[d] = part + other;
+    if (a.ctas == 1) {
+      total = part + other;
+    } else {
+      ptx::cluster_arrive_release();
+      ptx::cluster_wait_acquire();
+      uint32_t t[kSortCtas];
+#pragma unroll
+      for (int c = 0; c < kSortCtas; ++c) t[c] = d < digits && c < a.ctas ? ptx::ld_cluster_u32(ptx::cluster_map(ptx::smem_u32(totals + d), (uint32_t)c)) : 0u;
+#pragma unroll
+      for (int c = 0; c < kSortCtas; ++c) {
+        if (c < cta) before += t[c];
+        total += t[c];
       }
-      uint32_t run = total;
+    }
+    uint32_t run = threadIdx.x & 1 ? 0u : total;  // (a digit counted once)
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += up;
+    }
+    if (lane == 31) sums[warp] = run;
+    __syncthreads();
+    if (warp == 0) {
+      uint32_t s = sums[lane];
 #pragma unroll 1
       for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t up = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += up;
+        const uint32_t up = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += up;
       }
-      if (lane == 31) sums[warp] = run;
-      __syncthreads();
-      if (warp == 0) {
-        uint32_t s = sums[lane];
-#pragma unroll 1
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t up = __shfl_up_sync(0xffffffffu, s, o);
-          if (lane >= o) s += up;
-        }
-        sums[lane] = s;
-      }
-      __syncthreads();
-      run += (warp > 0 ? sums[warp - 1] : 0u) - total;
-      n = (int)sums[kSortWarps - 1];
-      if (d < digits) {
+      sums[lane] = s;
+    }
+    __syncthreads();
+    run += (warp > 0 ? sums[warp - 1] : 0u) - total + before + first_half;
+    n = (int)sums[kSortWarps - 1];
+    if (d < digits) {
 #pragma unroll 4
-        for (int w = 0; w < kSortWarps / 2; ++w) {
-          uint32_t* c = counts + (w0 + w) * kSortPitch + d;
-          const uint32_t here = *c;
-          *c = run;
-          run += here;
-        }
+      for (int w = 0; w < kSortWarps / 2; ++w) {
+        uint32_t* c = counts + (w0 + w) * kSortPitch + d;
+        const uint32_t here = *c;
+        *c = run;
+        run += here;
       }
     }
     __syncthreads();
+    if (turns == 1) {
+      if (key.x != 0xFFFFFFFFu) to[mine[digit(key)] + within] = key;
+    } else {
 #pragma unroll 1
-    for (int turn = 0; turn < turns; ++turn) {
-      const int i = begin + turn * 32 + lane;
-      const uint2 k = i < end ? from[i] : make_uint2(0xFFFFFFFFu, 0u);
-      if (in_shared) {
-        if (k.x != 0xFFFFFFFFu) to[mine[digit(k)] + (k.y >> 16)] = make_uint2(k.x, k.y & 0xFFFFu);
-      } else {
+      for (int turn = 0; turn < turns; ++turn) {
+        const uint2 k = get(turn);
         const uint32_t at = place(k);
         if (k.x != 0xFFFFFFFFu) to[at] = k;
       }
     }
-    __syncthreads();
+    // the next digit reads what all blocks have placed, and writes `totals` that others have read
+    if (a.ctas == 1) {
+      __syncthreads();
+    } else {
+      ptx::cluster_arrive_release();
+      ptx::cluster_wait_acquire();
+    }
   }
-  if (threadIdx.x == 0) a.live[g] = n;
+  if (cta == 0 && threadIdx.x == 0) a.live[g] = n;
 }
 
-// The first `groups` blocks sort; the others write zeros meanwhile, rows whose ids occur included (their sums follow).
+// The first groups * ctas blocks sort; the others write zeros meanwhile, rows whose ids occur included (their sums follow).
 template <int OTY, bool VEC>
 __global__ void __launch_bounds__(1024) embed_sort_kernel(const EmbedGradArgs a) {
   extern __shared__ uint32_t counts[];
   op_pdl_wait();
   op_pdl_trigger();
   if (blockIdx.x == 0 && threadIdx.x < sizeof(DeviceStatus) / 4) reinterpret_cast<unsigned int*>(a.status)[threadIdx.x] = 0u;
-  if (blockIdx.x < a.groups) {
-    embed_sort(a, blockIdx.x, counts);
+  const int64_t sorters = a.groups * a.ctas;
+  if (blockIdx.x < sorters) {                    // (whole clusters)
+    const int64_t g = blockIdx.x / a.ctas;
+    embed_sort(a, g, (int)(blockIdx.x - g * a.ctas), counts);
     return;
   }
   using O = typename ElemOf<OTY>::type;
   const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const int64_t rows = a.groups * a.vocab, blocks = gridDim.x - a.groups;
+  const int64_t rows = a.groups * a.vocab, blocks = gridDim.x - sorters;
   const int per = 1024 / a.lanes, sub = threadIdx.x / a.lanes, c0 = threadIdx.x - sub * a.lanes;
   if (sub >= per) return;
-  for (int64_t r = (blockIdx.x - a.groups) * per + sub; r < rows; r += blocks * per) {
+  for (int64_t r = (blockIdx.x - sorters) * per + sub; r < rows; r += blocks * per) {
     const int64_t g = r / a.vocab;
     O* to = static_cast<O*>(a.dtable) + g * a.t_group + (r - g * a.vocab) * a.t_row;
     for (int c = c0; c < a.chunks; c += a.lanes) store8<OTY, VEC>(to + c * 8, min(8, a.dim - c * 8), zero);

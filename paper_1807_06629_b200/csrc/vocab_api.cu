@@ -1,5 +1,6 @@
 // C entries of the cross entropy over a vocabulary.  See include/prsgd.h for the contract.
 #include <mutex>
+#include "kernels_vocab_few.cuh"
 #include "kernels_vocab_tc.cuh"
 
 using namespace prsgd;
@@ -96,6 +97,29 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
   return p;
 }
 
+// The loss of few tokens a group has its own form without tensor cores, where H fits in shared memory: up to two of 16-bit types (1 x 32000 x 1024, bf16:
+// one token 20 us against 27, two 24 against 27, four 30 against 27), up to four of fp32, which spares the copy of W as pairs (27 to 34
+// against 220).
+bool vocab_few(int type, int64_t T, int D) {
+  return T <= (type == PRSGD_TYPE_FP32 ? kFewTokens : 2) && (T <= 2 ? T : 4) * round_up(D, 8) * 4 <= kFewSmem;
+}
+
+VocabFew vocab_few_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned char* base, size_t* bytes) {
+  VocabFew a{};
+  a.T = (int)T; a.V = V; a.D = D; a.dp = (int)round_up(D, 8);
+  // as many blocks as run at a time by their registers: three an SM for one token, else two (four, in two rounds: 24 us for 20)
+  const int64_t turn = kFewWarps * kFewRows, most = std::max<int64_t>(1, 148 * (T <= 1 ? 3 : 2) / std::max<int64_t>(groups, 1));
+  a.per = up(up(V, turn), std::min(most, up(V, turn))) * turn;
+  a.blocks = (int)up(V, a.per);
+  size_t off = 0;
+  auto take = [&](size_t n) { unsigned char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
+  a.status = reinterpret_cast<DeviceStatus*>(take(sizeof(DeviceStatus)));
+  a.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * T * a.blocks));
+  a.zy = reinterpret_cast<float*>(take(4 * (size_t)groups * T));
+  *bytes = off;
+  return a;
+}
+
 // 16-bit values, box {64, box_y, box_z}, 128-byte swizzle; zeros beyond the edges
 int vt_map(CUtensorMap* m, const void* base, int64_t dx, int64_t dy, int64_t dz, int64_t sy, int64_t sz, int box_y, int box_z) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -128,6 +152,12 @@ int vocab_device(int* sms) {
     auto raise = [&](auto kernel, bool grad) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)vt_smem(grad)); };
     raise(vocab_chain_kernel<false, false>, false); raise(vocab_chain_kernel<false, true>, false);
     raise(vocab_chain_kernel<true, false>, true); raise(vocab_chain_kernel<true, true>, true);
+    auto few = [&](auto ty, auto nt) {
+      for (auto kernel : {vocab_few_kernel<decltype(ty)::value, true, decltype(nt)::value>, vocab_few_kernel<decltype(ty)::value, false, decltype(nt)::value>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+    };
+    for (int t : {PRSGD_TYPE_FP32, PRSGD_TYPE_BF16, PRSGD_TYPE_FP16})
+      with_type(t, [&](auto ty) { few(ty, std::integral_constant<int, 1>()); few(ty, std::integral_constant<int, 2>()); few(ty, std::integral_constant<int, 4>()); });
     if (e == cudaSuccess) known[dev] = n;
   }
   if (e != cudaSuccess) return op_fail(PRSGD_ERR_CUDA, std::string("vocab_loss: ") + cudaGetErrorString(e));
@@ -213,8 +243,10 @@ extern "C" {
 int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes) {
   if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
   const int rc = check_vocab(type, groups, tokens, vocab, dim);
-  if (rc == PRSGD_OK) *bytes = vocab_plan(type, groups, tokens, vocab, dim, w_aligned != 0, false, nullptr).bytes;
-  return rc;
+  if (rc != PRSGD_OK) return rc;
+  if (vocab_few(type, tokens, dim)) vocab_few_plan(groups, tokens, vocab, dim, nullptr, bytes);
+  else *bytes = vocab_plan(type, groups, tokens, vocab, dim, w_aligned != 0, false, nullptr).bytes;
+  return PRSGD_OK;
 }
 
 int prsgd_vocab_loss_grad_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes) {
@@ -235,6 +267,33 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
   if (rc == PRSGD_OK) rc = check_floats(d_labels, d_loss, d_stats, nullptr);
   if (rc != PRSGD_OK) return rc;
   if (!d_loss || !d_stats) return op_fail(PRSGD_ERR_ARG, "an output is NULL");
+  if (vocab_few(type, tokens, dim)) {
+    size_t need = 0;
+    VocabFew f = vocab_few_plan(groups, tokens, vocab, dim, static_cast<unsigned char*>(d_work), &need);
+    rc = check_work(d_work, work_bytes, need);
+    int sms = 0;
+    if (rc == PRSGD_OK) rc = vocab_device(&sms);
+    if (rc != PRSGD_OK) return rc;
+    f.H = d_H; f.h_row = h_row_stride; f.h_group = h_group_stride; f.W = d_W; f.w_row = w_row_stride; f.w_group = w_group_stride;
+    f.labels = d_labels; f.loss = d_loss; f.stats = d_stats;
+    const bool vec = rows_16(d_W, type, w_row_stride, w_group_stride);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const dim3 grid((unsigned)f.blocks, (unsigned)groups);
+    with_type(type, [&](auto ty) {
+      constexpr int TY = decltype(ty)::value;
+      auto go = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        const size_t smem = (size_t)NT * f.dp * 4;
+        if (vec) launch_pdl(vocab_few_kernel<TY, true, NT>, grid, dim3(32 * kFewWarps), smem, st, f);
+        else launch_pdl(vocab_few_kernel<TY, false, NT>, grid, dim3(32 * kFewWarps), smem, st, f);
+      };
+      if (tokens == 1) go(std::integral_constant<int, 1>());
+      else if (tokens == 2) go(std::integral_constant<int, 2>());
+      else go(std::integral_constant<int, 4>());
+    });
+    launch_pdl(vocab_few_join_kernel, dim3((unsigned)groups), dim3(128), 0, st, f);
+    return op_launched("vocab_loss");
+  }
   VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), false, static_cast<unsigned char*>(d_work));
   rc = check_work(d_work, work_bytes, p.bytes);
   if (rc != PRSGD_OK) return rc;

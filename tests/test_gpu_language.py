@@ -376,6 +376,23 @@ def test_vocab_loss_masked_values(b, dtype):
             assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("G,T,V,D", [(1, 1, 32000, 1024), (3, 2, 777, 1000), (2, 3, 5000, 130), (5, 4, 33, 7), (1, 5, 900, 64), (1, 4, 40, 9000), (600, 1, 50, 16)])
+def test_vocab_loss_few_tokens(b, G, T, V, D, dtype):
+    """One to five tokens a group, groups without any label among them."""
+    H, W, y = case(25, G, T, V, D, dtype)
+    if G > 1:
+        y[1] = -1
+        H[1] = float("nan")
+    work = b.vocab_loss_workspace(H, W).fill_(0xFF)
+    got = b.prsgd_vocab_loss(H, W, y, workspace=work)
+    b.prsgd_work_status(work)
+    check_loss(got, torch.where(ref.live_tokens(y, V)[..., None], H, 0), W, y)
+    wide = torch.zeros(G, V + 3, D + 5, dtype=dtype, device="cuda:0")
+    wide[:, :V, :D] = W
+    check_loss(b.prsgd_vocab_loss(H, wide[:, :V, :D], y), torch.where(ref.live_tokens(y, V)[..., None], H, 0), W, y)
+
+
 def test_vocab_loss_nan_stays_in_its_token(b):
     for dtype in (F32, BF16, F16):
         H, W, y = case(60, 2, 50, 300, 64, dtype, padded=False)
