@@ -191,6 +191,9 @@ __device__ __forceinline__ uint32_t vt_pack(int bf16, float x, float y) {
   }
   return pack_half2(x, y);
 }
+__device__ __forceinline__ float2 vt_unpack(int bf16, uint32_t u) {
+  return bf16 ? __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u)) : unpack_half2(u);
+}
 __device__ __forceinline__ void vt_write1(void* out, int type, int64_t o, float v) {
   if (type == PRSGD_TYPE_FP32) static_cast<float*>(out)[o] = v;
   else if (type == PRSGD_TYPE_BF16) static_cast<__nv_bfloat16*>(out)[o] = __float2bfloat16_rn(v);
@@ -255,6 +258,24 @@ __device__ __forceinline__ void vt_out32(const VOut& d, uint32_t box, int lane, 
       const uint4 u = ld_shared_v4(vt_chunk(box, 4 * i + (lane >> 3), lane & 7));
       if (o[i] >= 0)
         *reinterpret_cast<float4*>(out + o[i]) = make_float4(__uint_as_float(u.x) + old[i].x, __uint_as_float(u.y) + old[i].y, __uint_as_float(u.z) + old[i].z, __uint_as_float(u.w) + old[i].w);
+    }
+    return;
+  }
+  if (d.vec && c + 4 <= d.cols) {                          // 16-bit values that are added to
+    uint16_t* const out = static_cast<uint16_t*>(d.out) + c;
+    const int bf16 = d.type == PRSGD_TYPE_BF16;
+    int64_t o[8];
+    vt_rows(d, lane, o);
+    uint2 old[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) old[i] = d.add && o[i] >= 0 ? *reinterpret_cast<const uint2*>(out + o[i]) : make_uint2(0u, 0u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint4 u = ld_shared_v4(vt_chunk(box, 4 * i + (lane >> 3), lane & 7));
+      const float2 x = vt_unpack(bf16, old[i].x), y = vt_unpack(bf16, old[i].y);
+      if (o[i] >= 0)
+        *reinterpret_cast<uint2*>(out + o[i]) = make_uint2(vt_pack(bf16, __uint_as_float(u.x) + x.x, __uint_as_float(u.y) + x.y),
+                                                           vt_pack(bf16, __uint_as_float(u.z) + y.x, __uint_as_float(u.w) + y.y));
     }
     return;
   }

@@ -22,6 +22,7 @@ struct VocabPlan {
   VocabPrep prep{};
   VocabChain chain{};
   bool grad = false, split = false, copy_w = false;
+  int64_t tasks = 0;         // at most
   size_t bytes = 0;
 };
 
@@ -58,6 +59,7 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
     c.runs = (int)up(nv, c.run);
     c.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * c.runs * a.Tp));
     c.zy = reinterpret_cast<float*>(take(4 * (size_t)groups * a.Tp));
+    p.tasks = groups * tm * c.runs;
     a.n_counters = 1;
     a.counters = c.claim = reinterpret_cast<unsigned int*>(take(4));
     p.bytes = off;
@@ -87,6 +89,7 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
   c.lag = (int)std::max<int64_t>(1, std::min<int64_t>(seqs, up(2 * kPairs, tm * npv)));
   c.slots = (int)std::min<int64_t>(seqs, 2 * c.lag + 1);
   for (int i = 0; i < planes; ++i) c.G[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)c.slots * a.Tp * c.gp));
+  p.tasks = seqs * (tm * npv + up(npv, c.run_w) * td + tm * td * c.parts);
   c.acc_pitch = (int)round_up(D, 8);
   c.acc = reinterpret_cast<float*>(take(c.pieces * c.parts > 1 ? 4 * (size_t)groups * c.parts * a.Tp * c.acc_pitch : 0));
   if (c.pieces * c.parts == 1) c.acc = nullptr;
@@ -198,9 +201,7 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   a.w_blocks = p.copy_w ? (int)std::min<int64_t>(up(a.V, 8), most) : 0;
   if (p.split) launch_pdl(vocab_amax_kernel, dim3(2 * kVocabAmaxBlocks, (unsigned)G), dim3(256), 0, st, a);
   with_type(a.h_type, [&](auto ty) { launch_pdl(vocab_prep_kernel<decltype(ty)::value>, dim3((unsigned)(a.h_blocks + a.w_blocks), (unsigned)G), dim3(256), 0, st, a); });
-  const int64_t tm = up(a.T, 256), td = up(D, 256);
-  const int64_t tasks = p.grad ? G * c.pieces * (tm * (c.piece / 256) + (c.piece / 256) * td + tm * td * c.parts) : G * tm * c.runs;
-  const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, tasks));
+  const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, p.tasks));
   auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kVtThreads), vt_smem(p.grad), st, 2, maps, c); };
   if (p.grad && p.split) go(vocab_chain_kernel<true, true>);
   else if (p.grad) go(vocab_chain_kernel<true, false>);
@@ -215,6 +216,10 @@ int check_inputs(const void* H, int64_t hr, int64_t hg, const void* W, int64_t w
   if (rc != PRSGD_OK) return rc;
   if (labels == nullptr) return op_fail(PRSGD_ERR_ARG, "labels is NULL");
   return PRSGD_OK;
+}
+
+int check_tasks(int64_t tasks) {
+  return tasks < (1ll << 31) ? PRSGD_OK : op_fail(PRSGD_ERR_SIZE, "too many tiles in one call: take fewer tokens or classes");
 }
 
 int check_work(const void* work, size_t bytes, size_t need) {
@@ -295,7 +300,8 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
     return op_launched("vocab_loss");
   }
   VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), false, static_cast<unsigned char*>(d_work));
-  rc = check_work(d_work, work_bytes, p.bytes);
+  rc = check_tasks(p.tasks);
+  if (rc == PRSGD_OK) rc = check_work(d_work, work_bytes, p.bytes);
   if (rc != PRSGD_OK) return rc;
   VocabPrep& a = p.prep;
   set_inputs(a, d_H, h_row_stride, h_group_stride, d_W, w_row_stride, w_group_stride, type, d_labels);
@@ -343,7 +349,8 @@ int prsgd_vocab_loss_grad(const void* d_H, int64_t h_row_stride, int64_t h_group
   }
   if (!d_dH && !d_dW) return op_clear_status(d_work, work_bytes, cuda_stream);
   VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), true, static_cast<unsigned char*>(d_work));
-  rc = check_work(d_work, work_bytes, p.bytes);
+  rc = check_tasks(p.tasks);
+  if (rc == PRSGD_OK) rc = check_work(d_work, work_bytes, p.bytes);
   if (rc != PRSGD_OK) return rc;
   VocabPrep& a = p.prep;
   VocabChain& c = p.chain;

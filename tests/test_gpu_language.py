@@ -357,6 +357,34 @@ def test_vocab_loss_grad_into_fp32(b, G, T, V, D, dtype, accumulate):
     check_grad(b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dW=dW, accumulate=accumulate), H, W, y, dloss, None, before)
 
 
+@pytest.mark.parametrize("kind", LAYOUTS)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_vocab_loss_grad_added_to_16_bits(b, dtype, kind):
+    """One rounding of the sum: half of |before + sum|."""
+    G, T, V, D = 2, 130, 300, 100
+    H, W, y = case(45, G, T, V, D, dtype)
+    stats, dloss, before = exact_stats(H, W, y), randn(48, G, T), randn(49, G, V, D, dtype=dtype)
+    dW, around = layout(before, kind)
+    check_grad(b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dW=dW, accumulate=True), H, W, y, dloss, None, before)
+    assert untouched(dW, around)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [64, 65])
+@pytest.mark.parametrize("T", [1, 70])
+def test_vocab_loss_shared_weights(b, T, D, dtype):
+    """All groups' W is one array (group stride 0); each group has its own dW."""
+    H, W, y = case(46, 3, T, 400, D, dtype, padded=False)
+    W = W[:1].expand(3, 400, D)
+    got = b.prsgd_vocab_loss(H, W, y)
+    check_loss(got, H, W, y)
+    dloss = randn(47, 3, T)
+    dW = torch.empty(3, 400, D, dtype=dtype, device="cuda:0")
+    check_grad(b.prsgd_vocab_loss_grad(H, W, y, exact_stats(H, W, y), dloss=dloss, dW=dW), H, W, y, dloss, None)
+    with pytest.raises(b.PRSGDError, match="overlap"):
+        b.prsgd_vocab_loss_grad(H, W, y, got[1], dloss=dloss, dW=torch.empty(1, 400, D, dtype=dtype, device="cuda:0").expand(3, 400, D))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_vocab_loss_masked_values(b, dtype):
     """What padding tokens hold reaches nothing, whole groups of padding among them."""

@@ -112,6 +112,12 @@ def test_vocab_loss_grad_refusals(b):
         assert b.lib.prsgd_last_error(None)
     for kw in (dict(G=0), dict(T=0, acc=1), dict(T=0, dW=None)):
         assert loss_grad(b.lib, **{**dict(H=None, W=None, y=None, s=None, dH=None, work=None), **kw}) == OK
+    for call, size in ((loss, b.prsgd_vocab_loss_workspace_bytes), (loss_grad, b.prsgd_vocab_loss_grad_workspace_bytes)):
+        small = size(1, 2, 10, 100, 64, 1)                  # (of a W whose rows begin on 16-byte boundaries; these do not)
+        for kw in (dict(W=8194), dict(wr=65, wg=6500), dict(wg=6401)):
+            assert call(b.lib, bytes=small, **kw) == SIZE, kw
+    huge = dict(T=1 << 22, V=1 << 24, D=65536, hr=65536, wr=65536, hg=1 << 38, wg=1 << 40, dhr=65536, dwr=65536, dhg=1 << 38, dwg=1 << 40, bytes=1 << 62)
+    assert loss_grad(b.lib, **huge) == SIZE and b"tiles" in b.lib.prsgd_last_error(None)
     for fn in (b.lib.prsgd_vocab_loss_workspace_bytes, b.lib.prsgd_vocab_loss_grad_workspace_bytes):
         n = C.c_size_t()
         assert fn(1, 1, 1, 1, 1, 1, None) == ARG and fn(5, 1, 1, 1, 1, 1, C.byref(n)) == ARG and fn(1, 1, 1, 1, 0, 1, C.byref(n)) == ARG
