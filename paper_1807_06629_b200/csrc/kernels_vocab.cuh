@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
     return;
   }
   const int32_t* labels = a.labels + g * a.T;
-  const int64_t per = (a.T + a.h_blocks - 1) / a.h_blocks, begin = blockIdx.x * per, end = min(a.T, begin + per);
+  const int64_t per = (a.T + a.h_blocks - 1) / a.h_blocks, begin = min(a.T, blockIdx.x * per), end = min(a.T, begin + per);
   auto is_live = [&](int y) { return y >= 0 && y < a.V; };
   int before = 0;
   for (int64_t t = threadIdx.x; t < begin; t += 256) before += is_live(labels[t]) ? 1 : 0;

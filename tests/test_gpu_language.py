@@ -404,6 +404,20 @@ def test_vocab_loss_masked_values(b, dtype):
             assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
 
 
+@pytest.mark.parametrize("T", [1185, 9473, 11887])
+def test_vocab_loss_tokens_that_leave_blocks_without_any(b, T):
+    """Lengths whose equal shares of tokens end before the last of the blocks that move them together; the labels end where their memory does."""
+    V, D = 50, 16
+    room = torch.full((1 << 19,), 2, dtype=torch.int32, device="cuda:0")
+    y = room[-T:].view(1, T)
+    y.copy_(tokens(23, 1, T, V))
+    H, W = randn(21, 1, T, D, dtype=BF16), randn(22, 1, V, D, dtype=BF16)
+    got = b.prsgd_vocab_loss(H, W, y)
+    check_loss(got, H, W, y)
+    dloss = randn(24, 1, T)
+    check_grad(b.prsgd_vocab_loss_grad(H, W, y, got[1], dloss=dloss), H, W, y, dloss, None)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("G,T,V,D", [(1, 1, 32000, 1024), (3, 2, 777, 1000), (2, 3, 5000, 130), (5, 4, 33, 7), (1, 5, 900, 64), (1, 4, 40, 9000), (600, 1, 50, 16)])
 def test_vocab_loss_few_tokens(b, G, T, V, D, dtype):
