@@ -600,7 +600,8 @@ int prsgd_embed_grad(const void* d_dout, int32_t type, int64_t row_stride, int64
  * DEVICE pointer to a counter (a captured graph draws anew at each replay when the caller advances it), or NULL for 0.
  * The gradient with respect to x is the same call with the gradient in x's place and no residual; that of the residual
  * is the gradient itself.  A dropped element is 0 (+ residual) whatever x holds.  x, residual (or NULL) and out have one type;
- * out may be x or the residual themselves (same strides, else the call is refused).  p in [0, 1 - 2^-17]. */
+ * out may be x or the residual themselves (same strides, else the call is refused); it may share no memory with them in another way.
+ * p in [0, 1 - 2^-17]. */
 int prsgd_dropout(const void* d_x, int32_t type, int64_t row_stride, int64_t group_stride,
                   const void* d_residual, int64_t residual_row_stride, int64_t residual_group_stride,
                   void* d_out, int64_t out_row_stride, int64_t out_group_stride,
@@ -625,8 +626,8 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
 
 /* Gradient of sum dloss_t loss_t + sum dlse_t lse_t (lse the sum of the stats) with respect to H and W:
  *   G_tv = (dloss_t + dlse_t) e^(z_tv - lse_t) - dloss_t [v = y_t],   dH = G W,   dW = G^T H (or, accumulate, added to what dW holds).
- * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is held in the type of the operands (fp32:
- * as pairs), a piece of the vocabulary at a time.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
+ * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is held with one rounding of the operands' type
+ * (fp32: as pairs; none for one or two tokens a group), a piece of the vocabulary at a time.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
  * whose label is padding take no part: their rows of dH are zeros, whatever their H, stats, dloss and dlse hold.  The rows of dH and of dW may
  * not overlap (W shared by all groups has one gradient: call with groups = 1 and the groups' tokens behind one another);
  * neither may share memory with another array of the call. */

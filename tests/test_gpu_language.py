@@ -404,6 +404,30 @@ def test_vocab_loss_masked_values(b, dtype):
             assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("G,T,V,D", [(1, 1, 32000, 1024), (3, 2, 777, 1000), (2, 2, 500, 130), (5, 1, 33, 7), (1, 2, 900, 2048), (1, 2, 70, 2056), (300, 1, 50, 16), (2, 1, 1, 1)])
+def test_vocab_loss_grad_few_tokens(b, G, T, V, D, dtype, wide):
+    """One or two tokens a group, groups without any label among them; rows of any stride; added to fp32 and to W's type."""
+    H, W, y = case(26, G, T, V, D, dtype, "wide" if wide else "dense")
+    if G > 1:
+        y[1] = -1
+        H[1] = float("nan")
+    stats, dloss, dlse = exact_stats(torch.where(ref.live_tokens(y, V)[..., None], H, 0), W, y), randn(27, G, T), randn(28, G, T) * 0.1
+    Hz = torch.where(ref.live_tokens(y, V)[..., None], H, 0)
+    work = b.vocab_loss_grad_workspace(H, W).fill_(0xFF)
+    dH, dW = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dlse=dlse, workspace=work)
+    b.prsgd_work_status(work)
+    check_grad((dH, dW), Hz, W, y, dloss, dlse)
+    only = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dlse=dlse, want_dW=False)[0], b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dlse=dlse, want_dH=False)[1]
+    assert torch.equal(only[0], dH) and torch.equal(only[1], dW)
+    for kind in {dtype, F32}:
+        before = randn(29, G, V, D, dtype=kind)
+        to, around = layout(before, "wide" if wide else "odd")
+        check_grad(b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dlse=dlse, dW=to, accumulate=True), Hz, W, y, dloss, dlse, before)
+        assert untouched(to, around)
+
+
 @pytest.mark.parametrize("T", [1185, 9473, 11887])
 def test_vocab_loss_tokens_that_leave_blocks_without_any(b, T):
     """Lengths whose equal shares of tokens end before the last of the blocks that move them together; the labels end where their memory does."""
