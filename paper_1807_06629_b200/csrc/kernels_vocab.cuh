@@ -3,25 +3,20 @@
 // The tokens that have a label are moved together: row c of the operand H' of a group is its c-th live token (index[c] in the
 // call's order).  Padding then costs nothing in the products, whatever its rows hold reaches nothing, and the copy (4 D
 // bytes a token beside 2 V D operations) brings any stride, alignment and type to one form: rows of 16-bit values on 16-byte
-// boundaries.  fp32 operands become pairs of fp16 values (hi, and lo = what hi rounded off) of x 2^e, e per group such that the
-// largest finite magnitude lies in [2^14, 2^15): 22 bits, nothing below 2^-39 of that largest.  W is read where it lies unless
-// it is fp32 or its rows do not begin on 16-byte boundaries; then it is copied the same way.
+// boundaries.  W is read where it lies unless it is fp32 or its rows do not begin on 16-byte boundaries; then it is copied the same way.
+//
+// fp32 operands become pairs of fp16 values (hi, and lo = what hi rounded off) of x 2^e, e such that the largest finite magnitude lies
+// in [2^14, 2^15): 22 bits, nothing below 2^-39 of that largest.  Each operand is scaled along the axis that its product keeps, so
+// that a row or column of any size spoils no other: H and W by rows for the logits, and, in copies of their own for the gradient, W by
+// columns (dH = G W) and H, its rows times their share of the gradient, by columns (dW = G^T H).  G_t is held times 2^g_t, such that
+// |dloss_t| + |dlse_t| lies in [2^13, 2^14); that share is 2^-g_t.
 #pragma once
 #include "rows_io.cuh"
 
 namespace prsgd {
 
-constexpr int kVocabAmaxBlocks = 64;           // partial maxima per group and operand
-
-// Factors of a group, two for each power of two that may lie outside a float's range.
-struct VocabScale {
-  float z1, z2;              // logit = sum * z1 * z2
-  float g;                   // G is held times g
-  float dh1, dh2;            // dH = sum * dh1 * dh2
-  float dw1, dw2;
-  float h, w;                // operands are held times these
-  float pad[7];
-};
+// Factors of a group of 16-bit types: G is held times g, dH and dW are sums * back.
+struct VocabScale { float g, back; };
 
 struct VocabPrep {
   const void* H; int64_t h_row, h_group;
@@ -34,12 +29,20 @@ struct VocabPrep {
   int64_t Tp;                // rows of H' (T rounded up to 64)
   int pitch;                 // elements of an operand row (D rounded up to 8)
   int w_groups;              // groups of W (1: shared)
-  uint16_t* Hc[2]; uint16_t* Wc[2];            // [groups][Tp][pitch], [w_groups][V][pitch] or nullptr
+  uint16_t* Hc[2]; uint16_t* Wc[2];            // [groups][Tp][pitch], [w_groups][V][pitch] or nullptr (pairs: scaled by rows)
+  // fp32 operands only: factors that undo the scales, two powers of two each (their product may lie outside a float's range)
+  float2* rowf; float2* colf;                  // [groups][Tp], [w_groups][Vp] of the rows of H' and W
+  // and the gradient's
+  uint16_t* Hm[2]; uint16_t* Wm[2];            // as Hc and Wc, scaled by columns
+  float2* rowg;                                // [groups][Tp] of the rows of G
+  float2* dhf; float2* dwf;                    // [w_groups][Dp], [groups][Dp] of the columns of Wm and Hm
+  unsigned int* most;                          // [2][groups][Dp] largest finite magnitudes (bits) of those columns: W, H
+  int64_t Vp; int Dp;                          // V, D rounded up to 256
+  int most_h, most_w, most_rows;               // blocks that look for them in H and W, rows of one
   float4* rowp;              // [groups][Tp]: (max, log sum, dloss + dlse, dloss)
   int* rowy; int* index;     // [groups][Tp]: label; token
   int* live;                 // [groups]
   VocabScale* scale;         // [groups]
-  float* amax;               // [groups][2][kVocabAmaxBlocks]
   float* loss; float* out_stats;
   void* dH; int64_t dh_row, dh_group; int vec_dh;
   unsigned int* counters; int n_counters;
@@ -66,91 +69,158 @@ __device__ __forceinline__ int vocab_block_sum(int v, int* sm) {
   return v;
 }
 __device__ __forceinline__ float finite_abs(float x) { return fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.f; }
-// e with x 2^e in [2^top, 2^(top + 1)), 0 for x = 0; within a normal float's exponents
-__device__ __forceinline__ int vocab_exponent(float x, int top) { return x > 0.f ? max(-126, min(126, top - ilogbf(x))) : 0; }
-__device__ __forceinline__ void vocab_halves(int n, float& a, float& b) { a = exp2f((float)(n / 2)); b = exp2f((float)(n - n / 2)); }
-
-// Largest finite magnitudes of the live rows of H and of W (fp32 operands only), a warp a row and four requests of a lane at a time.
-__global__ void __launch_bounds__(256) vocab_amax_kernel(const VocabPrep a) {
-  __shared__ float sm[8];
-  op_pdl_wait();
-  op_pdl_trigger();
-  const int64_t g = blockIdx.y;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool of_w = blockIdx.x >= kVocabAmaxBlocks;
-  const int blk = blockIdx.x % kVocabAmaxBlocks;
-  const float* x = of_w ? static_cast<const float*>(a.W) + (a.w_groups > 1 ? g : 0) * a.w_group : static_cast<const float*>(a.H) + g * a.h_group;
-  const int64_t rows = of_w ? a.V : a.T, pitch = of_w ? a.w_row : a.h_row;
-  const bool vec = (of_w ? a.vec_w : a.vec_h) != 0;
-  float most = 0.f;
-  for (int64_t r = blk * 8 + warp; r < rows; r += kVocabAmaxBlocks * 8) {
-    if (!of_w) {
-      const int y = a.labels[g * a.T + r];
-      if (y < 0 || y >= a.V) continue;
-    }
-    const float* row = x + r * pitch;
-    const int wide = vec ? a.D & ~3 : 0;
-    for (int c0 = 0; c0 < wide; c0 += 512) {
-      float4 f[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int c = c0 + (j * 32 + lane) * 4;
-        f[j] = c < wide ? *reinterpret_cast<const float4*>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) most = fmaxf(fmaxf(fmaxf(most, finite_abs(f[j].x)), fmaxf(finite_abs(f[j].y), finite_abs(f[j].z))), finite_abs(f[j].w));
-    }
-    for (int c0 = wide; c0 < a.D; c0 += 128) {
-      float f[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = c0 + j * 32 + lane < a.D ? row[c0 + j * 32 + lane] : 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) most = fmaxf(most, finite_abs(f[j]));
-    }
-  }
-  most = vocab_block_max(most, sm);
-  if (threadIdx.x == 0) a.amax[(g * 2 + of_w) * kVocabAmaxBlocks + blk] = most;
+// e with x 2^e in [2^top, 2^(top + 1)) for finite x >= 0 by the exponent's bits, 126 at most (zeros and numbers below 2^-126 too)
+__device__ __forceinline__ int vocab_exponent(float x, int top) { return min(126, top + 127 - (int)(__float_as_uint(x) >> 23)); }
+__device__ __forceinline__ float vocab_power(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }       // -126 <= e <= 127
+__device__ __forceinline__ float2 vocab_halves(int n) { return make_float2(vocab_power(n / 2), vocab_power(n - n / 2)); }
+// Scale of a token's row of G, from what its gradients are, and its row's share of dW (none of a token without a gradient: its zeros must not meet
+// values that its scale sent beyond fp16).
+__device__ __forceinline__ int vocab_g_exponent(float dloss, float dlse) {
+  const float d = finite_abs(fabsf(dloss) + fabsf(dlse));
+  return d > 0.f ? vocab_exponent(d, 13) : 0;
+}
+__device__ __forceinline__ float vocab_share(float dloss, float dlse) {
+  return dloss == 0.f && dlse == 0.f ? 0.f : vocab_power(-vocab_g_exponent(dloss, dlse));
 }
 
-// A row of D elements into operand rows (of one plane or two), a warp's lanes eight elements each, several pieces in flight.
-template <int TY, bool VEC>
-__device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* from, uint16_t* hi, uint16_t* lo, int D, float scale, int lane) {
-  using T = typename ElemOf<TY>::type;
-  constexpr int kAhead = TY == PRSGD_TYPE_FP32 ? 2 : 4;
-  for (int c0 = lane * 8; c0 < D; c0 += 256 * kAhead) {
-    Raw8<TY> r[kAhead];
+__global__ void __launch_bounds__(256) vocab_zero_kernel(unsigned int* p, int64_t n) {
+  op_pdl_wait();
+  op_pdl_trigger();
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0u;
+}
+
+// Largest finite magnitudes of the columns of W and of the live rows of H times their share of the gradient (fp32 operands): a block takes
+// 128 columns of some rows, a warp every eighth of them, four requests of a lane at a time.
+__global__ void __launch_bounds__(256) vocab_columns_kernel(const VocabPrep a) {
+  __shared__ float sm[8][128];
+  op_pdl_wait();
+  op_pdl_trigger();
+  const int64_t g = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (int)blockIdx.y * 128 + lane * 4;
+  const bool of_w = (int)blockIdx.x >= a.most_h;
+  if (of_w && g >= a.w_groups) return;
+  const float* x = of_w ? static_cast<const float*>(a.W) + g * a.w_group : static_cast<const float*>(a.H) + g * a.h_group;
+  const int64_t begin = (int64_t)(blockIdx.x - (of_w ? a.most_h : 0)) * a.most_rows, end = min(of_w ? a.V : a.T, begin + a.most_rows);
+  const int64_t pitch = of_w ? a.w_row : a.h_row;
+  const bool vec = (of_w ? a.vec_w : a.vec_h) != 0 && c + 4 <= a.D;
+  float most[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t r0 = begin + warp; r0 < end; r0 += 32) {
+    float f[4][4], share[4];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int c = c0 + j * 256;
-      if (VEC && c + 8 <= D) {
-        r[j] = load_raw<TY>(from + c);
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = r0 + 8 * j;
+      share[j] = r < end ? 1.f : 0.f;
+      if (!of_w && r < end) {
+        const int64_t t = g * a.T + r;
+        const int y = a.labels[t];
+        const float dl = a.dloss ? a.dloss[t] : 0.f, ds = a.dlse ? a.dlse[t] : 0.f;
+        share[j] = y >= 0 && y < a.V ? vocab_share(dl, ds) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[j][i] = 0.f;
+      if (share[j] == 0.f) continue;
+      const float* from = x + r * pitch + c;
+      if (vec) {
+        const float4 q = *reinterpret_cast<const float4*>(from);
+        f[j][0] = q.x; f[j][1] = q.y; f[j][2] = q.z; f[j][3] = q.w;
       } else {
-        T* e = reinterpret_cast<T*>(&r[j]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = c + i < D ? from[c + i] : from_f32<T>(0.f);
+        for (int i = 0; i < 4; ++i)
+          if (c + i < a.D) f[j][i] = from[i];
       }
     }
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most[i] = fmaxf(most[i], finite_abs(f[j][i] * share[j]));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sm[warp][lane * 4 + i] = most[i];
+  __syncthreads();
+  if (threadIdx.x >= 128) return;
+  float m = sm[0][threadIdx.x];
+  for (int w = 1; w < 8; ++w) m = fmaxf(m, sm[w][threadIdx.x]);
+  if (m > 0.f) atomicMax(a.most + ((of_w ? 0 : a.groups) + g) * a.Dp + (int64_t)blockIdx.y * 128 + threadIdx.x, __float_as_uint(m));      // (order of no matter)
+}
+
+// A row of D elements into an operand row, a warp's lanes eight elements each, several pieces in flight.
+constexpr int kVocabAhead = 4;
+template <int TY, bool VEC>
+__device__ __forceinline__ void vocab_load_row(const typename ElemOf<TY>::type* from, int c0, int D, Raw8<TY> (&r)[kVocabAhead]) {
+  using T = typename ElemOf<TY>::type;
+#pragma unroll
+  for (int j = 0; j < kVocabAhead; ++j) {
+    const int c = c0 + j * 256;
+    if (VEC && c + 8 <= D) {
+      r[j] = load_raw<TY>(from + c);
+    } else {
+      T* e = reinterpret_cast<T*>(&r[j]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = c + i < D ? from[c + i] : from_f32<T>(0.f);
+    }
+  }
+}
+template <int TY, bool VEC>
+__device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* from, uint16_t* to, int D, int lane) {
+  for (int c0 = lane * 8; c0 < D; c0 += 256 * kVocabAhead) {
+    Raw8<TY> r[kVocabAhead];
+    vocab_load_row<TY, VEC>(from, c0, D, r);
+#pragma unroll
+    for (int j = 0; j < kVocabAhead; ++j)
+      if (c0 + j * 256 < D) *reinterpret_cast<uint4*>(to + c0 + j * 256) = r[j].q[0];
+  }
+}
+// Eight scaled values as pairs.
+__device__ __forceinline__ void vocab_pairs(const float (&v)[8], uint16_t* hi, uint16_t* lo) {
+  uint4 u, w;
+  __half* p = reinterpret_cast<__half*>(&u);
+  __half* q = reinterpret_cast<__half*>(&w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    p[i] = __float2half_rn(v[i]);
+    q[i] = __float2half_rn(v[i] - __half2float(p[i]));
+  }
+  *reinterpret_cast<uint4*>(hi) = u;
+  *reinterpret_cast<uint4*>(lo) = w;
+}
+// A row of fp32 values as pairs, scaled by its largest, whose factors go to `undo`; and, where by_col, times `share` and scaled by columns.  Read
+// once up to 1024 columns.
+template <bool VEC>
+__device__ __forceinline__ void vocab_split_row(const float* from, uint16_t* hi, uint16_t* lo, float2* undo, uint16_t* by_col, uint16_t* by_col_lo, float share,
+                                                const unsigned int* most, int D, int lane) {
+  constexpr int F = PRSGD_TYPE_FP32;
+  Raw8<F> r[kVocabAhead];
+  float v[8], top = 0.f;
+  for (int c0 = lane * 8; c0 < D; c0 += 256 * kVocabAhead) {
+    vocab_load_row<F, VEC>(from, c0, D, r);
+#pragma unroll
+    for (int j = 0; j < kVocabAhead; ++j) {
+      unpack8<F>(r[j], v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(v[i]));
+    }
+  }
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const int e = vocab_exponent(top, 14);
+  const float scale = vocab_power(e);
+  if (lane == 0) *undo = vocab_halves(-e);
+  for (int c0 = lane * 8; c0 < D; c0 += 256 * kVocabAhead) {
+    if (D > 256 * kVocabAhead) vocab_load_row<F, VEC>(from, c0, D, r);
+#pragma unroll
+    for (int j = 0; j < kVocabAhead; ++j) {
       const int c = c0 + j * 256;
       if (c >= D) break;
-      if constexpr (TY == PRSGD_TYPE_FP32) {
-        float v[8];
-        unpack8<TY>(r[j], v);
-        uint4 u, w;
-        __half* p = reinterpret_cast<__half*>(&u);
-        __half* q = reinterpret_cast<__half*>(&w);
+      float x[8];
+      unpack8<F>(r[j], v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float x = v[i] * scale;
-          p[i] = __float2half_rn(x);
-          q[i] = __float2half_rn(x - __half2float(p[i]));
-        }
-        *reinterpret_cast<uint4*>(hi + c) = u;
-        *reinterpret_cast<uint4*>(lo + c) = w;
-      } else {
-        *reinterpret_cast<uint4*>(hi + c) = r[j].q[0];
-      }
+      for (int i = 0; i < 8; ++i) x[i] = v[i] * scale;
+      vocab_pairs(x, hi + c, lo + c);
+      if (by_col == nullptr) continue;
+      const uint4 m[2] = {*reinterpret_cast<const uint4*>(most + c), *reinterpret_cast<const uint4*>(most + c + 4)};
+      const unsigned int* bits = reinterpret_cast<const unsigned int*>(m);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = v[i] * share * vocab_power(vocab_exponent(__uint_as_float(bits[i]), 14));
+      vocab_pairs(x, by_col + c, by_col_lo + c);
     }
   }
 }
@@ -163,31 +233,29 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
   __shared__ float smf[8];
   __shared__ int smi[8];
   __shared__ int place[256];
+  __shared__ float shares[256];
   op_pdl_wait();
   op_pdl_trigger();
   const int64_t g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int eh = 0, ew = 0;
-  if constexpr (TY == PRSGD_TYPE_FP32) {                   // (every warp by itself)
-    const float* m = a.amax + g * 2 * kVocabAmaxBlocks;
-    float h = fmaxf(m[lane], m[lane + 32]), w = fmaxf(m[lane + 64], m[lane + 96]);
-    static_assert(kVocabAmaxBlocks == 64);
-    for (int o = 16; o > 0; o >>= 1) {
-      h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, o));
-      w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, o));
-    }
-    eh = vocab_exponent(h, 14);
-    ew = vocab_exponent(w, 14);
-  }
+  constexpr bool SPLIT = TY == PRSGD_TYPE_FP32;
+  const unsigned int* most_w = SPLIT && a.grad ? a.most + g * a.Dp : nullptr;
+  const unsigned int* most_h = SPLIT && a.grad ? a.most + (a.groups + g) * a.Dp : nullptr;
   if ((int)blockIdx.x >= a.h_blocks) {                     // ---- W
     if (g >= a.w_groups) return;
-    const float scale = exp2f((float)ew);
     const T* W = static_cast<const T*>(a.W) + g * a.w_group;
     for (int64_t v = (int64_t)(blockIdx.x - a.h_blocks) * 8 + warp; v < a.V; v += (int64_t)a.w_blocks * 8) {
       const int64_t o = (g * a.V + v) * a.pitch;
-      uint16_t* lo = TY == PRSGD_TYPE_FP32 ? a.Wc[1] + o : nullptr;
-      if (a.vec_w) vocab_copy_row<TY, true>(W + v * a.w_row, a.Wc[0] + o, lo, a.D, scale, lane);
-      else vocab_copy_row<TY, false>(W + v * a.w_row, a.Wc[0] + o, lo, a.D, scale, lane);
+      const T* from = W + v * a.w_row;
+      if constexpr (SPLIT) {
+        float2* undo = a.colf + g * a.Vp + v;
+        uint16_t* m = a.grad ? a.Wm[0] + o : nullptr;
+        if (a.vec_w) vocab_split_row<true>(from, a.Wc[0] + o, a.Wc[1] + o, undo, m, a.Wm[1] + o, 1.f, most_w, a.D, lane);
+        else vocab_split_row<false>(from, a.Wc[0] + o, a.Wc[1] + o, undo, m, a.Wm[1] + o, 1.f, most_w, a.D, lane);
+      } else {
+        if (a.vec_w) vocab_copy_row<TY, true>(from, a.Wc[0] + o, a.D, lane);
+        else vocab_copy_row<TY, false>(from, a.Wc[0] + o, a.D, lane);
+      }
     }
     return;
   }
@@ -197,7 +265,6 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
   int before = 0;
   for (int64_t t = threadIdx.x; t < begin; t += 256) before += is_live(labels[t]) ? 1 : 0;
   before = vocab_block_sum(before, smi);
-  const float hs = exp2f((float)eh);
   if (blockIdx.x == 0) {
     if (g == 0) {
       if (threadIdx.x < sizeof(DeviceStatus) / 4) reinterpret_cast<unsigned int*>(a.status)[threadIdx.x] = 0u;
@@ -214,22 +281,22 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
     most = vocab_block_max(most, smf);
     if (threadIdx.x == 0) {
       a.live[g] = all;
-      const int e = vocab_exponent(most, 13);
-      VocabScale s{};
-      vocab_halves(-(eh + ew), s.z1, s.z2);
-      s.g = exp2f((float)e);
-      vocab_halves(-(e + ew), s.dh1, s.dh2);
-      vocab_halves(-(e + eh), s.dw1, s.dw2);
-      s.h = hs; s.w = exp2f((float)ew);
-      a.scale[g] = s;
+      const int e = most > 0.f ? vocab_exponent(most, 13) : 0;
+      a.scale[g] = {vocab_power(e), vocab_power(-e)};
+    }
+    if (SPLIT && a.grad) {
+      for (int c = threadIdx.x; c < a.D; c += 256) {
+        a.dwf[g * a.Dp + c] = vocab_halves(-vocab_exponent(__uint_as_float(most_h[c]), 14));
+        if (g < a.w_groups) a.dhf[g * a.Dp + c] = vocab_halves(-vocab_exponent(__uint_as_float(most_w[c]), 14));
+      }
     }
     if (a.grad) {
       const int64_t last = min((int64_t)(all + 63) / 64 * 64, a.T);      // (behind T the tensor maps read zeros)
       for (int64_t r = all + warp; r < last; r += 8)
         for (int c = lane * 8; c < a.pitch; c += 256) {
           const int64_t o = (g * a.Tp + r) * a.pitch + c;
-          *reinterpret_cast<uint4*>(a.Hc[0] + o) = make_uint4(0, 0, 0, 0);
-          if (TY == PRSGD_TYPE_FP32) *reinterpret_cast<uint4*>(a.Hc[1] + o) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>((SPLIT ? a.Hm[0] : a.Hc[0]) + o) = make_uint4(0, 0, 0, 0);
+          if (SPLIT) *reinterpret_cast<uint4*>(a.Hm[1] + o) = make_uint4(0, 0, 0, 0);
         }
     }
   }
@@ -254,8 +321,11 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
         a.rowy[c] = y;
         a.index[c] = (int)t;
         if (a.grad) {
-          const float dl = a.dloss ? a.dloss[o] : 0.f, both = dl + (a.dlse ? a.dlse[o] : 0.f);
-          a.rowp[c] = make_float4(a.stats[2 * o], a.stats[2 * o + 1], both, dl);
+          const float dl = a.dloss ? a.dloss[o] : 0.f, ds = a.dlse ? a.dlse[o] : 0.f;
+          const int e = SPLIT ? vocab_g_exponent(dl, ds) : 0;
+          const float up = vocab_power(e);
+          a.rowp[c] = make_float4(a.stats[2 * o], a.stats[2 * o + 1], (dl + ds) * up, dl * up);
+          if (SPLIT) { a.rowg[c] = vocab_halves(-e); shares[threadIdx.x] = vocab_share(dl, ds); }
         }
       } else if (!a.grad) {
         a.loss[o] = 0.f;
@@ -269,9 +339,17 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
       const int c = place[i];
       if (c >= 0) {
         const int64_t o = (g * a.Tp + c) * a.pitch;
-        uint16_t* lo = TY == PRSGD_TYPE_FP32 ? a.Hc[1] + o : nullptr;
-        if (a.vec_h) vocab_copy_row<TY, true>(H + (t0 + i) * a.h_row, a.Hc[0] + o, lo, a.D, hs, lane);
-        else vocab_copy_row<TY, false>(H + (t0 + i) * a.h_row, a.Hc[0] + o, lo, a.D, hs, lane);
+        const T* from = H + (t0 + i) * a.h_row;
+        if constexpr (SPLIT) {
+          float2* undo = a.rowf + g * a.Tp + c;
+          uint16_t* m = a.grad ? a.Hm[0] + o : nullptr;
+          const float share = a.grad ? shares[i] : 1.f;
+          if (a.vec_h) vocab_split_row<true>(from, a.Hc[0] + o, a.Hc[1] + o, undo, m, a.Hm[1] + o, share, most_h, a.D, lane);
+          else vocab_split_row<false>(from, a.Hc[0] + o, a.Hc[1] + o, undo, m, a.Hm[1] + o, share, most_h, a.D, lane);
+        } else {
+          if (a.vec_h) vocab_copy_row<TY, true>(from, a.Hc[0] + o, a.D, lane);
+          else vocab_copy_row<TY, false>(from, a.Hc[0] + o, a.D, lane);
+        }
       } else if (a.dH != nullptr) {
         const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         T* to = static_cast<T*>(a.dH) + g * a.dh_group + (t0 + i) * a.dh_row;

@@ -47,6 +47,7 @@ struct VocabChain {
   int w_shared, w_swap;                        // W of all groups is one; W's groups lie row by row in turn: map dimensions (D, groups, V)
   int bf16;                                    // operands are bf16 (else fp16)
   const int* live; const float4* rowp; const int* rowy; const int* index; const VocabScale* scale;
+  const float2* rowf; const float2* colf; const float2* rowg; const float2* dhf; const float2* dwf; int64_t Vp; int Dp;      // of pairs, see VocabPrep
   // loss
   int runs, run;                               // runs of the vocabulary, tiles of one
   float2* part; float* zy;
@@ -320,6 +321,16 @@ __device__ __forceinline__ void vt_out64(const VOut& d, uint32_t box, int lane, 
   }
 }
 
+// 32 sums of scaled operands: times the factors of the thread's row and of 32 columns.
+__device__ __forceinline__ void vt_undo32(float (&v)[32], float2 row, const float2* cols) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    const float4 f = *reinterpret_cast<const float4*>(cols + i);
+    v[i] = v[i] * (row.x * f.x) * (row.y * f.y);
+    v[i + 1] = v[i + 1] * (row.x * f.z) * (row.y * f.w);
+  }
+}
+
 // SPLIT: fp32 operands, products of fp16 pairs.
 template <bool GRAD, bool SPLIT>
 __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
@@ -588,8 +599,8 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
       if constexpr (!GRAD) {
         const int row = r0 + lane;
         const int y = row < k.live ? a.rowy[(int64_t)k.g * a.Tp + row] : -1;
-        float m = -INFINITY, sum = 0.f, zs1 = 1.f, zs2 = 1.f;
-        if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
+        float m = -INFINITY, sum = 0.f;
+        const float2 rf = SPLIT && row < k.live ? a.rowf[(int64_t)k.g * a.Tp + row] : make_float2(1.f, 1.f);
 #pragma unroll 1
         for (int j = 0; j < k.n; ++j) {
           ok = gather();
@@ -601,10 +612,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
             if (cols <= 0) break;
             float v[32];
             half(h, v);
-            if (SPLIT) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = v[i] * zs1 * zs2;
-            }
+            if (SPLIT) vt_undo32(v, rf, a.colf + (a.w_shared ? 0 : k.g) * a.Vp + c0);
             if (cols < 32) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : -INFINITY;
@@ -653,9 +661,8 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
             const int64_t at = (int64_t)k.g * a.Tp + row, piece0 = (int64_t)k.p * a.piece;
             const float4 rp = on ? a.rowp[at] : make_float4(0.f, 0.f, 0.f, 0.f);
             const int64_t y = on ? a.rowy[at] - piece0 : -1;       // its label's column of the piece
-            float zs1 = 1.f, zs2 = 1.f;
-            if (SPLIT) { zs1 = sc->z1; zs2 = sc->z2; }
-            const float both = rp.z * sc->g, hot = rp.w * sc->g;
+            const float2 rf = SPLIT && on ? a.rowf[at] : make_float2(1.f, 1.f);
+            const float up = SPLIT ? 1.f : sc->g, both = rp.z * up, hot = rp.w * up;
             // the rows a product reads: up to the next multiple of 64 (behind the call's last token zeros are read in any case), zeros
             // behind the last live one
             VOut d;
@@ -678,11 +685,9 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
                 half(unit * 2 + h, v);
                 if (h == 1 && round == kRounds - 1) release();
                 if (!some) continue;
+                if (SPLIT) vt_undo32(v, rf, a.colf + (a.w_shared ? 0 : k.g) * a.Vp + piece0 + c0);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  const float z = SPLIT ? v[i] * zs1 * zs2 : v[i];
-                  v[i] = both * vt_exp2(((z - rp.x) - rp.y) * kLog2e);
-                }
+                for (int i = 0; i < 32; ++i) v[i] = both * vt_exp2(((v[i] - rp.x) - rp.y) * kLog2e);
                 if (__any_sync(0xffffffffu, y >= 0 && mine >= 0 && mine < 32)) {
 #pragma unroll
                   for (int i = 0; i < 32; ++i) v[i] -= y >= 0 && mine == i ? hot : 0.f;
@@ -706,7 +711,9 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           }
         } else {
           const bool of_w = k.kind == VT_DW;
-          const float s1 = of_w ? sc->dw1 : sc->dh1, s2 = of_w ? sc->dw2 : sc->dh2, s12 = s1 * s2;
+          const float back = SPLIT ? 1.f : sc->back;
+          const float2 rf = SPLIT && !of_w && r0 + lane < k.live ? a.rowg[(int64_t)k.g * a.Tp + r0 + lane] : make_float2(1.f, 1.f);
+          const float2* const cf = of_w ? a.dwf + (int64_t)k.g * a.Dp : a.dhf + (int64_t)(a.w_shared ? 0 : k.g) * a.Dp;
           VOut d;
           d.cols = a.D; d.index = nullptr; d.reduce = 0;
 #pragma unroll 1
@@ -743,8 +750,12 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
                 if (kb > 0) {
                   half(unit * 2 + h, v);
                   if (h == 1 && unit == kWarpCols / 64 - 1) release();
+                  if (!SPLIT) {
 #pragma unroll
-                  for (int i = 0; i < 32; ++i) v[i] = SPLIT ? v[i] * s1 * s2 : v[i] * s12;
+                    for (int i = 0; i < 32; ++i) v[i] *= back;
+                  } else if (some) {
+                    vt_undo32(v, rf, cf + cu + h * 32);
+                  }
                 } else {
 #pragma unroll
                   for (int i = 0; i < 32; ++i) v[i] = 0.f;

@@ -44,12 +44,27 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
   a.status = c.status = reinterpret_cast<DeviceStatus*>(take(sizeof(DeviceStatus)));
   c.live = a.live = reinterpret_cast<int*>(take(4 * (size_t)groups));
   c.scale = a.scale = reinterpret_cast<VocabScale*>(take(sizeof(VocabScale) * (size_t)groups));
-  a.amax = reinterpret_cast<float*>(take(p.split ? (size_t)groups * 2 * kVocabAmaxBlocks * 4 : 0));
+  a.Vp = c.Vp = round_up(V, 256);
+  a.Dp = c.Dp = (int)round_up(D, 256);
+  if (p.split) {
+    c.rowf = a.rowf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Tp));
+    c.colf = a.colf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Vp));
+  }
   c.rowy = a.rowy = reinterpret_cast<int*>(take(4 * (size_t)groups * a.Tp));
   c.index = a.index = reinterpret_cast<int*>(take(4 * (size_t)groups * a.Tp));
   for (int i = 0; i < planes; ++i) {
     a.Hc[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
     a.Wc[i] = reinterpret_cast<uint16_t*>(take(p.copy_w ? 2 * (size_t)groups * V * a.pitch : 0));
+  }
+  if (p.split && grad) {
+    for (int i = 0; i < planes; ++i) {
+      a.Hm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
+      a.Wm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * V * a.pitch));
+    }
+    c.rowg = a.rowg = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Tp));
+    c.dhf = a.dhf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Dp));
+    c.dwf = a.dwf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Dp));
+    a.most = reinterpret_cast<unsigned int*>(take(4 * 2 * (size_t)groups * a.Dp));
   }
   c.tiles = (int)nv; c.td = (int)td; c.kd = (int)up(D, 64); c.by_td = FastDiv((uint32_t)td);
   if (!grad) {
@@ -202,13 +217,13 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   VocabMaps maps{};
   for (int i = 0; i < planes && rc == PRSGD_OK; ++i) {
     rc = vt_map(&maps.hk[i], a.Hc[i], D, a.Tp, G, a.pitch, a.Tp * a.pitch, 128, 1);
-    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], a.Hc[i], D, a.T, G, a.pitch, a.Tp * a.pitch, 64, 1);
-    const void* w = p.copy_w ? a.Wc[i] : a.W;
+    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], p.split ? a.Hm[i] : a.Hc[i], D, a.T, G, a.pitch, a.Tp * a.pitch, 64, 1);
     const int64_t row = p.copy_w ? a.pitch : a.w_row, group = a.w_groups == 1 ? row : p.copy_w ? a.V * a.pitch : a.w_group;
     c.w_swap = a.w_groups > 1 && group < row;
     for (int mn = 0; mn < (p.grad ? 2 : 1) && rc == PRSGD_OK; ++mn) {
       CUtensorMap* to = mn ? &maps.wm[i] : &maps.wk[i];
       const int box = mn ? 64 : 128;
+      const void* w = !p.copy_w ? a.W : mn && p.split ? a.Wm[i] : a.Wc[i];
       rc = c.w_swap ? vt_map(to, w, D, a.w_groups, a.V, group, row, 1, box) : vt_map(to, w, D, a.V, a.w_groups, row, group, box, 1);
     }
     if (!p.grad) continue;
@@ -220,7 +235,16 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   const int64_t most = std::max<int64_t>(1, 148 * 8 / G);
   a.h_blocks = (int)std::min<int64_t>(up(a.T, 8), most);
   a.w_blocks = p.copy_w ? (int)std::min<int64_t>(up(a.V, 8), most) : 0;
-  if (p.split) launch_pdl(vocab_amax_kernel, dim3(2 * kVocabAmaxBlocks, (unsigned)G), dim3(256), 0, st, a);
+  if (p.split && p.grad) {
+    const int64_t n = 2 * G * a.Dp;
+    launch_pdl(vocab_zero_kernel, dim3((unsigned)std::min<int64_t>(up(n, 256), 148 * 8)), dim3(256), 0, st, a.most, n);
+    // blocks of 64 rows or more, eight an SM over all groups and strips of 128 columns
+    const int64_t strips = up(D, 128), share = std::max<int64_t>(1, 148 * 8 / (G * strips));
+    a.most_rows = (int)round_up(std::max<int64_t>(64, up(a.T + a.V, share)), 32);
+    a.most_h = (int)up(a.T, a.most_rows);
+    a.most_w = (int)up(a.V, a.most_rows);
+    launch_pdl(vocab_columns_kernel, dim3((unsigned)(a.most_h + a.most_w), (unsigned)strips, (unsigned)G), dim3(256), 0, st, a);
+  }
   with_type(a.h_type, [&](auto ty) { launch_pdl(vocab_prep_kernel<decltype(ty)::value>, dim3((unsigned)(a.h_blocks + a.w_blocks), (unsigned)G), dim3(256), 0, st, a); });
   const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, p.tasks));
   auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kVtThreads), vt_smem(p.grad), st, 2, maps, c); };

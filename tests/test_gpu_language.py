@@ -10,7 +10,7 @@ Tolerances, by element, with half = finfo(type).eps / 2 (one rounding of a resul
    loss and log sum: 2 max e_z + 2^-14 (relative to the sum, so absolute for its logarithm) + 8 u (|max| + |loss|); the maximum: e_z.
  * its gradient: G = (dloss + dlse) p - dloss onehot is held with one rounding `hold` (16-bit types their own, fp32 pairs 2^-21), p is off by
    2 e_z + 2^-20 relative, and the sums over V or T by (n / 16 + 4) 2^-22 of the sum of magnitudes M: (hold + 2 e_z + 2^-20 + (n / 16 + 4) 2^-22) M +
-   half |want|.  fp16 and pairs hold nothing below 2^-38 of the group's largest |dloss| + |dlse|: 2^-38 of it times sum |w| (or |h|).
+   half |want|.  fp16 and pairs hold nothing below 2^-38 of the group's (pairs: the token's) largest |dloss| + |dlse|: 2^-38 of it times sum |w| (or |h|).
 """
 import math
 
@@ -507,6 +507,55 @@ def test_vocab_loss_operands_of_any_size(b, dtype):
     check_loss(got, H, W, y)
     dloss = randn(93, 3, 30)
     check_grad(b.prsgd_vocab_loss_grad(H, W, y, got[1], dloss=dloss), H, W, y, dloss, None)
+
+
+@pytest.mark.parametrize("G,T,V,D", [(1, 40, 301, 64), (2, 300, 2500, 100), (1, 70, 400, 1100)])
+def test_vocab_loss_rows_of_any_size(b, G, T, V, D):
+    """fp32: tokens, their gradients and classes of very different sizes spoil nothing of the others: rows of H from 2^-30 to 2^60, dloss from
+    2^-80 to 1, a class that a last column of ones and a weight of -1e9 mask (compared with the classes without it).
+
+    A token's own e_z bounds its logits.  dH: the terms of check_grad with them; what a token's row of G does not hold is 2^-38 |dloss_t|, what W's columns do not is
+    2^-38 of their largest.  dW: the same by columns of H times |dloss_t|, whose scale is known to a factor of two: 2^-37."""
+    H, W, y = case(100, G, T, V - 1, D, F32)
+    size = 2.0 ** (torch.arange(T, device="cuda:0") % 31 - 30.0)
+    size[T // 2] = 2.0 ** 60
+    H = H * size[:, None]
+    H[..., -1] = 1.0
+    W = torch.cat([W, torch.zeros(G, 1, D, device="cuda:0")], 1)
+    W[:, -1, -1] = -1e9
+    rest = W[:, :-1]
+    loss, stats = b.prsgd_vocab_loss(H, W, y)
+    masked = y == V - 1                       # (a label of that class: a loss of 1e9, or of what the token of 2^60 holds)
+    assert (loss[masked] >= 0.99e9).all()
+    y = torch.where(masked, -1, y)
+    check_loss((torch.where(masked, 0.0, loss), torch.where(masked[..., None], 0.0, stats)), H, rest, y)
+    dloss = randn(103, G, T) * 2.0 ** -(torch.arange(T, device="cuda:0") % 81).float()
+    stats = exact_stats(H, rest, y)
+    dH, dW = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss)
+    wH, wW, mH, mW, A = ref.vocab_grad(H, rest, y, dloss)
+    on = ref.live_tokens(y, V)
+    Hz, d = H.double().abs() * on[..., None], dloss.double().abs() * on
+    ez = z_error(Hz, rest, D).amax(-1, keepdim=True)
+    off = lambda n: 2.0 ** -21 + 2 * ez + 2.0 ** -20 + (n / 16 + 4) * 2.0 ** -22          # noqa: E731
+    tol = off(V) * mH + 2.0 ** -38 * (d[..., None] * W.double().abs().sum(1, keepdim=True) + A.sum(-1, keepdim=True) * W.double().abs().amax(1, keepdim=True))
+    check(dH, wH, tol + half(F32) * wH.abs())
+    weight = (A / d.clamp(min=1e-300)[..., None]).sum(1)[..., None]
+    tol = (A * off(T)).mT @ Hz + 2.0 ** -38 * (d[..., None] * Hz).sum(1, keepdim=True) + 2.0 ** -37 * weight * (Hz * d[..., None]).amax(1, keepdim=True)
+    check(dW[:, :-1], wW, tol + 2 * half(F32) * wW.abs())
+    assert (dW[:, -1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_vocab_loss_views_of_weights(b, dtype):
+    """W's groups as overlapping windows of one table, and columns of a table side by side."""
+    T, V, D = 70, 300, 64
+    H, _, y = case(110, 3, T, V, D, dtype)
+    table = randn(113, V + 40, 4 * D).to(dtype) * 0.25
+    for W in (table[:, :D].as_strided((3, V, D), (20 * 4 * D, 4 * D, 1)), table.as_strided((3, V, D), (D, 4 * D, 1)), table.as_strided((3, V, D), (8, 4 * D, 1))):
+        got = b.prsgd_vocab_loss(H, W, y)
+        check_loss(got, H, W, y)
+        dloss = randn(114, 3, T)
+        check_grad(b.prsgd_vocab_loss_grad(H, W, y, exact_stats(H, W, y), dloss=dloss), H, W, y, dloss, None)
 
 
 def test_vocab_loss_no_tokens(b):
