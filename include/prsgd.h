@@ -576,7 +576,8 @@ int prsgd_route_grad(const void* d_logits, int32_t type, int64_t row_stride, int
  * all groups share has group stride 0. */
 #define PRSGD_VOCAB_MAX (1 << 24)
 
-/* Lookup of token embeddings: out_t = scale * table[id_t], zeros for padding, rounded once to out's type. */
+/* Lookup of token embeddings: out_t = scale * table[id_t], zeros for padding, rounded once to out's type.  out may share no memory
+ * with an input. */
 int prsgd_embed(const void* d_table, int32_t type, int64_t row_stride, int64_t group_stride, const int32_t* d_ids,
                 int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, float scale,
                 void* d_out, int32_t out_type, int64_t out_row_stride, int64_t out_group_stride, void* cuda_stream);
@@ -601,7 +602,7 @@ int prsgd_embed_grad(const void* d_dout, int32_t type, int64_t row_stride, int64
  * The gradient with respect to x is the same call with the gradient in x's place and no residual; that of the residual
  * is the gradient itself.  A dropped element is 0 (+ residual) whatever x holds.  x, residual (or NULL) and out have one type;
  * out may be x or the residual themselves (same strides, else the call is refused); it may share no memory with them in another way.
- * p in [0, 1 - 2^-17]. */
+ * p in [0, 1 - 2^-17). */
 int prsgd_dropout(const void* d_x, int32_t type, int64_t row_stride, int64_t group_stride,
                   const void* d_residual, int64_t residual_row_stride, int64_t residual_group_stride,
                   void* d_out, int64_t out_row_stride, int64_t out_group_stride,
@@ -614,8 +615,9 @@ int prsgd_dropout_keep(uint64_t seed, int64_t group, int64_t row, int64_t col, i
  *   loss_t = log sum_v e^z_tv - z_ty,  y the token's label;  stats_t = (max_v z_tv, log sum_v e^(z_tv - max)), whose sum is the
  * logarithm of the softmax's denominator.  H: [groups][tokens][dim]; W: [groups][vocab][dim], row-major like the class layer's
  * weights; both of one type.  A token whose label is padding has loss 0 and stats 0 whatever its row of H holds.  loss: [groups][tokens],
- * stats: [groups][tokens][2], fp32, dense.  Products of 16-bit types are summed in fp32; fp32 operands are taken as pairs of
- * fp16 values (22 bits, scaled by powers of two per group), three products each.
+ * stats: [groups][tokens][2], fp32, dense; they share no memory with each other or with an input.  Products of 16-bit types are summed in
+ * fp32; fp32 operands are taken as pairs of fp16 values (22 bits and nothing below 2^-39 of the largest of their row, each row of H and W
+ * scaled by a power of two of its own), three products each.  Up to four tokens a group of fp32 are summed in fp32 as they are.
  * The workspace depends on whether W's rows begin on 16-byte boundaries (address and both strides multiples of 16 bytes: w_aligned
  * 1; else, or for fp32, it holds a copy of W). */
 int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes);
@@ -627,7 +629,7 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
 /* Gradient of sum dloss_t loss_t + sum dlse_t lse_t (lse the sum of the stats) with respect to H and W:
  *   G_tv = (dloss_t + dlse_t) e^(z_tv - lse_t) - dloss_t [v = y_t],   dH = G W,   dW = G^T H (or, accumulate, added to what dW holds).
  * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is held with one rounding of the operands' type
- * (fp32: as pairs; none for one or two tokens a group), a piece of the vocabulary at a time.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
+ * (fp32: as pairs, scaled by tokens, beside operands scaled by columns, H's after a token's dloss and dlse; none for one or two tokens a group), a piece of the vocabulary at a time.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
  * whose label is padding take no part: their rows of dH are zeros, whatever their H, stats, dloss and dlse hold.  The rows of dH and of dW may
  * not overlap (W shared by all groups has one gradient: call with groups = 1 and the groups' tokens behind one another);
  * neither may share memory with another array of the call. */

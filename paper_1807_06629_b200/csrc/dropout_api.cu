@@ -129,7 +129,7 @@ int prsgd_dropout(const void* d_x, int32_t type, int64_t row_stride, int64_t gro
   if (!type_known(type)) return op_fail(PRSGD_ERR_ARG, "unknown element type");
   if (groups < 0 || rows < 0 || cols < 0) return op_fail(PRSGD_ERR_ARG, "need groups, rows, cols >= 0");
   const int threshold = dropout_threshold(p);
-  if (threshold < 0) return op_fail(PRSGD_ERR_ARG, "p must be in [0, 1 - 2^-17]");
+  if (threshold < 0) return op_fail(PRSGD_ERR_ARG, "p must be in [0, 1 - 2^-17)");
   if (groups > 65535 || rows > 0x7fffffffll || cols > 0x7fffffffll) return op_fail(PRSGD_ERR_SIZE, "more than 65535 groups or 2^31 - 1 rows or columns");
   if (groups == 0 || rows == 0 || cols == 0) return PRSGD_OK;
   int rc = check_rows("x", d_x, type, row_stride, group_stride, groups, rows, cols, false);
@@ -166,7 +166,7 @@ int prsgd_dropout(const void* d_x, int32_t type, int64_t row_stride, int64_t gro
 
 int prsgd_dropout_keep(uint64_t seed, int64_t group, int64_t row, int64_t col, int64_t step, double p) {
   const int threshold = dropout_threshold(p);
-  if (threshold < 0) return op_fail(PRSGD_ERR_ARG, "p must be in [0, 1 - 2^-17]");
+  if (threshold < 0) return op_fail(PRSGD_ERR_ARG, "p must be in [0, 1 - 2^-17)");
   if (col < 0) return op_fail(PRSGD_ERR_ARG, "need col >= 0");
   const Words4 w = philox4x32_10({(uint32_t)(col / 8), (uint32_t)row, (uint32_t)group, (uint32_t)step}, seed);
   const uint32_t words[4] = {w.x, w.y, w.z, w.w}, word = words[(col % 8) / 2];

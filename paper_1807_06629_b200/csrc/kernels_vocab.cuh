@@ -33,7 +33,7 @@ struct VocabPrep {
   // fp32 operands only: factors that undo the scales, two powers of two each (their product may lie outside a float's range)
   float2* rowf; float2* colf;                  // [groups][Tp], [w_groups][Vp] of the rows of H' and W
   // and the gradient's
-  uint16_t* Hm[2]; uint16_t* Wm[2];            // as Hc and Wc, scaled by columns
+  uint16_t* Hm[2]; uint16_t* Wm[2];            // as Hc and Wc, scaled by columns; nullptr where no product wants them
   float2* rowg;                                // [groups][Tp] of the rows of G
   float2* dhf; float2* dwf;                    // [w_groups][Dp], [groups][Dp] of the columns of Wm and Hm
   unsigned int* most;                          // [2][groups][Dp] largest finite magnitudes (bits) of those columns: W, H
@@ -144,12 +144,12 @@ __global__ void __launch_bounds__(256) vocab_columns_kernel(const VocabPrep a) {
 }
 
 // A row of D elements into an operand row, a warp's lanes eight elements each, several pieces in flight.
-constexpr int kVocabAhead = 4;
-template <int TY, bool VEC>
-__device__ __forceinline__ void vocab_load_row(const typename ElemOf<TY>::type* from, int c0, int D, Raw8<TY> (&r)[kVocabAhead]) {
+constexpr int kVocabAhead = 4, kSplitAhead = 2;
+template <int TY, bool VEC, int N>
+__device__ __forceinline__ void vocab_load_row(const typename ElemOf<TY>::type* from, int c0, int D, Raw8<TY> (&r)[N]) {
   using T = typename ElemOf<TY>::type;
 #pragma unroll
-  for (int j = 0; j < kVocabAhead; ++j) {
+  for (int j = 0; j < N; ++j) {
     const int c = c0 + j * 256;
     if (VEC && c + 8 <= D) {
       r[j] = load_raw<TY>(from + c);
@@ -184,17 +184,17 @@ __device__ __forceinline__ void vocab_pairs(const float (&v)[8], uint16_t* hi, u
   *reinterpret_cast<uint4*>(lo) = w;
 }
 // A row of fp32 values as pairs, scaled by its largest, whose factors go to `undo`; and, where by_col, times `share` and scaled by columns.  Read
-// once up to 1024 columns.
+// once up to 512 columns.
 template <bool VEC>
 __device__ __forceinline__ void vocab_split_row(const float* from, uint16_t* hi, uint16_t* lo, float2* undo, uint16_t* by_col, uint16_t* by_col_lo, float share,
                                                 const unsigned int* most, int D, int lane) {
   constexpr int F = PRSGD_TYPE_FP32;
-  Raw8<F> r[kVocabAhead];
+  Raw8<F> r[kSplitAhead];
   float v[8], top = 0.f;
-  for (int c0 = lane * 8; c0 < D; c0 += 256 * kVocabAhead) {
+  for (int c0 = lane * 8; c0 < D; c0 += 256 * kSplitAhead) {
     vocab_load_row<F, VEC>(from, c0, D, r);
 #pragma unroll
-    for (int j = 0; j < kVocabAhead; ++j) {
+    for (int j = 0; j < kSplitAhead; ++j) {
       unpack8<F>(r[j], v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(v[i]));
@@ -204,10 +204,10 @@ __device__ __forceinline__ void vocab_split_row(const float* from, uint16_t* hi,
   const int e = vocab_exponent(top, 14);
   const float scale = vocab_power(e);
   if (lane == 0) *undo = vocab_halves(-e);
-  for (int c0 = lane * 8; c0 < D; c0 += 256 * kVocabAhead) {
-    if (D > 256 * kVocabAhead) vocab_load_row<F, VEC>(from, c0, D, r);
+  for (int c0 = lane * 8; c0 < D; c0 += 256 * kSplitAhead) {
+    if (D > 256 * kSplitAhead) vocab_load_row<F, VEC>(from, c0, D, r);
 #pragma unroll
-    for (int j = 0; j < kVocabAhead; ++j) {
+    for (int j = 0; j < kSplitAhead; ++j) {
       const int c = c0 + j * 256;
       if (c >= D) break;
       float x[8];
@@ -228,7 +228,7 @@ __device__ __forceinline__ void vocab_split_row(const float* from, uint16_t* hi,
 // Blocks x < h_blocks of a group move its live rows together, the others copy W.  A block counts the live tokens before its own; the
 // group's first block counts all, finds the scales, and zeroes the rows behind the last live one that a product may read.
 template <int TY>
-__global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
+__global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
   using T = typename ElemOf<TY>::type;
   __shared__ float smf[8];
   __shared__ int smi[8];
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
       const T* from = W + v * a.w_row;
       if constexpr (SPLIT) {
         float2* undo = a.colf + g * a.Vp + v;
-        uint16_t* m = a.grad ? a.Wm[0] + o : nullptr;
+        uint16_t* m = a.Wm[0] ? a.Wm[0] + o : nullptr;
         if (a.vec_w) vocab_split_row<true>(from, a.Wc[0] + o, a.Wc[1] + o, undo, m, a.Wm[1] + o, 1.f, most_w, a.D, lane);
         else vocab_split_row<false>(from, a.Wc[0] + o, a.Wc[1] + o, undo, m, a.Wm[1] + o, 1.f, most_w, a.D, lane);
       } else {
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
         if (g < a.w_groups) a.dhf[g * a.Dp + c] = vocab_halves(-vocab_exponent(__uint_as_float(most_w[c]), 14));
       }
     }
-    if (a.grad) {
+    if (a.grad && (!SPLIT || a.Hm[0])) {
       const int64_t last = min((int64_t)(all + 63) / 64 * 64, a.T);      // (behind T the tensor maps read zeros)
       for (int64_t r = all + warp; r < last; r += 8)
         for (int c = lane * 8; c < a.pitch; c += 256) {
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const VocabPrep a) {
         const T* from = H + (t0 + i) * a.h_row;
         if constexpr (SPLIT) {
           float2* undo = a.rowf + g * a.Tp + c;
-          uint16_t* m = a.grad ? a.Hm[0] + o : nullptr;
+          uint16_t* m = a.Hm[0] ? a.Hm[0] + o : nullptr;
           const float share = a.grad ? shares[i] : 1.f;
           if (a.vec_h) vocab_split_row<true>(from, a.Hc[0] + o, a.Hc[1] + o, undo, m, a.Hm[1] + o, share, most_h, a.D, lane);
           else vocab_split_row<false>(from, a.Hc[0] + o, a.Hc[1] + o, undo, m, a.Hm[1] + o, share, most_h, a.D, lane);

@@ -217,13 +217,13 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   VocabMaps maps{};
   for (int i = 0; i < planes && rc == PRSGD_OK; ++i) {
     rc = vt_map(&maps.hk[i], a.Hc[i], D, a.Tp, G, a.pitch, a.Tp * a.pitch, 128, 1);
-    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], p.split ? a.Hm[i] : a.Hc[i], D, a.T, G, a.pitch, a.Tp * a.pitch, 64, 1);
+    if (rc == PRSGD_OK && p.grad) rc = vt_map(&maps.hm[i], a.Hm[i] ? a.Hm[i] : a.Hc[i], D, a.T, G, a.pitch, a.Tp * a.pitch, 64, 1);
     const int64_t row = p.copy_w ? a.pitch : a.w_row, group = a.w_groups == 1 ? row : p.copy_w ? a.V * a.pitch : a.w_group;
     c.w_swap = a.w_groups > 1 && group < row;
     for (int mn = 0; mn < (p.grad ? 2 : 1) && rc == PRSGD_OK; ++mn) {
       CUtensorMap* to = mn ? &maps.wm[i] : &maps.wk[i];
       const int box = mn ? 64 : 128;
-      const void* w = !p.copy_w ? a.W : mn && p.split ? a.Wm[i] : a.Wc[i];
+      const void* w = !p.copy_w ? a.W : mn && a.Wm[i] ? a.Wm[i] : a.Wc[i];
       rc = c.w_swap ? vt_map(to, w, D, a.w_groups, a.V, group, row, 1, box) : vt_map(to, w, D, a.V, a.w_groups, row, group, box, 1);
     }
     if (!p.grad) continue;
@@ -241,8 +241,8 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
     // blocks of 64 rows or more, eight an SM over all groups and strips of 128 columns
     const int64_t strips = up(D, 128), share = std::max<int64_t>(1, 148 * 8 / (G * strips));
     a.most_rows = (int)round_up(std::max<int64_t>(64, up(a.T + a.V, share)), 32);
-    a.most_h = (int)up(a.T, a.most_rows);
-    a.most_w = (int)up(a.V, a.most_rows);
+    a.most_h = a.Hm[0] ? (int)up(a.T, a.most_rows) : 0;
+    a.most_w = a.Wm[0] ? (int)up(a.V, a.most_rows) : 0;
     launch_pdl(vocab_columns_kernel, dim3((unsigned)(a.most_h + a.most_w), (unsigned)strips, (unsigned)G), dim3(256), 0, st, a);
   }
   with_type(a.h_type, [&](auto ty) { launch_pdl(vocab_prep_kernel<decltype(ty)::value>, dim3((unsigned)(a.h_blocks + a.w_blocks), (unsigned)G), dim3(256), 0, st, a); });
@@ -286,6 +286,12 @@ int check_floats(const void* a, const void* b, const void* c, const void* d) {
   return PRSGD_OK;
 }
 
+// loss [n] and stats [2 n] are apart
+int check_outputs(const float* loss, const float* stats, int64_t n) {
+  const uintptr_t l = (uintptr_t)loss, s = (uintptr_t)stats;
+  return l < s + 8 * (uintptr_t)n && s < l + 4 * (uintptr_t)n ? op_fail(PRSGD_ERR_ARG, "loss and stats overlap") : PRSGD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -323,6 +329,7 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
     size_t need = 0;
     VocabFew f = vocab_few_plan(groups, tokens, vocab, dim, static_cast<unsigned char*>(d_work), &need);
     rc = check_work(d_work, work_bytes, need);
+    if (rc == PRSGD_OK) rc = check_outputs(d_loss, d_stats, groups * tokens);
     int sms = 0;
     if (rc == PRSGD_OK) rc = vocab_device(&sms);
     if (rc != PRSGD_OK) return rc;
@@ -349,6 +356,7 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
   VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), false, static_cast<unsigned char*>(d_work));
   rc = check_tasks(p.tasks);
   if (rc == PRSGD_OK) rc = check_work(d_work, work_bytes, p.bytes);
+  if (rc == PRSGD_OK) rc = check_outputs(d_loss, d_stats, groups * tokens);
   if (rc != PRSGD_OK) return rc;
   VocabPrep& a = p.prep;
   set_inputs(a, d_H, h_row_stride, h_group_stride, d_W, w_row_stride, w_group_stride, type, d_labels);
@@ -436,6 +444,8 @@ int prsgd_vocab_loss_grad(const void* d_H, int64_t h_row_stride, int64_t h_group
   VocabChain& c = p.chain;
   set_inputs(a, d_H, h_row_stride, h_group_stride, d_W, w_row_stride, w_group_stride, type, d_labels);
   a.stats = d_stats; a.dloss = d_dloss; a.dlse = d_dlse;
+  if (!d_dH) a.Wm[0] = a.Wm[1] = nullptr;
+  if (!d_dW) a.Hm[0] = a.Hm[1] = nullptr;
   a.dH = d_dH; a.dh_row = dh_row_stride; a.dh_group = dh_group_stride; a.vec_dh = d_dH && rows_16(d_dH, type, dh_row_stride, dh_group_stride);
   c.dH = d_dH; c.dh_row = dh_row_stride; c.dh_group = dh_group_stride; c.dh_type = type; c.vec_dh = a.vec_dh;
   c.dW = d_dW; c.dw_row = dw_row_stride; c.dw_group = dw_group_stride; c.dw_type = dw_type; c.accumulate = accumulate != 0;

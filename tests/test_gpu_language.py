@@ -543,6 +543,8 @@ def test_vocab_loss_rows_of_any_size(b, G, T, V, D):
     tol = (A * off(T)).mT @ Hz + 2.0 ** -38 * (d[..., None] * Hz).sum(1, keepdim=True) + 2.0 ** -37 * weight * (Hz * d[..., None]).amax(1, keepdim=True)
     check(dW[:, :-1], wW, tol + 2 * half(F32) * wW.abs())
     assert (dW[:, -1] == 0).all()
+    assert torch.equal(b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, want_dW=False)[0], dH)
+    assert torch.equal(b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, want_dH=False)[1], dW)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

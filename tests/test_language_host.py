@@ -104,6 +104,19 @@ def test_vocab_loss_refusals(b):
         assert loss(b.lib, **{**dict(H=None, W=None, y=None, l=None, s=None, work=None), **kw}) == OK
 
 
+@pytest.mark.parametrize("T", [1, 10])
+def test_vocab_loss_outputs_apart(b, T):
+    for l, s in [(4096, 4096), (4096, 4096 + 4 * 2 * T - 4), (4096 + 8 * 2 * T - 4, 4096)]:
+        assert loss(b.lib, T=T, l=l, s=s) == ARG
+
+
+def test_dropout_of_almost_all(b):
+    """65536 p is rounded to even: below 1 - 2^-17 something may stay."""
+    assert b.lib.prsgd_dropout_keep(1, 0, 0, 0, 0, 1 - 2.0 ** -17 - 2.0 ** -40) in (0, 1)
+    assert b.lib.prsgd_dropout_keep(1, 0, 0, 0, 0, 1 - 2.0 ** -17) == ARG
+    assert dropout(b.lib, p=1 - 2.0 ** -17) == ARG
+
+
 def test_vocab_loss_grad_refusals(b):
     for kw, want in VOCAB + [(dict(dl=257), ALIGN), (dict(ds=257), ALIGN), (dict(dH=12289), ALIGN), (dict(dW=16385), ALIGN), (dict(dhr=63), ARG), (dict(dwr=63), ARG),
                              (dict(dhg=0), ARG), (dict(dwg=0), ARG), (dict(dwg=63), ARG), (dict(dwt=2), ARG), (dict(dH=4096), ARG), (dict(dH=8192), ARG),
