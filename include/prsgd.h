@@ -617,7 +617,7 @@ int prsgd_dropout_keep(uint64_t seed, int64_t group, int64_t row, int64_t col, i
  * weights; both of one type.  A token whose label is padding has loss 0 and stats 0 whatever its row of H holds.  loss: [groups][tokens],
  * stats: [groups][tokens][2], fp32, dense; they share no memory with each other or with an input.  Products of 16-bit types are summed in
  * fp32; fp32 operands are taken as pairs of fp16 values (22 bits and nothing below 2^-39 of the largest of their row, each row of H and W
- * scaled by a power of two of its own), three products each.  Up to four tokens a group of fp32 are summed in fp32 as they are.
+ * scaled by a power of two of its own), three products each.  Up to eight tokens a group of fp32 are summed in fp32 as they are.
  * The workspace depends on whether W's rows begin on 16-byte boundaries (address and both strides multiples of 16 bytes: w_aligned
  * 1; else, or for fp32, it holds a copy of W). */
 int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes);

@@ -1,7 +1,7 @@
 // The vocabulary loss of few tokens a group: W is read once, where it lies and in any type, by dot products on the CUDA cores.
 //
 // The bytes of W bound it (22 elements of 16 bits a cycle and SM at the HBM rate); a token costs one product an element, in packed
-// pairs, so up to kFewTokens of them fit beside the loads.  A warp takes four rows of W at a time, so that what it reads of H from
+// pairs, so kFewTurn of them fit beside the loads; of more, neighbouring blocks take kFewTurn each and find W in L2.  A warp takes four rows of W at a time, so that what it reads of H from
 // shared memory serves four rows; the largest logit and the sum of exponentials run along in registers, and a second launch joins
 // the blocks'.  1 x 1 x 32000 x 1024: bf16 20 us (10 of them W from HBM, 8 two launches and the reading of H), fp32 27 (20).
 #pragma once
@@ -9,7 +9,7 @@
 
 namespace prsgd {
 
-constexpr int kFewTokens = 4, kFewRows = 4, kFewWarps = 8;
+constexpr int kFewTokens = 8, kFewTurn = 4, kFewRows = 4, kFewWarps = 8;
 constexpr int64_t kFewSmem = 96 * 1024;        // H of a group as fp32
 
 struct VocabFew {
@@ -18,7 +18,8 @@ struct VocabFew {
   const int32_t* labels;
   int64_t V, per;                              // rows of W a block takes
   int T, D, dp;                                // dp: D rounded up to 8
-  int blocks;                                  // of a group
+  int blocks;                                  // of a group, for each kFewTurn of its tokens
+  int turns;                                   // kFewTurn tokens each: the blocks of all turns that take the same rows lie side by side and read them at a time
   float2* part; float* zy;                     // [groups][T][blocks], [groups][T]
   float* loss; float* stats;
   DeviceStatus* status;
@@ -41,17 +42,18 @@ __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_kernel(const VocabFe
   op_pdl_trigger();
   const int64_t g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int blk = (int)(blockIdx.x / (unsigned)a.turns), first = (int)(blockIdx.x - (unsigned)(blk * a.turns)) * kFewTurn, count = min(NT, a.T - first);
   if (blockIdx.x == 0 && g == 0 && threadIdx.x < sizeof(DeviceStatus) / 4) reinterpret_cast<unsigned int*>(a.status)[threadIdx.x] = 0u;
   int y[NT];
   bool any = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    y[t] = t < a.T ? a.labels[g * a.T + t] : -1;
+    y[t] = t < count ? a.labels[g * a.T + first + t] : -1;
     if (y[t] >= a.V) y[t] = -1;
     any |= y[t] >= 0;
   }
   if (!any) return;                            // (nobody reads this group's parts)
-  const T* H = static_cast<const T*>(a.H) + g * a.h_group;
+  const T* H = static_cast<const T*>(a.H) + g * a.h_group + first * a.h_row;
   for (int i = threadIdx.x; i < NT * a.dp; i += 32 * kFewWarps) {
     const int t = i / a.dp, c = i - t * a.dp;
     bool on = false;
@@ -61,11 +63,11 @@ __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_kernel(const VocabFe
   }
   __syncthreads();
   const T* W = static_cast<const T*>(a.W) + g * a.w_group;
-  const int64_t end = min(a.V, (blockIdx.x + 1) * a.per);
+  const int64_t end = min(a.V, (blk + 1) * a.per);
   float2 run[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) run[t] = make_float2(-INFINITY, 0.f);
-  for (int64_t v0 = blockIdx.x * a.per + warp * kFewRows; v0 < end; v0 += kFewWarps * kFewRows) {
+  for (int64_t v0 = blk * a.per + warp * kFewRows; v0 < end; v0 += kFewWarps * kFewRows) {
     float2 acc[kFewRows][NT];
 #pragma unroll
     for (int r = 0; r < kFewRows; ++r)
@@ -105,7 +107,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_kernel(const VocabFe
         float z = acc[r][t].x + acc[r][t].y;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (lane == 0 && v0 + r == y[t]) a.zy[g * a.T + t] = z;
+        if (lane == 0 && v0 + r == y[t]) a.zy[g * a.T + first + t] = z;
         const float m = fmaxf(run[t].x, z);
         run[t] = make_float2(m, run[t].y * vt_exp2((run[t].x - m) * 1.4426950408889634f) + vt_exp2((z - m) * 1.4426950408889634f));
       }
@@ -116,15 +118,15 @@ __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_kernel(const VocabFe
     for (int t = 0; t < NT; ++t) sums[warp][t] = run[t];
   }
   __syncthreads();
-  if (threadIdx.x < NT && (int)threadIdx.x < a.T) {
+  if ((int)threadIdx.x < count) {
     float2 all = sums[0][threadIdx.x];
     for (int w = 1; w < kFewWarps; ++w) all = vocab_merge(all, sums[w][threadIdx.x]);
-    a.part[(g * a.T + threadIdx.x) * a.blocks + blockIdx.x] = all;
+    a.part[(g * a.T + first + threadIdx.x) * a.blocks + blk] = all;
   }
 }
 
 // A warp a token.
-__global__ void __launch_bounds__(128) vocab_few_join_kernel(const VocabFew a) {
+__global__ void __launch_bounds__(32 * kFewTokens) vocab_few_join_kernel(const VocabFew a) {
   op_pdl_wait();
   op_pdl_trigger();
   const int64_t g = blockIdx.x;

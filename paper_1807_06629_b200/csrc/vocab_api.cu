@@ -116,10 +116,10 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
 }
 
 // The loss of few tokens a group has its own form without tensor cores, where H fits in shared memory: up to two of 16-bit types (1 x 32000 x 1024, bf16:
-// one token 20 us against 27, two 24 against 27, four 30 against 27), up to four of fp32, which spares the copy of W as pairs (27 to 34
-// against 220).
+// one token 20 us against 27, two 24 against 27, four 30 against 27), up to eight of fp32, which spares the copy of W as pairs (cold caches: three
+// tokens 42 us against 100, eight 58, twelve 77, sixteen 95; but 4 x 100000 x 256 sixteen 413, as long as with the copy).
 bool vocab_few(int type, int64_t T, int D) {
-  return T <= (type == PRSGD_TYPE_FP32 ? kFewTokens : 2) && (T <= 2 ? T : 4) * round_up(D, 8) * 4 <= kFewSmem;
+  return T <= (type == PRSGD_TYPE_FP32 ? kFewTokens : 2) && (T <= 2 ? T : kFewTurn) * round_up(D, 8) * 4 <= kFewSmem;
 }
 
 VocabFew vocab_few_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned char* base, size_t* bytes) {
@@ -127,7 +127,9 @@ VocabFew vocab_few_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned ch
   a.T = (int)T; a.V = V; a.D = D; a.dp = (int)round_up(D, 8);
   // as many blocks as run at a time by their registers: three an SM for one token, else two (four, in two rounds: 24 us for 20)
   const int64_t turn = kFewWarps * kFewRows, most = std::max<int64_t>(1, 148 * (T <= 1 ? 3 : 2) / std::max<int64_t>(groups, 1));
-  a.per = up(up(V, turn), std::min(most, up(V, turn))) * turn;
+  a.turns = (int)up(std::max<int64_t>(T, 1), kFewTurn);
+  const int64_t blocks = std::max<int64_t>(1, std::min(most / a.turns, up(V, turn)));
+  a.per = up(up(V, turn), blocks) * turn;
   a.blocks = (int)up(V, a.per);
   size_t off = 0;
   auto take = [&](size_t n) { unsigned char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
@@ -138,7 +140,7 @@ VocabFew vocab_few_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned ch
   return a;
 }
 
-// The same for the gradient of a token or two: W is read and dW written once (1 x 32000 x 1024, bf16: 44 us against 78, fp32 76 against 329; rows off 16 bytes,
+// The same for the gradient of a token or two: W is read and dW written once (1 x 32000 x 1024, bf16: 44 us against 78, fp32 76 against 274; rows off 16 bytes,
 // bf16, 158 against 152).
 bool vocab_few_grad(int64_t T, int D) { return T <= kFewGradTokens && D <= kFewGradDim; }
 
@@ -337,7 +339,7 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
     f.labels = d_labels; f.loss = d_loss; f.stats = d_stats;
     const bool vec = rows_16(d_W, type, w_row_stride, w_group_stride);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const dim3 grid((unsigned)f.blocks, (unsigned)groups);
+    const dim3 grid((unsigned)(f.blocks * f.turns), (unsigned)groups);
     with_type(type, [&](auto ty) {
       constexpr int TY = decltype(ty)::value;
       auto go = [&](auto nt) {
@@ -350,7 +352,7 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
       else if (tokens == 2) go(std::integral_constant<int, 2>());
       else go(std::integral_constant<int, 4>());
     });
-    launch_pdl(vocab_few_join_kernel, dim3((unsigned)groups), dim3(128), 0, st, f);
+    launch_pdl(vocab_few_join_kernel, dim3((unsigned)groups), dim3((unsigned)(32 * tokens)), 0, st, f);
     return op_launched("vocab_loss");
   }
   VocabPlan p = vocab_plan(type, groups, tokens, vocab, dim, rows_16(d_W, type, w_row_stride, w_group_stride), false, static_cast<unsigned char*>(d_work));

@@ -443,9 +443,9 @@ def test_vocab_loss_tokens_that_leave_blocks_without_any(b, T):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("G,T,V,D", [(1, 1, 32000, 1024), (3, 2, 777, 1000), (2, 3, 5000, 130), (5, 4, 33, 7), (1, 5, 900, 64), (1, 4, 40, 9000), (600, 1, 50, 16)])
+@pytest.mark.parametrize("G,T,V,D", [(2, 5, 3001, 72), (1, 8, 500, 333), (40, 7, 100, 48), (1, 8, 20, 6144), (1, 8, 20, 6145), (3, 9, 300, 40), (1, 1, 32000, 1024), (3, 2, 777, 1000), (2, 3, 5000, 130), (5, 4, 33, 7), (1, 5, 900, 64), (1, 4, 40, 9000), (600, 1, 50, 16)])
 def test_vocab_loss_few_tokens(b, G, T, V, D, dtype):
-    """One to five tokens a group, groups without any label among them."""
+    """One to nine tokens a group, groups without any label among them."""
     H, W, y = case(25, G, T, V, D, dtype)
     if G > 1:
         y[1] = -1
