@@ -170,14 +170,14 @@ __device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* 
       if (c0 + j * 256 < D) *reinterpret_cast<uint4*>(to + c0 + j * 256) = r[j].q[0];
   }
 }
-// Eight scaled values as pairs.
+// Eight scaled values as pairs.  An infinity goes to lo beside a zero: as hi it would meet the zeros among the other operand's lo.
 __device__ __forceinline__ void vocab_pairs(const float (&v)[8], uint16_t* hi, uint16_t* lo) {
   uint4 u, w;
   __half* p = reinterpret_cast<__half*>(&u);
   __half* q = reinterpret_cast<__half*>(&w);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    p[i] = __float2half_rn(v[i]);
+    p[i] = __float2half_rn(fabsf(v[i]) == INFINITY ? 0.f : v[i]);
     q[i] = __float2half_rn(v[i] - __half2float(p[i]));
   }
   *reinterpret_cast<uint4*>(hi) = u;
@@ -375,11 +375,13 @@ __device__ __forceinline__ float vt_exp2(float x) {        // (to 2 ulp; results
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// What differences to a largest logit are taken to: classes may have logits of -infinity, and so many of them that a part has no others.
+__device__ __forceinline__ float vocab_base(float top) { return top == -INFINITY ? 0.f : top; }
 __device__ __forceinline__ float2 vocab_merge(float2 p, float2 q) {
   constexpr float kLog2e = 1.4426950408889634f;
   const float m = fmaxf(p.x, q.x);
-  if (m == -INFINITY && p.y == 0.f && q.y == 0.f) return make_float2(m, 0.f);      // (runs without columns)
-  return make_float2(m, p.y * vt_exp2((p.x - m) * kLog2e) + q.y * vt_exp2((q.x - m) * kLog2e));
+  const float base = vocab_base(m);
+  return make_float2(m, p.y * vt_exp2((p.x - base) * kLog2e) + q.y * vt_exp2((q.x - base) * kLog2e));
 }
 template <int ROWS>
 __global__ void __launch_bounds__(256) vocab_join_kernel(const VocabJoin a) {

@@ -108,8 +108,8 @@ __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_kernel(const VocabFe
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
         if (lane == 0 && v0 + r == y[t]) a.zy[g * a.T + first + t] = z;
-        const float m = fmaxf(run[t].x, z);
-        run[t] = make_float2(m, run[t].y * vt_exp2((run[t].x - m) * 1.4426950408889634f) + vt_exp2((z - m) * 1.4426950408889634f));
+        const float m = fmaxf(run[t].x, z), base = vocab_base(m);
+        run[t] = make_float2(m, run[t].y * vt_exp2((run[t].x - base) * 1.4426950408889634f) + vt_exp2((z - base) * 1.4426950408889634f));
       }
     }
   }

@@ -628,9 +628,10 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
 #pragma unroll
             for (int i = 4; i < 32; ++i) most[i & 3] = fmaxf(most[i & 3], v[i]);
             const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-            float part[4] = {sum * vt_exp2((m - top) * kLog2e), 0.f, 0.f, 0.f};
+            const float base = vocab_base(top);
+            float part[4] = {sum * vt_exp2((m - base) * kLog2e), 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) part[i & 3] += vt_exp2((v[i] - top) * kLog2e);
+            for (int i = 0; i < 32; ++i) part[i & 3] += vt_exp2((v[i] - base) * kLog2e);
             sum = (part[0] + part[1]) + (part[2] + part[3]);
             m = top;
           }

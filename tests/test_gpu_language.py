@@ -547,6 +547,28 @@ def test_vocab_loss_rows_of_any_size(b, G, T, V, D):
     assert torch.equal(b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, want_dH=False)[1], dW)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("T", [1, 2, 5, 40, 300])
+def test_vocab_loss_classes_of_minus_infinity(b, T, dtype):
+    """Classes masked by a last column of ones and weights of -infinity, whole tiles of them: as without them.  (Their weights times a gradient of zero leave
+    a NaN in that column of dH, as in the formula.)"""
+    V, D, masked = 900, 72, slice(200, 700)
+    H, W, y = case(120, 2, T, V, D, dtype, padded=False)
+    H[..., -1] = 1.0
+    W[:, masked, -1] = float("-inf")
+    y = torch.where((y >= 200) & (y < 700), y % 200, y)
+    rest, names = torch.cat([W[:, :200], W[:, 700:]], 1), torch.where(y >= 700, y - 500, y)
+    loss, stats = b.prsgd_vocab_loss(H, W, y)
+    check_loss((loss, stats), H, rest, names)
+    dloss = randn(123, 2, T)
+    dH, dW = b.prsgd_vocab_loss_grad(H, W, y, exact_stats(H, rest, names), dloss=dloss)
+    assert (dW[:, masked] == 0).all()
+    wH = ref.vocab_grad(H, rest, names, dloss)[0]
+    check_grad((torch.cat([dH[..., :-1], wH[..., -1:].to(dtype)], -1), torch.cat([dW[:, :200], dW[:, 700:]], 1)), H, rest, names, dloss, None)
+    y[0, 0] = 300
+    assert b.prsgd_vocab_loss(H, W, y)[0][0, 0] == float("inf")
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_vocab_loss_views_of_weights(b, dtype):
     """W's groups as overlapping windows of one table, and columns of a table side by side."""
