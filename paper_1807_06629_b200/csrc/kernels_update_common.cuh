@@ -122,19 +122,23 @@ __global__ void __launch_bounds__(kUpdCommonThreads, 1) tc_update_common_kernel(
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  // the common point is read from worker 0's row (every row holds the same bits)
-  auto load_master = [&](int tile) {
+  // The common point is read from the first row that this CTA stores (every row holds the same bits): of a tile that is
+  // shared, the neighbours may have stored theirs by then.
+  auto load_master = [&](int item) {
+    const int tile = item_tile(item);
+    int nb, ne;
+    item_rows(item, nb, ne);
     const int si = seg_of(tile);
     const int rel = tile - a.seg[si].tile0;
     const int m0 = (rel / a.seg[si].tiles_n) * 128, n0 = (rel % a.seg[si].tiles_n) * 64;
     mbar_expect_tx(mst_full, Cfg::kMaster);
-    tma_load_w(buf_u32, &maps.master[si], mst_full, a.seg[si].wt, n0, m0, 0);
-    tma_load_w(buf_u32 + 16384u, &maps.master[si], mst_full, a.seg[si].wt, n0 + 32, m0, 0);
+    tma_load_w(buf_u32, &maps.master[si], mst_full, a.seg[si].wt, n0, m0, nb);
+    tma_load_w(buf_u32 + 16384u, &maps.master[si], mst_full, a.seg[si].wt, n0 + 32, m0, nb);
   };
   // The master tiles were last written an iteration ago (the launch before this one only reads bf16 copies), so
   // the first one is requested while that launch drains.
   const bool pre = a.prefetch != 0 && *abort_flag == 0 && n_items_all > 0;
-  if (pre && warp == 0 && lane == 0) load_master(item_tile(0));
+  if (pre && warp == 0 && lane == 0) load_master(0);
   if (a.late == 0) {
     pdl_wait();
     pdl_trigger();
@@ -158,7 +162,7 @@ __global__ void __launch_bounds__(kUpdCommonThreads, 1) tc_update_common_kernel(
       const int m0 = (rel / a.seg[si].tiles_n) * 128, n0 = (rel % a.seg[si].tiles_n) * 64;
       if (ti >= 1) ok = mbar_wait(out_free, (ti - 1u) & 1u, abort_flag, a.status, 0x701);   // the store warps hold the previous tile in registers
       if (!ok) break;
-      if (!(pre && ti == 0)) load_master(w);
+      if (!(pre && ti == 0)) load_master((int)ti);
       for (int n = 0; n < a.N; ++n, ++it) {
         const int s = it % S;
         ok = mbar_wait(stage_empty(s), ((it / S) & 1u) ^ 1u, abort_flag, a.status, 0x702);
