@@ -21,7 +21,7 @@
 namespace prsgd {
 
 constexpr int kVtEpiWarps = 16, kVtThreads = 32 * (4 + kVtEpiWarps), kVtRing = 4;
-// Epilogue warps take 32 rows of a CTA's 128 x 256 sums each.  Where sums are added in registers all sixteen share a tile, 64 columns each; else
+// Epilogue warps take 32 rows of a CTA's 128 x 256 sums each.  Where sums are added in registers (PROMOTE) all sixteen share a tile, 64 columns each; else
 // eight take the tiles of one TMEM sum and eight those of the other, 128 columns each, so that one tile's stores run beside the next one's
 // exponentials (gradient, 256 x 256 tiles of G with D = 1024: 10.9 thousand cycles a tile, products 8.2).
 constexpr int kVtShares = kVtEpiWarps / 4;
@@ -32,6 +32,10 @@ constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kV
 // exact to fp32 is summed in TMEM over this many blocks of 64 only, and those sums are added in registers, where they are rounded (stats at
 // 16384 x 131072 x 2048: off by 1.9e-6 with one sum, by 4.3e-7 with sums of 512 products, for 2 to 5 % of the time).
 constexpr int kVtPromote = 8;
+// Gradients of 16-bit types are rounded by more, each term of a sum by 2^-9 or 2^-12 of its own: they are one sum while it has at most kVtLongest
+// products (cut off by about 2^-15 of it), and sums of 64 blocks beyond (131072 tokens of one sign, fp16: dW was off by 4.6e-4).
+constexpr int kVtPromoteLong = 64;
+constexpr int64_t kVtLongest = 8192;
 constexpr int kVtAhead = 8;                    // the next task is claimed when this many blocks of 64 of the current one are left to load
 enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE, VT_ERR_MEET };
 enum { VT_STATS = 0, VT_G, VT_DH, VT_DW };
@@ -69,11 +73,11 @@ struct VocabChain {
 // contraction; seq = g * pieces + p and the place of that piece's G; live tokens of the group.
 struct VTask { int kind, g, ti, tj, n, p, seq, slot, live, k0, kb, pad; };
 
-// Sums of a tile: one, or (PROMOTE) one of the small products of pairs and one per kVtPromote blocks.
-template <bool SPLIT, bool PROMOTE>
+// Sums of a tile: one, or (PROMOTE blocks each) one of the small products of pairs and as many as there are.
+template <bool SPLIT, int PROMOTE>
 __device__ __forceinline__ int vt_sums(int kb) {
-  if (!PROMOTE) return 1;
-  return (SPLIT ? 1 : 0) + (kb + kVtPromote - 1) / kVtPromote;
+  if constexpr (PROMOTE == 0) return 1;
+  else return (SPLIT ? 1 : 0) + (kb + PROMOTE - 1) / PROMOTE;
 }
 
 __device__ __forceinline__ int vt_tiles(int n) { return (n + 255) >> 8; }
@@ -331,12 +335,12 @@ __device__ __forceinline__ void vt_undo32(float (&v)[32], float2 row, const floa
   }
 }
 
-// SPLIT: fp32 operands, products of fp16 pairs.
-template <bool GRAD, bool SPLIT>
+// SPLIT: fp32 operands, products of fp16 pairs.  LONG: a gradient of 16-bit types with contractions of more than kVtLongest products.
+template <bool GRAD, bool SPLIT, bool LONG = false>
 __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
   constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1;
-  constexpr bool PROMOTE = SPLIT || !GRAD;               // (gradients of 16-bit types are rounded by far more)
-  constexpr int kGroups = PROMOTE ? 1 : 2, kWarpCols = PROMOTE ? 64 : 128;
+  constexpr int PROMOTE = SPLIT || !GRAD ? kVtPromote : LONG ? kVtPromoteLong : 0;      // blocks of a sum, 0: all
+  constexpr int kGroups = PROMOTE != 0 ? 1 : 2, kWarpCols = PROMOTE != 0 ? 64 : 128;
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kVtRing + 1];
@@ -470,7 +474,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           for (int q = 0; q < blocks; ++q) {
             const bool first = q == next;
             if (first) {
-              next = !PROMOTE ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + kVtPromote);
+              next = PROMOTE == 0 ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + PROMOTE);
               acc = sums & 1u;
               if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, VT_ERR_ACC_FREE)) { ok = false; break; }
               ptx::tc_fence_after();
@@ -536,7 +540,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
     }
   } else {                                               // ---- epilogue ---------------------------------------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    const int quarter = warp & 3, group = PROMOTE ? 0 : (warp - 4) >> 3, share = ((warp - 4) >> 2) & (kVtShares / kGroups - 1);
+    const int quarter = warp & 3, group = PROMOTE != 0 ? 0 : (warp - 4) >> 3, share = ((warp - 4) >> 2) & (kVtShares / kGroups - 1);
     const uint32_t box = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kWarpCols);
     uint32_t sums = 0;
@@ -556,7 +560,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
       };
       auto gather = [&]() -> bool {
-        if (!PROMOTE || parts == 1) {
+        if (PROMOTE == 0 || parts == 1) {
           acc = sums & 1u;                               // (one group: the sum is its own)
           if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
           ++sums;

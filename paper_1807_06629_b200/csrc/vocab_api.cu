@@ -192,7 +192,7 @@ int vocab_device(int* sms) {
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     auto raise = [&](auto kernel, bool grad) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)vt_smem(grad)); };
     raise(vocab_chain_kernel<false, false>, false); raise(vocab_chain_kernel<false, true>, false);
-    raise(vocab_chain_kernel<true, false>, true); raise(vocab_chain_kernel<true, true>, true);
+    raise(vocab_chain_kernel<true, false>, true); raise(vocab_chain_kernel<true, false, true>, true); raise(vocab_chain_kernel<true, true>, true);
     auto few = [&](auto ty, auto nt) {
       for (auto kernel : {vocab_few_kernel<decltype(ty)::value, true, decltype(nt)::value>, vocab_few_kernel<decltype(ty)::value, false, decltype(nt)::value>})
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
@@ -251,6 +251,7 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, p.tasks));
   auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kVtThreads), vt_smem(p.grad), st, 2, maps, c); };
   if (p.grad && p.split) go(vocab_chain_kernel<true, true>);
+  else if (p.grad && std::max<int64_t>(a.T, D) > kVtLongest) go(vocab_chain_kernel<true, false, true>);      // (dH: parts of 16384 columns at most)
   else if (p.grad) go(vocab_chain_kernel<true, false>);
   else if (p.split) go(vocab_chain_kernel<false, true>);
   else go(vocab_chain_kernel<false, false>);
