@@ -630,6 +630,8 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
  *   G_tv = (dloss_t + dlse_t) e^(z_tv - lse_t) - dloss_t [v = y_t],   dH = G W,   dW = G^T H (or, accumulate, added to what dW holds).
  * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is held with one rounding of the operands' type
  * (fp32: as pairs, scaled by tokens, beside operands scaled by columns, H's after a token's dloss and dlse; none for one or two tokens a group), a piece of the vocabulary at a time.
+ * fp16 holds entries of G down to 2^-15 |d_t| with all its bits and nothing below 2^-26 |d_t|, |d_t| = |dloss_t| + |dlse_t|, whatever the group's largest is
+ * (a token whose |d_t| is more than 2^12 smaller than that is held by its own size, and the copy of its row of H that dW reads is rounded to 2^-36 of that largest).
  * Logits, dH and dW of 16-bit types are summed by the tensor cores, which cut off up to 2^-23 of a running sum every 16 products: sums of 8192 products or fewer
  * (dH: 16384), longer ones in fp32 from sums of 4096.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
  * whose label is padding take no part: their rows of dH are zeros, whatever their H, stats, dloss and dlse hold.  The rows of dH and of dW may

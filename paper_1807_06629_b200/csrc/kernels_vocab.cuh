@@ -10,12 +10,17 @@
 // that a row or column of any size spoils no other: H and W by rows for the logits, and, in copies of their own for the gradient, W by
 // columns (dH = G W) and H, its rows times their share of the gradient, by columns (dW = G^T H).  G_t is held times 2^g_t, such that
 // |dloss_t| + |dlse_t| lies in [2^13, 2^14); that share is 2^-g_t.
+//
+// G of 16-bit types is held times one power of two a group, the same with the group's largest |dloss_t| + |dlse_t|.  fp16 then has
+// all its bits for p |dloss_t| down to 2^-27 of that largest and none below 2^-38: a token whose gradients are more than 2^kLiftFrom smaller is
+// lifted to 2^-kLiftFrom of it, its row of dH brought back by dH's epilogue, and its row of the copy of H that dW reads taken times
+// 2^-lift (what that rounds off is below 2^-36 of the largest a unit of H; lifted all the way, a token 2^10 smaller would lose bits of H there).
 #pragma once
 #include "rows_io.cuh"
 
 namespace prsgd {
 
-// Factors of a group of 16-bit types: G is held times g, dH and dW are sums * back.
+// Factors of a group of 16-bit types: G is held times g (and a token's lift), dH and dW are sums * back.
 struct VocabScale { float g, back; };
 
 struct VocabPrep {
@@ -33,8 +38,8 @@ struct VocabPrep {
   // fp32 operands only: factors that undo the scales, two powers of two each (their product may lie outside a float's range)
   float2* rowf; float2* colf;                  // [groups][Tp], [w_groups][Vp] of the rows of H' and W
   // and the gradient's
-  uint16_t* Hm[2]; uint16_t* Wm[2];            // as Hc and Wc, scaled by columns; nullptr where no product wants them
-  float2* rowg;                                // [groups][Tp] of the rows of G
+  uint16_t* Hm[2]; uint16_t* Wm[2];            // as Hc and Wc, scaled by columns; nullptr where no product wants them.  fp16: Hm[0] is Hc times 2^-lift
+  float2* rowg;                                // [groups][Tp] of the rows of G; fp16: (2^-lift times the group's `back`, 1)
   float2* dhf; float2* dwf;                    // [w_groups][Dp], [groups][Dp] of the columns of Wm and Hm
   unsigned int* most;                          // [2][groups][Dp] largest finite magnitudes (bits) of those columns: W, H
   int64_t Vp; int Dp;                          // V, D rounded up to 256
@@ -78,6 +83,11 @@ __device__ __forceinline__ float2 vocab_halves(int n) { return make_float2(vocab
 __device__ __forceinline__ int vocab_g_exponent(float dloss, float dlse) {
   const float d = finite_abs(fabsf(dloss) + fabsf(dlse));
   return d > 0.f ? vocab_exponent(d, 13) : 0;
+}
+constexpr int kLiftFrom = 12;
+__device__ __forceinline__ int vocab_lift(float dloss, float dlse, int group_exponent) {        // (0 of a token without a gradient)
+  const float d = finite_abs(fabsf(dloss) + fabsf(dlse));
+  return d > 0.f ? max(0, vocab_exponent(d, 13) - group_exponent - kLiftFrom) : 0;
 }
 __device__ __forceinline__ float vocab_share(float dloss, float dlse) {
   return dloss == 0.f && dlse == 0.f ? 0.f : vocab_power(-vocab_g_exponent(dloss, dlse));
@@ -160,14 +170,23 @@ __device__ __forceinline__ void vocab_load_row(const typename ElemOf<TY>::type* 
     }
   }
 }
+// Where `shared`, also times `share`, rounded again where that leaves fp16's normal numbers.
 template <int TY, bool VEC>
-__device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* from, uint16_t* to, int D, int lane) {
+__device__ __forceinline__ void vocab_copy_row(const typename ElemOf<TY>::type* from, uint16_t* to, int D, int lane, uint16_t* shared = nullptr, float share = 1.f) {
   for (int c0 = lane * 8; c0 < D; c0 += 256 * kVocabAhead) {
     Raw8<TY> r[kVocabAhead];
     vocab_load_row<TY, VEC>(from, c0, D, r);
 #pragma unroll
-    for (int j = 0; j < kVocabAhead; ++j)
-      if (c0 + j * 256 < D) *reinterpret_cast<uint4*>(to + c0 + j * 256) = r[j].q[0];
+    for (int j = 0; j < kVocabAhead; ++j) {
+      if (c0 + j * 256 >= D) break;
+      *reinterpret_cast<uint4*>(to + c0 + j * 256) = r[j].q[0];
+      if (TY != PRSGD_TYPE_FP16 || shared == nullptr) continue;
+      float v[8];
+      unpack8<TY>(r[j], v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= share;
+      store_raw<TY>(reinterpret_cast<typename ElemOf<TY>::type*>(shared + c0 + j * 256), v);
+    }
   }
 }
 // Eight scaled values as pairs.  An infinity goes to lo beside a zero: as hi it would meet the zeros among the other operand's lo.
@@ -225,8 +244,9 @@ __device__ __forceinline__ void vocab_split_row(const float* from, uint16_t* hi,
   }
 }
 
-// Blocks x < h_blocks of a group move its live rows together, the others copy W.  A block counts the live tokens before its own; the
-// group's first block counts all, finds the scales, and zeroes the rows behind the last live one that a product may read.
+// Blocks x < h_blocks of a group move its live rows together, the others copy W.  A block counts the live tokens before its own (and, of fp16,
+// looks for the group's largest gradient); the group's first block counts all, finds the scales, and zeroes the rows behind the last live one that a
+// product may read.
 template <int TY>
 __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
   using T = typename ElemOf<TY>::type;
@@ -238,7 +258,7 @@ __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
   op_pdl_trigger();
   const int64_t g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr bool SPLIT = TY == PRSGD_TYPE_FP32;
+  constexpr bool SPLIT = TY == PRSGD_TYPE_FP32, LIFT = TY == PRSGD_TYPE_FP16;
   const unsigned int* most_w = SPLIT && a.grad ? a.most + g * a.Dp : nullptr;
   const unsigned int* most_h = SPLIT && a.grad ? a.most + (a.groups + g) * a.Dp : nullptr;
   if ((int)blockIdx.x >= a.h_blocks) {                     // ---- W
@@ -262,27 +282,28 @@ __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
   const int32_t* labels = a.labels + g * a.T;
   const int64_t per = (a.T + a.h_blocks - 1) / a.h_blocks, begin = min(a.T, blockIdx.x * per), end = min(a.T, begin + per);
   auto is_live = [&](int y) { return y >= 0 && y < a.V; };
-  int before = 0;
-  for (int64_t t = threadIdx.x; t < begin; t += 256) before += is_live(labels[t]) ? 1 : 0;
+  const bool whole = blockIdx.x == 0 || (LIFT && a.grad);  // (looks at all tokens)
+  int before = 0, all = 0;
+  float most = 0.f;
+  for (int64_t t = threadIdx.x; t < (whole ? a.T : begin); t += 256) {
+    const int on = is_live(labels[t]) ? 1 : 0;
+    const float d = !whole || !a.grad ? 0.f : (a.dloss ? fabsf(a.dloss[g * a.T + t]) : 0.f) + (a.dlse ? fabsf(a.dlse[g * a.T + t]) : 0.f);
+    all += on;
+    before += t < begin ? on : 0;
+    most = fmaxf(most, on ? finite_abs(d) : 0.f);
+  }
   before = vocab_block_sum(before, smi);
+  if (blockIdx.x == 0) all = vocab_block_sum(all, smi);
+  if (whole && a.grad) most = vocab_block_max(most, smf);
+  const int e_group = most > 0.f ? vocab_exponent(most, 13) : 0;
   if (blockIdx.x == 0) {
     if (g == 0) {
       if (threadIdx.x < sizeof(DeviceStatus) / 4) reinterpret_cast<unsigned int*>(a.status)[threadIdx.x] = 0u;
       for (int i = threadIdx.x; i < a.n_counters; i += 256) a.counters[i] = 0u;
     }
-    int all = 0;
-    float most = 0.f;
-    for (int64_t t = threadIdx.x; t < a.T; t += 256) {
-      if (!is_live(labels[t])) continue;
-      ++all;
-      if (a.grad) most = fmaxf(most, finite_abs((a.dloss ? fabsf(a.dloss[g * a.T + t]) : 0.f) + (a.dlse ? fabsf(a.dlse[g * a.T + t]) : 0.f)));
-    }
-    all = vocab_block_sum(all, smi);
-    most = vocab_block_max(most, smf);
     if (threadIdx.x == 0) {
       a.live[g] = all;
-      const int e = most > 0.f ? vocab_exponent(most, 13) : 0;
-      a.scale[g] = {vocab_power(e), vocab_power(-e)};
+      a.scale[g] = {vocab_power(e_group), vocab_power(-e_group)};
     }
     if (SPLIT && a.grad) {
       for (int c = threadIdx.x; c < a.D; c += 256) {
@@ -295,7 +316,7 @@ __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
       for (int64_t r = all + warp; r < last; r += 8)
         for (int c = lane * 8; c < a.pitch; c += 256) {
           const int64_t o = (g * a.Tp + r) * a.pitch + c;
-          *reinterpret_cast<uint4*>((SPLIT ? a.Hm[0] : a.Hc[0]) + o) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>((a.Hm[0] ? a.Hm[0] : a.Hc[0]) + o) = make_uint4(0, 0, 0, 0);
           if (SPLIT) *reinterpret_cast<uint4*>(a.Hm[1] + o) = make_uint4(0, 0, 0, 0);
         }
     }
@@ -322,10 +343,14 @@ __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
         a.index[c] = (int)t;
         if (a.grad) {
           const float dl = a.dloss ? a.dloss[o] : 0.f, ds = a.dlse ? a.dlse[o] : 0.f;
-          const int e = SPLIT ? vocab_g_exponent(dl, ds) : 0;
-          const float up = vocab_power(e);
-          a.rowp[c] = make_float4(a.stats[2 * o], a.stats[2 * o + 1], (dl + ds) * up, dl * up);
+          const int e = SPLIT ? vocab_g_exponent(dl, ds) : LIFT ? vocab_lift(dl, ds, e_group) : 0;
+          const float2 up = vocab_halves(e);
+          a.rowp[c] = make_float4(a.stats[2 * o], a.stats[2 * o + 1], (dl + ds) * up.x * up.y, dl * up.x * up.y);
           if (SPLIT) { a.rowg[c] = vocab_halves(-e); shares[threadIdx.x] = vocab_share(dl, ds); }
+          if (LIFT) {                              // (e_group + e is at most the token's own exponent less kLiftFrom)
+            a.rowg[c] = make_float2(vocab_power(-(e_group + e)), 1.f);
+            shares[threadIdx.x] = e <= 126 ? vocab_power(-e) : 0.f;
+          }
         }
       } else if (!a.grad) {
         a.loss[o] = 0.f;
@@ -347,8 +372,10 @@ __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
           if (a.vec_h) vocab_split_row<true>(from, a.Hc[0] + o, a.Hc[1] + o, undo, m, a.Hm[1] + o, share, most_h, a.D, lane);
           else vocab_split_row<false>(from, a.Hc[0] + o, a.Hc[1] + o, undo, m, a.Hm[1] + o, share, most_h, a.D, lane);
         } else {
-          if (a.vec_h) vocab_copy_row<TY, true>(from, a.Hc[0] + o, a.D, lane);
-          else vocab_copy_row<TY, false>(from, a.Hc[0] + o, a.D, lane);
+          uint16_t* m = LIFT && a.Hm[0] ? a.Hm[0] + o : nullptr;
+          const float share = LIFT && a.grad ? shares[i] : 1.f;
+          if (a.vec_h) vocab_copy_row<TY, true>(from, a.Hc[0] + o, a.D, lane, m, share);
+          else vocab_copy_row<TY, false>(from, a.Hc[0] + o, a.D, lane, m, share);
         }
       } else if (a.dH != nullptr) {
         const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};

@@ -716,8 +716,8 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           }
         } else {
           const bool of_w = k.kind == VT_DW;
-          const float back = SPLIT ? 1.f : sc->back;
-          const float2 rf = SPLIT && !of_w && r0 + lane < k.live ? a.rowg[(int64_t)k.g * a.Tp + r0 + lane] : make_float2(1.f, 1.f);
+          const float2 rf = a.rowg != nullptr && !of_w && r0 + lane < k.live ? a.rowg[(int64_t)k.g * a.Tp + r0 + lane] : make_float2(SPLIT ? 1.f : sc->back, 1.f);
+          const float back = rf.x;                       // (of 16-bit types)
           const float2* const cf = of_w ? a.dwf + (int64_t)k.g * a.Dp : a.dhf + (int64_t)(a.w_shared ? 0 : k.g) * a.Dp;
           VOut d;
           d.cols = a.D; d.index = nullptr; d.reduce = 0;

@@ -56,12 +56,12 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
     a.Hc[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
     a.Wc[i] = reinterpret_cast<uint16_t*>(take(p.copy_w ? 2 * (size_t)groups * V * a.pitch : 0));
   }
-  if (p.split && grad) {
-    for (int i = 0; i < planes; ++i) {
-      a.Hm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
-      a.Wm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * V * a.pitch));
-    }
+  if (grad && type != PRSGD_TYPE_BF16) {
+    for (int i = 0; i < planes; ++i) a.Hm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
     c.rowg = a.rowg = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Tp));
+  }
+  if (p.split && grad) {
+    for (int i = 0; i < planes; ++i) a.Wm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * V * a.pitch));
     c.dhf = a.dhf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Dp));
     c.dwf = a.dwf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Dp));
     a.most = reinterpret_cast<unsigned int*>(take(4 * 2 * (size_t)groups * a.Dp));

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import language_reference as ref
-from test_gpu_language import BF16, F16, F32, U, b, check, gen, half, randn          # noqa: F401  (b: a fixture)
+from test_gpu_language import BF16, F16, F32, U, b, case, check, gen, half, randn, z_error          # noqa: F401  (b: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,52 @@ def test_gradient_of_many_columns(b):
     check(dW, torch.full_like(dW, T / V).double(), torch.tensor((off + one_sum(T)) * T / V, device="cuda:0"))
     want = row.double().expand(1, T, D)
     check(dH, want, (off + one_sum(V) + half(F16)) * want + 2.0 ** -25)
+
+
+# ---- fp16: gradients of different sizes in one group ----------------------------------------------------------
+@pytest.mark.parametrize("G,T,V,D", [(1, 60, 20000, 64), (2, 300, 2500, 100), (3, 70, 400, 1100), (1, 8300, 600, 40)])
+def test_fp16_gradients_of_any_size(b, G, T, V, D):
+    """fp16: tokens whose dloss and dlse are up to 2^30 smaller than the group's largest (2^13), beside some without any: a token's row of dH
+    is as good, relative to its own, as that of the largest.  A last column of ones in W makes that column of dH dlse_t: what G's smallest entries lose shows there.
+
+    G: one rounding, and 2^-26 d_t (d = |dloss| + |dlse|) where fp16 has no more bits: its row is held such that d_t lies in [2, 2^14).  dW: the same
+    with H's row, which is held in fp16 times d_t's share of the largest beyond 2^-12: 2^-25 of its unit, 2^-36 of the largest d_t a G of d_t."""
+    H, W, y = case(130, G, T, V, D, F16, padded=T < 1000)
+    W[..., -1] = 1.0
+    size = 2.0 ** (13.0 - (torch.arange(T, device="cuda:0") % 31))
+    dloss = (torch.rand(G, T, generator=gen(133), device="cuda:0") - 0.5) * 0.8 * size
+    dlse = (0.5 + 0.5 * torch.rand(G, T, generator=gen(134), device="cuda:0")) * 0.5 * size
+    dloss[:, 5::17], dlse[:, 5::17] = 0.0, 0.0
+    stats = ref.vocab_loss(H, W, y)[1].float()
+    dW = torch.full((G, V, D), float("nan"), device="cuda:0")
+    work = b.vocab_loss_grad_workspace(H, W).fill_(0xFF)
+    dH, _ = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dlse=dlse, dW=dW, workspace=work)
+    b.prsgd_work_status(work)
+    wH, wW, mH, mW, A = ref.vocab_grad(H, W, y, dloss, dlse)
+    on = ref.live_tokens(y, V)
+    Hz, d = H.double().abs() * on[..., None], (dloss.abs() + dlse.abs()).double() * on
+    top = d.amax(1)[:, None, None]
+    ez = z_error(Hz, W, D).amax(-1, keepdim=True) + 4 * U * stats.double().abs().sum(-1, keepdim=True)
+    off = lambda n: half(F16) + 2 * ez + 2.0 ** -20 + (n / 16 + 4) * 2.0 ** -22          # noqa: E731
+    check(dH, wH, off(V) * mH + 2.0 ** -26 * d[..., None] * W.double().abs().sum(1, keepdim=True) + half(F16) * wH.abs() + 2.0 ** -25)
+    share = (A / d.clamp(min=1e-300)[..., None]).sum(1)[..., None]
+    check(dW, wW, (A * off(T)).mT @ Hz + 2.0 ** -37 * top * Hz.sum(1, keepdim=True) + 2.0 ** -36 * top * share + 2 * half(F32) * wW.abs())
+    only = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dlse=dlse, want_dW=False)[0]
+    assert torch.equal(only, dH)
+
+
+def test_fp16_gradients_beyond_a_floats_exponents(b):
+    """Sizes whose quotient no float holds: the small ones' rows are theirs alone, the large ones' share of dW is not touched."""
+    H, W, y = case(140, 1, 40, 300, 64, F16, padded=False)
+    stats = ref.vocab_loss(H, W, y)[1].float()
+    dloss = torch.full((1, 40), 2.0 ** 100, device="cuda:0")
+    dloss[0, 20:] = 2.0 ** -60
+    dW = torch.empty(1, 300, 64, device="cuda:0")
+    b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss, dW=dW, want_dH=False)
+    alone, large = torch.where(dloss > 1, y, -1), torch.empty_like(dW)
+    b.prsgd_vocab_loss_grad(H, W, alone, stats, dloss=dloss, dW=large, want_dH=False)
+    assert torch.isfinite(dW).all() and torch.equal(dW, large)
+    dloss[0, 20:], dloss[0, :20] = 1.0, 2.0 ** 120
+    want = b.prsgd_vocab_loss_grad(H, W, torch.where(dloss == 1, y, -1), stats, dloss=dloss)[0]
+    got = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss)[0]
+    check(got[:, 20:], want[:, 20:].double(), 2.0 ** -9 * want[:, 20:].double().abs() + 2.0 ** -12)
