@@ -36,7 +36,7 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 template <int TY, bool VEC, int NT>
 __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_kernel(const VocabFew a) {
   using T = typename ElemOf<TY>::type;
-  extern __shared__ float h[];                 // [NT][dp], zeros for tokens without a label
+  extern __shared__ __align__(16) float h[];                 // [NT][dp], zeros for tokens without a label
   __shared__ float2 sums[kFewWarps][NT];
   op_pdl_wait();
   op_pdl_trigger();
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) vocab_few_grad_kernel(const Vo
   using T = typename ElemOf<TY>::type;
   using O = typename ElemOf<OTY>::type;
   constexpr float kLog2e = 1.4426950408889634f;
-  extern __shared__ float h[];                 // [NT][dp]; at the end [row groups][NT][dp]
+  extern __shared__ __align__(16) float h[];                 // [NT][dp]; at the end [row groups][NT][dp]
   __shared__ float gs[2][kFewTile][NT];
   const VocabFew& a = b.f;
   op_pdl_wait();
