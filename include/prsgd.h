@@ -583,8 +583,8 @@ int prsgd_embed(const void* d_table, int32_t type, int64_t row_stride, int64_t g
                 void* d_out, int32_t out_type, int64_t out_row_stride, int64_t out_group_stride, void* cuda_stream);
 
 /* Its gradient with respect to the table: dtable_v = scale * sum of dout_t over the tokens with id_t = v, or (accumulate) that added
- * to what dtable holds.  Tokens are sorted by id, sums are fp32 in an order that depends on the ids alone: the same call gives
- * the same bits.  Without accumulate rows of ids that do not occur are written as zeros; with it they are neither read nor
+ * to what dtable holds.  Tokens are sorted by id, sums are fp32 in an order that depends on the group's ids and the number of tokens alone: the
+ * same call gives the same bits, and a group of a sharded job those that it has in the whole one.  Without accumulate rows of ids that do not occur are written as zeros; with it they are neither read nor
  * written.  The rows of dtable may not overlap (a table that all groups share has one gradient: call with groups = 1 and the
  * groups' tokens behind one another), and dtable may share no memory with dout. */
 int prsgd_embed_grad_workspace_bytes(int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, size_t* bytes);

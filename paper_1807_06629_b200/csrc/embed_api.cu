@@ -18,11 +18,10 @@ int check_tokens(const int32_t* ids, int64_t groups, int64_t tokens, int64_t voc
   return PRSGD_OK;
 }
 
-// Sorted tokens of a unit: such that two threads' worth of units and columns falls on each place of the GPU, 8 at least, 256 at most.
-int embed_unit(int64_t groups, int64_t tokens, int chunks) {
-  const int64_t fit = groups * tokens * chunks / (148 * 2048);
-  return (int)std::max<int64_t>(8, std::min<int64_t>(256, fit / 8 * 8));
-}
+// Sorted tokens of a unit, at whose borders a run's sum is cut: by the number of tokens alone, so that a group's sums have the same bits whatever
+// other groups are in the call.  Few of them, so that short calls have many units (2 x 500 x 100: 8 22 us, 16 28, 32 37 with cold caches; 32 x 512 x 256 28, 30, 38);
+// more, so that long ones have few parts to join (1 x 8192 x 2048 back to back: 8 40 us, 16 35, 32 33; 4 x 8192 x 2048 108, 97, 92; 16 x 16384 x 64 84, 71, 72).
+int embed_unit(int64_t tokens) { return (int)std::max<int64_t>(8, std::min<int64_t>(32, tokens / 256 / 8 * 8)); }
 
 EmbedGradArgs embed_grad_carve(int64_t groups, int64_t tokens, int64_t vocab, int dim, unsigned char* base, size_t* bytes) {
   EmbedGradArgs a{};
@@ -37,7 +36,7 @@ EmbedGradArgs embed_grad_carve(int64_t groups, int64_t tokens, int64_t vocab, in
   a.ctas = 1;
   while (a.ctas < kSortCtas && a.ctas * kSortTurn < tokens) a.ctas *= 2;
   a.turns = (int)std::max<int64_t>(1, (tokens + a.ctas * kSortTurn - 1) / (a.ctas * kSortTurn));
-  a.unit = embed_unit(groups, tokens, a.chunks);
+  a.unit = embed_unit(tokens);
   a.units = (int)((tokens + a.unit - 1) / a.unit);
   size_t off = 0;
   auto take = [&](size_t n) { unsigned char* p = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return p; };
