@@ -17,6 +17,7 @@
 #pragma once
 #include "kernels_vocab.cuh"
 #include "tc_pair.cuh"
+#include "vocab_plan.h"
 
 namespace prsgd {
 
@@ -35,7 +36,6 @@ constexpr int kVtPromote = 8;
 // Gradients of 16-bit types are rounded by more, each term of a sum by 2^-9 or 2^-12 of its own: they are one sum while it has at most kVtLongest
 // products (cut off by about 2^-15 of it), and sums of 64 blocks beyond (131072 tokens of one sign, fp16: dW was off by 4.6e-4).
 constexpr int kVtPromoteLong = 64;
-constexpr int64_t kVtLongest = 8192;
 constexpr int kVtAhead = 8;                    // the next task is claimed when this many blocks of 64 of the current one are left to load
 enum { VT_ERR_DEP = 0x801, VT_ERR_FULL, VT_ERR_EMPTY, VT_ERR_ACC, VT_ERR_ACC_FREE, VT_ERR_RING, VT_ERR_RING_FREE, VT_ERR_MEET };
 enum { VT_STATS = 0, VT_G, VT_DH, VT_DW };

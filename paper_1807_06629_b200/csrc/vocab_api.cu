@@ -15,18 +15,14 @@ int check_vocab(int type, int64_t groups, int64_t tokens, int64_t vocab, int dim
   return PRSGD_OK;
 }
 
-constexpr int kPairs = 74;                     // CTA pairs of the GPU (148 SMs)
-
 // How a call is cut up and what its workspace holds.
 struct VocabPlan {
   VocabPrep prep{};
   VocabChain chain{};
-  bool grad = false, split = false, copy_w = false;
+  bool grad = false, split = false, copy_w = false, longest = false;
   int64_t tasks = 0;         // at most
   size_t bytes = 0;
 };
-
-int64_t up(int64_t x, int64_t by) { return (x + by - 1) / by; }
 
 VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool w_aligned, bool grad, unsigned char* base) {
   VocabPlan p;
@@ -35,9 +31,9 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
   VocabPrep& a = p.prep;
   VocabChain& c = p.chain;
   a.groups = groups; a.T = T; a.V = V; a.D = D; a.grad = grad; a.h_type = type;
-  a.Tp = round_up(std::max<int64_t>(T, 1), 64); a.pitch = (int)round_up(D, 8);
+  const VocabCuts cuts = vocab_cuts(p.split, grad, groups, T, V, D);
+  a.Tp = cuts.Tp; a.pitch = (int)round_up(D, 8);
   a.w_groups = (int)groups;
-  const int64_t tm = up(a.Tp, 256), nv = up(V, 256), td = up(D, 256);
   c.groups = (int)groups; c.D = D; c.T = T; c.V = V; c.Tp = a.Tp; c.bf16 = type == PRSGD_TYPE_BF16;
   size_t off = 0;
   auto take = [&](size_t n) { unsigned char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
@@ -66,45 +62,23 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
     c.dwf = a.dwf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Dp));
     a.most = reinterpret_cast<unsigned int*>(take(4 * 2 * (size_t)groups * a.Dp));
   }
-  c.tiles = (int)nv; c.td = (int)td; c.kd = (int)up(D, 64); c.by_td = FastDiv((uint32_t)td);
+  c.tiles = cuts.tiles; c.td = cuts.td; c.kd = cuts.kd; c.by_td = FastDiv((uint32_t)cuts.td);
+  p.tasks = cuts.tasks; p.longest = cuts.longest != 0;
   if (!grad) {
-    // A run: tiles along the vocabulary whose maxima and sums one task keeps in registers; longer ones leave fewer parts behind, as long
-    // as every pair gets eight.
-    c.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * tm * nv / (8 * kPairs)));
-    c.runs = (int)up(nv, c.run);
+    c.run = cuts.run; c.runs = cuts.runs;
     c.part = reinterpret_cast<float2*>(take(8 * (size_t)groups * c.runs * a.Tp));
     c.zy = reinterpret_cast<float*>(take(4 * (size_t)groups * a.Tp));
-    p.tasks = groups * tm * c.runs;
     a.n_counters = 1;
     a.counters = c.claim = reinterpret_cast<unsigned int*>(take(4));
     p.bytes = off;
     return p;
   }
   c.rowp = a.rowp = reinterpret_cast<float4*>(take(16 * (size_t)groups * a.Tp));
-  // A piece of G takes about 64 MB (8192 x 65536 x 2048: 16 MB 5.85 ms, 32 5.34, 64 5.04, 128 and 256 5.05: dH is added to once a piece).
-  const int64_t fit = (64ll << 20) / (a.Tp * 2 * planes) / 256 * 256;
-  c.piece = (int)std::min<int64_t>(nv * 256, std::max<int64_t>(512, fit));
-  c.pieces = (int)up(V, c.piece);
-  c.piece = (int)(up(nv, c.pieces) * 256);     // (equal ones)
-  c.pieces = (int)up(V, c.piece);
-  c.gp = (int)round_up(std::min<int64_t>(c.piece, V), 64);
-  const int64_t npv = c.piece / 256, seqs = groups * c.pieces;
-  // Parts of dH's contraction: of 4096 columns or fewer, and more while there are not two tiles a pair, but of 1024 or more.
-  const int64_t few = up(2 * kPairs, tm * td);
-  c.parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(c.piece / 4096, std::min<int64_t>(few, c.piece / 1024)), 32));
-  // Tiles of dW along the vocabulary that are one task: claiming takes about 2 us, as long as the products of 8 blocks of 64 tokens.
-  c.run_w = (int)std::max<int64_t>(1, std::min<int64_t>(8 * 64 / std::min<int64_t>(a.Tp, 512), groups * c.pieces * npv * td / (4 * kPairs)));
-  c.kpart = (int)up(up(std::min<int64_t>(c.piece, V), 64), c.parts);
-  c.h_first = c.kpart > a.Tp / 64 * c.run_w;   // the longer uses of a piece first
+  c.piece = cuts.piece; c.pieces = cuts.pieces; c.gp = cuts.gp; c.parts = cuts.parts; c.kpart = cuts.kpart; c.run_w = cuts.run_w;
+  c.h_first = cuts.h_first; c.last_tiles = cuts.last_tiles; c.last_blocks = cuts.last_blocks; c.lag = cuts.lag; c.slots = cuts.slots;
   c.by_run_w = FastDiv((uint32_t)c.run_w);
-  c.last_tiles = (int)(nv - (c.pieces - 1) * npv);
-  c.last_blocks = (int)up(V - (int64_t)(c.pieces - 1) * c.piece, 64);
-  // Uses of a piece follow its tiles of G by as many pieces as hold two tiles a pair (16 groups of 64 tokens and 1000 classes: all G first); a
-  // piece's place is taken again as many later.
-  c.lag = (int)std::max<int64_t>(1, std::min<int64_t>(seqs, up(2 * kPairs, tm * npv)));
-  c.slots = (int)std::min<int64_t>(seqs, 2 * c.lag + 1);
+  const int64_t seqs = cuts.seqs;
   for (int i = 0; i < planes; ++i) c.G[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)c.slots * a.Tp * c.gp));
-  p.tasks = seqs * (tm * npv + up(npv, c.run_w) * td + tm * td * c.parts);
   c.acc_pitch = (int)round_up(D, 8);
   c.acc = reinterpret_cast<float*>(take(c.pieces * c.parts > 1 ? 4 * (size_t)groups * c.parts * a.Tp * c.acc_pitch : 0));
   if (c.pieces * c.parts == 1) c.acc = nullptr;
@@ -251,7 +225,7 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
   const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, p.tasks));
   auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kVtThreads), vt_smem(p.grad), st, 2, maps, c); };
   if (p.grad && p.split) go(vocab_chain_kernel<true, true>);
-  else if (p.grad && std::max<int64_t>(a.T, D) > kVtLongest) go(vocab_chain_kernel<true, false, true>);      // (dH: parts of 16384 columns at most)
+  else if (p.longest) go(vocab_chain_kernel<true, false, true>);
   else if (p.grad) go(vocab_chain_kernel<true, false>);
   else if (p.split) go(vocab_chain_kernel<false, true>);
   else go(vocab_chain_kernel<false, false>);
