@@ -6,11 +6,11 @@
 // the blocks'.  1 x 1 x 32000 x 1024: bf16 20 us (10 of them W from HBM, 8 two launches and the reading of H), fp32 27 (20).
 #pragma once
 #include "kernels_vocab.cuh"
+#include "vocab_plan.h"
 
 namespace prsgd {
 
-constexpr int kFewTokens = 8, kFewTurn = 4, kFewRows = 4, kFewWarps = 8;
-constexpr int64_t kFewSmem = 96 * 1024;        // H of a group as fp32
+constexpr int kFewRows = 4, kFewWarps = 8;
 
 struct VocabFew {
   const void* H; int64_t h_row, h_group;
@@ -163,7 +163,8 @@ __global__ void __launch_bounds__(32 * kFewTokens) vocab_few_join_kernel(const V
 // way), then a thread takes eight columns of every row again (from L1), writes dW = sum_t g_t H_t and adds g_t W to its dH_t in
 // registers.  The blocks' dH are added up by a second launch.  Bytes bound it: W read, dW written; 1 x 1 x 32000 x 1024 bf16 44 us (20 of them the
 // bytes; two blocks an SM that take turns at waiting), 1 x 131072 x 2048 270 us (164).
-constexpr int kFewGradTokens = 2, kFewTile = kFewWarps * kFewRows, kFewGradDim = 32 * kFewWarps * 8;
+constexpr int kFewTile = kFewWarps * kFewRows;
+static_assert(kFewGradDim == 32 * kFewWarps * 8, "a thread has eight columns");
 
 struct VocabFewGrad {
   VocabFew f;

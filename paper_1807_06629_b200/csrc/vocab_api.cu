@@ -89,13 +89,6 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
   return p;
 }
 
-// The loss of few tokens a group has its own form without tensor cores, where H fits in shared memory: up to two of 16-bit types (1 x 32000 x 1024, bf16:
-// one token 20 us against 27, two 24 against 27, four 30 against 27), up to eight of fp32, which spares the copy of W as pairs (cold caches: three
-// tokens 42 us against 100, eight 58, twelve 77, sixteen 95; but 4 x 100000 x 256 sixteen 413, as long as with the copy).
-bool vocab_few(int type, int64_t T, int D) {
-  return T <= (type == PRSGD_TYPE_FP32 ? kFewTokens : 2) && (T <= 2 ? T : kFewTurn) * round_up(D, 8) * 4 <= kFewSmem;
-}
-
 VocabFew vocab_few_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned char* base, size_t* bytes) {
   VocabFew a{};
   a.T = (int)T; a.V = V; a.D = D; a.dp = (int)round_up(D, 8);
@@ -113,10 +106,6 @@ VocabFew vocab_few_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned ch
   *bytes = off;
   return a;
 }
-
-// The same for the gradient of a token or two: W is read and dW written once (1 x 32000 x 1024, bf16: 44 us against 78, fp32 76 against 274; rows off 16 bytes,
-// bf16, 158 against 152).
-bool vocab_few_grad(int64_t T, int D) { return T <= kFewGradTokens && D <= kFewGradDim; }
 
 VocabFewGrad vocab_few_grad_plan(int64_t groups, int64_t T, int64_t V, int D, unsigned char* base, size_t* bytes) {
   VocabFewGrad b{};
@@ -277,7 +266,7 @@ int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t token
   if (!bytes) return op_fail(PRSGD_ERR_ARG, "bytes is NULL");
   const int rc = check_vocab(type, groups, tokens, vocab, dim);
   if (rc != PRSGD_OK) return rc;
-  if (vocab_few(type, tokens, dim)) vocab_few_plan(groups, tokens, vocab, dim, nullptr, bytes);
+  if (vocab_few(type == PRSGD_TYPE_FP32, groups, tokens, vocab, dim)) vocab_few_plan(groups, tokens, vocab, dim, nullptr, bytes);
   else *bytes = vocab_plan(type, groups, tokens, vocab, dim, w_aligned != 0, false, nullptr).bytes;
   return PRSGD_OK;
 }
@@ -302,7 +291,7 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
   if (rc == PRSGD_OK) rc = check_floats(d_labels, d_loss, d_stats, nullptr);
   if (rc != PRSGD_OK) return rc;
   if (!d_loss || !d_stats) return op_fail(PRSGD_ERR_ARG, "an output is NULL");
-  if (vocab_few(type, tokens, dim)) {
+  if (vocab_few(type == PRSGD_TYPE_FP32, groups, tokens, vocab, dim)) {
     size_t need = 0;
     VocabFew f = vocab_few_plan(groups, tokens, vocab, dim, static_cast<unsigned char*>(d_work), &need);
     rc = check_work(d_work, work_bytes, need);

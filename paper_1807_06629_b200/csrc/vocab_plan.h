@@ -29,6 +29,25 @@ struct VocabCuts {
   int lag, slots;                              // uses follow G by that many pieces; pieces of G that have a place
 };
 
+// The loss of few tokens a group has its own form without tensor cores, where H fits in shared memory: two launches instead of three, but a class
+// costs each token a sum over a warp.
+// fp32, up to eight tokens: no copy of W as pairs (against the form of many tokens, us with cold caches; 1 x 32000 x 1024: one token 37 against 100, three 41 and 102, eight
+// 55 and 101; 4 x 8 x 100000 x 256 211 and 318; 16 x 8 x 1000 x 1024 37 and 64; 64 x 4 x 5000 x 300 172 and 305).
+// 16 bits, one or two tokens, while the tokens' classes are few (1 x 1 x 32000 x 1024 27 against 34, 1 x 2 31 and 35, 16 x 2 x 4000 x 1024 49 and 49; of more the sums decide:
+// 1 x 2 x 100000 x 384 51 and 37, x 1024 68 and 64; 64 x 1 x 5000 x 300 170 and 162, 4 x 2 x 100000 x 256 90 and 64).
+constexpr int kFewTokens = 8, kFewTurn = 4;    // tokens of a group at most, of a block at a time
+constexpr int64_t kFewSmem = 96 * 1024;        // H of a block's tokens as fp32
+constexpr int64_t kFewSums = 1 << 17;
+inline bool vocab_few(bool fp32, int64_t groups, int64_t T, int64_t V, int D) {
+  return T <= (fp32 ? kFewTokens : 2) && (T <= 2 ? T : kFewTurn) * up_to(D, 8) * 4 <= kFewSmem && (fp32 || groups * T * V <= kFewSums);
+}
+
+// The same for the gradient of a token or two: W is read and dW written once (against the form of many tokens, us with cold caches; 1 x 1 x 32000 x 1024 bf16 49 against 77,
+// fp32 80 and 274; 1 x 131072 x 2048 bf16 270 and 351; 16 x 2 x 1000 x 1024 bf16 33 and 51; 64 x 1 x 5000 x 300 bf16 531 and 855.  Rows off 16 bytes, bf16: 1 x 1 x 32000 x 1024 157
+// and 153, 1 x 2 149 and 153, 1 x 131072 x 2048 903 and 1095, 16 x 2 x 1000 x 1024 84 and 96, 4 x 2 x 100000 x 256 464 and 569).
+constexpr int kFewGradTokens = 2, kFewGradDim = 2048;
+inline bool vocab_few_grad(int64_t T, int D) { return T <= kFewGradTokens && D <= kFewGradDim; }
+
 // split: fp32 operands, two planes each.
 inline VocabCuts vocab_cuts(bool split, bool grad, int64_t groups, int64_t T, int64_t V, int D) {
   VocabCuts c{};

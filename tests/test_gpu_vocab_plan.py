@@ -3,6 +3,7 @@
 import pytest
 import torch
 
+import language_reference as ref
 import vocab_shapes as shapes
 from test_gpu_language import BF16, F16, F32, b, case, check_grad, check_loss, exact_stats, randn          # noqa: F401  (b: a fixture)
 
@@ -69,3 +70,17 @@ def test_loss_of_several_tiles_a_task(b, G, T, V, D, dtype):
         got = b.prsgd_vocab_loss(H, W, y, workspace=work)
         b.prsgd_work_status(work)
         assert torch.equal(got[0], first[0]) and torch.equal(got[1], first[1]), n
+
+
+@pytest.mark.parametrize("kind", ["dense", "odd"])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("G,T,V,D", shapes.FEW + shapes.NOT_FEW)
+def test_loss_of_few_tokens(b, G, T, V, D, dtype, kind):
+    H, W, y = case(420, G, T, V, D, dtype, kind)
+    if G > 1:
+        y[1] = -1
+        H[1] = float("nan")
+    work = b.vocab_loss_workspace(H, W).fill_(0xFF)
+    got = b.prsgd_vocab_loss(H, W, y, workspace=work)
+    b.prsgd_work_status(work)
+    check_loss(got, torch.where(ref.live_tokens(y, V)[..., None], H, 0), W, y)

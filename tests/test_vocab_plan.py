@@ -12,6 +12,7 @@ import vocab_shapes as shapes
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1807_06629_b200", "csrc")
 FIELDS = ["Tp", "tm", "tiles", "td", "kd", "tasks", "longest", "run", "runs", "piece", "pieces", "gp", "seqs", "parts", "kpart", "run_w", "h_first",
           "last_tiles", "last_blocks", "lag", "slots"]
+FORMS = ["few", "few_grad"]
 PROGRAM = r"""
 #include <cstdio>
 #include "vocab_plan.h"
@@ -20,7 +21,7 @@ int main() {
   long long G, T, V;
   while (std::scanf("%d %d %lld %lld %lld %d", &split, &grad, &G, &T, &V, &D) == 6) {
     const prsgd::VocabCuts c = prsgd::vocab_cuts(split, grad, G, T, V, D);
-    std::printf(""" + '"' + "%lld " * len(FIELDS) + r"\n" + '"' + "".join(", (long long)c." + f for f in FIELDS) + r""");
+    std::printf(""" + '"' + "%lld " * len(FIELDS + FORMS) + r"\n" + '"' + "".join(", (long long)c." + f for f in FIELDS) + r""", (long long)prsgd::vocab_few(split, G, T, V, D), (long long)prsgd::vocab_few_grad(T, D));
   }
 }
 """
@@ -36,7 +37,7 @@ def plans(tmp_path_factory):
     def run(calls):
         text = "\n".join(" ".join(str(int(x)) for x in c) for c in calls)
         out = subprocess.run([str(exe)], input=text, capture_output=True, text=True, check=True).stdout.splitlines()
-        return [dict(zip(FIELDS, map(int, line.split()))) for line in out]
+        return [dict(zip(FIELDS + FORMS, map(int, line.split()))) for line in out]
     return run
 
 
@@ -81,3 +82,14 @@ def test_sizes_reach_their_branches(plans):
     for shape in shapes.RUNS_OF_LOSS:
         for c in plans([(s, 0, *shape) for s in both]):
             assert c["run"] > 1 and c["tiles"] % c["run"] != 0 and c["kd"] > 8, (shape, c)
+
+
+def test_forms_of_few_tokens(plans):
+    for shapes_, want in ((shapes.FEW, 1), (shapes.NOT_FEW, 0)):
+        assert [c["few"] for c in plans([(0, 0, *s) for s in shapes_])] == [want] * len(shapes_)
+        assert all(c["few"] for c in plans([(1, 0, *s) for s in shapes_]))
+    # fp32: up to eight tokens, up to the columns that the contract names
+    for T, D, want in ((2, 12288, 1), (2, 12289, 0), (1, 24576, 1), (1, 24577, 0), (3, 6144, 1), (8, 6144, 1), (8, 6145, 0), (9, 64, 0)):
+        assert plans([(1, 0, 1, T, 1000, D)])[0]["few"] == want, (T, D)
+    for T, D, want in ((1, 2048, 1), (2, 2048, 1), (2, 2049, 0), (3, 8, 0)):
+        assert plans([(s, 1, 1, T, 1000, D) for s in (0, 1)])[0]["few_grad"] == want, (T, D)

@@ -9,3 +9,5 @@ PIECES = [(3, 2100, 17000, 300), (2, 1500, 50000, 520)]
 LONG = [(2, 8300, 9000, 600), (1, 70, 5000, 8264)]
 # loss: several tiles a task, each in several sums
 RUNS_OF_LOSS = [(2, 2100, 20000, 1000), (1, 3000, 60000, 1100)]
+# loss of one or two tokens a group: just below and above what the form of few tokens takes of 16-bit types
+FEW, NOT_FEW = [(1, 1, 1 << 17, 72), (4, 2, 1 << 14, 256)], [(1, 1, (1 << 17) + 1, 72), (4, 2, 100000, 256), (64, 1, 5000, 300)]
