@@ -617,7 +617,8 @@ int prsgd_dropout_keep(uint64_t seed, int64_t group, int64_t row, int64_t col, i
  * weights; both of one type.  A token whose label is padding has loss 0 and stats 0 whatever its row of H holds.  loss: [groups][tokens],
  * stats: [groups][tokens][2], fp32, dense; they share no memory with each other or with an input.  Products of 16-bit types are summed in
  * fp32; fp32 operands are taken as pairs of fp16 values (22 bits and nothing below 2^-39 of the largest of their row, each row of H and W
- * scaled by a power of two of its own), three products each.  Up to eight tokens a group of fp32 are summed in fp32 as they are.
+ * scaled by a power of two of its own), three products each.  Few tokens a group of fp32 are summed in fp32 as they are: one of up to 24576
+ * columns, two of up to 12288, three to eight of up to 6144.
  * The workspace depends on whether W's rows begin on 16-byte boundaries (address and both strides multiples of 16 bytes: w_aligned
  * 1; else, or for fp32, it holds a copy of W). */
 int prsgd_vocab_loss_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes);
@@ -628,15 +629,16 @@ int prsgd_vocab_loss(const void* d_H, int64_t h_row_stride, int64_t h_group_stri
 
 /* Gradient of sum dloss_t loss_t + sum dlse_t lse_t (lse the sum of the stats) with respect to H and W:
  *   G_tv = (dloss_t + dlse_t) e^(z_tv - lse_t) - dloss_t [v = y_t],   dH = G W,   dW = G^T H (or, accumulate, added to what dW holds).
- * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is held with one rounding of the operands' type
- * (fp32: as pairs, scaled by tokens, beside operands scaled by columns, H's after a token's dloss and dlse; none for one or two tokens a group), a piece of the vocabulary at a time.
- * fp16 holds entries of G down to 2^-15 |d_t| with all its bits and nothing below 2^-26 |d_t|, |d_t| = |dloss_t| + |dlse_t|, whatever the group's largest is
- * (a token whose |d_t| is more than 2^12 smaller than that is held by its own size, and the copy of its row of H that dW reads is rounded to 2^-36 of that largest).
- * Logits, dH and dW of 16-bit types are summed by the tensor cores, which cut off up to 2^-23 of a running sum every 16 products: sums of 8192 products or fewer
- * (dH: 16384), longer ones in fp32 from sums of 4096.  dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens
- * whose label is padding take no part: their rows of dH are zeros, whatever their H, stats, dloss and dlse hold.  The rows of dH and of dW may
- * not overlap (W shared by all groups has one gradient: call with groups = 1 and the groups' tokens behind one another);
- * neither may share memory with another array of the call. */
+ * stats as prsgd_vocab_loss wrote them; dloss, dlse: fp32 [groups][tokens], NULL = zeros.  G is formed a piece of the vocabulary at a time and
+ * held with one rounding of the operands' type (not rounded for one or two tokens a group of up to 2048 columns).
+ * fp32: as pairs, scaled by tokens, beside operands scaled by columns, H's after a token's dloss and dlse.  fp16: with |d_t| = |dloss_t| + |dlse_t|, entries down to
+ * 2^-15 |d_t| have all their bits, those below 2^-26 |d_t| none, whatever the group's largest is (of a token whose |d_t| is more than 2^12 smaller than that, the
+ * copy of its row of H that dW reads is rounded to 2^-36 of that largest).
+ * Logits, dH and dW of 16-bit types are summed by the tensor cores, which cut off up to 2^-23 of a running sum every 16 products: sums of 8192 products or
+ * fewer (dH: 16384) at once, longer ones in fp32 from sums of 4096.
+ * dH has H's type, dW W's type or fp32; either may be NULL (not wanted).  Tokens whose label is padding take no part: their rows of dH are zeros, whatever
+ * their H, stats, dloss and dlse hold.  The rows of dH and of dW may not overlap (W shared by all groups has one gradient: call with groups = 1 and
+ * the groups' tokens behind one another); neither may share memory with another array of the call. */
 int prsgd_vocab_loss_grad_workspace_bytes(int32_t type, int64_t groups, int64_t tokens, int64_t vocab, int32_t dim, int32_t w_aligned, size_t* bytes);
 int prsgd_vocab_loss_grad(const void* d_H, int64_t h_row_stride, int64_t h_group_stride,
                           const void* d_W, int64_t w_row_stride, int64_t w_group_stride, int32_t type, const int32_t* d_labels,

@@ -9,9 +9,10 @@
 //    from HBM once, H' stays in L2.
 //  * Gradient: the vocabulary is taken in pieces.  Tiles of G of a piece (logits again, then the softmax's gradient in the epilogue, held in
 //    16 bits) and tiles of dW = G^T H' and dH += G W that use it are tasks of one list: G of piece k, then the uses of piece k - lag, so
-//    that what a task waits for was claimed a phase earlier.  Pieces are sized so that a few of them stay in L2 (126 MB).  G^T, W^T and H'^T are read
-//    MN-major: nothing is transposed in memory.  dH of several pieces adds up in fp32 in the workspace, each tile in the order of
-//    the pieces; a long contraction is cut into parts with sums of their own, added up by a last launch.
+//    that what a task waits for was claimed a phase earlier.  A piece of G takes about 64 MB, the fastest between pieces that stay in L2
+//    (126 MB) and few additions to dH (vocab_plan.h).  G^T, W^T and H'^T are read MN-major: nothing is transposed in memory.  dH of several
+//    pieces adds up in fp32 in the workspace, each tile in the order of the pieces; a long contraction is cut into parts with sums of their
+//    own, added up by a last launch.
 // Tasks are claimed in order from a device counter, and a claimed task waits only for tasks claimed earlier, so the CTAs that run
 // always make progress, whatever share of the grid is resident.
 #pragma once
