@@ -107,3 +107,21 @@ def test_fp16_gradients_beyond_a_floats_exponents(b):
     want = b.prsgd_vocab_loss_grad(H, W, torch.where(dloss == 1, y, -1), stats, dloss=dloss)[0]
     got = b.prsgd_vocab_loss_grad(H, W, y, stats, dloss=dloss)[0]
     check(got[:, 20:], want[:, 20:].double(), 2.0 ** -9 * want[:, 20:].double().abs() + 2.0 ** -12)
+
+
+# ---- statistics -----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("D", [2048, 4000])
+def test_statistics_are_good_to_fp32(b, D, dtype):
+    """Largest logit and logarithm of the denominator of normal data: rms and mean of the signed error relative to their size.  Logits are sums of 512
+    products, each cut off 32 times by 2^-24 of what it holds, half its end on average: 9.5e-7; one sum of D = 2048 is off by 1.9e-6, of 4000 by
+    twice that."""
+    T, V = 512, 3000
+    H, W = randn(500, 1, T, D, dtype=dtype), (randn(501, 1, V, D) * (1.5 / math.sqrt(D))).to(dtype)
+    y = torch.randint(0, V, (1, T), generator=gen(502), device="cuda:0").to(torch.int32)
+    loss, stats = b.prsgd_vocab_loss(H, W, y)
+    want, exact = ref.vocab_loss(H, W, y)
+    for got, true in ((stats[..., 0], exact[..., 0]), (stats.double().sum(-1), exact.sum(-1)), (loss, want)):
+        error = got.double() - true
+        size = true.square().mean().sqrt()
+        assert error.square().mean().sqrt() <= 1e-6 * size and error.mean().abs() <= 1e-6 * size, (error.square().mean().sqrt() / size, error.mean() / size)
