@@ -44,6 +44,7 @@ struct VocabPrep {
   unsigned int* most;                          // [2][groups][Dp] largest finite magnitudes (bits) of those columns: W, H
   int64_t Vp; int Dp;                          // V, D rounded up to 256
   int most_h, most_w, most_rows;               // blocks that look for them in H and W, rows of one
+  float* largest;            // [groups], fp16 gradients of many tokens: largest |dloss| + |dlse|; nullptr: each block of vocab_prep_kernel looks for it
   float4* rowp;              // [groups][Tp]: (max, log sum, dloss + dlse, dloss)
   int* rowy; int* index;     // [groups][Tp]: label; token
   int* live;                 // [groups]
@@ -244,8 +245,53 @@ __device__ __forceinline__ void vocab_split_row(const float* from, uint16_t* hi,
   }
 }
 
-// Blocks x < h_blocks of a group move its live rows together, the others copy W.  A block counts the live tokens before its own (and, of fp16,
-// looks for the group's largest gradient); the group's first block counts all, finds the scales, and zeroes the rows behind the last live one that a
+// All tokens of a group by THREADS threads: f(token, whether it is live, |dloss| + |dlse|), eight of a thread requested together.
+template <int THREADS, typename F>
+__device__ __forceinline__ void vocab_tokens(const VocabPrep& a, int64_t g, F&& f) {
+  constexpr int kAhead = 8;
+  const int32_t* labels = a.labels + g * a.T;
+  const float* const dloss = a.grad && a.dloss ? a.dloss + g * a.T : nullptr;
+  const float* const dlse = a.grad && a.dlse ? a.dlse + g * a.T : nullptr;
+  for (int64_t t0 = threadIdx.x; t0 < a.T; t0 += THREADS * kAhead) {
+    int y[kAhead];
+    float d[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      y[j] = t0 + j * THREADS < a.T ? labels[t0 + j * THREADS] : -1;
+      d[j] = 0.f;
+    }
+    if (dloss != nullptr) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) d[j] = t0 + j * THREADS < a.T ? fabsf(dloss[t0 + j * THREADS]) : 0.f;
+    }
+    if (dlse != nullptr) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) d[j] += t0 + j * THREADS < a.T ? fabsf(dlse[t0 + j * THREADS]) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) f(t0 + j * THREADS, y[j] >= 0 && y[j] < a.V, d[j]);
+  }
+}
+
+// Largest |dloss| + |dlse| of a group's live tokens, before vocab_prep_kernel: of many tokens each of its blocks would read them all (16384
+// tokens: 150 MB from L2 in all, 15 us).
+__global__ void __launch_bounds__(1024) vocab_largest_kernel(const VocabPrep a) {
+  __shared__ float sm[32];
+  op_pdl_wait();
+  op_pdl_trigger();
+  float most = 0.f;
+  vocab_tokens<1024>(a, blockIdx.x, [&](int64_t, bool on, float d) { most = fmaxf(most, on ? finite_abs(d) : 0.f); });
+  for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  most = sm[threadIdx.x];
+  for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if (threadIdx.x == 0) a.largest[blockIdx.x] = most;
+}
+
+// Blocks x < h_blocks of a group move its live rows together, the others copy W.  A block counts the live tokens before its own (and, of fp16 and
+// up to kLargestApart tokens, looks for the group's largest gradient); the group's first block counts all, finds the scales, and zeroes the rows behind the last live one that a
 // product may read.
 template <int TY>
 __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
@@ -282,19 +328,22 @@ __global__ void __launch_bounds__(256, 4) vocab_prep_kernel(const VocabPrep a) {
   const int32_t* labels = a.labels + g * a.T;
   const int64_t per = (a.T + a.h_blocks - 1) / a.h_blocks, begin = min(a.T, blockIdx.x * per), end = min(a.T, begin + per);
   auto is_live = [&](int y) { return y >= 0 && y < a.V; };
-  const bool whole = blockIdx.x == 0 || (LIFT && a.grad);  // (looks at all tokens)
+  const bool whole = blockIdx.x == 0 || (LIFT && a.grad && a.largest == nullptr);          // (looks at all tokens)
   int before = 0, all = 0;
   float most = 0.f;
-  for (int64_t t = threadIdx.x; t < (whole ? a.T : begin); t += 256) {
-    const int on = is_live(labels[t]) ? 1 : 0;
-    const float d = !whole || !a.grad ? 0.f : (a.dloss ? fabsf(a.dloss[g * a.T + t]) : 0.f) + (a.dlse ? fabsf(a.dlse[g * a.T + t]) : 0.f);
-    all += on;
-    before += t < begin ? on : 0;
-    most = fmaxf(most, on ? finite_abs(d) : 0.f);
+  if (!whole) {
+    for (int64_t t = threadIdx.x; t < begin; t += 256) before += is_live(labels[t]) ? 1 : 0;
+  } else {
+    vocab_tokens<256>(a, g, [&](int64_t t, bool on, float d) {
+      all += on ? 1 : 0;
+      before += on && t < begin ? 1 : 0;
+      most = fmaxf(most, on ? finite_abs(d) : 0.f);
+    });
   }
   before = vocab_block_sum(before, smi);
   if (blockIdx.x == 0) all = vocab_block_sum(all, smi);
   if (whole && a.grad) most = vocab_block_max(most, smf);
+  if (LIFT && a.grad && a.largest != nullptr) most = a.largest[g];
   const int e_group = most > 0.f ? vocab_exponent(most, 13) : 0;
   if (blockIdx.x == 0) {
     if (g == 0) {

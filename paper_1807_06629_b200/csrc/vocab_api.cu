@@ -56,6 +56,7 @@ VocabPlan vocab_plan(int type, int64_t groups, int64_t T, int64_t V, int D, bool
     for (int i = 0; i < planes; ++i) a.Hm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * a.Tp * a.pitch));
     c.rowg = a.rowg = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Tp));
   }
+  if (grad && type == PRSGD_TYPE_FP16 && T > kLargestApart) a.largest = reinterpret_cast<float*>(take(4 * (size_t)groups));
   if (p.split && grad) {
     for (int i = 0; i < planes; ++i) a.Wm[i] = reinterpret_cast<uint16_t*>(take(2 * (size_t)groups * V * a.pitch));
     c.dhf = a.dhf = reinterpret_cast<float2*>(take(8 * (size_t)groups * a.Dp));
@@ -210,6 +211,7 @@ int vocab_run(VocabPlan& p, cudaStream_t st) {
     a.most_w = a.Wm[0] ? (int)up(a.V, a.most_rows) : 0;
     launch_pdl(vocab_columns_kernel, dim3((unsigned)(a.most_h + a.most_w), (unsigned)strips, (unsigned)G), dim3(256), 0, st, a);
   }
+  if (a.largest) launch_pdl(vocab_largest_kernel, dim3((unsigned)G), dim3(1024), 0, st, a);
   with_type(a.h_type, [&](auto ty) { launch_pdl(vocab_prep_kernel<decltype(ty)::value>, dim3((unsigned)(a.h_blocks + a.w_blocks), (unsigned)G), dim3(256), 0, st, a); });
   const dim3 grid(2 * (unsigned)std::min<int64_t>(sms / 2, p.tasks));
   auto go = [&](auto kernel) { launch_pdl_cluster(kernel, grid, dim3(kVtThreads), vt_smem(p.grad), st, 2, maps, c); };

@@ -11,6 +11,8 @@ constexpr int64_t kVtLongest = 8192;           // products that one running sum 
 inline int64_t up(int64_t x, int64_t by) { return (x + by - 1) / by; }
 inline int64_t up_to(int64_t x, int64_t by) { return up(x, by) * by; }
 
+constexpr int64_t kLargestApart = 4096;        // fp16 gradients of more tokens: their largest |dloss| + |dlse| by a launch of its own (4 x 2100 x 512 x 128 40 us with it, 38 without; 4 x 8192 94 and 96; 16384 x 1000 x 256 130 and 139)
+
 struct VocabCuts {
   int64_t Tp;                                  // rows of the copy of H
   int64_t tm;                                  // tiles along the tokens

@@ -61,7 +61,7 @@ def test_gradient_of_many_columns(b):
 
 
 # ---- fp16: gradients of different sizes in one group ----------------------------------------------------------
-@pytest.mark.parametrize("G,T,V,D", [(1, 60, 20000, 64), (2, 300, 2500, 100), (3, 70, 400, 1100), (1, 8300, 600, 40)])
+@pytest.mark.parametrize("G,T,V,D", [(1, 60, 20000, 64), (2, 300, 2500, 100), (3, 70, 400, 1100), (1, 8300, 600, 40), (3, 4100, 300, 24)])
 def test_fp16_gradients_of_any_size(b, G, T, V, D):
     """fp16: tokens whose dloss and dlse are up to 2^30 smaller than the group's largest (2^13), beside some without any: a token's row of dH
     is as good, relative to its own, as that of the largest.  A last column of ones in W makes that column of dH dlse_t: what G's smallest entries lose shows there.
