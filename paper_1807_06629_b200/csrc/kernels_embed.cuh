@@ -278,7 +278,7 @@ __device__ __forceinline__ void embed_write(const EmbedGradArgs& a, typename Ele
 }
 
 // One unit's sums for one thread's columns.  Rows of dout, and what the sums are added to, are requested two tokens ahead, with four blocks
-// an SM (4 x 8192 tokens, 2048 columns, whole call: 56 us; four ahead and two blocks 58, eight ahead 66).
+// an SM (4 x 8192 tokens with an id, 2048 columns, whole call: 92 us; four ahead and two blocks 95, eight ahead 112).
 template <int TY, int OTY, bool VEC, bool OVEC>
 __device__ __forceinline__ void embed_unit_sum(const EmbedGradArgs& a, int64_t g, int u, int c, int n, int live, int begin, int end) {
   using T = typename ElemOf<TY>::type;
