@@ -109,6 +109,38 @@ def test_fp16_gradients_beyond_a_floats_exponents(b):
     check(got[:, 20:], want[:, 20:].double(), 2.0 ** -9 * want[:, 20:].double().abs() + 2.0 ** -12)
 
 
+@pytest.mark.parametrize("T", [70, 4200])
+def test_fp16_gradients_captured(b, T):
+    """Replays with other gradients and labels, whose sizes move what is held by its own size, give what direct calls do; so do two streams at once."""
+    G, V, D = 2, 300, 24
+    H, W, y = case(150, G, T, V, D, F16)
+    stats = ref.vocab_loss(H, W, torch.where(y < 0, 0, y.clamp(max=V - 1)))[1].float()
+    size = lambda n: 2.0 ** -(torch.arange(T, device="cuda:0") * (n + 1) % 40).float()          # noqa: E731
+    dloss, labels = randn(153, G, T), y.clone()
+    dH, dW, work = torch.empty_like(H), torch.empty_like(W), b.vocab_loss_grad_workspace(H, W)
+    call = lambda: b.prsgd_vocab_loss_grad(H, W, labels, stats, dloss=dloss, dH=dH, dW=dW, workspace=work)          # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for n in range(3):
+        dloss.copy_(randn(160 + n, G, T) * size(n))
+        labels.copy_(y.roll(n, 1))
+        dH.fill_(float("nan")), dW.fill_(float("nan"))
+        graph.replay()
+        want = b.prsgd_vocab_loss_grad(H, W, labels, stats, dloss=dloss)
+        assert torch.equal(dH, want[0]) and torch.equal(dW, want[1]), n
+    torch.cuda.synchronize()
+    got = []
+    for s in (torch.cuda.Stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(s):
+            got.append(b.prsgd_vocab_loss_grad(H, W, labels, stats, dloss=dloss))
+    torch.cuda.synchronize()
+    for one in got:
+        assert torch.equal(one[0], want[0]) and torch.equal(one[1], want[1])
+
+
 # ---- statistics -----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("D", [2048, 4000])
