@@ -34,6 +34,10 @@ constexpr size_t vt_smem(bool grad) { return 1024 + (size_t)vt_stages(grad) * kV
 // exact to fp32 is summed in TMEM over this many blocks of 64 only, and those sums are added in registers, where they are rounded (stats at
 // 16384 x 131072 x 2048: off by 1.9e-6 with one sum, by 4.3e-7 with sums of 512 products, for 2 to 5 % of the time).
 constexpr int kVtPromote = 8;
+// Pairs: what a logit is off by, its softmax is off by relatively, and a learnt token's gradient 1 - p by more: with sums of 512 products dH and dW of few tokens were off
+// by up to 2.5e-6 (plain fp32 3e-7), logits by 5.5e-7 of theirs.  One block a sum for the gradient's logits (2.5e-7 of few tokens, logits 1.2e-7), else four:
+// 1 x 2048 x 32000 x 1024 gradient 1024 -> 1063 us (everything in sums of one block 1111), loss the same.
+constexpr int kVtPromotePairs = 4, kVtPromoteGrad = 1;
 // Gradients of 16-bit types are rounded by more, each term of a sum by 2^-9 or 2^-12 of its own: they are one sum while it has at most kVtLongest
 // products (cut off by about 2^-15 of it), and sums of 64 blocks beyond (131072 tokens of one sign, fp16: dW was off by 4.6e-4).
 constexpr int kVtPromoteLong = 64;
@@ -74,12 +78,13 @@ struct VocabChain {
 // contraction; seq = g * pieces + p and the place of that piece's G; live tokens of the group.
 struct VTask { int kind, g, ti, tj, n, p, seq, slot, live, k0, kb, pad; };
 
-// Sums of a tile: one, or (PROMOTE blocks each) one of the small products of pairs and as many as there are.
-template <bool SPLIT, int PROMOTE>
-__device__ __forceinline__ int vt_sums(int kb) {
-  if constexpr (PROMOTE == 0) return 1;
-  else return (SPLIT ? 1 : 0) + (kb + PROMOTE - 1) / PROMOTE;
+// Blocks of a sum of a task's tiles (0: all), and sums of a tile: one, or one of the small products of pairs and as many as there are.
+template <bool GRAD, bool SPLIT, bool LONG>
+__device__ __forceinline__ constexpr int vt_step(int kind) {
+  return SPLIT ? (kind == VT_G ? kVtPromoteGrad : kVtPromotePairs) : !GRAD ? kVtPromote : LONG ? kVtPromoteLong : 0;
 }
+template <bool SPLIT>
+__device__ __forceinline__ int vt_sums(int kb, int step) { return step == 0 ? 1 : (SPLIT ? 1 : 0) + (kb + step - 1) / step; }
 
 __device__ __forceinline__ int vt_tiles(int n) { return (n + 255) >> 8; }
 __device__ __forceinline__ int vt_piece_tiles(const VocabChain& a, int p) { return p + 1 == a.pieces ? a.last_tiles : a.piece >> 8; }
@@ -340,8 +345,8 @@ __device__ __forceinline__ void vt_undo32(float (&v)[32], float2 row, const floa
 template <bool GRAD, bool SPLIT, bool LONG = false>
 __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ VocabChain a) {
   constexpr int kStages = vt_stages(GRAD), kPasses = SPLIT ? 3 : 1;
-  constexpr int PROMOTE = SPLIT || !GRAD ? kVtPromote : LONG ? kVtPromoteLong : 0;      // blocks of a sum, 0: all
-  constexpr int kGroups = PROMOTE != 0 ? 1 : 2, kWarpCols = PROMOTE != 0 ? 64 : 128;
+  constexpr bool PROMOTE = SPLIT || !GRAD || LONG;
+  constexpr int kGroups = PROMOTE ? 1 : 2, kWarpCols = PROMOTE ? 64 : 128;
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kVtRing + 1];
@@ -461,6 +466,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         const VTask k = next_task(n);
         if (k.kind < 0) break;
         if (issue) free_task(n);
+        const int step = vt_step<GRAD, SPLIT, LONG>(k.kind);
         const int kb = k.kb, blocks = kb * kPasses, tiles = blocks > 0 ? (k.kind == VT_STATS || k.kind == VT_DW ? k.n : 1) : 0;
         const bool a_mn = GRAD && k.kind == VT_DW, b_mn = GRAD && k.kind >= VT_DH;
         const uint32_t idesc = ptx::idesc_f16(256, 256, a_mn, b_mn) | format;
@@ -475,7 +481,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
           for (int q = 0; q < blocks; ++q) {
             const bool first = q == next;
             if (first) {
-              next = PROMOTE == 0 ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + PROMOTE);
+              next = !PROMOTE ? blocks : SPLIT && q < 2 * kb ? 2 * kb : min(blocks, q + step);
               acc = sums & 1u;
               if (sums >= 2 && !ptx::warp_wait(tempty((int)acc), ((sums >> 1) - 1) & 1, ab, status, VT_ERR_ACC_FREE)) { ok = false; break; }
               ptx::tc_fence_after();
@@ -541,7 +547,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
     }
   } else {                                               // ---- epilogue ---------------------------------------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    const int quarter = warp & 3, group = PROMOTE != 0 ? 0 : (warp - 4) >> 3, share = ((warp - 4) >> 2) & (kVtShares / kGroups - 1);
+    const int quarter = warp & 3, group = PROMOTE ? 0 : (warp - 4) >> 3, share = ((warp - 4) >> 2) & (kVtShares / kGroups - 1);
     const uint32_t box = stage0 + kStages * kVtStageBytes + (uint32_t)(warp - 4) * kVtWarpBytes;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(share * kWarpCols);
     uint32_t sums = 0;
@@ -551,7 +557,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
       if (lane == 0) free_task(n);
       const VocabScale* sc = a.scale + k.g;
       const int r0 = k.ti * 256 + (int)rank * 128 + quarter * 32;
-      const int kb = k.kb, parts = vt_sums<SPLIT, PROMOTE>(kb);
+      const int kb = k.kb, parts = vt_sums<SPLIT>(kb, vt_step<GRAD, SPLIT, LONG>(k.kind));
       // Waits for the warp's 64 columns of a tile's sum; several sums (PROMOTE) are added in registers and the total goes back to TMEM, over
       // the last of them, so that what follows needs registers for 32 columns only.
       uint32_t acc = 0;
@@ -561,7 +567,7 @@ __global__ void __launch_bounds__(kVtThreads, 1) vocab_chain_kernel(const __grid
         if (lane == 0) ptx::mbar_arrive_cluster(ptx::cluster_map(tempty((int)acc), 0));
       };
       auto gather = [&]() -> bool {
-        if (PROMOTE == 0 || parts == 1) {
+        if (!PROMOTE || parts == 1) {
           acc = sums & 1u;                               // (one group: the sum is its own)
           if (!ptx::warp_wait(tfull((int)acc), (sums >> 1) & 1u, ab, status, VT_ERR_ACC)) return false;
           ++sums;

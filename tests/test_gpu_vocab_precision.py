@@ -141,6 +141,27 @@ def test_fp16_gradients_captured(b, T):
         assert torch.equal(one[0], want[0]) and torch.equal(one[1], want[1])
 
 
+# ---- fp32: the gradient's logits --------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,D", [(512, 2048), (40, 1000)])
+def test_gradient_logits_are_good_to_fp32(b, T, D):
+    """A column of ones in W makes that column of dH sum_v p_tv (dlse = 1, no dloss): off from 1 by the relative error of the softmax, which is the absolute one of the
+    logits that make it up (here 10 to 20 of learnt tokens).  A logit is a sum of sums of 64 products, each cut off four times, when it holds 1/4, 2/4, 3/4 and 4/4 of its
+    end, each time by 2^-22 of that at most (test_gpu_language.py) and by half as much on average: 2.5 x 2^-23 of it; dH sums of 256 products: 2^-21; pairs, exponential: 2^-21.
+    Additions in fp32 have no sign.  (A logit as sums of 512 products: 32 times, 16.5 x 2^-23.)"""
+    V = 1000
+    H, W, y = case(170, 1, T, V, D, F32, padded=False, spread=1.5)
+    H += 7.0 * W[0][y[0].long()]
+    W[..., -1] = 1.0
+    H[..., -1] = 0.0
+    exact = ref.vocab_loss(H, W, y)[1]
+    stats = exact.float()
+    dH, _ = b.prsgd_vocab_loss_grad(H, W, y, stats, dlse=torch.ones(1, T, device="cuda:0"))
+    want = (exact.sum(-1) - stats.double().sum(-1)).exp()    # (the stats' own rounding)
+    off = ((dH[0, :, -1].double() - want[0])).mean().abs().item()
+    z = exact[..., 0].abs().mean().item()
+    assert z > 8 and off <= 2.5 * 2.0 ** -23 * z + 2.0 ** -20, (off, z)
+
+
 # ---- statistics -----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("D", [2048, 4000])
